@@ -69,6 +69,7 @@ typedef enum {
   EPIKV_DEV_KEPT = 4,       /* kept list not strictly increasing / out of range */
   EPIKV_DEV_BUDGET = 5,     /* budget K < 1 or > max_cache_tokens */
   EPIKV_DEV_TIMEOUT = 6,    /* a bounded wait inside a kernel gave up */
+  EPIKV_DEV_POSITION = 7,   /* a token's position outside the rotation table */
 } epikv_device_error;
 
 /* Score kinds (bit mask in epikv_config.score_kinds, one value as policy).
@@ -328,6 +329,165 @@ epikv_status epikv_lagkv_score_noalloc(const epikv_kv_view* kv, int32_t seq, int
                                        int32_t num_layers, int32_t num_kv_heads, int32_t head_dim,
                                        int32_t lag, float lag_eps, int32_t window, float* d_scores,
                                        cudaStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Beside eviction: putting new tokens into the cache and attending over it.
+ *
+ * After an eviction a token's slot is no longer its position: new rows go to
+ * the slots behind the kept ones while the rotation goes on by position, and
+ * attention runs over slots.  These calls take both, from device arrays that
+ * the caller holds anyway (the lengths that epikv_step returns, the positions
+ * that it counts).  They have a context of their own (epikv_attn_ctx), which
+ * follows the conventions above: the caller's workspace, no allocation, no
+ * synchronisation, EPIKV_EINVAL before anything is enqueued, a sticky device
+ * error word.
+ * ------------------------------------------------------------------------ */
+
+/* What a cache row holds.
+ *   BF16   H*d bf16 values, the rows of every call above
+ *   E2M1   4 bits a value: for each head d/2 bytes of E2M1 codes (channel 2i in
+ *          the low half of byte i), then for each head d/16 bytes of E4M3
+ *          scales, one for every 16 channels; a channel is code * scale * the
+ *          head's kv_scale.  4.5 bits a value.  The row is padded to
+ *          epikv_cache_row's size.
+ * Strides of a view count 2-byte units for both, so a 4-bit cache is described
+ * by the same epikv_kv_view, and epikv_select, epikv_compact and epikv_step
+ * (with the band kinds, which do not read K and V) move its rows as they are:
+ * their context is configured with the num_kv_heads and head_dim that
+ * epikv_cache_row returns. */
+enum { EPIKV_CACHE_BF16 = 0, EPIKV_CACHE_E2M1 = 1 };
+
+/* Element types of epikv_rows. */
+enum { EPIKV_TYPE_BF16 = 0, EPIKV_TYPE_F16 = 1, EPIKV_TYPE_F32 = 2 };
+
+/* Which channels of a head form the rotated pairs: i and i + dim/2, or 2i and
+ * 2i + 1.  Channels from dim on pass unchanged. */
+enum { EPIKV_ROPE_HALF = 0, EPIKV_ROPE_INTERLEAVED = 1 };
+
+/* How the frequencies theta^(-2i/dim) are changed for long contexts.
+ *   LINEAR   divided by factor
+ *   NTK      theta multiplied by factor^(dim/(dim-2))
+ *   BYPARTS  freq * ((1-g)/factor + g), g = clamp((rot - low) / (high - low)),
+ *            rot = original * freq / 2pi: the turns that the frequency makes
+ *            over the original context */
+enum { EPIKV_ROPE_PLAIN = 0, EPIKV_ROPE_LINEAR = 1, EPIKV_ROPE_NTK = 2, EPIKV_ROPE_BYPARTS = 3 };
+
+typedef struct {
+  int32_t dim;              /* rotated channels of a head: even, >= 2 */
+  float theta;              /* base of the frequencies, > 1 */
+  int32_t scaling;          /* EPIKV_ROPE_PLAIN .. BYPARTS */
+  float factor;             /* >= 1 (read unless PLAIN) */
+  float low, high;          /* BYPARTS: 0 <= low < high */
+  int32_t original;         /* BYPARTS: tokens of the original context, >= 1 */
+  float magnitude;          /* cos and sin are multiplied by it (1: a pure rotation) */
+} epikv_rope_config;
+
+/* A table made once by epikv_rope_table (or by the caller): device float
+ * [n_pos][dim/2][2], cos and sin of every position and frequency. */
+typedef struct {
+  const float* table;       /* 16-byte aligned */
+  int32_t n_pos;
+  int32_t dim;
+  int32_t layout;           /* EPIKV_ROPE_HALF or INTERLEAVED */
+} epikv_rope_view;
+
+/* Heads of tokens, channels contiguous: element (token, head, channel) at
+ * token*stride_token + head*stride_head + channel (strides in elements).  The
+ * pointer and the strides are multiples of 16 bytes. */
+typedef struct {
+  void* ptr;
+  int64_t stride_token;
+  int64_t stride_head;
+  int32_t type;             /* EPIKV_TYPE_* */
+} epikv_rows;
+
+typedef struct {
+  int32_t max_seqs;         /* sequence ids are 0..max_seqs-1 */
+  int32_t max_cache_tokens; /* cache slots per sequence */
+  int32_t max_new_tokens;   /* new tokens per sequence and call, max */
+  int32_t num_layers;
+  int32_t num_heads;        /* query heads: a multiple of num_kv_heads; head h reads KV head
+                             * h / (num_heads / num_kv_heads) */
+  int32_t num_kv_heads;     /* 1..32 */
+  int32_t head_dim;         /* 64, 128 or 256 */
+  int32_t cache_format;     /* EPIKV_CACHE_* */
+  float softmax_scale;      /* 0: 1/sqrt(head_dim) */
+  const float* kv_scale;    /* E2M1: device float [2][num_layers][num_kv_heads], a positive scale of each
+                             * head's keys, then values, which the E4M3 scales multiply (E4M3 reaches from
+                             * 2^-9 to 448: heads whose values lie far from 1 need one); NULL: 1 */
+} epikv_attn_config;
+
+typedef struct epikv_attn_ctx epikv_attn_ctx;
+
+/* The row of one token, layer and of K or V as the eviction calls see it:
+ * *heads * *dim 2-byte units (for E2M1 the packed row, padded until it is such
+ * a product).  EPIKV_EINVAL if no such row exists (over 2,048 units). */
+epikv_status epikv_cache_row(int32_t num_kv_heads, int32_t head_dim, int32_t cache_format, int32_t* heads,
+                             int32_t* dim);
+
+/* Bytes of device workspace for cfg (0 if cfg is invalid). */
+size_t epikv_attn_workspace_bytes(const epikv_attn_config* cfg);
+
+/* Create a context over a caller-allocated workspace (256-byte aligned). */
+epikv_status epikv_attn_init(epikv_attn_ctx** out, const epikv_attn_config* cfg, void* d_workspace,
+                             size_t workspace_bytes, cudaStream_t stream);
+
+/* Fill d_table, float [n_pos][dim/2][2] (angles in 64 bits, rounded once). */
+epikv_status epikv_rope_table(const epikv_rope_config* cfg, int32_t n_pos, float* d_table, cudaStream_t stream);
+
+/* Rotate n_tokens x n_heads heads of ctx's head_dim by their positions
+ * d_pos [n_tokens] (32-bit arithmetic, rounded once).  inverse = 1 turns the
+ * other way, which is the rotation's gradient.  out may be x.  A token whose
+ * position is outside the table is skipped (EPIKV_DEV_POSITION). */
+epikv_status epikv_rope(epikv_attn_ctx* ctx, int32_t n_tokens, int32_t n_heads, const epikv_rows* x,
+                        const epikv_rows* out, const int32_t* d_pos, const epikv_rope_view* rope, int32_t inverse,
+                        cudaStream_t stream);
+
+/* Append the new tokens of a batch to one layer's cache.
+ *   d_seq_ids, d_cu_new, max_new   as in epikv_score_update
+ *   d_len [n_seq] (every len_stride-th int32 of it): the slots that each entry
+ *         holds before the call; token i of entry b goes to slot d_len[b] + i.
+ *         A per-layer length array is read with its layer stride.
+ *   d_pos [n_seq]  position of each entry's first new token; may be NULL if
+ *                  rope is NULL (no rotation)
+ *   q, q_out       bf16 queries [total_new][num_heads][d] and where they go,
+ *                  rotated (may be the same rows); both NULL: no queries
+ *   k, v           bf16 [total_new][num_kv_heads][d]
+ * Keys are rotated in 32 bits and rounded to bf16; a 4-bit cache then takes
+ * them to 4 bits: for 16 channels, scale = E4M3(min(448, max|x| / 6)), code =
+ * E2M1(x / scale), to nearest even, saturating (NaN: the 16 channels read as
+ * NaN).  Nothing but the new tokens' rows is written. */
+epikv_status epikv_append(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* d_seq_ids,
+                          const int32_t* d_cu_new, int32_t max_new, const int32_t* d_len, int32_t len_stride,
+                          const int32_t* d_pos, const epikv_rows* q, const epikv_rows* q_out, const epikv_rows* k,
+                          const epikv_rows* v, const epikv_rope_view* rope, const epikv_kv_view* kv,
+                          cudaStream_t stream);
+
+/* Attention of the batch's queries over one layer's cache: bf16 queries and
+ * outputs [total_new][num_heads][d], statistics in 32 bits.
+ *   d_len     as in epikv_append: the slots held before the new tokens
+ *   causal    1: the new tokens' rows are in the cache, query i of entry b
+ *             reads slots 0 .. d_len[b] + i.  0: every query reads the d_len[b]
+ *             slots (a shared prefix; join with d_lse)
+ *   d_lse     float [total_new][num_heads] or NULL: log of the sum of exponentials
+ * A row that sees no slot gives zeros and -infinity.  Slots that a row does not
+ * see do not reach it, whatever they hold. */
+epikv_status epikv_attention(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* d_seq_ids,
+                             const int32_t* d_cu_new, int32_t max_new, const int32_t* d_len, int32_t len_stride,
+                             int32_t causal, const epikv_rows* q, const epikv_rows* out, float* d_lse,
+                             const epikv_kv_view* kv, cudaStream_t stream);
+
+/* Read n_rows rows of one layer back as bf16 [n_rows][num_kv_heads][d]: slot
+ * d_slots[i] of sequence d_seqs[i].  k or v may be NULL.  Rows outside the view
+ * are skipped (EPIKV_DEV_SLOT). */
+epikv_status epikv_cache_read(epikv_attn_ctx* ctx, int32_t layer, int32_t n_rows, const int32_t* d_seqs,
+                              const int32_t* d_slots, const epikv_rows* k, const epikv_rows* v,
+                              const epikv_kv_view* kv, cudaStream_t stream);
+
+/* As epikv_get_error. */
+epikv_status epikv_attn_get_error(epikv_attn_ctx* ctx, int32_t* code);
+
+void epikv_attn_destroy(epikv_attn_ctx* ctx);
 
 void epikv_destroy(epikv_ctx* ctx);
 const char* epikv_status_string(epikv_status s);

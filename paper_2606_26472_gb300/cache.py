@@ -19,10 +19,16 @@ class KVCache:
                  and block_table [L][S][max_blocks_per_seq] gives every
                  (layer, sequence) its own blocks, so a layer that keeps
                  fewer tokens (per-layer budgets) holds fewer blocks.
+    cache_format E2M1: rows are 4-bit, stored as bf16 units; H and d are then
+                 the row's shape as the eviction calls see it (num_kv_heads and
+                 head_dim of their context), heads and head_dim the model's.
     """
 
     def __init__(self, layout, L, H, d, *, max_seqs, max_tokens, block_size=16, num_blocks=None,
-                 block_table=None, layer_tables=False, device="cuda"):
+                 block_table=None, layer_tables=False, cache_format=E.EPIKV_CACHE_BF16, device="cuda"):
+        self.heads, self.head_dim, self.cache_format = H, d, cache_format
+        if cache_format != E.EPIKV_CACHE_BF16:
+            H, d = E.epikv_cache_row(H, d, cache_format)
         self.layout, self.L, self.H, self.d = layout, L, H, d
         self.S, self.T = max_seqs, max_tokens
         self.block_size = block_size

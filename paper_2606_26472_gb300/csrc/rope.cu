@@ -1,0 +1,440 @@
+// Rotary positions, appending to the cache with the rotation on the way, and
+// reading cache rows back.
+//
+// The rotation turns each pair (a, b) of a head's channels by its position's
+// angle for that pair's frequency: a' = a cos - b sin, b' = b cos + a sin.  The
+// cosines come from a table (made once, in 64 bits: an angle formed in 32 bits
+// is off by 0.03 radians at position 10^6), the products and sums are rounded
+// one by one in 32 bits, so a 4-bit code never depends on how a compiler
+// contracts them.
+//
+// A thread takes a unit of 2 V channels that the rotation keeps among
+// themselves (V and V channels half a rotated range apart, or 2 V neighbours),
+// loads the unit's V cosines and sines once and then turns that unit of several
+// heads, so in place works and the table is read once per token and not per
+// head.  V = 8 (16-byte accesses) where the rotated range allows it, else 1.
+#include "attn.cuh"
+
+namespace epikv {
+namespace {
+
+constexpr int kBlock = 128;
+constexpr int kBatch = 4;  // heads that a thread has in flight
+
+template <typename T, int V>
+__device__ __forceinline__ void load_v(const T* p, float* f) {
+  if constexpr (V == 1) {
+    if constexpr (sizeof(T) == 4) f[0] = *p;
+    else if constexpr (sizeof(T) == 2 && !__is_same(T, __half)) f[0] = __bfloat162float(*p);
+    else f[0] = __half2float(*p);
+  } else if constexpr (sizeof(T) == 4) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  } else {
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    if constexpr (__is_same(T, __half)) {
+      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+        f[2 * i] = v.x;
+        f[2 * i + 1] = v.y;
+      }
+    } else {
+      unpack8(a, f);
+    }
+  }
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void store_v(T* p, const float* f) {
+  if constexpr (V == 1) {
+    if constexpr (sizeof(T) == 4) *p = f[0];
+    else if constexpr (__is_same(T, __half)) *p = __float2half_rn(f[0]);
+    else *p = __float2bfloat16_rn(f[0]);
+  } else if constexpr (sizeof(T) == 4) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (__is_same(T, __half)) {
+        const __half2 v = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&v);
+      } else {
+        w[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
+      }
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// First channels of unit u's two runs of V channels.
+template <int V>
+__device__ __forceinline__ int2 unit_channels(int u, int dim, int layout) {
+  if (u < dim / (2 * V) && layout == EPIKV_ROPE_HALF) return make_int2(u * V, dim / 2 + u * V);
+  return make_int2(2 * u * V, 2 * u * V + V);
+}
+
+template <int V>
+__device__ __forceinline__ void load_angles(const RopeDev& r, int pos, int u, float sign, float* c, float* s) {
+  const float2* t = r.table + (int64_t)pos * (r.dim / 2) + u * V;
+  if constexpr (V == 1) {
+    const float2 v = __ldg(t);
+    c[0] = v.x;
+    s[0] = sign * v.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+      const float4 v = __ldg(reinterpret_cast<const float4*>(t) + i);
+      c[2 * i] = v.x; s[2 * i] = sign * v.y;
+      c[2 * i + 1] = v.z; s[2 * i + 1] = sign * v.w;
+    }
+  }
+}
+
+// a cos - b sin and b cos + a sin, every operation rounded on its own.
+__device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
+  const float x = __fsub_rn(__fmul_rn(a, c), __fmul_rn(b, s));
+  b = __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
+  a = x;
+}
+
+template <int V>
+__device__ __forceinline__ void turn_unit(float* a, float* b, const float* c, const float* s, int layout) {
+  if (V == 1 || layout == EPIKV_ROPE_HALF) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) turn(a[i], b[i], c[i], s[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+      turn(a[2 * i], a[2 * i + 1], c[i], s[i]);
+      turn(b[2 * i], b[2 * i + 1], c[V / 2 + i], s[V / 2 + i]);
+    }
+  }
+}
+
+__global__ void rope_table_kernel(epikv_rope_config c, int n_pos, float2* table) {
+  const int half = c.dim / 2;
+  const int64_t n = (int64_t)n_pos * half;
+  for (int64_t k = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; k < n; k += (int64_t)gridDim.x * blockDim.x) {
+    const int pos = (int)(k / half), i = (int)(k - (int64_t)pos * half);
+    double theta = c.theta;
+    if (c.scaling == EPIKV_ROPE_NTK) theta *= pow((double)c.factor, (double)c.dim / (c.dim - 2));
+    double freq = pow(theta, -2.0 * i / c.dim);
+    if (c.scaling == EPIKV_ROPE_LINEAR) freq /= c.factor;
+    if (c.scaling == EPIKV_ROPE_BYPARTS) {
+      const double rot = c.original * freq / 6.283185307179586476925287;
+      const double g = fmin(fmax((rot - c.low) / ((double)c.high - c.low), 0.0), 1.0);
+      freq *= (1.0 - g) / c.factor + g;
+    }
+    double s, co;
+    sincos(pos * freq, &s, &co);
+    table[k] = make_float2((float)(co * c.magnitude), (float)(s * c.magnitude));
+  }
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(kBlock) rope_kernel(int32_t* err, Rows x, Rows y, const int32_t* __restrict__ pos,
+                                                      RopeDev r, int n_tokens, int heads, int d, float sign) {
+  const int U = d / (2 * V), slots = kBlock / U;  // units of a head; heads that the block takes at once
+  const int u = threadIdx.x % U, slot = threadIdx.x / U;
+  const int tpb = max(1, slots / heads);          // tokens of this block
+  const int step = heads < slots ? heads : slots;
+  if (slot >= tpb * step) return;
+  const int64_t token = (int64_t)blockIdx.x * tpb + slot / step;
+  if (token >= n_tokens) return;
+  const int p = pos[token];
+  if ((unsigned)p >= (unsigned)r.n_pos) {
+    set_error(err, EPIKV_DEV_POSITION);
+    return;
+  }
+  const bool turned = u < r.dim / (2 * V);
+  float c[V], s[V];
+  if (turned) load_angles<V>(r, p, u, sign, c, s);
+  const int2 ch = unit_channels<V>(u, r.dim, r.layout);
+  const T* src = reinterpret_cast<const T*>(x.p) + token * x.st;
+  T* dst = reinterpret_cast<T*>(y.p) + token * y.st;
+  for (int h0 = slot % step; h0 < heads; h0 += step * kBatch) {
+    float a[kBatch][V], b[kBatch][V];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int h = h0 + k * step;
+      if (h < heads) {
+        load_v<T, V>(src + h * x.sh + ch.x, a[k]);
+        load_v<T, V>(src + h * x.sh + ch.y, b[k]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int h = h0 + k * step;
+      if (h < heads) {
+        if (turned) turn_unit<V>(a[k], b[k], c, s, r.layout);
+        store_v<T, V>(dst + h * y.sh + ch.x, a[k]);
+        store_v<T, V>(dst + h * y.sh + ch.y, b[k]);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ append
+
+// Sixteen values in 4 bits: their codes (8 bytes) and scale.
+__device__ __forceinline__ uint2 quantize16(const float* x, float g, uint32_t* scale) {
+  float y[16];
+  float top = 0.f;
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    y[i] = __fdiv_rn(x[i], g);
+    nan |= y[i] != y[i];
+    top = fmaxf(top, fabsf(y[i]));
+  }
+  if (nan) {
+    *scale = 0x7f;  // E4M3's NaN: the group reads as NaN
+    return make_uint2(0, 0);
+  }
+  *scale = float_to_e4m3(fminf(__fdiv_rn(top, 6.f), 448.f));
+  const uint32_t h = e4m3x2_to_half2((uint16_t)*scale);
+  const float s = __half2float(__ushort_as_half((unsigned short)(h & 0xffffu)));
+  uint32_t w[2] = {0, 0};
+  if (s > 0.f) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      w[i / 4] |= float2_to_e2m1x2(__fdiv_rn(y[2 * i], s), __fdiv_rn(y[2 * i + 1], s)) << (8 * (i % 4));
+  }
+  return make_uint2(w[0], w[1]);
+}
+
+// Channels c0 .. c0+15 of a key, rotated and rounded to bf16 (kept as floats).
+// The partners of a half layout's channels are read beside them.
+__device__ __forceinline__ void turned16(const __nv_bfloat16* k, int c0, const RopeDev& r, int pos, float* x) {
+  load_v<__nv_bfloat16, 8>(k + c0, x);
+  load_v<__nv_bfloat16, 8>(k + c0 + 8, x + 8);
+  if (c0 >= r.dim) return;
+  const float2* t = r.table + (int64_t)pos * (r.dim / 2);
+  const int half = r.dim / 2;
+  if (r.layout == EPIKV_ROPE_INTERLEAVED) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c0 + 2 * i < r.dim) {
+        const float2 a = __ldg(t + c0 / 2 + i);
+        turn(x[2 * i], x[2 * i + 1], a.x, a.y);
+        x[2 * i] = __bfloat162float(__float2bfloat16_rn(x[2 * i]));
+        x[2 * i + 1] = __bfloat162float(__float2bfloat16_rn(x[2 * i + 1]));
+      }
+    return;
+  }
+  float z[16];
+  if (r.dim % 32 == 0) {  // the sixteen channels and their partners are whole runs
+    const int at = c0 < half ? c0 + half : c0 - half;
+    load_v<__nv_bfloat16, 8>(k + at, z);
+    load_v<__nv_bfloat16, 8>(k + at + 8, z + 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int c = c0 + i;
+      z[i] = c < r.dim ? __bfloat162float(k[c < half ? c + half : c - half]) : 0.f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int c = c0 + i;
+    if (c < r.dim) {
+      const float2 a = __ldg(t + (c < half ? c : c - half));
+      float lo = c < half ? x[i] : z[i], hi = c < half ? z[i] : x[i];
+      turn(lo, hi, a.x, a.y);
+      x[i] = __bfloat162float(__float2bfloat16_rn(c < half ? lo : hi));
+    }
+  }
+}
+
+// One block a token.  The queries (and, into a bf16 cache, the keys and values)
+// go by units; into a 4-bit cache a thread takes 16 channels that share a scale.
+template <int V, int kFmt>
+__global__ void __launch_bounds__(kBlock) append_kernel(AttnState st, AttnDims dm, int layer, Batch ba,
+                                                        const int32_t* __restrict__ pos, Rows q, Rows qo, Rows kr,
+                                                        Rows vr, RopeDev r, KvDev kv) {
+  const int b = blockIdx.y, i = blockIdx.x;
+  Entry e;
+  if (!batch_entry(ba, dm, b, true, st.err, &e) || i >= e.n) return;
+  int p = 0;
+  if (r.dim) {
+    const int64_t at = (int64_t)pos[b] + i;
+    if (at < 0 || at >= r.n_pos) {
+      set_error(st.err, EPIKV_DEV_POSITION);
+      return;
+    }
+    p = (int)at;
+  }
+  const int64_t row = kv_row_offset(kv, layer, e.seq, e.len + i, dm.T);
+  if (row < 0) {
+    set_error(st.err, EPIKV_DEV_SLOT);
+    return;
+  }
+  const int64_t token = (int64_t)e.tok0 + i;
+  const int nq = q.p ? dm.Hq : 0;
+  const int n = nq + (kFmt == EPIKV_CACHE_BF16 ? 2 * dm.H : 0);
+  const int U = dm.d / (2 * V), slots = kBlock / U;
+  const int u = threadIdx.x % U, slot = threadIdx.x / U;
+  using bf = __nv_bfloat16;
+  const bool turned = u < r.dim / (2 * V);
+  float c[V], s[V];
+  if (turned) load_angles<V>(r, p, u, 1.f, c, s);
+  const int2 ch = unit_channels<V>(u, r.dim, r.layout);
+  if (slot < slots)
+    for (int h0 = slot; h0 < n; h0 += slots * kBatch) {
+      float a[kBatch][V], z[kBatch][V];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int h = h0 + k * slots;
+        if (h < n) {
+          const Rows& from = h < nq ? q : h < nq + dm.H ? kr : vr;
+          const int hh = h < nq ? h : (h - nq) % dm.H;
+          const bf* src = reinterpret_cast<const bf*>(from.p) + token * from.st + hh * from.sh;
+          load_v<bf, V>(src + ch.x, a[k]);
+          load_v<bf, V>(src + ch.y, z[k]);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int h = h0 + k * slots;
+        if (h < n) {
+          if (turned && h < nq + dm.H) turn_unit<V>(a[k], z[k], c, s, r.layout);
+          bf* dst;
+          if (h < nq) dst = reinterpret_cast<bf*>(qo.p) + token * qo.st + h * qo.sh;
+          else dst = reinterpret_cast<bf*>(kv.base[h >= nq + dm.H]) + row + (int64_t)((h - nq) % dm.H) * dm.d;
+          store_v<bf, V>(dst + ch.x, a[k]);
+          store_v<bf, V>(dst + ch.y, z[k]);
+        }
+      }
+    }
+  if constexpr (kFmt == EPIKV_CACHE_E2M1) {
+    const int G = dm.d / kQuantGroup;
+    for (int j = threadIdx.x; j < 2 * dm.H * G; j += kBlock) {
+      const int which = j / (dm.H * G), h = j / G % dm.H, g = j % G;
+      float x[16];
+      if (which == 0) {
+        turned16(reinterpret_cast<const bf*>(kr.p) + token * kr.st + h * kr.sh, g * 16, r, p, x);
+      } else {
+        const bf* src = reinterpret_cast<const bf*>(vr.p) + token * vr.st + h * vr.sh + g * 16;
+        load_v<bf, 8>(src, x);
+        load_v<bf, 8>(src + 8, x + 8);
+      }
+      uint32_t scale;
+      const uint2 code = quantize16(x, head_scale(st, dm, which, layer, h), &scale);
+      char* dst = kv.base[which] + row * 2;
+      *reinterpret_cast<uint2*>(dst + h * (dm.d / 2) + g * 8) = code;
+      dst[scale_offset(dm, h) + g] = (char)scale;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ read-back
+
+// A thread takes 16 channels of one head of a row.
+__global__ void __launch_bounds__(kBlock) cache_read_kernel(AttnState st, AttnDims dm, int layer, int n_rows,
+                                                            const int32_t* __restrict__ seqs,
+                                                            const int32_t* __restrict__ slots, Rows k, Rows v,
+                                                            KvDev kv) {
+  const int G = dm.d / 16, per = dm.H * G;
+  const int64_t j = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+  if (j >= (int64_t)n_rows * per) return;
+  const int64_t i = j / per;
+  const int h = (int)(j - i * per) / G, g = (int)(j - i * per) % G;
+  const int seq = seqs[i];
+  const int64_t row = (unsigned)seq < (unsigned)dm.S ? kv_row_offset(kv, layer, seq, slots[i], dm.T) : -1;
+  if (row < 0) {
+    set_error(st.err, EPIKV_DEV_SLOT);
+    return;
+  }
+  using bf = __nv_bfloat16;
+  for (int w = 0; w < 2; ++w) {
+    const Rows& to = w ? v : k;
+    if (!to.p) continue;
+    bf* dst = reinterpret_cast<bf*>(to.p) + i * to.st + h * to.sh + g * 16;
+    const char* src = kv.base[w] + row * 2;
+    if (dm.fmt == EPIKV_CACHE_BF16) {
+      const uint4* s = reinterpret_cast<const uint4*>(src + (h * dm.d + g * 16) * 2);
+      reinterpret_cast<uint4*>(dst)[0] = s[0];
+      reinterpret_cast<uint4*>(dst)[1] = s[1];
+      continue;
+    }
+    const uint2 code = *reinterpret_cast<const uint2*>(src + h * (dm.d / 2) + g * 8);
+    const uint32_t sc = e4m3x2_to_half2((uint8_t)src[scale_offset(dm, h) + g]);
+    const float scale = __half2float(__ushort_as_half((unsigned short)(sc & 0xffffu)));
+    const float gs = head_scale(st, dm, w, layer, h);
+    uint32_t hw[8];
+    e2m1x8_to_half2(code.x, reinterpret_cast<uint32_t(&)[4]>(hw[0]));
+    e2m1x8_to_half2(code.y, reinterpret_cast<uint32_t(&)[4]>(hw[4]));
+    float f[16];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&hw[c]));
+      f[2 * c] = x.x * scale * gs;
+      f[2 * c + 1] = x.y * scale * gs;
+    }
+    store_v<bf, 8>(dst, f);
+    store_v<bf, 8>(dst + 8, f + 8);
+  }
+}
+
+template <typename T>
+cudaError_t rope_of(const AttnState& st, const AttnDims& dm, int n_tokens, int n_heads, const Rows& x, const Rows& y,
+                    const int32_t* pos, const RopeDev& rope, float sign, cudaStream_t stream) {
+  const bool vec = rope.dim % 16 == 0;
+  const int slots = kBlock / (vec ? dm.d / 16 : dm.d / 2);
+  const int tpb = slots / n_heads > 1 ? slots / n_heads : 1;
+  const unsigned grid = (unsigned)(((int64_t)n_tokens + tpb - 1) / tpb);
+  return vec ? plain_launch(rope_kernel<T, 8>, grid, kBlock, 0, stream, st.err, x, y, pos, rope, n_tokens, n_heads,
+                            dm.d, sign)
+             : plain_launch(rope_kernel<T, 1>, grid, kBlock, 0, stream, st.err, x, y, pos, rope, n_tokens, n_heads,
+                            dm.d, sign);
+}
+
+}  // namespace
+
+cudaError_t launch_rope_table(const epikv_rope_config& c, int n_pos, float* table, cudaStream_t stream) {
+  const int64_t n = (int64_t)n_pos * (c.dim / 2);
+  const int64_t want = (n + 255) / 256;
+  rope_table_kernel<<<(unsigned)(want < 4096 ? want : 4096), 256, 0, stream>>>(c, n_pos,
+                                                                              reinterpret_cast<float2*>(table));
+  return cudaGetLastError();
+}
+
+cudaError_t launch_rope(const AttnState& st, const AttnDims& dm, int n_tokens, int n_heads, const Rows& x,
+                        const Rows& y, int type, const int32_t* pos, const RopeDev& rope, bool inverse,
+                        cudaStream_t stream) {
+  const float sign = inverse ? -1.f : 1.f;
+  if (type == EPIKV_TYPE_F32) return rope_of<float>(st, dm, n_tokens, n_heads, x, y, pos, rope, sign, stream);
+  if (type == EPIKV_TYPE_F16) return rope_of<__half>(st, dm, n_tokens, n_heads, x, y, pos, rope, sign, stream);
+  return rope_of<__nv_bfloat16>(st, dm, n_tokens, n_heads, x, y, pos, rope, sign, stream);
+}
+
+cudaError_t launch_append(const AttnState& st, const AttnDims& dm, int layer, const Batch& ba, const int32_t* pos,
+                          const Rows& q, const Rows& qo, const Rows& k, const Rows& v, const RopeDev& rope,
+                          const KvDev& kv, cudaStream_t stream) {
+  const dim3 grid(ba.max_new, ba.n_seq);
+  const bool vec = rope.dim % 16 == 0;
+  const bool q4 = dm.fmt == EPIKV_CACHE_E2M1;
+  auto kern = vec ? (q4 ? append_kernel<8, EPIKV_CACHE_E2M1> : append_kernel<8, EPIKV_CACHE_BF16>)
+                  : (q4 ? append_kernel<1, EPIKV_CACHE_E2M1> : append_kernel<1, EPIKV_CACHE_BF16>);
+  return plain_launch(kern, grid, kBlock, 0, stream, st, dm, layer, ba, pos, q, qo, k, v, rope, kv);
+}
+
+cudaError_t launch_cache_read(const AttnState& st, const AttnDims& dm, int layer, int n_rows, const int32_t* seqs,
+                              const int32_t* slots, const Rows& k, const Rows& v, const KvDev& kv,
+                              cudaStream_t stream) {
+  const int64_t n = (int64_t)n_rows * dm.H * (dm.d / 16);
+  return plain_launch(cache_read_kernel, (unsigned)((n + kBlock - 1) / kBlock), kBlock, 0, stream, st, dm, layer,
+                      n_rows, seqs, slots, k, v, kv);
+}
+
+}  // namespace epikv

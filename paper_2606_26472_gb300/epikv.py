@@ -16,6 +16,11 @@ EPIKV_DEV_KEPT, EPIKV_DEV_BUDGET, EPIKV_DEV_TIMEOUT = 4, 5, 6
 EPIKV_SCORE_BANDZ, EPIKV_SCORE_LAGKV, EPIKV_SCORE_HSVAR = 1, 2, 4
 EPIKV_SCORE_KVKEY, EPIKV_SCORE_KVVAL, EPIKV_SCORE_LAGKEY = 8, 16, 32
 EPIKV_LAYOUT_CONTIGUOUS, EPIKV_LAYOUT_PAGED = 0, 1
+EPIKV_DEV_POSITION = 7
+EPIKV_CACHE_BF16, EPIKV_CACHE_E2M1 = 0, 1
+EPIKV_TYPE_BF16, EPIKV_TYPE_F16, EPIKV_TYPE_F32 = 0, 1, 2
+EPIKV_ROPE_HALF, EPIKV_ROPE_INTERLEAVED = 0, 1
+EPIKV_ROPE_PLAIN, EPIKV_ROPE_LINEAR, EPIKV_ROPE_NTK, EPIKV_ROPE_BYPARTS = 0, 1, 2, 3
 
 
 class epikv_config(C.Structure):
@@ -43,8 +48,29 @@ class epikv_stats(C.Structure):
                 ("layer_rows_moved", C.c_ulonglong)]
 
 
+class epikv_rope_config(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("theta", C.c_float), ("scaling", C.c_int32), ("factor", C.c_float),
+                ("low", C.c_float), ("high", C.c_float), ("original", C.c_int32), ("magnitude", C.c_float)]
+
+
+class epikv_rope_view(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("n_pos", C.c_int32), ("dim", C.c_int32), ("layout", C.c_int32)]
+
+
+class epikv_rows(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("stride_token", C.c_int64), ("stride_head", C.c_int64), ("type", C.c_int32)]
+
+
+class epikv_attn_config(C.Structure):
+    _fields_ = [("max_seqs", C.c_int32), ("max_cache_tokens", C.c_int32), ("max_new_tokens", C.c_int32),
+                ("num_layers", C.c_int32), ("num_heads", C.c_int32), ("num_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("cache_format", C.c_int32), ("softmax_scale", C.c_float),
+                ("kv_scale", C.c_void_p)]
+
+
 _P = C.c_void_p
 _I = C.c_int32
+_ROWS, _KV, _ROPE = C.POINTER(epikv_rows), C.POINTER(epikv_kv_view), C.POINTER(epikv_rope_view)
 _SIGS = {
     "epikv_workspace_bytes": (C.c_size_t, [C.POINTER(epikv_config)]),
     "epikv_init": (C.c_int, [C.POINTER(_P), C.POINTER(epikv_config), _P, C.c_size_t, _P]),
@@ -63,6 +89,16 @@ _SIGS = {
     "epikv_get_error": (C.c_int, [_P, C.POINTER(_I)]),
     "epikv_lagkv_score_noalloc": (C.c_int, [C.POINTER(epikv_kv_view), _I, _I, _I, _I, _I, _I, C.c_float, _I,
                                             _P, _P]),
+    "epikv_cache_row": (C.c_int, [_I, _I, _I, C.POINTER(_I), C.POINTER(_I)]),
+    "epikv_attn_workspace_bytes": (C.c_size_t, [C.POINTER(epikv_attn_config)]),
+    "epikv_attn_init": (C.c_int, [C.POINTER(_P), C.POINTER(epikv_attn_config), _P, C.c_size_t, _P]),
+    "epikv_rope_table": (C.c_int, [C.POINTER(epikv_rope_config), _I, _P, _P]),
+    "epikv_rope": (C.c_int, [_P, _I, _I, _ROWS, _ROWS, _P, _ROPE, _I, _P]),
+    "epikv_append": (C.c_int, [_P, _I, _I, _P, _P, _I, _P, _I, _P, _ROWS, _ROWS, _ROWS, _ROWS, _ROPE, _KV, _P]),
+    "epikv_attention": (C.c_int, [_P, _I, _I, _P, _P, _I, _P, _I, _I, _ROWS, _ROWS, _P, _KV, _P]),
+    "epikv_cache_read": (C.c_int, [_P, _I, _I, _P, _P, _ROWS, _ROWS, _KV, _P]),
+    "epikv_attn_get_error": (C.c_int, [_P, C.POINTER(_I)]),
+    "epikv_attn_destroy": (None, [_P]),
     "epikv_destroy": (None, [_P]),
     "epikv_status_string": (C.c_char_p, [C.c_int]),
 }
@@ -154,6 +190,38 @@ def kv_view(k, v, *, layout=EPIKV_LAYOUT_CONTIGUOUS, stride_layer, stride_seq=0,
             block_table=None, max_blocks_per_seq=0, block_size=0, num_blocks=0, stride_table_layer=0):
     return epikv_kv_view(_ptr(k), _ptr(v), layout, stride_layer, stride_seq, stride_block, stride_token,
                          _ptr(block_table), max_blocks_per_seq, block_size, num_blocks, stride_table_layer)
+
+
+def make_attn_config(*, max_seqs, max_cache_tokens, max_new_tokens, num_layers=32, num_heads=32, num_kv_heads=8,
+                     head_dim=128, cache_format=EPIKV_CACHE_BF16, softmax_scale=0.0, kv_scale=None):
+    """kv_scale: a device float tensor [2][num_layers][num_kv_heads] that outlives the context, or None."""
+    return epikv_attn_config(max_seqs, max_cache_tokens, max_new_tokens, num_layers, num_heads, num_kv_heads, head_dim,
+                             cache_format, softmax_scale, _ptr(kv_scale))
+
+
+def make_rope_config(dim, *, theta=10000.0, scaling=EPIKV_ROPE_PLAIN, factor=1.0, low=1.0, high=4.0, original=8192,
+                     magnitude=1.0):
+    return epikv_rope_config(dim, theta, scaling, factor, low, high, original, magnitude)
+
+
+def rope_view(table, layout=EPIKV_ROPE_HALF):
+    """A table [n_pos, dim / 2, 2] of epikv_rope_table's contents (float32, contiguous, on the device)."""
+    import torch
+    if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+        raise ValueError(f"a rotation table is contiguous float32 [n_pos, dim / 2, 2]: got {tuple(table.shape)}")
+    return epikv_rope_view(table.data_ptr(), table.shape[0], 2 * table.shape[1], layout)
+
+
+_TYPES = {"torch.bfloat16": EPIKV_TYPE_BF16, "torch.float16": EPIKV_TYPE_F16, "torch.float32": EPIKV_TYPE_F32}
+
+
+def rows(t):
+    """The heads of tokens that a tensor [tokens, heads, channels] holds (channels contiguous; the tensor may be a
+    slice of a wider one).  It describes memory: the tensor is the caller's to keep."""
+    if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] != 1) or str(t.dtype) not in _TYPES:
+        raise ValueError(f"rows are bf16, f16 or f32 [tokens, heads, channels], channels contiguous: got {t.dtype} "
+                         f"{tuple(t.shape)}, strides {t.stride()}")
+    return epikv_rows(t.data_ptr(), t.stride(0), t.stride(1), _TYPES[str(t.dtype)])
 
 
 # ---------------------------------------------------------------- same names
@@ -285,6 +353,73 @@ def epikv_lagkv_score_noalloc(kv, seq, n, num_layers, num_kv_heads, head_dim, la
     """Lag-KV scores of positions 0..n-1 of `seq` without any workspace (see epikv.h)."""
     _check(load().epikv_lagkv_score_noalloc(C.byref(kv), seq, n, num_layers, num_kv_heads, head_dim, lag, lag_eps,
                                             window, _ptr(scores), _stream(stream)), "epikv_lagkv_score_noalloc")
+
+
+# ---------------------------------------------------------------- tokens into the cache, and attention over it
+def epikv_cache_row(num_kv_heads, head_dim, cache_format):
+    """(heads, dim): a token's row as the eviction calls' num_kv_heads and head_dim."""
+    h, d = C.c_int32(), C.c_int32()
+    _check(load().epikv_cache_row(num_kv_heads, head_dim, cache_format, C.byref(h), C.byref(d)), "epikv_cache_row")
+    return h.value, d.value
+
+
+def epikv_attn_workspace_bytes(cfg):
+    return load().epikv_attn_workspace_bytes(C.byref(cfg))
+
+
+def epikv_attn_init(cfg, workspace, workspace_bytes, stream=None):
+    ctx = C.c_void_p()
+    _check(load().epikv_attn_init(C.byref(ctx), C.byref(cfg), _ptr(workspace), workspace_bytes, _stream(stream)),
+           "epikv_attn_init")
+    return ctx
+
+
+def epikv_rope_table(cfg, n_pos, device="cuda", stream=None):
+    """A new table [n_pos, dim / 2, 2] (the binding allocates it; the C call fills the caller's)."""
+    import torch
+    table = torch.empty(n_pos, cfg.dim // 2, 2, dtype=torch.float32, device=device)
+    _check(load().epikv_rope_table(C.byref(cfg), n_pos, _ptr(table), _stream(stream)), "epikv_rope_table")
+    return table
+
+
+def _ref(x):
+    return C.byref(x) if x is not None else None
+
+
+def epikv_rope(ctx, n_tokens, n_heads, x, out, pos, rope, *, inverse=False, stream=None):
+    _check(load().epikv_rope(ctx, n_tokens, n_heads, _ref(x), _ref(out), _ptr(pos), _ref(rope), 1 if inverse else 0,
+                             _stream(stream)), "epikv_rope")
+
+
+def epikv_append(ctx, layer, n_seq, seq_ids, cu_new, max_new, length, pos, q, q_out, k, v, rope, kv, *, len_stride=1,
+                 stream=None):
+    """q, q_out, k, v: rows(...) (q and q_out may be None); rope: rope_view(...) or None."""
+    _check(load().epikv_append(ctx, layer, n_seq, _ptr(seq_ids), _ptr(cu_new), max_new, _ptr(length), len_stride,
+                               _ptr(pos), _ref(q), _ref(q_out), _ref(k), _ref(v), _ref(rope), _ref(kv),
+                               _stream(stream)), "epikv_append")
+
+
+def epikv_attention(ctx, layer, n_seq, seq_ids, cu_new, max_new, length, q, out, kv, *, lse=None, causal=True,
+                    len_stride=1, stream=None):
+    _check(load().epikv_attention(ctx, layer, n_seq, _ptr(seq_ids), _ptr(cu_new), max_new, _ptr(length), len_stride,
+                                  1 if causal else 0, _ref(q), _ref(out), _ptr(lse), _ref(kv), _stream(stream)),
+           "epikv_attention")
+
+
+def epikv_cache_read(ctx, layer, n_rows, seqs, slots, k, v, kv, stream=None):
+    _check(load().epikv_cache_read(ctx, layer, n_rows, _ptr(seqs), _ptr(slots), _ref(k), _ref(v), _ref(kv),
+                                   _stream(stream)), "epikv_cache_read")
+
+
+def epikv_attn_get_error(ctx):
+    """(status, device code); clears the sticky device error word."""
+    code = C.c_int32()
+    st = load().epikv_attn_get_error(ctx, C.byref(code))
+    return st, code.value
+
+
+def epikv_attn_destroy(ctx):
+    load().epikv_attn_destroy(ctx)
 
 
 def epikv_destroy(ctx):

@@ -1,0 +1,291 @@
+"""epikv_attention against float64: head layouts, lengths from none to thousands, ragged batches, pages that end inside
+a tile, rows that see nothing, what stands in slots that a row does not see, and what is refused or reported."""
+import math
+
+import pytest
+import torch
+
+from paper_2606_26472_gb300 import epikv as E
+
+from . import cache_ops as R
+
+pytestmark = pytest.mark.gpu
+
+
+def run(c, ctx, q, new, held, *, layer=0, seqs=None, causal=True, max_new=None, lse=True, out=None, stream=None):
+    seq_ids, cu, ln = R.batch(new, held, seqs)
+    n = q.shape[0]
+    o = torch.full(q.shape, float("nan"), dtype=torch.bfloat16, device="cuda") if out is None else out
+    l = torch.full((n, q.shape[1]), float("nan"), device="cuda") if lse else None
+    E.epikv_attention(ctx, layer, len(new), seq_ids, cu, max(new) if max_new is None else max_new, ln, E.rows(q),
+                      E.rows(o), c.c.view(), lse=l, causal=causal, stream=stream)
+    return o, l
+
+
+def check(c, q, o, l, new, held, *, layer=0, seqs=None, causal=True, scale=None, what=""):
+    scale = 1 / math.sqrt(c.d) if scale is None else scale
+    t = 0
+    for b, n in enumerate(new):
+        s = b if seqs is None else seqs[b]
+        top = held[b] + (n if causal else 0)
+        k, v = c.read(0, layer, s, top), c.read(1, layer, s, top)
+        limits = [held[b] + (i + 1 if causal else 0) for i in range(n)]
+        ref = R.attention64(q[t:t + n], k, v, limits, scale)
+        R.assert_attention_close(o[t:t + n], l[t:t + n] if l is not None else None, ref, f"{what} entry {b}")
+        t += n
+
+
+def queries(n, Hq, d, seed=1):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(n, Hq, d, generator=g, device="cuda").to(torch.bfloat16)
+
+
+SHAPES = [(8, 32, 128), (1, 1, 64), (1, 8, 128), (2, 14, 128), (3, 3, 64), (4, 32, 64), (5, 20, 128), (2, 4, 256),
+          (4, 32, 256), (11, 11, 64), (16, 32, 64), (7, 7, 128), (1, 71, 64)]
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("H,Hq,d", SHAPES)
+def test_single_tokens(gpu_lib, bits, H, Hq, d):
+    """One new token of each sequence: lengths around the edges of tiles and pages."""
+    held = [0, 1, 14, 15, 16, 17, 30, 31, 32, 33, 63, 64, 127, 128, 300, 1023]
+    for block in (16, 0, 7):
+        c = R.Cache(seqs=16, T=1030, H=H, d=d, bits=bits, block=block, seed=H * d)
+        ctx = c.context(Hq, 1)
+        q = queries(16, Hq, d)
+        seqs = list(range(15, -1, -1))
+        o, l = run(c, ctx, q, [1] * 16, held, seqs=seqs)
+        check(c, q, o, l, [1] * 16, held, seqs=seqs, what=f"block {block}")
+        assert E.epikv_attn_get_error(ctx) == (E.EPIKV_OK, 0)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("H,Hq,d", SHAPES)
+def test_several_tokens(gpu_lib, bits, H, Hq, d):
+    """Ragged new tokens, none among them, over short and long caches: the causal edge at every place of a tile."""
+    new, held = [3, 0, 1, 17, 47, 8], [0, 5, 200, 31, 77, 1500]
+    for block in (16, 0, 48):
+        c = R.Cache(seqs=6, T=1600, H=H, d=d, bits=bits, block=block, seed=H + d)
+        ctx = c.context(Hq, 64)
+        q = queries(sum(new), Hq, d)
+        o, l = run(c, ctx, q, new, held)
+        check(c, q, o, l, new, held, what=f"block {block}")
+        assert E.epikv_attn_get_error(ctx) == (E.EPIKV_OK, 0)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_prompt_and_long(gpu_lib, bits):
+    c = R.Cache(seqs=2, T=20000, H=2, d=128, bits=bits, seed=5)
+    ctx = c.context(8, 300)
+    q = queries(301, 8, 128)
+    o, l = run(c, ctx, q, [300, 1], [0, 19999])
+    check(c, q, o, l, [300, 1], [0, 19999])
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_prefix_without_the_new_tokens(gpu_lib, bits):
+    """causal=0: every query sees the held slots; none held: zeros and -inf; two parts join by their lse."""
+    c = R.Cache(seqs=3, T=400, H=2, d=64, bits=bits, seed=2)
+    ctx = c.context(6, 5)
+    new, held = [5, 2, 3], [0, 399, 18]
+    q = queries(10, 6, 64)
+    o, l = run(c, ctx, q, new, held, causal=False)
+    check(c, q, o, l, new, held, causal=False)
+    assert not o[:5].any() and bool((l[:5] == -math.inf).all())
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("new", [1, 6, 40])
+def test_unseen_slots_do_not_reach_a_row(gpu_lib, bits, new):
+    """Slots behind a row's last one hold NaN: rows before them are untouched, rows that see them are NaN."""
+    held, T = 45, 128
+    c = R.Cache(seqs=1, T=T, H=2, d=128, bits=bits, seed=3)
+    ctx = c.context(8, 64)
+    q = queries(new, 8, 128)
+    for first_bad in sorted({held + new, held + new // 2 + 1, held + 1}):
+        if first_bad > held + new:
+            continue
+        saved = [c.raw(w).clone() for w in range(2)]
+        idx = c.index(0, 0, torch.arange(first_bad, T))
+        for w in range(2):
+            c.raw(w)[idx] = 0x7F if bits == 4 else 0xFF
+        o, l = run(c, ctx, q, [new], [held])
+        good = first_bad - held
+        k, v = c.read(0, 0, 0, held + new), c.read(1, 0, 0, held + new)
+        ref = R.attention64(q[:good], k[:first_bad], v[:first_bad], [held + i + 1 for i in range(good)], 128 ** -0.5)
+        R.assert_attention_close(o[:good], l[:good], ref, f"bad from {first_bad}")
+        assert bool(o[good:].isnan().all())
+        for w in range(2):
+            c.raw(w).copy_(saved[w])
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_values_of_one_unseen_row(gpu_lib, bits):
+    """An infinite value in the newest token's V alone, finite keys: earlier rows stay as they were."""
+    c = R.Cache(seqs=1, T=64, H=1, d=64, bits=bits, seed=4)
+    ctx = c.context(4, 8)
+    q = queries(8, 4, 64)
+    before, _ = run(c, ctx, q, [8], [30])
+    c.raw(1)[c.index(0, 0, torch.arange(35, 36))] = 0x7F if bits == 4 else 0xFF
+    after, _ = run(c, ctx, q, [8], [30])
+    assert torch.equal(before[:5], after[:5]) and bool(after[5:].isnan().all())
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_large_scores(gpu_lib, bits):
+    """Scores in the hundreds of both signs, growing along the sequence: the running maximum moves at every tile."""
+    c = R.Cache(seqs=1, T=700, H=2, d=64, bits=bits, seed=6)
+    ramp = torch.linspace(-40, 40, 700, device="cuda")
+    x = torch.ones(c.raw(0).shape[0], 2, 64, device="cuda")
+    x[c.index(0, 0, torch.arange(700))] = ramp[:, None, None].expand(-1, 2, 64)
+    c.put(c.c.k, x.to(torch.bfloat16), 0)
+    ctx = c.context(4, 2)
+    for sign in (1.0, -1.0):
+        q = (queries(2, 4, 64).abs() + 0.5) * sign
+        q = q.to(torch.bfloat16)
+        o, l = run(c, ctx, q, [2], [690])
+        check(c, q, o, l, [2], [690], what=f"sign {sign}")
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_query_magnitudes(gpu_lib, bits):
+    c = R.Cache(seqs=1, T=100, H=2, d=128, bits=bits, seed=7)
+    for mag in (0.0, 1e-30, 1e-3, 300.0, 1e5):
+        ctx = c.context(8, 1, softmax_scale=0.0 if mag <= 1 else 0.05 / mag)
+        q = (queries(1, 8, 128).float() * mag).to(torch.bfloat16)
+        o, l = run(c, ctx, q, [1], [99])
+        check(c, q, o, l, [1], [99], scale=None if mag <= 1 else float(torch.tensor(0.05 / mag)), what=f"|q| {mag}")
+
+
+def test_head_scales(gpu_lib):
+    s = torch.rand(2, 2, 4, device="cuda") * 3 + 0.01
+    c = R.Cache(seqs=2, T=200, H=4, d=64, bits=4, layers=2, kv_scale=s, seed=8)
+    ctx = c.context(8, 3)
+    q = queries(4, 8, 64)
+    o, l = run(c, ctx, q, [3, 1], [150, 20], layer=1)
+    check(c, q, o, l, [3, 1], [150, 20], layer=1)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_strided_rows_streams_and_graphs(gpu_lib, bits):
+    """Queries inside a wider tensor, outputs head-major, another stream, a captured graph, the same bits each time."""
+    c = R.Cache(seqs=4, T=600, H=8, d=128, bits=bits, seed=9)
+    ctx = c.context(32, 2)
+    new, held = [1, 2, 1, 2], [599, 100, 17, 333]
+    wide = queries(6, 48, 128)
+    q = wide[:, :32]
+    a = torch.empty(32, 6, 128, dtype=torch.bfloat16, device="cuda")
+    o, l = run(c, ctx, q, new, held, out=a.transpose(0, 1))
+    check(c, q.contiguous(), o, l, new, held)
+    first = a.clone()
+    seq_ids, cu, ln = R.batch(new, held)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    b = torch.zeros_like(a)
+    l2 = torch.zeros_like(l)
+    torch.cuda.synchronize()
+    kv, qr, orow = c.c.view(), E.rows(q), E.rows(b.transpose(0, 1))
+    E.epikv_attention(ctx, 0, 4, seq_ids, cu, 2, ln, qr, orow, kv, lse=l2, stream=s)
+    s.synchronize()
+    assert torch.equal(b, first) and torch.equal(l2, l)
+    b.zero_()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        E.epikv_attention(ctx, 0, 4, seq_ids, cu, 2, ln, qr, orow, kv)
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(b, first)
+    ln.copy_(torch.tensor([40, 300, 598, 5], dtype=torch.int32))     # the lengths are read on the device
+    g.replay()
+    torch.cuda.synchronize()
+    check(c, q.contiguous(), b.transpose(0, 1), None, new, [40, 300, 598, 5])
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_offsets_past_32_bits(gpu_lib, bits):
+    """Two blocks 6 GB apart in one pool."""
+    H, d, bs = 8, 128, 16
+    h2, d2 = E.epikv_cache_row(H, d, E.EPIKV_CACHE_E2M1 if bits == 4 else E.EPIKV_CACHE_BF16)
+    units = h2 * d2
+    blocks = 3 * 2 ** 30 // (units * bs) + 2
+    small = R.Cache(seqs=1, T=32, H=H, d=d, bits=bits, seed=10)
+    pools = [torch.empty(blocks * bs * units, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for w in range(2):
+        raw = pools[w].view(torch.uint8).view(-1, 2 * units)
+        src = small.raw(w)[small.index(0, 0, torch.arange(32))]
+        raw[(blocks - 1) * bs:] = src[:16]
+        raw[:bs] = src[16:]
+    bt = torch.tensor([[blocks - 1, 0]], dtype=torch.int32, device="cuda")
+    kv = E.kv_view(pools[0], pools[1], layout=E.EPIKV_LAYOUT_PAGED, stride_layer=0, stride_block=bs * units,
+                   stride_token=units, block_table=bt, max_blocks_per_seq=2, block_size=bs, num_blocks=blocks)
+    ctx = small.context(32, 1)
+    q = queries(1, 32, d)
+    seq_ids, cu, ln = R.batch([1], [31])
+    o = torch.empty_like(q)
+    E.epikv_attention(ctx, 0, 1, seq_ids, cu, 1, ln, E.rows(q), E.rows(o), kv)
+    check(small, q, o, None, [1], [31])
+    x = torch.randn(1, H, d, device="cuda").to(torch.bfloat16)
+    bt.copy_(bt.flip(1))
+    E.epikv_append(ctx, 0, 1, seq_ids, cu, 1, ln, None, None, None, E.rows(x), E.rows(x), None, kv)
+    want = R.pack(x, units)[0] if bits == 4 else x.view(1, -1).view(torch.uint8)[0]
+    used = H * (d // 2 + d // 16) if bits == 4 else 2 * units
+    assert torch.equal(pools[0].view(torch.uint8).view(-1, 2 * units)[blocks * bs - 1, :used], want[:used])
+    assert E.epikv_attn_get_error(ctx) == (E.EPIKV_OK, 0)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_many_sequences(gpu_lib, bits):
+    """More sequences than the grid has blocks, most of them short, none, or one long."""
+    S = 700
+    held = [(7 * i) % 60 for i in range(S)]
+    held[333] = 5000
+    new = [(i % 3) for i in range(S)]
+    c = R.Cache(seqs=S, T=5003, H=1, d=64, bits=bits, seed=11)
+    ctx = c.context(2, 2)
+    q = queries(sum(new), 2, 64)
+    o, l = run(c, ctx, q, new, held)
+    check(c, q, o, l, new, held)
+
+
+def test_reported_and_skipped(gpu_lib):
+    c = R.Cache(seqs=2, T=64, H=2, d=64, bits=4)
+    ctx = c.context(2, 4)
+    for kw, code in ((dict(new=[1, 1], held=[5, 64]), E.EPIKV_DEV_CAPACITY),
+                     (dict(new=[1, 1], held=[5, -2]), E.EPIKV_DEV_CAPACITY),
+                     (dict(new=[1, 1], held=[5, 5], seqs=[0, 9]), E.EPIKV_DEV_BATCH),
+                     (dict(new=[1, 3], held=[5, 5], max_new=2), E.EPIKV_DEV_BATCH)):
+        q = queries(sum(kw["new"]), 2, 64)
+        o, l = run(c, ctx, q, **kw)
+        assert E.epikv_attn_get_error(ctx) == (E.EPIKV_EDEVICE, code)
+        check(c, q[:1], o[:1], l[:1], [1], [5])
+        assert bool(o[1:].isnan().all())
+    c.c.block_table[1, 0] = -1
+    q = queries(2, 2, 64)
+    o, l = run(c, ctx, q, [1, 1], [5, 40])
+    assert E.epikv_attn_get_error(ctx) == (E.EPIKV_EDEVICE, E.EPIKV_DEV_SLOT)
+    check(c, q[:1], o[:1], l[:1], [1], [5])
+
+
+def test_refusals(gpu_lib):
+    c = R.Cache(seqs=2, T=32, H=2, d=64, bits=16)
+    ctx = c.context(4, 4)
+    q = queries(3, 4, 64)
+    seq_ids, cu, ln = R.batch([3], [0])
+    ok = dict(layer=0, n=1, seq_ids=seq_ids, cu=cu, max_new=3, ln=ln, q=E.rows(q), o=E.rows(q.clone()),
+              kv=c.c.view(), ls=1)
+
+    def call(**kw):
+        a = {**ok, **kw}
+        E.epikv_attention(ctx, a["layer"], a["n"], a["seq_ids"], a["cu"], a["max_new"], a["ln"], a["q"], a["o"],
+                          a["kv"], len_stride=a["ls"])
+
+    call()
+    call(n=0)
+    call(max_new=0)
+    for bad in (dict(layer=1), dict(n=3), dict(max_new=5), dict(seq_ids=None), dict(cu=None), dict(ln=None),
+                dict(q=None), dict(o=None), dict(q=E.rows(q.float())), dict(o=E.rows(q.half())), dict(kv=None),
+                dict(ls=0)):
+        with pytest.raises(E.EpikvError) as err:
+            call(**bad)
+        assert err.value.status == E.EPIKV_EINVAL, bad
+    assert E.epikv_attn_get_error(ctx) == (E.EPIKV_OK, 0)
