@@ -1,0 +1,122 @@
+"""Attention's plan (csrc/attn_plan.h, compiled for the host): every configuration's shared memory holds what its warps
+address, and the CTAs' shares cover each item's tiles once, with at most one partial result of either kind per CTA."""
+import ctypes as C
+import os
+import shutil
+import subprocess
+
+import pytest
+
+from .plans import CSRC
+
+_SOURCE = r"""
+#include "attn_plan.h"
+using namespace epikv;
+#define NEED(x) do { if (!(x)) return __LINE__; } while (0)
+extern "C" {
+// 0, or the line of the first check that fails
+int geometry_holds(int H, int rep, int d, int q4, int n_seq, int max_new) {
+  const AttnGeometry g = attn_geometry(H, rep, d, q4, n_seq, max_new, true);
+  const int nt = attn_row_blocks(d, rep, max_new), sub = attn_sub_blocks(q4, nt);
+  NEED(g.units >= 2 && g.units <= kMaxUnits && g.smem_bytes <= kAttnSmem);
+  NEED(g.sh.rows == 8 * nt && nt * d <= 256);
+  NEED(g.sh.tile % 16 == 0 && g.sh.tile >= 16 && g.sh.tile <= 32 * kRowsPerLane);
+  NEED(g.row_s % 16 == 0 && g.unit_bytes % 128 == 0 && g.unit_bytes >= g.sh.tile * g.row_s);
+  NEED(g.join_off >= g.units * g.unit_bytes && g.join_off % 16 == 0 && g.bar_off % 8 == 0 && g.pre_off % 8 == 0);
+  NEED(g.pre_off >= g.bar_off + (2 * kMaxUnits + 1) * 8 && g.smem_bytes >= g.pre_off + (n_seq + 1) * 8);
+  NEED(g.sh.groups * kAttnGroup >= H && (g.sh.groups - 1) * kAttnGroup < H);
+  for (int group = 0; group < g.sh.groups; ++group) {
+    const int heads = H - group * kAttnGroup < kAttnGroup ? H - group * kAttnGroup : kAttnGroup;
+    const int teams = attn_teams(heads);
+    NEED(teams == 1 || teams == 2 || teams == 4 || teams == 8);
+    NEED(teams * heads <= kAttnWarps);
+    for (int s = 0; s < g.sh.tile / 16; ++s) {   // each block of 16 slots is one team's, within its reach
+      int n = 0;
+      for (int team = 0; team < teams; ++team)
+        for (int u = 0; u < sub; ++u) n += u * teams + team == s;
+      NEED(n == 1);
+    }
+    const int row = q4 ? heads * (d / 2) + ((heads * (d / 16) + 15) & ~15) : heads * d * 2;
+    NEED(row <= g.row_s);
+    for (int step = teams / 2; step > 0; step >>= 1)
+      for (int team = 0; team < step; ++team)
+        for (int head = 0; head < heads; ++head)
+          NEED(g.join_off + (int64_t)(team * heads + head + 1) * attn_box_floats(d, nt) * 4 <= g.bar_off);
+  }
+  const AttnGeometry most = attn_geometry(H, rep, d, q4, 1, max_new, true);   // what the workspace is sized by
+  for (int n = 1; n <= max_new; n *= 2) NEED(attn_geometry(H, rep, d, q4, n_seq, n, false).slot_floats <= most.slot_floats);
+  return 0;
+}
+
+int shares_hold(int H, int rep, int d, int q4, int max_new, int causal, int n_seq, const int* n, const int* len) {
+  const AttnGeometry g = attn_geometry(H, rep, d, q4, n_seq, max_new, causal);
+  int64_t total = 0;
+  for (int b = 0; b < n_seq; ++b) total += entry_tiles(g.sh, n[b], len[b]);
+  if (!total) return 0;
+  NEED(first_tile(0, total) == 0 && first_tile(kAttnCtas, total) == total);
+  for (int c = 0; c < kAttnCtas; ++c) NEED(first_tile(c, total) <= first_tile(c + 1, total));
+  int parts[kAttnCtas][2] = {};
+  int64_t at = 0;
+  for (int b = 0; b < n_seq; ++b)
+    for (int group = 0; group < g.sh.groups; ++group)
+      for (int run = 0; run < row_runs(g.sh, n[b]); ++run) {
+        const int t = item_tiles(g.sh, n[b], len[b], run);
+        NEED(t >= 1 && slots_seen(g.sh, n[b], len[b], run) <= len[b] + (causal ? n[b] : 0));
+        NEED((int64_t)t * g.sh.tile >= slots_seen(g.sh, n[b], len[b], run));
+        const int c0 = cta_of_tile(at, total), c1 = cta_of_tile(at + t - 1, total);
+        NEED(c0 >= 0 && c1 >= c0 && c1 < kAttnCtas);
+        for (int64_t x = at; x < at + t; ++x) {
+          const int c = cta_of_tile(x, total);
+          NEED(first_tile(c, total) <= x && x < first_tile(c + 1, total));
+        }
+        if (c0 != c1)
+          for (int c = c0; c <= c1; ++c) {
+            if (first_tile(c, total) == first_tile(c + 1, total)) continue;
+            const int kind = at < first_tile(c, total) ? 0 : 1;   // as the computing kernel stores it
+            NEED(kind == (c == c0 ? 1 : 0));                      // as the joining kernel looks for it
+            NEED(++parts[c][kind] == 1);
+          }
+        at += t;
+      }
+  NEED(at == total);
+  return 0;
+}
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    cxx = shutil.which("g++") or shutil.which("c++")
+    out = str(tmp_path_factory.mktemp("plan") / "plan.so")
+    r = subprocess.run([cxx, "-std=c++17", "-O2", "-Wall", "-I" + CSRC, "-x", "c++", "-", "-shared", "-fPIC", "-o", out],
+                       input=_SOURCE, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    assert os.path.exists(out)
+    return C.CDLL(out)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("q4", [0, 1])
+def test_shared_memory(plan, d, q4):
+    for H in range(1, 33):
+        if H * d > 2048 and not q4:
+            continue
+        for rep in (1, 2, 3, 4, 7, 8, 9, 71):
+            for n_seq in (1, 64, 4096):
+                for max_new in (1, 2, 5, 64, 4096):
+                    assert plan.geometry_holds(H, rep, d, q4, n_seq, max_new) == 0, (H, rep, n_seq, max_new)
+
+
+def test_shares(plan):
+    import random
+    rng = random.Random(0)
+    for _ in range(400):
+        H, rep, d, q4 = rng.randint(1, 12), rng.choice([1, 3, 4, 8, 71]), rng.choice([64, 128]), rng.randint(0, 1)
+        n_seq = rng.choice([1, 1, 3, 20, 200])
+        most = rng.choice([1, 1, 4, 40])
+        n = [rng.randint(0 if rng.random() < 0.3 else 1, most) for _ in range(n_seq)]
+        ln = [rng.choice([0, 1, 15, 16, 17, rng.randint(0, 3000)]) for _ in range(n_seq)]
+        causal = rng.randint(0, 1)
+        arr = C.c_int * n_seq
+        assert plan.shares_hold(H, rep, d, q4, max(max(n), 1), causal, n_seq, arr(*n), arr(*ln)) == 0, (H, rep, d, q4, n, ln)
