@@ -8,8 +8,8 @@
 //
 //  - A CTA takes all heads of a group (up to 8) of a run of slots, because a
 //    token's row holds all heads together: whole rows go to shared memory by
-//    bulk copies from one warp, through a ring of tiles (K and V in turn)
-//    deep enough to cover HBM's latency; eight warps compute, one head each
+//    asynchronous copies from warps of their own, through a ring of tiles (K
+//    and V in turn) deep enough to cover HBM's latency; eight warps compute, one head each
 //    (fewer heads: several warps a head, each with its own part of the tile's
 //    slots, joined through shared memory at the end).
 //  - The slots of all entries are one line of tiles that the 152 CTAs share
@@ -29,7 +29,7 @@
 // if the queries follow it), a conversion turns two codes into a half pair,
 // and the product with the E4M3 scale is exact in half precision (2 + 4
 // significant bits).  Queries enter as halves scaled by a power of two per
-// row, probabilities as halves times 2^15 (11 bits from 1 down to 2^-29).  For
+// row, probabilities as halves times 2^7 (11 bits down to 2^-21).  For
 // a bf16 cache the probabilities go in as two bf16 terms (16 bits).
 #include "attn.cuh"
 #include "attn_plan.h"
@@ -37,14 +37,12 @@
 namespace epikv {
 namespace {
 
-constexpr int kThreads = 32 * (kAttnWarps + 1);
+constexpr int threads_of(int d) { return 32 * (attn_group(d) + kAttnCopyWarps); }
 constexpr uint64_t kWaitNs = 2000000000ull;
 using Geometry = AttnGeometry;
 
-// The rows of a 16-slot block in the order that the tensor instruction's rows
-// take them: with rows 32 bytes past a multiple of 128 apart, each load of a
-// quarter or half warp then touches every bank once.
-__device__ __forceinline__ int slot_of_row(int r) { return (0x57463120 >> (4 * r)) & 7; }   // 0 2 1 3 6 4 7 5
+// Row r of the tensor instruction's rows takes this slot of eight (attn_plan.h's AttnGeometry.order).
+__device__ __forceinline__ int slot_of_row(uint32_t order, int r) { return (order >> (4 * r)) & 7; }
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -80,24 +78,40 @@ __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 
+// Words, a 2-byte value or a byte at a shared-memory address.
 template <int kWords>
-__device__ __forceinline__ void lds_words(uint32_t (&w)[kWords], const char* p) {
+__device__ __forceinline__ void lds_words(uint32_t (&w)[kWords], uint32_t p) {
   if constexpr (kWords == 1) {
-    w[0] = *reinterpret_cast<const uint32_t*>(p);
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(p));
   } else if constexpr (kWords == 2) {
-    const uint2 v = *reinterpret_cast<const uint2*>(p);
-    w[0] = v.x; w[1] = v.y;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(p));
   } else {
 #pragma unroll
-    for (int i = 0; i < kWords / 4; ++i) {
-      const uint4 v = reinterpret_cast<const uint4*>(p)[i];
-      w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
-    }
+    for (int i = 0; i < kWords / 4; ++i)
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3]) : "r"(p + 16 * i));
   }
+}
+__device__ __forceinline__ uint32_t lds_u16(uint32_t p) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(p));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds_u8(uint32_t p) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(p));
+  return v;
 }
 
 __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
   const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// Both halves of a times the low or the high half of b.
+template <bool kHigh>
+__device__ __forceinline__ uint32_t hmul2_by(uint32_t a, uint32_t b) {
+  const __half2 s = *reinterpret_cast<const __half2*>(&b);
+  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), kHigh ? __high2half2(s) : __low2half2(s));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
@@ -109,47 +123,59 @@ __device__ __forceinline__ uint32_t bf162_of(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 
-// The walk along a CTA's items, the same in every thread.
+// A warp's walk along its CTA's items, in shared memory: its first lane moves it on, and what the loops over tiles do
+// not need stays out of their registers.  Tiles are counted from the CTA's first.
 struct Walk {
-  const int64_t* pre;
-  const Batch* ba;
-  const AttnDims* dm;
-  const AttnShape* sh;
-  int32_t* err;
-  int b, group, run, tiles;
-  int64_t at;   // the item's first tile
+  int b, group, run, at, tiles;   // the item, its first tile (below 0: an earlier CTA's), its tiles
   Entry e;
+};
+struct Walker {
+  const int64_t* pre;
+  const Batch& ba;
+  const AttnDims& dm;
+  const AttnShape& sh;
+  int32_t* err;
 
-  __device__ __forceinline__ void entry() {
-    group = run = 0;
-    batch_entry(*ba, *dm, b, sh->causal, err, &e);
-    tiles = item_tiles(*sh, e.n, e.len, 0);
+  __device__ __forceinline__ void entry(Walk* w) const {
+    w->group = w->run = 0;
+    Entry e;
+    batch_entry(ba, dm, w->b, sh.causal, err, &e);
+    w->e = e;
+    w->tiles = item_tiles(sh, e.n, e.len, 0);
   }
-  __device__ __forceinline__ void step() {
-    at += tiles;
-    if (++run == row_runs(*sh, e.n)) {
-      run = 0;
-      if (++group == sh->groups) {
-        do ++b;
-        while (b < ba->n_seq && pre[b + 1] == pre[b]);
-        if (b < ba->n_seq) entry();
+  __device__ __forceinline__ void step(Walk* w) const {
+    w->at += w->tiles;
+    if (++w->run == row_runs(sh, w->e.n)) {
+      w->run = 0;
+      if (++w->group == sh.groups) {
+        do ++w->b;
+        while (w->b < ba.n_seq && pre[w->b + 1] == pre[w->b]);
+        if (w->b < ba.n_seq) entry(w);
         return;
       }
     }
-    tiles = item_tiles(*sh, e.n, e.len, run);
+    w->tiles = item_tiles(sh, w->e.n, w->e.len, w->run);
   }
-  // The item that tile x is in (x below the batch's tiles).
-  __device__ __forceinline__ void seek(int64_t x) {
-    int lo = 0, hi = ba->n_seq - 1;   // the last entry that starts at or before x and has tiles
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if (pre[mid + 1] > x) hi = mid;
-      else lo = mid + 1;
+  // The item that tile lo of all is in (there is one).
+  __device__ __forceinline__ void seek(Walk* w, int64_t lo) const {
+    int first = 0, last = ba.n_seq - 1;   // the first entry that ends behind lo
+    while (first < last) {
+      const int mid = (first + last) / 2;
+      if (pre[mid + 1] > lo) last = mid;
+      else first = mid + 1;
     }
-    b = lo;
-    at = pre[b];
-    entry();
-    while (at + tiles <= x) step();
+    w->b = first;
+    w->at = (int)(pre[first] - lo);
+    entry(w);
+    while (w->at + w->tiles <= 0) step(w);
+  }
+  // Moves the warp's walk on to the item of tile i.
+  __device__ __forceinline__ void to(Walk* w, int i, int lane) const {
+    if (i < w->at + w->tiles) return;
+    __syncwarp();
+    if (lane == 0)
+      while (i >= w->at + w->tiles) step(w);
+    __syncwarp();
   }
 };
 
@@ -176,110 +202,267 @@ __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
   asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" :: "r"(smem_u32(bar)) : "memory");
 }
 
-// ------------------------------------------------------------------ the copying warp
-template <int D, int FMT>
-__device__ void copy_tiles(char* smem, uint64_t* full, uint64_t* empty, const Waiter& wait, const AttnState& st,
-                           const AttnDims& dm, const Geometry& ge, const KvDev& kv, int layer, Walk w, int64_t lo,
-                           int64_t hi, int lane) {
+// ------------------------------------------------------------------ the copying warps
+__device__ __forceinline__ void zero_rows(char* dst, int bytes) {
+  for (int i = 0; i < bytes; i += 16) *reinterpret_cast<uint4*>(dst + i) = make_uint4(0, 0, 0, 0);
+}
+
+// A copying warp's instruction chains are what its tiles cost (one warp alone took 2,000 cycles a tile of 18 KB, which
+// is a third of HBM's rate), so the tiles go round four warps; what a tile needs is formed once for K and V, its table
+// entries are read a turn ahead, and quotients go by a float reciprocal (exact: slots are below 2^24, and a quotient
+// that is off by one is put right).
+struct Divider {
+  int d;
+  float inv;
+  __device__ __forceinline__ explicit Divider(int d_) : d(d_), inv(1.f / (float)d_) {}
+  __device__ __forceinline__ int operator()(int n, int* rest) const {
+    int q = (int)((float)n * inv);
+    int r = n - q * d;
+    if (r < 0) {
+      --q;
+      r += d;
+    } else if (r >= d) {
+      ++q;
+      r -= d;
+    }
+    *rest = r;
+    return q;
+  }
+};
+
+struct Place {   // of one slot
+  int entry;     // of the block table (contiguous: 0)
+  int rest;      // slot within the block
+};
+__device__ __forceinline__ Place place_of(const KvDev& kv, const Divider& block, int layer, int seq, int slot) {
+  Place p{0, slot};
+  if (kv.layout == EPIKV_LAYOUT_CONTIGUOUS) return p;
+  const int bi = block(slot, &p.rest);
+  p.entry = bi < kv.max_blocks
+                ? __ldg(kv.block_table + (int64_t)layer * kv.table_stride_layer + (int64_t)seq * kv.max_blocks + bi)
+                : -1;
+  return p;
+}
+// Element offset, or -1.
+__device__ __forceinline__ int64_t offset_of(const KvDev& kv, int layer, int seq, const Place& p) {
+  const int64_t base = (int64_t)layer * kv.stride_layer + (int64_t)p.rest * kv.stride_token;
+  if (kv.layout == EPIKV_LAYOUT_CONTIGUOUS) return base + (int64_t)seq * kv.stride_seq;
+  if (p.entry < 0 || p.entry >= kv.num_blocks) return -1;
+  return base + (int64_t)p.entry * kv.stride_block;
+}
+
+// Tile i of the CTA stands in the ring's place i mod stages, and waits for the computing warps to have left it.
+struct Ring {
+  int stages, place, turn;   // place of the warp's next tile, times round the ring
+  __device__ __forceinline__ Ring(int stages_, int first) : stages(stages_), place(first), turn(0) { wrap(); }
+  __device__ __forceinline__ void wrap() {
+    while (place >= stages) {
+      place -= stages;
+      ++turn;
+    }
+  }
+  __device__ __forceinline__ void on(int n) {
+    place += n;
+    wrap();
+  }
+};
+
+// 4-bit rows: a bulk copy for each run of slots that is one piece of memory (a block's, where its rows stand side by
+// side), each 4 to 18 KB.  A lane looks after one run; where a tile has over 32 (rows that stand apart), the others are
+// looked up as they are copied.
+template <int D>
+__device__ void copy_q4(char* smem, uint64_t* full, uint64_t* empty, const Waiter& wait, const AttnState& st,
+                        const AttnDims& dm, const Geometry& ge, const KvDev& kv, int layer, const Walker& walker,
+                        Walk* w, int tiles, int warp, int lane) {
   const AttnShape& sh = ge.sh;
-  int unit = 0;
-  uint32_t phase = 0;
-  int issued = 0;
-  for (int64_t x = lo; x < hi;) {
-    const int64_t end = w.at + w.tiles < hi ? w.at + w.tiles : hi;
-    const int seen = slots_seen(sh, w.e.n, w.e.len, w.run);
-    const int h0 = w.group * kAttnGroup, heads = min(kAttnGroup, dm.H - h0);
-    // a row's part: one or two runs of bytes
-    int a_off, a_bytes, b_off = 0, b_bytes = 0;
-    if (FMT == EPIKV_CACHE_BF16) {
-      a_off = h0 * D * 2;
-      a_bytes = heads * D * 2;
-    } else if (sh.groups == 1) {
-      a_off = 0;
-      a_bytes = (dm.H * (D / 2 + D / kQuantGroup) + 15) & ~15;
-    } else {
+  const bool side = kv.stride_token * 2 == ge.row_s && sh.groups == 1;
+  const bool flat = kv.layout == EPIKV_LAYOUT_CONTIGUOUS;
+  const int rl = !side ? 1 : flat ? 1 << 24 : kv.block_size;   // slots of a run
+  const Divider block(flat ? 1 : kv.block_size), runs_of(rl);
+  Ring ring(ge.stages, warp);
+  int seq = 0, s0 = 0, n = 0, h0 = 0, run0 = 0, at = 0, upto = 0;
+  Place next{0, 0};
+  // run k of the tile: slots at .. upto - 1
+  auto run_of = [&](int k, int* a, int* u) {
+    const int64_t begin = (int64_t)(run0 + k) * rl;
+    *a = (int)max((int64_t)s0, min(begin, (int64_t)s0 + n));
+    *u = (int)min(begin + rl, (int64_t)s0 + n);
+  };
+  auto look = [&](int x) {
+    walker.to(w, x, lane);
+    seq = w->e.seq;
+    s0 = (x - w->at) * sh.tile;
+    n = max(min(sh.tile, slots_seen(sh, w->e.n, w->e.len, w->run) - s0), 0);
+    h0 = w->group * attn_group(D);
+    int rest;
+    run0 = runs_of(s0, &rest);
+    run_of(lane, &at, &upto);
+    if (at < upto) next = place_of(kv, block, layer, seq, at);
+  };
+  int x = warp;
+  if (x < tiles) look(x);
+  for (; x < tiles; x += ge.copiers) {
+    const int rows = max(upto - at, 0), row0 = at - s0, n_now = n, seq_now = seq, s_now = s0;
+    const int64_t off = rows ? offset_of(kv, layer, seq, next) : -1;
+    if (rows && off < 0) set_error(st.err, EPIKV_DEV_SLOT);
+    int there = off >= 0 ? rows : 0;
+    const int more = max(n_now - 32 * rl, 0);     // slots behind the lanes' runs: runs of one slot, n <= 128
+    for (int r = n_now - more + lane; r < n_now; r += 32) {
+      const bool in = offset_of(kv, layer, seq, place_of(kv, block, layer, seq, s0 + r)) >= 0;
+      there += in;
+      if (!in) set_error(st.err, EPIKV_DEV_SLOT);
+    }
+    there = __reduce_add_sync(0xffffffffu, there);
+    int a_off = 0, a_bytes = ge.row_s, b_off = 0, b_bytes = 0;   // of a row: one piece, or codes and scales
+    if (!side) {
+      const int heads = min(attn_group(D), dm.H - h0);
       a_off = h0 * (D / 2);
       a_bytes = heads * (D / 2);
       b_off = scale_offset(dm, h0);
       b_bytes = (heads * (D / kQuantGroup) + 15) & ~15;
     }
-    for (; x < end; ++x) {
-      const int s0 = (int)(x - w.at) * sh.tile;
-      int64_t off[kRowsPerLane];
-      int rows = 0;
-      bool hole = false;
-#pragma unroll
-      for (int k = 0; k < kRowsPerLane; ++k) {
-        const int r = lane + 32 * k;
-        off[k] = -1;
-        if (r < sh.tile && s0 + r < seen) {
-          off[k] = kv_row_offset(kv, layer, w.e.seq, s0 + r, dm.T);
-          if (off[k] < 0) set_error(st.err, EPIKV_DEV_SLOT);
+    if (x + ge.copiers < tiles) look(x + ge.copiers);
+    uint64_t* bar = &full[ring.place];
+    char* dst = smem + ring.place * (2 * ge.half_bytes);
+    if (ring.turn) wait(&empty[ring.place], (ring.turn & 1) ^ 1);
+    if (there < sh.tile) {  // rows that nothing fills: a probability of 0 must not meet what stood there before
+      char* values = dst + ge.half_bytes;
+      for (int r = n_now + lane; r < sh.tile; r += 32) zero_rows(values + r * ge.row_s, ge.row_s);
+      if (off < 0)
+        for (int r = 0; r < rows; ++r) {
+          zero_rows(dst + (row0 + r) * ge.row_s, ge.row_s);
+          zero_rows(values + (row0 + r) * ge.row_s, ge.row_s);
         }
-        hole |= r < sh.tile && off[k] < 0;
-        rows += __popc(__ballot_sync(0xffffffffu, off[k] >= 0));
+      for (int r = n_now - more + lane; r < n_now; r += 32)
+        if (offset_of(kv, layer, seq_now, place_of(kv, block, layer, seq_now, s_now + r)) < 0) {
+          zero_rows(dst + r * ge.row_s, ge.row_s);
+          zero_rows(values + r * ge.row_s, ge.row_s);
+        }
+      fence_proxy_async_smem();
+      __syncwarp();
+    }
+    if (lane == 0) mbar_arrive_expect_tx(bar, 2 * there * (a_bytes + b_bytes));
+    __syncwarp();
+    auto copy = [&](int row, int64_t o, int n_rows) {
+      char* d = dst + row * ge.row_s;
+      const char* k = kv.base[0] + o * 2;
+      const char* v = kv.base[1] + o * 2;
+      tma_load_1d(d, k + a_off, n_rows * a_bytes, bar);
+      tma_load_1d(d + ge.half_bytes, v + a_off, n_rows * a_bytes, bar);
+      if (b_bytes) {   // single rows
+        tma_load_1d(d + a_bytes, k + b_off, b_bytes, bar);
+        tma_load_1d(d + ge.half_bytes + a_bytes, v + b_off, b_bytes, bar);
       }
-      hole = __any_sync(0xffffffffu, hole);
+    };
+    if (off >= 0) copy(row0, off, rows);
+    for (int r = n_now - more + lane; r < n_now; r += 32) {
+      const int64_t o = offset_of(kv, layer, seq_now, place_of(kv, block, layer, seq_now, s_now + r));
+      if (o >= 0) copy(r, o, 1);
+    }
+    ring.on(ge.copiers);
+  }
+  if (*wait.gave_up) {   // the CTA may not end before its copies have landed: this warp's last ones
+    for (int j = tiles - 1; j >= 0 && j >= tiles - ge.stages; --j)
+      if (j % ge.copiers == warp) mbar_wait_bounded(&full[j % ge.stages], (uint32_t)(j / ge.stages) & 1, kWaitNs);
+  }
+}
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+// bf16 rows: 16 bytes a lane, into rows 16 bytes past a multiple of 128 apart (rows as they stand would put eight of
+// them on the same banks).  Lane i reads the table entries of rows i, i + 32, ...
+template <int D>
+__device__ void copy_bf16(char* smem, uint64_t* full, uint64_t* empty, const Waiter& wait, const AttnState& st,
+                          const AttnDims& dm, const Geometry& ge, const KvDev& kv, int layer, const Walker& walker,
+                          Walk* w, int tiles, int warp, int lane) {
+  const AttnShape& sh = ge.sh;
+  constexpr int kMost = kMaxTile / 32;
+  const Divider block(kv.layout == EPIKV_LAYOUT_CONTIGUOUS ? 1 : kv.block_size);
+  Ring ring(ge.stages, warp);
+  int group = -1, pieces = 0, at_once = 1, sub = 0, col = 0;   // 16-byte pieces of a row; rows taken at once
+  int seq = 0, n = 0, next_group = 0;
+  Place next[kMost];
+  auto look = [&](int x) {
+    walker.to(w, x, lane);
+    const int s0 = (x - w->at) * sh.tile;
+    seq = w->e.seq;
+    n = min(sh.tile, slots_seen(sh, w->e.n, w->e.len, w->run) - s0);
+    next_group = w->group;
 #pragma unroll
-      for (int which = 0; which < 2; ++which) {
-        if (issued >= ge.units) wait(&empty[unit], phase ^ 1);
-        char* dst = smem + unit * ge.unit_bytes;
-        if (hole) {  // rows that nothing fills: a probability of 0 must not meet what stood there before
+    for (int k = 0; k < kMost; ++k)
+      if (lane + 32 * k < n) next[k] = place_of(kv, block, layer, seq, s0 + lane + 32 * k);
+  };
+  int x = warp;
+  if (x < tiles) look(x);
+  for (; x < tiles; x += ge.copiers) {
+    if (next_group != group) {
+      group = next_group;
+      pieces = min(attn_group(D), dm.H - group * attn_group(D)) * (D / 8);
+      at_once = pieces < 32 ? 32 / pieces : 1;
+      sub = pieces < 32 ? lane / pieces : 0;
+      col = pieces < 32 ? lane % pieces : lane;
+    }
+    int64_t from[kMost];   // byte offsets, -1: a row that is not there, which is filled with zeros
 #pragma unroll
-          for (int k = 0; k < kRowsPerLane; ++k) {
-            const int r = lane + 32 * k;
-            if (r < sh.tile && off[k] < 0)
-              for (int i = 0; i < ge.row_s; i += 16) *reinterpret_cast<uint4*>(dst + r * ge.row_s + i) = make_uint4(0, 0, 0, 0);
+    for (int k = 0; k < kMost; ++k) {
+      from[k] = -1;
+      if (lane + 32 * k < n) {
+        const int64_t off = offset_of(kv, layer, seq, next[k]);
+        if (off < 0) set_error(st.err, EPIKV_DEV_SLOT);
+        else from[k] = off * 2;
+      }
+    }
+    if (x + ge.copiers < tiles) look(x + ge.copiers);
+    if (ring.turn) wait(&empty[ring.place], (ring.turn & 1) ^ 1);
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+      const uint32_t dst = smem_u32(smem) + (2 * ring.place + which) * ge.half_bytes + col * 16;
+      const char* base = kv.base[which] + group * (attn_group(D) * D * 2) + col * 16;
+#pragma unroll
+      for (int k = 0; k < kMost; ++k) {
+        const int end = min(sh.tile - 32 * k, 32);
+#pragma unroll 4
+        for (int i = 0; i < end; i += at_once) {
+          const int row = i + sub;
+          const int64_t o = __shfl_sync(0xffffffffu, from[k], row & 31);
+          const char* s = base + (o < 0 ? 0 : o);
+          const int take = o < 0 ? 0 : 16;
+          const uint32_t d = dst + (32 * k + row) * ge.row_s;
+          if (sub < at_once && row < end) {
+            if (col < pieces) cp_async16(d, s, take);
+#pragma unroll
+            for (int c = 1; c < attn_group(D) * D / 8 / 32; ++c)
+              if (col + 32 * c < pieces) cp_async16(d + 512 * c, s + 512 * c, take);
           }
-          fence_proxy_async_smem();
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive_expect_tx(&full[unit], rows * (a_bytes + b_bytes));
-        __syncwarp();
-        const char* base = kv.base[which];
-#pragma unroll
-        for (int k = 0; k < kRowsPerLane; ++k) {
-          if (off[k] >= 0) {
-            char* d = dst + (lane + 32 * k) * ge.row_s;
-            const char* s = base + off[k] * 2;
-            tma_load_1d(d, s + a_off, a_bytes, &full[unit]);
-            if (b_bytes) tma_load_1d(d + a_bytes, s + b_off, b_bytes, &full[unit]);
-          }
-        }
-        ++issued;
-        if (++unit == ge.units) {
-          unit = 0;
-          phase ^= 1;
         }
       }
     }
-    w.step();
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" :: "r"(smem_u32(&full[ring.place])) : "memory");
+    ring.on(ge.copiers);
   }
-  if (*wait.gave_up) {  // the CTA may not end before its copies have landed
-    for (int u = 0; u < ge.units && u < issued; ++u) {
-      const uint32_t parity = u < unit ? phase : phase ^ 1;
-      mbar_wait_bounded(&full[u], parity, kWaitNs);
-    }
-  }
+  asm volatile("cp.async.wait_all;" ::: "memory");   // the CTA may not end before its copies have landed
 }
 
 // ------------------------------------------------------------------ the computing warps
 // SUB: 16-slot blocks of a tile that a warp takes; NT: 8-row blocks of queries.
 template <int D, int FMT, int NT, int SUB>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(threads_of(D), 1)
     attention_kernel(AttnState st, AttnDims dm, Geometry ge, int layer, Batch ba, Rows q, Rows out, float* lse,
                      KvDev kv, float scale_log2) {
+  constexpr int kWarps = attn_group(D), kThreads = threads_of(D);
   extern __shared__ __align__(128) char smem[];
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + ge.bar_off);
-  uint64_t* empty = full + kMaxUnits;
-  int* gave_up = reinterpret_cast<int*>(empty + kMaxUnits);
+  uint64_t* empty = full + kMaxStages;
+  int* gave_up = reinterpret_cast<int*>(empty + kMaxStages);
   int64_t* pre = reinterpret_cast<int64_t*>(smem + ge.pre_off);
-  __shared__ int64_t s_warp[kAttnWarps];
+  __shared__ int64_t s_warp[8];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const AttnShape& sh = ge.sh;
 
   // tiles before each entry
-  if (tid < 2 * kMaxUnits) mbar_init(&full[tid], tid < kMaxUnits ? 1 : kAttnWarps);
+  if (tid < 2 * kMaxStages) mbar_init(&full[tid], tid >= kMaxStages ? kWarps : FMT == EPIKV_CACHE_BF16 ? 32 : 1);
   if (tid == 0) *gave_up = 0;
   const int per = (ba.n_seq + 255) / 256;
   int64_t mine = 0;
@@ -300,7 +483,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int64_t v = __shfl_up_sync(0xffffffffu, run, o);
     if (lane >= o) run += v;
   }
-  if (lane == 31 && warp < kAttnWarps) s_warp[warp] = run;
+  if (lane == 31 && warp < 8) s_warp[warp] = run;
   if (tid == 0) fence_barrier_init();
   __syncthreads();
   if (tid < 256) {
@@ -319,34 +502,61 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int64_t total = pre[ba.n_seq];
   const int64_t lo = first_tile(blockIdx.x, total), hi = first_tile(blockIdx.x + 1, total);
   if (lo == hi) return;
-  Walk w{pre, &ba, &dm, &sh, st.err};
-  w.seek(lo);
+  __shared__ Walk s_walk[kWarps + kAttnCopyWarps];
+  Walk* w = &s_walk[warp];
+  const Walker walker{pre, ba, dm, sh, st.err};
+  if (lane == 0) walker.seek(w, lo);
+  __syncwarp();
+  const int tiles = (int)(hi - lo);
   const Waiter wait{gave_up, st.err};
-  if (warp == kAttnWarps) {
-    copy_tiles<D, FMT>(smem, full, empty, wait, st, dm, ge, kv, layer, w, lo, hi, lane);
+  if (warp >= kWarps) {
+    if (warp - kWarps >= ge.copiers) return;
+    if constexpr (FMT == EPIKV_CACHE_BF16)
+      copy_bf16<D>(smem, full, empty, wait, st, dm, ge, kv, layer, walker, w, tiles, warp - kWarps, lane);
+    else
+      copy_q4<D>(smem, full, empty, wait, st, dm, ge, kv, layer, walker, w, tiles, warp - kWarps, lane);
     return;
   }
 
   constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
   constexpr int KS = D / 16;                 // blocks of 16 channels
-  constexpr float kUp = kBf16 ? 0.f : 15.f;  // probabilities are held times 2^kUp
+  // probabilities are held times 2^kUp: as halves they reach from 2^-14 (2^-24 with fewer bits) to 2^16, and may pass the
+  // maximum that they are taken against by 2^kSlack
+  constexpr float kUp = kBf16 ? 0.f : 7.f, kSlack = 8.f;
   const int g = lane >> 2, t = lane & 3;
-  int unit = 0;
+  int stage = 0;
   uint32_t phase = 0;
-  for (int64_t x = lo; x < hi;) {
-    const int64_t end = w.at + w.tiles < hi ? w.at + w.tiles : hi;
-    const Entry e = w.e;
-    const int h0 = w.group * kAttnGroup, heads = min(kAttnGroup, dm.H - h0);
-    const int teams = kAttnWarps / heads;    // warps of a head: 8, 4, 2 or 1
+  for (int x = 0; x < tiles;) {
+    walker.to(w, x, lane);
+    const Entry e = w->e;
+    const int h0 = w->group * attn_group(D), heads = min(attn_group(D), dm.H - h0);
+    const int teams = attn_teams(heads, kWarps);
     const bool idle = warp >= teams * heads;
     const int head = warp % heads, team = warp / heads;
     const int kh = h0 + head;
-    const int row0 = w.run * sh.rows, nrows = min(sh.rows, rows_of(sh, e.n) - row0);
+    const int row0 = w->run * sh.rows, nrows = min(sh.rows, rows_of(sh, e.n) - row0);
+
+    // where the lane reads in a tile: keys are rows (slots), values columns of the first operand
+    const uint32_t ring0 = smem_u32(smem);
+    const uint32_t hop = teams * 16 * ge.row_s, eight = 8 * ge.row_s;   // to the warp's next block of slots; 8 slots on
+    const int k0 = kBf16 ? 2 * t : slot_of_row(ge.order, 2 * t), k1 = kBf16 ? 2 * t + 1 : slot_of_row(ge.order, 2 * t + 1);
+    uint32_t key_code, key_scale = 0, value_code, value_scale = 0, odd = 0;
+    if constexpr (kBf16) {
+      key_code = (team * 16 + (lane & 15)) * ge.row_s + head * (D * 2) + (lane >> 4) * 16;
+      value_code = ge.half_bytes + (team * 16 + (lane & 7) + (lane >> 4) * 8) * ge.row_s + head * (D * 2) + ((lane >> 3) & 1) * 16;
+    } else {
+      const uint32_t key_row = (team * 16 + slot_of_row(ge.order, g)) * ge.row_s;
+      const uint32_t value_row = (team * 16 + k0) * ge.row_s, scales = heads * (D / 2) + head * (D / 16);
+      key_code = key_row + head * (D / 2) + t * (D / 8);
+      key_scale = key_row + scales + t * (D / 64);
+      value_code = ge.half_bytes + value_row + head * (D / 2) + g * (D / 16);
+      value_scale = ge.half_bytes + value_row + scales + g * (D / 8) / 16;
+      odd = (k1 - k0) * ge.row_s;
+    }
 
     // the queries as the second operand: column n of block nt is row nt * 8 + n
     uint32_t qf[NT][KS][2];
     float cf[NT][2];       // what turns a raw score into log2 units, per column 2t and 2t + 1
-    int lim[NT][2];        // slots that the columns' rows see
     const float gk = kBf16 ? scale_log2 : scale_log2 * head_scale(st, dm, 0, layer, kh);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -387,9 +597,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        const int col = nt * 8 + 2 * t + c;
         cf[nt][c] = gk * __shfl_sync(0xffffffffu, mul, (2 * t + c) * 4);
-        lim[nt][c] = col < nrows ? e.len + (sh.causal ? (row0 + col) / sh.rep + 1 : 0) : 0;
       }
     }
     const int least = e.len + (sh.causal ? row0 / sh.rep + 1 : 0);   // slots that every row of the item sees
@@ -405,13 +613,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = 0; i < 4; ++i) o[j][nt][i] = 0.f;
     }
 
-    for (; x < end; ++x) {
-      const int s0 = (int)(x - w.at) * sh.tile;
+    const int end = min(w->at + w->tiles, tiles);
+    int s0 = (x - w->at) * sh.tile;
+    for (; x < end; ++x, s0 += sh.tile) {
       // ---- scores
       float s[SUB][NT][4];
-      wait(&full[unit], phase);
+      wait(&full[stage], phase);
+      const uint32_t base = ring0 + stage * (2 * ge.half_bytes);
       {
-        const char* tile = smem + unit * ge.unit_bytes;
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
           const int sub = u * teams + team;
@@ -421,7 +630,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int i = 0; i < 4; ++i) s[u][nt][i] = 0.f;
           if (idle || sub * 16 >= sh.tile) continue;
           if constexpr (kBf16) {
-            const uint32_t addr = smem_u32(tile) + (sub * 16 + (lane & 15)) * ge.row_s + head * (D * 2) + (lane >> 4) * 16;
+            const uint32_t addr = base + u * hop + key_code;
 #pragma unroll
             for (int j = 0; j < KS; ++j) {
               uint32_t a[4];
@@ -430,80 +639,127 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int nt = 0; nt < NT; ++nt) mma<FMT>(s[u][nt], a, qf[nt][j][0], qf[nt][j][1]);
             }
           } else {
-            const char* r0 = tile + (sub * 16 + slot_of_row(g)) * ge.row_s;
-            const char* r1 = r0 + 8 * ge.row_s;
+            const uint32_t at = base + u * hop;
             uint32_t w0[D / 32], w1[D / 32];
-            lds_words(w0, r0 + head * (D / 2) + t * (D / 8));
-            lds_words(w1, r1 + head * (D / 2) + t * (D / 8));
-            const int so = heads * (D / 2) + head * (D / 16) + t * (D / 64);
+            lds_words(w0, at + key_code);
+            lds_words(w1, at + key_code + eight);
+            uint32_t s0x[D / 128 + 1], s1x[D / 128 + 1];   // the scales, two a register
+            if constexpr (D == 64) {
+              s0x[0] = e4m3x2_to_half2((uint16_t)lds_u8(at + key_scale));
+              s1x[0] = e4m3x2_to_half2((uint16_t)lds_u8(at + key_scale + eight));
+            } else {
 #pragma unroll
-            for (int p = 0; p < D / 64; ++p) {   // 16 channels that share a scale
-              const uint32_t b0 = (uint8_t)r0[so + p], b1 = (uint8_t)r1[so + p];
-              const uint32_t sc = e4m3x2_to_half2((uint16_t)(b0 | b1 << 8));
-              const uint32_t sc0 = __byte_perm(sc, sc, 0x1010), sc1 = __byte_perm(sc, sc, 0x3232);
+              for (int p = 0; p < D / 128; ++p) {
+                s0x[p] = e4m3x2_to_half2((uint16_t)lds_u16(at + key_scale + 2 * p));
+                s1x[p] = e4m3x2_to_half2((uint16_t)lds_u16(at + key_scale + eight + 2 * p));
+              }
+            }
+            float two[NT][4];   // a second chain of sums, half the first one's latencies
 #pragma unroll
-              for (int v = 0; v < 2; ++v) {
-                uint32_t x0[4], x1[4];
-                e2m1x8_to_half2(w0[2 * p + v], x0);
-                e2m1x8_to_half2(w1[2 * p + v], x1);
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                  const uint32_t a[4] = {hmul2(x0[2 * y], sc0), hmul2(x1[2 * y], sc1), hmul2(x0[2 * y + 1], sc0),
-                                         hmul2(x1[2 * y + 1], sc1)};
-                  const int j = 4 * p + 2 * v + y;
+              for (int i = 0; i < 4; ++i) two[nt][i] = 0.f;
 #pragma unroll
-                  for (int nt = 0; nt < NT; ++nt) mma<FMT>(s[u][nt], a, qf[nt][j][0], qf[nt][j][1]);
+            for (int v = 0; v < D / 32; ++v) {   // eight channels of a lane: two blocks
+              uint32_t x0[4], x1[4];
+              e2m1x8_to_half2(w0[v], x0);
+              e2m1x8_to_half2(w1[v], x1);
+#pragma unroll
+              for (int y = 0; y < 2; ++y) {
+                uint32_t a[4];
+                if ((v / 2) % 2 == 0) {
+                  a[0] = hmul2_by<false>(x0[2 * y], s0x[v / 4]);
+                  a[1] = hmul2_by<false>(x1[2 * y], s1x[v / 4]);
+                  a[2] = hmul2_by<false>(x0[2 * y + 1], s0x[v / 4]);
+                  a[3] = hmul2_by<false>(x1[2 * y + 1], s1x[v / 4]);
+                } else {
+                  a[0] = hmul2_by<true>(x0[2 * y], s0x[v / 4]);
+                  a[1] = hmul2_by<true>(x1[2 * y], s1x[v / 4]);
+                  a[2] = hmul2_by<true>(x0[2 * y + 1], s0x[v / 4]);
+                  a[3] = hmul2_by<true>(x1[2 * y + 1], s1x[v / 4]);
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                  if (y == 1) mma<FMT>(two[nt], a, qf[nt][2 * v + y][0], qf[nt][2 * v + y][1]);
+                  else
+                  mma<FMT>(s[u][nt], a, qf[nt][2 * v + y][0], qf[nt][2 * v + y][1]);
                 }
               }
             }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) s[u][nt][i] += two[nt][i];
           }
         }
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&empty[unit]);
-      if (++unit == ge.units) {
-        unit = 0;
-        phase ^= 1;
       }
 
-      // ---- probabilities
-      const bool edge = s0 + sh.tile > least;
-      uint32_t pb[SUB][NT][kBf16 ? 4 : 2];
-      float alpha[NT][2];
-      bool moved = false;
+      // ---- probabilities.  They are taken against a maximum that is moved only when a score passes it by 2^kSlack: the
+      // sums and outputs then need no rescaling, and the warp no exchange, in nearly every tile.
+      if (s0 + sh.tile > least || idle || SUB * teams * 16 > sh.tile) {
+        const int first_row = w->run * sh.rows, last_row = min(first_row + sh.rows, rows_of(sh, w->e.n));
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float top[2] = {-INFINITY, -INFINITY};
+        for (int nt = 0; nt < NT; ++nt) {
+          int lim[2];   // slots that the columns' rows see
 #pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-          const int sub = u * teams + team;
-          const int at = s0 + sub * 16 + (kBf16 ? g : slot_of_row(g));
-          const bool in = !idle && sub * 16 < sh.tile;
+          for (int c = 0; c < 2; ++c) {
+            const int r = first_row + nt * 8 + 2 * t + c;
+            lim[c] = r < last_row ? w->e.len + (sh.causal ? r / sh.rep + 1 : 0) : 0;
+          }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float v = s[u][nt][i] * cf[nt][i & 1];
-            if (!in || (edge && at + (i >> 1) * 8 >= lim[nt][i & 1])) v = -INFINITY;
-            s[u][nt][i] = v;
-            top[i & 1] = fmaxf(top[i & 1], v);
+          for (int u = 0; u < SUB; ++u) {
+            const int sub = u * teams + team;
+            const int at = s0 + sub * 16 + (kBf16 ? g : slot_of_row(ge.order, g));
+            const bool in = !idle && sub * 16 < sh.tile;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (!in || at + (i >> 1) * 8 >= lim[i & 1]) s[u][nt][i] = -INFINITY;
           }
         }
+      }
+      float top[NT][2];
+      bool past = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 4));
-          top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 8));
-          top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], 16));
-          const float mn = fmaxf(m[nt][c], top[c]), base = mn == -INFINITY ? 0.f : mn;
-          alpha[nt][c] = ex2(m[nt][c] - base);
-          moved |= mn != m[nt][c];
-          m[nt][c] = mn;
-          l[nt][c] *= alpha[nt][c];
-          top[c] = base - kUp;
+          top[nt][c] = -INFINITY;
+#pragma unroll
+          for (int u = 0; u < SUB; ++u) top[nt][c] = fmaxf(top[nt][c], fmaxf(s[u][nt][c], s[u][nt][2 + c]));
+          past |= top[nt][c] * cf[nt][c] > m[nt][c] + kSlack;
         }
+      if (__any_sync(0xffffffffu, past)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float alpha[2];
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float v = top[nt][c];
+            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+            const float mn = fmaxf(m[nt][c], v * cf[nt][c]);
+            alpha[c] = mn == -INFINITY ? 1.f : ex2(m[nt][c] - mn);
+            m[nt][c] = mn;
+            l[nt][c] *= alpha[c];
+          }
+#pragma unroll
+          for (int j = 0; j < KS; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[j][nt][i] *= alpha[i & 1];
+        }
+      }
+      uint32_t pb[SUB][NT][kBf16 ? 4 : 2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float add[2];   // a row without a score so far: against 0
+#pragma unroll
+        for (int c = 0; c < 2; ++c) add[c] = kUp - (m[nt][c] == -INFINITY ? 0.f : m[nt][c]);
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            s[u][nt][i] = ex2(s[u][nt][i] - top[i & 1]);
+            s[u][nt][i] = ex2(fmaf(s[u][nt][i], cf[nt][i & 1], add[i & 1]));
             l[nt][i & 1] += s[u][nt][i];
           }
 #pragma unroll
@@ -518,31 +774,18 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       }
-      if (__any_sync(0xffffffffu, moved)) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int j = 0; j < KS; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[j][nt][i] *= alpha[nt][i & 1];
-      }
 
       // ---- their sum of values
-      wait(&full[unit], phase);
       {
-        const char* tile = smem + unit * ge.unit_bytes;
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
           const int sub = u * teams + team;
           if (idle || sub * 16 >= sh.tile) continue;
           const int at = s0 + sub * 16;
-          // the slots of this lane's operand elements: k = 2t, 2t + 1 (and those + 8)
-          const int k0 = kBf16 ? 2 * t : slot_of_row(2 * t), k1 = kBf16 ? 2 * t + 1 : slot_of_row(2 * t + 1);
-          // Gives block mt of the operand (channels x slots) to f, for every mt.
+          // Gives block mt of the operand (channels x slots; the lane's slots are k0, k1 and 8 on) to f, for every mt.
           auto each = [&](auto&& f) {
             if constexpr (kBf16) {
-              const uint32_t addr = smem_u32(tile) + (sub * 16 + (lane & 7) + (lane >> 4) * 8) * ge.row_s +
-                                    head * (D * 2) + ((lane >> 3) & 1) * 16;
+              const uint32_t addr = base + u * hop + value_code;
 #pragma unroll
               for (int mt = 0; mt < KS; ++mt) {
                 uint32_t a[4];
@@ -550,22 +793,19 @@ __global__ void __launch_bounds__(kThreads, 1)
                 f(mt, a);
               }
             } else {
-              const char* base = tile + sub * 16 * ge.row_s;
-              const char* p0 = base + k0 * ge.row_s;
-              const char* p1 = base + k1 * ge.row_s;
-              const int co = head * (D / 2) + g * (D / 16), so = heads * (D / 2) + head * (D / 16) + g * (D / 8) / 16;
+              const uint32_t p0 = base + u * hop + value_code, p1 = p0 + odd;
+              const uint32_t c0 = base + u * hop + value_scale, c1 = c0 + odd;
               uint32_t wa[D / 64], wb[D / 64], wc[D / 64], wd[D / 64];
-              lds_words(wa, p0 + co);
-              lds_words(wb, p1 + co);
-              lds_words(wc, p0 + 8 * ge.row_s + co);
-              lds_words(wd, p1 + 8 * ge.row_s + co);
+              lds_words(wa, p0);
+              lds_words(wb, p1);
+              lds_words(wc, p0 + eight);
+              lds_words(wd, p1 + eight);
               uint32_t sl = 0, sh8 = 0;
 #pragma unroll
               for (int v = 0; v < D / 64; ++v) {   // eight channels: four blocks
                 if (v % 2 == 0) {
-                  const int o2 = so + v / 2;
-                  sl = e4m3x2_to_half2((uint16_t)((uint8_t)p0[o2] | (uint32_t)(uint8_t)p1[o2] << 8));
-                  sh8 = e4m3x2_to_half2((uint16_t)((uint8_t)p0[8 * ge.row_s + o2] | (uint32_t)(uint8_t)p1[8 * ge.row_s + o2] << 8));
+                  sl = e4m3x2_to_half2((uint16_t)(lds_u8(c0 + v / 2) + (lds_u8(c1 + v / 2) << 8)));
+                  sh8 = e4m3x2_to_half2((uint16_t)(lds_u8(c0 + eight + v / 2) + (lds_u8(c1 + eight + v / 2) << 8)));
                 }
                 // pairs of slots instead of pairs of channels: even channels, odd channels
                 constexpr uint32_t kLow = 0x0f0f0f0fu;
@@ -603,9 +843,9 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
             });
           } else {
-            const int last = (row0 + nrows - 1) / sh.rep;
-            for (int i = row0 / sh.rep; i <= last; ++i) {
-              const int n = e.len + (sh.causal ? i + 1 : 0) - at;   // of these slots, those that token i sees
+            const int first_row = w->run * sh.rows, last_row = min(first_row + sh.rows, rows_of(sh, w->e.n)) - 1;
+            for (int i = first_row / sh.rep; i <= last_row / sh.rep; ++i) {
+              const int n = w->e.len + (sh.causal ? i + 1 : 0) - at;   // of these slots, those that token i sees
               const uint32_t m0 = (k0 < n ? 0xffffu : 0u) | (k1 < n ? 0xffff0000u : 0u);
               const uint32_t m8 = (k0 + 8 < n ? 0xffffu : 0u) | (k1 + 8 < n ? 0xffff0000u : 0u);
               each([&](int mt, uint32_t (&a)[4]) {
@@ -620,7 +860,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                   if constexpr (kBf16) mma<FMT>(o[mt][nt], z, pb[u][nt][2], pb[u][nt][3]);
 #pragma unroll
                   for (int y = 0; y < 4; ++y)
-                    if ((row0 + nt * 8 + 2 * t + (y & 1)) / sh.rep != i) o[mt][nt][y] = keep[y];
+                    if ((first_row + nt * 8 + 2 * t + (y & 1)) / sh.rep != i) o[mt][nt][y] = keep[y];
                 }
               });
             }
@@ -628,9 +868,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(&empty[unit]);
-      if (++unit == ge.units) {
-        unit = 0;
+      if (lane == 0) mbar_arrive(&empty[stage]);
+      if (++stage == ge.stages) {
+        stage = 0;
         phase ^= 1;
       }
     }
@@ -648,7 +888,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int step = teams / 2; step > 0; step >>= 1) {
       float* box = reinterpret_cast<float*>(smem + ge.join_off);
       constexpr int kBox = attn_box_floats(D, NT);
-      asm volatile("bar.sync 1, 256;" ::: "memory");
+      asm volatile("bar.sync 1, %0;" :: "n"(32 * kWarps) : "memory");
       if (!idle && team >= step && team < 2 * step) {
         float* mineb = box + ((team - step) * heads + head) * kBox + lane;
 #pragma unroll
@@ -664,7 +904,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       }
-      asm volatile("bar.sync 1, 256;" ::: "memory");
+      asm volatile("bar.sync 1, %0;" :: "n"(32 * kWarps) : "memory");
       if (!idle && team < step) {
         const float* from = box + (team * heads + head) * kBox + lane;
 #pragma unroll
@@ -688,8 +928,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
     if (!idle && team == 0) {
-      const bool whole = x == w.at + w.tiles && x - w.tiles >= lo;
-      const bool inside = w.at < lo;   // the item began in an earlier CTA
+      const bool inside = w->at < 0;   // the item began in an earlier CTA
+      const bool whole = !inside && x == w->at + w->tiles;
+      const Entry e = w->e;
+      const int row0 = w->run * sh.rows, nrows = min(sh.rows, rows_of(sh, e.n) - row0);
+      const int kh = w->group * attn_group(D) + head;
       const float gv = kBf16 ? 1.f : head_scale(st, dm, 1, layer, kh);
       float* part = st.part + (int64_t)(blockIdx.x * 2 + (inside ? 0 : 1)) * ge.slot_floats;
 #pragma unroll
@@ -726,7 +969,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           if (g == 0) {
             if (!whole) {
-              *reinterpret_cast<float2*>(part + kAttnGroup * sh.rows * D + (head * sh.rows + row) * 2) =
+              *reinterpret_cast<float2*>(part + attn_group(D) * sh.rows * D + (head * sh.rows + row) * 2) =
                   make_float2(m[nt][c] - kUp, l[nt][c]);
             } else if (lse) {
               lse[token * dm.Hq + hq] = l[nt][c] == 0.f ? -INFINITY : (m[nt][c] - kUp + log2f(l[nt][c])) * 0.69314718055994531f;
@@ -734,92 +977,96 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
     }
-    w.step();
   }
 }
 
 // ------------------------------------------------------------------ joining the parts of an item
 constexpr int kJoinThreads = 256;
 
-// One block an item's KV head: the CTAs that worked on the item left their maxima, sums and unscaled outputs; threads
-// take four channels of a row each and, where rows are few, a share of the parts.
+// One block a row of an item's KV head.  The parts' weights 2^(m_i - max) come first, all parts at once; then each
+// thread adds up four channels of a share of the parts, and the shares are added in order.
 __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(AttnState st, AttnDims dm, Geometry ge, Batch ba,
                                                                       Rows out, float* lse) {
-  __shared__ float s_acc[kJoinThreads][6];
+  __shared__ int s_slot[kAttnCtas];
+  __shared__ float s_w[kAttnCtas], s_red[2][kJoinThreads / 32];
+  __shared__ float4 s_acc[kJoinThreads];
   const AttnShape& sh = ge.sh;
-  const int b = blockIdx.y, kh = blockIdx.x % dm.H, run = blockIdx.x / dm.H;
+  const int b = blockIdx.y, kh = blockIdx.x % dm.H, r = blockIdx.x / dm.H, run = r / sh.rows, row = r % sh.rows;
+  const int tid = threadIdx.x;
   pdl_wait();
-  const int64_t p0 = st.plan[b], p1 = st.plan[b + 1];
+  const int64_t p0 = st.plan[b], p1 = st.plan[b + 1], total = st.plan[ba.n_seq];
   if (p0 == p1) return;
-  const int64_t total = st.plan[ba.n_seq];
   Entry e;
-  if (!batch_entry(ba, dm, b, sh.causal, st.err, &e) || run >= row_runs(sh, e.n)) return;
-  const int group = kh / kAttnGroup, head = kh % kAttnGroup;
+  if (!batch_entry(ba, dm, b, sh.causal, st.err, &e) || r >= rows_of(sh, e.n)) return;
+  const int group = kh / attn_group(dm.d), head = kh % attn_group(dm.d);
   int64_t at = p0 + group * ((p1 - p0) / sh.groups);
-  for (int r = 0; r < run; ++r) at += item_tiles(sh, e.n, e.len, r);
-  const int c0 = cta_of_tile(at, total), c1 = cta_of_tile(at + item_tiles(sh, e.n, e.len, run) - 1, total);
+  for (int i = 0; i < run; ++i) at += item_tiles(sh, e.n, e.len, i);
+  const int tiles = item_tiles(sh, e.n, e.len, run);
+  const int c0 = cta_of_tile(at, total), c1 = cta_of_tile(at + tiles - 1, total);
   if (c0 == c1) return;
-  const int row0 = run * sh.rows, nrows = min(sh.rows, rows_of(sh, e.n) - row0);
-  const int lanes = dm.d / 4, work = nrows * lanes;          // float4 columns of the item's head
-  int shares = kJoinThreads / work;
-  shares = shares < 1 ? 1 : shares;
-  const int share = threadIdx.x / work;
-  for (int i0 = 0; i0 < work; i0 += kJoinThreads) {
-    const int i = shares > 1 ? threadIdx.x % work : i0 + threadIdx.x;
-    const bool on = i < work && share < shares;
-    const int row = i / lanes, ch = i % lanes * 4;
-    float m = -INFINITY, l = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (on) {
-#pragma unroll 4
-      for (int c = c0 + (shares > 1 ? share : 0); c <= c1; c += shares) {
-        if (first_tile(c, total) == first_tile(c + 1, total)) continue;   // fewer tiles than CTAs: no share, no part
-        const float* part = st.part + (int64_t)(c * 2 + (c == c0 ? 1 : 0)) * ge.slot_floats;
-        const float2 ml = *reinterpret_cast<const float2*>(part + kAttnGroup * sh.rows * dm.d + (head * sh.rows + row) * 2);
-        const float4 v = *reinterpret_cast<const float4*>(part + (int64_t)(head * sh.rows + row) * dm.d + ch);
-        const float mn = fmaxf(m, ml.x), base = mn == -INFINITY ? 0.f : mn;
-        const float a = ex2(m - base), z = ex2(ml.x - base);
-        l = l * a + ml.y * z;
-        acc.x = acc.x * a + v.x * z;
-        acc.y = acc.y * a + v.y * z;
-        acc.z = acc.z * a + v.z * z;
-        acc.w = acc.w * a + v.w * z;
-        m = mn;
-      }
-    }
-    if (shares > 1) {
-      float* mine = s_acc[threadIdx.x];
-      mine[0] = m; mine[1] = l; mine[2] = acc.x; mine[3] = acc.y; mine[4] = acc.z; mine[5] = acc.w;
-      __syncthreads();
-      if (share == 0) {
-        for (int k = 1; k < shares; ++k) {
-          const float* o = s_acc[threadIdx.x + k * work];
-          const float mn = fmaxf(m, o[0]), base = mn == -INFINITY ? 0.f : mn;
-          const float a = ex2(m - base), z = ex2(o[0] - base);
-          l = l * a + o[1] * z;
-          acc.x = acc.x * a + o[2] * z;
-          acc.y = acc.y * a + o[3] * z;
-          acc.z = acc.z * a + o[4] * z;
-          acc.w = acc.w * a + o[5] * z;
-          m = mn;
-        }
-      }
-    }
-    if (on && (shares == 1 || share == 0)) {
-      const int r = row0 + row;
-      const int64_t token = e.tok0 + r / sh.rep;
-      const int hq = kh * sh.rep + r % sh.rep;
-      const float mul = l == 0.f ? 0.f : 1.f / l;
-      *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(out.p) + token * out.st + hq * out.sh + ch) =
-          make_uint2(bf162_of(acc.x * mul, acc.y * mul), bf162_of(acc.z * mul, acc.w * mul));
-      if (lse && ch == 0) lse[token * dm.Hq + hq] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
-    }
+  // below one tile a CTA some CTAs have none: then every tile is a part
+  const int parts = total < kAttnCtas ? tiles : c1 - c0 + 1;
+  float m = -INFINITY, l = 0.f;
+  if (tid < parts) {
+    const int c = total < kAttnCtas ? cta_of_tile(at + tid, total) : c0 + tid;
+    const int slot = c * 2 + (c == c0 ? 1 : 0);
+    s_slot[tid] = slot;
+    const float2 ml = *reinterpret_cast<const float2*>(st.part + (int64_t)slot * ge.slot_floats +
+                                                       attn_group(dm.d) * sh.rows * dm.d + (head * sh.rows + row) * 2);
+    m = ml.x;
+    l = ml.y;
   }
+  float top = m;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if ((tid & 31) == 0) s_red[0][tid >> 5] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kJoinThreads / 32; ++i) top = fmaxf(top, s_red[0][i]);
+  const float base = top == -INFINITY ? 0.f : top;
+  const float weight = ex2(m - base);
+  if (tid < parts) s_w[tid] = weight;
+  l = warp_sum(l * weight);
+  if ((tid & 31) == 0) s_red[1][tid >> 5] = l;
+  __syncthreads();
+  l = 0.f;
+#pragma unroll
+  for (int i = 0; i < kJoinThreads / 32; ++i) l += s_red[1][i];
+
+  const int lanes = dm.d / 4, shares = kJoinThreads / lanes;
+  const int share = tid / lanes, ch = tid % lanes * 4;
+  const float* from = st.part + (int64_t)(head * sh.rows + row) * dm.d + ch;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int i = share; i < parts; i += shares) {
+    const float4 v = *reinterpret_cast<const float4*>(from + (int64_t)s_slot[i] * ge.slot_floats);
+    const float z = s_w[i];
+    acc.x += v.x * z;
+    acc.y += v.y * z;
+    acc.z += v.z * z;
+    acc.w += v.w * z;
+  }
+  s_acc[tid] = acc;
+  __syncthreads();
+  if (share) return;
+  for (int k = 1; k < shares; ++k) {
+    const float4 v = s_acc[tid + k * lanes];
+    acc.x += v.x;
+    acc.y += v.y;
+    acc.z += v.z;
+    acc.w += v.w;
+  }
+  const int64_t token = e.tok0 + r / sh.rep;
+  const int hq = kh * sh.rep + r % sh.rep;
+  const float mul = l == 0.f ? 0.f : 1.f / l;
+  *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(out.p) + token * out.st + hq * out.sh + ch) =
+      make_uint2(bf162_of(acc.x * mul, acc.y * mul), bf162_of(acc.z * mul, acc.w * mul));
+  if (lse && ch == 0) lse[token * dm.Hq + hq] = l == 0.f ? -INFINITY : (base + log2f(l)) * 0.69314718055994531f;
 }
 
 // ------------------------------------------------------------------ host
 Geometry geometry(const AttnDims& dm, int n_seq, int max_new, bool causal) {
-  return attn_geometry(dm.H, dm.rep, dm.d, dm.fmt == EPIKV_CACHE_E2M1, n_seq, max_new, causal);
+  return attn_geometry(dm.H, dm.rep, dm.d, dm.fmt == EPIKV_CACHE_E2M1, dm.units, n_seq, max_new, causal);
 }
 
 constexpr int sub_blocks(int fmt, int nt) { return attn_sub_blocks(fmt == EPIKV_CACHE_E2M1, nt); }
@@ -827,7 +1074,7 @@ constexpr int sub_blocks(int fmt, int nt) { return attn_sub_blocks(fmt == EPIKV_
 template <int D, int FMT, int NT>
 cudaError_t run(const AttnState& st, const AttnDims& dm, const Geometry& ge, int layer, const Batch& ba, const Rows& q,
                 const Rows& out, float* lse, const KvDev& kv, cudaStream_t stream) {
-  return plain_launch(attention_kernel<D, FMT, NT, sub_blocks(FMT, NT)>, kAttnCtas, kThreads, ge.smem_bytes, stream, st, dm, ge,
+  return plain_launch(attention_kernel<D, FMT, NT, sub_blocks(FMT, NT)>, kAttnCtas, threads_of(D), ge.smem_bytes, stream, st, dm, ge,
                       layer, ba, q, out, lse, kv, dm.scale * 1.4426950408889634f);
 }
 
@@ -880,7 +1127,7 @@ cudaError_t launch_attention(const AttnState& st, const AttnDims& dm, int layer,
                           : (q4 ? run_rows<256, EPIKV_CACHE_E2M1> : run_rows<256, EPIKV_CACHE_BF16>);
   const cudaError_t err = go(st, dm, ge, layer, ba, q, out, lse, kv, stream);
   if (err != cudaSuccess) return err;
-  const dim3 grid((unsigned)(dm.H * (int64_t)row_runs(ge.sh, ba.max_new)), ba.n_seq);
+  const dim3 grid((unsigned)dm.Hq * ba.max_new, ba.n_seq);
   return pdl_launch(attention_join_kernel, grid, kJoinThreads, 0, stream, st, dm, ge, ba, out, lse);
 }
 

@@ -16,11 +16,13 @@
 namespace epikv {
 
 constexpr int kAttnCtas = 152;   // one per SM of a GB300
-constexpr int kAttnWarps = 8;    // warps that compute
-constexpr int kAttnGroup = 8;    // KV heads of an item, at most
+constexpr int kAttnCopyWarps = 4;   // warps that copy, at most
+// KV heads of an item, at most, and warps that compute: a head's 16 slots of K and V are 8 KB at d = 128 in bf16, and a
+// ring needs several tiles.
+constexpr int attn_group(int d) { return d == 256 ? 4 : 8; }
 
 struct AttnShape {
-  int groups;    // of KV heads, kAttnGroup in each but the last
+  int groups;    // of KV heads, attn_group(d) in each but the last
   int rows;      // query rows of an item
   int tile;      // slots of a tile
   int rep;       // query heads of a KV head
@@ -53,17 +55,30 @@ EPIKV_PLAN int cta_of_tile(int64_t x, int64_t total) { return (int)(((x + 1) * k
 
 // ---- shared memory of a CTA: the ring of tiles, boxes to join a head's warps, barriers, the entries' first tiles
 constexpr int kAttnSmem = 226 * 1024;   // dynamic shared memory, at most
-constexpr int kMaxUnits = 16;           // tiles of the ring
-constexpr int kRowsPerLane = 4;         // rows of a tile that a lane of the copying warp looks after
+constexpr int kMaxStages = 8;           // tiles of the ring
+constexpr int kMaxTile = 128;           // slots of a tile, at most
 
 struct AttnGeometry {
   AttnShape sh;
   int row_s;         // bytes between a tile's rows in shared memory
-  int unit_bytes;    // one tile of K or V
-  int units;         // tiles in the ring
+  int half_bytes;    // a tile's K (its V follows)
+  int stages;        // tiles in the ring
+  int copiers;       // copying warps: each takes every copiers-th tile
   int join_off, bar_off, pre_off, smem_bytes;   // behind the ring
   int slot_floats;   // of a CTA's partial result
+  uint32_t order;    // 4-bit rows: nibble r, the slot of eight that row r of the tensor instruction's rows takes
 };
+
+// Shared memory serves a quarter warp's 16-byte loads (the codes of keys: two rows, four lanes each) or a half warp's
+// 8-byte ones (of values: every second row, four lanes each) at once if they fall on different banks.  Rows r bytes
+// apart, mod 128:
+//   32, 96   rows 0 2 1 3 6 4 7 5: neighbours differ by 2 mod 4, every second one by 0, 1, 2, 3
+//   64       rows 0 1 3 2 4 5 7 6: neighbours differ by an odd number; the values' loads go in two
+//   else     as they stand (one, two or more heads in a row that is not padded: at worst four ways)
+EPIKV_PLAN uint32_t attn_row_order(int row_s) {
+  const int r = row_s & 127;
+  return r == 32 || r == 96 ? 0x57463120u : r == 64 ? 0x67542310u : 0x76543210u;
+}
 
 // 8-row blocks of queries of an item: as many as the registers hold (256 / d) and the call's rows fill.
 EPIKV_PLAN int attn_row_blocks(int d, int rep, int max_new) {
@@ -72,39 +87,49 @@ EPIKV_PLAN int attn_row_blocks(int d, int rep, int max_new) {
   while (nt < 256 / d && nt < want) nt *= 2;
   return nt;
 }
-// 16-slot blocks of a tile that a warp takes.
+// 16-slot blocks of a tile that a warp takes: what a tile costs besides its products (waits, the check against the
+// maximum) is shared by so many (32 x 8,256 slots, d = 128: one 104, two 88, four 96 us, which leaves the ring 3 tiles).
 constexpr int attn_sub_blocks(bool q4, int nt) { return q4 && nt == 1 ? 2 : 1; }
 // Warps of a head in a group of so many heads: 8, 4, 2 or 1.
-EPIKV_PLAN int attn_teams(int heads) { return kAttnWarps / heads; }
+EPIKV_PLAN int attn_teams(int heads, int warps) {
+  const int t = warps / heads;
+  return t >= 8 ? 8 : t >= 4 ? 4 : t >= 2 ? 2 : 1;
+}
 // What a warp leaves for another to join: its outputs, maxima and sums.
 constexpr int attn_box_floats(int d, int nt) { return (d / 16 * nt * 4 + 4 * nt) * 32; }
 
-EPIKV_PLAN AttnGeometry attn_geometry(int H, int rep, int d, bool q4, int n_seq, int max_new, bool causal) {
+// units: 2-byte units of a cache row.
+EPIKV_PLAN AttnGeometry attn_geometry(int H, int rep, int d, bool q4, int units, int n_seq, int max_new, bool causal) {
   AttnGeometry ge;
-  const int nt = attn_row_blocks(d, rep, max_new);
-  const int heads = H < kAttnGroup ? H : kAttnGroup;              // of the first group
-  const int rest = H > kAttnGroup && H % kAttnGroup ? H % kAttnGroup : heads;   // of the last one
-  int tile = 16 * attn_teams(heads) * attn_sub_blocks(q4, nt);
-  if (tile > 32 * kRowsPerLane) tile = 32 * kRowsPerLane;
-  ge.sh = {(H + kAttnGroup - 1) / kAttnGroup, nt * 8, tile, rep, causal ? 1 : 0};
+  const int nt = attn_row_blocks(d, rep, max_new), group = attn_group(d);
+  const int heads = H < group ? H : group;                          // of the first group
+  const int rest = H > group && H % group ? H % group : heads;      // of the last one
+  int tile = 16 * attn_teams(heads, group) * attn_sub_blocks(q4, nt);
+  if (tile > kMaxTile) tile = kMaxTile;
+  ge.sh = {(H + group - 1) / group, nt * 8, tile, rep, causal ? 1 : 0};
   if (!q4) {
     ge.row_s = heads * d * 2 + 16;           // 16 past a multiple of 128: eight rows' 16-byte pieces fill the banks
   } else {
+    // as in the cache, so that several rows come in one copy; parts of rows are laid out for the banks
     const int used = heads * (d / 2) + ((heads * (d / 16) + 15) & ~15);
-    ge.row_s = used + ((32 - used) & 127);   // 32 past a multiple of 128
+    ge.row_s = H > group ? used + ((32 - used) & 127) : units * 2;
   }
-  ge.unit_bytes = (ge.sh.tile * ge.row_s + 127) & ~127;
+  ge.order = attn_row_order(ge.row_s);
+  ge.half_bytes = (ge.sh.tile * ge.row_s + 127) & ~127;
   // any group whose heads have several warps needs the boxes: half of the warps write one at a time
-  const bool join = attn_teams(heads) > 1 || attn_teams(rest) > 1;
-  const int boxes = join ? kAttnWarps / 2 * attn_box_floats(d, nt) * 4 : 0;
-  const int bars = (2 * kMaxUnits + 1) * 8, pre = (n_seq + 1) * 8;
-  ge.units = (kAttnSmem - boxes - bars - pre) / ge.unit_bytes;
-  if (ge.units > kMaxUnits) ge.units = kMaxUnits;
-  ge.join_off = ge.units * ge.unit_bytes;
+  const bool join = attn_teams(heads, group) > 1 || attn_teams(rest, group) > 1;
+  const int boxes = join ? group / 2 * attn_box_floats(d, nt) * 4 : 0;
+  const int bars = (2 * kMaxStages + 1) * 8, pre = (n_seq + 1) * 8;
+  ge.stages = (kAttnSmem - boxes - bars - pre) / (2 * ge.half_bytes);
+  if (ge.stages > kMaxStages) ge.stages = kMaxStages;
+  // A copying warp tells a place's turns apart by one bit.  It waits for tile j after it has filled tile j - copiers, for
+  // which tile j - copiers - stages was left: at least tile j - 2 stages if copiers <= stages, and then the bit is enough.
+  ge.copiers = ge.stages < kAttnCopyWarps ? ge.stages : kAttnCopyWarps;
+  ge.join_off = ge.stages * 2 * ge.half_bytes;
   ge.bar_off = ge.join_off + boxes;
   ge.pre_off = ge.bar_off + bars;
   ge.smem_bytes = ge.pre_off + pre;
-  ge.slot_floats = kAttnGroup * ge.sh.rows * (d + 2);
+  ge.slot_floats = group * ge.sh.rows * (d + 2);
   return ge;
 }
 

@@ -15,21 +15,25 @@ using namespace epikv;
 #define NEED(x) do { if (!(x)) return __LINE__; } while (0)
 extern "C" {
 // 0, or the line of the first check that fails
-int geometry_holds(int H, int rep, int d, int q4, int n_seq, int max_new) {
-  const AttnGeometry g = attn_geometry(H, rep, d, q4, n_seq, max_new, true);
-  const int nt = attn_row_blocks(d, rep, max_new), sub = attn_sub_blocks(q4, nt);
-  NEED(g.units >= 2 && g.units <= kMaxUnits && g.smem_bytes <= kAttnSmem);
+int geometry_holds(int H, int rep, int d, int q4, int units, int n_seq, int max_new) {
+  const AttnGeometry g = attn_geometry(H, rep, d, q4, units, n_seq, max_new, true);
+  const int nt = attn_row_blocks(d, rep, max_new), sub = attn_sub_blocks(q4, nt), group = attn_group(d);
+  NEED(g.stages >= 2 && g.stages <= kMaxStages && g.smem_bytes <= kAttnSmem);
+  NEED(g.copiers >= 1 && g.copiers <= kAttnCopyWarps && g.copiers <= g.stages);
   NEED(g.sh.rows == 8 * nt && nt * d <= 256);
-  NEED(g.sh.tile % 16 == 0 && g.sh.tile >= 16 && g.sh.tile <= 32 * kRowsPerLane);
-  NEED(g.row_s % 16 == 0 && g.unit_bytes % 128 == 0 && g.unit_bytes >= g.sh.tile * g.row_s);
-  NEED(g.join_off >= g.units * g.unit_bytes && g.join_off % 16 == 0 && g.bar_off % 8 == 0 && g.pre_off % 8 == 0);
-  NEED(g.pre_off >= g.bar_off + (2 * kMaxUnits + 1) * 8 && g.smem_bytes >= g.pre_off + (n_seq + 1) * 8);
-  NEED(g.sh.groups * kAttnGroup >= H && (g.sh.groups - 1) * kAttnGroup < H);
-  for (int group = 0; group < g.sh.groups; ++group) {
-    const int heads = H - group * kAttnGroup < kAttnGroup ? H - group * kAttnGroup : kAttnGroup;
-    const int teams = attn_teams(heads);
+  NEED(g.sh.tile % 16 == 0 && g.sh.tile >= 16 && g.sh.tile <= kMaxTile);
+  unsigned rows = 0;
+  for (int r = 0; r < 8; ++r) rows |= 1u << (g.order >> (4 * r) & 7);
+  NEED(rows == 255 && !(g.order & 0x88888888u));
+  NEED(g.row_s % 16 == 0 && g.half_bytes % 128 == 0 && g.half_bytes >= g.sh.tile * g.row_s);
+  NEED(g.join_off >= g.stages * 2 * g.half_bytes && g.join_off % 16 == 0 && g.bar_off % 8 == 0 && g.pre_off % 8 == 0);
+  NEED(g.pre_off >= g.bar_off + (2 * kMaxStages + 1) * 8 && g.smem_bytes >= g.pre_off + (n_seq + 1) * 8);
+  NEED(g.sh.groups * group >= H && (g.sh.groups - 1) * group < H);
+  for (int i = 0; i < g.sh.groups; ++i) {
+    const int heads = H - i * group < group ? H - i * group : group;
+    const int teams = attn_teams(heads, group);
     NEED(teams == 1 || teams == 2 || teams == 4 || teams == 8);
-    NEED(teams * heads <= kAttnWarps);
+    NEED(teams * heads <= group);
     for (int s = 0; s < g.sh.tile / 16; ++s) {   // each block of 16 slots is one team's, within its reach
       int n = 0;
       for (int team = 0; team < teams; ++team)
@@ -43,13 +47,13 @@ int geometry_holds(int H, int rep, int d, int q4, int n_seq, int max_new) {
         for (int head = 0; head < heads; ++head)
           NEED(g.join_off + (int64_t)(team * heads + head + 1) * attn_box_floats(d, nt) * 4 <= g.bar_off);
   }
-  const AttnGeometry most = attn_geometry(H, rep, d, q4, 1, max_new, true);   // what the workspace is sized by
-  for (int n = 1; n <= max_new; n *= 2) NEED(attn_geometry(H, rep, d, q4, n_seq, n, false).slot_floats <= most.slot_floats);
+  const AttnGeometry most = attn_geometry(H, rep, d, q4, units, 1, max_new, true);   // what the workspace is sized by
+  for (int n = 1; n <= max_new; n *= 2) NEED(attn_geometry(H, rep, d, q4, units, n_seq, n, false).slot_floats <= most.slot_floats);
   return 0;
 }
 
-int shares_hold(int H, int rep, int d, int q4, int max_new, int causal, int n_seq, const int* n, const int* len) {
-  const AttnGeometry g = attn_geometry(H, rep, d, q4, n_seq, max_new, causal);
+int shares_hold(int H, int rep, int d, int q4, int units, int max_new, int causal, int n_seq, const int* n, const int* len) {
+  const AttnGeometry g = attn_geometry(H, rep, d, q4, units, n_seq, max_new, causal);
   int64_t total = 0;
   for (int b = 0; b < n_seq; ++b) total += entry_tiles(g.sh, n[b], len[b]);
   if (!total) return 0;
@@ -96,16 +100,24 @@ def plan(tmp_path_factory):
     return C.CDLL(out)
 
 
+def units_of(H, d, q4):
+    from paper_2606_26472_gb300 import build, epikv as E
+    build.build()
+    h, x = E.epikv_cache_row(H, d, E.EPIKV_CACHE_E2M1 if q4 else E.EPIKV_CACHE_BF16)
+    return h * x
+
+
 @pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("q4", [0, 1])
 def test_shared_memory(plan, d, q4):
     for H in range(1, 33):
-        if H * d > 2048 and not q4:
+        if (H * d > 2048 and not q4) or (q4 and H * (d // 2 + d // 16) > 4096):
             continue
+        units = units_of(H, d, q4)
         for rep in (1, 2, 3, 4, 7, 8, 9, 71):
             for n_seq in (1, 64, 4096):
                 for max_new in (1, 2, 5, 64, 4096):
-                    assert plan.geometry_holds(H, rep, d, q4, n_seq, max_new) == 0, (H, rep, n_seq, max_new)
+                    assert plan.geometry_holds(H, rep, d, q4, units, n_seq, max_new) == 0, (H, rep, n_seq, max_new)
 
 
 def test_shares(plan):
@@ -119,4 +131,4 @@ def test_shares(plan):
         ln = [rng.choice([0, 1, 15, 16, 17, rng.randint(0, 3000)]) for _ in range(n_seq)]
         causal = rng.randint(0, 1)
         arr = C.c_int * n_seq
-        assert plan.shares_hold(H, rep, d, q4, max(max(n), 1), causal, n_seq, arr(*n), arr(*ln)) == 0, (H, rep, d, q4, n, ln)
+        assert plan.shares_hold(H, rep, d, q4, units_of(H, d, q4), max(max(n), 1), causal, n_seq, arr(*n), arr(*ln)) == 0, (H, rep, d, q4, n, ln)
