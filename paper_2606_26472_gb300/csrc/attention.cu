@@ -156,19 +156,6 @@ struct Walker {
     }
     w->tiles = item_tiles(sh, w->e.n, w->e.len, w->run);
   }
-  // The item that tile lo of all is in (there is one).
-  __device__ __forceinline__ void seek(Walk* w, int64_t lo) const {
-    int first = 0, last = ba.n_seq - 1;   // the first entry that ends behind lo
-    while (first < last) {
-      const int mid = (first + last) / 2;
-      if (pre[mid + 1] > lo) last = mid;
-      else first = mid + 1;
-    }
-    w->b = first;
-    w->at = (int)(pre[first] - lo);
-    entry(w);
-    while (w->at + w->tiles <= 0) step(w);
-  }
   // Moves the warp's walk on to the item of tile i.
   __device__ __forceinline__ void to(Walk* w, int i, int lane) const {
     if (i < w->at + w->tiles) return;
@@ -461,21 +448,25 @@ __global__ void __launch_bounds__(threads_of(D), 1)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const AttnShape& sh = ge.sh;
 
-  // tiles before each entry
+  __shared__ Walk s_walk[kWarps + kAttnCopyWarps], s_first;
   if (tid < 2 * kMaxStages) mbar_init(&full[tid], tid >= kMaxStages ? kWarps : FMT == EPIKV_CACHE_BF16 ? 32 : 1);
-  if (tid == 0) *gave_up = 0;
-  const int per = (ba.n_seq + 255) / 256;
+  if (tid == 0) {
+    *gave_up = 0;
+    fence_barrier_init();
+  }
+  pdl_wait();
+  pdl_trigger();
+  // tiles before each entry, and the entry that the CTA's first tile is in
+  const int per = (ba.n_seq + 255) >> 8;
   int64_t mine = 0;
+  Entry e0{};
   if (tid < 256)
     for (int i = 0; i < per; ++i) {
       const int b = tid * per + i;
-      Entry e;
-      if (b < ba.n_seq && batch_entry(ba, dm, b, sh.causal, st.err, &e)) {
-        const int64_t t = entry_tiles(sh, e.n, e.len);
+      if (b < ba.n_seq) {
+        const int64_t t = batch_entry(ba, dm, b, sh.causal, st.err, &e0) ? entry_tiles(sh, e0.n, e0.len) : 0;
         mine += t;
         pre[b + 1] = t;
-      } else if (b < ba.n_seq) {
-        pre[b + 1] = 0;
       }
     }
   int64_t run = mine;
@@ -484,28 +475,37 @@ __global__ void __launch_bounds__(threads_of(D), 1)
     if (lane >= o) run += v;
   }
   if (lane == 31 && warp < 8) s_warp[warp] = run;
-  if (tid == 0) fence_barrier_init();
   __syncthreads();
+  int64_t total = 0, at0 = run - mine;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    if (k < warp) at0 += s_warp[k];
+    total += s_warp[k];
+  }
+  const int64_t lo = first_tile(blockIdx.x, total), hi = first_tile(blockIdx.x + 1, total);
   if (tid < 256) {
-    int64_t at = run - mine;
-    for (int k = 0; k < warp; ++k) at += s_warp[k];
     for (int i = 0; i < per; ++i) {
       const int b = tid * per + i;
-      if (b < ba.n_seq) at = pre[b + 1] += at;
+      if (b >= ba.n_seq) break;
+      const int64_t end = at0 + pre[b + 1];
+      if (at0 <= lo && lo < end) {
+        if (per > 1) batch_entry(ba, dm, b, sh.causal, st.err, &e0);
+        s_first = Walk{b, 0, 0, (int)(at0 - lo), item_tiles(sh, e0.n, e0.len, 0), e0};
+      }
+      pre[b + 1] = at0 = end;
     }
     if (tid == 0) pre[0] = 0;
   }
   __syncthreads();
-  pdl_trigger();
   if (blockIdx.x == 0)
     for (int b = tid; b <= ba.n_seq; b += kThreads) st.plan[b] = pre[b];
-  const int64_t total = pre[ba.n_seq];
-  const int64_t lo = first_tile(blockIdx.x, total), hi = first_tile(blockIdx.x + 1, total);
   if (lo == hi) return;
-  __shared__ Walk s_walk[kWarps + kAttnCopyWarps];
   Walk* w = &s_walk[warp];
   const Walker walker{pre, ba, dm, sh, st.err};
-  if (lane == 0) walker.seek(w, lo);
+  if (lane == 0) {
+    *w = s_first;
+    while (w->at + w->tiles <= 0) walker.step(w);
+  }
   __syncwarp();
   const int tiles = (int)(hi - lo);
   const Waiter wait{gave_up, st.err};
@@ -991,13 +991,16 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(AttnState 
   __shared__ float s_w[kAttnCtas], s_red[2][kJoinThreads / 32];
   __shared__ float4 s_acc[kJoinThreads];
   const AttnShape& sh = ge.sh;
-  const int b = blockIdx.y, kh = blockIdx.x % dm.H, r = blockIdx.x / dm.H, run = r / sh.rows, row = r % sh.rows;
+  const int b = blockIdx.y, kh = blockIdx.x % dm.H, r = blockIdx.x / dm.H, run = r >> sh.rows_log,
+            row = r & (sh.rows - 1);
   const int tid = threadIdx.x;
   pdl_wait();
   const int64_t p0 = st.plan[b], p1 = st.plan[b + 1], total = st.plan[ba.n_seq];
-  if (p0 == p1) return;
   Entry e;
-  if (!batch_entry(ba, dm, b, sh.causal, st.err, &e) || r >= rows_of(sh, e.n)) return;
+  e.tok0 = ba.cu_new[b];
+  e.n = ba.cu_new[b + 1] - e.tok0;
+  e.len = ba.len[(int64_t)b * ba.len_stride];
+  if (p0 == p1 || r >= rows_of(sh, e.n)) return;   // no tiles: an entry without new tokens, or one that was refused
   const int group = kh / attn_group(dm.d), head = kh % attn_group(dm.d);
   int64_t at = p0 + group * ((p1 - p0) / sh.groups);
   for (int i = 0; i < run; ++i) at += item_tiles(sh, e.n, e.len, i);
@@ -1074,7 +1077,7 @@ constexpr int sub_blocks(int fmt, int nt) { return attn_sub_blocks(fmt == EPIKV_
 template <int D, int FMT, int NT>
 cudaError_t run(const AttnState& st, const AttnDims& dm, const Geometry& ge, int layer, const Batch& ba, const Rows& q,
                 const Rows& out, float* lse, const KvDev& kv, cudaStream_t stream) {
-  return plain_launch(attention_kernel<D, FMT, NT, sub_blocks(FMT, NT)>, kAttnCtas, threads_of(D), ge.smem_bytes, stream, st, dm, ge,
+  return pdl_launch(attention_kernel<D, FMT, NT, sub_blocks(FMT, NT)>, kAttnCtas, threads_of(D), ge.smem_bytes, stream, st, dm, ge,
                       layer, ba, q, out, lse, kv, dm.scale * 1.4426950408889634f);
 }
 

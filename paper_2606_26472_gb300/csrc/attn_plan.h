@@ -23,8 +23,9 @@ constexpr int attn_group(int d) { return d == 256 ? 4 : 8; }
 
 struct AttnShape {
   int groups;    // of KV heads, attn_group(d) in each but the last
-  int rows;      // query rows of an item
-  int tile;      // slots of a tile
+  int rows;      // query rows of an item, 1 << rows_log
+  int tile;      // slots of a tile, 1 << tile_log
+  int rows_log, tile_log;
   int rep;       // query heads of a KV head
   int causal;
 };
@@ -32,15 +33,15 @@ struct AttnShape {
 // Slots that the last of an item's rows sees: query row r of a KV head is
 // token r / rep's, and token i of an entry sees len + i + 1 slots.
 EPIKV_PLAN int rows_of(const AttnShape& s, int n) { return n * s.rep; }
-EPIKV_PLAN int row_runs(const AttnShape& s, int n) { return (n * s.rep + s.rows - 1) / s.rows; }
+EPIKV_PLAN int row_runs(const AttnShape& s, int n) { return (n * s.rep + s.rows - 1) >> s.rows_log; }
 EPIKV_PLAN int slots_seen(const AttnShape& s, int n, int len, int run) {
   if (!s.causal) return len;
-  const int last = (run + 1) * s.rows < n * s.rep ? (run + 1) * s.rows : n * s.rep;
-  return len + (last - 1) / s.rep + 1;
+  const int end = (run + 1) << s.rows_log;
+  return end >= n * s.rep ? len + n : len + (end - 1) / s.rep + 1;
 }
 // An item that sees nothing still has a tile: its rows' zeros are written.
 EPIKV_PLAN int item_tiles(const AttnShape& s, int n, int len, int run) {
-  const int t = (slots_seen(s, n, len, run) + s.tile - 1) / s.tile;
+  const int t = (slots_seen(s, n, len, run) + s.tile - 1) >> s.tile_log;
   return t > 1 ? t : 1;
 }
 EPIKV_PLAN int64_t entry_tiles(const AttnShape& s, int n, int len) {
@@ -106,7 +107,10 @@ EPIKV_PLAN AttnGeometry attn_geometry(int H, int rep, int d, bool q4, int units,
   const int rest = H > group && H % group ? H % group : heads;      // of the last one
   int tile = 16 * attn_teams(heads, group) * attn_sub_blocks(q4, nt);
   if (tile > kMaxTile) tile = kMaxTile;
-  ge.sh = {(H + group - 1) / group, nt * 8, tile, rep, causal ? 1 : 0};
+  int rows_log = 3, tile_log = 4;
+  while (1 << rows_log < nt * 8) ++rows_log;
+  while (1 << tile_log < tile) ++tile_log;
+  ge.sh = {(H + group - 1) / group, nt * 8, tile, rows_log, tile_log, rep, causal ? 1 : 0};
   if (!q4) {
     ge.row_s = heads * d * 2 + 16;           // 16 past a multiple of 128: eight rows' 16-byte pieces fill the banks
   } else {

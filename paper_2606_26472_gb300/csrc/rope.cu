@@ -151,6 +151,7 @@ __global__ void __launch_bounds__(kBlock) rope_kernel(int32_t* err, Rows x, Rows
   if (slot >= tpb * step) return;
   const int64_t token = (int64_t)blockIdx.x * tpb + slot / step;
   if (token >= n_tokens) return;
+  pdl_wait();
   const int p = pos[token];
   if ((unsigned)p >= (unsigned)r.n_pos) {
     set_error(err, EPIKV_DEV_POSITION);
@@ -264,6 +265,7 @@ __global__ void __launch_bounds__(kBlock) append_kernel(AttnState st, AttnDims d
                                                         Rows vr, RopeDev r, KvDev kv) {
   const int b = blockIdx.y, i = blockIdx.x;
   Entry e;
+  pdl_wait();
   if (!batch_entry(ba, dm, b, true, st.err, &e) || i >= e.n) return;
   int p = 0;
   if (r.dim) {
@@ -347,6 +349,7 @@ __global__ void __launch_bounds__(kBlock) cache_read_kernel(AttnState st, AttnDi
   const int G = dm.d / 16, per = dm.H * G;
   const int64_t j = (int64_t)blockIdx.x * kBlock + threadIdx.x;
   if (j >= (int64_t)n_rows * per) return;
+  pdl_wait();
   const int64_t i = j / per;
   const int h = (int)(j - i * per) / G, g = (int)(j - i * per) % G;
   const int seq = seqs[i];
@@ -393,9 +396,9 @@ cudaError_t rope_of(const AttnState& st, const AttnDims& dm, int n_tokens, int n
   const int slots = kBlock / (vec ? dm.d / 16 : dm.d / 2);
   const int tpb = slots / n_heads > 1 ? slots / n_heads : 1;
   const unsigned grid = (unsigned)(((int64_t)n_tokens + tpb - 1) / tpb);
-  return vec ? plain_launch(rope_kernel<T, 8>, grid, kBlock, 0, stream, st.err, x, y, pos, rope, n_tokens, n_heads,
+  return vec ? pdl_launch(rope_kernel<T, 8>, grid, kBlock, 0, stream, st.err, x, y, pos, rope, n_tokens, n_heads,
                             dm.d, sign)
-             : plain_launch(rope_kernel<T, 1>, grid, kBlock, 0, stream, st.err, x, y, pos, rope, n_tokens, n_heads,
+             : pdl_launch(rope_kernel<T, 1>, grid, kBlock, 0, stream, st.err, x, y, pos, rope, n_tokens, n_heads,
                             dm.d, sign);
 }
 
@@ -426,14 +429,14 @@ cudaError_t launch_append(const AttnState& st, const AttnDims& dm, int layer, co
   const bool q4 = dm.fmt == EPIKV_CACHE_E2M1;
   auto kern = vec ? (q4 ? append_kernel<8, EPIKV_CACHE_E2M1> : append_kernel<8, EPIKV_CACHE_BF16>)
                   : (q4 ? append_kernel<1, EPIKV_CACHE_E2M1> : append_kernel<1, EPIKV_CACHE_BF16>);
-  return plain_launch(kern, grid, kBlock, 0, stream, st, dm, layer, ba, pos, q, qo, k, v, rope, kv);
+  return pdl_launch(kern, grid, kBlock, 0, stream, st, dm, layer, ba, pos, q, qo, k, v, rope, kv);
 }
 
 cudaError_t launch_cache_read(const AttnState& st, const AttnDims& dm, int layer, int n_rows, const int32_t* seqs,
                               const int32_t* slots, const Rows& k, const Rows& v, const KvDev& kv,
                               cudaStream_t stream) {
   const int64_t n = (int64_t)n_rows * dm.H * (dm.d / 16);
-  return plain_launch(cache_read_kernel, (unsigned)((n + kBlock - 1) / kBlock), kBlock, 0, stream, st, dm, layer,
+  return pdl_launch(cache_read_kernel, (unsigned)((n + kBlock - 1) / kBlock), kBlock, 0, stream, st, dm, layer,
                       n_rows, seqs, slots, k, v, kv);
 }
 

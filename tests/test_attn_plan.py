@@ -20,6 +20,7 @@ int geometry_holds(int H, int rep, int d, int q4, int units, int n_seq, int max_
   const int nt = attn_row_blocks(d, rep, max_new), sub = attn_sub_blocks(q4, nt), group = attn_group(d);
   NEED(g.stages >= 2 && g.stages <= kMaxStages && g.smem_bytes <= kAttnSmem);
   NEED(g.copiers >= 1 && g.copiers <= kAttnCopyWarps && g.copiers <= g.stages);
+  NEED(g.sh.rows == 1 << g.sh.rows_log && g.sh.tile == 1 << g.sh.tile_log);
   NEED(g.sh.rows == 8 * nt && nt * d <= 256);
   NEED(g.sh.tile % 16 == 0 && g.sh.tile >= 16 && g.sh.tile <= kMaxTile);
   unsigned rows = 0;
