@@ -31,6 +31,8 @@
 // significant bits).  Queries enter as halves scaled by a power of two per
 // row, probabilities as halves times 2^7 (11 bits down to 2^-21).  For
 // a bf16 cache the probabilities go in as two bf16 terms (16 bits).
+#include <cuda.h>
+
 #include "attn.cuh"
 #include "attn_plan.h"
 
@@ -130,7 +132,7 @@ struct Walk {
   Entry e;
 };
 struct Walker {
-  const int64_t* pre;
+  const int* pre;
   const Batch& ba;
   const AttnDims& dm;
   const AttnShape& sh;
@@ -358,8 +360,79 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int by
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
-// bf16 rows: 16 bytes a lane, into rows 16 bytes past a multiple of 128 apart (rows as they stand would put eight of
-// them on the same banks).  Lane i reads the table entries of rows i, i + 32, ...
+// Where 16-byte part `part` of a row's piece of 64 channels stands: rows of a block are 128 bytes apart.
+__device__ __forceinline__ uint32_t swizzled(int row, int part) { return row * 128 + ((part ^ (row & 7)) << 4); }
+
+// The cache as a tensor [pieces of 64 channels][blocks or sequences][slots of one][64 channels]; a copy takes 16 slots of
+// a group's heads.
+struct CacheMaps {
+  CUtensorMap kv[2];
+  int on;   // 0: the cache cannot be described so (blocks that 16 does not divide); rows are copied by lanes
+};
+
+__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int c1, int c2, int c3, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      :: "r"(smem_u32(dst)), "l"(map), "r"(0), "r"(c1), "r"(c2), "r"(c3), "r"(smem_u32(bar)) : "memory");
+}
+
+// bf16 rows, 16 slots of a group's heads in one tensor copy (32 KB at 8 x 128): lane i looks after block i of the tile.
+// Slots behind the last seen one come as they are; the computing warps mask them.
+template <int D>
+__device__ void copy_tensor(char* smem, uint64_t* full, uint64_t* empty, const Waiter& wait, const AttnState& st,
+                            const AttnDims& dm, const Geometry& ge, const KvDev& kv, const CacheMaps& maps, int layer,
+                            const Walker& walker, Walk* w, int tiles, int warp, int lane) {
+  const AttnShape& sh = ge.sh;
+  const bool flat = kv.layout == EPIKV_LAYOUT_CONTIGUOUS;
+  const Divider block(flat ? 1 : kv.block_size);
+  const int bytes = 16 * ge.row_s;
+  Ring ring(ge.stages, warp);
+  int seq = 0, group = 0;
+  bool mine = false;
+  Place next{0, 0};
+  auto look = [&](int x) {
+    walker.to(w, x, lane);
+    const int at = (x - w->at) * sh.tile + 16 * lane;
+    seq = w->e.seq;
+    group = w->group;
+    mine = 16 * lane < sh.tile && at < slots_seen(sh, w->e.n, w->e.len, w->run);
+    if (mine) next = place_of(kv, block, layer, seq, at);
+  };
+  int x = warp;
+  if (x < tiles) look(x);
+  for (; x < tiles; x += ge.copiers) {
+    const bool there = mine && (flat || (next.entry >= 0 && next.entry < kv.num_blocks));
+    if (mine && !there) set_error(st.err, EPIKV_DEV_SLOT);
+    const int c1 = next.rest, c2 = flat ? seq : next.entry, c3 = group * (attn_group(D) * D / 64);
+    if (x + ge.copiers < tiles) look(x + ge.copiers);
+    uint64_t* bar = &full[ring.place];
+    char* dst = smem + ring.place * (2 * ge.half_bytes) + lane * bytes;
+    if (ring.turn) wait(&empty[ring.place], (ring.turn & 1) ^ 1);
+    const uint32_t blocks = __ballot_sync(0xffffffffu, there);
+    if (__popc(blocks) * 16 < sh.tile) {   // blocks that nothing fills
+      if (!there && 16 * lane < sh.tile) {
+        zero_rows(dst, bytes);
+        zero_rows(dst + ge.half_bytes, bytes);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+    }
+    if (lane == 0) mbar_arrive_expect_tx(bar, 2 * __popc(blocks) * bytes);
+    __syncwarp();
+    if (there) {
+      tma_load_4d(dst, &maps.kv[0], c1, c2, c3, bar);
+      tma_load_4d(dst + ge.half_bytes, &maps.kv[1], c1, c2, c3, bar);
+    }
+    ring.on(ge.copiers);
+  }
+  if (*wait.gave_up) {   // the CTA may not end before its copies have landed: this warp's last ones
+    for (int j = tiles - 1; j >= 0 && j >= tiles - ge.stages; --j)
+      if (j % ge.copiers == warp) mbar_wait_bounded(&full[j % ge.stages], (uint32_t)(j / ge.stages) & 1, kWaitNs);
+  }
+}
+
+// bf16 rows of any layout, 16 bytes a lane, to where a tensor copy would put them.  Lane i reads the table entries of
+// rows i, i + 32, ...
 template <int D>
 __device__ void copy_bf16(char* smem, uint64_t* full, uint64_t* empty, const Waiter& wait, const AttnState& st,
                           const AttnDims& dm, const Geometry& ge, const KvDev& kv, int layer, const Walker& walker,
@@ -405,7 +478,7 @@ __device__ void copy_bf16(char* smem, uint64_t* full, uint64_t* empty, const Wai
     if (ring.turn) wait(&empty[ring.place], (ring.turn & 1) ^ 1);
 #pragma unroll 1
     for (int which = 0; which < 2; ++which) {
-      const uint32_t dst = smem_u32(smem) + (2 * ring.place + which) * ge.half_bytes + col * 16;
+      const uint32_t dst = smem_u32(smem) + (2 * ring.place + which) * ge.half_bytes;
       const char* base = kv.base[which] + group * (attn_group(D) * D * 2) + col * 16;
 #pragma unroll
       for (int k = 0; k < kMost; ++k) {
@@ -416,12 +489,13 @@ __device__ void copy_bf16(char* smem, uint64_t* full, uint64_t* empty, const Wai
           const int64_t o = __shfl_sync(0xffffffffu, from[k], row & 31);
           const char* s = base + (o < 0 ? 0 : o);
           const int take = o < 0 ? 0 : 16;
-          const uint32_t d = dst + (32 * k + row) * ge.row_s;
+          const int slot = 32 * k + row;
+          const uint32_t d = dst + (slot >> 4) * (16 * ge.row_s) + (col >> 3) * 2048 + swizzled(slot & 15, col & 7);
           if (sub < at_once && row < end) {
             if (col < pieces) cp_async16(d, s, take);
 #pragma unroll
-            for (int c = 1; c < attn_group(D) * D / 8 / 32; ++c)
-              if (col + 32 * c < pieces) cp_async16(d + 512 * c, s + 512 * c, take);
+            for (int c = 1; c < attn_group(D) * D / 8 / 32; ++c)   // 32 parts on: four pieces
+              if (col + 32 * c < pieces) cp_async16(d + 8192 * c, s + 512 * c, take);
           }
         }
       }
@@ -437,19 +511,20 @@ __device__ void copy_bf16(char* smem, uint64_t* full, uint64_t* empty, const Wai
 template <int D, int FMT, int NT, int SUB>
 __global__ void __launch_bounds__(threads_of(D), 1)
     attention_kernel(AttnState st, AttnDims dm, Geometry ge, int layer, Batch ba, Rows q, Rows out, float* lse,
-                     KvDev kv, float scale_log2) {
+                     KvDev kv, const __grid_constant__ CacheMaps maps, float scale_log2) {
   constexpr int kWarps = attn_group(D), kThreads = threads_of(D);
-  extern __shared__ __align__(128) char smem[];
+  extern __shared__ __align__(1024) char smem_raw[];
+  char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + ge.bar_off);
   uint64_t* empty = full + kMaxStages;
   int* gave_up = reinterpret_cast<int*>(empty + kMaxStages);
-  int64_t* pre = reinterpret_cast<int64_t*>(smem + ge.pre_off);
-  __shared__ int64_t s_warp[8];
+  int* pre = reinterpret_cast<int*>(smem + ge.pre_off);
+  __shared__ int s_warp[8];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const AttnShape& sh = ge.sh;
 
   __shared__ Walk s_walk[kWarps + kAttnCopyWarps], s_first;
-  if (tid < 2 * kMaxStages) mbar_init(&full[tid], tid >= kMaxStages ? kWarps : FMT == EPIKV_CACHE_BF16 ? 32 : 1);
+  if (tid < 2 * kMaxStages) mbar_init(&full[tid], tid >= kMaxStages ? kWarps : FMT == EPIKV_CACHE_BF16 && !maps.on ? 32 : 1);
   if (tid == 0) {
     *gave_up = 0;
     fence_barrier_init();
@@ -458,39 +533,44 @@ __global__ void __launch_bounds__(threads_of(D), 1)
   pdl_trigger();
   // tiles before each entry, and the entry that the CTA's first tile is in
   const int per = (ba.n_seq + 255) >> 8;
-  int64_t mine = 0;
+  int mine = 0;
   Entry e0{};
   if (tid < 256)
     for (int i = 0; i < per; ++i) {
       const int b = tid * per + i;
       if (b < ba.n_seq) {
-        const int64_t t = batch_entry(ba, dm, b, sh.causal, st.err, &e0) ? entry_tiles(sh, e0.n, e0.len) : 0;
-        mine += t;
-        pre[b + 1] = t;
+        int64_t t = batch_entry(ba, dm, b, sh.causal, st.err, &e0) ? entry_tiles(sh, e0.n, e0.len) : 0;
+        if (t > kMostTiles - mine) {
+          set_error(st.err, EPIKV_DEV_CAPACITY);
+          t = 0;
+        }
+        mine += (int)t;
+        pre[b + 1] = (int)t;
       }
     }
-  int64_t run = mine;
+  int run = mine;
+#pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int64_t v = __shfl_up_sync(0xffffffffu, run, o);
+    const int v = __shfl_up_sync(0xffffffffu, run, o);
     if (lane >= o) run += v;
   }
   if (lane == 31 && warp < 8) s_warp[warp] = run;
   __syncthreads();
-  int64_t total = 0, at0 = run - mine;
+  int total = 0, at0 = run - mine;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     if (k < warp) at0 += s_warp[k];
     total += s_warp[k];
   }
-  const int64_t lo = first_tile(blockIdx.x, total), hi = first_tile(blockIdx.x + 1, total);
+  const int lo = first_tile(blockIdx.x, total), hi = first_tile(blockIdx.x + 1, total);
   if (tid < 256) {
     for (int i = 0; i < per; ++i) {
       const int b = tid * per + i;
       if (b >= ba.n_seq) break;
-      const int64_t end = at0 + pre[b + 1];
+      const int end = at0 + pre[b + 1];
       if (at0 <= lo && lo < end) {
         if (per > 1) batch_entry(ba, dm, b, sh.causal, st.err, &e0);
-        s_first = Walk{b, 0, 0, (int)(at0 - lo), item_tiles(sh, e0.n, e0.len, 0), e0};
+        s_first = Walk{b, 0, 0, at0 - lo, item_tiles(sh, e0.n, e0.len, 0), e0};
       }
       pre[b + 1] = at0 = end;
     }
@@ -507,11 +587,13 @@ __global__ void __launch_bounds__(threads_of(D), 1)
     while (w->at + w->tiles <= 0) walker.step(w);
   }
   __syncwarp();
-  const int tiles = (int)(hi - lo);
+  const int tiles = hi - lo;
   const Waiter wait{gave_up, st.err};
   if (warp >= kWarps) {
     if (warp - kWarps >= ge.copiers) return;
-    if constexpr (FMT == EPIKV_CACHE_BF16)
+    if (FMT == EPIKV_CACHE_BF16 && maps.on)
+      copy_tensor<D>(smem, full, empty, wait, st, dm, ge, kv, maps, layer, walker, w, tiles, warp - kWarps, lane);
+    else if constexpr (FMT == EPIKV_CACHE_BF16)
       copy_bf16<D>(smem, full, empty, wait, st, dm, ge, kv, layer, walker, w, tiles, warp - kWarps, lane);
     else
       copy_q4<D>(smem, full, empty, wait, st, dm, ge, kv, layer, walker, w, tiles, warp - kWarps, lane);
@@ -540,10 +622,13 @@ __global__ void __launch_bounds__(threads_of(D), 1)
     const uint32_t ring0 = smem_u32(smem);
     const uint32_t hop = teams * 16 * ge.row_s, eight = 8 * ge.row_s;   // to the warp's next block of slots; 8 slots on
     const int k0 = kBf16 ? 2 * t : slot_of_row(ge.order, 2 * t), k1 = kBf16 ? 2 * t + 1 : slot_of_row(ge.order, 2 * t + 1);
-    uint32_t key_code, key_scale = 0, value_code, value_scale = 0, odd = 0;
+    uint32_t key_code, key_scale, value_code, value_scale, odd = 0;
     if constexpr (kBf16) {
-      key_code = (team * 16 + (lane & 15)) * ge.row_s + head * (D * 2) + (lane >> 4) * 16;
-      value_code = ge.half_bytes + (team * 16 + (lane & 7) + (lane >> 4) * 8) * ge.row_s + head * (D * 2) + ((lane >> 3) & 1) * 16;
+      const uint32_t mine = team * 16 * ge.row_s + head * (D / 64) * 2048;
+      key_code = mine + (lane & 15) * 128;
+      key_scale = (lane >> 4) ^ (lane & 7);          // of a row's parts: 2 j + this lane's half, exchanged by the row
+      value_code = ge.half_bytes + mine + ((lane & 7) + (lane >> 4) * 8) * 128;
+      value_scale = ((lane >> 3) & 1) ^ (lane & 7);
     } else {
       const uint32_t key_row = (team * 16 + slot_of_row(ge.order, g)) * ge.row_s;
       const uint32_t value_row = (team * 16 + k0) * ge.row_s, scales = heads * (D / 2) + head * (D / 16);
@@ -634,7 +719,7 @@ __global__ void __launch_bounds__(threads_of(D), 1)
 #pragma unroll
             for (int j = 0; j < KS; ++j) {
               uint32_t a[4];
-              ldmatrix4<false>(a, addr + j * 32);
+              ldmatrix4<false>(a, addr + j / 4 * 2048 + (((2 * j & 6) ^ key_scale) << 4));
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) mma<FMT>(s[u][nt], a, qf[nt][j][0], qf[nt][j][1]);
             }
@@ -789,7 +874,7 @@ __global__ void __launch_bounds__(threads_of(D), 1)
 #pragma unroll
               for (int mt = 0; mt < KS; ++mt) {
                 uint32_t a[4];
-                ldmatrix4<true>(a, addr + mt * 32);
+                ldmatrix4<true>(a, addr + mt / 4 * 2048 + (((2 * mt & 6) ^ value_scale) << 4));
                 f(mt, a);
               }
             } else {
@@ -995,14 +1080,14 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(AttnState 
             row = r & (sh.rows - 1);
   const int tid = threadIdx.x;
   pdl_wait();
-  const int64_t p0 = st.plan[b], p1 = st.plan[b + 1], total = st.plan[ba.n_seq];
+  const int p0 = st.plan[b], p1 = st.plan[b + 1], total = st.plan[ba.n_seq];
   Entry e;
   e.tok0 = ba.cu_new[b];
   e.n = ba.cu_new[b + 1] - e.tok0;
   e.len = ba.len[(int64_t)b * ba.len_stride];
   if (p0 == p1 || r >= rows_of(sh, e.n)) return;   // no tiles: an entry without new tokens, or one that was refused
   const int group = kh / attn_group(dm.d), head = kh % attn_group(dm.d);
-  int64_t at = p0 + group * ((p1 - p0) / sh.groups);
+  int at = p0 + group * ((p1 - p0) / sh.groups);
   for (int i = 0; i < run; ++i) at += item_tiles(sh, e.n, e.len, i);
   const int tiles = item_tiles(sh, e.n, e.len, run);
   const int c0 = cta_of_tile(at, total), c1 = cta_of_tile(at + tiles - 1, total);
@@ -1074,11 +1159,53 @@ Geometry geometry(const AttnDims& dm, int n_seq, int max_new, bool causal) {
 
 constexpr int sub_blocks(int fmt, int nt) { return attn_sub_blocks(fmt == EPIKV_CACHE_E2M1, nt); }
 
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+  static const EncodeTiled fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return reinterpret_cast<EncodeTiled>(p);
+  }();
+  return fn;
+}
+
+// The layer's K and V as tensors, where their layout allows it.
+CacheMaps cache_maps(const AttnDims& dm, const Geometry& ge, int layer, const KvDev& kv) {
+  CacheMaps maps = {};
+  if (dm.fmt != EPIKV_CACHE_BF16) return maps;
+  const bool flat = kv.layout == EPIKV_LAYOUT_CONTIGUOUS;
+  if (!flat && kv.block_size % 16) return maps;
+  const int64_t outer = flat ? kv.stride_seq : kv.stride_block;   // elements
+  // slots of a sequence: no more than lie before the next one, whatever the configuration allows
+  const int64_t room = kv.stride_seq >= kv.stride_token ? kv.stride_seq / kv.stride_token : dm.T;
+  const cuuint64_t dims[4] = {64, (cuuint64_t)(!flat ? kv.block_size : room < dm.T ? room : dm.T), (cuuint64_t)(flat ? dm.S : kv.num_blocks), (cuuint64_t)(dm.H * dm.d / 64)};
+  const cuuint64_t strides[3] = {(cuuint64_t)kv.stride_token * 2, (cuuint64_t)outer * 2, 128};
+  for (int i = 0; i < 2; ++i)
+    if (strides[i] == 0 || strides[i] >= (cuuint64_t(1) << 40)) return maps;
+  const cuuint32_t box[4] = {64, 16, 1, (cuuint32_t)(ge.row_s / 128)}, ones[4] = {1, 1, 1, 1};
+  const EncodeTiled encode = encode_tiled();
+  if (!encode) return maps;
+  for (int w = 0; w < 2; ++w)
+    if (encode(&maps.kv[w], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, kv.base[w] + (int64_t)layer * kv.stride_layer * 2, dims,
+               strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return maps;
+  maps.on = 1;
+  return maps;
+}
+
 template <int D, int FMT, int NT>
 cudaError_t run(const AttnState& st, const AttnDims& dm, const Geometry& ge, int layer, const Batch& ba, const Rows& q,
                 const Rows& out, float* lse, const KvDev& kv, cudaStream_t stream) {
-  return pdl_launch(attention_kernel<D, FMT, NT, sub_blocks(FMT, NT)>, kAttnCtas, threads_of(D), ge.smem_bytes, stream, st, dm, ge,
-                      layer, ba, q, out, lse, kv, dm.scale * 1.4426950408889634f);
+  return pdl_launch(attention_kernel<D, FMT, NT, sub_blocks(FMT, NT)>, kAttnCtas, threads_of(D), ge.smem_bytes + 1024,
+                    stream, st, dm, ge, layer, ba, q, out, lse, kv, cache_maps(dm, ge, layer, kv),
+                    dm.scale * 1.4426950408889634f);
 }
 
 template <int D, int FMT>
@@ -1094,7 +1221,7 @@ cudaError_t run_rows(const AttnState& st, const AttnDims& dm, const Geometry& ge
 template <int D, int FMT, int NT>
 cudaError_t prepare_one() {
   return cudaFuncSetAttribute(attention_kernel<D, FMT, NT, sub_blocks(FMT, NT)>,
-                              cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem);
+                              cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem + 1024);
 }
 
 template <int D, int FMT>

@@ -22,7 +22,7 @@ struct AttnState {
   int32_t* err;           // [1] sticky device error word
   const float* kv_scale;  // [2][L][H] or null (the caller's)
   float* part;            // partial results of split rows
-  int64_t* plan;          // [max_seqs + 1] tiles before each entry
+  int32_t* plan;          // [max_seqs + 1] tiles before each entry
 };
 
 // A batch as the entry points take it.

@@ -78,7 +78,7 @@ size_t carve(const AttnDims& d, AttnState* st, char* base) {
   };
   memset(st, 0, sizeof(*st));
   st->err = (int32_t*)take(4);
-  st->plan = (int64_t*)take(((size_t)d.S + 1) * 8);
+  st->plan = (int32_t*)take(((size_t)d.S + 1) * 4);
   st->part = (float*)take(attention_part_floats(d) * 4);
   return align_up(off, 256);
 }

@@ -50,12 +50,19 @@ EPIKV_PLAN int64_t entry_tiles(const AttnShape& s, int n, int len) {
   return t * s.groups;
 }
 
-EPIKV_PLAN int64_t first_tile(int cta, int64_t total) { return total * cta / kAttnCtas; }
+// A batch's tiles are counted in 32 bits; a thread's entries, of which 256 threads share the batch, may have so many.
+constexpr int64_t kMostTiles = (int64_t(1) << 23) - 1;
+
+// floor(total * cta / kAttnCtas) without 64-bit products
+EPIKV_PLAN int first_tile(int cta, int total) {
+  const unsigned q = (unsigned)total / kAttnCtas, r = (unsigned)total % kAttnCtas;
+  return (int)(q * cta + r * cta / kAttnCtas);
+}
 // The CTA whose share tile x is in.
-EPIKV_PLAN int cta_of_tile(int64_t x, int64_t total) { return (int)(((x + 1) * kAttnCtas - 1) / total); }
+EPIKV_PLAN int cta_of_tile(int x, int total) { return (int)((((uint64_t)x + 1) * kAttnCtas - 1) / (unsigned)total); }
 
 // ---- shared memory of a CTA: the ring of tiles, boxes to join a head's warps, barriers, the entries' first tiles
-constexpr int kAttnSmem = 226 * 1024;   // dynamic shared memory, at most
+constexpr int kAttnSmem = 225 * 1024;   // dynamic shared memory, at most (its start is moved up to a multiple of 1,024)
 constexpr int kMaxStages = 8;           // tiles of the ring
 constexpr int kMaxTile = 128;           // slots of a tile, at most
 
@@ -112,18 +119,20 @@ EPIKV_PLAN AttnGeometry attn_geometry(int H, int rep, int d, bool q4, int units,
   while (1 << tile_log < tile) ++tile_log;
   ge.sh = {(H + group - 1) / group, nt * 8, tile, rows_log, tile_log, rep, causal ? 1 : 0};
   if (!q4) {
-    ge.row_s = heads * d * 2 + 16;           // 16 past a multiple of 128: eight rows' 16-byte pieces fill the banks
+    // 16 slots' pieces of 64 channels stand together (2 KB), a row's eight 16-byte parts exchanged by its number mod 8:
+    // as a tensor copy with 128-byte swizzling leaves them, and eight rows' parts fall on different banks
+    ge.row_s = heads * d * 2;
   } else {
     // as in the cache, so that several rows come in one copy; parts of rows are laid out for the banks
     const int used = heads * (d / 2) + ((heads * (d / 16) + 15) & ~15);
     ge.row_s = H > group ? used + ((32 - used) & 127) : units * 2;
   }
   ge.order = attn_row_order(ge.row_s);
-  ge.half_bytes = (ge.sh.tile * ge.row_s + 127) & ~127;
+  ge.half_bytes = (ge.sh.tile * ge.row_s + 1023) & ~1023;
   // any group whose heads have several warps needs the boxes: half of the warps write one at a time
   const bool join = attn_teams(heads, group) > 1 || attn_teams(rest, group) > 1;
   const int boxes = join ? group / 2 * attn_box_floats(d, nt) * 4 : 0;
-  const int bars = (2 * kMaxStages + 1) * 8, pre = (n_seq + 1) * 8;
+  const int bars = (2 * kMaxStages + 1) * 8, pre = (n_seq + 1) * 4;
   ge.stages = (kAttnSmem - boxes - bars - pre) / (2 * ge.half_bytes);
   if (ge.stages > kMaxStages) ge.stages = kMaxStages;
   // A copying warp tells a place's turns apart by one bit.  It waits for tile j after it has filled tile j - copiers, for

@@ -26,9 +26,9 @@ int geometry_holds(int H, int rep, int d, int q4, int units, int n_seq, int max_
   unsigned rows = 0;
   for (int r = 0; r < 8; ++r) rows |= 1u << (g.order >> (4 * r) & 7);
   NEED(rows == 255 && !(g.order & 0x88888888u));
-  NEED(g.row_s % 16 == 0 && g.half_bytes % 128 == 0 && g.half_bytes >= g.sh.tile * g.row_s);
+  NEED(g.row_s % 16 == 0 && g.half_bytes % 1024 == 0 && g.half_bytes >= g.sh.tile * g.row_s);
   NEED(g.join_off >= g.stages * 2 * g.half_bytes && g.join_off % 16 == 0 && g.bar_off % 8 == 0 && g.pre_off % 8 == 0);
-  NEED(g.pre_off >= g.bar_off + (2 * kMaxStages + 1) * 8 && g.smem_bytes >= g.pre_off + (n_seq + 1) * 8);
+  NEED(g.pre_off >= g.bar_off + (2 * kMaxStages + 1) * 8 && g.smem_bytes >= g.pre_off + (n_seq + 1) * 4);
   NEED(g.sh.groups * group >= H && (g.sh.groups - 1) * group < H);
   for (int i = 0; i < g.sh.groups; ++i) {
     const int heads = H - i * group < group ? H - i * group : group;
@@ -55,13 +55,16 @@ int geometry_holds(int H, int rep, int d, int q4, int units, int n_seq, int max_
 
 int shares_hold(int H, int rep, int d, int q4, int units, int max_new, int causal, int n_seq, const int* n, const int* len) {
   const AttnGeometry g = attn_geometry(H, rep, d, q4, units, n_seq, max_new, causal);
-  int64_t total = 0;
-  for (int b = 0; b < n_seq; ++b) total += entry_tiles(g.sh, n[b], len[b]);
-  if (!total) return 0;
+  int64_t sum = 0;
+  for (int b = 0; b < n_seq; ++b) sum += entry_tiles(g.sh, n[b], len[b]);
+  if (!sum) return 0;
+  NEED(sum < int64_t(1) << 31);
+  const int total = (int)sum;
+  for (int c = 0; c <= kAttnCtas; ++c) NEED(first_tile(c, total) == sum * c / kAttnCtas);
   NEED(first_tile(0, total) == 0 && first_tile(kAttnCtas, total) == total);
   for (int c = 0; c < kAttnCtas; ++c) NEED(first_tile(c, total) <= first_tile(c + 1, total));
   int parts[kAttnCtas][2] = {};
-  int64_t at = 0;
+  int at = 0;
   for (int b = 0; b < n_seq; ++b)
     for (int group = 0; group < g.sh.groups; ++group)
       for (int run = 0; run < row_runs(g.sh, n[b]); ++run) {
@@ -70,7 +73,7 @@ int shares_hold(int H, int rep, int d, int q4, int units, int max_new, int causa
         NEED((int64_t)t * g.sh.tile >= slots_seen(g.sh, n[b], len[b], run));
         const int c0 = cta_of_tile(at, total), c1 = cta_of_tile(at + t - 1, total);
         NEED(c0 >= 0 && c1 >= c0 && c1 < kAttnCtas);
-        for (int64_t x = at; x < at + t; ++x) {
+        for (int x = at; x < at + t; ++x) {
           const int c = cta_of_tile(x, total);
           NEED(first_tile(c, total) <= x && x < first_tile(c + 1, total));
         }
