@@ -19,32 +19,59 @@ namespace epikv {
 namespace {
 
 constexpr int kBlock = 128;
-constexpr int kBatch = 4;  // heads that a thread has in flight
+
+// V values as they stand in memory: what a thread has in flight takes no more registers than that.
+template <typename T, int V>
+struct Raw {
+  T v;
+};
+template <typename T>
+struct Raw<T, 8> {
+  uint4 v[sizeof(T) / 2];
+};
+
+template <typename T, int V>
+__device__ __forceinline__ void load_raw(const T* p, Raw<T, V>& r) {
+  if constexpr (V == 1) {
+    r.v = *p;
+  } else {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.v[i] = reinterpret_cast<const uint4*>(p)[i];
+  }
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void to_float(const Raw<T, V>& r, float* f) {
+  if constexpr (V == 1) {
+    if constexpr (sizeof(T) == 4) f[0] = r.v;
+    else if constexpr (__is_same(T, __half)) f[0] = __half2float(r.v);
+    else f[0] = __bfloat162float(r.v);
+  } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      f[4 * i] = __uint_as_float(r.v[i].x);
+      f[4 * i + 1] = __uint_as_float(r.v[i].y);
+      f[4 * i + 2] = __uint_as_float(r.v[i].z);
+      f[4 * i + 3] = __uint_as_float(r.v[i].w);
+    }
+  } else if constexpr (__is_same(T, __half)) {
+    const uint32_t w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      f[2 * i] = v.x;
+      f[2 * i + 1] = v.y;
+    }
+  } else {
+    unpack8(r.v[0], f);
+  }
+}
 
 template <typename T, int V>
 __device__ __forceinline__ void load_v(const T* p, float* f) {
-  if constexpr (V == 1) {
-    if constexpr (sizeof(T) == 4) f[0] = *p;
-    else if constexpr (sizeof(T) == 2 && !__is_same(T, __half)) f[0] = __bfloat162float(*p);
-    else f[0] = __half2float(*p);
-  } else if constexpr (sizeof(T) == 4) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-  } else {
-    const uint4 a = *reinterpret_cast<const uint4*>(p);
-    if constexpr (__is_same(T, __half)) {
-      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-        f[2 * i] = v.x;
-        f[2 * i + 1] = v.y;
-      }
-    } else {
-      unpack8(a, f);
-    }
-  }
+  Raw<T, V> r;
+  load_raw<T, V>(p, r);
+  to_float<T, V>(r, f);
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -141,9 +168,11 @@ __global__ void rope_table_kernel(epikv_rope_config c, int n_pos, float2* table)
   }
 }
 
+// kBatch heads of a thread are in flight; their loads go out before the position and the table's row are known.
 template <typename T, int V>
 __global__ void __launch_bounds__(kBlock) rope_kernel(int32_t* err, Rows x, Rows y, const int32_t* __restrict__ pos,
                                                       RopeDev r, int n_tokens, int heads, int d, float sign) {
+  constexpr int kBatch = sizeof(T) == 4 ? 2 : 3;
   const int U = d / (2 * V), slots = kBlock / U;  // units of a head; heads that the block takes at once
   const int u = threadIdx.x % U, slot = threadIdx.x / U;
   const int tpb = max(1, slots / heads);          // tokens of this block
@@ -151,35 +180,43 @@ __global__ void __launch_bounds__(kBlock) rope_kernel(int32_t* err, Rows x, Rows
   if (slot >= tpb * step) return;
   const int64_t token = (int64_t)blockIdx.x * tpb + slot / step;
   if (token >= n_tokens) return;
-  pdl_wait();
-  const int p = pos[token];
-  if ((unsigned)p >= (unsigned)r.n_pos) {
-    set_error(err, EPIKV_DEV_POSITION);
-    return;
-  }
   const bool turned = u < r.dim / (2 * V);
-  float c[V], s[V];
-  if (turned) load_angles<V>(r, p, u, sign, c, s);
   const int2 ch = unit_channels<V>(u, r.dim, r.layout);
   const T* src = reinterpret_cast<const T*>(x.p) + token * x.st;
   T* dst = reinterpret_cast<T*>(y.p) + token * y.st;
+  float c[V], s[V];
+  int p = 0;
+  bool first = true;
+  pdl_wait();
   for (int h0 = slot % step; h0 < heads; h0 += step * kBatch) {
-    float a[kBatch][V], b[kBatch][V];
+    Raw<T, V> a[kBatch], b[kBatch];
+    if (first) p = pos[token];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       const int h = h0 + k * step;
       if (h < heads) {
-        load_v<T, V>(src + h * x.sh + ch.x, a[k]);
-        load_v<T, V>(src + h * x.sh + ch.y, b[k]);
+        load_raw<T, V>(src + h * x.sh + ch.x, a[k]);
+        load_raw<T, V>(src + h * x.sh + ch.y, b[k]);
       }
+    }
+    if (first) {
+      if ((unsigned)p >= (unsigned)r.n_pos) {
+        set_error(err, EPIKV_DEV_POSITION);
+        return;
+      }
+      if (turned) load_angles<V>(r, p, u, sign, c, s);
+      first = false;
     }
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       const int h = h0 + k * step;
       if (h < heads) {
-        if (turned) turn_unit<V>(a[k], b[k], c, s, r.layout);
-        store_v<T, V>(dst + h * y.sh + ch.x, a[k]);
-        store_v<T, V>(dst + h * y.sh + ch.y, b[k]);
+        float fa[V], fb[V];
+        to_float<T, V>(a[k], fa);
+        to_float<T, V>(b[k], fb);
+        if (turned) turn_unit<V>(fa, fb, c, s, r.layout);
+        store_v<T, V>(dst + h * y.sh + ch.x, fa);
+        store_v<T, V>(dst + h * y.sh + ch.y, fb);
       }
     }
   }
@@ -194,7 +231,7 @@ __device__ __forceinline__ uint2 quantize16(const float* x, float g, uint32_t* s
   bool nan = false;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    y[i] = __fdiv_rn(x[i], g);
+    y[i] = g == 1.f ? x[i] : __fdiv_rn(x[i], g);
     nan |= y[i] != y[i];
     top = fmaxf(top, fabsf(y[i]));
   }
@@ -263,58 +300,65 @@ template <int V, int kFmt>
 __global__ void __launch_bounds__(kBlock) append_kernel(AttnState st, AttnDims dm, int layer, Batch ba,
                                                         const int32_t* __restrict__ pos, Rows q, Rows qo, Rows kr,
                                                         Rows vr, RopeDev r, KvDev kv) {
+  constexpr int kBatch = 3;
+  using bf = __nv_bfloat16;
   const int b = blockIdx.y, i = blockIdx.x;
+  const int nq = q.p ? dm.Hq : 0;
+  const int n = nq + (kFmt == EPIKV_CACHE_BF16 ? 2 * dm.H : 0);
+  const int U = dm.d / (2 * V), slots = kBlock / U;
+  const int u = threadIdx.x % U, slot = threadIdx.x / U;
+  const bool turned = u < r.dim / (2 * V);
+  const int2 ch = unit_channels<V>(u, r.dim, r.layout);
   Entry e;
   pdl_wait();
+  const int p0 = r.dim ? pos[b] : 0;
   if (!batch_entry(ba, dm, b, true, st.err, &e) || i >= e.n) return;
-  int p = 0;
-  if (r.dim) {
-    const int64_t at = (int64_t)pos[b] + i;
-    if (at < 0 || at >= r.n_pos) {
-      set_error(st.err, EPIKV_DEV_POSITION);
-      return;
+  const int64_t token = (int64_t)e.tok0 + i;
+  const bf* q0 = reinterpret_cast<const bf*>(q.p) + token * q.st;
+  const bf* k0 = reinterpret_cast<const bf*>(kr.p) + token * kr.st;
+  const bf* v0 = reinterpret_cast<const bf*>(vr.p) + token * vr.st;
+  // the first heads' loads go out with those of the position's row and the slot's block
+  Raw<bf, V> a[kBatch], z[kBatch];
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int h = h0 + k * slots;
+      if (h < n) {
+        const bf* src = h < nq ? q0 + h * q.sh : h < nq + dm.H ? k0 + (h - nq) * kr.sh : v0 + (h - nq - dm.H) * vr.sh;
+        load_raw<bf, V>(src + ch.x, a[k]);
+        load_raw<bf, V>(src + ch.y, z[k]);
+      }
     }
-    p = (int)at;
+  };
+  if (slot < slots) load(slot);
+  const int p = (int)((unsigned)p0 + (unsigned)i);
+  if (r.dim && (p0 < 0 || p0 >= r.n_pos || i >= r.n_pos - p0)) {
+    set_error(st.err, EPIKV_DEV_POSITION);
+    return;
   }
+  float c[V], s[V];
+  if (turned) load_angles<V>(r, p, u, 1.f, c, s);
   const int64_t row = kv_row_offset(kv, layer, e.seq, e.len + i, dm.T);
   if (row < 0) {
     set_error(st.err, EPIKV_DEV_SLOT);
     return;
   }
-  const int64_t token = (int64_t)e.tok0 + i;
-  const int nq = q.p ? dm.Hq : 0;
-  const int n = nq + (kFmt == EPIKV_CACHE_BF16 ? 2 * dm.H : 0);
-  const int U = dm.d / (2 * V), slots = kBlock / U;
-  const int u = threadIdx.x % U, slot = threadIdx.x / U;
-  using bf = __nv_bfloat16;
-  const bool turned = u < r.dim / (2 * V);
-  float c[V], s[V];
-  if (turned) load_angles<V>(r, p, u, 1.f, c, s);
-  const int2 ch = unit_channels<V>(u, r.dim, r.layout);
   if (slot < slots)
     for (int h0 = slot; h0 < n; h0 += slots * kBatch) {
-      float a[kBatch][V], z[kBatch][V];
+      if (h0 != slot) load(h0);
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
         const int h = h0 + k * slots;
         if (h < n) {
-          const Rows& from = h < nq ? q : h < nq + dm.H ? kr : vr;
-          const int hh = h < nq ? h : (h - nq) % dm.H;
-          const bf* src = reinterpret_cast<const bf*>(from.p) + token * from.st + hh * from.sh;
-          load_v<bf, V>(src + ch.x, a[k]);
-          load_v<bf, V>(src + ch.y, z[k]);
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const int h = h0 + k * slots;
-        if (h < n) {
-          if (turned && h < nq + dm.H) turn_unit<V>(a[k], z[k], c, s, r.layout);
-          bf* dst;
-          if (h < nq) dst = reinterpret_cast<bf*>(qo.p) + token * qo.st + h * qo.sh;
-          else dst = reinterpret_cast<bf*>(kv.base[h >= nq + dm.H]) + row + (int64_t)((h - nq) % dm.H) * dm.d;
-          store_v<bf, V>(dst + ch.x, a[k]);
-          store_v<bf, V>(dst + ch.y, z[k]);
+          float fa[V], fz[V];
+          to_float<bf, V>(a[k], fa);
+          to_float<bf, V>(z[k], fz);
+          if (turned && h < nq + dm.H) turn_unit<V>(fa, fz, c, s, r.layout);
+          bf* dst = h < nq ? reinterpret_cast<bf*>(qo.p) + token * qo.st + h * qo.sh
+                    : h < nq + dm.H ? reinterpret_cast<bf*>(kv.base[0]) + row + (int64_t)(h - nq) * dm.d
+                                    : reinterpret_cast<bf*>(kv.base[1]) + row + (int64_t)(h - nq - dm.H) * dm.d;
+          store_v<bf, V>(dst + ch.x, fa);
+          store_v<bf, V>(dst + ch.y, fz);
         }
       }
     }
@@ -324,15 +368,15 @@ __global__ void __launch_bounds__(kBlock) append_kernel(AttnState st, AttnDims d
       const int which = j / (dm.H * G), h = j / G % dm.H, g = j % G;
       float x[16];
       if (which == 0) {
-        turned16(reinterpret_cast<const bf*>(kr.p) + token * kr.st + h * kr.sh, g * 16, r, p, x);
+        turned16(k0 + h * kr.sh, g * 16, r, p, x);
       } else {
-        const bf* src = reinterpret_cast<const bf*>(vr.p) + token * vr.st + h * vr.sh + g * 16;
+        const bf* src = v0 + h * vr.sh + g * 16;
         load_v<bf, 8>(src, x);
         load_v<bf, 8>(src + 8, x + 8);
       }
       uint32_t scale;
       const uint2 code = quantize16(x, head_scale(st, dm, which, layer, h), &scale);
-      char* dst = kv.base[which] + row * 2;
+      char* dst = (which ? kv.base[1] : kv.base[0]) + row * 2;
       *reinterpret_cast<uint2*>(dst + h * (dm.d / 2) + g * 8) = code;
       dst[scale_offset(dm, h) + g] = (char)scale;
     }
@@ -360,10 +404,10 @@ __global__ void __launch_bounds__(kBlock) cache_read_kernel(AttnState st, AttnDi
   }
   using bf = __nv_bfloat16;
   for (int w = 0; w < 2; ++w) {
-    const Rows& to = w ? v : k;
-    if (!to.p) continue;
-    bf* dst = reinterpret_cast<bf*>(to.p) + i * to.st + h * to.sh + g * 16;
-    const char* src = kv.base[w] + row * 2;
+    char* to = w ? v.p : k.p;
+    if (!to) continue;
+    bf* dst = reinterpret_cast<bf*>(to) + i * (w ? v.st : k.st) + h * (w ? v.sh : k.sh) + g * 16;
+    const char* src = (w ? kv.base[1] : kv.base[0]) + row * 2;
     if (dm.fmt == EPIKV_CACHE_BF16) {
       const uint4* s = reinterpret_cast<const uint4*>(src + (h * dm.d + g * 16) * 2);
       reinterpret_cast<uint4*>(dst)[0] = s[0];
