@@ -614,24 +614,27 @@ __global__ void __launch_bounds__(threads_of(D), 1)
     const int h0 = w->group * attn_group(D), heads = min(attn_group(D), dm.H - h0);
     const int teams = attn_teams(heads, kWarps);
     const bool idle = warp >= teams * heads;
-    const int head = warp % heads, team = warp / heads;
+    const int head = warp % heads, team = idle ? 0 : warp / heads;   // idle warps follow team 0 and keep nothing
     const int kh = h0 + head;
     const int row0 = w->run * sh.rows, nrows = min(sh.rows, rows_of(sh, e.n) - row0);
 
     // where the lane reads in a tile: keys are rows (slots), values columns of the first operand
     const uint32_t ring0 = smem_u32(smem);
-    const uint32_t hop = teams * 16 * ge.row_s, eight = 8 * ge.row_s;   // to the warp's next block of slots; 8 slots on
+    // where the warp's blocks of slots start, and to its next one (what lies behind the tile: a block of it, masked);
+    // 8 slots on
+    const int block0 = team * 16 < sh.tile ? team * 16 : 0;
+    const uint32_t hop = teams * 16 < sh.tile ? teams * 16 * ge.row_s : 0, eight = 8 * ge.row_s;
     const int k0 = kBf16 ? 2 * t : slot_of_row(ge.order, 2 * t), k1 = kBf16 ? 2 * t + 1 : slot_of_row(ge.order, 2 * t + 1);
     uint32_t key_code, key_scale, value_code, value_scale, odd = 0;
     if constexpr (kBf16) {
-      const uint32_t mine = team * 16 * ge.row_s + head * (D / 64) * 2048;
+      const uint32_t mine = block0 * ge.row_s + head * (D / 64) * 2048;
       key_code = mine + (lane & 15) * 128;
       key_scale = (lane >> 4) ^ (lane & 7);          // of a row's parts: 2 j + this lane's half, exchanged by the row
       value_code = ge.half_bytes + mine + ((lane & 7) + (lane >> 4) * 8) * 128;
       value_scale = ((lane >> 3) & 1) ^ (lane & 7);
     } else {
-      const uint32_t key_row = (team * 16 + slot_of_row(ge.order, g)) * ge.row_s;
-      const uint32_t value_row = (team * 16 + k0) * ge.row_s, scales = heads * (D / 2) + head * (D / 16);
+      const uint32_t key_row = (block0 + slot_of_row(ge.order, g)) * ge.row_s;
+      const uint32_t value_row = (block0 + k0) * ge.row_s, scales = heads * (D / 2) + head * (D / 16);
       key_code = key_row + head * (D / 2) + t * (D / 8);
       key_scale = key_row + scales + t * (D / 64);
       value_code = ge.half_bytes + value_row + head * (D / 2) + g * (D / 16);
@@ -698,87 +701,141 @@ __global__ void __launch_bounds__(threads_of(D), 1)
         for (int i = 0; i < 4; ++i) o[j][nt][i] = 0.f;
     }
 
-    const int end = min(w->at + w->tiles, tiles);
-    int s0 = (x - w->at) * sh.tile;
-    for (; x < end; ++x, s0 += sh.tile) {
-      // ---- scores
-      float s[SUB][NT][4];
-      wait(&full[stage], phase);
-      const uint32_t base = ring0 + stage * (2 * ge.half_bytes);
-      {
+    // The scores of the tile at `base`.
+    auto keys = [&](uint32_t base, float (&s)[SUB][NT][4]) {
 #pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-          const int sub = u * teams + team;
+      for (int u = 0; u < SUB; ++u) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[u][nt][i] = 0.f;
+        if constexpr (kBf16) {
+          const uint32_t addr = base + u * hop + key_code;
+#pragma unroll
+          for (int j = 0; j < KS; ++j) {
+            uint32_t a[4];
+            ldmatrix4<false>(a, addr + j / 4 * 2048 + (((2 * j & 6) ^ key_scale) << 4));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma<FMT>(s[u][nt], a, qf[nt][j][0], qf[nt][j][1]);
+          }
+        } else {
+          const uint32_t at = base + u * hop;
+          uint32_t w0[D / 32], w1[D / 32];
+          lds_words(w0, at + key_code);
+          lds_words(w1, at + key_code + eight);
+          uint32_t s0x[D / 128 + 1], s1x[D / 128 + 1];   // the scales, two a register
+          if constexpr (D == 64) {
+            s0x[0] = e4m3x2_to_half2((uint16_t)lds_u8(at + key_scale));
+            s1x[0] = e4m3x2_to_half2((uint16_t)lds_u8(at + key_scale + eight));
+          } else {
+#pragma unroll
+            for (int p = 0; p < D / 128; ++p) {
+              s0x[p] = e4m3x2_to_half2((uint16_t)lds_u16(at + key_scale + 2 * p));
+              s1x[p] = e4m3x2_to_half2((uint16_t)lds_u16(at + key_scale + eight + 2 * p));
+            }
+          }
+          float two[NT][4];   // a second chain of sums, half the first one's latencies
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[u][nt][i] = 0.f;
-          if (idle || sub * 16 >= sh.tile) continue;
-          if constexpr (kBf16) {
-            const uint32_t addr = base + u * hop + key_code;
+            for (int i = 0; i < 4; ++i) two[nt][i] = 0.f;
 #pragma unroll
-            for (int j = 0; j < KS; ++j) {
+          for (int v = 0; v < D / 32; ++v) {   // eight channels of a lane: two blocks
+            uint32_t x0[4], x1[4];
+            e2m1x8_to_half2(w0[v], x0);
+            e2m1x8_to_half2(w1[v], x1);
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
               uint32_t a[4];
-              ldmatrix4<false>(a, addr + j / 4 * 2048 + (((2 * j & 6) ^ key_scale) << 4));
+              if ((v / 2) % 2 == 0) {
+                a[0] = hmul2_by<false>(x0[2 * y], s0x[v / 4]);
+                a[1] = hmul2_by<false>(x1[2 * y], s1x[v / 4]);
+                a[2] = hmul2_by<false>(x0[2 * y + 1], s0x[v / 4]);
+                a[3] = hmul2_by<false>(x1[2 * y + 1], s1x[v / 4]);
+              } else {
+                a[0] = hmul2_by<true>(x0[2 * y], s0x[v / 4]);
+                a[1] = hmul2_by<true>(x1[2 * y], s1x[v / 4]);
+                a[2] = hmul2_by<true>(x0[2 * y + 1], s0x[v / 4]);
+                a[3] = hmul2_by<true>(x1[2 * y + 1], s1x[v / 4]);
+              }
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma<FMT>(s[u][nt], a, qf[nt][j][0], qf[nt][j][1]);
-            }
-          } else {
-            const uint32_t at = base + u * hop;
-            uint32_t w0[D / 32], w1[D / 32];
-            lds_words(w0, at + key_code);
-            lds_words(w1, at + key_code + eight);
-            uint32_t s0x[D / 128 + 1], s1x[D / 128 + 1];   // the scales, two a register
-            if constexpr (D == 64) {
-              s0x[0] = e4m3x2_to_half2((uint16_t)lds_u8(at + key_scale));
-              s1x[0] = e4m3x2_to_half2((uint16_t)lds_u8(at + key_scale + eight));
-            } else {
-#pragma unroll
-              for (int p = 0; p < D / 128; ++p) {
-                s0x[p] = e4m3x2_to_half2((uint16_t)lds_u16(at + key_scale + 2 * p));
-                s1x[p] = e4m3x2_to_half2((uint16_t)lds_u16(at + key_scale + eight + 2 * p));
+              for (int nt = 0; nt < NT; ++nt) {
+                if (y == 1) mma<FMT>(two[nt], a, qf[nt][2 * v + y][0], qf[nt][2 * v + y][1]);
+                else
+                mma<FMT>(s[u][nt], a, qf[nt][2 * v + y][0], qf[nt][2 * v + y][1]);
               }
             }
-            float two[NT][4];   // a second chain of sums, half the first one's latencies
+          }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) two[nt][i] = 0.f;
+            for (int i = 0; i < 4; ++i) s[u][nt][i] += two[nt][i];
+        }
+      }
+    };
+    // Gives block mt of the operand (channels x slots; the lane's slots are k0, k1 and 8 on) to f, for every mt.
+    auto each = [&](uint32_t base, int u, auto&& f) {
+      if constexpr (kBf16) {
+        const uint32_t addr = base + u * hop + value_code;
 #pragma unroll
-            for (int v = 0; v < D / 32; ++v) {   // eight channels of a lane: two blocks
-              uint32_t x0[4], x1[4];
-              e2m1x8_to_half2(w0[v], x0);
-              e2m1x8_to_half2(w1[v], x1);
+        for (int mt = 0; mt < KS; ++mt) {
+          uint32_t a[4];
+          ldmatrix4<true>(a, addr + mt / 4 * 2048 + (((2 * mt & 6) ^ value_scale) << 4));
+          f(mt, a);
+        }
+      } else {
+        const uint32_t p0 = base + u * hop + value_code, p1 = p0 + odd;
+        const uint32_t c0 = base + u * hop + value_scale, c1 = c0 + odd;
+        uint32_t wa[D / 64], wb[D / 64], wc[D / 64], wd[D / 64];
+        lds_words(wa, p0);
+        lds_words(wb, p1);
+        lds_words(wc, p0 + eight);
+        lds_words(wd, p1 + eight);
+        uint32_t sl = 0, sh8 = 0;
 #pragma unroll
-              for (int y = 0; y < 2; ++y) {
-                uint32_t a[4];
-                if ((v / 2) % 2 == 0) {
-                  a[0] = hmul2_by<false>(x0[2 * y], s0x[v / 4]);
-                  a[1] = hmul2_by<false>(x1[2 * y], s1x[v / 4]);
-                  a[2] = hmul2_by<false>(x0[2 * y + 1], s0x[v / 4]);
-                  a[3] = hmul2_by<false>(x1[2 * y + 1], s1x[v / 4]);
-                } else {
-                  a[0] = hmul2_by<true>(x0[2 * y], s0x[v / 4]);
-                  a[1] = hmul2_by<true>(x1[2 * y], s1x[v / 4]);
-                  a[2] = hmul2_by<true>(x0[2 * y + 1], s0x[v / 4]);
-                  a[3] = hmul2_by<true>(x1[2 * y + 1], s1x[v / 4]);
-                }
+        for (int v = 0; v < D / 64; ++v) {   // eight channels: four blocks
+          if (v % 2 == 0) {
+            sl = e4m3x2_to_half2((uint16_t)(lds_u8(c0 + v / 2) + (lds_u8(c1 + v / 2) << 8)));
+            sh8 = e4m3x2_to_half2((uint16_t)(lds_u8(c0 + eight + v / 2) + (lds_u8(c1 + eight + v / 2) << 8)));
+          }
+          // pairs of slots instead of pairs of channels: even channels, odd channels
+          constexpr uint32_t kLow = 0x0f0f0f0fu;
+          uint32_t e0[4], e1[4], e2[4], e3[4];
+          e2m1x8_to_half2((wa[v] & kLow) | ((wb[v] << 4) & ~kLow), e0);
+          e2m1x8_to_half2(((wa[v] >> 4) & kLow) | (wb[v] & ~kLow), e1);
+          e2m1x8_to_half2((wc[v] & kLow) | ((wd[v] << 4) & ~kLow), e2);
+          e2m1x8_to_half2(((wc[v] >> 4) & kLow) | (wd[v] & ~kLow), e3);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                  if (y == 1) mma<FMT>(two[nt], a, qf[nt][2 * v + y][0], qf[nt][2 * v + y][1]);
-                  else
-                  mma<FMT>(s[u][nt], a, qf[nt][2 * v + y][0], qf[nt][2 * v + y][1]);
-                }
-              }
-            }
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) s[u][nt][i] += two[nt][i];
+          for (int y = 0; y < 4; ++y) {
+            uint32_t a[4] = {hmul2(e0[y], sl), hmul2(e1[y], sl), hmul2(e2[y], sh8), hmul2(e3[y], sh8)};
+            f(4 * v + y, a);
           }
         }
       }
+    };
+    // Adds the tile's values, weighted, to the outputs.
+    auto values = [&](uint32_t base, const uint32_t (&pb)[SUB][NT][kBf16 ? 4 : 2]) {
+#pragma unroll
+      for (int u = 0; u < SUB; ++u)
+        each(base, u, [&](int mt, uint32_t (&a)[4]) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            mma<FMT>(o[mt][nt], a, pb[u][nt][0], pb[u][nt][1]);
+            if constexpr (kBf16) mma<FMT>(o[mt][nt], a, pb[u][nt][2], pb[u][nt][3]);
+          }
+        });
+    };
 
+    const int end = min(w->at + w->tiles, tiles);
+    int s0 = (x - w->at) * sh.tile;
+    float s[SUB][NT][4];
+    bool scored = false;
+    for (; x < end; ++x, s0 += sh.tile) {
+      const uint32_t base = ring0 + stage * (2 * ge.half_bytes);
+      if (!scored) {
+        wait(&full[stage], phase);
+        keys(base, s);
+      }
       // ---- probabilities.  They are taken against a maximum that is moved only when a score passes it by 2^kSlack: the
       // sums and outputs then need no rescaling, and the warp no exchange, in nearly every tile.
       if (s0 + sh.tile > least || idle || SUB * teams * 16 > sh.tile) {
@@ -860,104 +917,63 @@ __global__ void __launch_bounds__(threads_of(D), 1)
         }
       }
 
-      // ---- their sum of values
-      {
+      // ---- their sum of values, and the next tile's scores: two chains that do not wait for each other
+      // Slots that some rows see and others do not may hold an infinity or a NaN, which a probability of 0 does not
+      // silence: then the rows of each token go by themselves, the values that they do not see taken as 0.
+      bool apart = false;
+      if (s0 + sh.tile > least) {
+        constexpr uint32_t kExp = kBf16 ? 0x7f80u : 0x7c00u;
+#pragma unroll 1
+        for (int u = 0; u < SUB; ++u)
+          each(base, u, [&](int, uint32_t (&a)[4]) {
 #pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-          const int sub = u * teams + team;
-          if (idle || sub * 16 >= sh.tile) continue;
-          const int at = s0 + sub * 16;
-          // Gives block mt of the operand (channels x slots; the lane's slots are k0, k1 and 8 on) to f, for every mt.
-          auto each = [&](auto&& f) {
-            if constexpr (kBf16) {
-              const uint32_t addr = base + u * hop + value_code;
+            for (int i = 0; i < 4; ++i) apart |= (a[i] & kExp) == kExp || (a[i] >> 16 & kExp) == kExp;
+          });
+        apart = __any_sync(0xffffffffu, apart);
+      }
+      int next = stage + 1;
+      uint32_t next_phase = phase;
+      if (next == ge.stages) {
+        next = 0;
+        next_phase ^= 1;
+      }
+      scored = !apart && x + 1 < end;
+      if (scored) {
+        wait(&full[next], next_phase);
+        keys(ring0 + next * (2 * ge.half_bytes), s);
+        values(base, pb);
+      } else if (!apart) {
+        values(base, pb);
+      } else {
+        const int first_row = w->run * sh.rows, last_row = min(first_row + sh.rows, rows_of(sh, w->e.n)) - 1;
 #pragma unroll
-              for (int mt = 0; mt < KS; ++mt) {
-                uint32_t a[4];
-                ldmatrix4<true>(a, addr + mt / 4 * 2048 + (((2 * mt & 6) ^ value_scale) << 4));
-                f(mt, a);
-              }
-            } else {
-              const uint32_t p0 = base + u * hop + value_code, p1 = p0 + odd;
-              const uint32_t c0 = base + u * hop + value_scale, c1 = c0 + odd;
-              uint32_t wa[D / 64], wb[D / 64], wc[D / 64], wd[D / 64];
-              lds_words(wa, p0);
-              lds_words(wb, p1);
-              lds_words(wc, p0 + eight);
-              lds_words(wd, p1 + eight);
-              uint32_t sl = 0, sh8 = 0;
-#pragma unroll
-              for (int v = 0; v < D / 64; ++v) {   // eight channels: four blocks
-                if (v % 2 == 0) {
-                  sl = e4m3x2_to_half2((uint16_t)(lds_u8(c0 + v / 2) + (lds_u8(c1 + v / 2) << 8)));
-                  sh8 = e4m3x2_to_half2((uint16_t)(lds_u8(c0 + eight + v / 2) + (lds_u8(c1 + eight + v / 2) << 8)));
-                }
-                // pairs of slots instead of pairs of channels: even channels, odd channels
-                constexpr uint32_t kLow = 0x0f0f0f0fu;
-                uint32_t e0[4], e1[4], e2[4], e3[4];
-                e2m1x8_to_half2((wa[v] & kLow) | ((wb[v] << 4) & ~kLow), e0);
-                e2m1x8_to_half2(((wa[v] >> 4) & kLow) | (wb[v] & ~kLow), e1);
-                e2m1x8_to_half2((wc[v] & kLow) | ((wd[v] << 4) & ~kLow), e2);
-                e2m1x8_to_half2(((wc[v] >> 4) & kLow) | (wd[v] & ~kLow), e3);
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                  uint32_t a[4] = {hmul2(e0[y], sl), hmul2(e1[y], sl), hmul2(e2[y], sh8), hmul2(e3[y], sh8)};
-                  f(4 * v + y, a);
-                }
-              }
-            }
-          };
-          // Slots that some rows see and others do not may hold an infinity or a NaN, which a probability of 0 does not
-          // silence: then the rows of each token go by themselves, the values that they do not see taken as 0.
-          bool apart = false;
-          if (at + 16 > least) {
-            constexpr uint32_t kExp = kBf16 ? 0x7f80u : 0x7c00u;
-            each([&](int, uint32_t (&a)[4]) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                apart |= (a[i] & kExp) == kExp || (a[i] >> 16 & kExp) == kExp;
-            });
-            apart = __any_sync(0xffffffffu, apart);
-          }
-          if (!apart) {
-            each([&](int mt, uint32_t (&a)[4]) {
+        for (int u = 0; u < SUB; ++u)
+          for (int i = first_row / sh.rep; i <= last_row / sh.rep; ++i) {
+            // of these slots, those that token i sees
+            const int n = w->e.len + (sh.causal ? i + 1 : 0) - (s0 + (u * teams + team) * 16);
+            const uint32_t m0 = (k0 < n ? 0xffffu : 0u) | (k1 < n ? 0xffff0000u : 0u);
+            const uint32_t m8 = (k0 + 8 < n ? 0xffffu : 0u) | (k1 + 8 < n ? 0xffff0000u : 0u);
+            each(base, u, [&](int mt, uint32_t (&a)[4]) {
+              const uint32_t z[4] = {a[0] & m0, a[1] & m0, a[2] & m8, a[3] & m8};
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
-                mma<FMT>(o[mt][nt], a, pb[u][nt][0], pb[u][nt][1]);
-                if constexpr (kBf16) mma<FMT>(o[mt][nt], a, pb[u][nt][2], pb[u][nt][3]);
+                // only the columns of token i; the others keep their sums
+                float keep[4];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) keep[y] = o[mt][nt][y];
+                mma<FMT>(o[mt][nt], z, pb[u][nt][0], pb[u][nt][1]);
+                if constexpr (kBf16) mma<FMT>(o[mt][nt], z, pb[u][nt][2], pb[u][nt][3]);
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                  if ((first_row + nt * 8 + 2 * t + (y & 1)) / sh.rep != i) o[mt][nt][y] = keep[y];
               }
             });
-          } else {
-            const int first_row = w->run * sh.rows, last_row = min(first_row + sh.rows, rows_of(sh, w->e.n)) - 1;
-            for (int i = first_row / sh.rep; i <= last_row / sh.rep; ++i) {
-              const int n = w->e.len + (sh.causal ? i + 1 : 0) - at;   // of these slots, those that token i sees
-              const uint32_t m0 = (k0 < n ? 0xffffu : 0u) | (k1 < n ? 0xffff0000u : 0u);
-              const uint32_t m8 = (k0 + 8 < n ? 0xffffu : 0u) | (k1 + 8 < n ? 0xffff0000u : 0u);
-              each([&](int mt, uint32_t (&a)[4]) {
-                const uint32_t z[4] = {a[0] & m0, a[1] & m0, a[2] & m8, a[3] & m8};
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                  // only the columns of token i; the others keep their sums
-                  float keep[4];
-#pragma unroll
-                  for (int y = 0; y < 4; ++y) keep[y] = o[mt][nt][y];
-                  mma<FMT>(o[mt][nt], z, pb[u][nt][0], pb[u][nt][1]);
-                  if constexpr (kBf16) mma<FMT>(o[mt][nt], z, pb[u][nt][2], pb[u][nt][3]);
-#pragma unroll
-                  for (int y = 0; y < 4; ++y)
-                    if ((first_row + nt * 8 + 2 * t + (y & 1)) / sh.rep != i) o[mt][nt][y] = keep[y];
-                }
-              });
-            }
           }
-        }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&empty[stage]);
-      if (++stage == ge.stages) {
-        stage = 0;
-        phase ^= 1;
-      }
+      stage = next;
+      phase = next_phase;
     }
 
     // ---- the end of the CTA's part of the item
