@@ -64,6 +64,19 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// The same, the sums starting at 0.
+template <int FMT>
+__device__ __forceinline__ void mma_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (FMT == EPIKV_CACHE_BF16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   uint32_t d;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
@@ -625,7 +638,8 @@ __global__ void __launch_bounds__(threads_of(D), 1)
     const int block0 = team * 16 < sh.tile ? team * 16 : 0;
     const uint32_t hop = teams * 16 < sh.tile ? teams * 16 * ge.row_s : 0, eight = 8 * ge.row_s;
     const int k0 = kBf16 ? 2 * t : slot_of_row(ge.order, 2 * t), k1 = kBf16 ? 2 * t + 1 : slot_of_row(ge.order, 2 * t + 1);
-    uint32_t key_code, key_scale, value_code, value_scale, odd = 0;
+    uint32_t key_code, key_scale, value_code, value_scale;
+    uint32_t key_code8 = 0, key_scale8 = 0, value_odd = 0, value_code8 = 0, value_odd8 = 0, scale_odd = 0, value_scale8 = 0, scale_odd8 = 0;
     if constexpr (kBf16) {
       const uint32_t mine = block0 * ge.row_s + head * (D / 64) * 2048;
       key_code = mine + (lane & 15) * 128;
@@ -639,7 +653,15 @@ __global__ void __launch_bounds__(threads_of(D), 1)
       key_scale = key_row + scales + t * (D / 64);
       value_code = ge.half_bytes + value_row + head * (D / 2) + g * (D / 16);
       value_scale = ge.half_bytes + value_row + scales + g * (D / 8) / 16;
-      odd = (k1 - k0) * ge.row_s;
+      const uint32_t odd = (k1 - k0) * ge.row_s;
+      key_code8 = key_code + eight;
+      key_scale8 = key_scale + eight;
+      value_odd = value_code + odd;
+      value_code8 = value_code + eight;
+      value_odd8 = value_odd + eight;
+      scale_odd = value_scale + odd;
+      value_scale8 = value_scale + eight;
+      scale_odd8 = scale_odd + eight;
     }
 
     // the queries as the second operand: column n of block nt is row nt * 8 + n
@@ -705,10 +727,6 @@ __global__ void __launch_bounds__(threads_of(D), 1)
     auto keys = [&](uint32_t base, float (&s)[SUB][NT][4]) {
 #pragma unroll
       for (int u = 0; u < SUB; ++u) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[u][nt][i] = 0.f;
         if constexpr (kBf16) {
           const uint32_t addr = base + u * hop + key_code;
 #pragma unroll
@@ -716,29 +734,28 @@ __global__ void __launch_bounds__(threads_of(D), 1)
             uint32_t a[4];
             ldmatrix4<false>(a, addr + j / 4 * 2048 + (((2 * j & 6) ^ key_scale) << 4));
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma<FMT>(s[u][nt], a, qf[nt][j][0], qf[nt][j][1]);
+            for (int nt = 0; nt < NT; ++nt) {
+              if (j == 0) mma_first<FMT>(s[u][nt], a, qf[nt][j][0], qf[nt][j][1]);
+              else mma<FMT>(s[u][nt], a, qf[nt][j][0], qf[nt][j][1]);
+            }
           }
         } else {
           const uint32_t at = base + u * hop;
           uint32_t w0[D / 32], w1[D / 32];
           lds_words(w0, at + key_code);
-          lds_words(w1, at + key_code + eight);
+          lds_words(w1, at + key_code8);
           uint32_t s0x[D / 128 + 1], s1x[D / 128 + 1];   // the scales, two a register
           if constexpr (D == 64) {
             s0x[0] = e4m3x2_to_half2((uint16_t)lds_u8(at + key_scale));
-            s1x[0] = e4m3x2_to_half2((uint16_t)lds_u8(at + key_scale + eight));
+            s1x[0] = e4m3x2_to_half2((uint16_t)lds_u8(at + key_scale8));
           } else {
 #pragma unroll
             for (int p = 0; p < D / 128; ++p) {
               s0x[p] = e4m3x2_to_half2((uint16_t)lds_u16(at + key_scale + 2 * p));
-              s1x[p] = e4m3x2_to_half2((uint16_t)lds_u16(at + key_scale + eight + 2 * p));
+              s1x[p] = e4m3x2_to_half2((uint16_t)lds_u16(at + key_scale8 + 2 * p));
             }
           }
           float two[NT][4];   // a second chain of sums, half the first one's latencies
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) two[nt][i] = 0.f;
 #pragma unroll
           for (int v = 0; v < D / 32; ++v) {   // eight channels of a lane: two blocks
             uint32_t x0[4], x1[4];
@@ -760,9 +777,9 @@ __global__ void __launch_bounds__(threads_of(D), 1)
               }
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
-                if (y == 1) mma<FMT>(two[nt], a, qf[nt][2 * v + y][0], qf[nt][2 * v + y][1]);
-                else
-                mma<FMT>(s[u][nt], a, qf[nt][2 * v + y][0], qf[nt][2 * v + y][1]);
+                float (&sum)[4] = y ? two[nt] : s[u][nt];
+                if (v == 0) mma_first<FMT>(sum, a, qf[nt][2 * v + y][0], qf[nt][2 * v + y][1]);
+                else mma<FMT>(sum, a, qf[nt][2 * v + y][0], qf[nt][2 * v + y][1]);
               }
             }
           }
@@ -784,19 +801,18 @@ __global__ void __launch_bounds__(threads_of(D), 1)
           f(mt, a);
         }
       } else {
-        const uint32_t p0 = base + u * hop + value_code, p1 = p0 + odd;
-        const uint32_t c0 = base + u * hop + value_scale, c1 = c0 + odd;
+        const uint32_t at = base + u * hop;
         uint32_t wa[D / 64], wb[D / 64], wc[D / 64], wd[D / 64];
-        lds_words(wa, p0);
-        lds_words(wb, p1);
-        lds_words(wc, p0 + eight);
-        lds_words(wd, p1 + eight);
+        lds_words(wa, at + value_code);
+        lds_words(wb, at + value_odd);
+        lds_words(wc, at + value_code8);
+        lds_words(wd, at + value_odd8);
         uint32_t sl = 0, sh8 = 0;
 #pragma unroll
         for (int v = 0; v < D / 64; ++v) {   // eight channels: four blocks
           if (v % 2 == 0) {
-            sl = e4m3x2_to_half2((uint16_t)(lds_u8(c0 + v / 2) + (lds_u8(c1 + v / 2) << 8)));
-            sh8 = e4m3x2_to_half2((uint16_t)(lds_u8(c0 + eight + v / 2) + (lds_u8(c1 + eight + v / 2) << 8)));
+            sl = e4m3x2_to_half2((uint16_t)(lds_u8(at + value_scale + v / 2) + (lds_u8(at + scale_odd + v / 2) << 8)));
+            sh8 = e4m3x2_to_half2((uint16_t)(lds_u8(at + value_scale8 + v / 2) + (lds_u8(at + scale_odd8 + v / 2) << 8)));
           }
           // pairs of slots instead of pairs of channels: even channels, odd channels
           constexpr uint32_t kLow = 0x0f0f0f0fu;
@@ -831,7 +847,7 @@ __global__ void __launch_bounds__(threads_of(D), 1)
     float s[SUB][NT][4];
     bool scored = false;
     for (; x < end; ++x, s0 += sh.tile) {
-      const uint32_t base = ring0 + stage * (2 * ge.half_bytes);
+      const uint32_t base = __shfl_sync(0xffffffffu, ring0 + stage * (2 * ge.half_bytes), 0);   // known to be the same in all lanes
       if (!scored) {
         wait(&full[stage], phase);
         keys(base, s);
@@ -940,7 +956,7 @@ __global__ void __launch_bounds__(threads_of(D), 1)
       scored = !apart && x + 1 < end;
       if (scored) {
         wait(&full[next], next_phase);
-        keys(ring0 + next * (2 * ge.half_bytes), s);
+        keys(__shfl_sync(0xffffffffu, ring0 + next * (2 * ge.half_bytes), 0), s);
         values(base, pb);
       } else if (!apart) {
         values(base, pb);
@@ -1082,90 +1098,109 @@ __global__ void __launch_bounds__(threads_of(D), 1)
 }
 
 // ------------------------------------------------------------------ joining the parts of an item
-constexpr int kJoinThreads = 256;
-
-// One block a row of an item's KV head.  The parts' weights 2^(m_i - max) come first, all parts at once; then each
-// thread adds up four channels of a share of the parts, and the shares are added in order.
-__global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(AttnState st, AttnDims dm, Geometry ge, Batch ba,
-                                                                      Rows out, float* lse) {
+// One block kRows rows of an item's KV head.  The parts' weights 2^(m_i - max) come first, all parts at
+// once; then each thread adds up four channels of a row over a share of the parts, and the shares are added in order.
+// What bounds it is a chain of dependent reads (the plan, the maxima, the outputs), so each step reads all that it can.
+template <int kRows, int kThreads>
+__global__ void __launch_bounds__(kThreads) attention_join_kernel(AttnState st, AttnDims dm, Geometry ge, Batch ba,
+                                                                  Rows out, float* lse, int lanes_log) {
+  constexpr int rb = kRows;
+  __shared__ float2 s_ml[kAttnCtas][rb];          // maximum and sum, then the weight in place of the maximum
   __shared__ int s_slot[kAttnCtas];
-  __shared__ float s_w[kAttnCtas], s_red[2][kJoinThreads / 32];
-  __shared__ float4 s_acc[kJoinThreads];
+  __shared__ float2 s_row[rb];                    // maximum and sum of all parts
+  __shared__ float4 s_acc[kThreads];
   const AttnShape& sh = ge.sh;
-  const int b = blockIdx.y, kh = blockIdx.x % dm.H, r = blockIdx.x / dm.H, run = r >> sh.rows_log,
-            row = r & (sh.rows - 1);
-  const int tid = threadIdx.x;
+  const int b = blockIdx.y, kh = blockIdx.x % dm.H, r0 = blockIdx.x / dm.H * rb, run = r0 >> sh.rows_log;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait();
   const int p0 = st.plan[b], p1 = st.plan[b + 1], total = st.plan[ba.n_seq];
   Entry e;
   e.tok0 = ba.cu_new[b];
   e.n = ba.cu_new[b + 1] - e.tok0;
   e.len = ba.len[(int64_t)b * ba.len_stride];
-  if (p0 == p1 || r >= rows_of(sh, e.n)) return;   // no tiles: an entry without new tokens, or one that was refused
+  const int there = min(rb, rows_of(sh, e.n) - r0);
+  if (p0 == p1 || there <= 0) return;   // no tiles: an entry without new tokens, or one that was refused
   const int group = kh / attn_group(dm.d), head = kh % attn_group(dm.d);
-  int at = p0 + group * ((p1 - p0) / sh.groups);
+  int at = p0;
+  if (sh.groups > 1) at += group * ((p1 - p0) / sh.groups);
   for (int i = 0; i < run; ++i) at += item_tiles(sh, e.n, e.len, i);
   const int tiles = item_tiles(sh, e.n, e.len, run);
   const int c0 = cta_of_tile(at, total), c1 = cta_of_tile(at + tiles - 1, total);
   if (c0 == c1) return;
   // below one tile a CTA some CTAs have none: then every tile is a part
   const int parts = total < kAttnCtas ? tiles : c1 - c0 + 1;
-  float m = -INFINITY, l = 0.f;
-  if (tid < parts) {
-    const int c = total < kAttnCtas ? cta_of_tile(at + tid, total) : c0 + tid;
+  const int64_t ml0 = attn_group(dm.d) * sh.rows * dm.d + (head * sh.rows + (r0 & (sh.rows - 1))) * 2;
+  for (int i = tid; i < parts * rb; i += kThreads) {
+    const int part = i / rb, row = i - part * rb;
+    const int c = total < kAttnCtas ? cta_of_tile(at + part, total) : c0 + part;
     const int slot = c * 2 + (c == c0 ? 1 : 0);
-    s_slot[tid] = slot;
-    const float2 ml = *reinterpret_cast<const float2*>(st.part + (int64_t)slot * ge.slot_floats +
-                                                       attn_group(dm.d) * sh.rows * dm.d + (head * sh.rows + row) * 2);
-    m = ml.x;
-    l = ml.y;
+    if (row == 0) s_slot[part] = slot;
+    if (row < there) s_ml[part][row] = *reinterpret_cast<const float2*>(st.part + (int64_t)slot * ge.slot_floats + ml0 + 2 * row);
   }
-  float top = m;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if ((tid & 31) == 0) s_red[0][tid >> 5] = top;
   __syncthreads();
+  if (warp < there) {
+    float top = -INFINITY, sum = 0.f;
+    for (int i = lane; i < parts; i += 32) top = fmaxf(top, s_ml[i][warp].x);
 #pragma unroll
-  for (int i = 0; i < kJoinThreads / 32; ++i) top = fmaxf(top, s_red[0][i]);
-  const float base = top == -INFINITY ? 0.f : top;
-  const float weight = ex2(m - base);
-  if (tid < parts) s_w[tid] = weight;
-  l = warp_sum(l * weight);
-  if ((tid & 31) == 0) s_red[1][tid >> 5] = l;
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float base = top == -INFINITY ? 0.f : top;
+    for (int i = lane; i < parts; i += 32) {
+      const float2 ml = s_ml[i][warp];
+      const float weight = ex2(ml.x - base);
+      s_ml[i][warp].x = weight;
+      sum += ml.y * weight;
+    }
+    sum = warp_sum(sum);
+    if (lane == 0) s_row[warp] = make_float2(base, sum);
+  }
   __syncthreads();
-  l = 0.f;
-#pragma unroll
-  for (int i = 0; i < kJoinThreads / 32; ++i) l += s_red[1][i];
-
-  const int lanes = dm.d / 4, shares = kJoinThreads / lanes;
-  const int share = tid / lanes, ch = tid % lanes * 4;
-  const float* from = st.part + (int64_t)(head * sh.rows + row) * dm.d + ch;
+  const int wide = rb << lanes_log, shares = kThreads / wide;   // float4 columns of the block's rows; threads for each
+  const int share = tid / wide, col = tid & (wide - 1), row = col >> lanes_log, ch = (col & ((1 << lanes_log) - 1)) * 4;
+  const bool on = share < shares && row < there;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-  for (int i = share; i < parts; i += shares) {
-    const float4 v = *reinterpret_cast<const float4*>(from + (int64_t)s_slot[i] * ge.slot_floats);
-    const float z = s_w[i];
-    acc.x += v.x * z;
-    acc.y += v.y * z;
-    acc.z += v.z * z;
-    acc.w += v.w * z;
+  if (on) {
+    const float* from = st.part + (int64_t)(head * sh.rows + (r0 & (sh.rows - 1)) + row) * dm.d + ch;
+#pragma unroll 1
+    for (int i0 = share; i0 < parts; i0 += 8 * shares) {
+      float4 v[8];
+      float z[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int i = i0 + k * shares;
+        v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        z[k] = 0.f;
+        if (i < parts) {
+          v[k] = *reinterpret_cast<const float4*>(from + (int64_t)s_slot[i] * ge.slot_floats);
+          z[k] = s_ml[i][row].x;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        acc.x += v[k].x * z[k];
+        acc.y += v[k].y * z[k];
+        acc.z += v[k].z * z[k];
+        acc.w += v[k].w * z[k];
+      }
+    }
   }
   s_acc[tid] = acc;
   __syncthreads();
-  if (share) return;
+  if (!on || share) return;
   for (int k = 1; k < shares; ++k) {
-    const float4 v = s_acc[tid + k * lanes];
+    const float4 v = s_acc[tid + k * wide];
     acc.x += v.x;
     acc.y += v.y;
     acc.z += v.z;
     acc.w += v.w;
   }
+  const int r = r0 + row;
   const int64_t token = e.tok0 + r / sh.rep;
   const int hq = kh * sh.rep + r % sh.rep;
-  const float mul = l == 0.f ? 0.f : 1.f / l;
+  const float2 all = s_row[row];
+  const float mul = all.y == 0.f ? 0.f : 1.f / all.y;
   *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(out.p) + token * out.st + hq * out.sh + ch) =
       make_uint2(bf162_of(acc.x * mul, acc.y * mul), bf162_of(acc.z * mul, acc.w * mul));
-  if (lse && ch == 0) lse[token * dm.Hq + hq] = l == 0.f ? -INFINITY : (base + log2f(l)) * 0.69314718055994531f;
+  if (lse && ch == 0) lse[token * dm.Hq + hq] = all.y == 0.f ? -INFINITY : (all.x + log2f(all.y)) * 0.69314718055994531f;
 }
 
 // ------------------------------------------------------------------ host
@@ -1273,8 +1308,17 @@ cudaError_t launch_attention(const AttnState& st, const AttnDims& dm, int layer,
                           : (q4 ? run_rows<256, EPIKV_CACHE_E2M1> : run_rows<256, EPIKV_CACHE_BF16>);
   const cudaError_t err = go(st, dm, ge, layer, ba, q, out, lse, kv, stream);
   if (err != cudaSuccess) return err;
-  const dim3 grid((unsigned)dm.Hq * ba.max_new, ba.n_seq);
-  return pdl_launch(attention_join_kernel, grid, kJoinThreads, 0, stream, st, dm, ge, ba, out, lse);
+  // A joining block of 512 threads takes one row where that gives at most two blocks an SM, and parts may be many (one
+  // sequence of 65,536 slots: 256 threads 36.2, 512 34.0 us in all); four rows, or the eight of several tokens, and 256
+  // threads where blocks are plenty (64 sequences: one row 213, four 204 us; chunks of 13 to 47 tokens: 61 / 50).
+  const int64_t rows = (int64_t)ba.max_new * dm.rep;
+  const int lanes_log = dm.d == 64 ? 4 : dm.d == 128 ? 5 : 6;
+  auto join = [&](auto kernel, int n, int threads) {
+    return pdl_launch(kernel, dim3((unsigned)((rows + n - 1) / n * dm.H), ba.n_seq), threads, 0, stream, st, dm, ge, ba, out,
+                      lse, lanes_log);
+  };
+  if (rows * dm.H * ba.n_seq <= 2 * kAttnCtas) return join(attention_join_kernel<1, 512>, 1, 512);
+  return rows >= 8 ? join(attention_join_kernel<8, 512>, 8, 512) : join(attention_join_kernel<4, 256>, 4, 256);
 }
 
 }  // namespace epikv

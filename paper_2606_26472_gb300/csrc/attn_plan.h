@@ -59,7 +59,13 @@ EPIKV_PLAN int first_tile(int cta, int total) {
   return (int)(q * cta + r * cta / kAttnCtas);
 }
 // The CTA whose share tile x is in.
-EPIKV_PLAN int cta_of_tile(int x, int total) { return (int)((((uint64_t)x + 1) * kAttnCtas - 1) / (unsigned)total); }
+EPIKV_PLAN int cta_of_tile(int x, int total) {
+  int c = (int)((float)x * (float)kAttnCtas / (float)total);   // near it; put right by the shares themselves
+  if (c > kAttnCtas - 1) c = kAttnCtas - 1;
+  while (first_tile(c, total) > x) --c;
+  while (first_tile(c + 1, total) <= x) ++c;
+  return c;
+}
 
 // ---- shared memory of a CTA: the ring of tiles, boxes to join a head's warps, barriers, the entries' first tiles
 constexpr int kAttnSmem = 225 * 1024;   // dynamic shared memory, at most (its start is moved up to a multiple of 1,024)
