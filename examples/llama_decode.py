@@ -9,10 +9,18 @@ its trigger, selects the kept tokens and compacts every layer's K/V in place;
 attention then runs over exactly the kept tokens.  Nothing in the model is
 changed for eviction: the cache it attends over is simply shorter.
 
+Attention runs as torch operations over gathered rows (the default), or
+through the library's own calls: epikv_append rotates the new queries and keys
+by position and stores keys and values at each sequence's next slot, which
+after an eviction is not its position, and epikv_attention reads the slots.
+The cache then holds bf16 rows or, with 4 bits, packed rows that the eviction
+moves as they are (the band kinds alone drive it: the K/V kinds read bf16).
+
 The weights are random (no checkpoint is available), so the tokens carry no
 meaning and there is no accuracy claim; the demo checks the plumbing.
 
     python examples/llama_decode.py --layers 32 --hidden 4096 --steps 256
+    python examples/llama_decode.py --small --attention library --cache-bits 4
 """
 from __future__ import annotations
 
@@ -127,6 +135,54 @@ class RandomLlama:
             hs.append(x)
         return self._rms(x) @ self.lm_head, hs
 
+    def step_library(self, tokens, attn, cache: KVCache):
+        """The same step with the library's rotation, append and attention.  attn: a CacheAttention that knows the
+        batch's lengths and positions."""
+        s = self.s
+        B = tokens.shape[0]
+        x = self.embed[tokens]
+        hs = []
+        for l, p in enumerate(self.layers):
+            h = self._rms(x)
+            q = (h @ p["wq"]).view(B, s.heads, s.head_dim)
+            k = (h @ p["wk"]).view(B, s.kv_heads, s.head_dim)
+            v = (h @ p["wv"]).view(B, s.kv_heads, s.head_dim)
+            o = attn(l, q, k, v, cache)
+            x = x + o.reshape(B, s.heads * s.head_dim) @ p["wo"]
+            h2 = self._rms(x)
+            x = x + (F.silu(h2 @ p["w1"]) * (h2 @ p["w3"])) @ p["w2"]
+            hs.append(x)
+        return self._rms(x) @ self.lm_head, hs
+
+
+class CacheAttention:
+    """epikv_append and epikv_attention of one token per sequence: the context, the rotation table and the batch's
+    device arrays, made once."""
+
+    def __init__(self, shape: ModelShape, cache: KVCache, batch, max_positions, device="cuda"):
+        cfg = E.make_attn_config(max_seqs=batch, max_cache_tokens=cache.T, max_new_tokens=1, num_layers=shape.layers,
+                                 num_heads=shape.heads, num_kv_heads=shape.kv_heads, head_dim=shape.head_dim,
+                                 cache_format=cache.cache_format)
+        self.ws = torch.empty(E.epikv_attn_workspace_bytes(cfg), dtype=torch.uint8, device=device)
+        self.ctx = E.epikv_attn_init(cfg, self.ws, self.ws.numel())
+        self.table = E.epikv_rope_table(E.make_rope_config(shape.head_dim), max_positions, device)
+        self.rope = E.rope_view(self.table, E.EPIKV_ROPE_INTERLEAVED)
+        self.batch = batch
+        self.seq_ids = torch.arange(batch, dtype=torch.int32, device=device)
+        self.cu = torch.arange(batch + 1, dtype=torch.int32, device=device)
+        self.length = torch.zeros(batch, dtype=torch.int32, device=device)    # slots held before the step
+        self.position = torch.zeros(batch, dtype=torch.int32, device=device)
+        self.q = torch.empty(batch, shape.heads, shape.head_dim, dtype=torch.bfloat16, device=device)
+        self.o = torch.empty_like(self.q)
+
+    def __call__(self, layer, q, k, v, cache: KVCache):
+        kv = cache.view()
+        E.epikv_append(self.ctx, layer, self.batch, self.seq_ids, self.cu, 1, self.length, self.position, E.rows(q),
+                       E.rows(self.q), E.rows(k), E.rows(v), self.rope, kv)
+        E.epikv_attention(self.ctx, layer, self.batch, self.seq_ids, self.cu, 1, self.length, E.rows(self.q),
+                          E.rows(self.o), kv)
+        return self.o
+
 
 @dataclasses.dataclass
 class DecodeResult:
@@ -137,12 +193,17 @@ class DecodeResult:
     kv_rows: dict                # seq -> (K, V) uint16 [T, L, H, d]
     ctx: object
     cache: KVCache
+    attn: object = None          # the CacheAttention of attention="library"
 
 
 def decode(shape: ModelShape, *, batch=4, prompt=8, steps=200, budget=96, slack=16, seed=0, record=False,
-           kinds=E.EPIKV_SCORE_BANDZ | E.EPIKV_SCORE_LAGKV, device="cuda"):
+           kinds=E.EPIKV_SCORE_BANDZ | E.EPIKV_SCORE_LAGKV, device="cuda", attention="torch", cache_bits=16):
     """Greedy decode of `batch` random prompts for `steps` tokens with EpiKV
     eviction (budget K, evict when the cache passes K + slack)."""
+    if attention not in ("torch", "library") or cache_bits not in (16, 4) or (cache_bits == 4 and attention == "torch"):
+        raise ValueError("attention is torch or library; a 4-bit cache needs the library's")
+    if cache_bits == 4:
+        kinds &= E.EPIKV_SCORE_BANDZ | E.EPIKV_SCORE_HSVAR    # the K/V kinds read bf16 rows
     model = RandomLlama(shape, seed, device)
     s = shape
     T_cap = budget + slack + 1
@@ -150,9 +211,10 @@ def decode(shape: ModelShape, *, batch=4, prompt=8, steps=200, budget=96, slack=
     mb = (T_cap + 15) // 16
     perm = torch.randperm(batch * mb, generator=torch.Generator().manual_seed(seed)).numpy().reshape(batch, mb)
     cache = KVCache(E.EPIKV_LAYOUT_PAGED, s.layers, s.kv_heads, s.head_dim, max_seqs=batch, max_tokens=T_cap,
-                    block_table=perm, device=device)
+                    block_table=perm, device=device,
+                    cache_format=E.EPIKV_CACHE_E2M1 if cache_bits == 4 else E.EPIKV_CACHE_BF16)
     cfg = E.make_config(max_seqs=batch, max_cache_tokens=T_cap, max_new_tokens=1, num_layers=s.layers,
-                        num_kv_heads=s.kv_heads, head_dim=s.head_dim, hidden=s.hidden,
+                        num_kv_heads=cache.H, head_dim=cache.d, hidden=s.hidden,
                         n_band_a=len(shape.band_a), n_band_b=len(shape.band_b), score_kinds=kinds)
     ws = torch.empty(E.epikv_workspace_bytes(cfg), dtype=torch.uint8, device=device)
     ctx = E.epikv_init(cfg, ws, ws.numel())
@@ -169,6 +231,7 @@ def decode(shape: ModelShape, *, batch=4, prompt=8, steps=200, budget=96, slack=
     trig = bud + slack
     n_out = torch.empty(batch, dtype=torch.int32, device=device)
     n_cache = torch.zeros(batch, dtype=torch.int64, device=device)
+    attn = CacheAttention(s, cache, batch, prompt + steps, device) if attention == "library" else None
     out_tokens = []
     band_rows = {}
     kv_rows = {b: ([], []) for b in range(batch)}
@@ -178,7 +241,12 @@ def decode(shape: ModelShape, *, batch=4, prompt=8, steps=200, budget=96, slack=
     for t in range(total):
         pos = torch.full((batch,), t, dtype=torch.int64, device=device)
         slots = n_cache.clone()
-        logits, hs = model.step(tok, pos, cache, seqs, slots, n_cache + 1)
+        if attn is None:
+            logits, hs = model.step(tok, pos, cache, seqs, slots, n_cache + 1)
+        else:
+            attn.length.copy_(n_cache)
+            attn.position.fill_(t)
+            logits, hs = model.step_library(tok, attn, cache)
         rows = [hs[l].contiguous() for l in bands]
         hv = E.hidden_view(rows, s.hidden)
         if record:
@@ -200,7 +268,7 @@ def decode(shape: ModelShape, *, batch=4, prompt=8, steps=200, budget=96, slack=
         band_rows = {k: np.stack(v) for k, v in band_rows.items()}
         kv_rows = {b: (np.stack(K), np.stack(V)) for b, (K, V) in kv_rows.items()}
     return DecodeResult(torch.stack(out_tokens, 1).cpu().numpy(), n_cache.cpu().tolist(), evictions, band_rows,
-                        kv_rows, ctx, cache)
+                        kv_rows, ctx, cache, attn)
 
 
 def main():
@@ -211,11 +279,13 @@ def main():
     p.add_argument("--steps", type=int, default=256)
     p.add_argument("--budget", type=int, default=128)
     p.add_argument("--small", action="store_true", help="an 8-layer, 512-wide model")
+    p.add_argument("--attention", choices=("torch", "library"), default="torch")
+    p.add_argument("--cache-bits", type=int, choices=(16, 4), default=16)
     a = p.parse_args()
     shape = small_shape() if a.small else ModelShape(layers=a.layers, hidden=a.hidden)
     import time
     t0 = time.time()
-    r = decode(shape, batch=a.batch, steps=a.steps, budget=a.budget)
+    r = decode(shape, batch=a.batch, steps=a.steps, budget=a.budget, attention=a.attention, cache_bits=a.cache_bits)
     dt = time.time() - t0
     st, code = E.epikv_get_error(r.ctx)
     print(f"decoded {a.batch} x {a.steps} tokens in {dt:.1f} s; cache lengths {r.n_cache}; "
