@@ -602,7 +602,14 @@ __global__ void __launch_bounds__(threads_of(D), 1)
   __syncwarp();
   const int tiles = hi - lo;
   const Waiter wait{gave_up, st.err};
+  // With 8 + 4 warps of 168 registers the copying ones give most of theirs to the computing ones:
+  // 256 x 216 + 128 x 72 = 256 x 200 + 128 x 104 = 384 x 168.
+  constexpr bool kSplit = kThreads == 384;
+  constexpr int kCopyRegs = FMT == EPIKV_CACHE_BF16 ? 104 : 72, kMoreRegs = FMT == EPIKV_CACHE_BF16 ? 200 : 216;
+  static_assert(kWarps * kMoreRegs + kAttnCopyWarps * kCopyRegs <= (kWarps + kAttnCopyWarps) * 168 || !kSplit,
+                "the computing warps would wait for registers that nobody gives");
   if (warp >= kWarps) {
+    if constexpr (kSplit) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kCopyRegs));
     if (warp - kWarps >= ge.copiers) return;
     if (FMT == EPIKV_CACHE_BF16 && maps.on)
       copy_tensor<D>(smem, full, empty, wait, st, dm, ge, kv, maps, layer, walker, w, tiles, warp - kWarps, lane);
@@ -613,6 +620,7 @@ __global__ void __launch_bounds__(threads_of(D), 1)
     return;
   }
 
+  if constexpr (kSplit) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kMoreRegs));
   constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
   constexpr int KS = D / 16;                 // blocks of 16 channels
   // probabilities are held times 2^kUp: as halves they reach from 2^-14 (2^-24 with fewer bits) to 2^16, and may pass the
@@ -633,10 +641,11 @@ __global__ void __launch_bounds__(threads_of(D), 1)
 
     // where the lane reads in a tile: keys are rows (slots), values columns of the first operand
     const uint32_t ring0 = smem_u32(smem);
-    // where the warp's blocks of slots start, and to its next one (what lies behind the tile: a block of it, masked);
-    // 8 slots on
-    const int block0 = team * 16 < sh.tile ? team * 16 : 0;
-    const uint32_t hop = teams * 16 < sh.tile ? teams * 16 * ge.row_s : 0, eight = 8 * ge.row_s;
+    // where the warp's blocks of slots start, and from there to its block u (what lies behind the tile: the first block
+    // again, masked); 8 slots on
+    const int block0 = team * 16 < sh.tile ? team * 16 : 0, blocks = sh.tile / (16 * teams);
+    const uint32_t hop = teams * 16 * ge.row_s, eight = 8 * ge.row_s;
+    auto block_at = [&](int u) { return u == 0 || u < blocks ? u * hop : 0u; };
     const int k0 = kBf16 ? 2 * t : slot_of_row(ge.order, 2 * t), k1 = kBf16 ? 2 * t + 1 : slot_of_row(ge.order, 2 * t + 1);
     uint32_t key_code, key_scale, value_code, value_scale;
     uint32_t key_code8 = 0, key_scale8 = 0, value_odd = 0, value_code8 = 0, value_odd8 = 0, scale_odd = 0, value_scale8 = 0, scale_odd8 = 0;
@@ -728,7 +737,7 @@ __global__ void __launch_bounds__(threads_of(D), 1)
 #pragma unroll
       for (int u = 0; u < SUB; ++u) {
         if constexpr (kBf16) {
-          const uint32_t addr = base + u * hop + key_code;
+          const uint32_t addr = base + block_at(u) + key_code;
 #pragma unroll
           for (int j = 0; j < KS; ++j) {
             uint32_t a[4];
@@ -740,7 +749,7 @@ __global__ void __launch_bounds__(threads_of(D), 1)
             }
           }
         } else {
-          const uint32_t at = base + u * hop;
+          const uint32_t at = base + block_at(u);
           uint32_t w0[D / 32], w1[D / 32];
           lds_words(w0, at + key_code);
           lds_words(w1, at + key_code8);
@@ -793,7 +802,7 @@ __global__ void __launch_bounds__(threads_of(D), 1)
     // Gives block mt of the operand (channels x slots; the lane's slots are k0, k1 and 8 on) to f, for every mt.
     auto each = [&](uint32_t base, int u, auto&& f) {
       if constexpr (kBf16) {
-        const uint32_t addr = base + u * hop + value_code;
+        const uint32_t addr = base + block_at(u) + value_code;
 #pragma unroll
         for (int mt = 0; mt < KS; ++mt) {
           uint32_t a[4];
@@ -801,7 +810,7 @@ __global__ void __launch_bounds__(threads_of(D), 1)
           f(mt, a);
         }
       } else {
-        const uint32_t at = base + u * hop;
+        const uint32_t at = base + block_at(u);
         uint32_t wa[D / 64], wb[D / 64], wc[D / 64], wd[D / 64];
         lds_words(wa, at + value_code);
         lds_words(wb, at + value_odd);
@@ -1205,10 +1214,9 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttnState st, 
 
 // ------------------------------------------------------------------ host
 Geometry geometry(const AttnDims& dm, int n_seq, int max_new, bool causal) {
-  return attn_geometry(dm.H, dm.rep, dm.d, dm.fmt == EPIKV_CACHE_E2M1, dm.units, n_seq, max_new, causal);
+  return attn_geometry(dm.H, dm.rep, dm.d, dm.fmt == EPIKV_CACHE_E2M1, dm.units, dm.T, n_seq, max_new, causal);
 }
 
-constexpr int sub_blocks(int fmt, int nt) { return attn_sub_blocks(fmt == EPIKV_CACHE_E2M1, nt); }
 
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
@@ -1251,10 +1259,10 @@ CacheMaps cache_maps(const AttnDims& dm, const Geometry& ge, int layer, const Kv
   return maps;
 }
 
-template <int D, int FMT, int NT>
+template <int D, int FMT, int NT, int SUB>
 cudaError_t run(const AttnState& st, const AttnDims& dm, const Geometry& ge, int layer, const Batch& ba, const Rows& q,
                 const Rows& out, float* lse, const KvDev& kv, cudaStream_t stream) {
-  return pdl_launch(attention_kernel<D, FMT, NT, sub_blocks(FMT, NT)>, kAttnCtas, threads_of(D), ge.smem_bytes + 1024,
+  return pdl_launch(attention_kernel<D, FMT, NT, SUB>, kAttnCtas, threads_of(D), ge.smem_bytes + 1024,
                     stream, st, dm, ge, layer, ba, q, out, lse, kv, cache_maps(dm, ge, layer, kv),
                     dm.scale * 1.4426950408889634f);
 }
@@ -1262,26 +1270,38 @@ cudaError_t run(const AttnState& st, const AttnDims& dm, const Geometry& ge, int
 template <int D, int FMT>
 cudaError_t run_rows(const AttnState& st, const AttnDims& dm, const Geometry& ge, int layer, const Batch& ba,
                      const Rows& q, const Rows& out, float* lse, const KvDev& kv, cudaStream_t stream) {
+  constexpr int kSub = FMT == EPIKV_CACHE_BF16 ? 1 : 2;
   if constexpr (D <= 64)
-    if (ge.sh.rows == 32) return run<D, FMT, 4>(st, dm, ge, layer, ba, q, out, lse, kv, stream);
-  if constexpr (D <= 128)
-    if (ge.sh.rows == 16) return run<D, FMT, 2>(st, dm, ge, layer, ba, q, out, lse, kv, stream);
-  return run<D, FMT, 1>(st, dm, ge, layer, ba, q, out, lse, kv, stream);
+    if (ge.sh.rows == 32) return run<D, FMT, 4, kSub>(st, dm, ge, layer, ba, q, out, lse, kv, stream);
+  if constexpr (D <= 128) {
+    if (ge.sh.rows == 16) return run<D, FMT, 2, kSub>(st, dm, ge, layer, ba, q, out, lse, kv, stream);
+    if constexpr (kSub == 2)
+      if (ge.sub == 4) return run<D, FMT, 1, 4>(st, dm, ge, layer, ba, q, out, lse, kv, stream);
+  }
+  return run<D, FMT, 1, kSub>(st, dm, ge, layer, ba, q, out, lse, kv, stream);
 }
 
-template <int D, int FMT, int NT>
+template <int D, int FMT, int NT, int SUB>
 cudaError_t prepare_one() {
-  return cudaFuncSetAttribute(attention_kernel<D, FMT, NT, sub_blocks(FMT, NT)>,
-                              cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem + 1024);
+  auto kernel = attention_kernel<D, FMT, NT, SUB>;
+  cudaFuncAttributes at;
+  cudaError_t e = cudaFuncGetAttributes(&at, kernel);
+  if (e != cudaSuccess) return e;
+  if (threads_of(D) == 384 && at.numRegs != 168) return cudaErrorInvalidConfiguration;   // what the split counts on
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem + 1024);
 }
 
 template <int D, int FMT>
 cudaError_t prepare_rows() {
-  cudaError_t e = prepare_one<D, FMT, 1>();
-  if constexpr (D <= 128)
-    if (e == cudaSuccess) e = prepare_one<D, FMT, 2>();
+  constexpr int kSub = FMT == EPIKV_CACHE_BF16 ? 1 : 2;
+  cudaError_t e = prepare_one<D, FMT, 1, kSub>();
+  if constexpr (D <= 128) {
+    if (e == cudaSuccess) e = prepare_one<D, FMT, 2, kSub>();
+    if constexpr (kSub == 2)
+      if (e == cudaSuccess) e = prepare_one<D, FMT, 1, 4>();
+  }
   if constexpr (D <= 64)
-    if (e == cudaSuccess) e = prepare_one<D, FMT, 4>();
+    if (e == cudaSuccess) e = prepare_one<D, FMT, 4, kSub>();
   return e;
 }
 

@@ -79,6 +79,7 @@ struct AttnGeometry {
   int stages;        // tiles in the ring
   int copiers;       // copying warps: each takes every copiers-th tile
   int join_off, bar_off, pre_off, smem_bytes;   // behind the ring
+  int sub;           // 16-slot blocks of a tile that a warp takes
   int slot_floats;   // of a CTA's partial result
   uint32_t order;    // 4-bit rows: nibble r, the slot of eight that row r of the tensor instruction's rows takes
 };
@@ -101,9 +102,13 @@ EPIKV_PLAN int attn_row_blocks(int d, int rep, int max_new) {
   while (nt < 256 / d && nt < want) nt *= 2;
   return nt;
 }
-// 16-slot blocks of a tile that a warp takes: what a tile costs besides its products (waits, the check against the
-// maximum) is shared by so many (32 x 8,256 slots, d = 128: one 104, two 88, four 96 us, which leaves the ring 3 tiles).
-constexpr int attn_sub_blocks(bool q4, int nt) { return q4 && nt == 1 ? 2 : 1; }
+// 16-slot blocks of a tile that a warp takes of 4-bit rows (bf16: one, whose tiles are 64 KB at 8 x 128): what a tile
+// costs besides its products (waits, the check against the maximum) is shared by so many.  Four where the caches, if
+// full, give each CTA 16 such tiles (`slots`: of all entries; 32 x 8,256 slots two 75, four 72 us; d = 64, 32 x 16,384 91
+// and 82), else two (4 x 136 slots two 14.0, four 17.1 us; one sequence of 65,536 33.6 and 34.2).
+EPIKV_PLAN int attn_sub_blocks(bool q4, int d, int nt, int64_t slots) {
+  return !q4 ? 1 : nt == 1 && d <= 128 && slots >= (int64_t)kAttnCtas * 16 * 64 ? 4 : 2;
+}
 // Warps of a head in a group of so many heads: 8, 4, 2 or 1.
 EPIKV_PLAN int attn_teams(int heads, int warps) {
   const int t = warps / heads;
@@ -112,14 +117,16 @@ EPIKV_PLAN int attn_teams(int heads, int warps) {
 // What a warp leaves for another to join: its outputs, maxima and sums.
 constexpr int attn_box_floats(int d, int nt) { return (d / 16 * nt * 4 + 4 * nt) * 32; }
 
-// units: 2-byte units of a cache row.
-EPIKV_PLAN AttnGeometry attn_geometry(int H, int rep, int d, bool q4, int units, int n_seq, int max_new, bool causal) {
+// units: 2-byte units of a cache row; slots: of a sequence's cache.
+EPIKV_PLAN AttnGeometry attn_geometry(int H, int rep, int d, bool q4, int units, int slots, int n_seq, int max_new,
+                                      bool causal) {
   AttnGeometry ge;
   const int nt = attn_row_blocks(d, rep, max_new), group = attn_group(d);
   const int heads = H < group ? H : group;                          // of the first group
   const int rest = H > group && H % group ? H % group : heads;      // of the last one
-  int tile = 16 * attn_teams(heads, group) * attn_sub_blocks(q4, nt);
+  int tile = 16 * attn_teams(heads, group) * attn_sub_blocks(q4, d, nt, (int64_t)slots * n_seq);
   if (tile > kMaxTile) tile = kMaxTile;
+  ge.sub = attn_sub_blocks(q4, d, nt, (int64_t)slots * n_seq);
   int rows_log = 3, tile_log = 4;
   while (1 << rows_log < nt * 8) ++rows_log;
   while (1 << tile_log < tile) ++tile_log;

@@ -15,9 +15,9 @@ using namespace epikv;
 #define NEED(x) do { if (!(x)) return __LINE__; } while (0)
 extern "C" {
 // 0, or the line of the first check that fails
-int geometry_holds(int H, int rep, int d, int q4, int units, int n_seq, int max_new) {
-  const AttnGeometry g = attn_geometry(H, rep, d, q4, units, n_seq, max_new, true);
-  const int nt = attn_row_blocks(d, rep, max_new), sub = attn_sub_blocks(q4, nt), group = attn_group(d);
+int geometry_holds(int H, int rep, int d, int q4, int units, int slots, int n_seq, int max_new) {
+  const AttnGeometry g = attn_geometry(H, rep, d, q4, units, slots, n_seq, max_new, true);
+  const int nt = attn_row_blocks(d, rep, max_new), sub = g.sub, group = attn_group(d);
   NEED(g.stages >= 2 && g.stages <= kMaxStages && g.smem_bytes <= kAttnSmem);
   NEED(g.copiers >= 1 && g.copiers <= kAttnCopyWarps && g.copiers <= g.stages);
   NEED(g.sh.rows == 1 << g.sh.rows_log && g.sh.tile == 1 << g.sh.tile_log);
@@ -48,13 +48,13 @@ int geometry_holds(int H, int rep, int d, int q4, int units, int n_seq, int max_
         for (int head = 0; head < heads; ++head)
           NEED(g.join_off + (int64_t)(team * heads + head + 1) * attn_box_floats(d, nt) * 4 <= g.bar_off);
   }
-  const AttnGeometry most = attn_geometry(H, rep, d, q4, units, 1, max_new, true);   // what the workspace is sized by
-  for (int n = 1; n <= max_new; n *= 2) NEED(attn_geometry(H, rep, d, q4, units, n_seq, n, false).slot_floats <= most.slot_floats);
+  const AttnGeometry most = attn_geometry(H, rep, d, q4, units, slots, 1, max_new, true);   // what the workspace is sized by
+  for (int n = 1; n <= max_new; n *= 2) NEED(attn_geometry(H, rep, d, q4, units, slots, n_seq, n, false).slot_floats <= most.slot_floats);
   return 0;
 }
 
-int shares_hold(int H, int rep, int d, int q4, int units, int max_new, int causal, int n_seq, const int* n, const int* len) {
-  const AttnGeometry g = attn_geometry(H, rep, d, q4, units, n_seq, max_new, causal);
+int shares_hold(int H, int rep, int d, int q4, int units, int slots, int max_new, int causal, int n_seq, const int* n, const int* len) {
+  const AttnGeometry g = attn_geometry(H, rep, d, q4, units, slots, n_seq, max_new, causal);
   int64_t sum = 0;
   for (int b = 0; b < n_seq; ++b) sum += entry_tiles(g.sh, n[b], len[b]);
   if (!sum) return 0;
@@ -120,8 +120,8 @@ def test_shared_memory(plan, d, q4):
         units = units_of(H, d, q4)
         for rep in (1, 2, 3, 4, 7, 8, 9, 71):
             for n_seq in (1, 64, 4096):
-                for max_new in (1, 2, 5, 64, 4096):
-                    assert plan.geometry_holds(H, rep, d, q4, units, n_seq, max_new) == 0, (H, rep, n_seq, max_new)
+                for max_new, slots in ((1, 100), (1, 1 << 20), (2, 100), (5, 1 << 24), (64, 3000), (4096, 70000)):
+                    assert plan.geometry_holds(H, rep, d, q4, units, slots, n_seq, max_new) == 0, (H, rep, n_seq, max_new)
 
 
 def test_shares(plan):
@@ -135,4 +135,4 @@ def test_shares(plan):
         ln = [rng.choice([0, 1, 15, 16, 17, rng.randint(0, 3000)]) for _ in range(n_seq)]
         causal = rng.randint(0, 1)
         arr = C.c_int * n_seq
-        assert plan.shares_hold(H, rep, d, q4, units_of(H, d, q4), max(max(n), 1), causal, n_seq, arr(*n), arr(*ln)) == 0, (H, rep, d, q4, n, ln)
+        assert plan.shares_hold(H, rep, d, q4, units_of(H, d, q4), rng.choice([5000, 1 << 22]), max(max(n), 1), causal, n_seq, arr(*n), arr(*ln)) == 0, (H, rep, d, q4, n, ln)

@@ -73,6 +73,20 @@ def test_several_tokens(gpu_lib, bits, H, Hq, d):
         assert E.epikv_attn_get_error(ctx) == (E.EPIKV_OK, 0)
 
 
+@pytest.mark.parametrize("H,Hq,d", [(8, 32, 128), (11, 11, 64), (4, 16, 64), (2, 4, 128), (3, 6, 64), (1, 8, 128), (9, 9, 128),
+                                     (5, 5, 64)])
+def test_large_tiles(gpu_lib, H, Hq, d):
+    """Caches that could hold enough for the largest tiles of 4-bit rows, short and longer entries."""
+    held = [0, 15, 63, 64, 127, 128, 700, 5000]
+    for block in (16, 0):
+        c = R.Cache(seqs=8, T=20000, H=H, d=d, bits=4, block=block, seed=H + d)
+        ctx = c.context(Hq, 1)
+        q = queries(8, Hq, d)
+        o, l = run(c, ctx, q, [1] * 8, held)
+        check(c, q, o, l, [1] * 8, held, what=f"block {block}")
+        assert E.epikv_attn_get_error(ctx) == (E.EPIKV_OK, 0)
+
+
 @pytest.mark.parametrize("bits", [16, 4])
 def test_prompt_and_long(gpu_lib, bits):
     c = R.Cache(seqs=2, T=20000, H=2, d=128, bits=bits, seed=5)
