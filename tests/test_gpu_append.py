@@ -107,6 +107,29 @@ def test_quantisation_edges(gpu_lib):
         assert c.read(0, 0, 0, 8)[4, 0, 16:32].isnan().all() and c.read(0, 0, 0, 8)[4, 0, :16].isfinite().all()
 
 
+def test_every_bf16_against_every_scale(gpu_lib):
+    """Every positive bf16 value of a binade range beside every maximum's scale: all quotients near a boundary."""
+    mant = torch.arange(128).float() / 128 + 1                       # all significands
+    tops = (mant[None, :] * 2.0 ** torch.arange(-8, 9)[:, None]).flatten()
+    vals = (mant[None, :] * 2.0 ** torch.arange(-5, 1)[:, None]).flatten()
+    x = torch.zeros(tops.numel(), 64)
+    gen = torch.Generator().manual_seed(5)
+    for g in range(4):
+        x[:, 16 * g] = tops
+        pick = torch.randint(0, vals.numel(), (tops.numel(), 15), generator=gen)
+        sign = torch.randint(0, 2, pick.shape, generator=gen).float() * 2 - 1
+        x[:, 16 * g + 1:16 * g + 16] = vals[pick] * sign * 2.0 ** torch.floor(torch.log2(tops))[:, None]
+    x = x.to(torch.bfloat16).cuda().view(-1, 1, 64)
+    n = x.shape[0]
+    c = R.Cache(seqs=1, T=n, H=1, d=64, bits=4, block=0)
+    ctx = c.context(1, n)
+    qkv = torch.cat([x, x, -x.flip(0)], 1).contiguous()
+    _, want = expected(c, qkv, 1, [n], [0], None, None, 0, HALF)
+    append(c, ctx, qkv, 1, [n], [0], None, None, q=False)
+    for w in range(2):
+        assert torch.equal(c.raw(w), want[w])
+
+
 def test_head_scales(gpu_lib):
     s = torch.rand(2, 3, 2, device="cuda") * 30 + 0.01
     c = R.Cache(seqs=2, T=40, H=2, d=64, bits=4, layers=3, kv_scale=s, spread=20.0)
