@@ -8,8 +8,8 @@
 //
 //  - A CTA takes all heads of a group (up to 8) of a run of slots, because a
 //    token's row holds all heads together: whole rows go to shared memory by
-//    asynchronous copies from warps of their own, through a ring of tiles (K
-//    and V in turn) deep enough to cover HBM's latency; eight warps compute, one head each
+//    asynchronous copies from four warps of their own, through a ring of tiles
+//    deep enough to cover HBM's latency; eight warps compute, one head each
 //    (fewer heads: several warps a head, each with its own part of the tile's
 //    slots, joined through shared memory at the end).
 //  - The slots of all entries are one line of tiles that the 152 CTAs share
@@ -21,8 +21,8 @@
 //    (S^T = K Q^T, O^T = V^T P^T): a KV head has 1 to 8 queries in a decode
 //    step, and the instruction's narrow side is 8 wide, where tcgen05's
 //    narrowest shape would spend 128 x 8 outputs and a trip through tensor
-//    memory on them.  The rotation of P from one product's result layout to the other's
-//    operand layout is one transposing move per 8 x 8.
+//    memory on them.  P goes from one product's result layout to the other's
+//    operand layout by one transposing move per 8 x 8.
 //
 // A 4-bit cache stays in 4 bits until the registers: the layout is such that a
 // lane's channels are neighbours (any order of channels serves a dot product
@@ -30,7 +30,17 @@
 // and the product with the E4M3 scale is exact in half precision (2 + 4
 // significant bits).  Queries enter as halves scaled by a power of two per
 // row, probabilities as halves times 2^7 (11 bits down to 2^-21).  For
-// a bf16 cache the probabilities go in as two bf16 terms (16 bits).
+// a bf16 cache the probabilities go in as two bf16 terms (16 bits), for which
+// the tensor instructions have time: one term alone would add an error of the
+// output's own rounding.
+//
+// What it measured (one token an entry, 32 query and 8 KV heads of 128): bf16,
+// 64 x 5,120 slots 204 us, 6.6 TB/s; 32 x 8,192 166 us: HBM.  4 bits, 32 x
+// 8,256 slots 71 us, 4.3 TB/s: 266 instructions for 16 slots of a head (64 of
+// them conversions, 64 products with scales, 16 tensor instructions) at 0.46 a
+// cycle and scheduler, with two computing warps each; four warps a scheduler
+// (96 or 128 registers) were slower, 104 to 121 us.  2,048 slots of one
+// sequence 13 us, 4 x 136 14 us: two launches and their chains of reads.
 #include <cuda.h>
 
 #include "attn.cuh"
@@ -209,9 +219,9 @@ __device__ __forceinline__ void zero_rows(char* dst, int bytes) {
   for (int i = 0; i < bytes; i += 16) *reinterpret_cast<uint4*>(dst + i) = make_uint4(0, 0, 0, 0);
 }
 
-// A copying warp's instruction chains are what its tiles cost (one warp alone took 2,000 cycles a tile of 18 KB, which
-// is a third of HBM's rate), so the tiles go round four warps; what a tile needs is formed once for K and V, its table
-// entries are read a turn ahead, and quotients go by a float reciprocal (exact: slots are below 2^24, and a quotient
+// A copying warp's instruction chains are what its tiles cost (one warp alone took 2,000 cycles for 18 KB, a third of
+// HBM's rate), so the tiles go round four warps; what a tile needs is formed once for K and V, its table entries are read
+// a turn ahead, and quotients go by a float reciprocal (exact: slots are below 2^24, and a quotient
 // that is off by one is put right).
 struct Divider {
   int d;
@@ -270,8 +280,8 @@ struct Ring {
 };
 
 // 4-bit rows: a bulk copy for each run of slots that is one piece of memory (a block's, where its rows stand side by
-// side), each 4 to 18 KB.  A lane looks after one run; where a tile has over 32 (rows that stand apart), the others are
-// looked up as they are copied.
+// side), each 4 to 18 KB (a copy of a row alone keeps the copy engine for about 110 cycles: a third of HBM's rate).  A
+// lane looks after one run; where a tile has over 32 (rows that stand apart), the others are looked up as they are copied.
 template <int D>
 __device__ void copy_q4(char* smem, uint64_t* full, uint64_t* empty, const Waiter& wait, const AttnState& st,
                         const AttnDims& dm, const Geometry& ge, const KvDev& kv, int layer, const Walker& walker,
@@ -422,11 +432,14 @@ __device__ void copy_tensor(char* smem, uint64_t* full, uint64_t* empty, const W
     char* dst = smem + ring.place * (2 * ge.half_bytes) + lane * bytes;
     if (ring.turn) wait(&empty[ring.place], (ring.turn & 1) ^ 1);
     const uint32_t blocks = __ballot_sync(0xffffffffu, there);
-    if (__popc(blocks) * 16 < sh.tile) {   // blocks that nothing fills
-      if (!there && 16 * lane < sh.tile) {
-        zero_rows(dst, bytes);
-        zero_rows(dst + ge.half_bytes, bytes);
-      }
+    if (__popc(blocks) * 16 < sh.tile) {   // blocks that nothing fills: a probability of 0 must not meet what stood there
+      for (int b = 0; b < sh.tile / 16; ++b)
+        if (!(blocks >> b & 1))
+          for (int i = lane * 16; i < bytes; i += 512) {
+            char* at = smem + ring.place * (2 * ge.half_bytes) + b * bytes + i;
+            *reinterpret_cast<uint4*>(at) = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(at + ge.half_bytes) = make_uint4(0, 0, 0, 0);
+          }
       fence_proxy_async_smem();
       __syncwarp();
     }
