@@ -154,6 +154,13 @@ struct Walk {
   int b, group, run, at, tiles;   // the item, its first tile (below 0: an earlier CTA's), its tiles
   Entry e;
 };
+// Tiles of the runs before `end` of a group of an entry, by a whole warp.
+__device__ __forceinline__ int tiles_before(const AttnShape& sh, int n, int len, int end, int lane) {
+  int64_t sum = 0;
+  for (int r = lane; r < end; r += 32) sum += item_tiles(sh, n, len, r);
+  return (int)__reduce_add_sync(0xffffffffu, (unsigned)(sum < kMostTiles ? sum : kMostTiles));
+}
+
 struct Walker {
   const int* pre;
   const Batch& ba;
@@ -180,6 +187,36 @@ struct Walker {
       }
     }
     w->tiles = item_tiles(sh, w->e.n, w->e.len, w->run);
+  }
+  // From the entry's first item, `from`, to the one of the CTA's first tile, by a whole warp.
+  __device__ __forceinline__ void seek(Walk* w, const Walk& from, int lane) const {
+    Walk at = from;
+    const int runs = row_runs(sh, at.e.n);
+    if (sh.groups > 1 || runs > 1) {
+      const int of_group = (pre[at.b + 1] - pre[at.b]) / sh.groups;
+      at.group = -at.at / of_group;
+      at.at += at.group * of_group;
+      for (int r0 = 0;; r0 += 32) {
+        const int t = r0 + lane < runs ? item_tiles(sh, at.e.n, at.e.len, r0 + lane) : 0;
+        int upto = t;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int v = __shfl_up_sync(0xffffffffu, upto, o);
+          if (lane >= o) upto += v;
+        }
+        const unsigned behind = __ballot_sync(0xffffffffu, at.at + upto > 0);
+        if (behind || r0 + 32 >= runs) {
+          const int k = behind ? __ffs(behind) - 1 : 0;
+          at.run = r0 + k;
+          at.tiles = __shfl_sync(0xffffffffu, t, k);
+          at.at += __shfl_sync(0xffffffffu, upto - t, k);
+          break;
+        }
+        at.at += __shfl_sync(0xffffffffu, upto, 31);
+      }
+    }
+    if (lane == 0) *w = at;
+    __syncwarp();
   }
   // Moves the warp's walk on to the item of tile i.
   __device__ __forceinline__ void to(Walk* w, int i, int lane) const {
@@ -314,11 +351,11 @@ __device__ void copy_q4(char* smem, uint64_t* full, uint64_t* empty, const Waite
   int x = warp;
   if (x < tiles) look(x);
   for (; x < tiles; x += ge.copiers) {
-    const int rows = max(upto - at, 0), row0 = at - s0, n_now = n, seq_now = seq, s_now = s0;
+    const int rows = max(upto - at, 0), row0 = at - s0, n_now = n, seq_now = seq, s_now = s0, run_now = run0;
     const int64_t off = rows ? offset_of(kv, layer, seq, next) : -1;
     if (rows && off < 0) set_error(st.err, EPIKV_DEV_SLOT);
     int there = off >= 0 ? rows : 0;
-    const int more = max(n_now - 32 * rl, 0);     // slots behind the lanes' runs: runs of one slot, n <= 128
+    const int more = max(n_now - (32 * rl - (s_now - run_now * rl)), 0);   // slots behind the lanes' runs
     for (int r = n_now - more + lane; r < n_now; r += 32) {
       const bool in = offset_of(kv, layer, seq, place_of(kv, block, layer, seq, s0 + r)) >= 0;
       there += in;
@@ -464,7 +501,7 @@ __device__ void copy_bf16(char* smem, uint64_t* full, uint64_t* empty, const Wai
                           const AttnDims& dm, const Geometry& ge, const KvDev& kv, int layer, const Walker& walker,
                           Walk* w, int tiles, int warp, int lane) {
   const AttnShape& sh = ge.sh;
-  constexpr int kMost = kMaxTile / 32;
+  constexpr int kMost = 4;   // 16 slots of up to eight warps
   const Divider block(kv.layout == EPIKV_LAYOUT_CONTIGUOUS ? 1 : kv.block_size);
   Ring ring(ge.stages, warp);
   int group = -1, pieces = 0, at_once = 1, sub = 0, col = 0;   // 16-byte pieces of a row; rows taken at once
@@ -564,15 +601,22 @@ __global__ void __launch_bounds__(threads_of(D), 1)
   if (tid < 256)
     for (int i = 0; i < per; ++i) {
       const int b = tid * per + i;
-      if (b < ba.n_seq) {
-        int64_t t = batch_entry(ba, dm, b, sh.causal, st.err, &e0) ? entry_tiles(sh, e0.n, e0.len) : 0;
-        if (t > kMostTiles - mine) {
-          set_error(st.err, EPIKV_DEV_CAPACITY);
-          t = 0;
-        }
-        mine += (int)t;
-        pre[b + 1] = (int)t;
+      const bool there = b < ba.n_seq && batch_entry(ba, dm, b, sh.causal, st.err, &e0);
+      const int runs = there ? row_runs(sh, e0.n) : 0;
+      int64_t t = runs == 1 ? item_tiles(sh, e0.n, e0.len, 0) : 0;
+      for (unsigned many = __ballot_sync(0xffffffffu, runs > 1); many; many &= many - 1) {   // such entries' runs by the warp
+        const int k = __ffs(many) - 1;
+        const int sum = tiles_before(sh, __shfl_sync(0xffffffffu, e0.n, k), __shfl_sync(0xffffffffu, e0.len, k),
+                                     __shfl_sync(0xffffffffu, runs, k), lane);
+        if (lane == k) t = sum;
       }
+      t *= sh.groups;
+      if (t > kMostTiles - mine) {
+        set_error(st.err, EPIKV_DEV_CAPACITY);
+        t = 0;
+      }
+      mine += (int)t;
+      if (b < ba.n_seq) pre[b + 1] = (int)t;
     }
   int run = mine;
 #pragma unroll
@@ -608,11 +652,7 @@ __global__ void __launch_bounds__(threads_of(D), 1)
   if (lo == hi) return;
   Walk* w = &s_walk[warp];
   const Walker walker{pre, ba, dm, sh, st.err};
-  if (lane == 0) {
-    *w = s_first;
-    while (w->at + w->tiles <= 0) walker.step(w);
-  }
-  __syncwarp();
+  walker.seek(w, s_first, lane);
   const int tiles = hi - lo;
   const Waiter wait{gave_up, st.err};
   // With 8 + 4 warps of 168 registers the copying ones give most of theirs to the computing ones:
@@ -1145,7 +1185,7 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttnState st, 
   const int group = kh / attn_group(dm.d), head = kh % attn_group(dm.d);
   int at = p0;
   if (sh.groups > 1) at += group * ((p1 - p0) / sh.groups);
-  for (int i = 0; i < run; ++i) at += item_tiles(sh, e.n, e.len, i);
+  if (run) at += tiles_before(sh, e.n, e.len, run, lane);
   const int tiles = item_tiles(sh, e.n, e.len, run);
   const int c0 = cta_of_tile(at, total), c1 = cta_of_tile(at + tiles - 1, total);
   if (c0 == c1) return;

@@ -70,7 +70,6 @@ EPIKV_PLAN int cta_of_tile(int x, int total) {
 // ---- shared memory of a CTA: the ring of tiles, boxes to join a head's warps, barriers, the entries' first tiles
 constexpr int kAttnSmem = 225 * 1024;   // dynamic shared memory, at most (its start is moved up to a multiple of 1,024)
 constexpr int kMaxStages = 8;           // tiles of the ring
-constexpr int kMaxTile = 128;           // slots of a tile, at most
 
 struct AttnGeometry {
   AttnShape sh;
@@ -124,8 +123,7 @@ EPIKV_PLAN AttnGeometry attn_geometry(int H, int rep, int d, bool q4, int units,
   const int nt = attn_row_blocks(d, rep, max_new), group = attn_group(d);
   const int heads = H < group ? H : group;                          // of the first group
   const int rest = H > group && H % group ? H % group : heads;      // of the last one
-  int tile = 16 * attn_teams(heads, group) * attn_sub_blocks(q4, d, nt, (int64_t)slots * n_seq);
-  if (tile > kMaxTile) tile = kMaxTile;
+  const int tile = 16 * attn_teams(heads, group) * attn_sub_blocks(q4, d, nt, (int64_t)slots * n_seq);
   ge.sub = attn_sub_blocks(q4, d, nt, (int64_t)slots * n_seq);
   int rows_log = 3, tile_log = 4;
   while (1 << rows_log < nt * 8) ++rows_log;

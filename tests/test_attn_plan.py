@@ -22,7 +22,7 @@ int geometry_holds(int H, int rep, int d, int q4, int units, int slots, int n_se
   NEED(g.copiers >= 1 && g.copiers <= kAttnCopyWarps && g.copiers <= g.stages);
   NEED(g.sh.rows == 1 << g.sh.rows_log && g.sh.tile == 1 << g.sh.tile_log);
   NEED(g.sh.rows == 8 * nt && nt * d <= 256);
-  NEED(g.sh.tile % 16 == 0 && g.sh.tile >= 16 && g.sh.tile <= kMaxTile);
+  NEED(g.sh.tile % 16 == 0 && g.sh.tile >= 16 && g.sh.tile <= (q4 ? 512 : 128));
   unsigned rows = 0;
   for (int r = 0; r < 8; ++r) rows |= 1u << (g.order >> (4 * r) & 7);
   NEED(rows == 255 && !(g.order & 0x88888888u));
