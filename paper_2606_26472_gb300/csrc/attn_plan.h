@@ -117,14 +117,14 @@ EPIKV_PLAN int attn_teams(int heads, int warps) {
 constexpr int attn_box_floats(int d, int nt) { return (d / 16 * nt * 4 + 4 * nt) * 32; }
 
 // units: 2-byte units of a cache row; slots: of a sequence's cache.
-EPIKV_PLAN AttnGeometry attn_geometry(int H, int rep, int d, bool q4, int units, int slots, int n_seq, int max_new,
-                                      bool causal) {
+EPIKV_PLAN AttnGeometry attn_geometry_of(int H, int rep, int d, bool q4, int units, int sub, int n_seq, int max_new,
+                                         bool causal) {
   AttnGeometry ge;
   const int nt = attn_row_blocks(d, rep, max_new), group = attn_group(d);
   const int heads = H < group ? H : group;                          // of the first group
   const int rest = H > group && H % group ? H % group : heads;      // of the last one
-  const int tile = 16 * attn_teams(heads, group) * attn_sub_blocks(q4, d, nt, (int64_t)slots * n_seq);
-  ge.sub = attn_sub_blocks(q4, d, nt, (int64_t)slots * n_seq);
+  const int tile = 16 * attn_teams(heads, group) * sub;
+  ge.sub = sub;
   int rows_log = 3, tile_log = 4;
   while (1 << rows_log < nt * 8) ++rows_log;
   while (1 << tile_log < tile) ++tile_log;
@@ -155,6 +155,15 @@ EPIKV_PLAN AttnGeometry attn_geometry(int H, int rep, int d, bool q4, int units,
   ge.smem_bytes = ge.pre_off + pre;
   ge.slot_floats = group * ge.sh.rows * (d + 2);
   return ge;
+}
+
+EPIKV_PLAN AttnGeometry attn_geometry(int H, int rep, int d, bool q4, int units, int slots, int n_seq, int max_new,
+                                      bool causal) {
+  const int sub = attn_sub_blocks(q4, d, attn_row_blocks(d, rep, max_new), (int64_t)slots * n_seq);
+  const AttnGeometry ge = attn_geometry_of(H, rep, d, q4, units, sub, n_seq, max_new, causal);
+  // four blocks a warp only where the ring then holds three tiles (4 KV heads of 128, 64 x 8,192 slots, two tiles of four
+  // blocks 105 us, five of two 75)
+  return ge.stages < 3 && sub == 4 ? attn_geometry_of(H, rep, d, q4, units, 2, n_seq, max_new, causal) : ge;
 }
 
 }  // namespace epikv

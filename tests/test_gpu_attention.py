@@ -216,6 +216,34 @@ def test_strided_rows_streams_and_graphs(gpu_lib, bits):
 
 
 @pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("H,T,block", [(8, 300, 16), (2, 300, 16), (8, 20000, 16), (8, 300, 5), (12, 300, 16), (2, 300, 0)])
+def test_rows_that_stand_apart(gpu_lib, bits, H, T, block):
+    """A token's rows further apart than they are long, and K's and V's blocks in one allocation."""
+    d, S, gap = 64, 8, 24
+    c = R.Cache(seqs=S, T=T, H=H, d=d, bits=bits, block=block, seed=H)
+    ctx = c.context(2 * H, 2)
+    units, st = c.units, c.units + gap
+    n = c.raw(0).shape[0]
+    wide = torch.full((n, 2, st), float("nan"), dtype=torch.bfloat16, device="cuda")     # [row][K, V][units and a gap]
+    for w in range(2):
+        wide[:, w, :units].view(torch.int16).copy_(c.raw(w).view(torch.int16).view(n, units))
+    k, v = wide.view(-1), wide.view(-1)[st:]
+    if block:
+        kv = E.kv_view(k, v, layout=E.EPIKV_LAYOUT_PAGED, stride_layer=0, stride_block=block * 2 * st, stride_token=2 * st,
+                       block_table=c.c.block_table, max_blocks_per_seq=c.c.max_blocks, block_size=block,
+                       num_blocks=c.c.num_blocks)
+    else:
+        kv = E.kv_view(k, v, layout=E.EPIKV_LAYOUT_CONTIGUOUS, stride_layer=0, stride_seq=T * 2 * st, stride_token=2 * st)
+    held, new = [0, 1, 17, 40, 65, 128, 199, 298], [2] * S
+    q = queries(2 * S, 2 * H, d)
+    seq_ids, cu, ln = R.batch(new, held)
+    o, l = torch.empty_like(q), torch.empty(2 * S, 2 * H, device="cuda")
+    E.epikv_attention(ctx, 0, S, seq_ids, cu, 2, ln, E.rows(q), E.rows(o), kv, lse=l)
+    check(c, q, o, l, new, held)
+    assert E.epikv_attn_get_error(ctx) == (E.EPIKV_OK, 0)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
 def test_offsets_past_32_bits(gpu_lib, bits):
     """Two blocks 6 GB apart in one pool."""
     H, d, bs = 8, 128, 16
