@@ -471,7 +471,11 @@ epikv_status epikv_append(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, con
  *             slots (a shared prefix; join with d_lse)
  *   d_lse     float [total_new][num_heads] or NULL: log of the sum of exponentials
  * A row that sees no slot gives zeros and -infinity.  Slots that a row does not
- * see do not reach it, whatever they hold. */
+ * see do not reach it, whatever they hold (memory of the view up to the next
+ * multiple of 16 slots may be read: a contiguous cache has max_cache_tokens
+ * slots, or stride_seq / stride_token, for every sequence).  A sequence's tiles
+ * of 16 slots and more are counted in 32 bits: entries that need over 2^23
+ * (134 million slots) are EPIKV_DEV_CAPACITY. */
 epikv_status epikv_attention(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* d_seq_ids,
                              const int32_t* d_cu_new, int32_t max_new, const int32_t* d_len, int32_t len_stride,
                              int32_t causal, const epikv_rows* q, const epikv_rows* out, float* d_lse,

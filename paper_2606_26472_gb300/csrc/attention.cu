@@ -1024,11 +1024,24 @@ __global__ void __launch_bounds__(threads_of(D), 1)
         values(base, pb);
       } else {
         const int first_row = w->run * sh.rows, last_row = min(first_row + sh.rows, rows_of(sh, w->e.n)) - 1;
+#pragma unroll 1   // rare: its instructions should not stand between the others
+        for (int u = 0; u < SUB; ++u) {
+          uint32_t pu[NT][kBf16 ? 4 : 2];
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int y = 0; y < (kBf16 ? 4 : 2); ++y) {
+              pu[nt][y] = pb[0][nt][y];
+#pragma unroll
+              for (int v = 1; v < SUB; ++v)
+                if (u == v) pu[nt][y] = pb[v][nt][y];
+            }
           for (int i = first_row / sh.rep; i <= last_row / sh.rep; ++i) {
             // of these slots, those that token i sees
             const int n = w->e.len + (sh.causal ? i + 1 : 0) - (s0 + (u * teams + team) * 16);
+            uint32_t mine = 0;   // bit 2 nt + c: column c of block nt is token i's
+#pragma unroll 1
+            for (int k = 0; k < 2 * NT; ++k) mine |= ((first_row + k / 2 * 8 + 2 * t + (k & 1)) / sh.rep == i ? 1u : 0u) << k;
             const uint32_t m0 = (k0 < n ? 0xffffu : 0u) | (k1 < n ? 0xffff0000u : 0u);
             const uint32_t m8 = (k0 + 8 < n ? 0xffffu : 0u) | (k1 + 8 < n ? 0xffff0000u : 0u);
             each(base, u, [&](int mt, uint32_t (&a)[4]) {
@@ -1039,14 +1052,15 @@ __global__ void __launch_bounds__(threads_of(D), 1)
                 float keep[4];
 #pragma unroll
                 for (int y = 0; y < 4; ++y) keep[y] = o[mt][nt][y];
-                mma<FMT>(o[mt][nt], z, pb[u][nt][0], pb[u][nt][1]);
-                if constexpr (kBf16) mma<FMT>(o[mt][nt], z, pb[u][nt][2], pb[u][nt][3]);
+                mma<FMT>(o[mt][nt], z, pu[nt][0], pu[nt][1]);
+                if constexpr (kBf16) mma<FMT>(o[mt][nt], z, pu[nt][2], pu[nt][3]);
 #pragma unroll
                 for (int y = 0; y < 4; ++y)
-                  if ((first_row + nt * 8 + 2 * t + (y & 1)) / sh.rep != i) o[mt][nt][y] = keep[y];
+                  if (!(mine >> (2 * nt + (y & 1)) & 1)) o[mt][nt][y] = keep[y];
               }
             });
           }
+        }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&empty[stage]);
