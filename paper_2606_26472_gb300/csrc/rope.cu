@@ -174,11 +174,13 @@ __global__ void rope_table_kernel(epikv_rope_config c, int n_pos, float2* table)
   }
 }
 
-// kBatch heads of a thread are in flight; their loads go out before the position and the table's row are known.
+// kBatch heads of a thread are in flight; their loads go out before the position and the table's row are known.  More of
+// them, or registers held down for more CTAs, cost occupancy or loads in flight: 8,192 x 40 heads of bf16 two 32.4, three
+// 31.7 us (held to 72 registers 34.1); 4,096 x 40 heads of 32-bit data one 27.6, two 30.5 us.
 template <typename T, int V>
 __global__ void __launch_bounds__(kBlock) rope_kernel(int32_t* err, Rows x, Rows y, const int32_t* __restrict__ pos,
                                                       RopeDev r, int n_tokens, int heads, int d, float sign) {
-  constexpr int kBatch = sizeof(T) == 4 ? 2 : 3;
+  constexpr int kBatch = sizeof(T) == 4 ? 1 : 3;
   const int U = d / (2 * V), slots = kBlock / U;  // units of a head; heads that the block takes at once
   const int u = threadIdx.x % U, slot = threadIdx.x / U;
   const int tpb = max(1, slots / heads);          // tokens of this block
