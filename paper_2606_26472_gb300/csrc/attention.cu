@@ -587,10 +587,14 @@ __global__ void __launch_bounds__(threads_of(D), 1)
   const AttnShape& sh = ge.sh;
 
   __shared__ Walk s_walk[kWarps + kAttnCopyWarps], s_first;
-  if (tid < 2 * kMaxStages) mbar_init(&full[tid], tid >= kMaxStages ? kWarps : FMT == EPIKV_CACHE_BF16 && !maps.on ? 32 : 1);
-  if (tid == 0) {
+  if (tid == 0) {   // the fences order this thread's own initialisations before the copy engine's use of them: all are its own
+    for (int s = 0; s < kMaxStages; ++s) {
+      mbar_init(&full[s], FMT == EPIKV_CACHE_BF16 && !maps.on ? 32 : 1);
+      mbar_init(&empty[s], kWarps);
+    }
     *gave_up = 0;
     fence_barrier_init();
+    fence_proxy_async_smem();
   }
   pdl_wait();
   pdl_trigger();
