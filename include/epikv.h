@@ -470,7 +470,10 @@ epikv_status epikv_append(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, con
  *             reads slots 0 .. d_len[b] + i.  0: every query reads the d_len[b]
  *             slots (a shared prefix; join with d_lse)
  *   d_lse     float [total_new][num_heads] or NULL: log of the sum of exponentials
- * A row that sees no slot gives zeros and -infinity.  Slots that a row does not
+ * A row that sees no slot, or only slots of score -infinity, gives zeros and
+ * -infinity.  An infinite value in a slot that a row sees is the row's output in
+ * that channel, however small its probability (NaN beside one of the other sign,
+ * or where the slot's score is -infinity).  Slots that a row does not
  * see do not reach it, whatever they hold (memory of the view up to the next
  * multiple of 16 slots may be read: a contiguous cache has max_cache_tokens
  * slots, or stride_seq / stride_token, for every sequence).  A sequence's tiles

@@ -147,6 +147,14 @@ __device__ __forceinline__ uint32_t bf162_of(float lo, float hi) {
   const __nv_bfloat162 r = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&r);
 }
+// acc + 0 a: NaN in a half from the first value on that is infinite or NaN.
+__device__ __forceinline__ void note_unbounded(uint32_t& acc, uint32_t a) {
+  asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(a), "r"(0u));
+}
+
+// What brings sums that were taken against one maximum to a larger one; never 0 (2^-149 of a bounded sum is nothing,
+// of an infinite one infinite).
+__device__ __forceinline__ float weight_of(float x) { return fmaxf(ex2(x), __uint_as_float(1u)); }
 
 // A warp's walk along its CTA's items, in shared memory: its first lane moves it on, and what the loops over tiles do
 // not need stays out of their registers.  Tiles are counted from the CTA's first.
@@ -663,6 +671,7 @@ __global__ void __launch_bounds__(threads_of(D), 1)
   // 256 x 216 + 128 x 72 = 256 x 200 + 128 x 104 = 384 x 168.
   constexpr bool kSplit = kThreads == 384;
   constexpr int kCopyRegs = FMT == EPIKV_CACHE_BF16 ? 104 : 72, kMoreRegs = FMT == EPIKV_CACHE_BF16 ? 200 : 216;
+  static_assert(FMT != EPIKV_CACHE_BF16 || SUB == 1, "the path of infinite values takes one block of slots");
   static_assert(kWarps * kMoreRegs + kAttnCopyWarps * kCopyRegs <= (kWarps + kAttnCopyWarps) * 168 || !kSplit,
                 "the computing warps would wait for registers that nobody gives");
   if (warp >= kWarps) {
@@ -963,7 +972,7 @@ __global__ void __launch_bounds__(threads_of(D), 1)
             v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
             v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
             const float mn = fmaxf(m[nt][c], v * cf[nt][c]);
-            alpha[c] = mn == -INFINITY ? 1.f : ex2(m[nt][c] - mn);
+            alpha[c] = mn == -INFINITY ? 1.f : weight_of(m[nt][c] - mn);
             m[nt][c] = mn;
             l[nt][c] *= alpha[c];
           }
@@ -972,6 +981,15 @@ __global__ void __launch_bounds__(threads_of(D), 1)
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[j][nt][i] *= alpha[i & 1];
         }
+      }
+      uint32_t odd[4] = {0u, 0u, 0u, 0u};   // bf16: whether a value is infinite or NaN
+      if constexpr (kBf16) {
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+          each(base, u, [&](int, uint32_t (&a)[4]) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) note_unbounded(odd[i], a[i]);
+          });
       }
       uint32_t pb[SUB][NT][kBf16 ? 4 : 2];
 #pragma unroll
@@ -1000,16 +1018,21 @@ __global__ void __launch_bounds__(threads_of(D), 1)
       }
 
       // ---- their sum of values, and the next tile's scores: two chains that do not wait for each other
-      // Slots that some rows see and others do not may hold an infinity or a NaN, which a probability of 0 does not
-      // silence: then the rows of each token go by themselves, the values that they do not see taken as 0.
+      // An infinity or a NaN among the values goes by a path of its own.  In a slot that some rows do not see, a
+      // probability of 0 does not silence it.  In one that they see it has to be weighted by one number above 0, and
+      // bf16's two terms of a probability may be of unlike signs or 0.  (4-bit values are finite or NaN, and NaN in a seen
+      // slot stays NaN: only tiles with unseen slots are looked through.)
       bool apart = false;
-      if (s0 + sh.tile > least) {
-        constexpr uint32_t kExp = kBf16 ? 0x7f80u : 0x7c00u;
+      if constexpr (kBf16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) apart |= (odd[i] & 0x7fff7fffu) != 0;   // else 0 or -0
+        apart = __any_sync(0xffffffffu, apart);
+      } else if (s0 + sh.tile > least) {
 #pragma unroll 1
         for (int u = 0; u < SUB; ++u)
           each(base, u, [&](int, uint32_t (&a)[4]) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) apart |= (a[i] & kExp) == kExp || (a[i] >> 16 & kExp) == kExp;
+            for (int i = 0; i < 4; ++i) apart |= (a[i] & 0x7c00u) == 0x7c00u || (a[i] >> 16 & 0x7c00u) == 0x7c00u;
           });
         apart = __any_sync(0xffffffffu, apart);
       }
@@ -1028,6 +1051,25 @@ __global__ void __launch_bounds__(threads_of(D), 1)
         values(base, pb);
       } else {
         const int first_row = w->run * sh.rows, last_row = min(first_row + sh.rows, rows_of(sh, w->e.n)) - 1;
+        // the weights of infinities: 1, or 0 where the score is minus infinity
+        uint32_t whole[kBf16 ? SUB : 1][NT][2];
+        if constexpr (kBf16) {
+          float raw[SUB][NT][4];
+          keys(base, raw);
+#pragma unroll
+          for (int u = 0; u < SUB; ++u)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int r = first_row + nt * 8 + 2 * t + (i & 1);
+                const bool sees = s0 + (u * teams + team) * 16 + g + (i >> 1) * 8 < w->e.len + (sh.causal ? r / sh.rep + 1 : 0);
+                raw[u][nt][i] = !sees || raw[u][nt][i] == -INFINITY ? 0.f : raw[u][nt][i] != raw[u][nt][i] ? raw[u][nt][i] : 1.f;
+              }
+#pragma unroll
+              for (int y = 0; y < 2; ++y) whole[u][nt][y] = transpose8x8(bf162_of(raw[u][nt][2 * y], raw[u][nt][2 * y + 1]));
+            }
+        }
 #pragma unroll 1   // rare: its instructions should not stand between the others
         for (int u = 0; u < SUB; ++u) {
           uint32_t pu[NT][kBf16 ? 4 : 2];
@@ -1040,16 +1082,26 @@ __global__ void __launch_bounds__(threads_of(D), 1)
               for (int v = 1; v < SUB; ++v)
                 if (u == v) pu[nt][y] = pb[v][nt][y];
             }
+          // the rows of each token by themselves, the values that they do not see taken as 0; a block behind the tile: all
           for (int i = first_row / sh.rep; i <= last_row / sh.rep; ++i) {
             // of these slots, those that token i sees
-            const int n = w->e.len + (sh.causal ? i + 1 : 0) - (s0 + (u * teams + team) * 16);
+            const int at = (u * teams + team) * 16;
+            const int n = !kBf16 || at < sh.tile ? w->e.len + (sh.causal ? i + 1 : 0) - (s0 + at) : 0;
             uint32_t mine = 0;   // bit 2 nt + c: column c of block nt is token i's
 #pragma unroll 1
             for (int k = 0; k < 2 * NT; ++k) mine |= ((first_row + k / 2 * 8 + 2 * t + (k & 1)) / sh.rep == i ? 1u : 0u) << k;
             const uint32_t m0 = (k0 < n ? 0xffffu : 0u) | (k1 < n ? 0xffff0000u : 0u);
             const uint32_t m8 = (k0 + 8 < n ? 0xffffu : 0u) | (k1 + 8 < n ? 0xffff0000u : 0u);
             each(base, u, [&](int mt, uint32_t (&a)[4]) {
-              const uint32_t z[4] = {a[0] & m0, a[1] & m0, a[2] & m8, a[3] & m8};
+              uint32_t z[4] = {a[0] & m0, a[1] & m0, a[2] & m8, a[3] & m8}, inf[4];
+              if constexpr (kBf16) {
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                  const uint32_t odd = ((z[y] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((z[y] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+                  inf[y] = z[y] & odd;
+                  z[y] &= ~odd;
+                }
+              }
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
                 // only the columns of token i; the others keep their sums
@@ -1057,7 +1109,10 @@ __global__ void __launch_bounds__(threads_of(D), 1)
 #pragma unroll
                 for (int y = 0; y < 4; ++y) keep[y] = o[mt][nt][y];
                 mma<FMT>(o[mt][nt], z, pu[nt][0], pu[nt][1]);
-                if constexpr (kBf16) mma<FMT>(o[mt][nt], z, pu[nt][2], pu[nt][3]);
+                if constexpr (kBf16) {
+                  mma<FMT>(o[mt][nt], z, pu[nt][2], pu[nt][3]);
+                  mma<FMT>(o[mt][nt], inf, whole[0][nt][0], whole[0][nt][1]);
+                }
 #pragma unroll
                 for (int y = 0; y < 4; ++y)
                   if (!(mine >> (2 * nt + (y & 1)) & 1)) o[mt][nt][y] = keep[y];
@@ -1111,8 +1166,8 @@ __global__ void __launch_bounds__(threads_of(D), 1)
           for (int c = 0; c < 2; ++c) {
             const float m2 = from[(KS * NT * 4 + nt * 4 + c) * 32], l2 = from[(KS * NT * 4 + nt * 4 + 2 + c) * 32];
             const float mn = fmaxf(m[nt][c], m2), base = mn == -INFINITY ? 0.f : mn;
-            a[c] = ex2(m[nt][c] - base);
-            b[c] = ex2(m2 - base);
+            a[c] = weight_of(m[nt][c] - base);
+            b[c] = weight_of(m2 - base);
             l[nt][c] = l[nt][c] * a[c] + l2 * b[c];
             m[nt][c] = mn;
           }
@@ -1226,7 +1281,7 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttnState st, 
     const float base = top == -INFINITY ? 0.f : top;
     for (int i = lane; i < parts; i += 32) {
       const float2 ml = s_ml[i][warp];
-      const float weight = ex2(ml.x - base);
+      const float weight = weight_of(ml.x - base);
       s_ml[i][warp].x = weight;
       sum += ml.y * weight;
     }

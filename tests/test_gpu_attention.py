@@ -145,6 +145,99 @@ def test_values_of_one_unseen_row(gpu_lib, bits):
     assert torch.equal(before[:5], after[:5]) and bool(after[5:].isnan().all())
 
 
+def unbounded_reference(c, q, new, held, scale, what):
+    """float64 outputs of the batch, infinities among the values included: the sums of products as they are."""
+    outs, t = [], 0
+    for b, n in enumerate(new):
+        top = held[b] + n
+        k, v = c.read(0, 0, b, top), c.read(1, 0, b, top)
+        outs.append(R.attention64(q[t:t + n], k, v, [held[b] + i + 1 for i in range(n)], scale))
+        t += n
+    return outs
+
+
+@pytest.mark.parametrize("block", [16, 7, 0])
+@pytest.mark.parametrize("H,Hq,d", [(8, 32, 128), (9, 9, 128), (9, 18, 64), (1, 8, 128), (3, 6, 64), (6, 6, 256), (5, 5, 256)])
+@pytest.mark.parametrize("new", [1, 5])
+def test_infinite_values(gpu_lib, H, Hq, d, block, new):
+    """Infinities of both signs in V's slots (seen by all rows, by some, by none; of one part of a long entry or the
+    other): an output is the infinity that its row sees, NaN where it sees both signs, and as ever in other channels."""
+    held = [3, 16, 40, 900, 2500]
+    c = R.Cache(seqs=5, T=2600, H=H, d=d, bits=16, block=block, seed=H + d)
+    pool = c.c.v.view(-1, H, d)
+    inf = math.inf
+    for b, n in enumerate(held):
+        for slot, h, ch, x in ((0, 0, 0, inf), (n // 2, H - 1, 1, -inf), (n // 3, H - 1, d - 1, inf), (n, 0, 5, inf),
+                               (n - 1, H // 2, 7, inf), (n // 2, H // 2, 7, -inf), (n + new - 1, H - 1, d - 2, -inf),
+                               (n + new, 0, 9, inf), (n + new + 1, H - 1, 3, math.nan)):
+            pool[c.index(0, b, torch.tensor([slot])), h, ch] = x
+    ctx = c.context(Hq, 8)
+    q = queries(5 * new, Hq, d)
+    o, l = run(c, ctx, q, [new] * 5, held)
+    assert E.epikv_attn_get_error(ctx) == (E.EPIKV_OK, 0)
+    seen = 0
+    for b, ref in enumerate(unbounded_reference(c, q, [new] * 5, held, d ** -0.5, "")):
+        want, lse, big, qk = ref
+        part, lpart = o[b * new:(b + 1) * new], l[b * new:(b + 1) * new]
+        odd = ~want.isfinite()
+        seen += int(want.isinf().sum())
+        assert torch.equal(part[odd].double().nan_to_num(nan=7.0), want[odd].nan_to_num(nan=7.0)), f"entry {b}"
+        assert part[~odd].isfinite().all(), f"entry {b}"
+        zero = torch.zeros_like(want)
+        R.assert_attention_close(torch.where(odd, zero, part.double()), lpart,
+                                 (torch.where(odd, zero, want), lse, torch.where(odd, zero, big), qk), f"entry {b}")
+    assert seen >= 5 * new
+
+
+@pytest.mark.parametrize("H,d", [(2, 64), (8, 128), (9, 128)])
+def test_infinite_values_of_the_least_probable_slots(gpu_lib, H, d):
+    """Probabilities far below 32 bits' least number are not 0: an infinity there is the output, whether the maximum
+    moves away from it within a block's share of the slots, between its warps or between blocks."""
+    T = 700
+    c = R.Cache(seqs=1, T=T, H=H, d=d, bits=16, seed=6)
+    ramp = torch.linspace(-20, 20, T, device="cuda")
+    keys, vals = c.c.k.view(-1, H, d), c.c.v.view(-1, H, d)
+    rows = c.index(0, 0, torch.arange(T))
+    keys[rows] = 0
+    keys[rows, :, 0] = ramp[:, None].to(torch.bfloat16)
+    q = torch.zeros(1, H, d, device="cuda", dtype=torch.bfloat16)
+    q[..., 0] = 10.0
+    for slot, ch, x in ((0, 3, math.inf), (5, 4, -math.inf), (T // 2, 5, math.inf), (1, 6, math.inf), (2, 6, -math.inf)):
+        vals[rows[slot], :, ch] = x
+    ctx = c.context(H, 1, softmax_scale=1.0)
+    o, l = run(c, ctx, q, [1], [T - 1])
+    want = R.attention64(q, c.read(0, 0, 0, T), c.read(1, 0, 0, T), [T], 1.0)[0]
+    odd = ~want.isfinite()
+    assert int(want.isinf().sum()) == 3 * H and int(want.isnan().sum()) == H
+    assert torch.equal(o[odd].double().nan_to_num(nan=7.0), want[odd].nan_to_num(nan=7.0))
+    assert o[~odd].isfinite().all()
+
+
+def test_infinite_value_of_a_slot_of_no_weight(gpu_lib):
+    """A score of minus infinity is a probability of exactly 0, which an infinite value makes NaN; the row's other
+    channels and a row whose score is finite are as ever."""
+    c = R.Cache(seqs=1, T=40, H=1, d=64, bits=16, seed=3)
+    keys, vals = c.c.k.view(-1, 1, 64), c.c.v.view(-1, 1, 64)
+    row = c.index(0, 0, torch.tensor([4]))
+    keys[row] = 0
+    keys[row, 0, 2] = -math.inf
+    vals[row, 0, 10] = math.inf
+    q = queries(1, 2, 64)
+    q[0, :, 2] = 1.0
+    ctx = c.context(2, 1)
+    o, l = run(c, ctx, q, [1], [30])
+    k, v = c.read(0, 0, 0, 31), c.read(1, 0, 0, 31)
+    assert o[0, :, 10].isnan().all()
+    k[4], v[4] = 0, 0
+    p = torch.einsum("hd,td->ht", q[0].double(), k[:, 0]) * 64 ** -0.5
+    p[:, 4] = -math.inf
+    want = torch.softmax(p, -1) @ v[:, 0]
+    rest = [ch for ch in range(64) if ch != 10]
+    big = torch.softmax(p, -1) @ v[:, 0].abs()
+    tol = 2.0 ** -8 * want.abs() + (2.0 ** -11 + 1e-4) * big
+    assert bool(((o[0].double() - want).abs() <= tol)[:, rest].all())
+
+
 @pytest.mark.parametrize("bits", [16, 4])
 def test_large_scores(gpu_lib, bits):
     """Scores in the hundreds of both signs, growing along the sequence: the running maximum moves at every tile."""
