@@ -334,7 +334,7 @@ __device__ void copy_q4(char* smem, uint64_t* full, uint64_t* empty, const Waite
   const AttnShape& sh = ge.sh;
   const bool side = kv.stride_token * 2 == ge.row_s && sh.groups == 1;
   const bool flat = kv.layout == EPIKV_LAYOUT_CONTIGUOUS;
-  const int rl = !side ? 1 : flat ? 1 << 24 : kv.block_size;   // slots of a run
+  const int rl = run_slots(side, flat, kv.block_size);
   const Divider block(flat ? 1 : kv.block_size), runs_of(rl);
   Ring ring(ge.stages, warp);
   int seq = 0, s0 = 0, n = 0, h0 = 0, run0 = 0, at = 0, upto = 0;
@@ -363,7 +363,7 @@ __device__ void copy_q4(char* smem, uint64_t* full, uint64_t* empty, const Waite
     const int64_t off = rows ? offset_of(kv, layer, seq, next) : -1;
     if (rows && off < 0) set_error(st.err, EPIKV_DEV_SLOT);
     int there = off >= 0 ? rows : 0;
-    const int more = max(n_now - (32 * rl - (s_now - run_now * rl)), 0);   // slots behind the lanes' runs
+    const int more = slots_behind(n_now, s_now, run_now, rl);
     for (int r = n_now - more + lane; r < n_now; r += 32) {
       const bool in = offset_of(kv, layer, seq, place_of(kv, block, layer, seq, s0 + r)) >= 0;
       there += in;

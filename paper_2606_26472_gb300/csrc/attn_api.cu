@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include "attn.cuh"
+#include "attn_plan.h"
 
 using namespace epikv;
 
@@ -45,7 +46,7 @@ bool cache_row(int H, int d, int fmt, int* heads, int* dim) {
 bool make_attn_dims(const epikv_attn_config* c, AttnDims* d) {
   if (!c) return false;
   if (c->max_seqs < 1 || c->max_seqs > kMaxSeqs) return false;
-  if (c->max_cache_tokens < 1 || c->max_cache_tokens > (1 << 24)) return false;
+  if (c->max_cache_tokens < 1 || c->max_cache_tokens > kMostSlots) return false;
   if (c->max_new_tokens < 1 || c->max_new_tokens > (1 << 20)) return false;
   if (c->num_layers < 1 || c->num_heads < 1 || c->num_heads > 1024) return false;
   int heads, dim;

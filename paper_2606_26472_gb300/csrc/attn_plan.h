@@ -67,6 +67,18 @@ EPIKV_PLAN int cta_of_tile(int x, int total) {
   return c;
 }
 
+// ---- runs of slots whose rows are one piece of memory, each of which a lane copies
+constexpr int kMostSlots = 1 << 24;   // of a sequence: a block that holds more is as good as one that holds so many
+// `side`: a token's rows stand side by side; `flat`: without blocks.
+EPIKV_PLAN int run_slots(bool side, bool flat, int block_size) {
+  return !side ? 1 : flat || block_size > kMostSlots ? kMostSlots : block_size;
+}
+// Of a tile's n slots from s0 on, which lie in run run0 and those behind it: slots behind the 32 lanes' runs.
+EPIKV_PLAN int slots_behind(int n, int s0, int run0, int run) {
+  const int rest = n - (32 * run - (s0 - run0 * run));
+  return rest > 0 ? rest : 0;
+}
+
 // ---- shared memory of a CTA: the ring of tiles, boxes to join a head's warps, barriers, the entries' first tiles
 constexpr int kAttnSmem = 225 * 1024;   // dynamic shared memory, at most (its start is moved up to a multiple of 1,024)
 constexpr int kMaxStages = 8;           // tiles of the ring

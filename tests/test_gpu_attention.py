@@ -337,6 +337,24 @@ def test_rows_that_stand_apart(gpu_lib, bits, H, T, block):
 
 
 @pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("block", [2 ** 24, 2 ** 26, 2 ** 27, 2 ** 31 - 16, 2 ** 31 - 1])
+def test_one_block_holds_the_whole_sequence(gpu_lib, bits, block):
+    """A block size far beyond the sequences: each has one block, at any size that the view's field takes."""
+    T, S, H, d = 544, 3, 4, 128
+    c = R.Cache(seqs=S, T=T, H=H, d=d, bits=bits, block=T, seed=12)
+    view = c.c.view()
+    view.block_size = block
+    ctx = c.context(16, 3)
+    new, held = [1, 3, 2], [0, 541, 64]
+    q = queries(6, 16, d)
+    seq_ids, cu, ln = R.batch(new, held)
+    o, l = torch.empty_like(q), torch.empty(6, 16, device="cuda")
+    E.epikv_attention(ctx, 0, S, seq_ids, cu, 3, ln, E.rows(q), E.rows(o), view, lse=l)
+    check(c, q, o, l, new, held)
+    assert E.epikv_attn_get_error(ctx) == (E.EPIKV_OK, 0)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
 def test_offsets_past_32_bits(gpu_lib, bits):
     """Two blocks 6 GB apart in one pool."""
     H, d, bs = 8, 128, 16
