@@ -782,7 +782,8 @@ __global__ void __launch_bounds__(threads_of(D), 1)
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        cf[nt][c] = gk * __shfl_sync(0xffffffffu, mul, (2 * t + c) * 4);
+        const float f = gk * __shfl_sync(0xffffffffu, mul, (2 * t + c) * 4);
+        cf[nt][c] = f < 0x1p-126f ? 0x1p-126f : f > 0x1.fffffep127f ? 0x1.fffffep127f : f;   // 0 x -inf and inf x 0 are NaN
       }
     }
     const int least = e.len + (sh.causal ? row0 / sh.rep + 1 : 0);   // slots that every row of the item sees

@@ -274,6 +274,23 @@ def test_head_scales(gpu_lib):
 
 
 @pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("mag", [0.0, 1e-38, 1e-30, 1.0])
+@pytest.mark.parametrize("held", [9, 40, 700])
+def test_scores_of_next_to_nothing(gpu_lib, bits, mag, held):
+    """Queries, head scales and softmax scales so small that their product is no 32-bit number: the scores are 0, and
+    the row is the mean of the values that it sees, tiles that it sees in part among them."""
+    H, d = 2, 64
+    s = torch.full((2, 1, H), 1e-8, device="cuda") if bits == 4 else None
+    c = R.Cache(seqs=1, T=704, H=H, d=d, bits=bits, kv_scale=s, seed=9, spread=1e-8 if bits == 4 else 1.0)
+    for softmax_scale in (0.0, 1e-12, 1e-30):
+        ctx = c.context(4, 3, softmax_scale=softmax_scale)
+        q = (queries(3, 4, d).float() * mag).to(torch.bfloat16)
+        o, l = run(c, ctx, q, [3], [held])
+        scale = float(torch.tensor(softmax_scale, dtype=torch.float32)) if softmax_scale else None
+        check(c, q, o, l, [3], [held], scale=scale, what=f"scale {softmax_scale}")
+
+
+@pytest.mark.parametrize("bits", [16, 4])
 def test_strided_rows_streams_and_graphs(gpu_lib, bits):
     """Queries inside a wider tensor, outputs head-major, another stream, a captured graph, the same bits each time."""
     c = R.Cache(seqs=4, T=600, H=8, d=128, bits=bits, seed=9)
