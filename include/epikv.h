@@ -64,7 +64,7 @@ typedef enum {
 typedef enum {
   EPIKV_DEV_OK = 0,
   EPIKV_DEV_BATCH = 1,      /* n_new < 0 or > max_new, or seq id out of range */
-  EPIKV_DEV_CAPACITY = 2,   /* n_cache + n_new would exceed max_cache_tokens */
+  EPIKV_DEV_CAPACITY = 2,   /* n_cache + n_new would exceed max_cache_tokens; epikv_attention: or too much work */
   EPIKV_DEV_SLOT = 3,       /* a slot or block index outside the KV view */
   EPIKV_DEV_KEPT = 4,       /* kept list not strictly increasing / out of range */
   EPIKV_DEV_BUDGET = 5,     /* budget K < 1 or > max_cache_tokens */
@@ -476,9 +476,13 @@ epikv_status epikv_append(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, con
  * or where the slot's score is -infinity).  Slots that a row does not
  * see do not reach it, whatever they hold (memory of the view up to the next
  * multiple of 16 slots may be read: a contiguous cache has max_cache_tokens
- * slots, or stride_seq / stride_token, for every sequence).  A sequence's tiles
- * of 16 slots and more are counted in 32 bits: entries that need over 2^23
- * (134 million slots) are EPIKV_DEV_CAPACITY. */
+ * slots, or stride_seq / stride_token, for every sequence).
+ * The work is counted in 32 bits, in tiles of 16 slots or more: an entry has one
+ * for every 16 slots that a run of 8 to 32 of its query rows (tokens times
+ * num_heads / num_kv_heads) sees, for each group of 8 KV heads (4 at head_dim
+ * 256).  The entry that takes a call's sum to 2^31 - 1 and those behind it are
+ * skipped (EPIKV_DEV_CAPACITY).  A prompt of 500,000 tokens with 32 query and 8
+ * KV heads of 128 has 1.95 * 10^9 tiles. */
 epikv_status epikv_attention(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* d_seq_ids,
                              const int32_t* d_cu_new, int32_t max_new, const int32_t* d_len, int32_t len_stride,
                              int32_t causal, const epikv_rows* q, const epikv_rows* out, float* d_lse,

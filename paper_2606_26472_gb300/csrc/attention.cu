@@ -162,11 +162,14 @@ struct Walk {
   int b, group, run, at, tiles;   // the item, its first tile (below 0: an earlier CTA's), its tiles
   Entry e;
 };
-// Tiles of the runs before `end` of a group of an entry, by a whole warp.
-__device__ __forceinline__ int tiles_before(const AttnShape& sh, int n, int len, int end, int lane) {
+// Tiles of the runs before `end` of a group of an entry, by a whole warp: a lane has up to 2^42, so the low 26 bits and
+// the others go by themselves.
+__device__ __forceinline__ int64_t tiles_before(const AttnShape& sh, int n, int len, int end, int lane) {
   int64_t sum = 0;
   for (int r = lane; r < end; r += 32) sum += item_tiles(sh, n, len, r);
-  return (int)__reduce_add_sync(0xffffffffu, (unsigned)(sum < kMostTiles ? sum : kMostTiles));
+  const unsigned low = __reduce_add_sync(0xffffffffu, (unsigned)sum & 0x3ffffffu);
+  const unsigned high = __reduce_add_sync(0xffffffffu, (unsigned)(sum >> 26));
+  return ((int64_t)high << 26) + low;
 }
 
 struct Walker {
@@ -590,7 +593,7 @@ __global__ void __launch_bounds__(threads_of(D), 1)
   uint64_t* empty = full + kMaxStages;
   int* gave_up = reinterpret_cast<int*>(empty + kMaxStages);
   int* pre = reinterpret_cast<int*>(smem + ge.pre_off);
-  __shared__ int s_warp[8];
+  __shared__ unsigned s_warp[8];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const AttnShape& sh = ge.sh;
 
@@ -608,7 +611,7 @@ __global__ void __launch_bounds__(threads_of(D), 1)
   pdl_trigger();
   // tiles before each entry, and the entry that the CTA's first tile is in
   const int per = (ba.n_seq + 255) >> 8;
-  int mine = 0;
+  unsigned mine = 0;
   Entry e0{};
   if (tid < 256)
     for (int i = 0; i < per; ++i) {
@@ -618,32 +621,53 @@ __global__ void __launch_bounds__(threads_of(D), 1)
       int64_t t = runs == 1 ? item_tiles(sh, e0.n, e0.len, 0) : 0;
       for (unsigned many = __ballot_sync(0xffffffffu, runs > 1); many; many &= many - 1) {   // such entries' runs by the warp
         const int k = __ffs(many) - 1;
-        const int sum = tiles_before(sh, __shfl_sync(0xffffffffu, e0.n, k), __shfl_sync(0xffffffffu, e0.len, k),
-                                     __shfl_sync(0xffffffffu, runs, k), lane);
+        const int64_t sum = tiles_before(sh, __shfl_sync(0xffffffffu, e0.n, k), __shfl_sync(0xffffffffu, e0.len, k),
+                                         __shfl_sync(0xffffffffu, runs, k), lane);
         if (lane == k) t = sum;
       }
-      t *= sh.groups;
-      if (t > kMostTiles - mine) {
-        set_error(st.err, EPIKV_DEV_CAPACITY);
-        t = 0;
-      }
-      mine += (int)t;
-      if (b < ba.n_seq) pre[b + 1] = (int)t;
+      const unsigned count = count_of(t * sh.groups);
+      mine = add_counts(mine, count);
+      if (b < ba.n_seq) pre[b + 1] = (int)count;
     }
-  int run = mine;
+  unsigned run = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int v = __shfl_up_sync(0xffffffffu, run, o);
-    if (lane >= o) run += v;
+    const unsigned v = __shfl_up_sync(0xffffffffu, run, o);
+    if (lane >= o) run = add_counts(run, v);
   }
   if (lane == 31 && warp < 8) s_warp[warp] = run;
+  unsigned before = __shfl_up_sync(0xffffffffu, run, 1), sum = 0;
+  if (lane == 0) before = 0;
   __syncthreads();
-  int total = 0, at0 = run - mine;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    if (k < warp) at0 += s_warp[k];
-    total += s_warp[k];
+    if (k < warp) before = add_counts(before, s_warp[k]);
+    sum = add_counts(sum, s_warp[k]);
   }
+  if (sum == kTooManyTiles) {   // rare: what stands behind the last entry that can be taken is skipped
+    __shared__ unsigned s_sum;
+    if (tid == 0) s_sum = 0;
+    __syncthreads();
+    if (tid < 256) {
+      unsigned end = before;
+      for (int i = 0; i < per; ++i) {
+        const int b = tid * per + i;
+        if (b >= ba.n_seq) break;
+        end = add_counts(end, (unsigned)pre[b + 1]);
+        if (end < kTooManyTiles) {
+          atomicMax(&s_sum, end);
+        } else if (pre[b + 1]) {
+          pre[b + 1] = 0;
+          set_error(st.err, EPIKV_DEV_CAPACITY);
+        }
+      }
+    }
+    __syncthreads();
+    sum = s_sum;
+    before = min(before, sum);
+  }
+  const int total = (int)sum;
+  int at0 = (int)before;
   const int lo = first_tile(blockIdx.x, total), hi = first_tile(blockIdx.x + 1, total);
   if (tid < 256) {
     for (int i = 0; i < per; ++i) {
@@ -1259,7 +1283,7 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttnState st, 
   const int group = kh / attn_group(dm.d), head = kh % attn_group(dm.d);
   int at = p0;
   if (sh.groups > 1) at += group * ((p1 - p0) / sh.groups);
-  if (run) at += tiles_before(sh, e.n, e.len, run, lane);
+  if (run) at += (int)tiles_before(sh, e.n, e.len, run, lane);
   const int tiles = item_tiles(sh, e.n, e.len, run);
   const int c0 = cta_of_tile(at, total), c1 = cta_of_tile(at + tiles - 1, total);
   if (c0 == c1) return;

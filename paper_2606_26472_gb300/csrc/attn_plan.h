@@ -50,8 +50,14 @@ EPIKV_PLAN int64_t entry_tiles(const AttnShape& s, int n, int len) {
   return t * s.groups;
 }
 
-// A batch's tiles are counted in 32 bits; a thread's entries, of which 256 threads share the batch, may have so many.
-constexpr int64_t kMostTiles = (int64_t(1) << 23) - 1;
+// A batch's tiles are counted in 32 bits.  Sums that would reach kTooManyTiles stay there, in whatever order they are
+// formed: the entry that takes the sum there and those behind it are refused.
+constexpr unsigned kTooManyTiles = 0x7fffffffu;
+EPIKV_PLAN unsigned count_of(int64_t tiles) { return tiles < (int64_t)kTooManyTiles ? (unsigned)tiles : kTooManyTiles; }
+EPIKV_PLAN unsigned add_counts(unsigned a, unsigned b) {   // neither above kTooManyTiles: no carry
+  const unsigned s = a + b;
+  return s < kTooManyTiles ? s : kTooManyTiles;
+}
 
 // floor(total * cta / kAttnCtas) without 64-bit products
 EPIKV_PLAN int first_tile(int cta, int total) {

@@ -417,6 +417,61 @@ def test_many_sequences(gpu_lib, bits):
     check(c, q, o, l, new, held)
 
 
+def long_batch(c, Hq, n_seq, max_new, **kw):
+    """A context for more entries than the cache has sequences (attention only reads it)."""
+    cfg = E.make_attn_config(max_seqs=n_seq, max_cache_tokens=c.T, max_new_tokens=max_new, num_layers=1, num_heads=Hq,
+                             num_kv_heads=c.H, head_dim=c.d, cache_format=c.fmt, **kw)
+    n = E.epikv_attn_workspace_bytes(cfg)
+    c.ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    return E.epikv_attn_init(cfg, c.ws, n)
+
+
+@pytest.mark.parametrize("new,heavy", [([33000], [0]), ([1] * 300 + [23300, 23300, 1], [300, 301])])
+def test_long_prompts(gpu_lib, new, heavy):
+    """Over 2^23 tiles in one prompt, and in two entries that one thread counts: every entry is taken."""
+    T, H, Hq, d = 33008, 8, 32, 128
+    c = R.Cache(seqs=2, T=T, H=H, d=d, bits=16, seed=13)
+    ctx = long_batch(c, Hq, len(new), max(new))
+    held = [0 if n > 1 else 50 + i for i, n in enumerate(new)]
+    seqs = [i % 2 for i in range(len(new))]
+    q = queries(sum(new), Hq, d)
+    o, l = run(c, ctx, q, new, held, seqs=seqs)
+    assert E.epikv_attn_get_error(ctx) == (E.EPIKV_OK, 0)
+    start = torch.tensor([0] + new).cumsum(0).tolist()
+    for b in set(heavy) | {0, len(new) - 1}:
+        for i in {0, new[b] // 3, max(new[b] - 3, 0)}:             # up to three tokens of each
+            m = min(3, new[b] - i)
+            t = start[b] + i
+            top = held[b] + i + m
+            k, v = c.read(0, 0, seqs[b], top), c.read(1, 0, seqs[b], top)
+            ref = R.attention64(q[t:t + m], k, v, [held[b] + i + j + 1 for j in range(m)], d ** -0.5)
+            R.assert_attention_close(o[t:t + m], l[t:t + m], ref, f"entry {b} from token {i}")
+
+
+def test_more_work_than_is_counted(gpu_lib):
+    """An entry of over 2^31 tiles is skipped with those behind it and reported; those before it are done."""
+    T, H, Hq, d = 2 ** 22, 8, 32, 128
+    c = R.Cache(seqs=1, T=64, H=H, d=d, bits=16, seed=14)
+    small = c.c.view()
+    table = torch.zeros(3, T // 16, dtype=torch.int32, device="cuda")    # many slots, one block
+    table[:, :4] = c.c.block_table
+    view = E.kv_view(c.c.k, c.c.v, layout=E.EPIKV_LAYOUT_PAGED, stride_layer=0, stride_block=small.stride_block,
+                     stride_token=small.stride_token, block_table=table, max_blocks_per_seq=T // 16, block_size=16,
+                     num_blocks=c.c.num_blocks)
+    new, held = [2, 2 ** 16, 1], [40, T - 2 ** 16, 5]
+    c.T = T
+    ctx = long_batch(c, Hq, 3, max(new))
+    n = sum(new)
+    q = torch.zeros(n, Hq, d, dtype=torch.bfloat16, device="cuda")
+    q[:2] = queries(2, Hq, d)
+    out = torch.full_like(q, 7.0)
+    seq_ids, cu, ln = R.batch(new, held)
+    E.epikv_attention(ctx, 0, 3, seq_ids, cu, max(new), ln, E.rows(q), E.rows(out), view)
+    assert E.epikv_attn_get_error(ctx) == (E.EPIKV_EDEVICE, E.EPIKV_DEV_CAPACITY)
+    check(c, q[:2], out[:2], None, [2], [40])
+    assert bool((out[2:] == 7.0).all())
+
+
 def test_reported_and_skipped(gpu_lib):
     c = R.Cache(seqs=2, T=64, H=2, d=64, bits=4)
     ctx = c.context(2, 4)
