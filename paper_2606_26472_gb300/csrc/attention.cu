@@ -1432,27 +1432,29 @@ cudaError_t run_rows(const AttnState& st, const AttnDims& dm, const Geometry& ge
   return run<D, FMT, 1, kSub>(st, dm, ge, layer, ba, q, out, lse, kv, stream);
 }
 
+// *runs becomes false where the compiler gave the kernel other registers than its warps' exchange of them counts on:
+// launched, it would wait for registers that nobody gives.
 template <int D, int FMT, int NT, int SUB>
-cudaError_t prepare_one() {
+cudaError_t prepare_one(bool* runs) {
   auto kernel = attention_kernel<D, FMT, NT, SUB>;
   cudaFuncAttributes at;
   cudaError_t e = cudaFuncGetAttributes(&at, kernel);
   if (e != cudaSuccess) return e;
-  if (threads_of(D) == 384 && at.numRegs != 168) return cudaErrorInvalidConfiguration;   // what the split counts on
+  if (threads_of(D) == 384 && at.numRegs != 168) *runs = false;
   return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem + 1024);
 }
 
 template <int D, int FMT>
-cudaError_t prepare_rows() {
+cudaError_t prepare_rows(bool* runs) {
   constexpr int kSub = FMT == EPIKV_CACHE_BF16 ? 1 : 2;
-  cudaError_t e = prepare_one<D, FMT, 1, kSub>();
+  cudaError_t e = prepare_one<D, FMT, 1, kSub>(runs);
   if constexpr (D <= 128) {
-    if (e == cudaSuccess) e = prepare_one<D, FMT, 2, kSub>();
+    if (e == cudaSuccess) e = prepare_one<D, FMT, 2, kSub>(runs);
     if constexpr (kSub == 2)
-      if (e == cudaSuccess) e = prepare_one<D, FMT, 1, 4>();
+      if (e == cudaSuccess) e = prepare_one<D, FMT, 1, 4>(runs);
   }
   if constexpr (D <= 64)
-    if (e == cudaSuccess) e = prepare_one<D, FMT, 4, kSub>();
+    if (e == cudaSuccess) e = prepare_one<D, FMT, 4, kSub>(runs);
   return e;
 }
 
@@ -1463,11 +1465,12 @@ size_t attention_part_floats(const AttnDims& dm) {
   return (size_t)2 * kAttnCtas * ge.slot_floats;
 }
 
-cudaError_t attention_prepare(const AttnDims& dm) {
+cudaError_t attention_prepare(const AttnDims& dm, bool* runs) {
   const bool q4 = dm.fmt == EPIKV_CACHE_E2M1;
-  if (dm.d == 64) return q4 ? prepare_rows<64, EPIKV_CACHE_E2M1>() : prepare_rows<64, EPIKV_CACHE_BF16>();
-  if (dm.d == 128) return q4 ? prepare_rows<128, EPIKV_CACHE_E2M1>() : prepare_rows<128, EPIKV_CACHE_BF16>();
-  return q4 ? prepare_rows<256, EPIKV_CACHE_E2M1>() : prepare_rows<256, EPIKV_CACHE_BF16>();
+  *runs = true;
+  if (dm.d == 64) return q4 ? prepare_rows<64, EPIKV_CACHE_E2M1>(runs) : prepare_rows<64, EPIKV_CACHE_BF16>(runs);
+  if (dm.d == 128) return q4 ? prepare_rows<128, EPIKV_CACHE_E2M1>(runs) : prepare_rows<128, EPIKV_CACHE_BF16>(runs);
+  return q4 ? prepare_rows<256, EPIKV_CACHE_E2M1>(runs) : prepare_rows<256, EPIKV_CACHE_BF16>(runs);
 }
 
 cudaError_t launch_attention(const AttnState& st, const AttnDims& dm, int layer, const Batch& ba, bool causal,

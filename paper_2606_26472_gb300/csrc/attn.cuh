@@ -119,6 +119,6 @@ cudaError_t launch_cache_read(const AttnState& st, const AttnDims& dm, int layer
 cudaError_t launch_attention(const AttnState& st, const AttnDims& dm, int layer, const Batch& ba, bool causal,
                              const Rows& q, const Rows& out, float* lse, const KvDev& kv, cudaStream_t stream);
 size_t attention_part_floats(const AttnDims& dm);
-cudaError_t attention_prepare(const AttnDims& dm);
+cudaError_t attention_prepare(const AttnDims& dm, bool* runs);
 
 }  // namespace epikv

@@ -13,6 +13,7 @@ struct epikv_attn_ctx {
   AttnDims dm;
   AttnState st;
   cudaStream_t last_stream;
+  bool attention_runs;   // false: this build's attention kernels cannot be launched; the other operators can
 };
 
 namespace {
@@ -181,7 +182,7 @@ epikv_status epikv_attn_init(epikv_attn_ctx** out, const epikv_attn_config* cfg,
   carve(dm, &ctx->st, (char*)d_workspace);
   ctx->st.kv_scale = cfg->kv_scale;
   ctx->last_stream = stream;
-  cudaError_t e = attention_prepare(dm);
+  cudaError_t e = attention_prepare(dm, &ctx->attention_runs);
   if (e == cudaSuccess) e = cudaMemsetAsync(ctx->st.err, 0, 4, stream);
   if (e != cudaSuccess) {
     free(ctx);
@@ -258,6 +259,7 @@ epikv_status epikv_attention(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, 
   if (!valid_rows(q, &qr) || !valid_rows(out, &yr) || q->type != EPIKV_TYPE_BF16 || out->type != EPIKV_TYPE_BF16)
     return EPIKV_EINVAL;
   if (((uintptr_t)d_lse & 3u) || !valid_cache(ctx->dm, layer, kv, &kd)) return EPIKV_EINVAL;
+  if (!ctx->attention_runs) return EPIKV_ECUDA;
   ctx->last_stream = stream;
   return cuda_status(launch_attention(ctx->st, ctx->dm, layer, ba, causal, qr, yr, d_lse, kd, stream));
 }
