@@ -59,6 +59,7 @@ class epikv_rope_view(C.Structure):
 
 class epikv_rows(C.Structure):
     _fields_ = [("ptr", C.c_void_p), ("stride_token", C.c_int64), ("stride_head", C.c_int64), ("type", C.c_int32)]
+    shape = None    # of the tensor that rows() described: (tokens, heads, channels)
 
 
 class epikv_attn_config(C.Structure):
@@ -217,11 +218,26 @@ _TYPES = {"torch.bfloat16": EPIKV_TYPE_BF16, "torch.float16": EPIKV_TYPE_F16, "t
 
 def rows(t):
     """The heads of tokens that a tensor [tokens, heads, channels] holds (channels contiguous; the tensor may be a
-    slice of a wider one).  It describes memory: the tensor is the caller's to keep."""
+    slice of a wider one).  It describes memory: the tensor is the caller's to keep.  The calls refuse a tensor that
+    has fewer heads or channels than they take of it, or, where the host knows their number, fewer tokens."""
     if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] != 1) or str(t.dtype) not in _TYPES:
         raise ValueError(f"rows are bf16, f16 or f32 [tokens, heads, channels], channels contiguous: got {t.dtype} "
                          f"{tuple(t.shape)}, strides {t.stride()}")
-    return epikv_rows(t.data_ptr(), t.stride(0), t.stride(1), _TYPES[str(t.dtype)])
+    r = epikv_rows(t.data_ptr(), t.stride(0), t.stride(1), _TYPES[str(t.dtype)])
+    r.shape = tuple(t.shape)
+    return r
+
+
+def _heads(ctx):
+    """(query heads, KV heads, channels) of a context made by epikv_attn_init; of a bare handle nothing is known."""
+    return getattr(ctx, "heads", (0, 0, 0))
+
+
+def _check_rows(what, r, tokens, heads, dim):
+    if r is not None and r.shape is not None:
+        n, h, d = r.shape
+        if n < tokens or h < heads or d < dim:
+            raise ValueError(f"{what} takes {tokens} tokens or more of {heads} heads of {dim} channels: got rows of {r.shape}")
 
 
 # ---------------------------------------------------------------- same names
@@ -371,6 +387,7 @@ def epikv_attn_init(cfg, workspace, workspace_bytes, stream=None):
     ctx = C.c_void_p()
     _check(load().epikv_attn_init(C.byref(ctx), C.byref(cfg), _ptr(workspace), workspace_bytes, _stream(stream)),
            "epikv_attn_init")
+    ctx.heads = (cfg.num_heads, cfg.num_kv_heads, cfg.head_dim)     # what the calls take of their rows
     return ctx
 
 
@@ -382,33 +399,42 @@ def epikv_rope_table(cfg, n_pos, device="cuda", stream=None):
     return table
 
 
-def _ref(x):
-    return C.byref(x) if x is not None else None
-
-
 def epikv_rope(ctx, n_tokens, n_heads, x, out, pos, rope, *, inverse=False, stream=None):
-    _check(load().epikv_rope(ctx, n_tokens, n_heads, _ref(x), _ref(out), _ptr(pos), _ref(rope), 1 if inverse else 0,
+    _, _, dim = _heads(ctx)
+    _check_rows("epikv_rope", x, n_tokens, n_heads, dim)
+    _check_rows("epikv_rope", out, n_tokens, n_heads, dim)
+    _check(load().epikv_rope(ctx, n_tokens, n_heads, x, out, _ptr(pos), rope, 1 if inverse else 0,
                              _stream(stream)), "epikv_rope")
 
 
 def epikv_append(ctx, layer, n_seq, seq_ids, cu_new, max_new, length, pos, q, q_out, k, v, rope, kv, *, len_stride=1,
                  stream=None):
     """q, q_out, k, v: rows(...) (q and q_out may be None); rope: rope_view(...) or None."""
+    hq, h, dim = _heads(ctx)
+    _check_rows("epikv_append", q, 0, hq, dim)
+    _check_rows("epikv_append", q_out, 0, hq, dim)
+    _check_rows("epikv_append", k, 0, h, dim)
+    _check_rows("epikv_append", v, 0, h, dim)
     _check(load().epikv_append(ctx, layer, n_seq, _ptr(seq_ids), _ptr(cu_new), max_new, _ptr(length), len_stride,
-                               _ptr(pos), _ref(q), _ref(q_out), _ref(k), _ref(v), _ref(rope), _ref(kv),
-                               _stream(stream)), "epikv_append")
+                               _ptr(pos), q, q_out, k, v, rope, kv, _stream(stream)), "epikv_append")
 
 
 def epikv_attention(ctx, layer, n_seq, seq_ids, cu_new, max_new, length, q, out, kv, *, lse=None, causal=True,
                     len_stride=1, stream=None):
+    hq, _, dim = _heads(ctx)
+    _check_rows("epikv_attention", q, 0, hq, dim)
+    _check_rows("epikv_attention", out, 0, hq, dim)
     _check(load().epikv_attention(ctx, layer, n_seq, _ptr(seq_ids), _ptr(cu_new), max_new, _ptr(length), len_stride,
-                                  1 if causal else 0, _ref(q), _ref(out), _ptr(lse), _ref(kv), _stream(stream)),
+                                  1 if causal else 0, q, out, _ptr(lse), kv, _stream(stream)),
            "epikv_attention")
 
 
 def epikv_cache_read(ctx, layer, n_rows, seqs, slots, k, v, kv, stream=None):
-    _check(load().epikv_cache_read(ctx, layer, n_rows, _ptr(seqs), _ptr(slots), _ref(k), _ref(v), _ref(kv),
-                                   _stream(stream)), "epikv_cache_read")
+    _, h, dim = _heads(ctx)
+    _check_rows("epikv_cache_read", k, n_rows, h, dim)
+    _check_rows("epikv_cache_read", v, n_rows, h, dim)
+    _check(load().epikv_cache_read(ctx, layer, n_rows, _ptr(seqs), _ptr(slots), k, v, kv, _stream(stream)),
+           "epikv_cache_read")
 
 
 def epikv_attn_get_error(ctx):
