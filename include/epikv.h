@@ -475,8 +475,9 @@ epikv_status epikv_append(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, con
  * that channel, however small its probability (NaN beside one of the other sign,
  * or where the slot's score is -infinity).  Slots that a row does not
  * see do not reach it, whatever they hold (memory of the view up to the next
- * multiple of 16 slots may be read: a contiguous cache has max_cache_tokens
- * slots, or stride_seq / stride_token, for every sequence).
+ * multiple of 16 slots may be read: of a block, or of the max_cache_tokens slots
+ * of a contiguous sequence; where stride_seq / stride_token is between 1 and
+ * max_cache_tokens - 1, only slots that are seen, by a slower way).
  * The work is counted in 32 bits, in tiles of 16 slots or more: an entry has one
  * for every 16 slots that a run of 8 to 32 of its query rows (tokens times
  * num_heads / num_kv_heads) sees, for each group of 8 KV heads (4 at head_dim

@@ -1392,9 +1392,11 @@ CacheMaps cache_maps(const AttnDims& dm, const Geometry& ge, int layer, const Kv
   const bool flat = kv.layout == EPIKV_LAYOUT_CONTIGUOUS;
   if (!flat && kv.block_size % 16) return maps;
   const int64_t outer = flat ? kv.stride_seq : kv.stride_block;   // elements
-  // slots of a sequence: no more than lie before the next one, whatever the configuration allows
-  const int64_t room = kv.stride_seq >= kv.stride_token ? kv.stride_seq / kv.stride_token : dm.T;
-  const cuuint64_t dims[4] = {64, (cuuint64_t)(!flat ? kv.block_size : room < dm.T ? room : dm.T), (cuuint64_t)(flat ? dm.S : kv.num_blocks), (cuuint64_t)(dm.H * dm.d / 64)};
+  // Fewer slots before the next sequence than the configuration allows: a tensor that ends there would lack the slots of
+  // a single sequence (whose stride says nothing) or of sequences that overlap, one that does not may end behind the
+  // memory.  Copied by lanes, every slot is its row and nothing else is read.
+  if (flat && kv.stride_seq >= kv.stride_token && kv.stride_seq / kv.stride_token < dm.T) return maps;
+  const cuuint64_t dims[4] = {64, (cuuint64_t)(flat ? dm.T : kv.block_size), (cuuint64_t)(flat ? dm.S : kv.num_blocks), (cuuint64_t)(dm.H * dm.d / 64)};
   const cuuint64_t strides[3] = {(cuuint64_t)kv.stride_token * 2, (cuuint64_t)outer * 2, 128};
   for (int i = 0; i < 2; ++i)
     if (strides[i] == 0 || strides[i] >= (cuuint64_t(1) << 40)) return maps;

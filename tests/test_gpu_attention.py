@@ -354,6 +354,32 @@ def test_rows_that_stand_apart(gpu_lib, bits, H, T, block):
 
 
 @pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("S,stride", [(1, 1), (1, 0), (1, 100), (3, 100), (2, 144), (3, 1)])
+def test_contiguous_sequences_closer_than_they_are_long(gpu_lib, bits, S, stride):
+    """stride_seq of 0, one row or some: a single sequence whose stride says nothing, sequences that overlap.  Slot s of
+    sequence b is row b * stride + s."""
+    T, H, d = 304, 4, 64
+    c = R.Cache(seqs=1, T=T + S * stride, H=H, d=d, bits=bits, block=0, seed=15)
+    view = c.c.view()
+    view.stride_seq = stride * c.units
+    cfg = E.make_attn_config(max_seqs=S, max_cache_tokens=T, max_new_tokens=2, num_layers=1, num_heads=8, num_kv_heads=H,
+                             head_dim=d, cache_format=c.fmt)
+    ws = torch.empty(E.epikv_attn_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+    ctx = E.epikv_attn_init(cfg, ws, ws.numel())
+    q = queries(2 * S, 8, d)
+    seq_ids, cu, ln = R.batch([2] * S, [T - 2 - 7 * b for b in range(S)])
+    o, l = torch.empty_like(q), torch.empty(2 * S, 8, device="cuda")
+    E.epikv_attention(ctx, 0, S, seq_ids, cu, 2, ln, E.rows(q), E.rows(o), view, lse=l)
+    k, v = c.read(0, 0, 0, T + S * stride), c.read(1, 0, 0, T + S * stride)
+    for b in range(S):
+        n = T - 2 - 7 * b
+        ref = R.attention64(q[2 * b:2 * b + 2], k[b * stride:b * stride + n + 2], v[b * stride:b * stride + n + 2],
+                            [n + 1, n + 2], d ** -0.5)
+        R.assert_attention_close(o[2 * b:2 * b + 2], l[2 * b:2 * b + 2], ref, f"sequence {b}")
+    assert E.epikv_attn_get_error(ctx) == (E.EPIKV_OK, 0)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
 @pytest.mark.parametrize("block", [2 ** 24, 2 ** 26, 2 ** 27, 2 ** 31 - 16, 2 ** 31 - 1])
 def test_one_block_holds_the_whole_sequence(gpu_lib, bits, block):
     """A block size far beyond the sequences: each has one block, at any size that the view's field takes."""
