@@ -29,7 +29,7 @@
 // if the queries follow it), a conversion turns two codes into a half pair,
 // and the product with the E4M3 scale is exact in half precision (2 + 4
 // significant bits).  Queries enter as halves scaled by a power of two per
-// row, probabilities as halves times 2^7 (11 bits down to 2^-21).  For
+// row (exact but for channels below 2^-31 of the row's largest), probabilities as halves times 2^7 (11 bits down to 2^-21).  For
 // a bf16 cache the probabilities go in as two bf16 terms (16 bits), for which
 // the tensor instructions have time: one term alone would add an error of the
 // output's own rounding.
@@ -781,8 +781,9 @@ __global__ void __launch_bounds__(threads_of(D), 1)
           qf[nt][j][1] = there ? *reinterpret_cast<const uint32_t*>(qp + 16 * j + 8 + 2 * t) : 0u;
         }
       } else {
-        // a lane's channels are t * D/4 .. : as halves, scaled by a power of two that brings the row's largest
-        // below 2 (a row with an infinity or a NaN is left as it is)
+        // a lane's channels are t * D/4 .. : as halves, scaled by a power of two that brings the row's largest to
+        // 2^14 .. 2^15: bf16's 8 bits then stand whole in channels down to 2^-31 of it (of rows below 2^-112, which get
+        // 2^126, down to 2^-17 or more).  256 products with keys of up to 2,688 stay below 2^35.
         uint2 raw[KS];
         float top = 0.f;
 #pragma unroll
@@ -793,11 +794,10 @@ __global__ void __launch_bounds__(threads_of(D), 1)
         }
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const int ex = (int)(__float_as_uint(top) >> 23);      // biased exponent
-        // 2^(127 - ex) and its inverse, both normal numbers
-        const int sh2 = ex == 255 ? 127 : min(max(ex, 1), 253);
-        const float down = __uint_as_float((uint32_t)(254 - sh2) << 23);
-        mul = __uint_as_float((uint32_t)sh2 << 23);
+        // 2^(141 - ex) of the biased exponent ex and its inverse, both normal numbers (ex = 255: the finite ones' largest)
+        const int ex = min(max((int)(__float_as_uint(top) >> 23), 15), 254);
+        const float down = __uint_as_float((uint32_t)(268 - ex) << 23);
+        mul = __uint_as_float((uint32_t)(ex - 14) << 23);
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
           qf[nt][j][0] = half2_of(bf16_lo(raw[j].x) * down, bf16_hi(raw[j].x) * down);

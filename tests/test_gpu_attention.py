@@ -264,6 +264,27 @@ def test_query_magnitudes(gpu_lib, bits):
         check(c, q, o, l, [1], [99], scale=None if mag <= 1 else float(torch.tensor(0.05 / mag)), what=f"|q| {mag}")
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("down", [12, 19, 27])
+def test_queries_of_unlike_channels(gpu_lib, d, down):
+    """A row's largest channel meets keys of 0, channels 2^down smaller make the scores: each keeps its 8 bits."""
+    s = torch.full((2, 1, 2), 2.0 ** (down - 13), device="cuda")
+    c = R.Cache(seqs=1, T=300, H=2, d=d, bits=4, kv_scale=s, seed=16, spread=1.0)
+    g = torch.Generator(device="cuda").manual_seed(17)
+    k = torch.randn(c.raw(0).shape[0], 2, d, generator=g, device="cuda") * 500.0 * float(s[0, 0, 0])
+    k[..., :16] = 0
+    c.put(c.c.k, k.to(torch.bfloat16), 0)
+    for first in (1.0, 1.7, 3e-20, 1e30):
+        q = queries(2, 8, d).float() * 2.0 ** -down
+        q[..., :16] = 0
+        q[..., 3] = 1.0
+        q = (q * first).to(torch.bfloat16)
+        scale = float(torch.tensor(8.0 / d ** 0.5 / first, dtype=torch.float32))
+        ctx = c.context(8, 2, softmax_scale=scale)
+        o, l = run(c, ctx, q, [2], [290])
+        check(c, q, o, l, [2], [290], scale=scale, what=f"first {first}")
+
+
 def test_head_scales(gpu_lib):
     s = torch.rand(2, 2, 4, device="cuda") * 3 + 0.01
     c = R.Cache(seqs=2, T=200, H=4, d=64, bits=4, layers=2, kv_scale=s, seed=8)
