@@ -68,8 +68,10 @@ class KVCache:
 
     def view(self, block_table=None):
         bt = self.block_table if block_table is None else block_table
-        return E.kv_view(self.k, self.v, layout=self.layout, block_table=bt, max_blocks_per_seq=self.max_blocks,
-                         block_size=self.block_size, num_blocks=self.num_blocks, **self.strides)
+        kv = E.kv_view(self.k, self.v, layout=self.layout, block_table=bt, max_blocks_per_seq=self.max_blocks,
+                       block_size=self.block_size, num_blocks=self.num_blocks, **self.strides)
+        kv.cache_format = self.cache_format
+        return kv
 
     def synth_kwargs(self, block_table=None):
         assert not self.layer_tables, "the generator writes one slot for every layer; use write_layer_rows"

@@ -41,6 +41,7 @@ class epikv_kv_view(C.Structure):
                 ("stride_seq", C.c_int64), ("stride_block", C.c_int64), ("stride_token", C.c_int64),
                 ("block_table", C.c_void_p), ("max_blocks_per_seq", C.c_int32), ("block_size", C.c_int32),
                 ("num_blocks", C.c_int32), ("stride_table_layer", C.c_int64)]
+    cache_format = None    # what the rows hold, where it is known (a KVCache's view): EPIKV_CACHE_*
 
 
 class epikv_stats(C.Structure):
@@ -240,6 +241,20 @@ def _check_rows(what, r, tokens, heads, dim):
             raise ValueError(f"{what} takes {tokens} tokens or more of {heads} heads of {dim} channels: got rows of {r.shape}")
 
 
+def _check_format(what, ctx, kv):
+    known = getattr(ctx, "cache_format", None)
+    if kv is not None and kv.cache_format is not None and known is not None and kv.cache_format != known:
+        raise ValueError(f"{what}: the context's cache_format is {known}, the cache's {kv.cache_format}")
+
+
+_KV_KINDS = EPIKV_SCORE_LAGKV | EPIKV_SCORE_KVKEY | EPIKV_SCORE_KVVAL | EPIKV_SCORE_LAGKEY
+
+
+def _check_scored(what, kinds, kv):
+    if kv is not None and kv.cache_format not in (None, EPIKV_CACHE_BF16) and kinds & _KV_KINDS:
+        raise ValueError(f"{what}: the K/V score kinds read bf16 rows (score_kinds {kinds}, cache_format {kv.cache_format})")
+
+
 # ---------------------------------------------------------------- same names
 def epikv_workspace_bytes(cfg):
     return load().epikv_workspace_bytes(C.byref(cfg))
@@ -249,6 +264,7 @@ def epikv_init(cfg, workspace, workspace_bytes, stream=None):
     ctx = C.c_void_p()
     _check(load().epikv_init(C.byref(ctx), C.byref(cfg), _ptr(workspace), workspace_bytes, _stream(stream)),
            "epikv_init")
+    ctx.score_kinds = cfg.score_kinds
     return ctx
 
 
@@ -257,6 +273,7 @@ def epikv_seq_reset(ctx, seq, prefill_len=0, policy=EPIKV_SCORE_BANDZ, stream=No
 
 
 def epikv_score_update(ctx, n_seq, seq_ids, cu_new, max_new, hidden, kv, stream=None):
+    _check_scored("epikv_score_update", getattr(ctx, "score_kinds", 0), kv)
     _check(load().epikv_score_update(ctx, n_seq, _ptr(seq_ids), _ptr(cu_new), max_new,
                                      C.byref(hidden) if hidden is not None else None,
                                      C.byref(kv) if kv is not None else None, _stream(stream)),
@@ -274,6 +291,7 @@ def epikv_compact(ctx, n_seq, seq_ids, kept, kept_stride, kv, stream=None):
 
 
 def epikv_step(ctx, n_seq, seq_ids, cu_new, max_new, budget, trigger, hidden, kv, n_cache_out=None, stream=None):
+    _check_scored("epikv_step", getattr(ctx, "score_kinds", 0), kv)
     _check(load().epikv_step(ctx, n_seq, _ptr(seq_ids), _ptr(cu_new), max_new, _ptr(budget), _ptr(trigger),
                              C.byref(hidden) if hidden is not None else None, C.byref(kv), _ptr(n_cache_out),
                              _stream(stream)),
@@ -367,6 +385,7 @@ def epikv_get_error(ctx):
 def epikv_lagkv_score_noalloc(kv, seq, n, num_layers, num_kv_heads, head_dim, lag, lag_eps, window, scores,
                               stream=None):
     """Lag-KV scores of positions 0..n-1 of `seq` without any workspace (see epikv.h)."""
+    _check_scored("epikv_lagkv_score_noalloc", EPIKV_SCORE_LAGKV, kv)
     _check(load().epikv_lagkv_score_noalloc(C.byref(kv), seq, n, num_layers, num_kv_heads, head_dim, lag, lag_eps,
                                             window, _ptr(scores), _stream(stream)), "epikv_lagkv_score_noalloc")
 
@@ -388,6 +407,7 @@ def epikv_attn_init(cfg, workspace, workspace_bytes, stream=None):
     _check(load().epikv_attn_init(C.byref(ctx), C.byref(cfg), _ptr(workspace), workspace_bytes, _stream(stream)),
            "epikv_attn_init")
     ctx.heads = (cfg.num_heads, cfg.num_kv_heads, cfg.head_dim)     # what the calls take of their rows
+    ctx.cache_format = cfg.cache_format
     return ctx
 
 
@@ -415,6 +435,7 @@ def epikv_append(ctx, layer, n_seq, seq_ids, cu_new, max_new, length, pos, q, q_
     _check_rows("epikv_append", q_out, 0, hq, dim)
     _check_rows("epikv_append", k, 0, h, dim)
     _check_rows("epikv_append", v, 0, h, dim)
+    _check_format("epikv_append", ctx, kv)
     _check(load().epikv_append(ctx, layer, n_seq, _ptr(seq_ids), _ptr(cu_new), max_new, _ptr(length), len_stride,
                                _ptr(pos), q, q_out, k, v, rope, kv, _stream(stream)), "epikv_append")
 
@@ -424,6 +445,7 @@ def epikv_attention(ctx, layer, n_seq, seq_ids, cu_new, max_new, length, q, out,
     hq, _, dim = _heads(ctx)
     _check_rows("epikv_attention", q, 0, hq, dim)
     _check_rows("epikv_attention", out, 0, hq, dim)
+    _check_format("epikv_attention", ctx, kv)
     _check(load().epikv_attention(ctx, layer, n_seq, _ptr(seq_ids), _ptr(cu_new), max_new, _ptr(length), len_stride,
                                   1 if causal else 0, q, out, _ptr(lse), kv, _stream(stream)),
            "epikv_attention")
@@ -433,6 +455,7 @@ def epikv_cache_read(ctx, layer, n_rows, seqs, slots, k, v, kv, stream=None):
     _, h, dim = _heads(ctx)
     _check_rows("epikv_cache_read", k, n_rows, h, dim)
     _check_rows("epikv_cache_read", v, n_rows, h, dim)
+    _check_format("epikv_cache_read", ctx, kv)
     _check(load().epikv_cache_read(ctx, layer, n_rows, _ptr(seqs), _ptr(slots), k, v, kv, _stream(stream)),
            "epikv_cache_read")
 
