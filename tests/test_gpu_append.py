@@ -130,6 +130,36 @@ def test_every_bf16_against_every_scale(gpu_lib):
         assert torch.equal(c.raw(w), want[w])
 
 
+def test_every_significand_at_every_scale(gpu_lib):
+    """For each of E4M3's positive scales, subnormal ones too, every bf16 value from an eighth of it to its group's
+    maximum, of both signs in turn: 15 of them beside the maximum in each group of 16."""
+    groups = []
+    every = torch.arange(1, 0x7F, dtype=torch.uint8).view(torch.float8_e4m3fn).float()
+    positive = torch.arange(0x0001, 0x7F80, dtype=torch.int32).to(torch.int16).view(torch.bfloat16).float()
+    scales = (positive / 6.0).clamp(max=448.0).to(torch.float8_e4m3fn).float()     # what a maximum gives
+    for s in every.tolist():
+        tops = positive[scales == s]
+        assert tops.numel(), s
+        for top in {tops[0].item(), tops[-1].item(), tops[tops.numel() // 2].item()} if s < 448 else {2688.0, 3000.0, 1e5}:
+            top = torch.tensor(top).to(torch.bfloat16).item()
+            x = positive[(positive >= s / 8) & (positive <= top)]
+            x = torch.cat([x, x.new_zeros(-x.numel() % 15)]).view(-1, 15)
+            x = x * (1.0 - 2.0 * (torch.arange(x.numel()) % 2)).view(-1, 15)
+            groups.append(torch.cat([x.new_full((x.shape[0], 1), top), x], 1))
+    x = torch.cat(groups)
+    x = torch.cat([x, x.new_zeros(-x.shape[0] % 4, 16)]).view(-1, 1, 64).to(torch.bfloat16).cuda()
+    n = x.shape[0]
+    c = R.Cache(seqs=1, T=n, H=1, d=64, bits=4, block=0)
+    ctx = c.context(1, n)
+    qkv = torch.cat([x, x, -x.flip(0)], 1).contiguous()
+    _, want = expected(c, qkv, 1, [n], [0], None, None, 0, HALF)
+    append(c, ctx, qkv, 1, [n], [0], None, None, q=False)
+    for w in range(2):
+        assert torch.equal(c.raw(w), want[w])
+    got = c.raw(0)[c.index(0, 0, torch.arange(n))][:, 32:36].flatten()
+    assert set(range(1, 0x7F)) <= set(got.tolist())
+
+
 def test_head_scales(gpu_lib):
     s = torch.rand(2, 3, 2, device="cuda") * 30 + 0.01
     c = R.Cache(seqs=2, T=40, H=2, d=64, bits=4, layers=3, kv_scale=s, spread=20.0)

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from paper_2606_26472_gb300 import epikv as E
+from paper_2606_26472_gb300.cache import KVCache
 
 from . import cache_ops as R
 
@@ -344,6 +345,78 @@ def test_strided_rows_streams_and_graphs(gpu_lib, bits):
     g.replay()
     torch.cuda.synchronize()
     check(c, q.contiguous(), b.transpose(0, 1), None, new, [40, 300, 598, 5])
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("H,Hq,block", [(8, 32, 16), (2, 8, 16), (8, 8, 7), (9, 9, 16), (3, 6, 48)])
+@pytest.mark.parametrize("new", [1, 5])
+def test_lengths_and_tables_of_a_layer(gpu_lib, bits, H, Hq, block, new):
+    """As after per-layer budgets: lengths [entry][layer] read at one layer with their stride, every layer with blocks of
+    its own; entries of no slots, of some, and of enough to be shared by many blocks of the grid and joined."""
+    L, S, T, d = 3, 4, 3008, 64
+    held = [[0, 5, 40], [2900, 17, 3000], [3000, 2999, 64], [31, 300, 1]]
+    mb = -(-T // block)
+    table = torch.randperm(L * S * mb, generator=torch.Generator().manual_seed(H)).view(L, S, mb).int()
+    fmt = E.EPIKV_CACHE_E2M1 if bits == 4 else E.EPIKV_CACHE_BF16
+    cache = KVCache(E.EPIKV_LAYOUT_PAGED, L, H, d, max_seqs=S, max_tokens=T, block_size=block, block_table=table.numpy(),
+                    layer_tables=True, cache_format=fmt)
+    units, g = cache.H * cache.d, torch.Generator(device="cuda").manual_seed(d)
+    pools = []
+    for pool in (cache.k, cache.v):
+        x = torch.randn(L * S * mb * block, H, d, generator=g, device="cuda").to(torch.bfloat16)
+        raw = pool.view(torch.uint8).view(-1, 2 * units)
+        raw.copy_(R.pack(x, units) if bits == 4 else x.view(-1, units).view(torch.uint8))
+        pools.append(raw)
+    cfg = E.make_attn_config(max_seqs=S, max_cache_tokens=T, max_new_tokens=8, num_layers=L, num_heads=Hq, num_kv_heads=H,
+                             head_dim=d, cache_format=fmt)
+    ws = torch.empty(E.epikv_attn_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+    ctx = E.epikv_attn_init(cfg, ws, ws.numel())
+    seqs = [2, 0, 3, 1]
+    seq_ids, cu, _ = R.batch([new] * S, [0] * S, seqs)
+    lens = torch.tensor(held, dtype=torch.int32, device="cuda")
+    q = queries(S * new, Hq, d)
+    for layer in range(L):
+        o, l = torch.full_like(q, float("nan")), torch.empty(S * new, Hq, device="cuda")
+        E.epikv_attention(ctx, layer, S, seq_ids, cu, new, lens[:, layer:].data_ptr(), E.rows(q), E.rows(o), cache.view(),
+                          lse=l, len_stride=L)
+        for b in range(S):
+            n = held[b][layer] + new
+            slots = torch.arange(n)
+            rows = (table[layer, seqs[b]].long()[slots // block] * block + slots % block).cuda()
+            k, v = (p[rows] for p in pools)
+            if bits == 4:
+                k, v = R.values(k, H, d), R.values(v, H, d)
+            else:
+                k, v = (x.contiguous().view(torch.bfloat16).view(n, H, d).double() for x in (k, v))
+            part = slice(b * new, (b + 1) * new)
+            ref = R.attention64(q[part], k, v, [held[b][layer] + i + 1 for i in range(new)], d ** -0.5)
+            R.assert_attention_close(o[part], l[part], ref, f"layer {layer} entry {b}")
+    assert E.epikv_attn_get_error(ctx) == (E.EPIKV_OK, 0)
+
+
+@pytest.mark.parametrize("n", [2, 7, 16, 40])
+def test_probabilities_of_a_bf16_cache(gpu_lib, n):
+    """Values of +1 and -1 whose sum nearly cancels: what is left shows the probabilities' own bits.  Two bf16 terms hold
+    a probability to 2^-16 (each 2^-8 of what it takes); 32-bit sums of up to 40 products, their exponentials and the
+    division add less than 2^-17.  One term alone would be outside the bound, which is checked on the reference."""
+    H, d = 4, 64
+    c = R.Cache(seqs=1, T=64, H=H, d=d, bits=16, seed=18, spread=0.05)
+    sign = torch.where(torch.arange(c.c.v.numel() // (H * d)) % 2 == 0, 1.0, -1.0)
+    vals = c.c.v.view(-1, H, d)
+    vals[c.index(0, 0, torch.arange(64))] = sign[:64, None, None].to(torch.bfloat16).cuda().expand(64, H, d)
+    ctx = c.context(16, 1)
+    q = queries(1, 16, d)
+    o, _ = run(c, ctx, q, [1], [n - 1])
+    k, v = c.read(0, 0, 0, n), c.read(1, 0, 0, n)
+    want, _, big, qk = R.attention64(q, k, v, [n], d ** -0.5)
+    tol = 2.0 ** -8 * want.abs() + (2.0 ** -15 + 2 * (d * 2.0 ** -24 * qk + 1e-6)[..., None]) * big
+    assert bool(((o.double() - want).abs() <= tol).all())
+    if n % 2:       # one value more of a sign: the output's own rounding hides the term
+        return
+    s = torch.einsum("hd,thd->ht", q[0].double(), k.repeat_interleave(4, 1)) * d ** -0.5
+    p = torch.exp(s - s.amax(-1, keepdim=True))
+    one = torch.einsum("ht,thd->hd", p.to(torch.bfloat16).double(), v.repeat_interleave(4, 1)) / p.sum(-1)[:, None]
+    assert float(((one - want[0]).abs() > tol[0]).double().mean()) > 0.5
 
 
 @pytest.mark.parametrize("bits", [16, 4])
