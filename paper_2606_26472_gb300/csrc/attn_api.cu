@@ -138,8 +138,8 @@ bool valid_cache(const AttnDims& dm, int layer, const epikv_kv_view* kv, KvDev* 
 
 epikv_status cuda_status(cudaError_t e) { return e == cudaSuccess ? EPIKV_OK : EPIKV_ECUDA; }
 
-bool valid_batch(const epikv_attn_ctx* ctx, int32_t n_seq, const int32_t* seq_ids, const int32_t* cu_new,
-                 int32_t max_new, const int32_t* len, int32_t len_stride, Batch* out) {
+bool valid_batch(int32_t n_seq, const int32_t* seq_ids, const int32_t* cu_new, int32_t max_new, const int32_t* len,
+                 int32_t len_stride, Batch* out) {
   if (!seq_ids || !cu_new || !len || len_stride < 1) return false;
   out->seq_ids = seq_ids;
   out->cu_new = cu_new;
@@ -228,7 +228,7 @@ epikv_status epikv_append(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, con
   if (!ctx || n_seq < 0 || n_seq > ctx->dm.S || max_new < 0 || max_new > ctx->dm.max_new) return EPIKV_EINVAL;
   if (n_seq == 0 || max_new == 0) return EPIKV_OK;  // nothing to append
   Batch ba;
-  if (!valid_batch(ctx, n_seq, d_seq_ids, d_cu_new, max_new, d_len, len_stride, &ba)) return EPIKV_EINVAL;
+  if (!valid_batch(n_seq, d_seq_ids, d_cu_new, max_new, d_len, len_stride, &ba)) return EPIKV_EINVAL;
   Rows qr = {}, qo = {}, kr, vr;
   RopeDev rd = {};
   KvDev kd;
@@ -255,7 +255,7 @@ epikv_status epikv_attention(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, 
   Batch ba;
   Rows qr, yr;
   KvDev kd;
-  if (!valid_batch(ctx, n_seq, d_seq_ids, d_cu_new, max_new, d_len, len_stride, &ba)) return EPIKV_EINVAL;
+  if (!valid_batch(n_seq, d_seq_ids, d_cu_new, max_new, d_len, len_stride, &ba)) return EPIKV_EINVAL;
   if (!valid_rows(q, &qr) || !valid_rows(out, &yr) || q->type != EPIKV_TYPE_BF16 || out->type != EPIKV_TYPE_BF16)
     return EPIKV_EINVAL;
   if (((uintptr_t)d_lse & 3u) || !valid_cache(ctx->dm, layer, kv, &kd)) return EPIKV_EINVAL;

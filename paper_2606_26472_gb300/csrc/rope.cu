@@ -73,13 +73,6 @@ __device__ __forceinline__ void to_float(const Raw<T, V>& r, float* f) {
   }
 }
 
-template <typename T, int V>
-__device__ __forceinline__ void load_v(const T* p, float* f) {
-  Raw<T, V> r;
-  load_raw<T, V>(p, r);
-  to_float<T, V>(r, f);
-}
-
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
