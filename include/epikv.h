@@ -369,7 +369,10 @@ enum { EPIKV_ROPE_HALF = 0, EPIKV_ROPE_INTERLEAVED = 1 };
  *   NTK      theta multiplied by factor^(dim/(dim-2))
  *   BYPARTS  freq * ((1-g)/factor + g), g = clamp((rot - low) / (high - low)),
  *            rot = original * freq / 2pi: the turns that the frequency makes
- *            over the original context */
+ *            over the original context.  The ramp is linear in turns, as Llama
+ *            3.1's is; checkpoints whose ramp is linear over the frequency's
+ *            index between two rounded ends (the usual YaRN code) need a table
+ *            of their own in epikv_rope_view */
 enum { EPIKV_ROPE_PLAIN = 0, EPIKV_ROPE_LINEAR = 1, EPIKV_ROPE_NTK = 2, EPIKV_ROPE_BYPARTS = 3 };
 
 typedef struct {

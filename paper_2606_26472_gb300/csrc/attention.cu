@@ -29,18 +29,32 @@
 // if the queries follow it), a conversion turns two codes into a half pair,
 // and the product with the E4M3 scale is exact in half precision (2 + 4
 // significant bits).  Queries enter as halves scaled by a power of two per
-// row (exact but for channels below 2^-31 of the row's largest), probabilities as halves times 2^7 (11 bits down to 2^-21).  For
-// a bf16 cache the probabilities go in as two bf16 terms (16 bits), for which
-// the tensor instructions have time: one term alone would add an error of the
-// output's own rounding.
+// row (exact but for channels below 2^-31 of the row's largest).
+//
+// Roundings to fewer than 32 bits, all of single factors (maxima, sums and
+// products are held in 32):
+//  - a probability over a 4-bit cache: a half times 2^7, 11 bits down to 2^-21.
+//    Its 2^-12 stands beside the output's own 2^-9 (the error against 64 bits
+//    grows from 0.00166 to 0.00167 of the output) and beside values of 3 bits; a
+//    second term would be half as many tensor instructions again, where
+//    instructions bound the kernel.
+//  - a probability over a bf16 cache: two bf16 terms, 16 bits, for which the
+//    tensor instructions have time (HBM bounds it); one alone, of 8 bits, would
+//    add an error of the output's own rounding.
+//  - exponentials by the hardware's base-2 approximation: 2^-22 of each, and 0
+//    below 2^-126 of the largest.
+// The sums of probabilities take them unrounded, so lse has 32-bit accuracy.
 //
 // What it measured (one token an entry, 32 query and 8 KV heads of 128): bf16,
-// 64 x 5,120 slots 204 us, 6.6 TB/s; 32 x 8,192 166 us: HBM.  4 bits, 32 x
-// 8,256 slots 71 us, 4.3 TB/s: 266 instructions for 16 slots of a head (64 of
-// them conversions, 64 products with scales, 16 tensor instructions) at 0.46 a
-// cycle and scheduler, with two computing warps each; four warps a scheduler
-// (96 or 128 registers) were slower, 104 to 121 us.  2,048 slots of one
-// sequence 13 us, 4 x 136 14 us: two launches and their chains of reads.
+// 64 x 5,120 slots 201 to 204 us, 6.6 TB/s; 32 x 8,192 163 us: HBM.  4 bits, 32
+// x 8,256 slots 72 to 75 us, 4.1 TB/s: 269 instructions for 16 slots of a head
+// (64 of them conversions, 64 products with scales, 16 tensor instructions) at
+// 0.46 a cycle and scheduler, with two computing warps each; four warps a
+// scheduler (96 or 128 registers) were slower, 104 to 121 us.  2,048 slots of
+// one sequence 13 us, 4 x 136 14 us: two launches and their chains of reads.
+// Far from its floor where an item's 8 to 32 rows read the cache anew: 8 x 64
+// tokens over 4,096 slots 270 us in bf16, 209 in 4 bits (floor 21 and 18), a
+// prompt of 4,096 tokens 1.36 ms (floor 0.07).
 #include <cuda.h>
 
 #include "attn.cuh"
@@ -328,8 +342,9 @@ struct Ring {
 };
 
 // 4-bit rows: a bulk copy for each run of slots that is one piece of memory (a block's, where its rows stand side by
-// side), each 4 to 18 KB (a copy of a row alone keeps the copy engine for about 110 cycles: a third of HBM's rate).  A
-// lane looks after one run; where a tile has over 32 (rows that stand apart), the others are looked up as they are copied.
+// side), each 4 to 18 KB (a copy of a row alone keeps the copy engine for about 110 cycles: a third of HBM's rate, which
+// is what rows apart or in parts cost: 32 x 4,096 slots of 11 heads 127 us, a quarter of the rate).  A lane looks after
+// one run; where a tile has over 32 (rows that stand apart), the others are looked up as they are copied.
 template <int D>
 __device__ void copy_q4(char* smem, uint64_t* full, uint64_t* empty, const Waiter& wait, const AttnState& st,
                         const AttnDims& dm, const Geometry& ge, const KvDev& kv, int layer, const Walker& walker,
@@ -506,7 +521,7 @@ __device__ void copy_tensor(char* smem, uint64_t* full, uint64_t* empty, const W
 }
 
 // bf16 rows of any layout, 16 bytes a lane, to where a tensor copy would put them.  Lane i reads the table entries of
-// rows i, i + 32, ...
+// rows i, i + 32, ...  (64 x 4,096 slots, blocks of 7: 234 us; of 16, by tensor copies: 165 to 169.)
 template <int D>
 __device__ void copy_bf16(char* smem, uint64_t* full, uint64_t* empty, const Waiter& wait, const AttnState& st,
                           const AttnDims& dm, const Geometry& ge, const KvDev& kv, int layer, const Walker& walker,
@@ -1367,7 +1382,6 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttnState st, 
 Geometry geometry(const AttnDims& dm, int n_seq, int max_new, bool causal) {
   return attn_geometry(dm.H, dm.rep, dm.d, dm.fmt == EPIKV_CACHE_E2M1, dm.units, dm.T, n_seq, max_new, causal);
 }
-
 
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,

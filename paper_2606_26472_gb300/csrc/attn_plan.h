@@ -121,8 +121,11 @@ EPIKV_PLAN int attn_row_blocks(int d, int rep, int max_new) {
 }
 // 16-slot blocks of a tile that a warp takes of 4-bit rows (bf16: one, whose tiles are 64 KB at 8 x 128): what a tile
 // costs besides its products (waits, the check against the maximum) is shared by so many.  Four where the caches, if
-// full, give each CTA 16 such tiles (`slots`: of all entries; 32 x 8,256 slots two 75, four 72 us; d = 64, 32 x 16,384 91
-// and 82), else two (4 x 136 slots two 14.0, four 17.1 us; one sequence of 65,536 33.6 and 34.2).
+// full, give each CTA 16 such tiles (`slots`: of all entries; 32 x 8,256 slots two 77, four 75 us; d = 64, 32 x 16,384 92
+// and 82), else two (4 x 136 slots two 14.4, four 18.1 us; one sequence of 65,536 34.1 and 34.9).  The host knows what
+// the caches can hold, not what they do: 32 sequences of 131,072 slots that hold 500 to 1,000 take 23.0 with four, 22.0
+// with two, 2,000 to 4,000 42.8 and 41.3, 500 to 8,000 53.3 and 51.0.  A caller whose caches stay that far from full
+// does better with the capacity that they reach as max_cache_tokens.
 EPIKV_PLAN int attn_sub_blocks(bool q4, int d, int nt, int64_t slots) {
   return !q4 ? 1 : nt == 1 && d <= 128 && slots >= (int64_t)kAttnCtas * 16 * 64 ? 4 : 2;
 }

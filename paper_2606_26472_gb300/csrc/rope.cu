@@ -18,7 +18,9 @@
 // in 31.6 us (5.4 TB/s), four prompts of 517 to 4,099 tokens (32 + 8 + 8 heads)
 // appended in 45.0 us (5.1 TB/s).  Into a 4-bit cache the quantisation does: 32
 // x 128 tokens 20 us, 890 instructions a warp.  One token an entry is a launch
-// and a chain of four reads (lengths, block, position's row, rows): 6.1 us.
+// and a chain of four reads (lengths, block, position's row, rows): 5.5 us.  With
+// V = 1, for a rotated range that 16 does not divide, heads go by single
+// elements: 8,192 x 40 heads 48 us, the four prompts 69 us.
 #include "attn.cuh"
 
 namespace epikv {
@@ -169,7 +171,7 @@ __global__ void rope_table_kernel(epikv_rope_config c, int n_pos, float2* table)
 
 // kBatch heads of a thread are in flight; their loads go out before the position and the table's row are known.  More of
 // them, or registers held down for more CTAs, cost occupancy or loads in flight: 8,192 x 40 heads of bf16 two 32.4, three
-// 31.7 us (held to 72 registers 34.1); 4,096 x 40 heads of 32-bit data one 27.6, two 30.5 us.
+// 31.7 us (held to 72 registers 34.1); 4,096 x 40 heads of 32-bit data one 27.5, two 30.5 us.
 template <typename T, int V>
 __global__ void __launch_bounds__(kBlock) rope_kernel(int32_t* err, Rows x, Rows y, const int32_t* __restrict__ pos,
                                                       RopeDev r, int n_tokens, int heads, int d, float sign) {
@@ -228,7 +230,8 @@ __global__ void __launch_bounds__(kBlock) rope_kernel(int32_t* err, Rows x, Rows
 // Sixteen values in 4 bits: their codes (8 bytes) and scale.  Without a head scale the values are bf16, and a quotient
 // needs no division: x has 8 significant bits, a boundary between two codes times the scale 7, so x / scale is such a
 // boundary or at least 2^-8 of it away.  The product with the rounded reciprocal, rounded to 12 bits, is then the boundary
-// itself or on the same side.  (32 x 128 tokens of 8 x 128, with the queries and the read-back: divisions 35.0, this 33.7 us.)
+// itself or on the same side.  (32 x 128 tokens of 8 x 128, with the queries and the read-back: 33.7 instead of 35.0 us when
+// it was taken in, 30.9 with what came later.)
 __device__ __forceinline__ uint2 quantize16(const float* x, float g, uint32_t* scale) {
   float y[16];
   float top = 0.f;
@@ -423,8 +426,8 @@ __global__ void __launch_bounds__(kBlock) append_kernel(AttnState st, AttnDims d
 
 // ------------------------------------------------------------------ read-back
 
-// A thread takes 16 channels of one head of a row (4,096 rows of 8 x 128 out of 4 bits: 11 us, bound by the latency of
-// its reads: the sequence and slot, the block, the row).
+// A thread takes 16 channels of one head of a row (4,096 rows of 8 x 128 out of 4 bits: 11 us, where their 21 MB would take
+// 3, for the latency of its reads: the sequence and slot, the block, the row).
 __global__ void __launch_bounds__(kBlock) cache_read_kernel(AttnState st, AttnDims dm, int layer, int n_rows,
                                                             const int32_t* __restrict__ seqs,
                                                             const int32_t* __restrict__ slots, Rows k, Rows v,
