@@ -473,6 +473,10 @@ epikv_status epikv_append(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, con
  *             reads slots 0 .. d_len[b] + i.  0: every query reads the d_len[b]
  *             slots (a shared prefix; join with d_lse)
  *   d_lse     float [total_new][num_heads] or NULL: log of the sum of exponentials
+ * A probability is held in 16 bits (bf16 cache; below 2^-126 of the row's largest
+ * it is 0) or, over a 4-bit cache, in 11 bits down to 2^-21 of about the row's
+ * largest and to within 2^-32 of it below: a channel to which only slots of less
+ * weight contribute keeps that absolute accuracy, not the relative one.
  * A row that sees no slot, or only slots of score -infinity, gives zeros and
  * -infinity.  An infinite value in a slot that a row sees is the row's output in
  * that channel, however small its probability (NaN beside one of the other sign,

@@ -33,7 +33,8 @@
 //
 // Roundings to fewer than 32 bits, all of single factors (maxima, sums and
 // products are held in 32):
-//  - a probability over a 4-bit cache: a half times 2^7, 11 bits down to 2^-21.
+//  - a probability over a 4-bit cache: a half times 2^7, 11 bits down to 2^-21
+//    of the maximum that it is taken against, within 2^-32 below.
 //    Its 2^-12 stands beside the output's own 2^-9 (the error against 64 bits
 //    grows from 0.00166 to 0.00167 of the output) and beside values of 3 bits; a
 //    second term would be half as many tensor instructions again, where
