@@ -79,6 +79,9 @@ typedef enum {
  *   KVKEY   KV-key: rolling mean of the stored keys' head variance (Sec. 3.3)
  *   KVVAL   KV-val: the same for the values (Sec. 3.3)
  *   LAGKEY  lag-kv-key: Lag-KV's key term only (Tab. "acc-math" rows)
+ *   WEIGHT  accumulated attention weight, which needs what attention-free kinds do without: what
+ *           epikv_attention_weights finds, added up by epikv_weigh.  Not frozen: a new token's
+ *           score is 0 until then
  * The band kinds use z_window as their window; the K/V kinds lag_window. */
 enum {
   EPIKV_SCORE_BANDZ = 1,
@@ -87,6 +90,7 @@ enum {
   EPIKV_SCORE_KVKEY = 8,
   EPIKV_SCORE_KVVAL = 16,
   EPIKV_SCORE_LAGKEY = 32,
+  EPIKV_SCORE_WEIGHT = 128,   /* (64 is no kind) */
 };
 
 /* KV cache layouts. */
@@ -108,7 +112,8 @@ typedef struct {
   float lag_eps;            /* epsilon of the range normalisation (1e-6) */
   int32_t lag_window;       /* rolling-mean window of the K/V scores (64), 1..1024 */
   int32_t recency_cap;      /* recency window R = min(recency_cap, K/4) (App. D: 128) */
-  int32_t score_kinds;      /* EPIKV_SCORE_* mask (1..63) computed by every update */
+  int32_t score_kinds;      /* EPIKV_SCORE_* mask computed by every update (WEIGHT: by epikv_weigh; not with
+                             * layer_budgets) */
   int32_t select_chunk;     /* C, 0..65536 (0 reads as 1).  1: the paper's token-level top-K.
                              * C > 1: chunk-level selection, which the paper names as future
                              * work (Sec. 5, after ChunkKV's contiguous chunks, Sec. 2): the
@@ -495,6 +500,53 @@ epikv_status epikv_attention(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, 
                              const int32_t* d_cu_new, int32_t max_new, const int32_t* d_len, int32_t len_stride,
                              int32_t causal, const epikv_rows* q, const epikv_rows* out, float* d_lse,
                              const epikv_kv_view* kv, cudaStream_t stream);
+
+/* The same attention for many query rows: chunks of prompts, drafts, turns, of one token or more a sequence.
+ * Arguments, order of the slots, what a row sees, empty rows and d_lse as in epikv_attention; nothing is split
+ * between calls, so a prompt may be taken in by pieces.  It reads the cache once for 256 rows (tokens times
+ * num_heads / num_kv_heads; 128 at head_dim 256) where epikv_attention does so for 8 to 32, and is the faster one
+ * from about 16 new tokens a sequence on.
+ * A probability is held in 8 significant bits over a bf16 cache, in 11 (down to 2^-31 of about the row's largest)
+ * over a 4-bit one; sums, maxima and d_lse in 32 bits.  In a channel where a slot that a row sees holds an infinity or a NaN the
+ * row's output is infinite or NaN.  Slots that a row does not see do not reach it, whatever they hold; no memory
+ * behind them is read. */
+epikv_status epikv_attention_chunk(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* d_seq_ids,
+                                   const int32_t* d_cu_new, int32_t max_new, const int32_t* d_len, int32_t len_stride,
+                                   int32_t causal, const epikv_rows* q, const epikv_rows* out, float* d_lse,
+                                   const epikv_kv_view* kv, cudaStream_t stream);
+
+/* A number for every slot and KV head: device float, that of (sequence, head, slot) at seq*stride_seq +
+ * head*stride_head + slot (strides in elements; the caller keeps the rows of max_cache_tokens slots apart). */
+typedef struct {
+  float* ptr;               /* 4-byte aligned */
+  int64_t stride_seq;
+  int64_t stride_head;
+} epikv_weights;
+
+/* What each slot of one layer's cache receives of the attention of the batch's queries: for KV head h,
+ *   sum over the entry's new tokens and the query heads that read h of exp(scale q.k - lse)
+ * over the queries that see the slot.  In 32 bits, in an order that depends on the sizes alone.
+ *   d_seq_ids .. causal, q, kv   as in the attention call that gave d_lse
+ *   last      only the last so many of each entry's new tokens count; 0: all of them
+ *   d_lse     float [total_new][num_heads]: the attention's, or its joined parts'
+ *   add       0: store, 1: add to what stands there (the next layer of a step)
+ *   w         written for the entries' sequences and all KV heads, slots 0 .. d_len + n - 1 (causal = 0: 0 ..
+ *             d_len - 1), nothing else.  An entry without new tokens stores zeros
+ * A query whose lse is minus infinity saw nothing and gives nothing; a NaN in what a slot receives is NaN there.
+ * A slot outside the view receives nothing (EPIKV_DEV_SLOT). */
+epikv_status epikv_attention_weights(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* d_seq_ids,
+                                     const int32_t* d_cu_new, int32_t max_new, const int32_t* d_len, int32_t len_stride,
+                                     int32_t causal, int32_t last, const epikv_rows* q, const float* d_lse, int32_t add,
+                                     const epikv_weights* w, const epikv_kv_view* kv, cudaStream_t stream);
+
+/* Add a step's weights to the WEIGHT scores of a context's slots (its score_kinds hold EPIKV_SCORE_WEIGHT): for slots
+ * 0 .. n_cache-1 of each entry's sequence
+ *   score = decay * score + sum over h = 0 .. n_heads-1 of w(seq, h, slot)
+ * (32 bits, each product and sum rounded, heads first, in order).  decay is in 0 .. 1; 1 accumulates for good.
+ * Belongs between epikv_score_update, which registers the step's tokens, and epikv_select; the scores move with their
+ * tokens from then on, and epikv_read_slots returns them. */
+epikv_status epikv_weigh(epikv_ctx* ctx, int32_t n_seq, const int32_t* d_seq_ids, const epikv_weights* w, int32_t n_heads,
+                         float decay, cudaStream_t stream);
 
 /* Read n_rows rows of one layer back as bf16 [n_rows][num_kv_heads][d]: slot
  * d_slots[i] of sequence d_seqs[i].  k or v may be NULL.  Rows outside the view

@@ -42,7 +42,9 @@ bool valid_config(const epikv_config* c) {
   if (c->max_seqs < 1 || c->max_seqs > kMaxSeqs) return false;
   if (c->max_cache_tokens < 1 || c->max_cache_tokens > (1 << 24)) return false;
   if (c->max_new_tokens < 1 || c->max_new_tokens > (1 << 20)) return false;
-  if (c->score_kinds < 1 || c->score_kinds > 63) return false;
+  if (c->score_kinds < 1 || (c->score_kinds & ~(63 | EPIKV_SCORE_WEIGHT))) return false;
+  // each layer would have slots, and so scores, of its own
+  if ((c->score_kinds & EPIKV_SCORE_WEIGHT) && c->layer_budgets) return false;
   if (c->recency_cap < 0) return false;
   if (c->select_chunk < 0 || c->select_chunk > 65536) return false;
   if (c->layer_budgets != 0 && c->layer_budgets != 1) return false;
@@ -115,7 +117,7 @@ size_t carve(const Dims& d, DevState* st, char* base) {
   st->kept = (int32_t*)take(S * LB * T * 4);
   st->n_kept = (int32_t*)take(S * LB * 4);
   for (int k = 0; k < kNumKinds; ++k)
-    if (d.kinds & (1 << k)) st->score[k] = (float*)take(S * T * 4);
+    if (d.kinds & kind_bit(k)) st->score[k] = (float*)take(S * T * 4);
   if (d.kinds & kBandKinds) {
     const size_t nb = d.nA + d.nB;
     st->h_prev = (__nv_bfloat16*)take(S * 2 * nb * d.D * 2);
@@ -261,6 +263,18 @@ epikv_status epikv_score_update(epikv_ctx* ctx, int32_t n_seq, const int32_t* d_
   int launches = 0;
   ClockScope clock(ctx);
   return score_update_impl(ctx, n_seq, d_seq_ids, d_cu_new, max_new, hidden, kv, stream, &launches);
+}
+
+epikv_status epikv_weigh(epikv_ctx* ctx, int32_t n_seq, const int32_t* d_seq_ids, const epikv_weights* w, int32_t n_heads,
+                         float decay, cudaStream_t stream) {
+  if (!ctx || !(ctx->dm.kinds & EPIKV_SCORE_WEIGHT) || n_seq < 0 || n_seq > ctx->dm.S) return EPIKV_EINVAL;
+  if (n_seq == 0) return EPIKV_OK;  // nothing to weigh
+  if (!d_seq_ids || !w || !w->ptr || ((uintptr_t)w->ptr & 3u) || w->stride_seq < 0 || w->stride_head < 0) return EPIKV_EINVAL;
+  if (n_heads < 1 || n_heads > 1024 || !(decay >= 0.f) || !(decay <= 1.f)) return EPIKV_EINVAL;
+  ctx->last_stream = stream;
+  ClockScope clock(ctx);
+  return cuda_status(launch_weigh(ctx->st, ctx->dm, n_seq, d_seq_ids, w->ptr, w->stride_seq, w->stride_head, n_heads, decay,
+                                  stream));
 }
 
 epikv_status epikv_select(epikv_ctx* ctx, int32_t n_seq, const int32_t* d_seq_ids, const int32_t* d_budget,

@@ -118,6 +118,13 @@ cudaError_t launch_cache_read(const AttnState& st, const AttnDims& dm, int layer
                               cudaStream_t stream);
 cudaError_t launch_attention(const AttnState& st, const AttnDims& dm, int layer, const Batch& ba, bool causal,
                              const Rows& q, const Rows& out, float* lse, const KvDev& kv, cudaStream_t stream);
+cudaError_t launch_attention_chunk(const AttnState& st, const AttnDims& dm, int layer, const Batch& ba, bool causal,
+                                   const Rows& q, const Rows& out, float* lse, const KvDev& kv, cudaStream_t stream);
+cudaError_t chunk_prepare(const AttnDims& dm);
+cudaError_t launch_attention_weights(const AttnState& st, const AttnDims& dm, int layer, const Batch& ba, bool causal,
+                                     int last, const Rows& q, const float* lse, bool add, float* w, int64_t stride_seq,
+                                     int64_t stride_head, const KvDev& kv, cudaStream_t stream);
+cudaError_t weights_prepare(const AttnDims& dm);
 size_t attention_part_floats(const AttnDims& dm);
 cudaError_t attention_prepare(const AttnDims& dm, bool* runs);
 

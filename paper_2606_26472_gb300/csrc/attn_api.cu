@@ -136,6 +136,17 @@ bool valid_cache(const AttnDims& dm, int layer, const epikv_kv_view* kv, KvDev* 
   return true;
 }
 
+// Rows of T slots for every sequence and head, none of which meets another.
+bool valid_weights(const epikv_weights* w, int S, int H, int T) {
+  if (!w || !w->ptr || ((uintptr_t)w->ptr & 3u) || w->stride_seq < 0 || w->stride_head < 0) return false;
+  const int64_t lo = S > 1 && (H == 1 || w->stride_seq < w->stride_head) ? w->stride_seq : w->stride_head;
+  if (S == 1 && H == 1) return true;
+  if (lo < T) return false;
+  if (S == 1 || H == 1) return true;
+  const int64_t n = lo == w->stride_seq ? S : H, hi = lo == w->stride_seq ? w->stride_head : w->stride_seq;
+  return hi / lo >= n || (hi - T) / lo >= n - 1;
+}
+
 epikv_status cuda_status(cudaError_t e) { return e == cudaSuccess ? EPIKV_OK : EPIKV_ECUDA; }
 
 bool valid_batch(int32_t n_seq, const int32_t* seq_ids, const int32_t* cu_new, int32_t max_new, const int32_t* len,
@@ -183,6 +194,8 @@ epikv_status epikv_attn_init(epikv_attn_ctx** out, const epikv_attn_config* cfg,
   ctx->st.kv_scale = cfg->kv_scale;
   ctx->last_stream = stream;
   cudaError_t e = attention_prepare(dm, &ctx->attention_runs);
+  if (e == cudaSuccess) e = chunk_prepare(dm);
+  if (e == cudaSuccess) e = weights_prepare(dm);
   if (e == cudaSuccess) e = cudaMemsetAsync(ctx->st.err, 0, 4, stream);
   if (e != cudaSuccess) {
     free(ctx);
@@ -262,6 +275,44 @@ epikv_status epikv_attention(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, 
   if (!ctx->attention_runs) return EPIKV_ECUDA;
   ctx->last_stream = stream;
   return cuda_status(launch_attention(ctx->st, ctx->dm, layer, ba, causal, qr, yr, d_lse, kd, stream));
+}
+
+epikv_status epikv_attention_chunk(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* d_seq_ids,
+                                   const int32_t* d_cu_new, int32_t max_new, const int32_t* d_len, int32_t len_stride,
+                                   int32_t causal, const epikv_rows* q, const epikv_rows* out, float* d_lse,
+                                   const epikv_kv_view* kv, cudaStream_t stream) {
+  if (!ctx || n_seq < 0 || n_seq > ctx->dm.S || max_new < 0 || max_new > ctx->dm.max_new ||
+      (causal != 0 && causal != 1))
+    return EPIKV_EINVAL;
+  if (n_seq == 0 || max_new == 0) return EPIKV_OK;  // no queries
+  Batch ba;
+  Rows qr, yr;
+  KvDev kd;
+  if (!valid_batch(n_seq, d_seq_ids, d_cu_new, max_new, d_len, len_stride, &ba)) return EPIKV_EINVAL;
+  if (!valid_rows(q, &qr) || !valid_rows(out, &yr) || q->type != EPIKV_TYPE_BF16 || out->type != EPIKV_TYPE_BF16)
+    return EPIKV_EINVAL;
+  if (((uintptr_t)d_lse & 3u) || !valid_cache(ctx->dm, layer, kv, &kd)) return EPIKV_EINVAL;
+  ctx->last_stream = stream;
+  return cuda_status(launch_attention_chunk(ctx->st, ctx->dm, layer, ba, causal, qr, yr, d_lse, kd, stream));
+}
+
+epikv_status epikv_attention_weights(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* d_seq_ids,
+                                     const int32_t* d_cu_new, int32_t max_new, const int32_t* d_len, int32_t len_stride,
+                                     int32_t causal, int32_t last, const epikv_rows* q, const float* d_lse, int32_t add,
+                                     const epikv_weights* w, const epikv_kv_view* kv, cudaStream_t stream) {
+  if (!ctx || n_seq < 0 || n_seq > ctx->dm.S || max_new < 0 || max_new > ctx->dm.max_new ||
+      (causal != 0 && causal != 1) || (add != 0 && add != 1) || last < 0)
+    return EPIKV_EINVAL;
+  if (n_seq == 0) return EPIKV_OK;  // no sequences
+  Batch ba;
+  Rows qr;
+  KvDev kd;
+  if (!valid_batch(n_seq, d_seq_ids, d_cu_new, max_new, d_len, len_stride, &ba)) return EPIKV_EINVAL;
+  if (!valid_rows(q, &qr) || q->type != EPIKV_TYPE_BF16 || !d_lse || ((uintptr_t)d_lse & 3u)) return EPIKV_EINVAL;
+  if (!valid_weights(w, ctx->dm.S, ctx->dm.H, ctx->dm.T) || !valid_cache(ctx->dm, layer, kv, &kd)) return EPIKV_EINVAL;
+  ctx->last_stream = stream;
+  return cuda_status(launch_attention_weights(ctx->st, ctx->dm, layer, ba, causal, last, qr, d_lse, add, w->ptr,
+                                              w->stride_seq, w->stride_head, kd, stream));
 }
 
 epikv_status epikv_cache_read(epikv_attn_ctx* ctx, int32_t layer, int32_t n_rows, const int32_t* d_seqs,

@@ -15,7 +15,7 @@ namespace epikv {
 
 constexpr int kMaxSeqs = 4096;  // sequences of a context, so entries of a batch
 constexpr int kMaxBand = 32;
-constexpr int kNumKinds = 6;  // score kind index k <-> mask bit (1 << k)
+constexpr int kNumKinds = 7;  // score kind index k <-> mask bit kind_bit(k)
 constexpr int kBandKinds = EPIKV_SCORE_BANDZ | EPIKV_SCORE_HSVAR;
 constexpr int kNormKinds = EPIKV_SCORE_LAGKV | EPIKV_SCORE_LAGKEY;   // need the chunk ranges
 constexpr int kRawKinds = EPIKV_SCORE_KVKEY | EPIKV_SCORE_KVVAL;
@@ -25,13 +25,14 @@ __host__ __device__ __forceinline__ int kv_kind(int q) {
   return q == 0 ? EPIKV_SCORE_LAGKV : q == 1 ? EPIKV_SCORE_KVKEY : q == 2 ? EPIKV_SCORE_KVVAL : EPIKV_SCORE_LAGKEY;
 }
 
+__host__ __device__ __forceinline__ int kind_bit(int k) { return k < kNumKinds - 1 ? 1 << k : EPIKV_SCORE_WEIGHT; }
 __host__ __device__ __forceinline__ int kind_index(int bit) {
   int k = 0;
   while (bit > 1) {
     bit >>= 1;
     ++k;
   }
-  return k;
+  return k < kNumKinds ? k : kNumKinds - 1;   // WEIGHT's bit leaves one out
 }
 
 // Device pointers carved out of the caller's workspace (one context).
@@ -39,13 +40,13 @@ struct DevState {
   int32_t* n_cache;        // [S] slots in use
   int32_t* n_seen;         // [S] next position
   int32_t* prefill;        // [S]
-  int32_t* policy;         // [S] score kind driving selection (1 or 2)
+  int32_t* policy;         // [S] score kind driving selection
   int32_t* hp_parity;      // [S] which h_prev buffer holds the last row
   int32_t* first_changed;  // [S] first slot moved by the last selection
   uint32_t* ticket;        // [S] last-CTA tickets of the finalize kernel
   int32_t* err;            // [1] sticky device error word
   unsigned long long* stats;  // [4] epikv_stats
-  float* score[kNumKinds]; // [S][T] frozen scores per kind (null when the kind is off)
+  float* score[kNumKinds]; // [S][T] scores per kind (null when the kind is off); frozen but for WEIGHT's
   int32_t* pos;            // [S][T] position of each slot
   __nv_bfloat16* h_prev;   // [S][2][n_band][D] last hidden row per band layer
   float* g_ring;           // [S][n_band][G] g by position (mod G)

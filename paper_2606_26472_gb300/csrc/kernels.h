@@ -21,6 +21,10 @@ cudaError_t launch_compact(const DevState& st, const Dims& dm, int n_seq, const 
                            const int32_t* kept, int kept_stride, const KvDev& kv, int ctas,
                            cudaStream_t stream, int* launches);
 
+// Adds the heads' weights of a step to the slots' WEIGHT scores.
+cudaError_t launch_weigh(const DevState& st, const Dims& dm, int n_seq, const int32_t* seq_ids, const float* w,
+                         int64_t stride_seq, int64_t stride_head, int heads, float decay, cudaStream_t stream);
+
 cudaError_t compact_prepare(int device, int* ctas_per_sm);
 cudaError_t finalize_prepare();
 cudaError_t select_prepare();

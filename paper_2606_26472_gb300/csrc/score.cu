@@ -1140,6 +1140,41 @@ __global__ void __launch_bounds__(kGThreads, EPIKV_TOKEN_MINB) token_kernel(DevS
   if (tid == 64) token_commit(st, dm, seq, nc0, pos);
 }
 
+// The WEIGHT kind: a new token's score is 0 until epikv_weigh adds to it.  Where it is the only kind (`alone`), the kernel
+// is the whole update: positions and counters too.  One CTA per batch entry.
+__global__ void __launch_bounds__(1024) weight_rows_kernel(DevState st, Dims dm, const int32_t* __restrict__ seq_ids,
+                                                           const int32_t* __restrict__ cu_new, int max_new, int alone) {
+  pdl_wait();
+  pdl_trigger();
+  const int b = blockIdx.x, tid = threadIdx.x;
+  const int seq = seq_ids[b];
+  const int n_new = cu_new[b + 1] - cu_new[b];
+  if (seq < 0 || seq >= dm.S || n_new < 0 || n_new > max_new) {
+    if (tid == 0 && alone) set_error(st.err, EPIKV_DEV_BATCH);
+    return;   // (with other kinds their kernels report it)
+  }
+  const int nc0 = st.n_cache[seq], p0 = st.n_seen[seq];
+  if (nc0 + n_new > dm.T) {
+    if (tid == 0 && alone) set_error(st.err, EPIKV_DEV_CAPACITY);
+    return;
+  }
+  const size_t base = (size_t)seq * dm.T + nc0;
+  float* score = st.score[kind_index(EPIKV_SCORE_WEIGHT)] + base;
+  for (int i = tid; i < n_new; i += blockDim.x) {
+    score[i] = 0.f;
+    if (alone) st.pos[base + i] = p0 + i;
+  }
+  if (!alone) return;
+  __syncthreads();   // every thread has read the counters
+  if (tid == 0) {
+    if (st.first_changed[seq] < nc0) set_error(st.err, EPIKV_DEV_KEPT);   // selected, not compacted
+    st.first_changed[seq] = nc0 + n_new;
+    st.n_cache[seq] = nc0 + n_new;
+    st.n_seen[seq] = p0 + n_new;
+    atomicAdd(&st.stats[0], (unsigned long long)n_new);
+  }
+}
+
 // ------------------------------------------------------------------ launchers
 // dynamic shared memory of the finalize kernel: the band windows of a tile, or
 // a K/V kind's u over it
@@ -1184,6 +1219,12 @@ cudaError_t launch_score_update(const DevState& st, const Dims& dm, int n_seq, c
   if (n_seq == 0 || max_new == 0) return cudaSuccess;
   const int nb = dm.nA + dm.nB;
   const bool band = dm.kinds & kBandKinds;
+  if (dm.kinds & EPIKV_SCORE_WEIGHT) {
+    const bool alone = dm.kinds == EPIKV_SCORE_WEIGHT;
+    const cudaError_t e = pdl_launch(weight_rows_kernel, dim3(n_seq), 1024, 0, stream, st, dm, seq_ids, cu_new, max_new, alone ? 1 : 0);
+    ++*launches;
+    if (alone || e != cudaSuccess) return e;
+  }
   BandRows rows;
   for (int i = 0; i < kMaxBand; ++i)
     rows.p[i] = band && i < nb ? static_cast<const __nv_bfloat16*>(hv->band_rows[i]) : nullptr;

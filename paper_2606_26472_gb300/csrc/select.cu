@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(kSelThreads) select_kernel(DevState st, Dims d
     unsigned on = 0;   // the policy's column: the kinds held before it
 #pragma unroll
     for (int k = 0; k < kNumKinds; ++k) on |= (st.score[k] != nullptr ? 1u : 0u) << k;
-    const int pc = __popc(on & (unsigned)(policy - 1));
+    const int pc = __popc(on & ((1u << kind_index(policy)) - 1u));
     chunk_keys(reinterpret_cast<const int32_t*>(smeta) + (ncol - 1) * n, reinterpret_cast<const float*>(smeta) + pc * n,
                [&](int i, int j, uint32_t k) {
                  for (int q = i; q < j; ++q) skey[q - c0] = k;

@@ -1,0 +1,215 @@
+// The fifth-generation tensor instructions as the operators of many query rows
+// use them: operands in shared memory in rows of 128 bytes (swizzled), results
+// and probabilities in tensor memory, and bounded waits between the warps.
+#pragma once
+
+#include "attn.cuh"
+
+namespace epikv {
+
+// ------------------------------------------------------------ tensor memory
+// Whole warp; columns a power of two from 32 to 512.  The address is written to shared memory.
+__device__ __forceinline__ void tmem_alloc(uint32_t* dst, uint32_t columns) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+               :: "r"(smem_u32(dst)), "r"(columns) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_free(uint32_t addr, uint32_t columns) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(addr), "r"(columns));
+}
+__device__ __forceinline__ void tensor_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tensor_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// 32 columns of the warp's 32 lanes; r[i] is column i of the thread's lane.  Valid after tmem_wait_load.
+__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr));
+}
+__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr));
+}
+__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      :: "r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+         "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
+         "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
+         "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      :: "r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+         "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// ------------------------------------------------------------ products
+// A tile stands in shared memory as panels of 64 channels: its rows' 128 bytes side by side, a row's eight 16-byte parts
+// exchanged by its number mod 8, so that eight rows (1,024 bytes, aligned to it) are one swizzled block.
+__device__ __forceinline__ uint32_t panel_at(int row, int part) { return row * 128 + ((part ^ (row & 7)) << 4); }
+
+// Such rows as an operand whose products run along the channels (the block's 64 channels are four steps of 32 bytes) ...
+__device__ __forceinline__ uint64_t rows_operand(uint32_t smem) {
+  return (uint64_t)((smem & 0x3ffff) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+         (uint64_t)2 << 61;
+}
+// ... and as one whose products run along the rows (16 rows are a step of 2,048 bytes); the next 64 channels stand `panel`
+// bytes behind.
+__device__ __forceinline__ uint64_t columns_operand(uint32_t smem, uint32_t panel) {
+  return (uint64_t)((smem & 0x3ffff) >> 4) | (uint64_t)(panel >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
+         (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// Sums in 32 bits; both operands half or bf16.  `along_rows`: the second operand is a columns_operand.
+constexpr uint32_t product_of(int m, int n, bool bf16, bool along_rows) {
+  return 1u << 4 | (bf16 ? 1u : 0u) << 7 | (bf16 ? 1u : 0u) << 10 | (along_rows ? 1u : 0u) << 16 | (uint32_t)(n >> 3) << 17 |
+         (uint32_t)(m >> 4) << 24;
+}
+// One thread; d (+)= a b over 16 values.
+__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+               :: "r"(d), "l"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
+}
+// The same, a in tensor memory (two values a column).
+__device__ __forceinline__ void multiply_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t what, bool add) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+               :: "r"(d), "r"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
+}
+// The barrier completes when all that this thread issued before has.
+__device__ __forceinline__ void products_done(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];"
+               :: "r"(smem_u32(bar)) : "memory");
+}
+
+// ------------------------------------------------------------ waits
+__device__ __forceinline__ void mbar_arrive_one(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" :: "r"(smem_u32(bar)) : "memory");
+}
+
+constexpr uint64_t kTensorWaitNs = 2000000000ull;
+struct TensorWaiter {
+  volatile int* gave_up;
+  int32_t* err;
+  // Ends when the phase completes, or (with the error word set) when any wait of the CTA has taken too long: what
+  // follows then runs on without waiting, on data that the error word disowns.
+  __device__ __forceinline__ void operator()(uint64_t* bar, uint32_t parity) const {
+    if (mbar_try_wait(bar, parity)) return;
+    const uint64_t t0 = global_ns();
+    while (!mbar_try_wait(bar, parity)) {
+      if (*gave_up) return;
+      if (global_ns() - t0 > kTensorWaitNs) {
+        *gave_up = 1;
+        set_error(err, EPIKV_DEV_TIMEOUT);
+        return;
+      }
+    }
+  }
+};
+
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src, int bytes) {   // the rest of the 16 is zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
+
+__device__ __forceinline__ void named_sync(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" :: "r"(id), "r"(threads) : "memory");
+}
+
+__device__ __forceinline__ uint4 lds16(uint32_t p) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts16(uint32_t p, const uint4& v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" :: "r"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {   // 2^-22 of the value; 0 below 2^-126
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
+  const __half2 r = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  const __nv_bfloat162 r = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// Both halves of a times the half in the low or high bits of b.
+__device__ __forceinline__ uint32_t half_pair_times(uint32_t a, uint32_t b, bool high) {
+  const __half2 s = *reinterpret_cast<const __half2*>(&b);
+  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), high ? __high2half2(s) : __low2half2(s));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+
+// ------------------------------------------------------------ rows of a tile
+// 32 channels of a 4-bit row (16 bytes of codes, two scales) as 64 bytes of halves, exact: 2 + 4 significant bits between
+// 2^-10 and 2688.
+__device__ __forceinline__ void expand32(const uint4& codes, uint32_t scales, uint4 (&out)[4]) {
+  const uint32_t s = e4m3x2_to_half2((uint16_t)scales);
+  const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t h[4];
+    e2m1x8_to_half2(w[i], h);
+    out[i] = make_uint4(half_pair_times(h[0], s, i >= 2), half_pair_times(h[1], s, i >= 2),
+                        half_pair_times(h[2], s, i >= 2), half_pair_times(h[3], s, i >= 2));
+  }
+}
+
+// A row of D bf16 queries into a tile's row.  Over a 4-bit cache they become halves, scaled by a power of two to below
+// 2^15: exact down to 2^-31 of the row's largest.  What undoes the scaling is returned.
+template <int D, bool kHalf>
+__device__ __forceinline__ float store_query(uint32_t tile, int panel, int row, const uint4* src) {
+  if constexpr (!kHalf) {
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c)
+      sts16(tile + (c >> 3) * panel + panel_at(row, c & 7), src ? __ldg(src + c) : make_uint4(0, 0, 0, 0));
+    return 1.f;
+  } else {
+    uint32_t top = 0;   // largest magnitude, as bf16 bits: they are ordered like the values
+    if (src)
+      for (int c = 0; c < D / 8; ++c) {
+        const uint4 v = __ldg(src + c);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
+      }
+    // 2^e <= largest < 2^(e + 1); up to 2^100, so that neither factor leaves the normal numbers
+    const int up = min(14 - ((int)(top >> 7) - 127), 100);
+    const float mul = __uint_as_float((uint32_t)(up + 127) << 23);
+    for (int c = 0; c < D / 8; ++c) {
+      const uint4 v = src ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+      sts16(tile + (c >> 3) * panel + panel_at(row, c & 7),
+            make_uint4(half_pair(bf16_lo(v.x) * mul, bf16_hi(v.x) * mul), half_pair(bf16_lo(v.y) * mul, bf16_hi(v.y) * mul),
+                       half_pair(bf16_lo(v.z) * mul, bf16_hi(v.z) * mul), half_pair(bf16_lo(v.w) * mul, bf16_hi(v.w) * mul)));
+    }
+    return __uint_as_float((uint32_t)(127 - up) << 23);
+  }
+}
+
+}  // namespace epikv

@@ -15,6 +15,7 @@ EPIKV_DEV_OK, EPIKV_DEV_BATCH, EPIKV_DEV_CAPACITY, EPIKV_DEV_SLOT = 0, 1, 2, 3
 EPIKV_DEV_KEPT, EPIKV_DEV_BUDGET, EPIKV_DEV_TIMEOUT = 4, 5, 6
 EPIKV_SCORE_BANDZ, EPIKV_SCORE_LAGKV, EPIKV_SCORE_HSVAR = 1, 2, 4
 EPIKV_SCORE_KVKEY, EPIKV_SCORE_KVVAL, EPIKV_SCORE_LAGKEY = 8, 16, 32
+EPIKV_SCORE_WEIGHT = 128
 EPIKV_LAYOUT_CONTIGUOUS, EPIKV_LAYOUT_PAGED = 0, 1
 EPIKV_DEV_POSITION = 7
 EPIKV_CACHE_BF16, EPIKV_CACHE_E2M1 = 0, 1
@@ -70,8 +71,14 @@ class epikv_attn_config(C.Structure):
                 ("kv_scale", C.c_void_p)]
 
 
+class epikv_weights(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("stride_seq", C.c_int64), ("stride_head", C.c_int64)]
+    shape = None    # of the tensor that weights_view() described: (sequences, heads, slots)
+
+
 _P = C.c_void_p
 _I = C.c_int32
+_WEIGHTS = C.POINTER(epikv_weights)
 _ROWS, _KV, _ROPE = C.POINTER(epikv_rows), C.POINTER(epikv_kv_view), C.POINTER(epikv_rope_view)
 _SIGS = {
     "epikv_workspace_bytes": (C.c_size_t, [C.POINTER(epikv_config)]),
@@ -98,6 +105,9 @@ _SIGS = {
     "epikv_rope": (C.c_int, [_P, _I, _I, _ROWS, _ROWS, _P, _ROPE, _I, _P]),
     "epikv_append": (C.c_int, [_P, _I, _I, _P, _P, _I, _P, _I, _P, _ROWS, _ROWS, _ROWS, _ROWS, _ROPE, _KV, _P]),
     "epikv_attention": (C.c_int, [_P, _I, _I, _P, _P, _I, _P, _I, _I, _ROWS, _ROWS, _P, _KV, _P]),
+    "epikv_attention_chunk": (C.c_int, [_P, _I, _I, _P, _P, _I, _P, _I, _I, _ROWS, _ROWS, _P, _KV, _P]),
+    "epikv_attention_weights": (C.c_int, [_P, _I, _I, _P, _P, _I, _P, _I, _I, _I, _ROWS, _P, _I, _WEIGHTS, _KV, _P]),
+    "epikv_weigh": (C.c_int, [_P, _I, _P, _WEIGHTS, _I, C.c_float, _P]),
     "epikv_cache_read": (C.c_int, [_P, _I, _I, _P, _P, _ROWS, _ROWS, _KV, _P]),
     "epikv_attn_get_error": (C.c_int, [_P, C.POINTER(_I)]),
     "epikv_attn_destroy": (None, [_P]),
@@ -229,6 +239,22 @@ def rows(t):
     return r
 
 
+def weights_view(t):
+    """A number for every slot and KV head, as epikv_attention_weights fills them and epikv_weigh reads them: a float32
+    tensor [sequences, heads, slots], slots contiguous.  It describes memory: the tensor is the caller's to keep."""
+    if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] != 1) or str(t.dtype) != "torch.float32":
+        raise ValueError(f"weights are float32 [sequences, heads, slots], slots contiguous: got {t.dtype} {tuple(t.shape)}, "
+                         f"strides {t.stride()}")
+    w = epikv_weights(t.data_ptr(), t.stride(0), t.stride(1))
+    w.shape = tuple(t.shape)
+    return w
+
+
+def _check_weights(what, w, seqs, heads, slots):
+    if w is not None and w.shape is not None and any(a < b for a, b in zip(w.shape, (seqs, heads, slots))):
+        raise ValueError(f"{what} takes weights of {seqs} sequences or more, {heads} heads, {slots} slots: got {w.shape}")
+
+
 def _heads(ctx):
     """(query heads, KV heads, channels) of a context made by epikv_attn_init; of a bare handle nothing is known."""
     return getattr(ctx, "heads", (0, 0, 0))
@@ -265,6 +291,7 @@ def epikv_init(cfg, workspace, workspace_bytes, stream=None):
     _check(load().epikv_init(C.byref(ctx), C.byref(cfg), _ptr(workspace), workspace_bytes, _stream(stream)),
            "epikv_init")
     ctx.score_kinds = cfg.score_kinds
+    ctx.slots = (cfg.max_seqs, cfg.max_cache_tokens)
     return ctx
 
 
@@ -278,6 +305,15 @@ def epikv_score_update(ctx, n_seq, seq_ids, cu_new, max_new, hidden, kv, stream=
                                      C.byref(hidden) if hidden is not None else None,
                                      C.byref(kv) if kv is not None else None, _stream(stream)),
            "epikv_score_update")
+
+
+def epikv_weigh(ctx, n_seq, seq_ids, weights, decay=1.0, *, n_heads=None, stream=None):
+    """weights: weights_view(...); n_heads: the heads that count (all that the view has)."""
+    if n_heads is None:
+        n_heads = weights.shape[1]
+    seqs, slots = getattr(ctx, "slots", (0, 0))
+    _check_weights("epikv_weigh", weights, seqs, n_heads, slots)
+    _check(load().epikv_weigh(ctx, n_seq, _ptr(seq_ids), weights, n_heads, decay, _stream(stream)), "epikv_weigh")
 
 
 def epikv_select(ctx, n_seq, seq_ids, budget, trigger, kept, kept_stride, n_kept, stream=None):
@@ -408,6 +444,7 @@ def epikv_attn_init(cfg, workspace, workspace_bytes, stream=None):
            "epikv_attn_init")
     ctx.heads = (cfg.num_heads, cfg.num_kv_heads, cfg.head_dim)     # what the calls take of their rows
     ctx.cache_format = cfg.cache_format
+    ctx.slots = (cfg.max_seqs, cfg.max_cache_tokens)
     return ctx
 
 
@@ -449,6 +486,29 @@ def epikv_attention(ctx, layer, n_seq, seq_ids, cu_new, max_new, length, q, out,
     _check(load().epikv_attention(ctx, layer, n_seq, _ptr(seq_ids), _ptr(cu_new), max_new, _ptr(length), len_stride,
                                   1 if causal else 0, q, out, _ptr(lse), kv, _stream(stream)),
            "epikv_attention")
+
+
+def epikv_attention_chunk(ctx, layer, n_seq, seq_ids, cu_new, max_new, length, q, out, kv, *, lse=None, causal=True,
+                          len_stride=1, stream=None):
+    hq, _, dim = _heads(ctx)
+    _check_rows("epikv_attention_chunk", q, 0, hq, dim)
+    _check_rows("epikv_attention_chunk", out, 0, hq, dim)
+    _check_format("epikv_attention_chunk", ctx, kv)
+    _check(load().epikv_attention_chunk(ctx, layer, n_seq, _ptr(seq_ids), _ptr(cu_new), max_new, _ptr(length), len_stride,
+                                        1 if causal else 0, q, out, _ptr(lse), kv, _stream(stream)),
+           "epikv_attention_chunk")
+
+
+def epikv_attention_weights(ctx, layer, n_seq, seq_ids, cu_new, max_new, length, q, lse, weights, kv, *, causal=True,
+                            last=0, add=False, len_stride=1, stream=None):
+    """lse: what the attention call gave; weights: weights_view(...)."""
+    hq, h, dim = _heads(ctx)
+    _check_rows("epikv_attention_weights", q, 0, hq, dim)
+    _check_weights("epikv_attention_weights", weights, getattr(ctx, "slots", (0, 0))[0], h, getattr(ctx, "slots", (0, 0))[1])
+    _check_format("epikv_attention_weights", ctx, kv)
+    _check(load().epikv_attention_weights(ctx, layer, n_seq, _ptr(seq_ids), _ptr(cu_new), max_new, _ptr(length), len_stride,
+                                          1 if causal else 0, last, q, _ptr(lse), 1 if add else 0, weights, kv,
+                                          _stream(stream)), "epikv_attention_weights")
 
 
 def epikv_cache_read(ctx, layer, n_rows, seqs, slots, k, v, kv, stream=None):

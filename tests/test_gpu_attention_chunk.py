@@ -1,0 +1,281 @@
+"""epikv_attention_chunk against float64: head layouts, chunks of one token to hundreds, ragged batches, pages that end
+inside a tile, rows that see nothing, what stands in slots that a row does not see, strides, streams and graphs."""
+import math
+
+import pytest
+import torch
+
+from paper_2606_26472_gb300 import epikv as E
+
+from . import cache_ops as R
+from .chunk_ops import attend, check_attention, queries
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [(8, 32, 128), (1, 1, 64), (1, 8, 128), (2, 14, 128), (3, 3, 64), (4, 32, 64), (5, 20, 128), (2, 4, 256),
+          (4, 32, 256), (11, 11, 64), (1, 71, 64)]
+OK = (E.EPIKV_OK, 0)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_one_tile(gpu_lib, bits, d):
+    """One tile of rows and of slots."""
+    c = R.Cache(seqs=1, T=256, H=1, d=d, bits=bits, seed=d)
+    ctx = c.context(1, 128)
+    q = queries(32, 1, d)
+    o, l = attend(c, ctx, q, [32], [0])
+    check_attention(c, q, o, l, [32], [0])
+    assert E.epikv_attn_get_error(ctx) == OK
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("H,Hq,d", SHAPES)
+def test_ragged_chunks(gpu_lib, bits, H, Hq, d):
+    new, held = [3, 0, 1, 17, 147, 8, 64], [0, 5, 200, 31, 77, 1500, 63]
+    for block in (16, 0, 7, 48):
+        c = R.Cache(seqs=7, T=1600, H=H, d=d, bits=bits, block=block, seed=H + d)
+        ctx = c.context(Hq, 200)
+        q = queries(sum(new), Hq, d)
+        seqs = [3, 0, 6, 1, 2, 5, 4]
+        o, l = attend(c, ctx, q, new, held, seqs=seqs)
+        check_attention(c, q, o, l, new, held, seqs=seqs, what=f"block {block}")
+        assert E.epikv_attn_get_error(ctx) == OK
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("H,Hq,d", [(8, 32, 128), (1, 1, 64), (2, 4, 256)])
+def test_single_tokens(gpu_lib, bits, H, Hq, d):
+    held = [0, 1, 14, 15, 16, 63, 64, 65, 126, 127, 128, 129, 300, 1023]
+    c = R.Cache(seqs=14, T=1030, H=H, d=d, bits=bits, seed=H * d)
+    ctx = c.context(Hq, 1)
+    q = queries(14, Hq, d)
+    o, l = attend(c, ctx, q, [1] * 14, held)
+    check_attention(c, q, o, l, [1] * 14, held)
+    assert E.epikv_attn_get_error(ctx) == OK
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("H,Hq,d", [(2, 8, 128), (1, 2, 64), (1, 1, 256), (2, 32, 128)])
+def test_prompts(gpu_lib, bits, H, Hq, d):
+    """Whole prompts, pieces behind held slots, and one long cache."""
+    new, held = [700, 300, 1, 33], [0, 900, 9000, 4001]
+    c = R.Cache(seqs=4, T=9100, H=H, d=d, bits=bits, seed=5)
+    ctx = c.context(Hq, 700)
+    q = queries(sum(new), Hq, d)
+    o, l = attend(c, ctx, q, new, held)
+    check_attention(c, q, o, l, new, held)
+    assert E.epikv_attn_get_error(ctx) == OK
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_prefix_without_the_new_tokens(gpu_lib, bits):
+    """causal=0: every query sees the held slots; none held: zeros and -inf."""
+    c = R.Cache(seqs=3, T=400, H=2, d=64, bits=bits, seed=2)
+    ctx = c.context(6, 90)
+    new, held = [5, 90, 3], [0, 399, 18]
+    q = queries(98, 6, 64)
+    o, l = attend(c, ctx, q, new, held, causal=False)
+    check_attention(c, q, o, l, new, held, causal=False)
+    assert not o[:5].any() and bool((l[:5] == -math.inf).all())
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("H,Hq,d", [(2, 8, 128), (1, 1, 64), (1, 4, 256)])
+@pytest.mark.parametrize("new", [1, 40, 150])
+def test_unseen_slots_do_not_reach_a_row(gpu_lib, bits, H, Hq, d, new):
+    """From some slot on the cache holds NaN: rows that do not see it are as in the clean cache bit for bit, rows that see it
+    are NaN."""
+    held, T = 45, 256
+    c = R.Cache(seqs=1, T=T, H=H, d=d, bits=bits, seed=3)
+    ctx = c.context(Hq, 160)
+    q = queries(new, Hq, d)
+    clean, lclean = attend(c, ctx, q, [new], [held])
+    for first in sorted({held + new, held + new // 2 + 1, held + 1}):
+        raw = [c.raw(w).clone() for w in (0, 1)]
+        rows = c.index(0, 0, torch.arange(first, T))
+        for w in (0, 1):
+            c.raw(w)[rows] = 0x7F if bits == 4 else torch.tensor([0xC0, 0x7F], dtype=torch.uint8,
+                                                                 device="cuda").repeat(c.units)
+        o, l = attend(c, ctx, q, [new], [held])
+        n = min(new, max(0, first - held))
+        assert torch.equal(o[:n], clean[:n]) and torch.equal(l[:n], lclean[:n])
+        assert bool(o[n:].isnan().all())
+        for w in (0, 1):
+            c.raw(w).copy_(raw[w])
+
+
+@pytest.mark.parametrize("H,Hq,d", [(1, 4, 128), (2, 2, 64), (1, 3, 256)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_infinite_values(gpu_lib, H, Hq, d, sign):
+    """An infinite value is the output of the rows that see it, in its channel alone."""
+    held, new = 100, 70
+    c = R.Cache(seqs=1, T=200, H=H, d=d, seed=4)
+    ctx = c.context(Hq, 70)
+    q = queries(new, Hq, d)
+    clean, _ = attend(c, ctx, q, [new], [held])
+    for slot in (3, 100, 131, 169):
+        row, ch = int(c.index(0, 0, [slot])[0]), slot % d
+        pool = c.c.v.view(-1, H, d)
+        keep = pool[row, H - 1, ch].clone()
+        pool[row, H - 1, ch] = sign * math.inf
+        o, _ = attend(c, ctx, q, [new], [held])
+        pool[row, H - 1, ch] = keep
+        sees = torch.arange(new, device="cuda") + held >= slot
+        mine = torch.zeros(new, Hq, d, dtype=torch.bool, device="cuda")
+        mine[sees, Hq - Hq // H:, ch] = True
+        assert bool((o[mine] == sign * math.inf).all())
+        assert torch.equal(o[~mine], clean[~mine])
+
+
+def test_scores_of_minus_infinity(gpu_lib):
+    """Keys of -inf beside queries above 0: rows whose every score is -inf give zeros and -inf."""
+    c = R.Cache(seqs=1, T=300, H=1, d=64, seed=6)
+    ctx = c.context(2, 64)
+    q = queries(64, 2, 64)
+    q[:, :, 5] = q[:, :, 5].abs() + 0.5
+    q[:, 1, 5] = -q[:, 1, 5]                        # the other head's scores are +inf
+    pool = c.c.k.view(-1, 64)
+    pool[c.index(0, 0, torch.arange(0, 210)), 5] = -math.inf
+    o, l = attend(c, ctx, q, [64], [180])
+    assert not o[:30, 0].any() and bool((l[:30, 0] == -math.inf).all())
+    assert bool(o[30:, 0].isfinite().all()) and bool(l[30:, 0].isfinite().all())
+    assert bool(o[:, 1].isnan().all())
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("mag", [2.0 ** -60, 1e-3, 30.0, 2.0 ** 20])
+def test_query_magnitudes(gpu_lib, bits, mag):
+    """Maxima that grow along the slots and queries far from 1; scores up to the millions stay exact enough."""
+    c = R.Cache(seqs=1, T=800, H=2, d=128, bits=bits, seed=7)
+    ctx = c.context(4, 80, softmax_scale=0.09 / mag if mag > 1 else 0.0)
+    q = (queries(80, 4, 128).float() * mag).to(torch.bfloat16)
+    o, l = attend(c, ctx, q, [80], [700])
+    check_attention(c, q, o, l, [80], [700], scale=0.09 / mag if mag > 1 else None)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_growing_maxima(gpu_lib, bits):
+    """Each tile's scores are far above the last one's, so that sums are rescaled in every tile."""
+    c = R.Cache(seqs=1, T=1024, H=1, d=64, bits=bits, seed=8)
+    x = torch.randn(1024, 1, 64, generator=torch.Generator(device="cuda").manual_seed(9), device="cuda") * 0.1
+    x += torch.arange(1024, device="cuda")[:, None, None] / 64.0
+    flat = torch.zeros_like(c.raw(0)).view(torch.bfloat16)
+    order = c.index(0, 0, torch.arange(1024))
+    if bits == 16:
+        flat[order] = x.to(torch.bfloat16).view(1024, 64)
+        c.raw(0).copy_(flat.view(torch.uint8))
+    else:
+        c.raw(0)[order] = R.pack(x.to(torch.bfloat16), c.units)
+    ctx = c.context(1, 130)
+    q = queries(130, 1, 64).abs()
+    o, l = attend(c, ctx, q, [130], [890])
+    check_attention(c, q, o, l, [130], [890])
+
+
+def test_head_scales(gpu_lib):
+    ks = torch.tensor([[[0.01, 3.0], [1.0, 0.5]], [[20.0, 0.125], [1e-3, 1.0]]], device="cuda")
+    c = R.Cache(seqs=2, T=300, H=2, d=64, bits=4, layers=2, kv_scale=ks, seed=10)
+    ctx = c.context(4, 60)
+    q = queries(90, 4, 64)
+    for layer in (0, 1):
+        o, l = attend(c, ctx, q, [30, 60], [200, 100], layer=layer)
+        check_attention(c, q, o, l, [30, 60], [200, 100], layer=layer)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_strided_rows_streams_and_graphs(gpu_lib, bits):
+    """Rows out of wider ones, a length array with a stride, another stream, and a graph replayed with other lengths."""
+    c = R.Cache(seqs=3, T=700, H=2, d=128, bits=bits, seed=11)
+    ctx = c.context(8, 64)
+    wide = queries(100, 14, 128)
+    q, buf = wide[:, 3:11], torch.zeros(100, 11, 128, dtype=torch.bfloat16, device="cuda")
+    out = buf[:, 2:10]
+    lse = torch.zeros(100, 8, device="cuda")
+    lens = torch.zeros(3, 5, dtype=torch.int32, device="cuda")
+    seq_ids, cu, _ = R.batch([40, 10, 50], [0, 0, 0])
+    cases = ([300, 0, 11], [77, 600, 128])
+    s = torch.cuda.Stream()
+    call = lambda: E.epikv_attention_chunk(ctx, 0, 3, seq_ids, cu, 64, lens[:, 2:], E.rows(q), E.rows(out), c.c.view(),  # noqa: E731
+                                           lse=lse, len_stride=5)
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        lens[:, 2] = torch.tensor(cases[0], dtype=torch.int32, device="cuda")
+        call()
+        check_attention(c, q.contiguous(), out, lse, [40, 10, 50], cases[0])
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            call()
+        for held in cases:
+            lens[:, 2] = torch.tensor(held, dtype=torch.int32, device="cuda")
+            out.zero_()
+            g.replay()
+            check_attention(c, q.contiguous(), out, lse, [40, 10, 50], held)
+    torch.cuda.current_stream().wait_stream(s)
+    assert not buf[:, :2].any() and not buf[:, 10:].any()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_repeated_calls_agree(gpu_lib, bits):
+    """The same call gives the same bits, whatever else was computed between."""
+    c = R.Cache(seqs=4, T=3000, H=2, d=128, bits=bits, seed=12)
+    ctx = c.context(8, 200)
+    new, held = [200, 1, 64, 130], [2000, 2999, 0, 777]
+    q = queries(sum(new), 8, 128)
+    first = attend(c, ctx, q, new, held)
+    for _ in range(3):
+        attend(c, ctx, q[:64], [64], [100])
+        again = attend(c, ctx, q, new, held)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_offsets_past_32_bits(gpu_lib):
+    """A contiguous cache of more than 2^32 bytes, its last sequence's slots far behind that."""
+    S, T, H, d = 5, 262144, 8, 128
+    c = R.Cache(seqs=1, T=16, H=H, d=d, block=0)
+    k = torch.zeros(S * T, H, d, dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    g = torch.Generator(device="cuda").manual_seed(13)
+    held, new = 1000, 40
+    lo = (S - 1) * T
+    for x in (k, v):
+        x[lo:lo + held + new] = torch.randn(held + new, H, d, generator=g, device="cuda").to(torch.bfloat16)
+    cfg = E.make_attn_config(max_seqs=S, max_cache_tokens=T, max_new_tokens=new, num_layers=1, num_heads=16, num_kv_heads=H,
+                             head_dim=d)
+    ws = torch.empty(E.epikv_attn_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+    ctx = E.epikv_attn_init(cfg, ws, ws.numel())
+    kv = E.kv_view(k, v, stride_layer=0, stride_seq=T * H * d, stride_token=H * d)
+    q = queries(new, 16, d)
+    o, l = torch.empty_like(q), torch.empty(new, 16, device="cuda")
+    seq_ids, cu, ln = R.batch([new], [held], [S - 1])
+    E.epikv_attention_chunk(ctx, 0, 1, seq_ids, cu, new, ln, E.rows(q), E.rows(o), kv, lse=l)
+    ref = R.attention64(q, k[lo:lo + held + new].double(), v[lo:lo + held + new].double(), [held + i + 1 for i in range(new)],
+                        d ** -0.5)
+    assert float((o.double() - ref[0]).abs().max()) <= float(((2.0 ** -8) * 2.1 * ref[2]).max())
+    assert E.epikv_attn_get_error(ctx) == OK
+
+
+def test_reported_and_skipped(gpu_lib):
+    """Entries that cannot be taken are reported and leave their rows; the others are as without them."""
+    c = R.Cache(seqs=4, T=256, H=2, d=64, seed=14)
+    ctx = c.context(4, 32)
+    q = queries(64, 4, 64)
+    good, lgood = attend(c, ctx, q, [32, 32], [100, 50], seqs=[0, 3])
+    for seqs, held, code in (([0, 9], [100, 50], E.EPIKV_DEV_BATCH), ([0, -1], [100, 50], E.EPIKV_DEV_BATCH),
+                             ([0, 3], [100, 225], E.EPIKV_DEV_CAPACITY), ([0, 3], [100, -1], E.EPIKV_DEV_CAPACITY)):
+        o, l = attend(c, ctx, q, [32, 32], held, seqs=seqs)
+        assert E.epikv_attn_get_error(ctx) == (E.EPIKV_EDEVICE, code)
+        assert torch.equal(o[:32], good[:32]) and torch.equal(l[:32], lgood[:32])
+        assert bool(o[32:].isnan().all())
+    # a block that the pool does not have: its slots are rows of zeros
+    table = c.c.block_table.clone()
+    table[0, 2] = c.c.num_blocks
+    seq_ids, cu, ln = R.batch([32], [100], [0])
+    o, l = torch.empty_like(q[:32]), torch.empty(32, 4, device="cuda")
+    E.epikv_attention_chunk(ctx, 0, 1, seq_ids, cu, 32, ln, E.rows(q[:32]), E.rows(o), c.c.view(table), lse=l)
+    assert E.epikv_attn_get_error(ctx) == (E.EPIKV_EDEVICE, E.EPIKV_DEV_SLOT)
+    k, v = c.read(0, 0, 0, 132), c.read(1, 0, 0, 132)
+    k[32:48], v[32:48] = 0, 0
+    ref = R.attention64(q[:32], k, v, [101 + i for i in range(32)], 0.125)
+    assert float((l.double() - ref[1]).abs().max()) < 1e-4
+    assert float((o.double() - ref[0]).abs().max()) <= float(((2.0 ** -8) * 2.1 * ref[2]).max())
