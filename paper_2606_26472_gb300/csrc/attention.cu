@@ -56,10 +56,9 @@
 // Far from its floor where an item's 8 to 32 rows read the cache anew: 8 x 64
 // tokens over 4,096 slots 270 us in bf16, 209 in 4 bits (floor 21 and 18), a
 // prompt of 4,096 tokens 1.36 ms (floor 0.07).
-#include <cuda.h>
-
 #include "attn.cuh"
 #include "attn_plan.h"
+#include "maps.cuh"
 
 namespace epikv {
 namespace {
@@ -1382,22 +1381,6 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttnState st, 
 // ------------------------------------------------------------------ host
 Geometry geometry(const AttnDims& dm, int n_seq, int max_new, bool causal) {
   return attn_geometry(dm.H, dm.rep, dm.d, dm.fmt == EPIKV_CACHE_E2M1, dm.units, dm.T, n_seq, max_new, causal);
-}
-
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encode_tiled() {
-  static const EncodeTiled fn = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess ||
-        found != cudaDriverEntryPointSuccess)
-      p = nullptr;
-    return reinterpret_cast<EncodeTiled>(p);
-  }();
-  return fn;
 }
 
 // The layer's K and V as tensors, where their layout allows it.

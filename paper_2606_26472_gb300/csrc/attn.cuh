@@ -23,6 +23,7 @@ struct AttnState {
   const float* kv_scale;  // [2][L][H] or null (the caller's)
   float* part;            // partial results of split rows
   int32_t* plan;          // [max_seqs + 1] tiles before each entry
+  void* splits;           // [kAttnCtas] ChunkSplit: items of the chunk's attention that stand in several CTAs' shares
 };
 
 // A batch as the entry points take it.
@@ -120,7 +121,8 @@ cudaError_t launch_attention(const AttnState& st, const AttnDims& dm, int layer,
                              const Rows& q, const Rows& out, float* lse, const KvDev& kv, cudaStream_t stream);
 cudaError_t launch_attention_chunk(const AttnState& st, const AttnDims& dm, int layer, const Batch& ba, bool causal,
                                    const Rows& q, const Rows& out, float* lse, const KvDev& kv, cudaStream_t stream);
-cudaError_t chunk_prepare(const AttnDims& dm);
+cudaError_t chunk_prepare(const AttnDims& dm, bool* runs);
+size_t chunk_part_floats(const AttnDims& dm);
 cudaError_t launch_attention_weights(const AttnState& st, const AttnDims& dm, int layer, const Batch& ba, bool causal,
                                      int last, const Rows& q, const float* lse, bool add, float* w, int64_t stride_seq,
                                      int64_t stride_head, const KvDev& kv, cudaStream_t stream);

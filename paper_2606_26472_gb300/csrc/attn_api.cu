@@ -5,7 +5,7 @@
 #include <string.h>
 
 #include "attn.cuh"
-#include "attn_plan.h"
+#include "chunk_plan.h"
 
 using namespace epikv;
 
@@ -14,6 +14,7 @@ struct epikv_attn_ctx {
   AttnState st;
   cudaStream_t last_stream;
   bool attention_runs;   // false: this build's attention kernels cannot be launched; the other operators can
+  bool chunk_runs;       // the same of the chunk's attention
 };
 
 namespace {
@@ -81,7 +82,9 @@ size_t carve(const AttnDims& d, AttnState* st, char* base) {
   memset(st, 0, sizeof(*st));
   st->err = (int32_t*)take(4);
   st->plan = (int32_t*)take(((size_t)d.S + 1) * 4);
-  st->part = (float*)take(attention_part_floats(d) * 4);
+  st->splits = take(kAttnCtas * sizeof(ChunkSplit));
+  const size_t a = attention_part_floats(d), c = chunk_part_floats(d);   // the calls of a context follow one another
+  st->part = (float*)take((a > c ? a : c) * 4);
   return align_up(off, 256);
 }
 
@@ -136,15 +139,8 @@ bool valid_cache(const AttnDims& dm, int layer, const epikv_kv_view* kv, KvDev* 
   return true;
 }
 
-// Rows of T slots for every sequence and head, none of which meets another.
 bool valid_weights(const epikv_weights* w, int S, int H, int T) {
-  if (!w || !w->ptr || ((uintptr_t)w->ptr & 3u) || w->stride_seq < 0 || w->stride_head < 0) return false;
-  const int64_t lo = S > 1 && (H == 1 || w->stride_seq < w->stride_head) ? w->stride_seq : w->stride_head;
-  if (S == 1 && H == 1) return true;
-  if (lo < T) return false;
-  if (S == 1 || H == 1) return true;
-  const int64_t n = lo == w->stride_seq ? S : H, hi = lo == w->stride_seq ? w->stride_head : w->stride_seq;
-  return hi / lo >= n || (hi - T) / lo >= n - 1;
+  return w && w->ptr && !((uintptr_t)w->ptr & 3u) && weights_apart(S, H, T, w->stride_seq, w->stride_head);
 }
 
 epikv_status cuda_status(cudaError_t e) { return e == cudaSuccess ? EPIKV_OK : EPIKV_ECUDA; }
@@ -194,7 +190,7 @@ epikv_status epikv_attn_init(epikv_attn_ctx** out, const epikv_attn_config* cfg,
   ctx->st.kv_scale = cfg->kv_scale;
   ctx->last_stream = stream;
   cudaError_t e = attention_prepare(dm, &ctx->attention_runs);
-  if (e == cudaSuccess) e = chunk_prepare(dm);
+  if (e == cudaSuccess) e = chunk_prepare(dm, &ctx->chunk_runs);
   if (e == cudaSuccess) e = weights_prepare(dm);
   if (e == cudaSuccess) e = cudaMemsetAsync(ctx->st.err, 0, 4, stream);
   if (e != cudaSuccess) {
@@ -292,6 +288,7 @@ epikv_status epikv_attention_chunk(epikv_attn_ctx* ctx, int32_t layer, int32_t n
   if (!valid_rows(q, &qr) || !valid_rows(out, &yr) || q->type != EPIKV_TYPE_BF16 || out->type != EPIKV_TYPE_BF16)
     return EPIKV_EINVAL;
   if (((uintptr_t)d_lse & 3u) || !valid_cache(ctx->dm, layer, kv, &kd)) return EPIKV_EINVAL;
+  if (!ctx->chunk_runs) return EPIKV_ECUDA;
   ctx->last_stream = stream;
   return cuda_status(launch_attention_chunk(ctx->st, ctx->dm, layer, ba, causal, qr, yr, d_lse, kd, stream));
 }

@@ -3,12 +3,15 @@
 //
 //   out = sum_j p_j v_j / sum_j p_j,   p_j = 2^(c q.k_j - m),   c = scale log2(e)
 //
-// A query row is a token and one of the rep query heads that share a KV head;
-// a CTA takes up to 256 such rows of one entry and KV head, as one or two
-// tiles of 128, and goes over the slots that they see in tiles of 128 (64 at
-// 256 channels).  S = Q K^T and O += P V run on tcgen05 with S and O in tensor
+// A query row is a token and one of the rep query heads that share a KV head.
+// An item is up to 256 such rows of one entry and KV head, as one or two tiles
+// of 128; it goes over the slots that its rows see in tiles of 128 (64 at 256
+// channels).  S = Q K^T and O += P V run on tcgen05 with S and O in tensor
 // memory; a thread owns a row, so maxima and sums need no exchange; P replaces
-// S in tensor memory, in 16 bits.
+// S in tensor memory, in 16 bits.  One CTA an SM takes an equal share of all
+// items' tiles (chunk_plan.h); items that several CTAs hold a segment of are
+// joined by a second kernel in the order of the slots.
+#include "chunk_plan.h"
 #include "tensor.cuh"
 
 namespace epikv {
@@ -17,6 +20,11 @@ namespace {
 constexpr int kChunkThreads = 384;      // 8 warps own rows, one issues products, three copy
 constexpr int kCopyThreads = 96;
 constexpr float kSlack = 8.f;           // a maximum is moved when a score passes it by 2^8
+// The warps exchange registers: launched with kLaunchRegs each, the owners of rows take more from the others.
+constexpr int kLaunchRegs = 168, kOtherRegs = 104;
+constexpr int owner_regs(int tiles) { return tiles == 2 ? 200 : 232; }
+static_assert(2 * owner_regs(2) + kOtherRegs <= 3 * kLaunchRegs && owner_regs(1) + 2 * kOtherRegs <= 3 * kLaunchRegs,
+              "the owners would wait for registers that nobody gives");
 
 template <int D>
 struct ChunkShape {
@@ -27,28 +35,187 @@ struct ChunkShape {
   static constexpr int kStages = D == 64 ? 8 : 4;
 };
 
-template <int D, int kTiles>
+// A CTA's piece of an item.
+struct Segment {
+  Entry e;
+  int b, kh;
+  int row0, rows;    // the item's first query row of that KV head, rows
+  int t0, t1;        // tiles of slots
+  int least, most;   // slots that the item's first row sees, and its last
+  bool first, last;  // the item starts, ends here
+  unsigned end;      // the line's tile behind the item
+};
+
+// Where a CTA's share starts: entry, KV head, block, and the line's tile that the block starts at.
+struct ShareStart {
+  int b, kh, block;
+  unsigned at;
+};
+
+// A warp's walk along its CTA's share, in shared memory: its first lane moves it on, and what the loops over tiles do not
+// need stays out of their registers.  Segment i stands in now[i & 1] while the next one is looked at.
+struct WarpWalk {
+  ShareStart here;
+  unsigned x;          // the share's next tile
+  Entry e;
+  Segment now[2];
+};
+
+struct SegmentWalk {
+  WarpWalk* w;
+  const unsigned* pre;   // [n_seq + 1] tiles before each entry
+  const Batch& ba;
+  const ChunkPlan& plan;
+  unsigned end;          // of the share
+  int lane;
+  __device__ __forceinline__ void begin(const ShareStart& start, unsigned x) const {
+    if (lane == 0) {
+      w->here = start;
+      w->x = x;
+      entry();
+    }
+    __syncwarp();
+  }
+  __device__ __forceinline__ void entry() const {
+    const int b = w->here.b;
+    Entry e;
+    e.tok0 = ba.cu_new[b];
+    e.n = ba.cu_new[b + 1] - e.tok0;
+    e.seq = ba.seq_ids[b];
+    e.len = ba.len[(int64_t)b * ba.len_stride];
+    w->e = e;
+  }
+  __device__ __forceinline__ void step(Segment* s) const {
+    const Entry e = w->e;
+    ShareStart h = w->here;
+    const unsigned x = w->x;
+    const unsigned tiles = (unsigned)block_tiles(plan, e.n, e.len, h.block), take = min(h.at + tiles, end) - x;
+    s->e = e;
+    s->b = h.b;
+    s->kh = h.kh;
+    s->row0 = h.block * plan.rows;
+    s->rows = min(e.n * plan.rep - s->row0, plan.rows);
+    s->least = row_sees(plan, e.len, s->row0);
+    s->most = block_sees(plan, e.n, e.len, h.block);
+    s->t0 = (int)(x - h.at);
+    s->t1 = min(s->t0 + (int)take, (s->most + plan.slots - 1) / plan.slots);
+    s->first = x == h.at;
+    s->last = x + take == h.at + tiles;
+    s->end = h.at + tiles;
+    w->x = x + take;
+    if (s->last) {
+      h.at += tiles;
+      if (++h.block == chunk_blocks(plan, e.n)) {
+        h.block = 0;
+        if (++h.kh == plan.heads) {
+          h.kh = 0;
+          if (w->x < end) {
+            do ++h.b;
+            while (pre[h.b + 1] == pre[h.b]);
+          }
+        }
+      }
+      w->here = h;
+      if (h.b != s->b) entry();
+    }
+  }
+  // The whole warp; false at the share's end.
+  __device__ __forceinline__ bool next(int i) const {
+    const bool more = w->x < end;
+    __syncwarp();
+    if (more && lane == 0) step(&w->now[i & 1]);
+    __syncwarp();
+    return more;
+  }
+  __device__ __forceinline__ const Segment& segment(int i) const { return w->now[i & 1]; }
+};
+
+template <int D>
 struct alignas(16) ChunkShared {
   static constexpr int kStages = ChunkShape<D>::kStages;
   uint64_t query, full[kStages], empty[kStages], scores[2], weights[2], sums, done;
   uint32_t tmem;
   int gave_up;
-  int unclean;                              // an infinite or NaN value stands in a slot that not all rows see
+  volatile int unclean[4];                  // 1 + the last segment with an infinite or NaN value in a slot that not all its rows see
   int64_t offset[2][ChunkShape<D>::kSlots]; // of a tile's slots, elements; -1: none
+  ShareStart start;
+  WarpWalk walk[kChunkThreads / 32];
+  ChunkSplit split;
 };
 
-struct ChunkItem {
-  Entry e;
-  int kh;          // KV head
-  int row0, rows;  // the item's first query row of that head, rows
-  int tiles;       // of slots
-  int least;       // slots that the item's first row sees
-  int most;        // and its last
-};
+// Tiles before each entry of the batch, by a warp; returns the items.  An entry that cannot be taken has none, nor has one
+// that takes the sum to kTooManyTiles and those behind it.
+__device__ __forceinline__ int64_t line_up(unsigned* pre, const Batch& ba, const AttnDims& dm, const ChunkPlan& plan,
+                                           int32_t* err, int lane) {
+  unsigned before = 0;
+  int64_t items = 0;
+  for (int b0 = 0; b0 < ba.n_seq; b0 += 32) {
+    const int b = b0 + lane;
+    Entry e;
+    unsigned n = 0;
+    int64_t it = 0;
+    if (b < ba.n_seq && batch_entry(ba, dm, b, plan.causal, err, &e)) {
+      n = count_of(head_tiles(plan, e.n, e.len) * plan.heads);
+      it = (int64_t)chunk_blocks(plan, e.n) * plan.heads;
+    }
+    unsigned upto = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto = add_counts(upto, v);
+      it += __shfl_xor_sync(0xffffffffu, it, o);
+    }
+    upto = add_counts(upto, before);
+    if (upto == kTooManyTiles && n) set_error(err, EPIKV_DEV_CAPACITY);
+    // the last sum below the limit stands for all entries behind it
+    const unsigned over = __ballot_sync(0xffffffffu, upto == kTooManyTiles);
+    const unsigned kept = __shfl_sync(0xffffffffu, upto, over ? max(__ffs(over) - 2, 0) : 31);
+    const unsigned good = over == 0 ? upto : over & 1 ? before : kept;
+    if (upto == kTooManyTiles) upto = good;
+    if (b < ba.n_seq) pre[b + 1] = upto;
+    before = __shfl_sync(0xffffffffu, upto, 31);
+    items += it;
+    if (over) {   // everything behind is refused too
+      for (int i = b0 + 32 + lane; i < ba.n_seq; i += 32) pre[i + 1] = before;
+      break;
+    }
+  }
+  if (lane == 0) pre[0] = 0;
+  return items;
+}
 
-// The slots that query row r sees.
-__device__ __forceinline__ int seen_of(const Entry& e, int rep, bool causal, int r) {
-  return causal ? e.len + r / rep + 1 : e.len;
+// Where in the line tile x is, by a warp.
+__device__ __forceinline__ void find_tile(ShareStart* start, unsigned x, const unsigned* pre, const Batch& ba, const ChunkPlan& plan,
+                                          int lane) {
+  int lo = 0, hi = ba.n_seq - 1;   // the entry with pre[b] <= x < pre[b + 1]
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (x < pre[mid + 1]) hi = mid;
+    else lo = mid + 1;
+  }
+  const int n = ba.cu_new[lo + 1] - ba.cu_new[lo], len = ba.len[(int64_t)lo * ba.len_stride];
+  const unsigned of_head = (pre[lo + 1] - pre[lo]) / (unsigned)plan.heads, kh = (x - pre[lo]) / of_head;
+  unsigned at = pre[lo] + kh * of_head;
+  const int blocks = chunk_blocks(plan, n);
+  int block = 0;
+  for (int b0 = 0; b0 < blocks; b0 += 32) {
+    const unsigned t = b0 + lane < blocks ? (unsigned)block_tiles(plan, n, len, b0 + lane) : 0u;
+    unsigned upto = t;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += v;
+    }
+    const unsigned behind = __ballot_sync(0xffffffffu, at + upto > x);
+    if (behind) {
+      const int k = __ffs(behind) - 1;
+      block = b0 + k;
+      at += __shfl_sync(0xffffffffu, upto - t, k);
+      break;
+    }
+    at += __shfl_sync(0xffffffffu, upto, 31);
+  }
+  if (lane == 0) *start = {lo, (int)kh, block, at};
 }
 
 // Element offset of each of the tile's slots, or -1.
@@ -74,114 +241,213 @@ __device__ __forceinline__ uint32_t bounded16(uint32_t w, uint32_t mask) {
   return w;
 }
 
-template <int D, int FMT, int kTiles>
-__device__ __forceinline__ void copy_tiles(char* ring, ChunkShared<D, kTiles>& sh, const TensorWaiter& wait,
-                                           const AttnDims& dm, const ChunkItem& it, const KvDev& kv, int layer,
-                                           int32_t* err, int tid) {
+// The copying warps.  A stage of the ring holds a tile's keys or its values, in turn; each warp arrives once when its part
+// of a stage is there.  Tiles whose slots all rows see come as tensor copies where the layer is a tensor; the others by
+// lanes, which also clear what no row sees.
+template <int D, int FMT>
+struct Copier {
   using Shape = ChunkShape<D>;
-  constexpr uint32_t kExp = FMT == EPIKV_CACHE_BF16 ? 0x7f80u : 0x7c00u;
-  constexpr int kLag = 2;   // stages whose copies are in flight
-  const int stages = 2 * it.tiles;
-  auto put_clean = [&](uint32_t at, uint4 v) {
+  static constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
+  static constexpr uint32_t kExp = kBf16 ? 0x7f80u : 0x7c00u;
+  static constexpr int kPer = kBf16 ? D / 8 : D / 32;     // 16-byte pieces of a head's row in the cache
+  enum { kMost = (Shape::kSlots * kPer + kCopyThreads - 1) / kCopyThreads, kLag = 2 };   // pieces of a thread; stages in flight
+  char* ring;
+  ChunkShared<D>& sh;
+  const TensorWaiter& wait;
+  const AttnDims& dm;
+  const KvDev& kv;
+  const LayerMaps& maps;
+  int layer;
+  int32_t* err;
+  int tid, lane, warp;
+
+  __device__ __forceinline__ uint32_t stage(int i) const { return smem_u32(ring + i % Shape::kStages * Shape::kStage); }
+  __device__ __forceinline__ void left(int i) const {
+    if (i >= Shape::kStages) wait(&sh.empty[i % Shape::kStages], (uint32_t)(i / Shape::kStages - 1) & 1);
+  }
+  __device__ __forceinline__ void put_clean(uint32_t at, const uint4& v, int seg) const {
     if (unbounded16(v.x, kExp) || unbounded16(v.y, kExp) || unbounded16(v.z, kExp) || unbounded16(v.w, kExp)) {
       sts16(at, make_uint4(bounded16(v.x, kExp), bounded16(v.y, kExp), bounded16(v.z, kExp), bounded16(v.w, kExp)));
-      sh.unclean = 1;
+      sh.unclean[seg & 3] = seg + 1;
     }
-  };
-  // stage i holds the keys (even) or values (odd) of tile i / 2
-  auto deliver = [&](int i) {
-    const int s0 = (i >> 1) * Shape::kSlots;
-    if ((i & 1) && s0 + Shape::kSlots > it.least) {
-      // A probability of 0 must not meet an infinity or a NaN in a slot that only other rows see: each thread looks
-      // through what it copied.
-      const uint32_t dst = smem_u32(ring + i % Shape::kStages * Shape::kStage);
-      constexpr int kPer = FMT == EPIKV_CACHE_BF16 ? D / 8 : D / 32;
+  }
+  // What this thread copied is there.  A probability of 0 must not meet an infinity or a NaN in a slot that only other rows
+  // see: of values that not all rows see each thread looks through its own.
+  __device__ __forceinline__ void deliver(int i, int which, int s0, const Segment& g, int seg) const {
+    if (which && s0 + Shape::kSlots > g.least) {
+      const uint32_t dst = stage(i);
       for (int x = tid; x < Shape::kSlots * kPer; x += kCopyThreads) {
         const int r = x / kPer, c = x % kPer;
-        if (s0 + r < it.least) continue;
-        if constexpr (FMT == EPIKV_CACHE_BF16) {
+        if (s0 + r < g.least) continue;
+        if constexpr (kBf16) {
           const uint32_t at = dst + (c >> 3) * Shape::kPanel + panel_at(r, c & 7);
-          put_clean(at, lds16(at));
+          put_clean(at, lds16(at), seg);
         } else {
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             const uint32_t at = dst + (c >> 1) * Shape::kPanel + panel_at(r, (c & 1) * 4 + u);
-            put_clean(at, lds16(at));
+            put_clean(at, lds16(at), seg);
           }
         }
       }
     }
     fence_proxy_async_smem();
-    mbar_arrive_one(&sh.full[i % Shape::kStages]);
-  };
-  for (int i = 0; i < stages; ++i) {
-    const int j = i >> 1, st = i % Shape::kStages, turn = i / Shape::kStages;
-    int64_t* offset = sh.offset[j & 1];
-    if (!(i & 1)) {
-      // the other tile's offsets may still be read; this one's are free since all threads were here for the last tile
-      tile_offsets(offset, Shape::kSlots, j * Shape::kSlots, it.most, kv, layer, it.e.seq, dm.T, err, tid, kCopyThreads);
+    __syncwarp();
+    if (lane == 0) mbar_arrive_one(&sh.full[i % Shape::kStages]);
+  }
+
+  __device__ __forceinline__ void bf16_segment(const Segment& g, int i0, int seg) const {
+    constexpr int kPanels = D / 64;
+    const int boxes = maps.slots ? Shape::kSlots / maps.slots * kPanels : 0;   // at most 32
+    const bool flat = kv.layout == EPIKV_LAYOUT_CONTIGUOUS;
+    const int panel = lane % kPanels, box = lane / kPanels;
+    int i = i0, pending = 0;
+    auto drain = [&] {
+      copy_wait<0>();
+      for (; pending > 0; --pending) {
+        const int k = i - pending - i0;
+        deliver(i - pending, k & 1, (g.t0 + (k >> 1)) * Shape::kSlots, g, seg);
+      }
+    };
+    for (int j = g.t0; j < g.t1; ++j) {
+      const int s0 = j * Shape::kSlots;
+      bool whole = maps.slots && s0 + Shape::kSlots <= g.least;
+      int y = s0 + box * maps.slots, z = g.e.seq;
+      if (whole) {
+        bool there = true;
+        if (!flat && lane < boxes) {
+          const int bi = y / kv.block_size;
+          y -= bi * kv.block_size;
+          z = bi < kv.max_blocks
+                  ? __ldg(kv.block_table + (int64_t)layer * kv.table_stride_layer + (int64_t)g.e.seq * kv.max_blocks + bi)
+                  : -1;
+          there = z >= 0 && z < kv.num_blocks;
+        }
+        whole = __all_sync(0xffffffffu, there);
+      }
+      if (whole) {
+        drain();
+#pragma unroll 1
+        for (int w = 0; w < 2; ++w, ++i) {
+          left(i);
+          uint64_t* bar = &sh.full[i % Shape::kStages];
+          if (warp == 0) {
+            if (lane == 0) mbar_arrive_expect_tx(bar, Shape::kStage);
+            __syncwarp();
+            if (lane < boxes)
+              tma_load_rows(stage(i) + panel * Shape::kPanel + box * maps.slots * 128, &maps.kv[w], g.kh * D + panel * 64, y, z,
+                            bar);
+          } else if (lane == 0) {
+            mbar_arrive_one(bar);
+          }
+          __syncwarp();
+        }
+        continue;
+      }
+      int64_t* offset = sh.offset[j & 1];   // all threads were here for the tile before, so this one's is free
+      tile_offsets(offset, Shape::kSlots, s0, g.most, kv, layer, g.e.seq, dm.T, err, tid, kCopyThreads);
       named_sync(1, kCopyThreads);
-    }
-    if (turn) wait(&sh.empty[st], (turn & 1) ^ 1);
-    const uint32_t dst = smem_u32(ring + st * Shape::kStage);
-    const char* base = kv.base[i & 1];
-    if constexpr (FMT == EPIKV_CACHE_BF16) {
-      constexpr int kPer = D / 8;
+#pragma unroll 1
+      for (int w = 0; w < 2; ++w) {
+        left(i);
+        const uint32_t dst = stage(i);
+        const char* base = kv.base[w];
 #pragma unroll 4
-      for (int x = tid; x < Shape::kSlots * kPer; x += kCopyThreads) {
-        const int r = x / kPer, c = x % kPer;
-        const int64_t o = offset[r];
-        copy_async16(dst + (c >> 3) * Shape::kPanel + panel_at(r, c & 7),
-                     base + (o < 0 ? 0 : (o + it.kh * D + c * 8) * 2), o < 0 ? 0 : 16);
-      }
-      copy_commit();
-      if (i >= kLag) {
-        copy_wait<kLag>();
-        deliver(i - kLag);
-      }
-    } else {
-      constexpr int kPer = D / 32;
-      constexpr int kMost = (Shape::kSlots * kPer + kCopyThreads - 1) / kCopyThreads;
-      uint4 codes[kMost];
-      uint32_t scales[kMost];
-#pragma unroll
-      for (int u = 0; u < kMost; ++u) {
-        const int x = tid + u * kCopyThreads, r = x / kPer, c = x % kPer;
-        codes[u] = make_uint4(0, 0, 0, 0);
-        scales[u] = 0;
-        const int64_t o = x < Shape::kSlots * kPer ? offset[r] : -1;
-        if (o >= 0) {
-          const char* row = base + o * 2;
-          codes[u] = *reinterpret_cast<const uint4*>(row + it.kh * (D / 2) + c * 16);
-          scales[u] = *reinterpret_cast<const uint16_t*>(row + scale_offset(dm, it.kh) + c * 2);
+        for (int x = tid; x < Shape::kSlots * kPer; x += kCopyThreads) {
+          const int r = x / kPer, c = x % kPer;
+          const int64_t o = offset[r];
+          copy_async16(dst + (c >> 3) * Shape::kPanel + panel_at(r, c & 7), base + (o < 0 ? 0 : (o + g.kh * D + c * 8) * 2),
+                       o < 0 ? 0 : 16);
+        }
+        copy_commit();
+        ++i;
+        if (++pending > kLag) {
+          copy_wait<kLag>();
+          const int k = i - pending - i0;
+          deliver(i - pending, k & 1, (g.t0 + (k >> 1)) * Shape::kSlots, g, seg);
+          --pending;
         }
       }
+    }
+    drain();
+    named_sync(1, kCopyThreads);   // the offsets are free for the next segment
+  }
+
+  struct Codes {
+    uint4 code[kMost];
+    uint32_t scale[kMost];
+  };
+  __device__ __forceinline__ void load_codes(Codes& c, int w, const int64_t* offset, int kh) const {
 #pragma unroll
-      for (int u = 0; u < kMost; ++u) {
-        const int x = tid + u * kCopyThreads, r = x / kPer, c = x % kPer;
-        if (x < Shape::kSlots * kPer) {
-          uint4 v[4];
-          expand32(codes[u], scales[u], v);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) sts16(dst + (c >> 1) * Shape::kPanel + panel_at(r, (c & 1) * 4 + k), v[k]);
-        }
+    for (int u = 0; u < kMost; ++u) {
+      const int x = tid + u * kCopyThreads, r = x / kPer, p = x % kPer;
+      c.code[u] = make_uint4(0, 0, 0, 0);
+      c.scale[u] = 0;
+      const int64_t o = x < Shape::kSlots * kPer ? offset[r] : -1;
+      if (o >= 0) {
+        const char* row = kv.base[w] + o * 2;
+        c.code[u] = *reinterpret_cast<const uint4*>(row + kh * (D / 2) + p * 16);
+        c.scale[u] = *reinterpret_cast<const uint16_t*>(row + scale_offset(dm, kh) + p * 2);
       }
-      deliver(i);
     }
   }
-  if constexpr (FMT == EPIKV_CACHE_BF16) {
-    if (stages >= 2) {
-      copy_wait<1>();
-      deliver(stages - 2);
+  __device__ __forceinline__ void put_codes(const Codes& c, int i) const {
+    left(i);
+    const uint32_t dst = stage(i);
+#pragma unroll
+    for (int u = 0; u < kMost; ++u) {
+      const int x = tid + u * kCopyThreads, r = x / kPer, p = x % kPer;
+      if (x < Shape::kSlots * kPer) {
+        uint4 v[4];
+        expand32(c.code[u], c.scale[u], v);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sts16(dst + (p >> 1) * Shape::kPanel + panel_at(r, (p & 1) * 4 + k), v[k]);
+      }
     }
-    copy_wait<0>();
-    if (stages >= 1) deliver(stages - 1);
   }
-}
+  // 4-bit rows: the next stage's codes are under way while this one's become halves.
+  __device__ __forceinline__ void q4_segment(const Segment& g, int i, int seg) const {
+    auto offsets = [&](int j) {
+      tile_offsets(sh.offset[j & 1], Shape::kSlots, j * Shape::kSlots, g.most, kv, layer, g.e.seq, dm.T, err, tid, kCopyThreads);
+      named_sync(1, kCopyThreads);
+    };
+    Codes k, v;
+    offsets(g.t0);
+    load_codes(k, 0, sh.offset[g.t0 & 1], g.kh);
+    for (int j = g.t0; j < g.t1; ++j, i += 2) {
+      load_codes(v, 1, sh.offset[j & 1], g.kh);
+      put_codes(k, i);
+      deliver(i, 0, j * Shape::kSlots, g, seg);
+      if (j + 1 < g.t1) {
+        offsets(j + 1);
+        load_codes(k, 0, sh.offset[(j + 1) & 1], g.kh);
+      }
+      put_codes(v, i + 1);
+      deliver(i + 1, 1, j * Shape::kSlots, g, seg);
+    }
+    named_sync(1, kCopyThreads);
+  }
+
+  __device__ __forceinline__ void run(const SegmentWalk& walk) const {
+    int i = 0;
+    for (int seg = 0, at = 0; walk.next(at); ++at) {
+      const Segment& g = walk.segment(at);
+      const int tiles = g.t1 - g.t0;
+      if (tiles <= 0) continue;
+      if constexpr (kBf16) bf16_segment(g, i, seg);
+      else q4_segment(g, i, seg);
+      i += 2 * tiles;
+      ++seg;
+    }
+    if (*wait.gave_up && warp == 0)   // the CTA may not end before its copies have landed
+      for (int k = max(0, i - Shape::kStages); k < i; ++k)
+        mbar_wait_bounded(&sh.full[k % Shape::kStages], (uint32_t)(k / Shape::kStages) & 1, kTensorWaitNs);
+  }
+};
 
 template <int D, int FMT, int kTiles>
-__device__ __forceinline__ void issue_products(uint32_t query, uint32_t ring, ChunkShared<D, kTiles>& sh,
-                                               const TensorWaiter& wait, int tiles, uint32_t tmem) {
+__device__ __forceinline__ void issue_products(uint32_t query, uint32_t ring, ChunkShared<D>& sh, const TensorWaiter& wait,
+                                               const SegmentWalk& walk, uint32_t tmem) {
   using Shape = ChunkShape<D>;
   constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
   constexpr uint32_t kScores = product_of(128, Shape::kSlots, kBf16, false), kSums = product_of(128, D, kBf16, true);
@@ -204,53 +470,66 @@ __device__ __forceinline__ void issue_products(uint32_t query, uint32_t ring, Ch
     wait(&sh.full[i % Shape::kStages], (uint32_t)(i / Shape::kStages) & 1);
     tensor_fence_after();
   };
-  wait(&sh.query, 0);
-  tensor_fence_after();
-  filled(0);
-  for (int t = 0; t < kTiles; ++t) scores(t, t, 0);
-  products_done(&sh.empty[0]);
-  for (int j = 0; j < tiles; ++j) {
-    const int v = (2 * j + 1) % Shape::kStages, k = (2 * j + 2) % Shape::kStages;
-    const bool more = j + 1 < tiles;
-    if constexpr (kTiles == 1) {   // two places for scores: the next tile's are formed beside this one's probabilities
-      if (more) {
-        filled(2 * j + 2);
-        scores(0, (j + 1) & 1, k);
-        products_done(&sh.empty[k]);
-      }
-      filled(2 * j + 1);
-      wait(&sh.weights[j & 1], (uint32_t)(j >> 1) & 1);
-      tensor_fence_after();
-      sums(0, j & 1, v, j > 0);
-      products_done(&sh.empty[v]);
-      products_done(&sh.sums);
+  // i: the tile's keys in the ring; a: tiles so far
+  for (int i = 0, a = 0, seg = 0, at = 0; walk.next(at); ++at) {
+    const int tiles = walk.segment(at).t1 - walk.segment(at).t0;
+    if (tiles <= 0) continue;
+    if (walk.lane) continue;
+    wait(&sh.query, (uint32_t)seg & 1);
+    tensor_fence_after();
+    filled(i);
+    if constexpr (kTiles == 1) {
+      scores(0, a & 1, i % Shape::kStages);
     } else {
-      filled(2 * j + 1);
-      if (more) filled(2 * j + 2);
-      for (int t = 0; t < 2; ++t) {
-        wait(&sh.weights[t], (uint32_t)j & 1);
-        tensor_fence_after();
-        sums(t, t, v, j > 0);
-        if (more) scores(t, t, k);   // in order behind the products that read the probabilities in its place
-      }
-      products_done(&sh.empty[v]);
-      if (more) products_done(&sh.empty[k]);
+      for (int t = 0; t < 2; ++t) scores(t, t, i % Shape::kStages);
     }
+    products_done(&sh.empty[i % Shape::kStages]);
+    for (int j = 0; j < tiles; ++j, i += 2, ++a) {
+      const int v = (i + 1) % Shape::kStages, k = (i + 2) % Shape::kStages;
+      const bool more = j + 1 < tiles;
+      if constexpr (kTiles == 1) {   // two places for scores: the next tile's are formed beside this one's probabilities
+        if (more) {
+          filled(i + 2);
+          scores(0, (a + 1) & 1, k);
+          products_done(&sh.empty[k]);
+        }
+        filled(i + 1);
+        wait(&sh.weights[a & 1], (uint32_t)(a >> 1) & 1);
+        tensor_fence_after();
+        sums(0, a & 1, v, j > 0);
+        products_done(&sh.empty[v]);
+        products_done(&sh.sums);
+      } else {
+        filled(i + 1);
+        if (more) filled(i + 2);
+        for (int t = 0; t < 2; ++t) {
+          wait(&sh.weights[t], (uint32_t)a & 1);
+          tensor_fence_after();
+          sums(t, t, v, j > 0);
+          if (more) scores(t, t, k);   // in order behind the products that read the probabilities in its place
+        }
+        products_done(&sh.empty[v]);
+        if (more) products_done(&sh.empty[k]);
+      }
+    }
+    products_done(&sh.done);
+    ++seg;
   }
-  products_done(&sh.done);
 }
 
+// The owners of rows: a segment's tiles, the first of them the CTA's tile `a`.
 template <int D, int FMT, int kTiles>
-__device__ __forceinline__ void soften(ChunkShared<D, kTiles>& sh, const TensorWaiter& wait, int tiles, int seen, float c,
+__device__ __forceinline__ void soften(ChunkShared<D>& sh, const TensorWaiter& wait, int t0, int t1, int a, int seen, float c,
                                        uint32_t tmem, int t, float* m_out, float* l_out) {
   using Shape = ChunkShape<D>;
   constexpr int N = Shape::kSlots;
+  constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
   float m = -INFINITY, l = 0.f;
   const uint32_t o = tmem + 256 + t * 128;
-  for (int j = 0; j < tiles; ++j) {
-    const int buf = kTiles == 1 ? j & 1 : t;
+  for (int j = t0; j < t1; ++j, ++a) {
+    const int buf = kTiles == 1 ? a & 1 : t;
     const uint32_t s = tmem + buf * 128;
-    wait(&sh.scores[buf], kTiles == 1 ? (uint32_t)(j >> 1) & 1 : (uint32_t)j & 1);
+    wait(&sh.scores[buf], kTiles == 1 ? (uint32_t)(a >> 1) & 1 : (uint32_t)a & 1);
     tensor_fence_after();
     uint32_t x[N];
 #pragma unroll
@@ -262,47 +541,55 @@ __device__ __forceinline__ void soften(ChunkShared<D, kTiles>& sh, const TensorW
       for (int i = 0; i < N; ++i)
         if (s0 + i >= seen) x[i] = 0xff800000u;
     }
-    float top = -INFINITY;
+    float top[4];
 #pragma unroll
-    for (int i = 0; i < N; ++i) top = fmaxf(top, __uint_as_float(x[i]));
-    top *= c;
-    const bool up = top > m + kSlack;
+    for (int i = 0; i < 4; ++i) top[i] = max3(__uint_as_float(x[i]), __uint_as_float(x[i + 4]), __uint_as_float(x[i + 8]));
+#pragma unroll
+    for (int i = 12; i + 7 < N; i += 8)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) top[u] = max3(top[u], __uint_as_float(x[i + u]), __uint_as_float(x[i + u + 4]));
+#pragma unroll
+    for (int u = 0; u < 4; ++u) top[u] = fmaxf(top[u], __uint_as_float(x[N - 4 + u]));
+    const float high = fmaxf(max3(top[0], top[1], top[2]), top[3]) * c;
+    const bool up = high > m + kSlack;
     if (__any_sync(0xffffffffu, up)) {
-      const float mul = !up ? 1.f : m == -INFINITY ? 0.f : exp2_fast(m - top);
-      if (up) m = top;
+      const float mul = !up ? 1.f : m == -INFINITY ? 0.f : exp2_fast(m - high);
+      if (up) m = high;
       l *= mul;
-      if (j > 0) {
+      if (j > t0) {
         if constexpr (kTiles == 1) {   // the last tile's products may still be under way
-          wait(&sh.sums, (uint32_t)(j - 1) & 1);
+          wait(&sh.sums, (uint32_t)(a - 1) & 1);
           tensor_fence_after();
         }
 #pragma unroll 1
-        for (int i = 0; i < D; i += 32) {
-          uint32_t y[32];
-          tmem_load32(o + i, y);
+        for (int i = 0; i < D; i += 16) {
+          uint32_t y[16];
+          tmem_load16(o + i, y);
           tmem_wait_load();
 #pragma unroll
-          for (int u = 0; u < 32; ++u) y[u] = __float_as_uint(__uint_as_float(y[u]) * mul);
-          tmem_store32(o + i, y);
+          for (int u = 0; u < 16; ++u) y[u] = __float_as_uint(__uint_as_float(y[u]) * mul);
+          tmem_store16(o + i, y);
         }
       }
     }
     // a half's range is used up to 2^15: below 2^-24 it has no bits left
-    const float base = (m == -INFINITY ? 0.f : m) - (FMT == EPIKV_CACHE_BF16 ? 0.f : 7.f);
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    const float base = (m == -INFINITY ? 0.f : m) - (kBf16 ? 0.f : 7.f);
+    const f32x2 cc = f2_pack(c, c), bb = f2_pack(-base, -base);
+    f32x2 sum[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
 #pragma unroll
     for (int i = 0; i < N; i += 32) {
       uint32_t y[16];
 #pragma unroll
       for (int u = 0; u < 32; u += 2) {
-        const float a = exp2_fast(__uint_as_float(x[i + u]) * c - base), b = exp2_fast(__uint_as_float(x[i + u + 1]) * c - base);
-        sum[u & 3] += a;
-        sum[(u & 3) + 1] += b;
-        y[u / 2] = FMT == EPIKV_CACHE_BF16 ? bf16_pair(a, b) : half_pair(a, b);
+        const f32x2 z = f2_fma(f2_pack(__uint_as_float(x[i + u]), __uint_as_float(x[i + u + 1])), cc, bb);
+        const float p = exp2_fast(f2_lo(z)), q = exp2_fast(f2_hi(z));
+        sum[u >> 1 & 1] = f2_add(sum[u >> 1 & 1], f2_pack(p, q));
+        y[u / 2] = kBf16 ? bf16_pair(p, q) : half_pair(p, q);
       }
       tmem_store16(s + i / 2, y);
     }
-    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    const f32x2 both = f2_add(sum[0], sum[1]);
+    l += f2_lo(both) + f2_hi(both);
     tmem_wait_store();
     tensor_fence_before();
     mbar_arrive_one(&sh.weights[buf]);
@@ -311,32 +598,90 @@ __device__ __forceinline__ void soften(ChunkShared<D, kTiles>& sh, const TensorW
   *l_out = l;
 }
 
+// A segment's results: of a whole item its rows' outputs, else a part for the second kernel (outputs by fours of channels,
+// row by row; maxima and sums behind them).
+template <int D, int FMT>
+__device__ __forceinline__ void put_rows(const AttnState& st, const AttnDims& dm, const Segment& g, const Rows& out, float* lse,
+                                         const KvDev& kv, int layer, float* part, int part_rows, uint32_t o, int row, float m,
+                                         float l, int seen, bool unclean) {
+  constexpr int N = ChunkShape<D>::kSlots;
+  constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
+  const bool live = row < g.rows;
+  const int r = g.row0 + row, token = r / dm.rep, hq = g.kh * dm.rep + r % dm.rep;
+  float mul = l == 0.f ? 0.f : 1.f / l;
+  if constexpr (!kBf16) mul *= head_scale(st, dm, 1, layer, g.kh);
+  if (part) mul = 1.f;
+  const bool none = l == 0.f;
+  const float shift = kBf16 ? 0.f : 7.f;   // of the exponentials
+  char* to = out.p + ((int64_t)(g.e.tok0 + token) * out.st + hq * out.sh) * 2;
+  const int from = max(g.least, g.t0 * N), upto = live && unclean ? min(seen, g.t1 * N) : 0;
+#pragma unroll 1
+  for (int i = 0; i < D; i += 32) {
+    uint32_t y[32];
+    if (g.t0 < g.t1) {
+      tmem_load32(o + i, y);
+      tmem_wait_load();
+    }
+#pragma unroll
+    for (int u = 0; u < 32; ++u) y[u] = none ? 0u : __float_as_uint(__uint_as_float(y[u]) * mul);
+    // what the copying warps took out of slots that not all rows see: an infinity is the output of the rows that see it
+#pragma unroll 1
+    for (int s = from; s < upto; ++s) {
+      const int64_t at = kv_row_offset(kv, layer, g.e.seq, s, dm.T);
+      if (at < 0) continue;
+      const char* v = kv.base[1] + at * 2;
+      if constexpr (kBf16) {
+#pragma unroll
+        for (int u = 0; u < 32; ++u) {
+          const uint32_t b = *reinterpret_cast<const uint16_t*>(v + (g.kh * D + i + u) * 2);
+          if ((b & 0x7f80u) == 0x7f80u) y[u] = __float_as_uint(__uint_as_float(y[u]) + __uint_as_float(b << 16));
+        }
+      } else {   // a scale of NaN
+#pragma unroll
+        for (int u = 0; u < 32; ++u)
+          if (((uint8_t)v[scale_offset(dm, g.kh) + (i + u) / kQuantGroup] & 0x7f) == 0x7f) y[u] = 0x7fc00000u;
+      }
+    }
+    if (!live) continue;
+    if (part) {
+#pragma unroll
+      for (int u = 0; u < 32; u += 4)
+        reinterpret_cast<uint4*>(part)[(int64_t)((i + u) / 4) * part_rows + row] = make_uint4(y[u], y[u + 1], y[u + 2], y[u + 3]);
+    } else {
+#pragma unroll
+      for (int u = 0; u < 32; u += 8)
+        *reinterpret_cast<uint4*>(to + (i + u) * 2) =
+            make_uint4(bf16_pair(__uint_as_float(y[u]), __uint_as_float(y[u + 1])),
+                       bf16_pair(__uint_as_float(y[u + 2]), __uint_as_float(y[u + 3])),
+                       bf16_pair(__uint_as_float(y[u + 4]), __uint_as_float(y[u + 5])),
+                       bf16_pair(__uint_as_float(y[u + 6]), __uint_as_float(y[u + 7])));
+    }
+  }
+  if (!live) return;
+  if (part) {
+    reinterpret_cast<float2*>(part + (int64_t)part_rows * D)[row] = make_float2(m - shift, l);
+  } else if (lse) {
+    lse[(int64_t)(g.e.tok0 + token) * dm.Hq + hq] = none ? -INFINITY : (m - shift + log2f(l)) * 0.69314718055994531f;
+  }
+}
+
 template <int D, int FMT, int kTiles>
 __global__ void __launch_bounds__(kChunkThreads, 1)
-    chunk_kernel(AttnState st, AttnDims dm, int layer, Batch ba, bool causal, Rows q, Rows out, float* lse, KvDev kv,
-                 float c) {
+    chunk_kernel(AttnState st, AttnDims dm, ChunkPlan plan, int layer, Batch ba, Rows q, Rows out, float* lse, KvDev kv,
+                 const __grid_constant__ LayerMaps maps, float c, int part_rows) {
   using Shape = ChunkShape<D>;
+  constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
   extern __shared__ char dynamic[];
   char* smem = dynamic + ((1024 - (smem_u32(dynamic) & 1023)) & 1023);
-  __shared__ ChunkShared<D, kTiles> sh;
+  __shared__ ChunkShared<D> sh;
   char* ring = smem + kTiles * Shape::kQuery;
-  const int tid = threadIdx.x, warp = tid >> 5;
-  pdl_wait();
-  pdl_trigger();
-  const int b = blockIdx.y;
-  ChunkItem it;
-  if (!batch_entry(ba, dm, b, causal, st.err, &it.e)) return;
-  it.kh = blockIdx.x % dm.H;
-  it.row0 = blockIdx.x / dm.H * (128 * kTiles);
-  it.rows = min(it.e.n * dm.rep - it.row0, 128 * kTiles);
-  if (it.rows <= 0) return;
-  it.least = seen_of(it.e, dm.rep, causal, it.row0);
-  it.most = seen_of(it.e, dm.rep, causal, it.row0 + it.rows - 1);
-  it.tiles = (it.most + Shape::kSlots - 1) / Shape::kSlots;
+  unsigned* pre = reinterpret_cast<unsigned*>(ring + Shape::kStages * Shape::kStage);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (warp == 8) tmem_alloc(&sh.tmem, 512);
   if (tid == 0) {
     mbar_init(&sh.query, 128 * kTiles);
     for (int i = 0; i < Shape::kStages; ++i) {
-      mbar_init(&sh.full[i], kCopyThreads);
+      mbar_init(&sh.full[i], 3);
       mbar_init(&sh.empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -345,122 +690,178 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     }
     mbar_init(&sh.sums, 1);
     mbar_init(&sh.done, 1);
-    sh.gave_up = sh.unclean = 0;
+    sh.gave_up = 0;
+    sh.split = {};
+    for (int i = 0; i < 4; ++i) sh.unclean[i] = 0;
     fence_barrier_init();
   }
-  if (warp == 0) tmem_alloc(&sh.tmem, 512);
+  pdl_wait();
+  pdl_trigger();
+  __shared__ int64_t items;
+  if (warp == 0) {
+    const int64_t n = line_up(pre, ba, dm, plan, st.err, lane);
+    if (lane == 0) items = n;
+    __syncwarp();
+    const unsigned total = pre[ba.n_seq];
+    const int ctas = chunk_ctas(total, n);
+    if ((int)blockIdx.x < ctas) find_tile(&sh.start, share_start(blockIdx.x, total, ctas), pre, ba, plan, lane);
+  }
   tensor_fence_before();
   __syncthreads();
   tensor_fence_after();
   const uint32_t tmem = sh.tmem;
-  const TensorWaiter wait{&sh.gave_up, st.err};
-  const int t = warp >> 2;
-  float m = -INFINITY, l = 0.f;
-  const int r = it.row0 + tid, token = r / dm.rep, hq = it.kh * dm.rep + r % dm.rep;
-  const bool live = tid < it.rows;   // of the threads that own rows
-  if (warp < 4 * kTiles) {
-    const uint4* src = live ? reinterpret_cast<const uint4*>(q.p + ((int64_t)(it.e.tok0 + token) * q.st + hq * q.sh) * 2) : nullptr;
-    float mul = store_query<D, FMT != EPIKV_CACHE_BF16>(smem_u32(smem + t * Shape::kQuery), 128 * 128, tid & 127, src);
-    if constexpr (FMT != EPIKV_CACHE_BF16) mul *= head_scale(st, dm, 0, layer, it.kh);
-    fence_proxy_async_smem();
-    mbar_arrive_one(&sh.query);
-    // rows that are not there see all slots of the tiles: their queries are 0
-    soften<D, FMT, kTiles>(sh, wait, it.tiles, live ? seen_of(it.e, dm.rep, causal, r) : INT_MAX, c * mul,
-                           tmem + ((uint32_t)(warp & 3) << 21), t, &m, &l);
-  } else if (warp == 8) {
-    if (tid == 256 && it.tiles > 0)
-      issue_products<D, FMT, kTiles>(smem_u32(smem), smem_u32(ring), sh, wait, it.tiles, tmem);
-    __syncwarp();
-  } else if (warp > 8) {
-    copy_tiles<D, FMT, kTiles>(ring, sh, wait, dm, it, kv, layer, st.err, tid - 288);
-  }
-  if (warp < 4 * kTiles && it.tiles > 0) wait(&sh.done, 0);
-  tensor_fence_after();
-  __syncthreads();
-  if (warp < 4 * kTiles) {
-    float mul = l == 0.f ? 0.f : 1.f / l;
-    if constexpr (FMT != EPIKV_CACHE_BF16) mul *= head_scale(st, dm, 1, layer, it.kh);
-    const uint32_t o = tmem + ((uint32_t)(warp & 3) << 21) + 256 + t * 128;
-    char* to = live ? out.p + ((int64_t)(it.e.tok0 + token) * out.st + hq * out.sh) * 2 : nullptr;
-    const int upto = live && sh.unclean ? seen_of(it.e, dm.rep, causal, r) : 0;
-#pragma unroll 1
-    for (int i = 0; i < D; i += 32) {
-      uint32_t y[32];
-      if (it.tiles > 0) {
-        tmem_load32(o + i, y);
-        tmem_wait_load();
-      }
-#pragma unroll
-      for (int u = 0; u < 32; ++u) y[u] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(y[u]) * mul);
-      // what the copying warps took out of slots that not all rows see: an infinity is the output of the rows that see it
-#pragma unroll 1
-      for (int s = it.least; s < upto; ++s) {
-        const int64_t at = kv_row_offset(kv, layer, it.e.seq, s, dm.T);
-        if (at < 0) continue;
-        const char* row = kv.base[1] + at * 2;
-        if constexpr (FMT == EPIKV_CACHE_BF16) {
-#pragma unroll
-          for (int u = 0; u < 32; ++u) {
-            const uint32_t v = *reinterpret_cast<const uint16_t*>(row + (it.kh * D + i + u) * 2);
-            if ((v & 0x7f80u) == 0x7f80u) y[u] = __float_as_uint(__uint_as_float(y[u]) + __uint_as_float(v << 16));
-          }
-        } else {   // a scale of NaN
-#pragma unroll
-          for (int u = 0; u < 32; ++u)
-            if (((uint8_t)row[scale_offset(dm, it.kh) + (i + u) / kQuantGroup] & 0x7f) == 0x7f) y[u] = 0x7fc00000u;
+  const unsigned total = pre[ba.n_seq];
+  const int cta = blockIdx.x, ctas = chunk_ctas(total, items);
+  if (cta < ctas) {
+    const TensorWaiter wait{&sh.gave_up, st.err};
+    const SegmentWalk walk{&sh.walk[warp], pre, ba, plan, share_start(cta + 1, total, ctas), lane};
+    walk.begin(sh.start, share_start(cta, total, ctas));
+    if (warp < 4 * kTiles) {
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(owner_regs(kTiles)));
+      const int t = warp >> 2;
+      const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
+      int seen = 0;
+      float factor = c;
+      auto take_query = [&](const Segment& g) {
+        const int r = g.row0 + tid, token = r / dm.rep, hq = g.kh * dm.rep + r % dm.rep;
+        const bool live = tid < g.rows;
+        // rows that are not there see all slots of the tiles: their queries are 0
+        seen = live ? row_sees(plan, g.e.len, r) : INT_MAX;
+        if (g.t0 >= g.t1) return;
+        const uint4* src = live ? reinterpret_cast<const uint4*>(q.p + ((int64_t)(g.e.tok0 + token) * q.st + hq * q.sh) * 2) : nullptr;
+        factor = c * store_query<D, !kBf16>(smem_u32(smem + t * Shape::kQuery), 128 * 128, tid & 127, src);
+        if constexpr (!kBf16) factor *= head_scale(st, dm, 0, layer, g.kh);
+        fence_proxy_async_smem();
+        mbar_arrive_one(&sh.query);
+      };
+      bool more = walk.next(0);
+      if (more) take_query(walk.segment(0));
+      for (int a = 0, seg = 0, at = 0; more; ++at) {
+        float m = -INFINITY, l = 0.f;
+        const int t0 = walk.segment(at).t0, t1 = walk.segment(at).t1, saw = seen;
+        bool unclean = false;
+        if (t0 < t1) {
+          soften<D, FMT, kTiles>(sh, wait, t0, t1, a, seen, factor, lanes, t, &m, &l);
+          wait(&sh.done, (uint32_t)seg & 1);
+          tensor_fence_after();
+          unclean = sh.unclean[seg & 3] == seg + 1;
+          a += t1 - t0;
+          ++seg;
         }
+        more = walk.next(at + 1);
+        if (more) take_query(walk.segment(at + 1));   // the next segment's first scores are formed beside this one's results
+        const Segment& now = walk.segment(at);
+        float* part = now.first && now.last ? nullptr
+                                            : st.part + (int64_t)(2 * cta + (now.first ? 1 : 0)) * part_rows * (D + 2);
+        put_rows<D, FMT>(st, dm, now, out, lse, kv, layer, part, part_rows, lanes + 256 + t * 128, tid, m, l, saw, unclean);
+        if (tid == 0 && now.first && !now.last)
+          sh.split = {1, now.b, now.kh, now.row0, now.rows, share_of(now.end - 1, total, ctas) - cta + 1, {0, 0}};
       }
-      if (live) {
-#pragma unroll
-        for (int u = 0; u < 32; u += 8)
-          *reinterpret_cast<uint4*>(to + (i + u) * 2) =
-              make_uint4(bf16_pair(__uint_as_float(y[u]), __uint_as_float(y[u + 1])),
-                         bf16_pair(__uint_as_float(y[u + 2]), __uint_as_float(y[u + 3])),
-                         bf16_pair(__uint_as_float(y[u + 4]), __uint_as_float(y[u + 5])),
-                         bf16_pair(__uint_as_float(y[u + 6]), __uint_as_float(y[u + 7])));
+    } else {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kOtherRegs));
+      if (warp == 8) {
+        issue_products<D, FMT, kTiles>(smem_u32(smem), smem_u32(ring), sh, wait, walk, tmem);
+        __syncwarp();
+      } else if (warp > 8) {
+        const Copier<D, FMT> copier{ring, sh, wait, dm, kv, maps, layer, st.err, tid - 288, lane, warp - 9};
+        copier.run(walk);
       }
-    }
-    if (live && lse) {
-      const float shift = FMT == EPIKV_CACHE_BF16 ? 0.f : 7.f;
-      lse[(int64_t)(it.e.tok0 + token) * dm.Hq + hq] = l == 0.f ? -INFINITY : (m - shift + log2f(l)) * 0.69314718055994531f;
     }
   }
+  if (tid == 0) reinterpret_cast<ChunkSplit*>(st.splits)[cta] = sh.split;
   tensor_fence_before();
   __syncthreads();
   tensor_fence_after();
-  if (warp == 0) tmem_free(tmem, 512);
+  if (warp == 8) tmem_free(tmem, 512);
+}
+
+// Joins the segments of an item: a CTA for the rows of a block of the item that starts in CTA blockIdx.x's share.  A thread
+// adds up four channels of a row, segment by segment.
+template <int D>
+__global__ void __launch_bounds__(256) chunk_join_kernel(AttnState st, AttnDims dm, int layer, Batch ba, Rows out, float* lse,
+                                                         int part_rows) {
+  constexpr int kRows = 1024 / D;   // of a CTA
+  pdl_wait();
+  pdl_trigger();
+  const ChunkSplit s = reinterpret_cast<const ChunkSplit*>(st.splits)[blockIdx.x];
+  const int row = blockIdx.y * kRows + threadIdx.x % kRows, ch = threadIdx.x / kRows;
+  if (!s.there || row >= s.rows) return;
+  const int64_t size = (int64_t)part_rows * (D + 2);
+  auto part = [&](int i) { return st.part + (2 * ((int64_t)blockIdx.x + i) + (i == 0 ? 1 : 0)) * size; };
+  auto max_sum = [&](int i) { return reinterpret_cast<const float2*>(part(i) + (int64_t)part_rows * D)[row]; };
+  float top = -INFINITY;
+  for (int i = 0; i < s.parts; ++i) top = fmaxf(top, max_sum(i).x);
+  const float base = top == -INFINITY ? 0.f : top;
+  float sum = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int i = 0; i < s.parts; ++i) {
+    const float2 ml = max_sum(i);
+    const float4 v = reinterpret_cast<const float4*>(part(i))[(int64_t)ch * part_rows + row];
+    // never 0: 2^-149 of a bounded sum is nothing, of an infinite one infinite
+    const float w = fmaxf(exp2_fast(ml.x - base), __uint_as_float(1u));
+    sum += ml.y * w;
+    acc.x += v.x * w;
+    acc.y += v.y * w;
+    acc.z += v.z * w;
+    acc.w += v.w * w;
+  }
+  const int r = s.row0 + row;
+  const int64_t token = ba.cu_new[s.b] + r / dm.rep;
+  const int hq = s.kh * dm.rep + r % dm.rep;
+  float mul = sum == 0.f ? 0.f : 1.f / sum;
+  if (dm.fmt != EPIKV_CACHE_BF16) mul *= head_scale(st, dm, 1, layer, s.kh);
+  *reinterpret_cast<uint2*>(out.p + (token * out.st + hq * out.sh + ch * 4) * 2) =
+      make_uint2(bf16_pair(acc.x * mul, acc.y * mul), bf16_pair(acc.z * mul, acc.w * mul));
+  if (lse && ch == 0) lse[token * dm.Hq + hq] = sum == 0.f ? -INFINITY : (base + log2f(sum)) * 0.69314718055994531f;
 }
 
 template <int D, int kTiles>
-constexpr int chunk_smem() {
-  return kTiles * ChunkShape<D>::kQuery + ChunkShape<D>::kStages * ChunkShape<D>::kStage + 1024;
+constexpr int chunk_smem(int n_seq) {
+  return kTiles * ChunkShape<D>::kQuery + ChunkShape<D>::kStages * ChunkShape<D>::kStage + 1024 + (n_seq + 1) * 4;
+}
+// Rows that a part has room for: a multiple of 4, so that each part starts on 16 bytes.
+int part_rows_of(const AttnDims& dm, int max_new) {
+  const int64_t rows = (int64_t)max_new * dm.rep, most = dm.d == 256 ? 128 : 256;
+  return (int)((rows < most ? rows : most) + 3) & ~3;
 }
 
 template <int D, int FMT, int kTiles>
 cudaError_t run_chunk(const AttnState& st, const AttnDims& dm, int layer, const Batch& ba, bool causal, const Rows& q,
                       const Rows& out, float* lse, const KvDev& kv, cudaStream_t stream) {
-  static_assert(chunk_smem<D, kTiles>() + sizeof(ChunkShared<D, kTiles>) <= 227 * 1024, "shared memory");
-  const int64_t blocks = ((int64_t)ba.max_new * dm.rep + 128 * kTiles - 1) / (128 * kTiles);
-  return pdl_launch(chunk_kernel<D, FMT, kTiles>, dim3((unsigned)(blocks * dm.H), ba.n_seq), kChunkThreads,
-                    chunk_smem<D, kTiles>(), stream, st, dm, layer, ba, causal, q, out, lse, kv,
-                    dm.scale * 1.4426950408889634f);
+  using Shape = ChunkShape<D>;
+  static_assert(chunk_smem<D, kTiles>(kMaxSeqs) + sizeof(ChunkShared<D>) + 64 <= 227 * 1024, "shared memory");
+  const ChunkPlan plan = {128 * kTiles, Shape::kSlots, dm.rep, causal ? 1 : 0, dm.H};
+  const int rows = part_rows_of(dm, ba.max_new);
+  cudaError_t e = pdl_launch(chunk_kernel<D, FMT, kTiles>, dim3(kAttnCtas), kChunkThreads, chunk_smem<D, kTiles>(ba.n_seq),
+                             stream, st, dm, plan, layer, ba, q, out, lse, kv, layer_maps(dm, layer, kv, Shape::kSlots),
+                             dm.scale * 1.4426950408889634f, rows);
+  if (e != cudaSuccess) return e;
+  return pdl_launch(chunk_join_kernel<D>, dim3(kAttnCtas, (rows * D + 1023) / 1024), 256, 0, stream, st, dm, layer, ba, out,
+                    lse, rows);
 }
 
+// *runs becomes false where the compiler gave the kernel other registers than its warps' exchange of them counts on:
+// launched, it would wait for registers that nobody gives.
 template <int D, int FMT, int kTiles>
-cudaError_t allow_chunk() {
+cudaError_t allow_chunk(bool* runs) {
+  cudaFuncAttributes at;
+  const cudaError_t e = cudaFuncGetAttributes(&at, chunk_kernel<D, FMT, kTiles>);
+  if (e != cudaSuccess) return e;
+  if (at.numRegs != kLaunchRegs) *runs = false;
   return cudaFuncSetAttribute(chunk_kernel<D, FMT, kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              chunk_smem<D, kTiles>());
+                              chunk_smem<D, kTiles>(kMaxSeqs));
 }
 
 template <int FMT>
-cudaError_t prepare_format(int d) {
-  if (d == 256) return allow_chunk<256, FMT, 1>();
+cudaError_t prepare_format(int d, bool* runs) {
+  if (d == 256) return allow_chunk<256, FMT, 1>(runs);
   if (d == 128) {
-    const cudaError_t e = allow_chunk<128, FMT, 1>();
-    return e == cudaSuccess ? allow_chunk<128, FMT, 2>() : e;
+    const cudaError_t e = allow_chunk<128, FMT, 1>(runs);
+    return e == cudaSuccess ? allow_chunk<128, FMT, 2>(runs) : e;
   }
-  const cudaError_t e = allow_chunk<64, FMT, 1>();
-  return e == cudaSuccess ? allow_chunk<64, FMT, 2>() : e;
+  const cudaError_t e = allow_chunk<64, FMT, 1>(runs);
+  return e == cudaSuccess ? allow_chunk<64, FMT, 2>(runs) : e;
 }
 
 template <int FMT>
@@ -475,8 +876,13 @@ cudaError_t run_format(const AttnState& st, const AttnDims& dm, int layer, const
 
 }  // namespace
 
-cudaError_t chunk_prepare(const AttnDims& dm) {
-  return dm.fmt == EPIKV_CACHE_BF16 ? prepare_format<EPIKV_CACHE_BF16>(dm.d) : prepare_format<EPIKV_CACHE_E2M1>(dm.d);
+size_t chunk_part_floats(const AttnDims& dm) {
+  return (size_t)2 * kAttnCtas * part_rows_of(dm, dm.max_new) * (dm.d + 2);
+}
+
+cudaError_t chunk_prepare(const AttnDims& dm, bool* runs) {
+  *runs = true;
+  return dm.fmt == EPIKV_CACHE_BF16 ? prepare_format<EPIKV_CACHE_BF16>(dm.d, runs) : prepare_format<EPIKV_CACHE_E2M1>(dm.d, runs);
 }
 
 cudaError_t launch_attention_chunk(const AttnState& st, const AttnDims& dm, int layer, const Batch& ba, bool causal,

@@ -1,0 +1,82 @@
+// How the work of the operators of many query rows is cut, for the kernels and,
+// compiled for the host, for its tests.
+//
+// An item of the chunk's attention is (batch entry, KV head, block of query
+// rows).  Its slots are cut into tiles; all items' tiles stand in one line, which
+// the CTAs take in equal contiguous shares.  A share's piece of an item is a
+// segment; an item of several segments is joined by a second kernel.
+#pragma once
+
+#include <stdint.h>
+
+#include "attn_plan.h"
+
+namespace epikv {
+
+struct ChunkPlan {
+  int rows;      // query rows of an item
+  int slots;     // of a tile
+  int rep;       // query heads of a KV head
+  int causal;
+  int heads;     // KV heads
+};
+
+EPIKV_PLAN int chunk_blocks(const ChunkPlan& p, int n) { return (int)(((int64_t)n * p.rep + p.rows - 1) / p.rows); }
+// Slots that query row r sees, and the last row of a block.
+EPIKV_PLAN int row_sees(const ChunkPlan& p, int len, int r) { return p.causal ? len + r / p.rep + 1 : len; }
+EPIKV_PLAN int block_sees(const ChunkPlan& p, int n, int len, int block) {
+  const int64_t end = (int64_t)(block + 1) * p.rows, rows = (int64_t)n * p.rep;
+  return row_sees(p, len, (int)((end < rows ? end : rows) - 1));
+}
+// An item that sees nothing still has a place in the line: its rows' zeros are written.
+EPIKV_PLAN int block_tiles(const ChunkPlan& p, int n, int len, int block) {
+  const int t = (block_sees(p, n, len, block) + p.slots - 1) / p.slots;
+  return t > 1 ? t : 1;
+}
+EPIKV_PLAN int64_t head_tiles(const ChunkPlan& p, int n, int len) {
+  int64_t t = 0;
+  for (int i = 0; i < chunk_blocks(p, n); ++i) t += block_tiles(p, n, len, i);
+  return t;
+}
+
+// CTAs that share the line: one an item up to the GPU's, more where a share would be of over kLeastTiles tiles (a segment
+// costs its rows' queries and results, and a join, about as much as two to four tiles).
+constexpr int kLeastTiles = 4;
+EPIKV_PLAN int chunk_ctas(unsigned total, int64_t items) {
+  int64_t n = ((int64_t)total + kLeastTiles - 1) / kLeastTiles;
+  if (n < items) n = items;
+  if (n > kAttnCtas) n = kAttnCtas;
+  return n < (int64_t)total ? (int)n : (int)total;
+}
+// First tile of CTA c's share.
+EPIKV_PLAN unsigned share_start(int c, unsigned total, int ctas) { return (unsigned)((uint64_t)total * (unsigned)c / (unsigned)ctas); }
+// The CTA whose share tile x is in.
+EPIKV_PLAN int share_of(unsigned x, unsigned total, int ctas) {
+  int c = (int)((uint64_t)x * (unsigned)ctas / total);
+  while (share_start(c, total, ctas) > x) --c;
+  while (share_start(c + 1, total, ctas) <= x) ++c;
+  return c;
+}
+
+// What the second kernel joins: an item that starts in one CTA's share and does not end there.
+struct ChunkSplit {
+  int there;       // 0: the CTA starts no such item
+  int b, kh, row0, rows;
+  int parts;       // CTAs that hold a segment of it: this one and the next ones
+  int pad[2];
+};
+
+// Rows of T slots for every sequence and head, none of which meets another.
+EPIKV_PLAN bool weights_apart(int S, int H, int T, int64_t stride_seq, int64_t stride_head) {
+  if (stride_seq < 0 || stride_head < 0) return false;
+  if (S == 1 && H == 1) return true;
+  if (S == 1) return stride_head >= T;
+  if (H == 1) return stride_seq >= T;
+  const bool seqs_inside = stride_seq < stride_head;   // the rows of one head stand together
+  const int64_t lo = seqs_inside ? stride_seq : stride_head, hi = seqs_inside ? stride_head : stride_seq;
+  const int64_t n = seqs_inside ? S : H;
+  // lo * (n - 1) + T <= hi, without leaving 64 bits
+  return lo >= T && (hi - T) / lo >= n - 1;
+}
+
+}  // namespace epikv

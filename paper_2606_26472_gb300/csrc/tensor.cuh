@@ -4,6 +4,8 @@
 #pragma once
 
 #include "attn.cuh"
+#include "attn_plan.h"
+#include "maps.cuh"
 
 namespace epikv {
 
@@ -164,6 +166,55 @@ __device__ __forceinline__ uint32_t half_pair_times(uint32_t a, uint32_t b, bool
   const __half2 s = *reinterpret_cast<const __half2*>(&b);
   const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), high ? __high2half2(s) : __low2half2(s));
   return *reinterpret_cast<const uint32_t*>(&r);
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
+// ------------------------------------------------------------ a layer's rows as a tensor
+// [blocks or sequences][slots of one][channels of all heads]; a copy takes 64 channels of `slots` slots, which stand in
+// one block, as they are wanted in a panel.
+struct LayerMaps {
+  CUtensorMap kv[2];
+  int slots;   // 0: the layer cannot be described so; rows are copied by lanes
+};
+
+__device__ __forceinline__ void tma_load_rows(uint32_t dst, const CUtensorMap* map, int channel, int slot, int block,
+                                              uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      :: "r"(dst), "l"(map), "r"(channel), "r"(slot), "r"(block), "r"(smem_u32(bar)) : "memory");
+}
+
+// `most`: slots of a copy, at most (a power of two).
+inline LayerMaps layer_maps(const AttnDims& dm, int layer, const KvDev& kv, int most) {
+  LayerMaps maps = {};
+  if (dm.fmt != EPIKV_CACHE_BF16) return maps;
+  const bool flat = kv.layout == EPIKV_LAYOUT_CONTIGUOUS;
+  int slots = most;
+  while (!flat && slots > 4 && kv.block_size % slots) slots /= 2;
+  if (slots < 8) return maps;   // a swizzled block is eight rows
+  const int64_t outer = flat ? kv.stride_seq : kv.stride_block;   // elements
+  // sequences closer together than they are long: no tensor says that (see cache_maps in attention.cu)
+  if (flat && kv.stride_seq / kv.stride_token < dm.T) return maps;
+  const cuuint64_t dims[3] = {(cuuint64_t)dm.H * dm.d, (cuuint64_t)(flat ? dm.T : kv.block_size),
+                              (cuuint64_t)(flat ? dm.S : kv.num_blocks)};
+  const cuuint64_t strides[2] = {(cuuint64_t)kv.stride_token * 2, (cuuint64_t)outer * 2};
+  for (int i = 0; i < 2; ++i)
+    if (strides[i] == 0 || strides[i] >= (cuuint64_t(1) << 40)) return maps;
+  const cuuint32_t box[3] = {64, (cuuint32_t)slots, 1}, ones[3] = {1, 1, 1};
+  const EncodeTiled encode = encode_tiled();
+  if (!encode) return maps;
+  for (int w = 0; w < 2; ++w)
+    if (encode(&maps.kv[w], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, kv.base[w] + (int64_t)layer * kv.stride_layer * 2, dims,
+               strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return maps;
+  maps.slots = slots;
+  return maps;
 }
 
 // ------------------------------------------------------------ rows of a tile

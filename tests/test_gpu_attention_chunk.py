@@ -256,17 +256,17 @@ def test_offsets_past_32_bits(gpu_lib):
 
 
 def test_reported_and_skipped(gpu_lib):
-    """Entries that cannot be taken are reported and leave their rows; the others are as without them."""
+    """Entries that cannot be taken are reported and leave their rows; the others are right (where a row's slots are split
+    goes by the whole batch's work, so not the same bits as without them)."""
     c = R.Cache(seqs=4, T=256, H=2, d=64, seed=14)
     ctx = c.context(4, 32)
     q = queries(64, 4, 64)
-    good, lgood = attend(c, ctx, q, [32, 32], [100, 50], seqs=[0, 3])
     for seqs, held, code in (([0, 9], [100, 50], E.EPIKV_DEV_BATCH), ([0, -1], [100, 50], E.EPIKV_DEV_BATCH),
                              ([0, 3], [100, 225], E.EPIKV_DEV_CAPACITY), ([0, 3], [100, -1], E.EPIKV_DEV_CAPACITY)):
         o, l = attend(c, ctx, q, [32, 32], held, seqs=seqs)
         assert E.epikv_attn_get_error(ctx) == (E.EPIKV_EDEVICE, code)
-        assert torch.equal(o[:32], good[:32]) and torch.equal(l[:32], lgood[:32])
-        assert bool(o[32:].isnan().all())
+        check_attention(c, q[:32], o[:32], l[:32], [32], [100])
+        assert bool(o[32:].isnan().all()) and bool(l[32:].isnan().all())
     # a block that the pool does not have: its slots are rows of zeros
     table = c.c.block_table.clone()
     table[0, 2] = c.c.num_blocks
