@@ -29,7 +29,6 @@ static_assert(2 * owner_regs(2) + kOtherRegs <= 3 * kLaunchRegs && owner_regs(1)
 template <int D>
 struct ChunkShape {
   static constexpr int kSlots = D == 256 ? 64 : 128;   // of a tile
-  static constexpr int kPanel = kSlots * 128;          // bytes of 64 channels of a tile's slots
   static constexpr int kStage = kSlots * D * 2;
   static constexpr int kQuery = 128 * D * 2;           // bytes of a tile of query rows
   static constexpr int kStages = D == 64 ? 8 : 4;
@@ -50,6 +49,7 @@ struct Segment {
 struct ShareStart {
   int b, kh, block;
   unsigned at;
+  Entry e;
 };
 
 // A warp's walk along its CTA's share, in shared memory: its first lane moves it on, and what the loops over tiles do not
@@ -57,9 +57,17 @@ struct ShareStart {
 struct WarpWalk {
   ShareStart here;
   unsigned x;          // the share's next tile
-  Entry e;
   Segment now[2];
 };
+
+__device__ __forceinline__ Entry entry_of(const Batch& ba, int b) {
+  Entry e;
+  e.tok0 = ba.cu_new[b];
+  e.n = ba.cu_new[b + 1] - e.tok0;
+  e.seq = ba.seq_ids[b];
+  e.len = ba.len[(int64_t)b * ba.len_stride];
+  return e;
+}
 
 struct SegmentWalk {
   WarpWalk* w;
@@ -72,22 +80,12 @@ struct SegmentWalk {
     if (lane == 0) {
       w->here = start;
       w->x = x;
-      entry();
     }
     __syncwarp();
   }
-  __device__ __forceinline__ void entry() const {
-    const int b = w->here.b;
-    Entry e;
-    e.tok0 = ba.cu_new[b];
-    e.n = ba.cu_new[b + 1] - e.tok0;
-    e.seq = ba.seq_ids[b];
-    e.len = ba.len[(int64_t)b * ba.len_stride];
-    w->e = e;
-  }
   __device__ __forceinline__ void step(Segment* s) const {
-    const Entry e = w->e;
     ShareStart h = w->here;
+    const Entry e = h.e;
     const unsigned x = w->x;
     const unsigned tiles = (unsigned)block_tiles(plan, e.n, e.len, h.block), take = min(h.at + tiles, end) - x;
     s->e = e;
@@ -98,7 +96,7 @@ struct SegmentWalk {
     s->least = row_sees(plan, e.len, s->row0);
     s->most = block_sees(plan, e.n, e.len, h.block);
     s->t0 = (int)(x - h.at);
-    s->t1 = min(s->t0 + (int)take, (s->most + plan.slots - 1) / plan.slots);
+    s->t1 = min(s->t0 + (int)take, (s->most + plan.slots - 1) >> plan.slots_log);
     s->first = x == h.at;
     s->last = x + take == h.at + tiles;
     s->end = h.at + tiles;
@@ -112,11 +110,11 @@ struct SegmentWalk {
           if (w->x < end) {
             do ++h.b;
             while (pre[h.b + 1] == pre[h.b]);
+            h.e = entry_of(ba, h.b);
           }
         }
       }
       w->here = h;
-      if (h.b != s->b) entry();
     }
   }
   // The whole warp; false at the share's end.
@@ -133,7 +131,7 @@ struct SegmentWalk {
 template <int D>
 struct alignas(16) ChunkShared {
   static constexpr int kStages = ChunkShape<D>::kStages;
-  uint64_t query, full[kStages], empty[kStages], scores[2], weights[2], sums, done;
+  uint64_t query, full[kStages], empty[kStages], scores[2], weights[2][2], sums, done, landed;
   uint32_t tmem;
   int gave_up;
   volatile int unclean[4];                  // 1 + the last segment with an infinite or NaN value in a slot that not all its rows see
@@ -154,9 +152,26 @@ __device__ __forceinline__ int64_t line_up(unsigned* pre, const Batch& ba, const
     Entry e;
     unsigned n = 0;
     int64_t it = 0;
-    if (b < ba.n_seq && batch_entry(ba, dm, b, plan.causal, err, &e)) {
-      n = count_of(head_tiles(plan, e.n, e.len) * plan.heads);
-      it = (int64_t)chunk_blocks(plan, e.n) * plan.heads;
+    const bool taken = b < ba.n_seq && batch_entry(ba, dm, b, plan.causal, err, &e);
+    const int blocks = taken ? chunk_blocks(plan, e.n) : 0;
+    int64_t tiles = 0;
+    if (__all_sync(0xffffffffu, blocks <= 8)) {
+      if (taken) tiles = head_tiles(plan, e.n, e.len);
+    } else {   // long entries one by one
+      for (unsigned left = __ballot_sync(0xffffffffu, blocks > 0); left; left &= left - 1) {
+        const int who = __ffs(left) - 1;
+        const int en = __shfl_sync(0xffffffffu, e.n, who), len = __shfl_sync(0xffffffffu, e.len, who);
+        const int eb = __shfl_sync(0xffffffffu, blocks, who);
+        int64_t sum = 0;
+        for (int i = lane; i < eb; i += 32) sum += block_tiles(plan, en, len, i);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == who) tiles = sum;
+      }
+    }
+    if (taken) {
+      n = count_of(tiles * plan.heads);
+      it = (int64_t)blocks * plan.heads;
     }
     unsigned upto = n;
 #pragma unroll
@@ -193,7 +208,8 @@ __device__ __forceinline__ void find_tile(ShareStart* start, unsigned x, const u
     if (x < pre[mid + 1]) hi = mid;
     else lo = mid + 1;
   }
-  const int n = ba.cu_new[lo + 1] - ba.cu_new[lo], len = ba.len[(int64_t)lo * ba.len_stride];
+  const Entry e = entry_of(ba, lo);
+  const int n = e.n, len = e.len;
   const unsigned of_head = (pre[lo + 1] - pre[lo]) / (unsigned)plan.heads, kh = (x - pre[lo]) / of_head;
   unsigned at = pre[lo] + kh * of_head;
   const int blocks = chunk_blocks(plan, n);
@@ -215,7 +231,7 @@ __device__ __forceinline__ void find_tile(ShareStart* start, unsigned x, const u
     }
     at += __shfl_sync(0xffffffffu, upto, 31);
   }
-  if (lane == 0) *start = {lo, (int)kh, block, at};
+  if (lane == 0) *start = {lo, (int)kh, block, at, e};
 }
 
 // Element offset of each of the tile's slots, or -1.
@@ -231,26 +247,36 @@ __device__ __forceinline__ void tile_offsets(int64_t* offset, int n, int s0, int
   }
 }
 
-__device__ __forceinline__ bool unbounded16(uint32_t w, uint32_t mask) {   // an exponent of all ones in either half
-  return (w & mask) == mask || (w >> 16 & mask) == mask;
+// Whether any of eight 16-bit values has an exponent of all ones (kBit: its lowest bit): infinite or NaN.
+template <uint32_t kBit>
+__device__ __forceinline__ bool unbounded(const uint4& v) {
+  constexpr uint32_t kExp = (0x8000u - kBit) * 0x10001u, kOne = kBit * 0x10001u;
+  return (((v.x & kExp) + kOne) | ((v.y & kExp) + kOne) | ((v.z & kExp) + kOne) | ((v.w & kExp) + kOne)) & 0x80008000u;
 }
-// The value with 0 in the place of what is infinite or NaN.
-__device__ __forceinline__ uint32_t bounded16(uint32_t w, uint32_t mask) {
-  if ((w & mask) == mask) w &= 0xffff0000u;
-  if ((w >> 16 & mask) == mask) w &= 0xffffu;
+// acc + 0 a: NaN in a half from the first value on that is infinite or NaN.
+template <bool kBf16>
+__device__ __forceinline__ void note_unbounded(uint32_t& acc, uint32_t a) {
+  if constexpr (kBf16) asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(a), "r"(0u));
+  else asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(a), "r"(0u));
+}
+// The values with 0 in the place of those.
+template <uint32_t kBit>
+__device__ __forceinline__ uint32_t bounded(uint32_t w) {
+  constexpr uint32_t kExp = 0x8000u - kBit;
+  if ((w & kExp) == kExp) w &= 0xffff0000u;
+  if ((w >> 16 & kExp) == kExp) w &= 0xffffu;
   return w;
 }
 
 // The copying warps.  A stage of the ring holds a tile's keys or its values, in turn; each warp arrives once when its part
-// of a stage is there.  Tiles whose slots all rows see come as tensor copies where the layer is a tensor; the others by
-// lanes, which also clear what no row sees.
+// of a stage is there.  Tiles come as tensor copies where the layer is a tensor, else by lanes.
 template <int D, int FMT>
 struct Copier {
   using Shape = ChunkShape<D>;
   static constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
-  static constexpr uint32_t kExp = kBf16 ? 0x7f80u : 0x7c00u;
+  static constexpr uint32_t kBit = kBf16 ? 0x80u : 0x400u;   // lowest of the exponent
   static constexpr int kPer = kBf16 ? D / 8 : D / 32;     // 16-byte pieces of a head's row in the cache
-  enum { kMost = (Shape::kSlots * kPer + kCopyThreads - 1) / kCopyThreads, kLag = 2 };   // pieces of a thread; stages in flight
+  enum { kMost = (Shape::kSlots * kPer + kCopyThreads - 1) / kCopyThreads };   // pieces of a thread
   char* ring;
   ChunkShared<D>& sh;
   const TensorWaiter& wait;
@@ -265,57 +291,80 @@ struct Copier {
   __device__ __forceinline__ void left(int i) const {
     if (i >= Shape::kStages) wait(&sh.empty[i % Shape::kStages], (uint32_t)(i / Shape::kStages - 1) & 1);
   }
-  __device__ __forceinline__ void put_clean(uint32_t at, const uint4& v, int seg) const {
-    if (unbounded16(v.x, kExp) || unbounded16(v.y, kExp) || unbounded16(v.z, kExp) || unbounded16(v.w, kExp)) {
-      sts16(at, make_uint4(bounded16(v.x, kExp), bounded16(v.y, kExp), bounded16(v.z, kExp), bounded16(v.w, kExp)));
-      sh.unclean[seg & 3] = seg + 1;
-    }
-  }
-  // What this thread copied is there.  A probability of 0 must not meet an infinity or a NaN in a slot that only other rows
-  // see: of values that not all rows see each thread looks through its own.
-  __device__ __forceinline__ void deliver(int i, int which, int s0, const Segment& g, int seg) const {
-    if (which && s0 + Shape::kSlots > g.least) {
-      const uint32_t dst = stage(i);
-      for (int x = tid; x < Shape::kSlots * kPer; x += kCopyThreads) {
-        const int r = x / kPer, c = x % kPer;
-        if (s0 + r < g.least) continue;
-        if constexpr (kBf16) {
-          const uint32_t at = dst + (c >> 3) * Shape::kPanel + panel_at(r, c & 7);
-          put_clean(at, lds16(at), seg);
-        } else {
+  // A probability of 0 must not meet an infinity or a NaN in a slot that other rows see or none: of a stage of values, rows
+  // that not all query rows see are looked through (0 times a value, added up: NaN from the first that is not bounded), and
+  // those that none sees cleared.
+  __device__ __forceinline__ void clean(int i, int s0, const Segment& g, int seg) const {
+    constexpr int kRow = D / 8, kAtOnce = 4;
+    const uint32_t dst = stage(i);
+    const int from = max(g.least - s0, 0) * kRow, to = min(g.most - s0, Shape::kSlots) * kRow;
+    auto place = [&](int x) { return dst + tile_at<D>(x / kRow, x % kRow); };
+    uint32_t acc[4] = {0, 0, 0, 0};
+    for (int x0 = from + tid; x0 < to; x0 += kAtOnce * kCopyThreads) {
+      uint4 v[kAtOnce];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const uint32_t at = dst + (c >> 1) * Shape::kPanel + panel_at(r, (c & 1) * 4 + u);
-            put_clean(at, lds16(at), seg);
-          }
-        }
+      for (int u = 0; u < kAtOnce; ++u) v[u] = lds16_pure(place(min(x0 + u * kCopyThreads, to - 1)));
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        note_unbounded<kBf16>(acc[0], v[u].x);
+        note_unbounded<kBf16>(acc[1], v[u].y);
+        note_unbounded<kBf16>(acc[2], v[u].z);
+        note_unbounded<kBf16>(acc[3], v[u].w);
       }
     }
+    if (unbounded<kBit>(make_uint4(acc[0], acc[1], acc[2], acc[3])))   // (the last piece of all may be another thread's)
+      for (int x = from + tid; x < to; x += kCopyThreads) {
+        const uint4 v = lds16(place(x));
+        if (unbounded<kBit>(v)) {
+          sts16(place(x), make_uint4(bounded<kBit>(v.x), bounded<kBit>(v.y), bounded<kBit>(v.z), bounded<kBit>(v.w)));
+          sh.unclean[seg & 3] = seg + 1;
+        }
+      }
+    for (int x = max(to, 0) + tid; x < Shape::kSlots * kRow; x += kCopyThreads) sts16(place(x), make_uint4(0, 0, 0, 0));
+  }
+  // The warp's part of a stage that was written by lanes is there.
+  __device__ __forceinline__ void deliver(int i) const {
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) mbar_arrive_one(&sh.full[i % Shape::kStages]);
   }
 
-  __device__ __forceinline__ void bf16_segment(const Segment& g, int i0, int seg) const {
-    constexpr int kPanels = D / 64;
-    const int boxes = maps.slots ? Shape::kSlots / maps.slots * kPanels : 0;   // at most 32
-    const bool flat = kv.layout == EPIKV_LAYOUT_CONTIGUOUS;
-    const int panel = lane % kPanels, box = lane / kPanels;
-    int i = i0, pending = 0;
-    auto drain = [&] {
-      copy_wait<0>();
-      for (; pending > 0; --pending) {
-        const int k = i - pending - i0;
-        deliver(i - pending, k & 1, (g.t0 + (k >> 1)) * Shape::kSlots, g, seg);
+  // Lane l looks after box l of the tile.  Keys that no row sees may stay as they are (their scores are replaced); boxes that
+  // hold nothing but those are left out.
+  __device__ __forceinline__ void tensor_tile(int i, int j, int y, int z, const Segment& g, int seg, int* turns) const {
+    const int s0 = j * Shape::kSlots;
+    const int slots = min(Shape::kSlots, (g.most - s0 + maps.slots - 1) & -maps.slots);   // that come
+    const bool whole = s0 + Shape::kSlots <= g.least;
+#pragma unroll 1
+    for (int w = 0; w < 2; ++w, ++i) {
+      left(i);
+      uint64_t* full = &sh.full[i % Shape::kStages];
+      uint64_t* bar = w && !whole ? &sh.landed : full;
+      if (warp == 0) {
+        if (lane == 0) mbar_arrive_expect_tx(bar, slots * D * 2);
+        __syncwarp();
+        if (lane * maps.slots < slots)
+          tma_load_rows(stage(i) + lane * maps.slots * (D * 2), &maps.kv[w], g.kh * (D / 64), y >> 3, z, bar);
+        __syncwarp();
+      } else if (bar == full && lane == 0) {
+        mbar_arrive_one(full);
       }
-    };
-    for (int j = g.t0; j < g.t1; ++j) {
+      if (bar == full) continue;
+      wait(bar, (uint32_t)(*turns)++ & 1);
+      clean(i, s0, g, seg);
+      deliver(i);
+    }
+  }
+
+  __device__ __forceinline__ void bf16_segment(const Segment& g, int i, int seg, int* turns) const {
+    const bool flat = kv.layout == EPIKV_LAYOUT_CONTIGUOUS;
+    for (int j = g.t0; j < g.t1; ++j, i += 2) {
       const int s0 = j * Shape::kSlots;
-      bool whole = maps.slots && s0 + Shape::kSlots <= g.least;
-      int y = s0 + box * maps.slots, z = g.e.seq;
+      bool whole = maps.slots && min(s0 + Shape::kSlots, g.most) <= maps.end;
       if (whole) {
+        int y = s0 + lane * maps.slots, z = g.e.seq;
         bool there = true;
-        if (!flat && lane < boxes) {
+        if (!flat && y < g.most && lane * maps.slots < Shape::kSlots) {
           const int bi = y / kv.block_size;
           y -= bi * kv.block_size;
           z = bi < kv.max_blocks
@@ -323,54 +372,48 @@ struct Copier {
                   : -1;
           there = z >= 0 && z < kv.num_blocks;
         }
-        whole = __all_sync(0xffffffffu, there);
+        whole = __all_sync(0xffffffffu, there);   // else by lanes, which report it
+        if (whole) tensor_tile(i, j, y, z, g, seg, turns);
       }
-      if (whole) {
-        drain();
-#pragma unroll 1
-        for (int w = 0; w < 2; ++w, ++i) {
-          left(i);
-          uint64_t* bar = &sh.full[i % Shape::kStages];
-          if (warp == 0) {
-            if (lane == 0) mbar_arrive_expect_tx(bar, Shape::kStage);
-            __syncwarp();
-            if (lane < boxes)
-              tma_load_rows(stage(i) + panel * Shape::kPanel + box * maps.slots * 128, &maps.kv[w], g.kh * D + panel * 64, y, z,
-                            bar);
-          } else if (lane == 0) {
-            mbar_arrive_one(bar);
-          }
-          __syncwarp();
-        }
-        continue;
-      }
-      int64_t* offset = sh.offset[j & 1];   // all threads were here for the tile before, so this one's is free
-      tile_offsets(offset, Shape::kSlots, s0, g.most, kv, layer, g.e.seq, dm.T, err, tid, kCopyThreads);
-      named_sync(1, kCopyThreads);
-#pragma unroll 1
-      for (int w = 0; w < 2; ++w) {
-        left(i);
-        const uint32_t dst = stage(i);
-        const char* base = kv.base[w];
-#pragma unroll 4
-        for (int x = tid; x < Shape::kSlots * kPer; x += kCopyThreads) {
-          const int r = x / kPer, c = x % kPer;
-          const int64_t o = offset[r];
-          copy_async16(dst + (c >> 3) * Shape::kPanel + panel_at(r, c & 7), base + (o < 0 ? 0 : (o + g.kh * D + c * 8) * 2),
-                       o < 0 ? 0 : 16);
-        }
-        copy_commit();
-        ++i;
-        if (++pending > kLag) {
-          copy_wait<kLag>();
-          const int k = i - pending - i0;
-          deliver(i - pending, k & 1, (g.t0 + (k >> 1)) * Shape::kSlots, g, seg);
-          --pending;
-        }
-      }
+      if (!whole) lane_tile(i, j, g, seg);
     }
-    drain();
     named_sync(1, kCopyThreads);   // the offsets are free for the next segment
+  }
+
+  // By lanes: the values' copies are under way while the keys' are waited for.
+  __device__ __forceinline__ void lane_tile(int i, int j, const Segment& g, int seg) const {
+    const int s0 = j * Shape::kSlots;
+    int64_t* offset = sh.offset[j & 1];   // all threads were here for the tile before, so this one's is free
+    tile_offsets(offset, Shape::kSlots, s0, g.most, kv, layer, g.e.seq, dm.T, err, tid, kCopyThreads);
+    named_sync(1, kCopyThreads);
+#pragma unroll 1
+    for (int w = 0; w < 2; ++w) {
+      left(i + w);
+      const uint32_t dst = stage(i + w);
+      const char* base = kv.base[w];
+      constexpr int kAtOnce = 8;
+      for (int x0 = tid; x0 < Shape::kSlots * kPer; x0 += kAtOnce * kCopyThreads) {
+        int64_t o[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) o[u] = offset[min((x0 + u * kCopyThreads) / kPer, Shape::kSlots - 1)];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const int x = x0 + u * kCopyThreads, r = x / kPer, c = x % kPer;
+          if (x < Shape::kSlots * kPer)
+            copy_async16(dst + tile_at<D>(r, c),
+                         base + (o[u] < 0 ? 0 : (o[u] + g.kh * D + c * 8) * 2), o[u] < 0 ? 0 : 16);
+        }
+      }
+      copy_commit();
+    }
+    copy_wait<1>();
+    deliver(i);
+    copy_wait<0>();
+    if (s0 + Shape::kSlots > g.least) {
+      named_sync(1, kCopyThreads);   // what others copied is looked through too
+      clean(i + 1, s0, g, seg);
+    }
+    deliver(i + 1);
   }
 
   struct Codes {
@@ -401,7 +444,7 @@ struct Copier {
         uint4 v[4];
         expand32(c.code[u], c.scale[u], v);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) sts16(dst + (p >> 1) * Shape::kPanel + panel_at(r, (p & 1) * 4 + k), v[k]);
+        for (int k = 0; k < 4; ++k) sts16(dst + tile_at<D>(r, p * 4 + k), v[k]);
       }
     }
   }
@@ -415,26 +458,31 @@ struct Copier {
     offsets(g.t0);
     load_codes(k, 0, sh.offset[g.t0 & 1], g.kh);
     for (int j = g.t0; j < g.t1; ++j, i += 2) {
+      const int s0 = j * Shape::kSlots;
       load_codes(v, 1, sh.offset[j & 1], g.kh);
       put_codes(k, i);
-      deliver(i, 0, j * Shape::kSlots, g, seg);
+      deliver(i);
       if (j + 1 < g.t1) {
         offsets(j + 1);
         load_codes(k, 0, sh.offset[(j + 1) & 1], g.kh);
       }
       put_codes(v, i + 1);
-      deliver(i + 1, 1, j * Shape::kSlots, g, seg);
+      if (s0 + Shape::kSlots > g.least) {
+        named_sync(1, kCopyThreads);   // what others wrote is looked through too
+        clean(i + 1, s0, g, seg);
+      }
+      deliver(i + 1);
     }
-    named_sync(1, kCopyThreads);
+    named_sync(1, kCopyThreads);   // the offsets are free for the next segment
   }
 
   __device__ __forceinline__ void run(const SegmentWalk& walk) const {
-    int i = 0;
+    int i = 0, turns = 0;
     for (int seg = 0, at = 0; walk.next(at); ++at) {
       const Segment& g = walk.segment(at);
       const int tiles = g.t1 - g.t0;
       if (tiles <= 0) continue;
-      if constexpr (kBf16) bf16_segment(g, i, seg);
+      if constexpr (kBf16) bf16_segment(g, i, seg, &turns);
       else q4_segment(g, i, seg);
       i += 2 * tiles;
       ++seg;
@@ -442,39 +490,58 @@ struct Copier {
     if (*wait.gave_up && warp == 0)   // the CTA may not end before its copies have landed
       for (int k = max(0, i - Shape::kStages); k < i; ++k)
         mbar_wait_bounded(&sh.full[k % Shape::kStages], (uint32_t)(k / Shape::kStages) & 1, kTensorWaitNs);
+    if (*wait.gave_up && warp == 0 && turns) mbar_wait_bounded(&sh.landed, (uint32_t)(turns - 1) & 1, kTensorWaitNs);
   }
 };
 
+// The issuing warp.  All its lanes go through the loops, so that the operands' descriptions are formed once for the warp (by
+// one lane alone, the registers' way to the instruction took 110 cycles a product, of 64 that the product takes).
 template <int D, int FMT, int kTiles>
 __device__ __forceinline__ void issue_products(uint32_t query, uint32_t ring, ChunkShared<D>& sh, const TensorWaiter& wait,
                                                const SegmentWalk& walk, uint32_t tmem) {
   using Shape = ChunkShape<D>;
   constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
   constexpr uint32_t kScores = product_of(128, Shape::kSlots, kBf16, false), kSums = product_of(128, D, kBf16, true);
+  const uint64_t q0 = rows_operand<D>(query), k0 = rows_operand<D>(ring), v0 = columns_operand<D>(ring);
   auto scores = [&](int t, int buf, int st) {
-    const uint32_t q = query + t * Shape::kQuery, k = ring + st * Shape::kStage;
+    const uint64_t q = q0 + (uint32_t)(t * (Shape::kQuery >> 4)), k = k0 + (uint32_t)(st * (Shape::kStage >> 4));
+    const uint32_t d = tmem + buf * 128;
+    if (elected()) {
 #pragma unroll
-    for (int x = 0; x < D / 16; ++x)
-      multiply(tmem + buf * 128, rows_operand(q + (x >> 2) * (128 * 128) + (x & 3) * 32),
-               rows_operand(k + (x >> 2) * Shape::kPanel + (x & 3) * 32), kScores, x > 0);
-    products_done(&sh.scores[buf]);
+      for (int x = 0; x < D / 16; ++x)
+        multiply(d, q + rows_step(x), k + rows_step(x), kScores, x > 0);
+      products_done(&sh.scores[buf]);
+    }
+    __syncwarp();
   };
-  auto sums = [&](int t, int buf, int st, bool add) {
-    const uint32_t v = ring + st * Shape::kStage;
+  // the products with the first half of a tile's slots go ahead while the others' probabilities are formed
+  auto sums = [&](int t, int buf, int st, bool add, uint32_t parity) {
+    const uint64_t v = v0 + (uint32_t)(st * (Shape::kStage >> 4));
+    const uint32_t d = tmem + 256 + t * 128, p = tmem + buf * 128;
 #pragma unroll
-    for (int x = 0; x < Shape::kSlots / 16; ++x)
-      multiply_tmem(tmem + 256 + t * 128, tmem + buf * 128 + x * 8, columns_operand(v + x * 2048, Shape::kPanel), kSums,
-                    add || x > 0);
+    for (int h = 0; h < 2; ++h) {
+      wait(&sh.weights[buf][h], parity);
+      tensor_fence_after();
+      if (elected()) {
+#pragma unroll
+        for (int x = h * Shape::kSlots / 32; x < (h + 1) * Shape::kSlots / 32; ++x)
+          multiply_tmem(d, p + x * 8, v + columns_step<D>(x), kSums, add || x > 0);
+      }
+      __syncwarp();
+    }
   };
   auto filled = [&](int i) {
     wait(&sh.full[i % Shape::kStages], (uint32_t)(i / Shape::kStages) & 1);
     tensor_fence_after();
   };
+  auto done = [&](uint64_t* bar) {
+    if (elected()) products_done(bar);
+    __syncwarp();
+  };
   // i: the tile's keys in the ring; a: tiles so far
   for (int i = 0, a = 0, seg = 0, at = 0; walk.next(at); ++at) {
-    const int tiles = walk.segment(at).t1 - walk.segment(at).t0;
+    const int tiles = __shfl_sync(0xffffffffu, walk.segment(at).t1 - walk.segment(at).t0, 0);
     if (tiles <= 0) continue;
-    if (walk.lane) continue;
     wait(&sh.query, (uint32_t)seg & 1);
     tensor_fence_after();
     filled(i);
@@ -483,7 +550,7 @@ __device__ __forceinline__ void issue_products(uint32_t query, uint32_t ring, Ch
     } else {
       for (int t = 0; t < 2; ++t) scores(t, t, i % Shape::kStages);
     }
-    products_done(&sh.empty[i % Shape::kStages]);
+    done(&sh.empty[i % Shape::kStages]);
     for (int j = 0; j < tiles; ++j, i += 2, ++a) {
       const int v = (i + 1) % Shape::kStages, k = (i + 2) % Shape::kStages;
       const bool more = j + 1 < tiles;
@@ -491,28 +558,26 @@ __device__ __forceinline__ void issue_products(uint32_t query, uint32_t ring, Ch
         if (more) {
           filled(i + 2);
           scores(0, (a + 1) & 1, k);
-          products_done(&sh.empty[k]);
+          done(&sh.empty[k]);
         }
         filled(i + 1);
-        wait(&sh.weights[a & 1], (uint32_t)(a >> 1) & 1);
-        tensor_fence_after();
-        sums(0, a & 1, v, j > 0);
-        products_done(&sh.empty[v]);
-        products_done(&sh.sums);
+        sums(0, a & 1, v, j > 0, (uint32_t)(a >> 1) & 1);
+        done(&sh.empty[v]);
+        done(&sh.sums);
       } else {
         filled(i + 1);
-        if (more) filled(i + 2);
+#pragma unroll
         for (int t = 0; t < 2; ++t) {
-          wait(&sh.weights[t], (uint32_t)a & 1);
-          tensor_fence_after();
-          sums(t, t, v, j > 0);
-          if (more) scores(t, t, k);   // in order behind the products that read the probabilities in its place
+          sums(t, t, v, j > 0, (uint32_t)a & 1);
+          if (t == 1) done(&sh.empty[v]);
+          if (!more) continue;
+          if (t == 0) filled(i + 2);
+          scores(t, t, k);   // in order behind the products that read the probabilities in its place
         }
-        products_done(&sh.empty[v]);
-        if (more) products_done(&sh.empty[k]);
+        if (more) done(&sh.empty[k]);
       }
     }
-    products_done(&sh.done);
+    done(&sh.done);
     ++seg;
   }
 }
@@ -587,15 +652,28 @@ __device__ __forceinline__ void soften(ChunkShared<D>& sh, const TensorWaiter& w
         y[u / 2] = kBf16 ? bf16_pair(p, q) : half_pair(p, q);
       }
       tmem_store16(s + i / 2, y);
+      if (i + 32 == N / 2 || i + 32 == N) {
+        tmem_wait_store();
+        tensor_fence_before();
+        mbar_arrive_one(&sh.weights[buf][i + 32 == N]);
+      }
     }
     const f32x2 both = f2_add(sum[0], sum[1]);
     l += f2_lo(both) + f2_hi(both);
-    tmem_wait_store();
-    tensor_fence_before();
-    mbar_arrive_one(&sh.weights[buf]);
   }
   *m_out = m;
   *l_out = l;
+}
+
+// Lanes o apart: the one without the bit keeps a and gets the other's a for its b, the one with it keeps b and gets the
+// other's b for its a.
+__device__ __forceinline__ void exchange(uint4& a, uint4& b, int o, int lane) {
+  const bool up = lane & o;
+  const uint4 give = up ? a : b;
+  const uint4 get = make_uint4(__shfl_xor_sync(0xffffffffu, give.x, o), __shfl_xor_sync(0xffffffffu, give.y, o),
+                               __shfl_xor_sync(0xffffffffu, give.z, o), __shfl_xor_sync(0xffffffffu, give.w, o));
+  if (up) a = get;
+  else b = get;
 }
 
 // A segment's results: of a whole item its rows' outputs, else a part for the second kernel (outputs by fours of channels,
@@ -613,9 +691,16 @@ __device__ __forceinline__ void put_rows(const AttnState& st, const AttnDims& dm
   if (part) mul = 1.f;
   const bool none = l == 0.f;
   const float shift = kBf16 ? 0.f : 7.f;   // of the exponentials
-  char* to = out.p + ((int64_t)(g.e.tok0 + token) * out.st + hq * out.sh) * 2;
+  char* to = live ? out.p + ((int64_t)(g.e.tok0 + token) * out.st + hq * out.sh) * 2 : nullptr;
   const int from = max(g.least, g.t0 * N), upto = live && unclean ? min(seen, g.t1 * N) : 0;
-#pragma unroll 1
+  const int lane = threadIdx.x & 31;
+  char* row_of[4];   // of the four lanes that exchange pieces
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    row_of[u] = reinterpret_cast<char*>(__shfl_sync(0xffffffffu, (uint64_t)to, (lane & 28) + u));
+    if (row_of[u]) row_of[u] += (lane & 3) * 16;
+  }
+#pragma unroll 2
   for (int i = 0; i < D; i += 32) {
     uint32_t y[32];
     if (g.t0 < g.t1) {
@@ -642,19 +727,28 @@ __device__ __forceinline__ void put_rows(const AttnState& st, const AttnDims& dm
           if (((uint8_t)v[scale_offset(dm, g.kh) + (i + u) / kQuantGroup] & 0x7f) == 0x7f) y[u] = 0x7fc00000u;
       }
     }
-    if (!live) continue;
     if (part) {
+      if (live) {
 #pragma unroll
-      for (int u = 0; u < 32; u += 4)
-        reinterpret_cast<uint4*>(part)[(int64_t)((i + u) / 4) * part_rows + row] = make_uint4(y[u], y[u + 1], y[u + 2], y[u + 3]);
+        for (int u = 0; u < 32; u += 4)
+          reinterpret_cast<uint4*>(part)[(int64_t)((i + u) / 4) * part_rows + row] = make_uint4(y[u], y[u + 1], y[u + 2], y[u + 3]);
+      }
     } else {
+      uint4 v[4];   // the row's 64 bytes
 #pragma unroll
-      for (int u = 0; u < 32; u += 8)
-        *reinterpret_cast<uint4*>(to + (i + u) * 2) =
-            make_uint4(bf16_pair(__uint_as_float(y[u]), __uint_as_float(y[u + 1])),
-                       bf16_pair(__uint_as_float(y[u + 2]), __uint_as_float(y[u + 3])),
-                       bf16_pair(__uint_as_float(y[u + 4]), __uint_as_float(y[u + 5])),
-                       bf16_pair(__uint_as_float(y[u + 6]), __uint_as_float(y[u + 7])));
+      for (int u = 0; u < 4; ++u)
+        v[u] = make_uint4(bf16_pair(__uint_as_float(y[8 * u]), __uint_as_float(y[8 * u + 1])),
+                          bf16_pair(__uint_as_float(y[8 * u + 2]), __uint_as_float(y[8 * u + 3])),
+                          bf16_pair(__uint_as_float(y[8 * u + 4]), __uint_as_float(y[8 * u + 5])),
+                          bf16_pair(__uint_as_float(y[8 * u + 6]), __uint_as_float(y[8 * u + 7])));
+      // four lanes exchange: v[u] becomes the lane's piece of the u-th of their rows, so that they write its 64 bytes at once
+      exchange(v[0], v[1], 1, lane);
+      exchange(v[2], v[3], 1, lane);
+      exchange(v[0], v[2], 2, lane);
+      exchange(v[1], v[3], 2, lane);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (row_of[u]) *reinterpret_cast<uint4*>(row_of[u] + i * 2) = v[u];
     }
   }
   if (!live) return;
@@ -686,10 +780,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh.scores[i], 1);
-      mbar_init(&sh.weights[i], 128);
+      for (int h = 0; h < 2; ++h) mbar_init(&sh.weights[i][h], 128);
     }
     mbar_init(&sh.sums, 1);
     mbar_init(&sh.done, 1);
+    mbar_init(&sh.landed, 1);
     sh.gave_up = 0;
     sh.split = {};
     for (int i = 0; i < 4; ++i) sh.unclean[i] = 0;
@@ -728,8 +823,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         // rows that are not there see all slots of the tiles: their queries are 0
         seen = live ? row_sees(plan, g.e.len, r) : INT_MAX;
         if (g.t0 >= g.t1) return;
-        const uint4* src = live ? reinterpret_cast<const uint4*>(q.p + ((int64_t)(g.e.tok0 + token) * q.st + hq * q.sh) * 2) : nullptr;
-        factor = c * store_query<D, !kBf16>(smem_u32(smem + t * Shape::kQuery), 128 * 128, tid & 127, src);
+        const char* src = live ? q.p + ((int64_t)(g.e.tok0 + token) * q.st + hq * q.sh) * 2 : nullptr;
+        factor = c * store_queries<D, !kBf16>(smem_u32(smem + t * Shape::kQuery), tid & 96, src, lane);
         if constexpr (!kBf16) factor *= head_scale(st, dm, 0, layer, g.kh);
         fence_proxy_async_smem();
         mbar_arrive_one(&sh.query);
@@ -831,7 +926,7 @@ cudaError_t run_chunk(const AttnState& st, const AttnDims& dm, int layer, const 
                       const Rows& out, float* lse, const KvDev& kv, cudaStream_t stream) {
   using Shape = ChunkShape<D>;
   static_assert(chunk_smem<D, kTiles>(kMaxSeqs) + sizeof(ChunkShared<D>) + 64 <= 227 * 1024, "shared memory");
-  const ChunkPlan plan = {128 * kTiles, Shape::kSlots, dm.rep, causal ? 1 : 0, dm.H};
+  const ChunkPlan plan = {128 * kTiles, Shape::kSlots, kTiles == 2 ? 8 : 7, Shape::kSlots == 128 ? 7 : 6, dm.rep, causal ? 1 : 0, dm.H};
   const int rows = part_rows_of(dm, ba.max_new);
   cudaError_t e = pdl_launch(chunk_kernel<D, FMT, kTiles>, dim3(kAttnCtas), kChunkThreads, chunk_smem<D, kTiles>(ba.n_seq),
                              stream, st, dm, plan, layer, ba, q, out, lse, kv, layer_maps(dm, layer, kv, Shape::kSlots),

@@ -14,23 +14,25 @@
 namespace epikv {
 
 struct ChunkPlan {
-  int rows;      // query rows of an item
-  int slots;     // of a tile
+  int rows;      // query rows of an item, 1 << rows_log
+  int slots;     // of a tile, 1 << slots_log
+  int rows_log, slots_log;
   int rep;       // query heads of a KV head
   int causal;
   int heads;     // KV heads
 };
 
-EPIKV_PLAN int chunk_blocks(const ChunkPlan& p, int n) { return (int)(((int64_t)n * p.rep + p.rows - 1) / p.rows); }
+// (a call's tokens are at most 2^20, a KV head's query heads 1,024)
+EPIKV_PLAN int chunk_blocks(const ChunkPlan& p, int n) { return (n * p.rep + p.rows - 1) >> p.rows_log; }
 // Slots that query row r sees, and the last row of a block.
 EPIKV_PLAN int row_sees(const ChunkPlan& p, int len, int r) { return p.causal ? len + r / p.rep + 1 : len; }
 EPIKV_PLAN int block_sees(const ChunkPlan& p, int n, int len, int block) {
-  const int64_t end = (int64_t)(block + 1) * p.rows, rows = (int64_t)n * p.rep;
-  return row_sees(p, len, (int)((end < rows ? end : rows) - 1));
+  const int end = (block + 1) << p.rows_log, rows = n * p.rep;
+  return row_sees(p, len, (end < rows ? end : rows) - 1);
 }
 // An item that sees nothing still has a place in the line: its rows' zeros are written.
 EPIKV_PLAN int block_tiles(const ChunkPlan& p, int n, int len, int block) {
-  const int t = (block_sees(p, n, len, block) + p.slots - 1) / p.slots;
+  const int t = (block_sees(p, n, len, block) + p.slots - 1) >> p.slots_log;
   return t > 1 ? t : 1;
 }
 EPIKV_PLAN int64_t head_tiles(const ChunkPlan& p, int n, int len) {
@@ -48,11 +50,15 @@ EPIKV_PLAN int chunk_ctas(unsigned total, int64_t items) {
   if (n > kAttnCtas) n = kAttnCtas;
   return n < (int64_t)total ? (int)n : (int)total;
 }
-// First tile of CTA c's share.
-EPIKV_PLAN unsigned share_start(int c, unsigned total, int ctas) { return (unsigned)((uint64_t)total * (unsigned)c / (unsigned)ctas); }
+// First tile of CTA c's share, floor(total * c / ctas) in 32 bits.
+EPIKV_PLAN unsigned share_start(int c, unsigned total, int ctas) {
+  const unsigned q = total / (unsigned)ctas, r = total % (unsigned)ctas;
+  return q * c + r * c / (unsigned)ctas;
+}
 // The CTA whose share tile x is in.
 EPIKV_PLAN int share_of(unsigned x, unsigned total, int ctas) {
-  int c = (int)((uint64_t)x * (unsigned)ctas / total);
+  int c = (int)((float)x * (float)ctas / (float)total);   // near it; put right by the shares themselves
+  if (c > ctas - 1) c = ctas - 1;
   while (share_start(c, total, ctas) > x) --c;
   while (share_start(c + 1, total, ctas) <= x) ++c;
   return c;

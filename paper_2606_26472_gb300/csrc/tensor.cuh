@@ -65,25 +65,39 @@ __device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::l
 __device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // ------------------------------------------------------------ products
-// A tile stands in shared memory as panels of 64 channels: its rows' 128 bytes side by side, a row's eight 16-byte parts
-// exchanged by its number mod 8, so that eight rows (1,024 bytes, aligned to it) are one swizzled block.
-__device__ __forceinline__ uint32_t panel_at(int row, int part) { return row * 128 + ((part ^ (row & 7)) << 4); }
+// A tile stands in shared memory by eight rows: for each 64 channels the eight rows' 128 bytes side by side, a row's eight
+// 16-byte parts exchanged by its number mod 8 (1,024 bytes, aligned to it: a swizzled block), then the next 64 channels.
+// A tensor copy of any number of such rows, all channels, leaves them so.
+template <int D>
+__device__ __forceinline__ uint32_t tile_at(int row, int part) {   // part: of the row's 16 bytes
+  return (row >> 3) * (D * 16) + (part >> 3) * 1024 + (row & 7) * 128 + (((part ^ row) & 7) << 4);
+}
 
-// Such rows as an operand whose products run along the channels (the block's 64 channels are four steps of 32 bytes) ...
+// Such rows as an operand whose products run along the channels (16 channels are a step of 32 bytes, 64 of 1,024) ...
+template <int D>
 __device__ __forceinline__ uint64_t rows_operand(uint32_t smem) {
-  return (uint64_t)((smem & 0x3ffff) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
+  return (uint64_t)((smem & 0x3ffff) >> 4) | (uint64_t)1 << 16 | (uint64_t)(D * 16 >> 4) << 32 | (uint64_t)1 << 46 |
          (uint64_t)2 << 61;
 }
-// ... and as one whose products run along the rows (16 rows are a step of 2,048 bytes); the next 64 channels stand `panel`
-// bytes behind.
-__device__ __forceinline__ uint64_t columns_operand(uint32_t smem, uint32_t panel) {
-  return (uint64_t)((smem & 0x3ffff) >> 4) | (uint64_t)(panel >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
+constexpr uint32_t rows_step(int x) { return ((x >> 2) * 1024 + (x & 3) * 32) >> 4; }
+// ... and as one whose products run along the rows (16 rows are a step).
+template <int D>
+__device__ __forceinline__ uint64_t columns_operand(uint32_t smem) {
+  return (uint64_t)((smem & 0x3ffff) >> 4) | (uint64_t)(1024 >> 4) << 16 | (uint64_t)(D * 16 >> 4) << 32 |
          (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
+template <int D>
+constexpr uint32_t columns_step(int x) { return x * D * 32 >> 4; }
 // Sums in 32 bits; both operands half or bf16.  `along_rows`: the second operand is a columns_operand.
 constexpr uint32_t product_of(int m, int n, bool bf16, bool along_rows) {
   return 1u << 4 | (bf16 ? 1u : 0u) << 7 | (bf16 ? 1u : 0u) << 10 | (along_rows ? 1u : 0u) << 16 | (uint32_t)(n >> 3) << 17 |
          (uint32_t)(m >> 4) << 24;
+}
+// The warp's lane that issues: the same one each time.
+__device__ __forceinline__ bool elected() {
+  uint32_t is;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+  return is;
 }
 // One thread; d (+)= a b over 16 values.
 __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
@@ -144,6 +158,10 @@ __device__ __forceinline__ uint4 lds16(uint32_t p) {
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(p) : "memory");
   return v;
 }
+// The same, which the compiler may move up to the last barrier or wait.
+__device__ __forceinline__ uint4 lds16_pure(uint32_t p) {
+  return *reinterpret_cast<const uint4*>(__cvta_shared_to_generic(p));
+}
 __device__ __forceinline__ void sts16(uint32_t p, const uint4& v) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" :: "r"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
@@ -175,18 +193,19 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // ------------------------------------------------------------ a layer's rows as a tensor
-// [blocks or sequences][slots of one][channels of all heads]; a copy takes 64 channels of `slots` slots, which stand in
-// one block, as they are wanted in a panel.
+// [blocks or sequences][eights of slots][64s of channels of all heads][8 slots][64 channels]; a copy takes all channels of a
+// head of `slots` slots, which stand in one block.
 struct LayerMaps {
   CUtensorMap kv[2];
   int slots;   // 0: the layer cannot be described so; rows are copied by lanes
+  int end;     // slots of a sequence that the tensor has (a contiguous cache: eights only)
 };
 
-__device__ __forceinline__ void tma_load_rows(uint32_t dst, const CUtensorMap* map, int channel, int slot, int block,
+__device__ __forceinline__ void tma_load_rows(uint32_t dst, const CUtensorMap* map, int channels, int eight, int block,
                                               uint64_t* bar) {
   asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-      :: "r"(dst), "l"(map), "r"(channel), "r"(slot), "r"(block), "r"(smem_u32(bar)) : "memory");
+      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+      :: "r"(dst), "l"(map), "r"(0), "r"(0), "r"(channels), "r"(eight), "r"(block), "r"(smem_u32(bar)) : "memory");
 }
 
 // `most`: slots of a copy, at most (a power of two).
@@ -196,24 +215,25 @@ inline LayerMaps layer_maps(const AttnDims& dm, int layer, const KvDev& kv, int 
   const bool flat = kv.layout == EPIKV_LAYOUT_CONTIGUOUS;
   int slots = most;
   while (!flat && slots > 4 && kv.block_size % slots) slots /= 2;
-  if (slots < 8) return maps;   // a swizzled block is eight rows
+  if (slots < 8 || (flat && dm.T < 8)) return maps;
   const int64_t outer = flat ? kv.stride_seq : kv.stride_block;   // elements
   // sequences closer together than they are long: no tensor says that (see cache_maps in attention.cu)
   if (flat && kv.stride_seq / kv.stride_token < dm.T) return maps;
-  const cuuint64_t dims[3] = {(cuuint64_t)dm.H * dm.d, (cuuint64_t)(flat ? dm.T : kv.block_size),
+  const cuuint64_t dims[5] = {64, 8, (cuuint64_t)dm.H * dm.d / 64, (cuuint64_t)(flat ? dm.T : kv.block_size) / 8,
                               (cuuint64_t)(flat ? dm.S : kv.num_blocks)};
-  const cuuint64_t strides[2] = {(cuuint64_t)kv.stride_token * 2, (cuuint64_t)outer * 2};
-  for (int i = 0; i < 2; ++i)
+  const cuuint64_t strides[4] = {(cuuint64_t)kv.stride_token * 2, 128, (cuuint64_t)kv.stride_token * 16, (cuuint64_t)outer * 2};
+  for (int i = 0; i < 4; ++i)
     if (strides[i] == 0 || strides[i] >= (cuuint64_t(1) << 40)) return maps;
-  const cuuint32_t box[3] = {64, (cuuint32_t)slots, 1}, ones[3] = {1, 1, 1};
+  const cuuint32_t box[5] = {64, 8, (cuuint32_t)dm.d / 64, (cuuint32_t)slots / 8, 1}, ones[5] = {1, 1, 1, 1, 1};
   const EncodeTiled encode = encode_tiled();
   if (!encode) return maps;
   for (int w = 0; w < 2; ++w)
-    if (encode(&maps.kv[w], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, kv.base[w] + (int64_t)layer * kv.stride_layer * 2, dims,
+    if (encode(&maps.kv[w], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, kv.base[w] + (int64_t)layer * kv.stride_layer * 2, dims,
                strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
       return maps;
   maps.slots = slots;
+  maps.end = flat ? dm.T & ~7 : INT32_MAX;
   return maps;
 }
 
@@ -232,35 +252,51 @@ __device__ __forceinline__ void expand32(const uint4& codes, uint32_t scales, ui
   }
 }
 
-// A row of D bf16 queries into a tile's row.  Over a 4-bit cache they become halves, scaled by a power of two to below
-// 2^15: exact down to 2^-31 of the row's largest.  What undoes the scaling is returned.
+// A warp's 32 rows of D bf16 queries into rows `row0` to row0 + 31 of a tile; src: each lane's row, or null for zeros.  Lanes
+// beside each other load neighbouring pieces.  Over a 4-bit cache the queries become halves, scaled by a power of two to
+// below 2^15: exact down to 2^-31 of the row's largest.  What undoes the scaling of the lane's row is returned.
 template <int D, bool kHalf>
-__device__ __forceinline__ float store_query(uint32_t tile, int panel, int row, const uint4* src) {
-  if constexpr (!kHalf) {
+__device__ __forceinline__ float store_queries(uint32_t tile, int row0, const void* src, int lane) {
+  constexpr int kPer = D / 8;            // 16-byte pieces of a row: 8, 16 or 32
+  constexpr int kRows = 32 / kPer;       // rows at once
+  constexpr int kAtOnce = 16;            // loads in flight
+  const int piece = lane % kPer, sub = lane / kPer;
+  const uint64_t mine = (uint64_t)src;
+  float back = 1.f;
 #pragma unroll
-    for (int c = 0; c < D / 8; ++c)
-      sts16(tile + (c >> 3) * panel + panel_at(row, c & 7), src ? __ldg(src + c) : make_uint4(0, 0, 0, 0));
-    return 1.f;
-  } else {
-    uint32_t top = 0;   // largest magnitude, as bf16 bits: they are ordered like the values
-    if (src)
-      for (int c = 0; c < D / 8; ++c) {
-        const uint4 v = __ldg(src + c);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  for (int r0 = 0; r0 < 32 / kRows; r0 += kAtOnce) {
+    uint4 v[kAtOnce];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
-      }
-    // 2^e <= largest < 2^(e + 1); up to 2^100, so that neither factor leaves the normal numbers
-    const int up = min(14 - ((int)(top >> 7) - 127), 100);
-    const float mul = __uint_as_float((uint32_t)(up + 127) << 23);
-    for (int c = 0; c < D / 8; ++c) {
-      const uint4 v = src ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
-      sts16(tile + (c >> 3) * panel + panel_at(row, c & 7),
-            make_uint4(half_pair(bf16_lo(v.x) * mul, bf16_hi(v.x) * mul), half_pair(bf16_lo(v.y) * mul, bf16_hi(v.y) * mul),
-                       half_pair(bf16_lo(v.z) * mul, bf16_hi(v.z) * mul), half_pair(bf16_lo(v.w) * mul, bf16_hi(v.w) * mul)));
+    for (int i = 0; i < kAtOnce; ++i) {
+      if (r0 + i >= 32 / kRows) break;
+      const uint4* p = reinterpret_cast<const uint4*>(__shfl_sync(0xffffffffu, mine, (r0 + i) * kRows + sub));
+      v[i] = p ? __ldg(p + piece) : make_uint4(0, 0, 0, 0);
     }
-    return __uint_as_float((uint32_t)(127 - up) << 23);
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      if (r0 + i >= 32 / kRows) break;
+      const int row = (r0 + i) * kRows + sub;
+      uint4 x = v[i];
+      if constexpr (kHalf) {
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        uint32_t top = 0;   // largest magnitude, as bf16 bits: they are ordered like the values
+#pragma unroll
+        for (int u = 0; u < 4; ++u) top = max(top, max(w[u] & 0x7fffu, w[u] >> 16 & 0x7fffu));
+#pragma unroll
+        for (int o = kPer / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        // 2^e <= largest < 2^(e + 1); up to 2^100, so that neither factor leaves the normal numbers
+        const int up = min(14 - ((int)(top >> 7) - 127), 100);
+        const float mul = __uint_as_float((uint32_t)(up + 127) << 23);
+        // to the lane that owns the row
+        const float undo = __shfl_sync(0xffffffffu, __uint_as_float((uint32_t)(127 - up) << 23), lane % kRows * kPer);
+        if (lane / kRows == r0 + i) back = undo;
+        x = make_uint4(half_pair(bf16_lo(x.x) * mul, bf16_hi(x.x) * mul), half_pair(bf16_lo(x.y) * mul, bf16_hi(x.y) * mul),
+                       half_pair(bf16_lo(x.z) * mul, bf16_hi(x.z) * mul), half_pair(bf16_lo(x.w) * mul, bf16_hi(x.w) * mul));
+      }
+      sts16(tile + tile_at<D>(row0 + row, piece), x);
+    }
   }
+  return back;
 }
 
 }  // namespace epikv

@@ -23,9 +23,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 template <int D, int N>
 struct WeightShape {
   static constexpr int kKeys = kUnitSlots * D * 2;     // bytes of a unit's keys
-  static constexpr int kPanel = kUnitSlots * 128;
   static constexpr int kQuery = N * D * 2;
-  static constexpr int kQueryPanel = N * 128;
   static constexpr int kKeyStages = N == 16 ? (D == 64 ? 8 : D == 128 ? 5 : 2) : 2;
   static constexpr int kQueryStages = N == 16 ? kKeyStages : D == 256 ? 1 : 3;
   static constexpr int kLag = (kKeyStages < kQueryStages ? kKeyStages : kQueryStages) - 1;   // steps in flight behind the newest
@@ -45,6 +43,27 @@ struct alignas(16) WeightShared {
   int partly[Shape::kQueryStages];                     // not every row sees all slots of the unit that any sees
   float half[2][kUnitSlots];                           // a unit's sums of every second tile of rows
 };
+
+template <int D, bool kHalf>
+__device__ __forceinline__ float store_query(uint32_t tile, int row, const uint4* src) {
+  uint32_t top = 0;
+  if (src)
+    for (int c = 0; c < D / 8; ++c) {
+      const uint4 v = __ldg(src + c);
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
+    }
+  const int up = min(14 - ((int)(top >> 7) - 127), 100);
+  const float mul = __uint_as_float((uint32_t)(up + 127) << 23);
+  for (int c = 0; c < D / 8; ++c) {
+    const uint4 v = src ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+    sts16(tile + tile_at<D>(row, c),
+          make_uint4(half_pair(bf16_lo(v.x) * mul, bf16_hi(v.x) * mul), half_pair(bf16_lo(v.y) * mul, bf16_hi(v.y) * mul),
+                     half_pair(bf16_lo(v.z) * mul, bf16_hi(v.z) * mul), half_pair(bf16_lo(v.w) * mul, bf16_hi(v.w) * mul)));
+  }
+  return __uint_as_float((uint32_t)(127 - up) << 23);
+}
 
 struct WeightCall {
   int layer, causal, last, add;
@@ -112,7 +131,7 @@ __device__ __forceinline__ void copy_unit_keys(uint32_t dst, const int64_t* offs
     for (int x = tid; x < kUnitSlots * kPer; x += kCopyThreads) {
       const int r = x / kPer, c = x % kPer;
       const int64_t o = offset[r];
-      copy_async16(dst + (c >> 3) * Shape::kPanel + panel_at(r, c & 7), base + (o < 0 ? 0 : (o + kh * D + c * 8) * 2),
+      copy_async16(dst + tile_at<D>(r, c), base + (o < 0 ? 0 : (o + kh * D + c * 8) * 2),
                    o < 0 ? 0 : 16);
     }
   } else {
@@ -141,7 +160,7 @@ __device__ __forceinline__ void copy_unit_keys(uint32_t dst, const int64_t* offs
           uint4 v[4];
           expand32(codes[u], scales[u], v);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) sts16(dst + (c >> 1) * Shape::kPanel + panel_at(r, (c & 1) * 4 + k), v[k]);
+          for (int k = 0; k < 4; ++k) sts16(dst + tile_at<D>(r, c * 4 + k), v[k]);
         }
       }
     }
@@ -190,7 +209,7 @@ __device__ __forceinline__ void copy_units(char* ring, WeightShared<D, N>& sh, c
           const int r = x / kPer, c = x % kPer, at = row0 + r;
           const bool in = r < rows;
           const int token = at / dm.rep, hq = u.kh * dm.rep + at % dm.rep;
-          copy_async16(dst + (c >> 3) * Shape::kQueryPanel + panel_at(r, c & 7),
+          copy_async16(dst + tile_at<D>(r, c),
                        q.p + (in ? ((int64_t)(u.e.tok0 + token) * q.st + hq * q.sh + c * 8) * 2 : 0), in ? 16 : 0);
         }
       }
@@ -201,7 +220,7 @@ __device__ __forceinline__ void copy_units(char* ring, WeightShared<D, N>& sh, c
         const float lse = in ? __ldg(call.lse + (int64_t)(u.e.tok0 + token) * dm.Hq + hq) : -INFINITY;
         float c = call.c * mul_k;
         if constexpr (!kBf16)
-          c *= store_query<D, true>(dst, Shape::kQueryPanel, r,
+          c *= store_query<D, true>(dst, r,
                                     in ? reinterpret_cast<const uint4*>(q.p + ((int64_t)(u.e.tok0 + token) * q.st + hq * q.sh) * 2)
                                        : nullptr);
         const int seen = lse == -INFINITY ? 0 : call.causal ? u.e.len + token + 1 : u.e.len;
@@ -242,8 +261,7 @@ __device__ __forceinline__ void issue_units(uint32_t ring, WeightShared<D, N>& s
       const uint32_t a = ring + ks * Shape::kKeys, b = ring + Shape::kKeyStages * Shape::kKeys + qs * Shape::kQuery;
 #pragma unroll
       for (int x = 0; x < D / 16; ++x)
-        multiply(tmem + buf * N, rows_operand(a + (x >> 2) * Shape::kPanel + (x & 3) * 32),
-                 rows_operand(b + (x >> 2) * Shape::kQueryPanel + (x & 3) * 32), kScores, x > 0);
+        multiply(tmem + buf * N, rows_operand<D>(a) + rows_step(x), rows_operand<D>(b) + rows_step(x), kScores, x > 0);
       products_done(&sh.scores[buf]);
       products_done(&sh.query_left[qs]);
       if (k + 1 == u.steps) products_done(&sh.keys_left[ks]);
