@@ -83,8 +83,10 @@ size_t carve(const AttnDims& d, AttnState* st, char* base) {
   st->err = (int32_t*)take(4);
   st->plan = (int32_t*)take(((size_t)d.S + 1) * 4);
   st->splits = take(kAttnCtas * sizeof(ChunkSplit));
-  const size_t a = attention_part_floats(d), c = chunk_part_floats(d);   // the calls of a context follow one another
-  st->part = (float*)take((a > c ? a : c) * 4);
+  size_t floats = attention_part_floats(d);   // one of them at a time: the calls of a context follow one another
+  if (floats < chunk_part_floats(d)) floats = chunk_part_floats(d);
+  if (floats < weights_part_floats()) floats = weights_part_floats();
+  st->part = (float*)take(floats * 4);
   return align_up(off, 256);
 }
 

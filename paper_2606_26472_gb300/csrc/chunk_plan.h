@@ -64,6 +64,50 @@ EPIKV_PLAN int share_of(unsigned x, unsigned total, int ctas) {
   return c;
 }
 
+// ---- what slots receive
+// A unit is (entry, run of slots, KV head); its steps are tiles of query rows.  A slot is seen by the rows from some row on
+// (causal), so a unit has the rows from the first that sees its first slot to the last.  All units' steps stand in one line,
+// slots before heads; shares and segments as above.
+struct WeightPlan {
+  int slots, slots_log;   // of a unit
+  int rows, rows_log;     // of a step
+  int rep, causal, heads;
+  int last;               // tokens that count, 0: all
+};
+
+EPIKV_PLAN int weight_slots(const WeightPlan& p, int n, int len) { return len + (p.causal ? n : 0); }
+EPIKV_PLAN int weight_units(const WeightPlan& p, int n, int len) {
+  return (weight_slots(p, n, len) + p.slots - 1) >> p.slots_log;
+}
+// First query row of a unit.
+EPIKV_PLAN int weight_row(const WeightPlan& p, int n, int len, int unit) {
+  const int first = p.last && p.last < n ? (n - p.last) * p.rep : 0, s0 = unit << p.slots_log;
+  const int sees = p.causal && s0 > len ? (s0 - len) * p.rep : 0;
+  return sees > first ? sees : first;
+}
+// Steps of a unit: 0 where no row counts ...
+EPIKV_PLAN int weight_steps(const WeightPlan& p, int n, int len, int unit) {
+  return (n * p.rep - weight_row(p, n, len, unit) + p.rows - 1) >> p.rows_log;
+}
+// ... which still has a place in the line: its zeros are stored.
+EPIKV_PLAN int weight_places(const WeightPlan& p, int n, int len, int unit) {
+  const int t = weight_steps(p, n, len, unit);
+  return t > 1 ? t : 1;
+}
+// Units from an entry's start on that have as many places as its first.
+EPIKV_PLAN int weight_alike(const WeightPlan& p, int n, int len) {
+  const int all = weight_units(p, n, len);
+  if (!p.causal) return all;
+  const int t = (len >> p.slots_log) + 1;   // start at or before the first new slot
+  return t < all ? t : all;
+}
+EPIKV_PLAN int64_t weight_entry(const WeightPlan& p, int n, int len) {
+  const int all = weight_units(p, n, len), alike = weight_alike(p, n, len);
+  int64_t t = all ? (int64_t)alike * weight_places(p, n, len, 0) : 0;
+  for (int i = alike; i < all; ++i) t += weight_places(p, n, len, i);
+  return t * p.heads;
+}
+
 // What the second kernel joins: an item that starts in one CTA's share and does not end there.
 struct ChunkSplit {
   int there;       // 0: the CTA starts no such item

@@ -252,9 +252,27 @@ __device__ __forceinline__ void expand32(const uint4& codes, uint32_t scales, ui
   }
 }
 
+// Eight bf16 queries as halves.  The kPer lanes that hold a row scale it by a power of two to below 2^15: exact down to 2^-31
+// of the row's largest.  Returns what undoes the scaling.
+template <int kPer>
+__device__ __forceinline__ float halves_of(uint4& x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t top = 0;   // largest magnitude, as bf16 bits: they are ordered like the values
+#pragma unroll
+  for (int u = 0; u < 4; ++u) top = max(top, max(w[u] & 0x7fffu, w[u] >> 16 & 0x7fffu));
+#pragma unroll
+  for (int o = kPer / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  // 2^e <= largest < 2^(e + 1); up to 2^100, so that neither factor leaves the normal numbers
+  const int up = min(14 - ((int)(top >> 7) - 127), 100);
+  const float mul = __uint_as_float((uint32_t)(up + 127) << 23);
+  x = make_uint4(half_pair(bf16_lo(x.x) * mul, bf16_hi(x.x) * mul), half_pair(bf16_lo(x.y) * mul, bf16_hi(x.y) * mul),
+                 half_pair(bf16_lo(x.z) * mul, bf16_hi(x.z) * mul), half_pair(bf16_lo(x.w) * mul, bf16_hi(x.w) * mul));
+  return __uint_as_float((uint32_t)(127 - up) << 23);
+}
+
 // A warp's 32 rows of D bf16 queries into rows `row0` to row0 + 31 of a tile; src: each lane's row, or null for zeros.  Lanes
-// beside each other load neighbouring pieces.  Over a 4-bit cache the queries become halves, scaled by a power of two to
-// below 2^15: exact down to 2^-31 of the row's largest.  What undoes the scaling of the lane's row is returned.
+// beside each other load neighbouring pieces.  Over a 4-bit cache the queries become halves; what undoes the scaling of the
+// lane's row is returned.
 template <int D, bool kHalf>
 __device__ __forceinline__ float store_queries(uint32_t tile, int row0, const void* src, int lane) {
   constexpr int kPer = D / 8;            // 16-byte pieces of a row: 8, 16 or 32
@@ -278,20 +296,8 @@ __device__ __forceinline__ float store_queries(uint32_t tile, int row0, const vo
       const int row = (r0 + i) * kRows + sub;
       uint4 x = v[i];
       if constexpr (kHalf) {
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-        uint32_t top = 0;   // largest magnitude, as bf16 bits: they are ordered like the values
-#pragma unroll
-        for (int u = 0; u < 4; ++u) top = max(top, max(w[u] & 0x7fffu, w[u] >> 16 & 0x7fffu));
-#pragma unroll
-        for (int o = kPer / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        // 2^e <= largest < 2^(e + 1); up to 2^100, so that neither factor leaves the normal numbers
-        const int up = min(14 - ((int)(top >> 7) - 127), 100);
-        const float mul = __uint_as_float((uint32_t)(up + 127) << 23);
-        // to the lane that owns the row
-        const float undo = __shfl_sync(0xffffffffu, __uint_as_float((uint32_t)(127 - up) << 23), lane % kRows * kPer);
+        const float undo = __shfl_sync(0xffffffffu, halves_of<kPer>(x), lane % kRows * kPer);   // to the lane that owns the row
         if (lane / kRows == r0 + i) back = undo;
-        x = make_uint4(half_pair(bf16_lo(x.x) * mul, bf16_hi(x.x) * mul), half_pair(bf16_lo(x.y) * mul, bf16_hi(x.y) * mul),
-                       half_pair(bf16_lo(x.z) * mul, bf16_hi(x.z) * mul), half_pair(bf16_lo(x.w) * mul, bf16_hi(x.w) * mul));
       }
       sts16(tile + tile_at<D>(row0 + row, piece), x);
     }

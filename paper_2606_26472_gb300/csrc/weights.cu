@@ -2,413 +2,728 @@
 //
 //   w[h][slot] (+)= sum over rows r of KV head h of 2^(c q_r.k_slot - lse_r log2(e)),   c = scale log2(e)
 //
-// A unit is 128 slots of one entry and KV head.  Its products run on tcgen05
-// with the slots as the instruction's 128 rows and the query rows as its
-// columns, so that a thread owns a slot and adds up its columns: no exchange
-// between threads, and no sum that two CTAs share.  Keys stay in shared memory
-// while tiles of query rows pass by; each slot's sum is formed in the order of
-// the rows.
-#include "attn_plan.h"
+// The products run on tcgen05 with the slots as the instruction's 128 rows and
+// the query rows as its columns, so that a thread owns a slot and adds up its
+// columns: no exchange between threads, and each slot's sum is formed in the
+// order of the rows.  A unit is a run of slots of one entry and KV head: its
+// keys stay in shared memory while tiles of query rows (steps) pass by.  Two
+// forms: units of 128 slots and 16 rows a step, where a call has no more (a
+// decode step: reading the keys bounds it), and of 256 slots and 128 rows (a
+// chunk: exponentials and products).  One CTA an SM takes an equal share of all
+// units' steps (chunk_plan.h); the few units that two shares meet in are joined
+// by a second kernel, part by part.
+#include "chunk_plan.h"
 #include "kernels.h"
 #include "tensor.cuh"
 
 namespace epikv {
 namespace {
 
-constexpr int kUnitSlots = 128;
-constexpr int kWeightThreads = 384;    // 8 warps add up, one issues products, three copy
-constexpr int kCopyThreads = 96;
+constexpr int kWeightThreads = 512;
+constexpr int kQueryWarps = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 
+// N query rows a step; T tiles of 128 slots a unit, each with four warps that own its slots.
 template <int D, int N>
 struct WeightShape {
-  static constexpr int kKeys = kUnitSlots * D * 2;     // bytes of a unit's keys
-  static constexpr int kQuery = N * D * 2;
-  static constexpr int kKeyStages = N == 16 ? (D == 64 ? 8 : D == 128 ? 5 : 2) : 2;
-  static constexpr int kQueryStages = N == 16 ? kKeyStages : D == 256 ? 1 : 3;
-  static constexpr int kLag = (kKeyStages < kQueryStages ? kKeyStages : kQueryStages) - 1;   // steps in flight behind the newest
+  static constexpr int T = N == 16 ? 1 : 2;
+  static constexpr int kSlots = 128 * T;
+  static constexpr int kKeys = kSlots * D * 2;         // bytes of a unit's keys
+  static constexpr int kQuery = N * D * 2;             // of a step's rows
+  static constexpr int kKeyStages = N == 16 ? (D == 64 ? 9 : D == 128 ? 5 : 2) : D == 256 ? 1 : 2;
+  static constexpr int kQueryStages = N == 16 ? kKeyStages : D == 64 ? 4 : D == 128 ? 2 : 1;
   static constexpr int kRing = kKeyStages * kKeys + kQueryStages * kQuery;
+  static constexpr int kMmaWarp = 4 * T, kQueryWarp = kMmaWarp + 1, kKeyWarp = kQueryWarp + kQueryWarps;
+  static constexpr int kKeyWarps = kWeightThreads / 32 - kKeyWarp;   // 7 or 3
+  static constexpr int kKeyThreads = kKeyWarps * 32;
+  static constexpr uint32_t kColumns = 2 * N * T < 32 ? 32 : 2 * N * T;   // two tiles of scores for each tile of slots
+};
+
+// Where a CTA's share starts, and a walk along it.
+struct WeightStart {
+  int b, unit, kh, step;
+  Entry e;
 };
 
 template <int D, int N>
 struct alignas(16) WeightShared {
   using Shape = WeightShape<D, N>;
-  uint64_t full[Shape::kQueryStages], query_left[Shape::kQueryStages], keys_left[Shape::kKeyStages], scores[2], taken[2];
+  uint64_t keys[Shape::kKeyStages], keys_left[Shape::kKeyStages], query[Shape::kQueryStages], query_left[Shape::kQueryStages];
+  uint64_t scores[2][2], taken[2][2];
   uint32_t tmem;
   int gave_up;
-  int64_t offset[2][kUnitSlots];
-  uint8_t there[Shape::kKeyStages][kUnitSlots];        // the slot is in the view
-  float2 row[Shape::kQueryStages][N];                  // factor of the row's scores, log2 of its sum
-  int seen[Shape::kQueryStages][N];                    // slots that the row sees
-  int partly[Shape::kQueryStages];                     // not every row sees all slots of the unit that any sees
-  float half[2][kUnitSlots];                           // a unit's sums of every second tile of rows
+  uint32_t there[Shape::kKeyStages][Shape::kSlots / 32];   // the slot is in the view
+  alignas(16) float factor[Shape::kQueryStages][N];        // of a row's scores (4-bit rows; else the same for all)
+  alignas(16) float lse2[Shape::kQueryStages][N];          // minus log2 of a row's sum
+  alignas(16) int seen[Shape::kQueryStages][N];            // slots that the row sees
+  int partly[Shape::kQueryStages][kQueryWarps];            // not every row sees all slots of the unit
+  int64_t offset[2][Shape::kSlots];
+  WeightStart start;
 };
 
-template <int D, bool kHalf>
-__device__ __forceinline__ float store_query(uint32_t tile, int row, const uint4* src) {
-  uint32_t top = 0;
-  if (src)
-    for (int c = 0; c < D / 8; ++c) {
-      const uint4 v = __ldg(src + c);
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7fffu, w[i] >> 16 & 0x7fffu));
-    }
-  const int up = min(14 - ((int)(top >> 7) - 127), 100);
-  const float mul = __uint_as_float((uint32_t)(up + 127) << 23);
-  for (int c = 0; c < D / 8; ++c) {
-    const uint4 v = src ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
-    sts16(tile + tile_at<D>(row, c),
-          make_uint4(half_pair(bf16_lo(v.x) * mul, bf16_hi(v.x) * mul), half_pair(bf16_lo(v.y) * mul, bf16_hi(v.y) * mul),
-                     half_pair(bf16_lo(v.z) * mul, bf16_hi(v.z) * mul), half_pair(bf16_lo(v.w) * mul, bf16_hi(v.w) * mul)));
-  }
-  return __uint_as_float((uint32_t)(127 - up) << 23);
-}
-
 struct WeightCall {
-  int layer, causal, last, add;
+  int layer, add;
   float* w;
   int64_t stride_seq, stride_head;
   const float* lse;
   float c;
 };
 
-struct Unit {
-  int b, kh, s0;       // entry, KV head, first slot
+// A CTA's piece of a unit.
+struct WeightSegment {
   Entry e;
-  int slots;           // of the entry
-  int row0, steps;     // first query row that sees the unit, tiles of rows from there
+  int b, kh, unit;
+  int slots;        // of the entry
+  int row0;         // the segment's first query row
+  int steps;        // 0: the unit has no rows, its zeros are stored
+  bool first, last; // the unit starts, ends here
+  unsigned end;     // the line's place behind the unit
 };
 
-// Goes through the units of a CTA: every gridDim.x-th of the line of (entry, 128 slots, KV head).
-template <int N>
-struct UnitWalk {
-  const uint32_t* pre;    // [n_seq + 1] tiles before each entry
+struct WeightWalk {
+  const unsigned* pre;
   const Batch& ba;
-  const AttnDims& dm;
-  const WeightCall& call;
-  int64_t at;
-  int b = -1;
-  Entry e = {};
-  int first = 0;          // first row that counts
-  __device__ __forceinline__ UnitWalk(const uint32_t* pre_, const Batch& ba_, const AttnDims& dm_, const WeightCall& call_)
-      : pre(pre_), ba(ba_), dm(dm_), call(call_), at((int64_t)blockIdx.x - gridDim.x) {}
-  __device__ __forceinline__ bool next(Unit* u) {
-    at += gridDim.x;
-    const int64_t total = (int64_t)pre[ba.n_seq] * dm.H;
-    if (at >= total) return false;
-    const uint32_t tile = (uint32_t)(at / dm.H);
-    int nb = b < 0 ? 0 : b;
-    while (tile >= pre[nb + 1]) ++nb;
-    if (nb != b) {
-      b = nb;
-      e.tok0 = ba.cu_new[b];
-      e.n = ba.cu_new[b + 1] - e.tok0;
-      e.seq = ba.seq_ids[b];
-      e.len = ba.len[(int64_t)b * ba.len_stride];
-      first = call.last && call.last < e.n ? (e.n - call.last) * dm.rep : 0;
+  const WeightPlan& plan;
+  unsigned x, end;
+  int b, unit, kh, step, units;
+  Entry e;
+  __device__ __forceinline__ WeightWalk(const unsigned* pre_, const Batch& ba_, const WeightPlan& plan_, const WeightStart& s,
+                                        unsigned x_, unsigned end_)
+      : pre(pre_), ba(ba_), plan(plan_), x(x_), end(end_), b(s.b), unit(s.unit), kh(s.kh), step(s.step), e(s.e) {
+    units = weight_units(plan, e.n, e.len);
+  }
+  __device__ __forceinline__ bool next(WeightSegment* s) {
+    if (x >= end) return false;
+    const int places = weight_places(plan, e.n, e.len, unit), all = weight_steps(plan, e.n, e.len, unit);
+    const int take = min((unsigned)(places - step), end - x);
+    s->e = e;
+    s->b = b;
+    s->kh = kh;
+    s->unit = unit;
+    s->slots = weight_slots(plan, e.n, e.len);
+    s->row0 = weight_row(plan, e.n, e.len, unit) + (step << plan.rows_log);
+    s->steps = min(take, max(all - step, 0));
+    s->first = step == 0;
+    s->last = step + take == places;
+    s->end = x + (places - step);
+    x += take;
+    step += take;
+    if (s->last) {
+      step = 0;
+      if (++kh == plan.heads) {
+        kh = 0;
+        if (++unit == units && x < end) {
+          unit = 0;
+          do ++b;
+          while (pre[b + 1] == pre[b]);
+          e.tok0 = ba.cu_new[b];
+          e.n = ba.cu_new[b + 1] - e.tok0;
+          e.seq = ba.seq_ids[b];
+          e.len = ba.len[(int64_t)b * ba.len_stride];
+          units = weight_units(plan, e.n, e.len);
+        }
+      }
     }
-    u->b = b;
-    u->e = e;
-    u->kh = (int)(at - (int64_t)tile * dm.H);
-    u->s0 = (int)(tile - pre[b]) * kUnitSlots;
-    u->slots = e.len + (call.causal ? e.n : 0);
-    u->row0 = first;
-    if (call.causal && u->s0 > e.len) u->row0 = max(first, (u->s0 - e.len) * dm.rep);
-    u->steps = (max(e.n * dm.rep - u->row0, 0) + N - 1) / N;
     return true;
   }
 };
 
-template <int D, int FMT, int N>
-__device__ __forceinline__ void copy_unit_keys(uint32_t dst, const int64_t* offset, const AttnDims& dm, const KvDev& kv, int kh,
-                                               int tid) {
-  using Shape = WeightShape<D, N>;
-  const char* base = kv.base[0];
-  if constexpr (FMT == EPIKV_CACHE_BF16) {
-    constexpr int kPer = D / 8;
-#pragma unroll 4
-    for (int x = tid; x < kUnitSlots * kPer; x += kCopyThreads) {
-      const int r = x / kPer, c = x % kPer;
-      const int64_t o = offset[r];
-      copy_async16(dst + tile_at<D>(r, c), base + (o < 0 ? 0 : (o + kh * D + c * 8) * 2),
-                   o < 0 ? 0 : 16);
+// Places before each entry of the batch, by a warp; an entry that cannot be taken has none, nor has one that takes the sum to
+// kTooManyTiles and those behind it.
+__device__ __forceinline__ void line_up_weights(unsigned* pre, const Batch& ba, const AttnDims& dm, const WeightPlan& plan,
+                                                int32_t* err, int lane) {
+  unsigned before = 0;
+  for (int b0 = 0; b0 < ba.n_seq; b0 += 32) {
+    const int b = b0 + lane;
+    Entry e;
+    unsigned n = 0;
+    if (b < ba.n_seq && batch_entry(ba, dm, b, plan.causal, err, &e)) n = count_of(weight_entry(plan, e.n, e.len));
+    unsigned upto = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto = add_counts(upto, v);
     }
-  } else {
-    constexpr int kPer = D / 32;
-    constexpr int kAtOnce = 6;
-#pragma unroll 1
-    for (int x0 = tid; x0 < kUnitSlots * kPer; x0 += kAtOnce * kCopyThreads) {
-      uint4 codes[kAtOnce];
-      uint32_t scales[kAtOnce];
-#pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        const int x = x0 + u * kCopyThreads, r = x / kPer, c = x % kPer;
-        codes[u] = make_uint4(0, 0, 0, 0);
-        scales[u] = 0;
-        const int64_t o = x < kUnitSlots * kPer ? offset[r] : -1;
-        if (o >= 0) {
-          const char* row = base + o * 2;
-          codes[u] = *reinterpret_cast<const uint4*>(row + kh * (D / 2) + c * 16);
-          scales[u] = *reinterpret_cast<const uint16_t*>(row + scale_offset(dm, kh) + c * 2);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        const int x = x0 + u * kCopyThreads, r = x / kPer, c = x % kPer;
-        if (x < kUnitSlots * kPer) {
-          uint4 v[4];
-          expand32(codes[u], scales[u], v);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) sts16(dst + tile_at<D>(r, c * 4 + k), v[k]);
-        }
-      }
+    upto = add_counts(upto, before);
+    if (upto == kTooManyTiles && n) set_error(err, EPIKV_DEV_CAPACITY);
+    const unsigned over = __ballot_sync(0xffffffffu, upto == kTooManyTiles);
+    const unsigned kept = __shfl_sync(0xffffffffu, upto, over ? max(__ffs(over) - 2, 0) : 31);
+    const unsigned good = over == 0 ? upto : over & 1 ? before : kept;   // the last sum below the limit
+    if (upto == kTooManyTiles) upto = good;
+    if (b < ba.n_seq) pre[b + 1] = upto;
+    before = __shfl_sync(0xffffffffu, upto, 31);
+    if (over) {   // everything behind is refused too
+      for (int i = b0 + 32 + lane; i < ba.n_seq; i += 32) pre[i + 1] = before;
+      break;
     }
   }
+  if (lane == 0) pre[0] = 0;
 }
 
+// Where in the line place x is, by one thread.
+__device__ __forceinline__ void find_place(WeightStart* s, unsigned x, const unsigned* pre, const Batch& ba,
+                                           const WeightPlan& plan) {
+  int lo = 0, hi = ba.n_seq - 1;   // the entry with pre[b] <= x < pre[b + 1]
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (x < pre[mid + 1]) hi = mid;
+    else lo = mid + 1;
+  }
+  Entry e;
+  e.tok0 = ba.cu_new[lo];
+  e.n = ba.cu_new[lo + 1] - e.tok0;
+  e.seq = ba.seq_ids[lo];
+  e.len = ba.len[(int64_t)lo * ba.len_stride];
+  unsigned at = x - pre[lo];
+  const int alike = weight_alike(plan, e.n, e.len), last = weight_units(plan, e.n, e.len) - 1;
+  unsigned wide = (unsigned)weight_places(plan, e.n, e.len, 0) * plan.heads;
+  int unit = min((int)(at / wide), alike);
+  at -= unit * wide;
+  for (; unit < last; ++unit) {
+    wide = (unsigned)weight_places(plan, e.n, e.len, unit) * plan.heads;
+    if (at < wide) break;
+    at -= wide;
+  }
+  const unsigned places = (unsigned)weight_places(plan, e.n, e.len, unit);
+  s->b = lo;
+  s->unit = unit;
+  s->kh = (int)(at / places);
+  s->step = (int)(at % places);
+  s->e = e;
+}
+
+// ------------------------------------------------------------------ keys
 template <int D, int FMT, int N>
-__device__ __forceinline__ void copy_units(char* ring, WeightShared<D, N>& sh, const TensorWaiter& wait, const AttnState& st,
-                                           const AttnDims& dm, const WeightCall& call, const Rows& q, const KvDev& kv,
-                                           UnitWalk<N> walk, int tid) {
+struct KeyCopier {
   using Shape = WeightShape<D, N>;
-  constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
-  Unit u;
-  int step = 0, unit = 0;   // counted over the CTA's units that have steps
-  auto deliver = [&](int i) {
-    fence_proxy_async_smem();
-    mbar_arrive_one(&sh.full[i % Shape::kQueryStages]);
+  static constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
+  static constexpr int kThreads = Shape::kKeyThreads, kPer = kBf16 ? D / 8 : D / 32;   // 16-byte pieces of a head's row in the cache
+  enum {
+    kPieces = Shape::kSlots * kPer,
+    kAtOnce = (kPieces + kThreads - 1) / kThreads < 6 ? (kPieces + kThreads - 1) / kThreads : 6,
+    kAhead = kAtOnce * kThreads >= kPieces,   // a unit's codes are read while the last one's become halves
+    kLag = Shape::kKeyStages - 1 < 3 ? Shape::kKeyStages - 1 : 3,   // units in flight behind the newest
   };
-  while (walk.next(&u)) {
-    if (u.steps == 0) continue;
-    const int ks = unit % Shape::kKeyStages;
-    int64_t* offset = sh.offset[unit & 1];
-    if (unit >= Shape::kKeyStages) wait(&sh.keys_left[ks], (uint32_t)(unit / Shape::kKeyStages - 1) & 1);
-    for (int r = tid; r < kUnitSlots; r += kCopyThreads) {
-      const int s = u.s0 + r;
+  char* ring;
+  WeightShared<D, N>& sh;
+  const TensorWaiter& wait;
+  const AttnDims& dm;
+  const KvDev& kv;
+  const LayerMaps& maps;
+  int layer;
+  int32_t* err;
+  int tid, lane, warp;
+
+  __device__ __forceinline__ uint32_t stage(int i) const { return smem_u32(ring + i % Shape::kKeyStages * Shape::kKeys); }
+  __device__ __forceinline__ void left(int i) const {
+    if (i >= Shape::kKeyStages) wait(&sh.keys_left[i % Shape::kKeyStages], (uint32_t)(i / Shape::kKeyStages - 1) & 1);
+  }
+  __device__ __forceinline__ void deliver(int i) const {
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive_one(&sh.keys[i % Shape::kKeyStages]);
+  }
+  // Element offsets of a unit's slots (-1: none) and which of them are there, for all key threads.
+  __device__ __forceinline__ void offsets(int64_t* offset, const WeightSegment& g) const {
+    const int s0 = g.unit * Shape::kSlots;
+    for (int r = tid; r < Shape::kSlots; r += kThreads) {
       int64_t o = -1;
-      if (s < u.slots) {
-        o = kv_row_offset(kv, call.layer, u.e.seq, s, dm.T);
-        if (o < 0) set_error(st.err, EPIKV_DEV_SLOT);
+      if (s0 + r < g.slots) {
+        o = kv_row_offset(kv, layer, g.e.seq, s0 + r, dm.T);
+        if (o < 0) set_error(err, EPIKV_DEV_SLOT);
       }
       offset[r] = o;
-      sh.there[ks][r] = o >= 0;
     }
-    named_sync(1, kCopyThreads);
-    const float mul_k = kBf16 ? 1.f : head_scale(st, dm, 0, call.layer, u.kh);
-    for (int k = 0; k < u.steps; ++k, ++step) {
-      const int qs = step % Shape::kQueryStages, row0 = u.row0 + k * N;
-      if (step >= Shape::kQueryStages) wait(&sh.query_left[qs], (uint32_t)(step / Shape::kQueryStages - 1) & 1);
-      if (k == 0) copy_unit_keys<D, FMT, N>(smem_u32(ring + ks * Shape::kKeys), offset, dm, kv, u.kh, tid);
-      const uint32_t dst = smem_u32(ring + Shape::kKeyStages * Shape::kKeys + qs * Shape::kQuery);
-      const int rows = min(u.e.n * dm.rep - row0, N);
-      if constexpr (kBf16) {
-        constexpr int kPer = D / 8;
-#pragma unroll 4
-        for (int x = tid; x < N * kPer; x += kCopyThreads) {
-          const int r = x / kPer, c = x % kPer, at = row0 + r;
-          const bool in = r < rows;
-          const int token = at / dm.rep, hq = u.kh * dm.rep + at % dm.rep;
-          copy_async16(dst + tile_at<D>(r, c),
-                       q.p + (in ? ((int64_t)(u.e.tok0 + token) * q.st + hq * q.sh + c * 8) * 2 : 0), in ? 16 : 0);
+    named_sync(1, kThreads);
+  }
+  __device__ __forceinline__ void mark(int i, const int64_t* offset) const {   // (a warp's 32 slots a word)
+    for (int w = warp; w < Shape::kSlots / 32; w += Shape::kKeyWarps) {
+      const uint32_t in = offset ? __ballot_sync(0xffffffffu, offset[w * 32 + lane] >= 0) : 0xffffffffu;
+      if (lane == 0) sh.there[i % Shape::kKeyStages][w] = in;
+    }
+  }
+
+  __device__ __forceinline__ void run_bf16(WeightWalk walk) const {
+    const bool flat = kv.layout == EPIKV_LAYOUT_CONTIGUOUS;
+    int i = 0, pending = 0, tables = 0, unit = -1, b = -1;
+    int64_t* offset = sh.offset[0];
+    int y = 0, z = 0;
+    bool whole = false, known = false;
+    WeightSegment g;
+    while (walk.next(&g)) {
+      if (g.steps == 0) continue;
+      const int s0 = g.unit * Shape::kSlots;
+      if (g.unit != unit || g.b != b) {   // the heads of the same slots follow one another
+        unit = g.unit;
+        b = g.b;
+        known = false;
+        whole = maps.slots && min(s0 + Shape::kSlots, g.slots) <= maps.end;
+        if (whole) {
+          y = s0 + lane * maps.slots;
+          z = g.e.seq;
+          bool there = true;
+          if (!flat && y < g.slots && lane * maps.slots < Shape::kSlots) {
+            const int bi = y / kv.block_size;
+            y -= bi * kv.block_size;
+            z = bi < kv.max_blocks
+                    ? __ldg(kv.block_table + (int64_t)layer * kv.table_stride_layer + (int64_t)g.e.seq * kv.max_blocks + bi)
+                    : -1;
+            there = z >= 0 && z < kv.num_blocks;
+          }
+          whole = __all_sync(0xffffffffu, there);   // else by lanes, which report it
         }
       }
-      bool partly = false;
-      for (int r = tid; r < N; r += kCopyThreads) {
-        const bool in = r < rows;
-        const int at = row0 + r, token = at / dm.rep, hq = u.kh * dm.rep + at % dm.rep;
-        const float lse = in ? __ldg(call.lse + (int64_t)(u.e.tok0 + token) * dm.Hq + hq) : -INFINITY;
-        float c = call.c * mul_k;
-        if constexpr (!kBf16)
-          c *= store_query<D, true>(dst, r,
-                                    in ? reinterpret_cast<const uint4*>(q.p + ((int64_t)(u.e.tok0 + token) * q.st + hq * q.sh) * 2)
-                                       : nullptr);
-        const int seen = lse == -INFINITY ? 0 : call.causal ? u.e.len + token + 1 : u.e.len;
-        sh.row[qs][r] = make_float2(c, lse * kLog2e);
-        sh.seen[qs][r] = seen;
-        partly |= seen < min(u.s0 + kUnitSlots, u.slots);
+      if (whole) {
+        if (pending) {
+          copy_wait<0>();
+          for (; pending > 0; --pending) deliver(i - pending);
+        }
+        left(i);
+        mark(i, nullptr);
+        uint64_t* bar = &sh.keys[i % Shape::kKeyStages];
+        if (warp == 0) {
+          const int slots = min(Shape::kSlots, (g.slots - s0 + maps.slots - 1) & -maps.slots);   // that come
+          if (lane == 0) mbar_arrive_expect_tx(bar, slots * D * 2);
+          __syncwarp();
+          if (lane * maps.slots < slots)
+            tma_load_rows(stage(i) + lane * maps.slots * (D * 2), &maps.kv[0], g.kh * (D / 64), y >> 3, z, bar);
+        } else if (lane == 0) {
+          mbar_arrive_one(bar);
+        }
+        __syncwarp();
+        ++i;
+        continue;
       }
-      if (tid == 0) sh.partly[qs] = 0;
-      named_sync(1, kCopyThreads);
-      if (partly) sh.partly[qs] = 1;
+      if (!known) {   // the table before may still be read: two take turns, and all threads were here for the last one
+        offset = sh.offset[tables++ & 1];
+        offsets(offset, g);
+        known = true;
+      }
+      left(i);
+      mark(i, offset);
+      const uint32_t dst = stage(i);
+      constexpr int kRound = 8;
+      for (int x0 = tid; x0 < kPieces; x0 += kRound * kThreads) {
+        int64_t o[kRound];
+#pragma unroll
+        for (int u = 0; u < kRound; ++u) o[u] = offset[min((x0 + u * kThreads) / kPer, Shape::kSlots - 1)];
+#pragma unroll
+        for (int u = 0; u < kRound; ++u) {
+          const int x = x0 + u * kThreads, r = x / kPer, c = x % kPer;
+          if (x < kPieces)
+            copy_async16(dst + tile_at<D>(r, c), kv.base[0] + (o[u] < 0 ? 0 : (o[u] + g.kh * D + c * 8) * 2), o[u] < 0 ? 0 : 16);
+        }
+      }
       copy_commit();
-      if (step >= Shape::kLag) {
-        copy_wait<Shape::kLag>();
-        deliver(step - Shape::kLag);
+      ++i;
+      if (++pending > kLag) {
+        copy_wait<kLag>();
+        deliver(i - pending);
+        --pending;
       }
     }
-    ++unit;
+    copy_wait<0>();
+    for (; pending > 0; --pending) deliver(i - pending);
+    if (*wait.gave_up && warp == 0)   // the CTA may not end before its copies have landed
+      for (int k = max(0, i - Shape::kKeyStages); k < i; ++k)
+        mbar_wait_bounded(&sh.keys[k % Shape::kKeyStages], (uint32_t)(k / Shape::kKeyStages) & 1, kTensorWaitNs);
   }
-  copy_wait<0>();
-  for (int i = max(step - Shape::kLag, 0); i < step; ++i) deliver(i);
+
+  struct Codes {
+    uint4 code[kAtOnce];
+    uint32_t scale[kAtOnce];
+  };
+  __device__ __forceinline__ void load(Codes& c, const int64_t* offset, int kh, int x0) const {
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int x = x0 + u * kThreads, r = x / kPer, p = x % kPer;
+      c.code[u] = make_uint4(0, 0, 0, 0);
+      c.scale[u] = 0;
+      const int64_t o = x < kPieces ? offset[r] : -1;
+      if (o >= 0) {
+        const char* row = kv.base[0] + o * 2;
+        c.code[u] = *reinterpret_cast<const uint4*>(row + kh * (D / 2) + p * 16);
+        c.scale[u] = *reinterpret_cast<const uint16_t*>(row + scale_offset(dm, kh) + p * 2);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(const Codes& c, uint32_t dst, int x0) const {
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int x = x0 + u * kThreads, r = x / kPer, p = x % kPer;
+      if (x < kPieces) {
+        uint4 v[4];
+        expand32(c.code[u], c.scale[u], v);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sts16(dst + tile_at<D>(r, p * 4 + k), v[k]);
+      }
+    }
+  }
+  // 4-bit rows: a unit's codes are under way while the one before becomes halves.
+  __device__ __forceinline__ void run_q4(WeightWalk walk) const {
+    int i = 0, tables = 0, unit = -1, b = -1;
+    const int64_t* offset = sh.offset[0];
+    WeightSegment g;
+    auto ahead = [&] {   // the next segment with rows, and its slots' offsets
+      while (walk.next(&g)) {
+        if (g.steps == 0) continue;
+        if (g.unit != unit || g.b != b) {
+          unit = g.unit;
+          b = g.b;
+          int64_t* o = sh.offset[tables++ & 1];
+          offsets(o, g);
+          offset = o;
+        }
+        return true;
+      }
+      return false;
+    };
+    bool more = ahead();
+    if constexpr (kAhead) {
+      Codes now, next;
+      if (more) load(next, offset, g.kh, tid);
+      while (more) {
+        now = next;
+        const int64_t* mine = offset;
+        left(i);
+        mark(i, mine);
+        more = ahead();
+        if (more) load(next, offset, g.kh, tid);
+        store(now, stage(i), tid);
+        deliver(i++);
+      }
+    } else {
+      while (more) {
+        left(i);
+        mark(i, offset);
+        for (int x0 = tid; x0 < kPieces; x0 += kAtOnce * kThreads) {
+          Codes c;
+          load(c, offset, g.kh, x0);
+          store(c, stage(i), x0);
+        }
+        deliver(i++);
+        more = ahead();
+      }
+    }
+  }
+};
+
+// ------------------------------------------------------------------ query rows
+// Warp w of four brings rows w N/4 .. of each step; a step's rows are under way while the one before is stored.
+template <int D, int FMT, int N>
+__device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh, const TensorWaiter& wait, const AttnState& st,
+                                             const AttnDims& dm, const WeightCall& call, const Rows& q, WeightWalk walk,
+                                             int warp, int lane) {
+  using Shape = WeightShape<D, N>;
+  constexpr bool kHalf = FMT != EPIKV_CACHE_BF16;
+  constexpr int R = N / kQueryWarps;                     // rows of the warp
+  constexpr int kPer = D / 8, kRows = 32 / kPer;         // pieces of a row; rows at once
+  constexpr int kLoads = (R + kRows - 1) / kRows;
+  constexpr int kBatch = kLoads < 16 ? kLoads : 16;      // loads in flight
+  const int piece = lane % kPer, sub = lane / kPer;
+  WeightSegment g = {};
+  int k = 0;
+  struct Row {
+    uint64_t src;    // lane's row, or 0
+    float lse;
+    int seen;
+    bool in;
+  };
+  auto row_of = [&](int step) {
+    Row r;
+    const int at = g.row0 + step * N + warp * R + lane, token = at / dm.rep, hq = g.kh * dm.rep + at % dm.rep;
+    r.in = lane < R && at < g.e.n * dm.rep;
+    r.src = r.in ? (uint64_t)(q.p + ((int64_t)(g.e.tok0 + token) * q.st + hq * q.sh) * 2) : 0;
+    r.lse = r.in ? __ldg(call.lse + (int64_t)(g.e.tok0 + token) * dm.Hq + hq) : -INFINITY;
+    r.seen = walk.plan.causal ? g.e.len + token + 1 : g.e.len;
+    return r;
+  };
+  auto load = [&](uint4 (&v)[kBatch], const Row& r, int l0) {
+#pragma unroll
+    for (int l = 0; l < kBatch; ++l) {
+      const int row = (l0 + l) * kRows + sub;
+      const uint4* p = reinterpret_cast<const uint4*>(__shfl_sync(0xffffffffu, r.src, row & 31));
+      v[l] = p && row < R ? __ldg(p + piece) : make_uint4(0, 0, 0, 0);
+    }
+  };
+  auto advance = [&] {   // to the next step; false at the share's end
+    if (k + 1 < g.steps) {
+      ++k;
+      return true;
+    }
+    k = 0;
+    do {
+      if (!walk.next(&g)) return false;
+    } while (g.steps == 0);
+    return true;
+  };
+  bool more = advance();
+  Row next = {}, now;
+  uint4 v[kBatch];
+  if (more) {
+    next = row_of(k);
+    load(v, next, 0);
+  }
+  for (int step = 0; more; ++step) {
+    now = next;
+    const int qs = step % Shape::kQueryStages;
+    const int upto = min(g.unit * Shape::kSlots + Shape::kSlots, g.slots);
+    const float scale = kHalf ? call.c * head_scale(st, dm, 0, call.layer, g.kh) : call.c;
+    if (step >= Shape::kQueryStages) wait(&sh.query_left[qs], (uint32_t)(step / Shape::kQueryStages - 1) & 1);
+    const uint32_t dst = smem_u32(ring + Shape::kKeyStages * Shape::kKeys + qs * Shape::kQuery);
+    float back = 1.f;
+#pragma unroll
+    for (int l0 = 0; l0 < kLoads; l0 += kBatch) {
+      if (l0) load(v, now, l0);
+#pragma unroll
+      for (int l = 0; l < kBatch; ++l) {
+        const int row = (l0 + l) * kRows + sub;
+        uint4 x = v[l];
+        if constexpr (kHalf) {
+          const float undo = halves_of<kPer>(x);   // of the row that the lane's piece is of
+          const float mine = __shfl_sync(0xffffffffu, undo, lane % kRows * kPer);
+          if (lane / kRows == l0 + l) back = mine;
+        }
+        if (row < R) sts16(dst + tile_at<D>(warp * R + row, piece), x);
+      }
+    }
+    if (lane < R) {
+      const bool counts = now.lse != -INFINITY;   // else the row saw nothing
+      sh.lse2[qs][warp * R + lane] = -now.lse * kLog2e;
+      sh.factor[qs][warp * R + lane] = scale * back;
+      sh.seen[qs][warp * R + lane] = counts ? now.seen : 0;
+    }
+    const bool partly = __any_sync(0xffffffffu, lane < R && (now.lse == -INFINITY || now.seen < upto));
+    if (lane == 0) sh.partly[qs][warp] = partly;
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive_one(&sh.query[qs]);
+    more = advance();
+    if (more) {
+      next = row_of(k);
+      load(v, next, 0);
+    }
+  }
 }
 
+// ------------------------------------------------------------------ products
 template <int D, int FMT, int N>
-__device__ __forceinline__ void issue_units(uint32_t ring, WeightShared<D, N>& sh, const TensorWaiter& wait, UnitWalk<N> walk,
+__device__ __forceinline__ void issue_units(uint32_t ring, WeightShared<D, N>& sh, const TensorWaiter& wait, WeightWalk walk,
                                             uint32_t tmem) {
   using Shape = WeightShape<D, N>;
   constexpr uint32_t kScores = product_of(128, N, FMT == EPIKV_CACHE_BF16, false);
-  Unit u;
-  int step = 0, unit = 0;
-  while (walk.next(&u)) {
-    if (u.steps == 0) continue;
-    const int ks = unit % Shape::kKeyStages;
-    for (int k = 0; k < u.steps; ++k, ++step) {
+  const uint64_t k0 = rows_operand<D>(ring), q0 = rows_operand<D>(ring + Shape::kKeyStages * Shape::kKeys);
+  WeightSegment g;
+  int step = 0;
+  for (int i = 0; walk.next(&g);) {
+    const int steps = __shfl_sync(0xffffffffu, g.steps, 0);
+    if (steps == 0) continue;
+    const int ks = i % Shape::kKeyStages;
+    wait(&sh.keys[ks], (uint32_t)(i / Shape::kKeyStages) & 1);
+    for (int k = 0; k < steps; ++k, ++step) {
       const int qs = step % Shape::kQueryStages, buf = step & 1;
-      wait(&sh.full[qs], (uint32_t)(step / Shape::kQueryStages) & 1);
-      if (step >= 2) wait(&sh.taken[buf], (uint32_t)(step / 2 - 1) & 1);
-      tensor_fence_after();
-      const uint32_t a = ring + ks * Shape::kKeys, b = ring + Shape::kKeyStages * Shape::kKeys + qs * Shape::kQuery;
+      wait(&sh.query[qs], (uint32_t)(step / Shape::kQueryStages) & 1);
+      const uint64_t b = q0 + (uint32_t)(qs * (Shape::kQuery >> 4));
 #pragma unroll
-      for (int x = 0; x < D / 16; ++x)
-        multiply(tmem + buf * N, rows_operand<D>(a) + rows_step(x), rows_operand<D>(b) + rows_step(x), kScores, x > 0);
-      products_done(&sh.scores[buf]);
-      products_done(&sh.query_left[qs]);
-      if (k + 1 == u.steps) products_done(&sh.keys_left[ks]);
+      for (int t = 0; t < Shape::T; ++t) {
+        const uint64_t a = k0 + (uint32_t)(ks * (Shape::kKeys >> 4) + t * (128 * D * 2 >> 4));
+        if (step >= 2) wait(&sh.taken[t][buf], (uint32_t)(step / 2 - 1) & 1);
+        tensor_fence_after();
+        if (elected()) {
+#pragma unroll
+          for (int x = 0; x < D / 16; ++x)
+            multiply(tmem + (2 * t + buf) * N, a + rows_step(x), b + rows_step(x), kScores, x > 0);
+          products_done(&sh.scores[t][buf]);
+          if (t + 1 == Shape::T) {
+            products_done(&sh.query_left[qs]);
+            if (k + 1 == steps) products_done(&sh.keys_left[ks]);
+          }
+        }
+        __syncwarp();
+      }
     }
-    ++unit;
+    ++i;
   }
 }
 
-template <int D, int N>
-__device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaiter& wait, const AttnDims& dm,
-                                       const WeightCall& call, UnitWalk<N> walk, uint32_t tmem, int group, int tid) {
+// ------------------------------------------------------------------ sums
+template <int D, int FMT, int N>
+__device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaiter& wait, const WeightCall& call, float* part0,
+                                       float* part1, ChunkSplit* split, unsigned total, int ctas, WeightWalk walk,
+                                       uint32_t tmem, int t, int tid) {
   using Shape = WeightShape<D, N>;
-  Unit u;
-  int step = 0, unit = 0, joint = 0;
-  const int lane = tid & 31;
-  while (walk.next(&u)) {
-    float* to = call.w + u.e.seq * call.stride_seq + u.kh * call.stride_head + u.s0 + tid;
-    const int s = u.s0 + tid;
-    if (u.steps == 0) {
-      if (group == 0 && s < u.slots && !call.add) *to = 0.f;
+  constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
+  constexpr int kRound = N < 32 ? N : 32;   // columns at once
+  WeightSegment g;
+  int step = 0;
+  const int lane = tid & 31, own = t * 128 + tid;
+  for (int i = 0; walk.next(&g);) {
+    const int s = g.unit * Shape::kSlots + own;
+    float* to = call.w + g.e.seq * call.stride_seq + g.kh * call.stride_head + s;
+    const bool alone = g.first && g.last, mine = s < g.slots;
+    float old = 0.f;   // on its way while the scores are formed
+    if (call.add && alone && mine) old = *to;
+    if (g.steps == 0) {
+      if (mine && !call.add) *to = 0.f;
       continue;
     }
-    const int ks = unit % Shape::kKeyStages;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < u.steps; ++k, ++step) {
+    const int ks = i % Shape::kKeyStages;
+    f32x2 sum[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
+    for (int k = 0; k < g.steps; ++k, ++step) {
       const int qs = step % Shape::kQueryStages, buf = step & 1;
-      if (buf != group) continue;   // the two groups take tiles of rows in turn
-      wait(&sh.scores[buf], (uint32_t)(step / 2) & 1);
+      wait(&sh.scores[t][buf], (uint32_t)(step / 2) & 1);
       tensor_fence_after();
-      uint32_t x[N];
-      if constexpr (N == 16) {
-        tmem_load16(tmem + buf * N, x);
-      } else {
+      const float4* lse2 = reinterpret_cast<const float4*>(sh.lse2[qs]);
+      const float4* factor = reinterpret_cast<const float4*>(sh.factor[qs]);
+      bool partly = false;
 #pragma unroll
-        for (int i = 0; i < N; i += 32) tmem_load32(tmem + buf * N + i, x + i);
-      }
-      tmem_wait_load();
-      tensor_fence_before();
-      mbar_arrive_one(&sh.taken[buf]);
-      const float2* row = sh.row[qs];
-      if (!sh.partly[qs]) {
+      for (int w = 0; w < kQueryWarps; ++w) partly |= sh.partly[qs][w] != 0;
 #pragma unroll
-        for (int i = 0; i < N; ++i) sum[i & 3] += exp2_fast(__uint_as_float(x[i]) * row[i].x - row[i].y);
-      } else {
+      for (int i0 = 0; i0 < N; i0 += kRound) {
+        uint32_t x[kRound];
+        if constexpr (kRound == 16) tmem_load16(tmem + (2 * t + buf) * N + i0, x);
+        else tmem_load32(tmem + (2 * t + buf) * N + i0, x);
+        tmem_wait_load();
+        if (i0 + kRound == N) {
+          tensor_fence_before();
+          mbar_arrive_one(&sh.taken[t][buf]);
+        }
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const float p = exp2_fast(__uint_as_float(x[i]) * row[i].x - row[i].y);
-          sum[i & 3] += s < sh.seen[qs][i] ? p : 0.f;
+        for (int j = 0; j < kRound; j += 4) {
+          const float4 l = lse2[(i0 + j) / 4];
+          const float4 f = kBf16 ? make_float4(call.c, call.c, call.c, call.c) : factor[(i0 + j) / 4];
+          const f32x2 a = f2_fma(f2_pack(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), f2_pack(f.x, f.y), f2_pack(l.x, l.y));
+          const f32x2 b = f2_fma(f2_pack(__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])), f2_pack(f.z, f.w), f2_pack(l.z, l.w));
+          float p[4] = {exp2_fast(f2_lo(a)), exp2_fast(f2_hi(a)), exp2_fast(f2_lo(b)), exp2_fast(f2_hi(b))};
+          if (partly) {
+            const int4 e = reinterpret_cast<const int4*>(sh.seen[qs])[(i0 + j) / 4];
+            p[0] = s < e.x ? p[0] : 0.f;
+            p[1] = s < e.y ? p[1] : 0.f;
+            p[2] = s < e.z ? p[2] : 0.f;
+            p[3] = s < e.w ? p[3] : 0.f;
+          }
+          sum[0] = f2_add(sum[0], f2_pack(p[0], p[1]));
+          sum[1] = f2_add(sum[1], f2_pack(p[2], p[3]));
         }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive_one(&sh.query_left[qs]);
     }
-    float w = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    bool mine = ((step - 1) & 1) == group;   // the group of the last tile writes
-    if (u.steps > 1) {
-      if (!mine) sh.half[joint & 1][tid] = w;
-      named_sync(2, 256);
-      if (mine) w += sh.half[joint & 1][tid];
-      ++joint;
+    const f32x2 both = f2_add(sum[0], sum[1]);
+    float w = f2_lo(both) + f2_hi(both);
+    const bool there = sh.there[ks][own / 32] >> lane & 1;
+    __syncwarp();
+    if (lane == 0) mbar_arrive_one(&sh.keys_left[ks]);
+    if (!there) w = 0.f;
+    if (alone) {
+      if (mine) *to = old + w;
+    } else {   // a part for the second kernel
+      (g.first ? part1 : part0)[own] = w;
+      if (own == 0 && g.first)
+        *split = {1, g.b, g.kh, g.unit * Shape::kSlots, min(Shape::kSlots, g.slots - g.unit * Shape::kSlots),
+                  share_of(g.end - 1, total, ctas) - (int)blockIdx.x + 1, {0, 0}};
     }
-    if (mine) {
-      const bool there = sh.there[ks][tid];
-      __syncwarp();
-      if (lane == 0) mbar_arrive_one(&sh.keys_left[ks]);
-      if (s < u.slots) {
-        if (!there) w = 0.f;
-        *to = call.add ? *to + w : w;
-      }
-    }
-    ++unit;
+    ++i;
   }
 }
 
 template <int D, int FMT, int N>
 __global__ void __launch_bounds__(kWeightThreads, 1)
-    weights_kernel(AttnState st, AttnDims dm, Batch ba, WeightCall call, Rows q, KvDev kv) {
+    weights_kernel(AttnState st, AttnDims dm, WeightPlan plan, Batch ba, WeightCall call, Rows q, KvDev kv,
+                   const __grid_constant__ LayerMaps maps) {
   using Shape = WeightShape<D, N>;
   extern __shared__ char dynamic[];
   char* ring = dynamic + ((1024 - (smem_u32(dynamic) & 1023)) & 1023);
-  uint32_t* pre = reinterpret_cast<uint32_t*>(ring + Shape::kRing);
+  unsigned* pre = reinterpret_cast<unsigned*>(ring + Shape::kRing);
   __shared__ WeightShared<D, N> sh;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  constexpr uint32_t kColumns = 2 * N < 32 ? 32 : 2 * N;
-  if (warp == 8) tmem_alloc(&sh.tmem, kColumns);
+  if (warp == Shape::kMmaWarp) tmem_alloc(&sh.tmem, Shape::kColumns);
   if (tid == 0) {
     for (int i = 0; i < Shape::kQueryStages; ++i) {
-      mbar_init(&sh.full[i], kCopyThreads);
-      mbar_init(&sh.query_left[i], 1 + 4);
+      mbar_init(&sh.query[i], kQueryWarps);
+      mbar_init(&sh.query_left[i], 1 + 4 * Shape::T);
     }
-    for (int i = 0; i < Shape::kKeyStages; ++i) mbar_init(&sh.keys_left[i], 1 + 4);
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh.scores[i], 1);
-      mbar_init(&sh.taken[i], 128);
+    for (int i = 0; i < Shape::kKeyStages; ++i) {
+      mbar_init(&sh.keys[i], Shape::kKeyWarps);
+      mbar_init(&sh.keys_left[i], 1 + 4 * Shape::T);
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&sh.scores[i >> 1][i & 1], 1);
+      mbar_init(&sh.taken[i >> 1][i & 1], 128);
     }
     sh.gave_up = 0;
     fence_barrier_init();
   }
   pdl_wait();
   pdl_trigger();
-  if (warp == 0) {   // tiles before each entry; an entry that cannot be taken has none
-    uint32_t before = 0;
-    for (int b0 = 0; b0 < ba.n_seq; b0 += 32) {
-      uint32_t n = 0;
-      Entry e;
-      if (b0 + lane < ba.n_seq && batch_entry(ba, dm, b0 + lane, call.causal, st.err, &e))
-        n = (e.len + (call.causal ? e.n : 0) + kUnitSlots - 1) / kUnitSlots;
-      uint32_t upto = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += v;
-      }
-      if (b0 + lane < ba.n_seq) pre[b0 + lane + 1] = before + upto;
-      before += __shfl_sync(0xffffffffu, upto, 31);
+  ChunkSplit* split = reinterpret_cast<ChunkSplit*>(st.splits) + blockIdx.x;
+  if (warp == 0) {
+    line_up_weights(pre, ba, dm, plan, st.err, lane);
+    __syncwarp();
+    const unsigned total = pre[ba.n_seq];
+    const int ctas = (int)min(total, (unsigned)kAttnCtas);
+    if (lane == 0) {
+      *split = {};
+      if ((int)blockIdx.x < ctas) find_place(&sh.start, share_start(blockIdx.x, total, ctas), pre, ba, plan);
     }
-    if (lane == 0) pre[0] = 0;
   }
   tensor_fence_before();
   __syncthreads();
   tensor_fence_after();
   const uint32_t tmem = sh.tmem;
-  const TensorWaiter wait{&sh.gave_up, st.err};
-  const UnitWalk<N> walk(pre, ba, dm, call);
-  if (warp < 8) {
-    add_up<D, N>(sh, wait, dm, call, walk, tmem + ((uint32_t)(warp & 3) << 21), warp >> 2, tid & 127);
-  } else if (warp == 8) {
-    if (lane == 0) issue_units<D, FMT, N>(smem_u32(ring), sh, wait, walk, tmem);
-    __syncwarp();
-  } else {
-    copy_units<D, FMT, N>(ring, sh, wait, st, dm, call, q, kv, walk, tid - 288);
+  const unsigned total = pre[ba.n_seq];
+  const int cta = blockIdx.x, ctas = (int)min(total, (unsigned)kAttnCtas);
+  if (cta < ctas) {
+    const TensorWaiter wait{&sh.gave_up, st.err};
+    const WeightWalk walk(pre, ba, plan, sh.start, share_start(cta, total, ctas), share_start(cta + 1, total, ctas));
+    if (warp < Shape::kMmaWarp) {
+      float* part = st.part + (int64_t)cta * 2 * Shape::kSlots;
+      add_up<D, FMT, N>(sh, wait, call, part, part + Shape::kSlots, split, total, ctas, walk,
+                        tmem + ((uint32_t)(warp & 3) << 21), warp >> 2, tid & 127);
+    } else if (warp == Shape::kMmaWarp) {
+      issue_units<D, FMT, N>(smem_u32(ring), sh, wait, walk, tmem);
+    } else if (warp < Shape::kKeyWarp) {
+      copy_queries<D, FMT, N>(ring, sh, wait, st, dm, call, q, walk, warp - Shape::kQueryWarp, lane);
+    } else {
+      const KeyCopier<D, FMT, N> copier{ring, sh, wait, dm, kv, maps, call.layer, st.err, tid - Shape::kKeyWarp * 32, lane,
+                                        warp - Shape::kKeyWarp};
+      if constexpr (FMT == EPIKV_CACHE_BF16) copier.run_bf16(walk);
+      else copier.run_q4(walk);
+    }
   }
   tensor_fence_before();
   __syncthreads();
   tensor_fence_after();
-  if (warp == 8) tmem_free(tmem, kColumns);
+  if (warp == Shape::kMmaWarp) tmem_free(tmem, Shape::kColumns);
+}
+
+// Joins the parts of a unit that several shares hold, in their order.  A CTA for each share that starts such a unit; a
+// thread a slot.
+__global__ void __launch_bounds__(256) weights_join_kernel(AttnState st, Batch ba, WeightCall call) {
+  pdl_wait();
+  pdl_trigger();
+  const ChunkSplit s = reinterpret_cast<const ChunkSplit*>(st.splits)[blockIdx.x];
+  const int own = threadIdx.x;
+  if (!s.there || own >= s.rows) return;
+  float w = st.part[(int64_t)(2 * blockIdx.x + 1) * 256 + own];
+  for (int i = 1; i < s.parts; ++i) w += st.part[(int64_t)2 * (blockIdx.x + i) * 256 + own];
+  float* to = call.w + ba.seq_ids[s.b] * call.stride_seq + s.kh * call.stride_head + s.row0 + own;
+  *to = call.add ? *to + w : w;
 }
 
 template <int D, int N>
 constexpr int weights_smem(int n_seq) { return WeightShape<D, N>::kRing + 1024 + (n_seq + 1) * 4; }
 
 template <int D, int FMT, int N>
-cudaError_t run_weights(const AttnState& st, const AttnDims& dm, const Batch& ba, const WeightCall& call, const Rows& q,
-                        const KvDev& kv, cudaStream_t stream) {
+cudaError_t run_weights(const AttnState& st, const AttnDims& dm, const Batch& ba, bool causal, int last,
+                        const WeightCall& call, const Rows& q, const KvDev& kv, cudaStream_t stream) {
+  using Shape = WeightShape<D, N>;
   static_assert(weights_smem<D, N>(kMaxSeqs) + sizeof(WeightShared<D, N>) <= 227 * 1024, "shared memory");
-  return pdl_launch(weights_kernel<D, FMT, N>, dim3(kAttnCtas), kWeightThreads, weights_smem<D, N>(ba.n_seq), stream, st, dm, ba,
-                    call, q, kv);
+  const WeightPlan plan = {Shape::kSlots, N == 16 ? 7 : 8, N, N == 16 ? 4 : 7, dm.rep, causal ? 1 : 0, dm.H, last};
+  const cudaError_t e = pdl_launch(weights_kernel<D, FMT, N>, dim3(kAttnCtas), kWeightThreads, weights_smem<D, N>(ba.n_seq),
+                                   stream, st, dm, plan, ba, call, q, kv, layer_maps(dm, call.layer, kv, 128));
+  if (e != cudaSuccess || N == 16) return e;   // 16 rows are one step: no unit is split
+  return pdl_launch(weights_join_kernel, dim3(kAttnCtas), 256, 0, stream, st, ba, call);
 }
 
 template <int D, int FMT, int N>
@@ -455,10 +770,12 @@ cudaError_t weights_prepare(const AttnDims& dm) {
   return bf16 ? prepare_dim<256, EPIKV_CACHE_BF16>() : prepare_dim<256, EPIKV_CACHE_E2M1>();
 }
 
+size_t weights_part_floats() { return (size_t)2 * kAttnCtas * 256; }
+
 cudaError_t launch_attention_weights(const AttnState& st, const AttnDims& dm, int layer, const Batch& ba, bool causal,
                                      int last, const Rows& q, const float* lse, bool add, float* w, int64_t stride_seq,
                                      int64_t stride_head, const KvDev& kv, cudaStream_t stream) {
-  const WeightCall call = {layer, causal, last, add, w, stride_seq, stride_head, lse, dm.scale * kLog2e};
+  const WeightCall call = {layer, add, w, stride_seq, stride_head, lse, dm.scale * kLog2e};
   const int64_t tokens = last && last < ba.max_new ? last : ba.max_new;
   const bool few = tokens * dm.rep <= 16, bf16 = dm.fmt == EPIKV_CACHE_BF16;
   auto pick = [&](auto d) {
@@ -469,7 +786,7 @@ cudaError_t launch_attention_weights(const AttnState& st, const AttnDims& dm, in
   auto go = dm.d == 64    ? pick(std::integral_constant<int, 64>{})
             : dm.d == 128 ? pick(std::integral_constant<int, 128>{})
                           : pick(std::integral_constant<int, 256>{});
-  return go(st, dm, ba, call, q, kv, stream);
+  return go(st, dm, ba, causal, last, call, q, kv, stream);
 }
 
 cudaError_t launch_weigh(const DevState& st, const Dims& dm, int n_seq, const int32_t* seq_ids, const float* w,
