@@ -17,14 +17,19 @@
 namespace epikv {
 namespace {
 
-constexpr int kChunkThreads = 384;      // 8 warps own rows, one issues products, three copy
-constexpr int kCopyThreads = 96;
 constexpr float kSlack = 8.f;           // a maximum is moved when a score passes it by 2^8
-// The warps exchange registers: launched with kLaunchRegs each, the owners of rows take more from the others.
-constexpr int kLaunchRegs = 168, kOtherRegs = 104;
-constexpr int owner_regs(int tiles) { return tiles == 2 ? 200 : 232; }
-static_assert(2 * owner_regs(2) + kOtherRegs <= 3 * kLaunchRegs && owner_regs(1) + 2 * kOtherRegs <= 3 * kLaunchRegs,
-              "the owners would wait for registers that nobody gives");
+// 8 warps own rows, one issues products; the others copy: three, seven where they turn 4-bit rows into halves.  They exchange
+// registers: launched with the same number each, the owners of rows take more from the others.
+constexpr int chunk_threads(int fmt) { return fmt == EPIKV_CACHE_BF16 ? 384 : 512; }
+constexpr int launch_regs(int fmt) { return 65536 / chunk_threads(fmt) & ~7; }
+constexpr int other_regs(int fmt) { return fmt == EPIKV_CACHE_BF16 ? 104 : 88; }
+constexpr int owner_regs(int fmt, int tiles) { return tiles == 1 ? 232 : fmt == EPIKV_CACHE_BF16 ? 200 : 168; }
+constexpr bool enough_regs(int fmt, int tiles) {
+  const int groups = chunk_threads(fmt) / 128;
+  return tiles * owner_regs(fmt, tiles) + (groups - tiles) * other_regs(fmt) <= groups * launch_regs(fmt);
+}
+static_assert(enough_regs(EPIKV_CACHE_BF16, 1) && enough_regs(EPIKV_CACHE_BF16, 2) && enough_regs(EPIKV_CACHE_E2M1, 1) &&
+              enough_regs(EPIKV_CACHE_E2M1, 2), "the owners would wait for registers that nobody gives");
 
 template <int D>
 struct ChunkShape {
@@ -137,7 +142,7 @@ struct alignas(16) ChunkShared {
   volatile int unclean[4];                  // 1 + the last segment with an infinite or NaN value in a slot that not all its rows see
   int64_t offset[2][ChunkShape<D>::kSlots]; // of a tile's slots, elements; -1: none
   ShareStart start;
-  WarpWalk walk[kChunkThreads / 32];
+  WarpWalk walk[16];
   ChunkSplit split;
 };
 
@@ -275,8 +280,7 @@ struct Copier {
   using Shape = ChunkShape<D>;
   static constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
   static constexpr uint32_t kBit = kBf16 ? 0x80u : 0x400u;   // lowest of the exponent
-  static constexpr int kPer = kBf16 ? D / 8 : D / 32;     // 16-byte pieces of a head's row in the cache
-  enum { kMost = (Shape::kSlots * kPer + kCopyThreads - 1) / kCopyThreads };   // pieces of a thread
+  static constexpr int kWarps = chunk_threads(FMT) / 32 - 9, kCopyThreads = kWarps * 32;
   char* ring;
   ChunkShared<D>& sh;
   const TensorWaiter& wait;
@@ -391,7 +395,7 @@ struct Copier {
       left(i + w);
       const uint32_t dst = stage(i + w);
       const char* base = kv.base[w];
-      constexpr int kAtOnce = 8;
+      constexpr int kAtOnce = 8, kPer = D / 8;   // 16-byte pieces of a row
       for (int x0 = tid; x0 < Shape::kSlots * kPer; x0 += kAtOnce * kCopyThreads) {
         int64_t o[kAtOnce];
 #pragma unroll
@@ -416,57 +420,40 @@ struct Copier {
     deliver(i + 1);
   }
 
-  struct Codes {
-    uint4 code[kMost];
-    uint32_t scale[kMost];
-  };
-  __device__ __forceinline__ void load_codes(Codes& c, int w, const int64_t* offset, int kh) const {
-#pragma unroll
-    for (int u = 0; u < kMost; ++u) {
-      const int x = tid + u * kCopyThreads, r = x / kPer, p = x % kPer;
-      c.code[u] = make_uint4(0, 0, 0, 0);
-      c.scale[u] = 0;
-      const int64_t o = x < Shape::kSlots * kPer ? offset[r] : -1;
-      if (o >= 0) {
-        const char* row = kv.base[w] + o * 2;
-        c.code[u] = *reinterpret_cast<const uint4*>(row + kh * (D / 2) + p * 16);
-        c.scale[u] = *reinterpret_cast<const uint16_t*>(row + scale_offset(dm, kh) + p * 2);
-      }
-    }
-  }
-  __device__ __forceinline__ void put_codes(const Codes& c, int i) const {
-    left(i);
-    const uint32_t dst = stage(i);
-#pragma unroll
-    for (int u = 0; u < kMost; ++u) {
-      const int x = tid + u * kCopyThreads, r = x / kPer, p = x % kPer;
-      if (x < Shape::kSlots * kPer) {
-        uint4 v[4];
-        expand32(c.code[u], c.scale[u], v);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) sts16(dst + tile_at<D>(r, p * 4 + k), v[k]);
-      }
-    }
-  }
-  // 4-bit rows: the next stage's codes are under way while this one's become halves.
+  // 4-bit rows: a stage's codes are under way while the one before becomes halves, and the table's entries of the next tile
+  // before those.
   __device__ __forceinline__ void q4_segment(const Segment& g, int i, int seg) const {
-    auto offsets = [&](int j) {
-      tile_offsets(sh.offset[j & 1], Shape::kSlots, j * Shape::kSlots, g.most, kv, layer, g.e.seq, dm.T, err, tid, kCopyThreads);
+    constexpr int kStep = kCopyThreads / (D / 32), kRounds = (Shape::kSlots + kStep - 1) / kStep;
+    static_assert(kCopyThreads >= Shape::kSlots, "a thread a slot");
+    using Codes = CodeRows<D, kCopyThreads, kRounds>;
+    const int codes = g.kh * (D / 2), scales = scale_offset(dm, g.kh);
+    auto look = [&](int j) {   // the thread's slot of tile j
+      const int s = j * Shape::kSlots + tid;
+      if (tid >= Shape::kSlots || s >= g.most) return (int64_t)-1;
+      const int64_t o = kv_row_offset(kv, layer, g.e.seq, s, dm.T);
+      if (o < 0) set_error(err, EPIKV_DEV_SLOT);
+      return o;
+    };
+    auto tell = [&](int j, int64_t o) {
+      if (tid < Shape::kSlots) sh.offset[j & 1][tid] = o;
       named_sync(1, kCopyThreads);
     };
     Codes k, v;
-    offsets(g.t0);
-    load_codes(k, 0, sh.offset[g.t0 & 1], g.kh);
+    tell(g.t0, look(g.t0));
+    k.load(kv.base[0], sh.offset[g.t0 & 1], codes, scales, 0, Shape::kSlots, tid);
     for (int j = g.t0; j < g.t1; ++j, i += 2) {
       const int s0 = j * Shape::kSlots;
-      load_codes(v, 1, sh.offset[j & 1], g.kh);
-      put_codes(k, i);
+      v.load(kv.base[1], sh.offset[j & 1], codes, scales, 0, Shape::kSlots, tid);
+      const int64_t ahead = j + 1 < g.t1 ? look(j + 1) : -1;
+      left(i);
+      k.store(stage(i), 0, Shape::kSlots, tid);
       deliver(i);
       if (j + 1 < g.t1) {
-        offsets(j + 1);
-        load_codes(k, 0, sh.offset[(j + 1) & 1], g.kh);
+        tell(j + 1, ahead);
+        k.load(kv.base[0], sh.offset[(j + 1) & 1], codes, scales, 0, Shape::kSlots, tid);
       }
-      put_codes(v, i + 1);
+      left(i + 1);
+      v.store(stage(i + 1), 0, Shape::kSlots, tid);
       if (s0 + Shape::kSlots > g.least) {
         named_sync(1, kCopyThreads);   // what others wrote is looked through too
         clean(i + 1, s0, g, seg);
@@ -760,7 +747,7 @@ __device__ __forceinline__ void put_rows(const AttnState& st, const AttnDims& dm
 }
 
 template <int D, int FMT, int kTiles>
-__global__ void __launch_bounds__(kChunkThreads, 1)
+__global__ void __launch_bounds__(chunk_threads(FMT), 1)
     chunk_kernel(AttnState st, AttnDims dm, ChunkPlan plan, int layer, Batch ba, Rows q, Rows out, float* lse, KvDev kv,
                  const __grid_constant__ LayerMaps maps, float c, int part_rows) {
   using Shape = ChunkShape<D>;
@@ -775,7 +762,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
   if (tid == 0) {
     mbar_init(&sh.query, 128 * kTiles);
     for (int i = 0; i < Shape::kStages; ++i) {
-      mbar_init(&sh.full[i], 3);
+      mbar_init(&sh.full[i], Copier<D, FMT>::kWarps);
       mbar_init(&sh.empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -812,7 +799,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     const SegmentWalk walk{&sh.walk[warp], pre, ba, plan, share_start(cta + 1, total, ctas), lane};
     walk.begin(sh.start, share_start(cta, total, ctas));
     if (warp < 4 * kTiles) {
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(owner_regs(kTiles)));
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(owner_regs(FMT, kTiles)));
       const int t = warp >> 2;
       const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
       int seen = 0;
@@ -820,10 +807,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       auto take_query = [&](const Segment& g) {
         const int r = g.row0 + tid, token = r / dm.rep, hq = g.kh * dm.rep + r % dm.rep;
         const bool live = tid < g.rows;
-        // rows that are not there see all slots of the tiles: their queries are 0
+        // rows that are not there see all slots of the tiles
         seen = live ? row_sees(plan, g.e.len, r) : INT_MAX;
         if (g.t0 >= g.t1) return;
-        const char* src = live ? q.p + ((int64_t)(g.e.tok0 + token) * q.st + hq * q.sh) * 2 : nullptr;
+        // (a row that is not there has the item's first one's queries: nobody looks at its results)
+        const char* src = q.p + (live ? (int64_t)(g.e.tok0 + token) * q.st + hq * q.sh
+                                      : (int64_t)(g.e.tok0 + g.row0 / dm.rep) * q.st + (g.kh * dm.rep + g.row0 % dm.rep) * q.sh) * 2;
         factor = c * store_queries<D, !kBf16>(smem_u32(smem + t * Shape::kQuery), tid & 96, src, lane);
         if constexpr (!kBf16) factor *= head_scale(st, dm, 0, layer, g.kh);
         fence_proxy_async_smem();
@@ -853,7 +842,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           sh.split = {1, now.b, now.kh, now.row0, now.rows, share_of(now.end - 1, total, ctas) - cta + 1, {0, 0}};
       }
     } else {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kOtherRegs));
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(other_regs(FMT)));
       if (warp == 8) {
         issue_products<D, FMT, kTiles>(smem_u32(smem), smem_u32(ring), sh, wait, walk, tmem);
         __syncwarp();
@@ -928,7 +917,7 @@ cudaError_t run_chunk(const AttnState& st, const AttnDims& dm, int layer, const 
   static_assert(chunk_smem<D, kTiles>(kMaxSeqs) + sizeof(ChunkShared<D>) + 64 <= 227 * 1024, "shared memory");
   const ChunkPlan plan = {128 * kTiles, Shape::kSlots, kTiles == 2 ? 8 : 7, Shape::kSlots == 128 ? 7 : 6, dm.rep, causal ? 1 : 0, dm.H};
   const int rows = part_rows_of(dm, ba.max_new);
-  cudaError_t e = pdl_launch(chunk_kernel<D, FMT, kTiles>, dim3(kAttnCtas), kChunkThreads, chunk_smem<D, kTiles>(ba.n_seq),
+  cudaError_t e = pdl_launch(chunk_kernel<D, FMT, kTiles>, dim3(kAttnCtas), chunk_threads(FMT), chunk_smem<D, kTiles>(ba.n_seq),
                              stream, st, dm, plan, layer, ba, q, out, lse, kv, layer_maps(dm, layer, kv, Shape::kSlots),
                              dm.scale * 1.4426950408889634f, rows);
   if (e != cudaSuccess) return e;
@@ -943,7 +932,7 @@ cudaError_t allow_chunk(bool* runs) {
   cudaFuncAttributes at;
   const cudaError_t e = cudaFuncGetAttributes(&at, chunk_kernel<D, FMT, kTiles>);
   if (e != cudaSuccess) return e;
-  if (at.numRegs != kLaunchRegs) *runs = false;
+  if (at.numRegs != launch_regs(FMT)) *runs = false;
   return cudaFuncSetAttribute(chunk_kernel<D, FMT, kTiles>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               chunk_smem<D, kTiles>(kMaxSeqs));
 }

@@ -79,15 +79,15 @@ EPIKV_PLAN int weight_slots(const WeightPlan& p, int n, int len) { return len + 
 EPIKV_PLAN int weight_units(const WeightPlan& p, int n, int len) {
   return (weight_slots(p, n, len) + p.slots - 1) >> p.slots_log;
 }
-// First query row of a unit.
-EPIKV_PLAN int weight_row(const WeightPlan& p, int n, int len, int unit) {
-  const int first = p.last && p.last < n ? (n - p.last) * p.rep : 0, s0 = unit << p.slots_log;
-  const int sees = p.causal && s0 > len ? (s0 - len) * p.rep : 0;
+// First new token of a unit.
+EPIKV_PLAN int weight_token(const WeightPlan& p, int n, int len, int unit) {
+  const int first = p.last && p.last < n ? n - p.last : 0, s0 = unit << p.slots_log;
+  const int sees = p.causal && s0 > len ? s0 - len : 0;
   return sees > first ? sees : first;
 }
 // Steps of a unit: 0 where no row counts ...
 EPIKV_PLAN int weight_steps(const WeightPlan& p, int n, int len, int unit) {
-  return (n * p.rep - weight_row(p, n, len, unit) + p.rows - 1) >> p.rows_log;
+  return ((n - weight_token(p, n, len, unit)) * p.rep + p.rows - 1) >> p.rows_log;
 }
 // ... which still has a place in the line: its zeros are stored.
 EPIKV_PLAN int weight_places(const WeightPlan& p, int n, int len, int unit) {

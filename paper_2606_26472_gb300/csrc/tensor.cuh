@@ -270,9 +270,9 @@ __device__ __forceinline__ float halves_of(uint4& x) {
   return __uint_as_float((uint32_t)(127 - up) << 23);
 }
 
-// A warp's 32 rows of D bf16 queries into rows `row0` to row0 + 31 of a tile; src: each lane's row, or null for zeros.  Lanes
-// beside each other load neighbouring pieces.  Over a 4-bit cache the queries become halves; what undoes the scaling of the
-// lane's row is returned.
+// A warp's 32 rows of D bf16 queries into rows `row0` to row0 + 31 of a tile; src: each lane's row.  Lanes beside each other
+// load neighbouring pieces.  Over a 4-bit cache the queries become halves; what undoes the scaling of the lane's row is
+// returned.
 template <int D, bool kHalf>
 __device__ __forceinline__ float store_queries(uint32_t tile, int row0, const void* src, int lane) {
   constexpr int kPer = D / 8;            // 16-byte pieces of a row: 8, 16 or 32
@@ -285,24 +285,66 @@ __device__ __forceinline__ float store_queries(uint32_t tile, int row0, const vo
   for (int r0 = 0; r0 < 32 / kRows; r0 += kAtOnce) {
     uint4 v[kAtOnce];
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
-      if (r0 + i >= 32 / kRows) break;
-      const uint4* p = reinterpret_cast<const uint4*>(__shfl_sync(0xffffffffu, mine, (r0 + i) * kRows + sub));
-      v[i] = p ? __ldg(p + piece) : make_uint4(0, 0, 0, 0);
-    }
+    for (int i = 0; i < kAtOnce; ++i)
+      if (r0 + i < 32 / kRows)
+        v[i] = __ldg(reinterpret_cast<const uint4*>(__shfl_sync(0xffffffffu, mine, (r0 + i) * kRows + sub)) + piece);
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
-      if (r0 + i >= 32 / kRows) break;
-      const int row = (r0 + i) * kRows + sub;
+      if (r0 + i >= 32 / kRows) continue;
       uint4 x = v[i];
       if constexpr (kHalf) {
         const float undo = __shfl_sync(0xffffffffu, halves_of<kPer>(x), lane % kRows * kPer);   // to the lane that owns the row
         if (lane / kRows == r0 + i) back = undo;
       }
-      sts16(tile + tile_at<D>(row0 + row, piece), x);
+      sts16(tile + tile_at<D>(row0 + (r0 + i) * kRows + sub, piece), x);
     }
   }
   return back;
 }
+
+// Pieces of 4-bit rows that each of kThreads threads turns into halves: 32 channels of every kStep-th row from row `first` on,
+// R rows at a time.
+template <int D, int kThreads, int R>
+struct CodeRows {
+  static constexpr int kPer = D / 32, kStep = kThreads / kPer;
+  static_assert(kThreads % kPer == 0, "a thread's pieces are of the same channels");
+  uint4 code[R];
+  uint32_t scale[R];
+  // `codes`, `scales`: the head's, in bytes of a row; offset: of the rows, elements (-1: zeros)
+  __device__ __forceinline__ void load(const char* base, const int64_t* offset, int codes, int scales, int first, int rows,
+                                       int tid) {
+    const int p = tid % kPer, r0 = first + tid / kPer;
+    int64_t o[R];
+#pragma unroll
+    for (int u = 0; u < R; ++u) o[u] = r0 + u * kStep < rows ? offset[r0 + u * kStep] : -1;
+    codes += p * 16;
+    scales += p * 2;
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+      code[u] = make_uint4(0, 0, 0, 0);
+      scale[u] = 0;
+      if (o[u] >= 0) {
+        const char* row = base + o[u] * 2;
+        code[u] = __ldg(reinterpret_cast<const uint4*>(row + codes));
+        scale[u] = __ldg(reinterpret_cast<const uint16_t*>(row + scales));
+      }
+    }
+  }
+  __device__ __forceinline__ void store(uint32_t tile, int first, int rows, int tid) const {
+    const int p = tid % kPer, r0 = first + tid / kPer;
+    uint32_t at[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) at[k] = tile + tile_at<D>(r0, p * 4 + k);
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+      if (r0 + u * kStep >= rows) break;
+      uint4 v[4];
+      expand32(code[u], scale[u], v);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        sts16(kStep % 8 == 0 ? at[k] + u * (kStep / 8) * (D * 16) : tile + tile_at<D>(r0 + u * kStep, p * 4 + k), v[k]);
+    }
+  }
+};
 
 }  // namespace epikv

@@ -74,56 +74,67 @@ struct WeightSegment {
   Entry e;
   int b, kh, unit;
   int slots;        // of the entry
-  int row0;         // the segment's first query row
-  int steps;        // 0: the unit has no rows, its zeros are stored
+  int token;        // the unit's first new token
+  int step, steps;  // the segment's first step of the unit, steps (0: the unit has no rows, its zeros are stored)
   bool first, last; // the unit starts, ends here
   unsigned end;     // the line's place behind the unit
 };
 
+// (What is the same for all heads of a unit is formed once: units of a decode step come every 1,400 cycles.)
 struct WeightWalk {
   const unsigned* pre;
   const Batch& ba;
   const WeightPlan& plan;
   unsigned x, end;
-  int b, unit, kh, step, units;
-  Entry e;
+  int step, units, all, places;
+  WeightSegment now;
   __device__ __forceinline__ WeightWalk(const unsigned* pre_, const Batch& ba_, const WeightPlan& plan_, const WeightStart& s,
                                         unsigned x_, unsigned end_)
-      : pre(pre_), ba(ba_), plan(plan_), x(x_), end(end_), b(s.b), unit(s.unit), kh(s.kh), step(s.step), e(s.e) {
-    units = weight_units(plan, e.n, e.len);
+      : pre(pre_), ba(ba_), plan(plan_), x(x_), end(end_), step(s.step) {
+    now = {};
+    now.e = s.e;
+    now.b = s.b;
+    now.unit = s.unit;
+    now.kh = s.kh - 1;   // before the first
+    entry();
+    unit();
+    now.last = true;
   }
-  __device__ __forceinline__ bool next(WeightSegment* s) {
+  __device__ __forceinline__ void entry() {
+    units = weight_units(plan, now.e.n, now.e.len);
+    now.slots = weight_slots(plan, now.e.n, now.e.len);
+  }
+  __device__ __forceinline__ void unit() {
+    now.token = weight_token(plan, now.e.n, now.e.len, now.unit);
+    all = weight_steps(plan, now.e.n, now.e.len, now.unit);
+    places = all > 1 ? all : 1;
+  }
+  // Moves `now` on to the next segment; false at the share's end.
+  __device__ __forceinline__ bool next() {
     if (x >= end) return false;
-    const int places = weight_places(plan, e.n, e.len, unit), all = weight_steps(plan, e.n, e.len, unit);
-    const int take = min((unsigned)(places - step), end - x);
-    s->e = e;
-    s->b = b;
-    s->kh = kh;
-    s->unit = unit;
-    s->slots = weight_slots(plan, e.n, e.len);
-    s->row0 = weight_row(plan, e.n, e.len, unit) + (step << plan.rows_log);
-    s->steps = min(take, max(all - step, 0));
-    s->first = step == 0;
-    s->last = step + take == places;
-    s->end = x + (places - step);
-    x += take;
-    step += take;
-    if (s->last) {
-      step = 0;
-      if (++kh == plan.heads) {
-        kh = 0;
-        if (++unit == units && x < end) {
-          unit = 0;
-          do ++b;
-          while (pre[b + 1] == pre[b]);
-          e.tok0 = ba.cu_new[b];
-          e.n = ba.cu_new[b + 1] - e.tok0;
-          e.seq = ba.seq_ids[b];
-          e.len = ba.len[(int64_t)b * ba.len_stride];
-          units = weight_units(plan, e.n, e.len);
-        }
+    // (a segment that does not end its unit is the share's last)
+    if (++now.kh == plan.heads) {
+      now.kh = 0;
+      if (++now.unit == units) {
+        now.unit = 0;
+        do ++now.b;
+        while (pre[now.b + 1] == pre[now.b]);
+        now.e.tok0 = ba.cu_new[now.b];
+        now.e.n = ba.cu_new[now.b + 1] - now.e.tok0;
+        now.e.seq = ba.seq_ids[now.b];
+        now.e.len = ba.len[(int64_t)now.b * ba.len_stride];
+        entry();
       }
+      unit();
     }
+    const int take = (int)min((unsigned)(places - step), end - x);
+    now.step = step;
+    now.steps = min(take, all - step);
+    now.first = step == 0;
+    now.last = step + take == places;
+    now.end = x + (places - step);
+    x += take;
+    step = 0;
     return true;
   }
 };
@@ -200,8 +211,10 @@ struct KeyCopier {
   static constexpr int kThreads = Shape::kKeyThreads, kPer = kBf16 ? D / 8 : D / 32;   // 16-byte pieces of a head's row in the cache
   enum {
     kPieces = Shape::kSlots * kPer,
-    kAtOnce = (kPieces + kThreads - 1) / kThreads < 6 ? (kPieces + kThreads - 1) / kThreads : 6,
-    kAhead = kAtOnce * kThreads >= kPieces,   // a unit's codes are read while the last one's become halves
+    kStep = kThreads / (D / 32),              // 4-bit rows: rows at once, rounds of them
+    kRounds = (Shape::kSlots + kStep - 1) / kStep,
+    kAtOnce = kRounds < 6 ? kRounds : 6,
+    kAhead = kAtOnce == kRounds,              // a unit's codes are read while the last one's become halves
     kLag = Shape::kKeyStages - 1 < 3 ? Shape::kKeyStages - 1 : 3,   // units in flight behind the newest
   };
   char* ring;
@@ -249,8 +262,8 @@ struct KeyCopier {
     int64_t* offset = sh.offset[0];
     int y = 0, z = 0;
     bool whole = false, known = false;
-    WeightSegment g;
-    while (walk.next(&g)) {
+    const WeightSegment& g = walk.now;
+    while (walk.next()) {
       if (g.steps == 0) continue;
       const int s0 = g.unit * Shape::kSlots;
       if (g.unit != unit || g.b != b) {   // the heads of the same slots follow one another
@@ -329,43 +342,13 @@ struct KeyCopier {
         mbar_wait_bounded(&sh.keys[k % Shape::kKeyStages], (uint32_t)(k / Shape::kKeyStages) & 1, kTensorWaitNs);
   }
 
-  struct Codes {
-    uint4 code[kAtOnce];
-    uint32_t scale[kAtOnce];
-  };
-  __device__ __forceinline__ void load(Codes& c, const int64_t* offset, int kh, int x0) const {
-#pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) {
-      const int x = x0 + u * kThreads, r = x / kPer, p = x % kPer;
-      c.code[u] = make_uint4(0, 0, 0, 0);
-      c.scale[u] = 0;
-      const int64_t o = x < kPieces ? offset[r] : -1;
-      if (o >= 0) {
-        const char* row = kv.base[0] + o * 2;
-        c.code[u] = *reinterpret_cast<const uint4*>(row + kh * (D / 2) + p * 16);
-        c.scale[u] = *reinterpret_cast<const uint16_t*>(row + scale_offset(dm, kh) + p * 2);
-      }
-    }
-  }
-  __device__ __forceinline__ void store(const Codes& c, uint32_t dst, int x0) const {
-#pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) {
-      const int x = x0 + u * kThreads, r = x / kPer, p = x % kPer;
-      if (x < kPieces) {
-        uint4 v[4];
-        expand32(c.code[u], c.scale[u], v);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) sts16(dst + tile_at<D>(r, p * 4 + k), v[k]);
-      }
-    }
-  }
   // 4-bit rows: a unit's codes are under way while the one before becomes halves.
   __device__ __forceinline__ void run_q4(WeightWalk walk) const {
     int i = 0, tables = 0, unit = -1, b = -1;
     const int64_t* offset = sh.offset[0];
-    WeightSegment g;
+    const WeightSegment& g = walk.now;
     auto ahead = [&] {   // the next segment with rows, and its slots' offsets
-      while (walk.next(&g)) {
+      while (walk.next()) {
         if (g.steps == 0) continue;
         if (g.unit != unit || g.b != b) {
           unit = g.unit;
@@ -378,28 +361,31 @@ struct KeyCopier {
       }
       return false;
     };
+    using Codes = CodeRows<D, kThreads, kAtOnce>;
+    auto load = [&](Codes& c, int first) {
+      c.load(kv.base[0], offset, g.kh * (D / 2), scale_offset(dm, g.kh), first, Shape::kSlots, tid);
+    };
     bool more = ahead();
     if constexpr (kAhead) {
       Codes now, next;
-      if (more) load(next, offset, g.kh, tid);
+      if (more) load(next, 0);
       while (more) {
         now = next;
-        const int64_t* mine = offset;
         left(i);
-        mark(i, mine);
+        mark(i, offset);
         more = ahead();
-        if (more) load(next, offset, g.kh, tid);
-        store(now, stage(i), tid);
+        if (more) load(next, 0);
+        now.store(stage(i), 0, Shape::kSlots, tid);
         deliver(i++);
       }
     } else {
       while (more) {
         left(i);
         mark(i, offset);
-        for (int x0 = tid; x0 < kPieces; x0 += kAtOnce * kThreads) {
+        for (int first = 0; first < Shape::kSlots; first += kAtOnce * kStep) {
           Codes c;
-          load(c, offset, g.kh, x0);
-          store(c, stage(i), x0);
+          load(c, first);
+          c.store(stage(i), first, Shape::kSlots, tid);
         }
         deliver(i++);
         more = ahead();
@@ -421,54 +407,65 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh,
   constexpr int kLoads = (R + kRows - 1) / kRows;
   constexpr int kBatch = kLoads < 16 ? kLoads : 16;      // loads in flight
   const int piece = lane % kPer, sub = lane / kPer;
-  WeightSegment g = {};
-  int k = 0;
+  const WeightSegment& g = walk.now;
+  // the lane's row of a step is head `head` of the unit's token `token`; both go on from step to step
+  const int rep = dm.rep, own = warp * R + lane, own_token = own / rep, own_head = own - own_token * rep;
+  const int more_tokens = N / rep, more_heads = N - more_tokens * rep;
+  int k = -1, token = 0, head = 0;
   struct Row {
-    uint64_t src;    // lane's row, or 0
+    uint64_t src;    // the lane's row (one that is not there: the step's first, nobody looks at it)
     float lse;
     int seen;
-    bool in;
   };
-  auto row_of = [&](int step) {
+  auto row_of = [&] {
     Row r;
-    const int at = g.row0 + step * N + warp * R + lane, token = at / dm.rep, hq = g.kh * dm.rep + at % dm.rep;
-    r.in = lane < R && at < g.e.n * dm.rep;
-    r.src = r.in ? (uint64_t)(q.p + ((int64_t)(g.e.tok0 + token) * q.st + hq * q.sh) * 2) : 0;
-    r.lse = r.in ? __ldg(call.lse + (int64_t)(g.e.tok0 + token) * dm.Hq + hq) : -INFINITY;
-    r.seen = walk.plan.causal ? g.e.len + token + 1 : g.e.len;
+    const int at = g.token + token, hq = g.kh * rep + head;
+    const bool in = lane < R && at < g.e.n;
+    r.src = (uint64_t)(q.p + ((int64_t)(g.e.tok0 + (in ? at : g.token)) * q.st + (in ? hq : g.kh * rep) * q.sh) * 2);
+    r.lse = in ? __ldg(call.lse + (int64_t)(g.e.tok0 + at) * dm.Hq + hq) : -INFINITY;
+    r.seen = walk.plan.causal ? g.e.len + at + 1 : g.e.len;
     return r;
   };
   auto load = [&](uint4 (&v)[kBatch], const Row& r, int l0) {
 #pragma unroll
     for (int l = 0; l < kBatch; ++l) {
       const int row = (l0 + l) * kRows + sub;
-      const uint4* p = reinterpret_cast<const uint4*>(__shfl_sync(0xffffffffu, r.src, row & 31));
-      v[l] = p && row < R ? __ldg(p + piece) : make_uint4(0, 0, 0, 0);
+      v[l] = __ldg(reinterpret_cast<const uint4*>(__shfl_sync(0xffffffffu, r.src, row & 31)) + piece);
     }
   };
   auto advance = [&] {   // to the next step; false at the share's end
-    if (k + 1 < g.steps) {
-      ++k;
+    if (++k < g.steps) {
+      token += more_tokens;
+      head += more_heads;
+      if (head >= rep) {
+        head -= rep;
+        ++token;
+      }
       return true;
     }
-    k = 0;
     do {
-      if (!walk.next(&g)) return false;
+      if (!walk.next()) return false;
     } while (g.steps == 0);
+    k = 0;
+    token = own_token;
+    head = own_head;
+    if (g.step) {
+      token = (g.step * N + own) / rep;
+      head = g.step * N + own - token * rep;
+    }
     return true;
   };
   bool more = advance();
   Row next = {}, now;
   uint4 v[kBatch];
   if (more) {
-    next = row_of(k);
+    next = row_of();
     load(v, next, 0);
   }
   for (int step = 0; more; ++step) {
     now = next;
     const int qs = step % Shape::kQueryStages;
     const int upto = min(g.unit * Shape::kSlots + Shape::kSlots, g.slots);
-    const float scale = kHalf ? call.c * head_scale(st, dm, 0, call.layer, g.kh) : call.c;
     if (step >= Shape::kQueryStages) wait(&sh.query_left[qs], (uint32_t)(step / Shape::kQueryStages - 1) & 1);
     const uint32_t dst = smem_u32(ring + Shape::kKeyStages * Shape::kKeys + qs * Shape::kQuery);
     float back = 1.f;
@@ -490,7 +487,7 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh,
     if (lane < R) {
       const bool counts = now.lse != -INFINITY;   // else the row saw nothing
       sh.lse2[qs][warp * R + lane] = -now.lse * kLog2e;
-      sh.factor[qs][warp * R + lane] = scale * back;
+      if constexpr (kHalf) sh.factor[qs][warp * R + lane] = call.c * head_scale(st, dm, 0, call.layer, g.kh) * back;
       sh.seen[qs][warp * R + lane] = counts ? now.seen : 0;
     }
     const bool partly = __any_sync(0xffffffffu, lane < R && (now.lse == -INFINITY || now.seen < upto));
@@ -500,7 +497,7 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh,
     if (lane == 0) mbar_arrive_one(&sh.query[qs]);
     more = advance();
     if (more) {
-      next = row_of(k);
+      next = row_of();
       load(v, next, 0);
     }
   }
@@ -513,9 +510,9 @@ __device__ __forceinline__ void issue_units(uint32_t ring, WeightShared<D, N>& s
   using Shape = WeightShape<D, N>;
   constexpr uint32_t kScores = product_of(128, N, FMT == EPIKV_CACHE_BF16, false);
   const uint64_t k0 = rows_operand<D>(ring), q0 = rows_operand<D>(ring + Shape::kKeyStages * Shape::kKeys);
-  WeightSegment g;
+  const WeightSegment& g = walk.now;
   int step = 0;
-  for (int i = 0; walk.next(&g);) {
+  for (int i = 0; walk.next();) {
     const int steps = __shfl_sync(0xffffffffu, g.steps, 0);
     if (steps == 0) continue;
     const int ks = i % Shape::kKeyStages;
@@ -554,10 +551,10 @@ __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaite
   using Shape = WeightShape<D, N>;
   constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
   constexpr int kRound = N < 32 ? N : 32;   // columns at once
-  WeightSegment g;
+  const WeightSegment& g = walk.now;
   int step = 0;
   const int lane = tid & 31, own = t * 128 + tid;
-  for (int i = 0; walk.next(&g);) {
+  for (int i = 0; walk.next();) {
     const int s = g.unit * Shape::kSlots + own;
     float* to = call.w + g.e.seq * call.stride_seq + g.kh * call.stride_head + s;
     const bool alone = g.first && g.last, mine = s < g.slots;
@@ -578,13 +575,19 @@ __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaite
       bool partly = false;
 #pragma unroll
       for (int w = 0; w < kQueryWarps; ++w) partly |= sh.partly[qs][w] != 0;
+      uint32_t columns[2][kRound];   // those after the next are on their way
+      auto load = [&](int i0) {
+        if constexpr (kRound == 16) tmem_load16(tmem + (2 * t + buf) * N + i0, columns[i0 / kRound & 1]);
+        else tmem_load32(tmem + (2 * t + buf) * N + i0, columns[i0 / kRound & 1]);
+      };
+      load(0);
 #pragma unroll
       for (int i0 = 0; i0 < N; i0 += kRound) {
-        uint32_t x[kRound];
-        if constexpr (kRound == 16) tmem_load16(tmem + (2 * t + buf) * N + i0, x);
-        else tmem_load32(tmem + (2 * t + buf) * N + i0, x);
+        const uint32_t(&x)[kRound] = columns[i0 / kRound & 1];
         tmem_wait_load();
-        if (i0 + kRound == N) {
+        if (i0 + kRound < N) {
+          load(i0 + kRound);
+        } else {
           tensor_fence_before();
           mbar_arrive_one(&sh.taken[t][buf]);
         }
