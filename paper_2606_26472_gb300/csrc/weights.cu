@@ -565,7 +565,9 @@ __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaite
       continue;
     }
     const int ks = i % Shape::kKeyStages;
-    f32x2 sum[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
+    f32x2 sum[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[j] = f2_pack(0.f, 0.f);
     for (int k = 0; k < g.steps; ++k, ++step) {
       const int qs = step % Shape::kQueryStages, buf = step & 1;
       wait(&sh.scores[t][buf], (uint32_t)(step / 2) & 1);
@@ -584,6 +586,10 @@ __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaite
 #pragma unroll
       for (int i0 = 0; i0 < N; i0 += kRound) {
         const uint32_t(&x)[kRound] = columns[i0 / kRound & 1];
+        f32x2 p[kRound / 2];
+        float4 l[kRound / 4];
+#pragma unroll
+        for (int j = 0; j < kRound / 4; ++j) l[j] = lse2[i0 / 4 + j];
         tmem_wait_load();
         if (i0 + kRound < N) {
           load(i0 + kRound);
@@ -592,27 +598,28 @@ __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaite
           mbar_arrive_one(&sh.taken[t][buf]);
         }
 #pragma unroll
-        for (int j = 0; j < kRound; j += 4) {
-          const float4 l = lse2[(i0 + j) / 4];
-          const float4 f = kBf16 ? make_float4(call.c, call.c, call.c, call.c) : factor[(i0 + j) / 4];
-          const f32x2 a = f2_fma(f2_pack(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), f2_pack(f.x, f.y), f2_pack(l.x, l.y));
-          const f32x2 b = f2_fma(f2_pack(__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])), f2_pack(f.z, f.w), f2_pack(l.z, l.w));
-          float p[4] = {exp2_fast(f2_lo(a)), exp2_fast(f2_hi(a)), exp2_fast(f2_lo(b)), exp2_fast(f2_hi(b))};
-          if (partly) {
-            const int4 e = reinterpret_cast<const int4*>(sh.seen[qs])[(i0 + j) / 4];
-            p[0] = s < e.x ? p[0] : 0.f;
-            p[1] = s < e.y ? p[1] : 0.f;
-            p[2] = s < e.z ? p[2] : 0.f;
-            p[3] = s < e.w ? p[3] : 0.f;
-          }
-          sum[0] = f2_add(sum[0], f2_pack(p[0], p[1]));
-          sum[1] = f2_add(sum[1], f2_pack(p[2], p[3]));
+        for (int j = 0; j < kRound / 4; ++j) {
+          const float4 f = kBf16 ? make_float4(call.c, call.c, call.c, call.c) : factor[i0 / 4 + j];
+          p[2 * j] = f2_fma(f2_pack(__uint_as_float(x[4 * j]), __uint_as_float(x[4 * j + 1])), f2_pack(f.x, f.y), f2_pack(l[j].x, l[j].y));
+          p[2 * j + 1] = f2_fma(f2_pack(__uint_as_float(x[4 * j + 2]), __uint_as_float(x[4 * j + 3])), f2_pack(f.z, f.w), f2_pack(l[j].z, l[j].w));
         }
+#pragma unroll
+        for (int j = 0; j < kRound / 2; ++j) p[j] = f2_pack(exp2_fast(f2_lo(p[j])), exp2_fast(f2_hi(p[j])));
+        if (partly) {
+          const int2* seen = reinterpret_cast<const int2*>(sh.seen[qs]) + i0 / 2;
+#pragma unroll
+          for (int j = 0; j < kRound / 2; ++j) {
+            const int2 e = seen[j];
+            p[j] = f2_pack(s < e.x ? f2_lo(p[j]) : 0.f, s < e.y ? f2_hi(p[j]) : 0.f);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < kRound / 2; ++j) sum[j & 3] = f2_add(sum[j & 3], p[j]);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive_one(&sh.query_left[qs]);
     }
-    const f32x2 both = f2_add(sum[0], sum[1]);
+    const f32x2 both = f2_add(f2_add(sum[0], sum[1]), f2_add(sum[2], sum[3]));
     float w = f2_lo(both) + f2_hi(both);
     const bool there = sh.there[ks][own / 32] >> lane & 1;
     __syncwarp();
