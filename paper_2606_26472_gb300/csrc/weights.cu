@@ -19,22 +19,24 @@
 namespace epikv {
 namespace {
 
-constexpr int kWeightThreads = 512;
-constexpr int kQueryWarps = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 
-// N query rows a step; T tiles of 128 slots a unit, each with four warps that own its slots.
+// N query rows a step; T tiles of 128 slots a unit, the columns of each in P parts: four warps for each part of a tile, a
+// thread a slot.  (One part of 128 columns left two warps a scheduler, which hid little of a column's latencies: a prompt of
+// 4,096 tokens 112 us, two parts XX.)
 template <int D, int N>
 struct WeightShape {
-  static constexpr int T = N == 16 ? 1 : 2;
+  static constexpr int T = N == 16 && D == 256 ? 1 : 2, P = N == 16 ? 1 : 2;
+  static constexpr int kThreads = N == 16 ? 768 : 896;
+  static constexpr int kQueryWarps = N == 16 ? 4 : 8;
   static constexpr int kSlots = 128 * T;
   static constexpr int kKeys = kSlots * D * 2;         // bytes of a unit's keys
   static constexpr int kQuery = N * D * 2;             // of a step's rows
-  static constexpr int kKeyStages = N == 16 ? (D == 64 ? 9 : D == 128 ? 5 : 2) : D == 256 ? 1 : 2;
+  static constexpr int kKeyStages = N == 16 ? (D == 64 ? 5 : D == 128 ? 3 : 2) : D == 256 ? 1 : 2;
   static constexpr int kQueryStages = N == 16 ? kKeyStages : D == 64 ? 4 : D == 128 ? 2 : 1;
   static constexpr int kRing = kKeyStages * kKeys + kQueryStages * kQuery;
-  static constexpr int kMmaWarp = 4 * T, kQueryWarp = kMmaWarp + 1, kKeyWarp = kQueryWarp + kQueryWarps;
-  static constexpr int kKeyWarps = kWeightThreads / 32 - kKeyWarp;   // 7 or 3
+  static constexpr int kMmaWarp = 4 * T * P, kQueryWarp = kMmaWarp + 1, kKeyWarp = kQueryWarp + kQueryWarps;
+  static constexpr int kKeyWarps = kThreads / 32 - kKeyWarp;
   static constexpr int kKeyThreads = kKeyWarps * 32;
   static constexpr uint32_t kColumns = 2 * N * T < 32 ? 32 : 2 * N * T;   // two tiles of scores for each tile of slots
 };
@@ -56,8 +58,9 @@ struct alignas(16) WeightShared {
   alignas(16) float factor[Shape::kQueryStages][N];        // of a row's scores (4-bit rows; else the same for all)
   alignas(16) float lse2[Shape::kQueryStages][N];          // minus log2 of a row's sum
   alignas(16) int seen[Shape::kQueryStages][N];            // slots that the row sees
-  int partly[Shape::kQueryStages][kQueryWarps];            // not every row sees all slots of the unit
+  int partly[Shape::kQueryStages][Shape::kQueryWarps];            // not every row sees all slots of the unit
   int64_t offset[2][Shape::kSlots];
+  float half[2][Shape::P == 2 ? Shape::T : 1][Shape::P == 2 ? 128 : 1];         // sums of the tiles' second parts, units in turn
   WeightStart start;
 };
 
@@ -395,17 +398,17 @@ struct KeyCopier {
 };
 
 // ------------------------------------------------------------------ query rows
-// Warp w of four brings rows w N/4 .. of each step; a step's rows are under way while the one before is stored.
+// Each warp brings so many rows of each step; a step's rows are under way while the one before is stored.
 template <int D, int FMT, int N>
 __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh, const TensorWaiter& wait, const AttnState& st,
                                              const AttnDims& dm, const WeightCall& call, const Rows& q, WeightWalk walk,
                                              int warp, int lane) {
   using Shape = WeightShape<D, N>;
   constexpr bool kHalf = FMT != EPIKV_CACHE_BF16;
-  constexpr int R = N / kQueryWarps;                     // rows of the warp
+  constexpr int R = N / Shape::kQueryWarps;                     // rows of the warp
   constexpr int kPer = D / 8, kRows = 32 / kPer;         // pieces of a row; rows at once
   constexpr int kLoads = (R + kRows - 1) / kRows;
-  constexpr int kBatch = kLoads < 16 ? kLoads : 16;      // loads in flight
+  constexpr int kBatch = kLoads < 8 ? kLoads : 8;       // loads in flight
   const int piece = lane % kPer, sub = lane / kPer;
   const WeightSegment& g = walk.now;
   // the lane's row of a step is head `head` of the unit's token `token`; both go on from step to step
@@ -547,10 +550,11 @@ __device__ __forceinline__ void issue_units(uint32_t ring, WeightShared<D, N>& s
 template <int D, int FMT, int N>
 __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaiter& wait, const WeightCall& call, float* part0,
                                        float* part1, ChunkSplit* split, unsigned total, int ctas, WeightWalk walk,
-                                       uint32_t tmem, int t, int tid) {
+                                       uint32_t tmem, int t, int part, int tid) {
   using Shape = WeightShape<D, N>;
   constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
-  constexpr int kRound = N < 32 ? N : 32;   // columns at once
+  constexpr int kColumns = N / Shape::P;                        // of the thread's part
+  constexpr int kRound = 16;                                    // at once
   const WeightSegment& g = walk.now;
   int step = 0;
   const int lane = tid & 31, own = t * 128 + tid;
@@ -559,9 +563,9 @@ __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaite
     float* to = call.w + g.e.seq * call.stride_seq + g.kh * call.stride_head + s;
     const bool alone = g.first && g.last, mine = s < g.slots;
     float old = 0.f;   // on its way while the scores are formed
-    if (call.add && alone && mine) old = *to;
+    if (call.add && alone && mine && part == 0) old = *to;
     if (g.steps == 0) {
-      if (mine && !call.add) *to = 0.f;
+      if (mine && !call.add && part == 0) *to = 0.f;
       continue;
     }
     const int ks = i % Shape::kKeyStages;
@@ -572,28 +576,21 @@ __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaite
       const int qs = step % Shape::kQueryStages, buf = step & 1;
       wait(&sh.scores[t][buf], (uint32_t)(step / 2) & 1);
       tensor_fence_after();
-      const float4* lse2 = reinterpret_cast<const float4*>(sh.lse2[qs]);
-      const float4* factor = reinterpret_cast<const float4*>(sh.factor[qs]);
+      const float4* lse2 = reinterpret_cast<const float4*>(sh.lse2[qs] + part * kColumns);
+      const float4* factor = reinterpret_cast<const float4*>(sh.factor[qs] + part * kColumns);
       bool partly = false;
 #pragma unroll
-      for (int w = 0; w < kQueryWarps; ++w) partly |= sh.partly[qs][w] != 0;
-      uint32_t columns[2][kRound];   // those after the next are on their way
-      auto load = [&](int i0) {
-        if constexpr (kRound == 16) tmem_load16(tmem + (2 * t + buf) * N + i0, columns[i0 / kRound & 1]);
-        else tmem_load32(tmem + (2 * t + buf) * N + i0, columns[i0 / kRound & 1]);
-      };
-      load(0);
+      for (int w = 0; w < Shape::kQueryWarps; ++w) partly |= sh.partly[qs][w] != 0;
 #pragma unroll
-      for (int i0 = 0; i0 < N; i0 += kRound) {
-        const uint32_t(&x)[kRound] = columns[i0 / kRound & 1];
+      for (int i0 = 0; i0 < kColumns; i0 += kRound) {
+        uint32_t x[kRound];
         f32x2 p[kRound / 2];
         float4 l[kRound / 4];
+        tmem_load16(tmem + (2 * t + buf) * N + part * kColumns + i0, x);
 #pragma unroll
         for (int j = 0; j < kRound / 4; ++j) l[j] = lse2[i0 / 4 + j];
         tmem_wait_load();
-        if (i0 + kRound < N) {
-          load(i0 + kRound);
-        } else {
+        if (i0 + kRound == kColumns) {
           tensor_fence_before();
           mbar_arrive_one(&sh.taken[t][buf]);
         }
@@ -606,7 +603,7 @@ __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaite
 #pragma unroll
         for (int j = 0; j < kRound / 2; ++j) p[j] = f2_pack(exp2_fast(f2_lo(p[j])), exp2_fast(f2_hi(p[j])));
         if (partly) {
-          const int2* seen = reinterpret_cast<const int2*>(sh.seen[qs]) + i0 / 2;
+          const int2* seen = reinterpret_cast<const int2*>(sh.seen[qs] + part * kColumns) + i0 / 2;
 #pragma unroll
           for (int j = 0; j < kRound / 2; ++j) {
             const int2 e = seen[j];
@@ -624,8 +621,14 @@ __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaite
     const bool there = sh.there[ks][own / 32] >> lane & 1;
     __syncwarp();
     if (lane == 0) mbar_arrive_one(&sh.keys_left[ks]);
+    if constexpr (Shape::P == 2) {
+      if (part) sh.half[i & 1][t][tid] = w;
+      named_sync(2 + t, 256);
+      w += sh.half[i & 1][t][tid];
+    }
     if (!there) w = 0.f;
-    if (alone) {
+    if (part) {
+    } else if (alone) {
       if (mine) *to = old + w;
     } else {   // a part for the second kernel
       (g.first ? part1 : part0)[own] = w;
@@ -638,7 +641,7 @@ __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaite
 }
 
 template <int D, int FMT, int N>
-__global__ void __launch_bounds__(kWeightThreads, 1)
+__global__ void __launch_bounds__(WeightShape<D, N>::kThreads, 1)
     weights_kernel(AttnState st, AttnDims dm, WeightPlan plan, Batch ba, WeightCall call, Rows q, KvDev kv,
                    const __grid_constant__ LayerMaps maps) {
   using Shape = WeightShape<D, N>;
@@ -650,16 +653,16 @@ __global__ void __launch_bounds__(kWeightThreads, 1)
   if (warp == Shape::kMmaWarp) tmem_alloc(&sh.tmem, Shape::kColumns);
   if (tid == 0) {
     for (int i = 0; i < Shape::kQueryStages; ++i) {
-      mbar_init(&sh.query[i], kQueryWarps);
-      mbar_init(&sh.query_left[i], 1 + 4 * Shape::T);
+      mbar_init(&sh.query[i], Shape::kQueryWarps);
+      mbar_init(&sh.query_left[i], 1 + Shape::kMmaWarp);
     }
     for (int i = 0; i < Shape::kKeyStages; ++i) {
       mbar_init(&sh.keys[i], Shape::kKeyWarps);
-      mbar_init(&sh.keys_left[i], 1 + 4 * Shape::T);
+      mbar_init(&sh.keys_left[i], 1 + Shape::kMmaWarp);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(&sh.scores[i >> 1][i & 1], 1);
-      mbar_init(&sh.taken[i >> 1][i & 1], 128);
+      mbar_init(&sh.taken[i >> 1][i & 1], 128 * Shape::P);
     }
     sh.gave_up = 0;
     fence_barrier_init();
@@ -689,7 +692,7 @@ __global__ void __launch_bounds__(kWeightThreads, 1)
     if (warp < Shape::kMmaWarp) {
       float* part = st.part + (int64_t)cta * 2 * Shape::kSlots;
       add_up<D, FMT, N>(sh, wait, call, part, part + Shape::kSlots, split, total, ctas, walk,
-                        tmem + ((uint32_t)(warp & 3) << 21), warp >> 2, tid & 127);
+                        tmem + ((uint32_t)(warp & 3) << 21), (warp >> 2) / Shape::P, (warp >> 2) % Shape::P, tid & 127);
     } else if (warp == Shape::kMmaWarp) {
       issue_units<D, FMT, N>(smem_u32(ring), sh, wait, walk, tmem);
     } else if (warp < Shape::kKeyWarp) {
@@ -729,8 +732,8 @@ cudaError_t run_weights(const AttnState& st, const AttnDims& dm, const Batch& ba
                         const WeightCall& call, const Rows& q, const KvDev& kv, cudaStream_t stream) {
   using Shape = WeightShape<D, N>;
   static_assert(weights_smem<D, N>(kMaxSeqs) + sizeof(WeightShared<D, N>) <= 227 * 1024, "shared memory");
-  const WeightPlan plan = {Shape::kSlots, N == 16 ? 7 : 8, N, N == 16 ? 4 : 7, dm.rep, causal ? 1 : 0, dm.H, last};
-  const cudaError_t e = pdl_launch(weights_kernel<D, FMT, N>, dim3(kAttnCtas), kWeightThreads, weights_smem<D, N>(ba.n_seq),
+  const WeightPlan plan = {Shape::kSlots, Shape::T == 1 ? 7 : 8, N, N == 16 ? 4 : 7, dm.rep, causal ? 1 : 0, dm.H, last};
+  const cudaError_t e = pdl_launch(weights_kernel<D, FMT, N>, dim3(kAttnCtas), Shape::kThreads, weights_smem<D, N>(ba.n_seq),
                                    stream, st, dm, plan, ba, call, q, kv, layer_maps(dm, call.layer, kv, 128));
   if (e != cudaSuccess || N == 16) return e;   // 16 rows are one step: no unit is split
   return pdl_launch(weights_join_kernel, dim3(kAttnCtas), 256, 0, stream, st, ba, call);
