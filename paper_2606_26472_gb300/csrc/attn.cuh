@@ -126,7 +126,7 @@ size_t chunk_part_floats(const AttnDims& dm);
 cudaError_t launch_attention_weights(const AttnState& st, const AttnDims& dm, int layer, const Batch& ba, bool causal,
                                      int last, const Rows& q, const float* lse, bool add, float* w, int64_t stride_seq,
                                      int64_t stride_head, const KvDev& kv, cudaStream_t stream);
-cudaError_t weights_prepare(const AttnDims& dm);
+cudaError_t weights_prepare(const AttnDims& dm, bool* runs);
 size_t weights_part_floats();
 size_t attention_part_floats(const AttnDims& dm);
 cudaError_t attention_prepare(const AttnDims& dm, bool* runs);

@@ -14,7 +14,7 @@ struct epikv_attn_ctx {
   AttnState st;
   cudaStream_t last_stream;
   bool attention_runs;   // false: this build's attention kernels cannot be launched; the other operators can
-  bool chunk_runs;       // the same of the chunk's attention
+  bool chunk_runs, weights_run;   // the same of the chunk's attention and the weights
 };
 
 namespace {
@@ -193,7 +193,7 @@ epikv_status epikv_attn_init(epikv_attn_ctx** out, const epikv_attn_config* cfg,
   ctx->last_stream = stream;
   cudaError_t e = attention_prepare(dm, &ctx->attention_runs);
   if (e == cudaSuccess) e = chunk_prepare(dm, &ctx->chunk_runs);
-  if (e == cudaSuccess) e = weights_prepare(dm);
+  if (e == cudaSuccess) e = weights_prepare(dm, &ctx->weights_run);
   if (e == cudaSuccess) e = cudaMemsetAsync(ctx->st.err, 0, 4, stream);
   if (e != cudaSuccess) {
     free(ctx);
@@ -309,6 +309,7 @@ epikv_status epikv_attention_weights(epikv_attn_ctx* ctx, int32_t layer, int32_t
   if (!valid_batch(n_seq, d_seq_ids, d_cu_new, max_new, d_len, len_stride, &ba)) return EPIKV_EINVAL;
   if (!valid_rows(q, &qr) || q->type != EPIKV_TYPE_BF16 || !d_lse || ((uintptr_t)d_lse & 3u)) return EPIKV_EINVAL;
   if (!valid_weights(w, ctx->dm.S, ctx->dm.H, ctx->dm.T) || !valid_cache(ctx->dm, layer, kv, &kd)) return EPIKV_EINVAL;
+  if (!ctx->weights_run) return EPIKV_ECUDA;
   ctx->last_stream = stream;
   return cuda_status(launch_attention_weights(ctx->st, ctx->dm, layer, ba, causal, last, qr, d_lse, add, w->ptr,
                                               w->stride_seq, w->stride_head, kd, stream));

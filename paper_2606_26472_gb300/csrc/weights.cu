@@ -12,6 +12,8 @@
 // chunk: exponentials and products).  One CTA an SM takes an equal share of all
 // units' steps (chunk_plan.h); the few units that two shares meet in are joined
 // by a second kernel, part by part.
+#include <new>
+
 #include "chunk_plan.h"
 #include "kernels.h"
 #include "tensor.cuh"
@@ -20,22 +22,23 @@ namespace epikv {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+// Steps of 128 rows: the 8 warps that own slots hold 128 scores each, and take registers from the 8 others.
+constexpr int kLaunchRegs = 128, kOwnerRegs = 168, kOtherRegs = 88;
+static_assert(kOwnerRegs + kOtherRegs <= 2 * kLaunchRegs, "the owners would wait for registers that nobody gives");
 
-// N query rows a step; T tiles of 128 slots a unit, the columns of each in P parts: four warps for each part of a tile, a
-// thread a slot.  (One part of 128 columns left two warps a scheduler, which hid little of a column's latencies: a prompt of
-// 4,096 tokens 112 us, two parts XX.)
+// N query rows a step; T tiles of 128 slots a unit, each with four warps that own its slots.
 template <int D, int N>
 struct WeightShape {
-  static constexpr int T = N == 16 && D == 256 ? 1 : 2, P = N == 16 ? 1 : 2;
-  static constexpr int kThreads = N == 16 ? 768 : 896;
-  static constexpr int kQueryWarps = N == 16 ? 4 : 8;
+  static constexpr int T = D == 256 ? 1 : 2;
+  static constexpr int kThreads = N == 16 ? 768 : 512;
+  static constexpr int kQueryWarps = 4;
   static constexpr int kSlots = 128 * T;
   static constexpr int kKeys = kSlots * D * 2;         // bytes of a unit's keys
   static constexpr int kQuery = N * D * 2;             // of a step's rows
-  static constexpr int kKeyStages = N == 16 ? (D == 64 ? 5 : D == 128 ? 3 : 2) : D == 256 ? 1 : 2;
-  static constexpr int kQueryStages = N == 16 ? kKeyStages : D == 64 ? 4 : D == 128 ? 2 : 1;
+  static constexpr int kKeyStages = N == 16 ? (D == 64 ? 5 : D == 128 ? 3 : 2) : D == 64 ? 2 : 1;
+  static constexpr int kQueryStages = N == 16 ? kKeyStages : D == 256 ? 2 : 4;
   static constexpr int kRing = kKeyStages * kKeys + kQueryStages * kQuery;
-  static constexpr int kMmaWarp = 4 * T * P, kQueryWarp = kMmaWarp + 1, kKeyWarp = kQueryWarp + kQueryWarps;
+  static constexpr int kMmaWarp = 4 * T, kQueryWarp = kMmaWarp + 1, kKeyWarp = kQueryWarp + kQueryWarps;
   static constexpr int kKeyWarps = kThreads / 32 - kKeyWarp;
   static constexpr int kKeyThreads = kKeyWarps * 32;
   static constexpr uint32_t kColumns = 2 * N * T < 32 ? 32 : 2 * N * T;   // two tiles of scores for each tile of slots
@@ -60,7 +63,6 @@ struct alignas(16) WeightShared {
   alignas(16) int seen[Shape::kQueryStages][N];            // slots that the row sees
   int partly[Shape::kQueryStages][Shape::kQueryWarps];            // not every row sees all slots of the unit
   int64_t offset[2][Shape::kSlots];
-  float half[2][Shape::P == 2 ? Shape::T : 1][Shape::P == 2 ? 128 : 1];         // sums of the tiles' second parts, units in turn
   WeightStart start;
 };
 
@@ -141,6 +143,16 @@ struct WeightWalk {
     return true;
   }
 };
+
+// kShared: the walk stands in shared memory, for a warp whose registers are full, and its first lane moves it on.
+template <bool kShared>
+__device__ __forceinline__ bool move_on(WeightWalk& walk, int lane) {
+  if constexpr (!kShared) return walk.next();
+  __syncwarp();
+  int more = 0;
+  if (lane == 0) more = walk.next();
+  return __shfl_sync(0xffffffffu, more, 0);
+}
 
 // Places before each entry of the batch, by a warp; an entry that cannot be taken has none, nor has one that takes the sum to
 // kTooManyTiles and those behind it.
@@ -398,17 +410,17 @@ struct KeyCopier {
 };
 
 // ------------------------------------------------------------------ query rows
-// Each warp brings so many rows of each step; a step's rows are under way while the one before is stored.
+// Each warp brings so many rows of each step.  bf16 rows are copied as they are, some steps in flight; those that become
+// halves are under way while the step before is stored.
 template <int D, int FMT, int N>
 __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh, const TensorWaiter& wait, const AttnState& st,
-                                             const AttnDims& dm, const WeightCall& call, const Rows& q, WeightWalk walk,
+                                             const AttnDims& dm, const WeightCall& call, const Rows& q, WeightWalk& walk,
                                              int warp, int lane) {
   using Shape = WeightShape<D, N>;
   constexpr bool kHalf = FMT != EPIKV_CACHE_BF16;
   constexpr int R = N / Shape::kQueryWarps;                     // rows of the warp
   constexpr int kPer = D / 8, kRows = 32 / kPer;         // pieces of a row; rows at once
   constexpr int kLoads = (R + kRows - 1) / kRows;
-  constexpr int kBatch = kLoads < 8 ? kLoads : 8;       // loads in flight
   const int piece = lane % kPer, sub = lane / kPer;
   const WeightSegment& g = walk.now;
   // the lane's row of a step is head `head` of the unit's token `token`; both go on from step to step
@@ -425,16 +437,9 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh,
     const int at = g.token + token, hq = g.kh * rep + head;
     const bool in = lane < R && at < g.e.n;
     r.src = (uint64_t)(q.p + ((int64_t)(g.e.tok0 + (in ? at : g.token)) * q.st + (in ? hq : g.kh * rep) * q.sh) * 2);
-    r.lse = in ? __ldg(call.lse + (int64_t)(g.e.tok0 + at) * dm.Hq + hq) : -INFINITY;
+    r.lse = in ? load_now(call.lse + (int64_t)(g.e.tok0 + at) * dm.Hq + hq) : -INFINITY;
     r.seen = walk.plan.causal ? g.e.len + at + 1 : g.e.len;
     return r;
-  };
-  auto load = [&](uint4 (&v)[kBatch], const Row& r, int l0) {
-#pragma unroll
-    for (int l = 0; l < kBatch; ++l) {
-      const int row = (l0 + l) * kRows + sub;
-      v[l] = __ldg(reinterpret_cast<const uint4*>(__shfl_sync(0xffffffffu, r.src, row & 31)) + piece);
-    }
   };
   auto advance = [&] {   // to the next step; false at the share's end
     if (++k < g.steps) {
@@ -447,7 +452,7 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh,
       return true;
     }
     do {
-      if (!walk.next()) return false;
+      if (!move_on<N != 16>(walk, lane)) return false;
     } while (g.steps == 0);
     k = 0;
     token = own_token;
@@ -458,50 +463,86 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh,
     }
     return true;
   };
-  bool more = advance();
-  Row next = {}, now;
-  uint4 v[kBatch];
-  if (more) {
-    next = row_of();
-    load(v, next, 0);
-  }
-  for (int step = 0; more; ++step) {
-    now = next;
-    const int qs = step % Shape::kQueryStages;
+  auto source = [&](const Row& r, int row) {   // the lane's piece of a row
+    return reinterpret_cast<const uint4*>(__shfl_sync(0xffffffffu, r.src, row & 31)) + piece;
+  };
+  auto tell = [&](const Row& r, int qs, float back) {   // what is needed beside the rows
+    if (lane < R) {
+      sh.lse2[qs][own] = -r.lse * kLog2e;
+      if constexpr (kHalf) sh.factor[qs][own] = call.c * head_scale(st, dm, 0, call.layer, g.kh) * back;
+      sh.seen[qs][own] = r.lse == -INFINITY ? 0 : r.seen;   // (the row saw nothing)
+    }
     const int upto = min(g.unit * Shape::kSlots + Shape::kSlots, g.slots);
+    const bool partly = __any_sync(0xffffffffu, lane < R && (r.lse == -INFINITY || r.seen < upto));
+    if (lane == 0) sh.partly[qs][warp] = partly;
+  };
+  auto deliver = [&](int step) {
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive_one(&sh.query[step % Shape::kQueryStages]);
+  };
+  auto stage = [&](int step) {   // waits for it to be free
+    const int qs = step % Shape::kQueryStages;
     if (step >= Shape::kQueryStages) wait(&sh.query_left[qs], (uint32_t)(step / Shape::kQueryStages - 1) & 1);
-    const uint32_t dst = smem_u32(ring + Shape::kKeyStages * Shape::kKeys + qs * Shape::kQuery);
-    float back = 1.f;
+    return smem_u32(ring + Shape::kKeyStages * Shape::kKeys + qs * Shape::kQuery);
+  };
+  bool more = advance();
+  Row next = {};
+  if (more) next = row_of();
+  int step = 0;
+  if constexpr (!kHalf) {
+    constexpr int kLag = Shape::kQueryStages - 1 < 2 ? Shape::kQueryStages - 1 : 2;   // steps in flight behind the newest
+    for (; more; ++step) {
+      const uint32_t dst = stage(step);
 #pragma unroll
-    for (int l0 = 0; l0 < kLoads; l0 += kBatch) {
-      if (l0) load(v, now, l0);
+      for (int l = 0; l < kLoads; ++l) {
+        const int row = l * kRows + sub;
+        const uint4* from = source(next, row);
+        if (row < R) copy_async16(dst + tile_at<D>(warp * R + row, piece), from, 16);
+      }
+      copy_commit();
+      tell(next, step % Shape::kQueryStages, 1.f);
+      more = advance();
+      if (more) next = row_of();
+      if (step >= kLag) {
+        copy_wait<kLag>();
+        deliver(step - kLag);
+      }
+    }
+    copy_wait<0>();
+    for (int k0 = max(0, step - kLag); k0 < step; ++k0) deliver(k0);
+  } else {
+    constexpr int kBatch = kLoads < 8 ? kLoads : 8;   // loads in flight
+    uint4 v[kBatch];
+    auto load = [&](const Row& r, int l0) {
 #pragma unroll
-      for (int l = 0; l < kBatch; ++l) {
-        const int row = (l0 + l) * kRows + sub;
-        uint4 x = v[l];
-        if constexpr (kHalf) {
+      for (int l = 0; l < kBatch; ++l) v[l] = load_now(source(r, (l0 + l) * kRows + sub));
+    };
+    if (more) load(next, 0);
+    for (; more; ++step) {
+      const Row now = next;
+      const uint32_t dst = stage(step);
+      float back = 1.f;
+#pragma unroll
+      for (int l0 = 0; l0 < kLoads; l0 += kBatch) {
+        if (l0) load(now, l0);
+#pragma unroll
+        for (int l = 0; l < kBatch; ++l) {
+          const int row = (l0 + l) * kRows + sub;
+          uint4 x = v[l];
           const float undo = halves_of<kPer>(x);   // of the row that the lane's piece is of
           const float mine = __shfl_sync(0xffffffffu, undo, lane % kRows * kPer);
           if (lane / kRows == l0 + l) back = mine;
+          if (row < R) sts16(dst + tile_at<D>(warp * R + row, piece), x);
         }
-        if (row < R) sts16(dst + tile_at<D>(warp * R + row, piece), x);
       }
-    }
-    if (lane < R) {
-      const bool counts = now.lse != -INFINITY;   // else the row saw nothing
-      sh.lse2[qs][warp * R + lane] = -now.lse * kLog2e;
-      if constexpr (kHalf) sh.factor[qs][warp * R + lane] = call.c * head_scale(st, dm, 0, call.layer, g.kh) * back;
-      sh.seen[qs][warp * R + lane] = counts ? now.seen : 0;
-    }
-    const bool partly = __any_sync(0xffffffffu, lane < R && (now.lse == -INFINITY || now.seen < upto));
-    if (lane == 0) sh.partly[qs][warp] = partly;
-    fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0) mbar_arrive_one(&sh.query[qs]);
-    more = advance();
-    if (more) {
-      next = row_of();
-      load(v, next, 0);
+      tell(now, step % Shape::kQueryStages, back);
+      deliver(step);
+      more = advance();
+      if (more) {
+        next = row_of();
+        load(next, 0);
+      }
     }
   }
 }
@@ -549,23 +590,21 @@ __device__ __forceinline__ void issue_units(uint32_t ring, WeightShared<D, N>& s
 // ------------------------------------------------------------------ sums
 template <int D, int FMT, int N>
 __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaiter& wait, const WeightCall& call, float* part0,
-                                       float* part1, ChunkSplit* split, unsigned total, int ctas, WeightWalk walk,
-                                       uint32_t tmem, int t, int part, int tid) {
+                                       float* part1, ChunkSplit* split, unsigned total, int ctas, WeightWalk& walk,
+                                       uint32_t tmem, int t, int tid) {
   using Shape = WeightShape<D, N>;
   constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
-  constexpr int kColumns = N / Shape::P;                        // of the thread's part
-  constexpr int kRound = 16;                                    // at once
   const WeightSegment& g = walk.now;
   int step = 0;
   const int lane = tid & 31, own = t * 128 + tid;
-  for (int i = 0; walk.next();) {
+  for (int i = 0; move_on<N != 16>(walk, lane);) {
     const int s = g.unit * Shape::kSlots + own;
     float* to = call.w + g.e.seq * call.stride_seq + g.kh * call.stride_head + s;
     const bool alone = g.first && g.last, mine = s < g.slots;
     float old = 0.f;   // on its way while the scores are formed
-    if (call.add && alone && mine && part == 0) old = *to;
+    if (call.add && alone && mine) old = *to;
     if (g.steps == 0) {
-      if (mine && !call.add && part == 0) *to = 0.f;
+      if (mine && !call.add) *to = 0.f;
       continue;
     }
     const int ks = i % Shape::kKeyStages;
@@ -576,43 +615,43 @@ __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaite
       const int qs = step % Shape::kQueryStages, buf = step & 1;
       wait(&sh.scores[t][buf], (uint32_t)(step / 2) & 1);
       tensor_fence_after();
-      const float4* lse2 = reinterpret_cast<const float4*>(sh.lse2[qs] + part * kColumns);
-      const float4* factor = reinterpret_cast<const float4*>(sh.factor[qs] + part * kColumns);
+      const float4* lse2 = reinterpret_cast<const float4*>(sh.lse2[qs]);
+      const float4* factor = reinterpret_cast<const float4*>(sh.factor[qs]);
       bool partly = false;
 #pragma unroll
       for (int w = 0; w < Shape::kQueryWarps; ++w) partly |= sh.partly[qs][w] != 0;
+      uint32_t x[N];   // all columns at once: their exponentials follow one another without a pause
+      const uint32_t from = tmem + (2 * t + buf) * N;
+      if constexpr (N == 16) {
+        tmem_load16(from, x);
+      } else {
 #pragma unroll
-      for (int i0 = 0; i0 < kColumns; i0 += kRound) {
-        uint32_t x[kRound];
-        f32x2 p[kRound / 2];
-        float4 l[kRound / 4];
-        tmem_load16(tmem + (2 * t + buf) * N + part * kColumns + i0, x);
-#pragma unroll
-        for (int j = 0; j < kRound / 4; ++j) l[j] = lse2[i0 / 4 + j];
-        tmem_wait_load();
-        if (i0 + kRound == kColumns) {
-          tensor_fence_before();
-          mbar_arrive_one(&sh.taken[t][buf]);
-        }
-#pragma unroll
-        for (int j = 0; j < kRound / 4; ++j) {
-          const float4 f = kBf16 ? make_float4(call.c, call.c, call.c, call.c) : factor[i0 / 4 + j];
-          p[2 * j] = f2_fma(f2_pack(__uint_as_float(x[4 * j]), __uint_as_float(x[4 * j + 1])), f2_pack(f.x, f.y), f2_pack(l[j].x, l[j].y));
-          p[2 * j + 1] = f2_fma(f2_pack(__uint_as_float(x[4 * j + 2]), __uint_as_float(x[4 * j + 3])), f2_pack(f.z, f.w), f2_pack(l[j].z, l[j].w));
-        }
-#pragma unroll
-        for (int j = 0; j < kRound / 2; ++j) p[j] = f2_pack(exp2_fast(f2_lo(p[j])), exp2_fast(f2_hi(p[j])));
-        if (partly) {
-          const int2* seen = reinterpret_cast<const int2*>(sh.seen[qs] + part * kColumns) + i0 / 2;
-#pragma unroll
-          for (int j = 0; j < kRound / 2; ++j) {
-            const int2 e = seen[j];
-            p[j] = f2_pack(s < e.x ? f2_lo(p[j]) : 0.f, s < e.y ? f2_hi(p[j]) : 0.f);
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < kRound / 2; ++j) sum[j & 3] = f2_add(sum[j & 3], p[j]);
+        for (int j = 0; j < N; j += 32) tmem_load32(from + j, x + j);
       }
+      tmem_wait_load();
+      tensor_fence_before();
+      mbar_arrive_one(&sh.taken[t][buf]);
+      auto columns = [&](auto masked) {
+#pragma unroll
+        for (int j = 0; j < N; j += 4) {
+          const float4 l = lse2[j / 4];
+          const float4 f = kBf16 ? make_float4(call.c, call.c, call.c, call.c) : factor[j / 4];
+          const f32x2 a = f2_fma(f2_pack(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), f2_pack(f.x, f.y), f2_pack(l.x, l.y));
+          const f32x2 b = f2_fma(f2_pack(__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])), f2_pack(f.z, f.w), f2_pack(l.z, l.w));
+          float p[4] = {exp2_fast(f2_lo(a)), exp2_fast(f2_hi(a)), exp2_fast(f2_lo(b)), exp2_fast(f2_hi(b))};
+          if constexpr (decltype(masked)::value) {
+            const int4 e = reinterpret_cast<const int4*>(sh.seen[qs])[j / 4];
+            p[0] = s < e.x ? p[0] : 0.f;
+            p[1] = s < e.y ? p[1] : 0.f;
+            p[2] = s < e.z ? p[2] : 0.f;
+            p[3] = s < e.w ? p[3] : 0.f;
+          }
+          sum[j / 2 & 2] = f2_add(sum[j / 2 & 2], f2_pack(p[0], p[1]));
+          sum[(j / 2 & 2) + 1] = f2_add(sum[(j / 2 & 2) + 1], f2_pack(p[2], p[3]));
+        }
+      };
+      if (partly) columns(std::true_type{});
+      else columns(std::false_type{});
       __syncwarp();
       if (lane == 0) mbar_arrive_one(&sh.query_left[qs]);
     }
@@ -621,14 +660,8 @@ __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaite
     const bool there = sh.there[ks][own / 32] >> lane & 1;
     __syncwarp();
     if (lane == 0) mbar_arrive_one(&sh.keys_left[ks]);
-    if constexpr (Shape::P == 2) {
-      if (part) sh.half[i & 1][t][tid] = w;
-      named_sync(2 + t, 256);
-      w += sh.half[i & 1][t][tid];
-    }
     if (!there) w = 0.f;
-    if (part) {
-    } else if (alone) {
+    if (alone) {
       if (mine) *to = old + w;
     } else {   // a part for the second kernel
       (g.first ? part1 : part0)[own] = w;
@@ -662,7 +695,7 @@ __global__ void __launch_bounds__(WeightShape<D, N>::kThreads, 1)
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(&sh.scores[i >> 1][i & 1], 1);
-      mbar_init(&sh.taken[i >> 1][i & 1], 128 * Shape::P);
+      mbar_init(&sh.taken[i >> 1][i & 1], 128);
     }
     sh.gave_up = 0;
     fence_barrier_init();
@@ -688,20 +721,30 @@ __global__ void __launch_bounds__(WeightShape<D, N>::kThreads, 1)
   const int cta = blockIdx.x, ctas = (int)min(total, (unsigned)kAttnCtas);
   if (cta < ctas) {
     const TensorWaiter wait{&sh.gave_up, st.err};
-    const WeightWalk walk(pre, ba, plan, sh.start, share_start(cta, total, ctas), share_start(cta + 1, total, ctas));
+    const WeightWalk start(pre, ba, plan, sh.start, share_start(cta, total, ctas), share_start(cta + 1, total, ctas));
+    __shared__ alignas(16) char walks[N == 16 ? 1 : Shape::kKeyWarp][sizeof(WeightWalk)];
+    WeightWalk own = start;
+    WeightWalk* shared = reinterpret_cast<WeightWalk*>(walks[N == 16 ? 0 : min(warp, Shape::kKeyWarp - 1)]);
+    if (N != 16 && lane == 0 && warp < Shape::kKeyWarp) new (shared) WeightWalk(start);
+    __syncwarp();
+    WeightWalk& walk = N == 16 ? own : *shared;
     if (warp < Shape::kMmaWarp) {
+      if constexpr (N != 16) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kOwnerRegs));
       float* part = st.part + (int64_t)cta * 2 * Shape::kSlots;
       add_up<D, FMT, N>(sh, wait, call, part, part + Shape::kSlots, split, total, ctas, walk,
-                        tmem + ((uint32_t)(warp & 3) << 21), (warp >> 2) / Shape::P, (warp >> 2) % Shape::P, tid & 127);
-    } else if (warp == Shape::kMmaWarp) {
-      issue_units<D, FMT, N>(smem_u32(ring), sh, wait, walk, tmem);
-    } else if (warp < Shape::kKeyWarp) {
-      copy_queries<D, FMT, N>(ring, sh, wait, st, dm, call, q, walk, warp - Shape::kQueryWarp, lane);
+                        tmem + ((uint32_t)(warp & 3) << 21), warp >> 2, tid & 127);
     } else {
-      const KeyCopier<D, FMT, N> copier{ring, sh, wait, dm, kv, maps, call.layer, st.err, tid - Shape::kKeyWarp * 32, lane,
-                                        warp - Shape::kKeyWarp};
-      if constexpr (FMT == EPIKV_CACHE_BF16) copier.run_bf16(walk);
-      else copier.run_q4(walk);
+      if constexpr (N != 16) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kOtherRegs));
+      if (warp == Shape::kMmaWarp) {
+        issue_units<D, FMT, N>(smem_u32(ring), sh, wait, own, tmem);
+      } else if (warp < Shape::kKeyWarp) {
+        copy_queries<D, FMT, N>(ring, sh, wait, st, dm, call, q, walk, warp - Shape::kQueryWarp, lane);
+      } else {
+        const KeyCopier<D, FMT, N> copier{ring, sh, wait, dm, kv, maps, call.layer, st.err, tid - Shape::kKeyWarp * 32, lane,
+                                          warp - Shape::kKeyWarp};
+        if constexpr (FMT == EPIKV_CACHE_BF16) copier.run_bf16(own);
+        else copier.run_q4(own);
+      }
     }
   }
   tensor_fence_before();
@@ -712,14 +755,14 @@ __global__ void __launch_bounds__(WeightShape<D, N>::kThreads, 1)
 
 // Joins the parts of a unit that several shares hold, in their order.  A CTA for each share that starts such a unit; a
 // thread a slot.
-__global__ void __launch_bounds__(256) weights_join_kernel(AttnState st, Batch ba, WeightCall call) {
+__global__ void __launch_bounds__(256) weights_join_kernel(AttnState st, Batch ba, WeightCall call, int slots) {
   pdl_wait();
   pdl_trigger();
   const ChunkSplit s = reinterpret_cast<const ChunkSplit*>(st.splits)[blockIdx.x];
   const int own = threadIdx.x;
   if (!s.there || own >= s.rows) return;
-  float w = st.part[(int64_t)(2 * blockIdx.x + 1) * 256 + own];
-  for (int i = 1; i < s.parts; ++i) w += st.part[(int64_t)2 * (blockIdx.x + i) * 256 + own];
+  float w = st.part[(int64_t)(2 * blockIdx.x + 1) * slots + own];
+  for (int i = 1; i < s.parts; ++i) w += st.part[(int64_t)2 * (blockIdx.x + i) * slots + own];
   float* to = call.w + ba.seq_ids[s.b] * call.stride_seq + s.kh * call.stride_head + s.row0 + own;
   *to = call.add ? *to + w : w;
 }
@@ -736,19 +779,24 @@ cudaError_t run_weights(const AttnState& st, const AttnDims& dm, const Batch& ba
   const cudaError_t e = pdl_launch(weights_kernel<D, FMT, N>, dim3(kAttnCtas), Shape::kThreads, weights_smem<D, N>(ba.n_seq),
                                    stream, st, dm, plan, ba, call, q, kv, layer_maps(dm, call.layer, kv, 128));
   if (e != cudaSuccess || N == 16) return e;   // 16 rows are one step: no unit is split
-  return pdl_launch(weights_join_kernel, dim3(kAttnCtas), 256, 0, stream, st, ba, call);
+  return pdl_launch(weights_join_kernel, dim3(kAttnCtas), Shape::kSlots, 0, stream, st, ba, call, (int)Shape::kSlots);
 }
 
+// *runs becomes false where the compiler gave the kernel other registers than its warps' exchange of them counts on.
 template <int D, int FMT, int N>
-cudaError_t allow_weights() {
+cudaError_t allow_weights(bool* runs) {
+  cudaFuncAttributes at;
+  const cudaError_t e = cudaFuncGetAttributes(&at, weights_kernel<D, FMT, N>);
+  if (e != cudaSuccess) return e;
+  if (N != 16 && at.numRegs != kLaunchRegs) *runs = false;
   return cudaFuncSetAttribute(weights_kernel<D, FMT, N>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               weights_smem<D, N>(kMaxSeqs));
 }
 
 template <int D, int FMT>
-cudaError_t prepare_dim() {
-  const cudaError_t e = allow_weights<D, FMT, 16>();
-  return e == cudaSuccess ? allow_weights<D, FMT, 128>() : e;
+cudaError_t prepare_dim(bool* runs) {
+  const cudaError_t e = allow_weights<D, FMT, 16>(runs);
+  return e == cudaSuccess ? allow_weights<D, FMT, 128>(runs) : e;
 }
 
 // ------------------------------------------------------------ into the eviction context
@@ -776,11 +824,12 @@ __global__ void __launch_bounds__(256) weigh_kernel(DevState st, Dims dm, const 
 
 }  // namespace
 
-cudaError_t weights_prepare(const AttnDims& dm) {
+cudaError_t weights_prepare(const AttnDims& dm, bool* runs) {
+  *runs = true;
   const bool bf16 = dm.fmt == EPIKV_CACHE_BF16;
-  if (dm.d == 64) return bf16 ? prepare_dim<64, EPIKV_CACHE_BF16>() : prepare_dim<64, EPIKV_CACHE_E2M1>();
-  if (dm.d == 128) return bf16 ? prepare_dim<128, EPIKV_CACHE_BF16>() : prepare_dim<128, EPIKV_CACHE_E2M1>();
-  return bf16 ? prepare_dim<256, EPIKV_CACHE_BF16>() : prepare_dim<256, EPIKV_CACHE_E2M1>();
+  if (dm.d == 64) return bf16 ? prepare_dim<64, EPIKV_CACHE_BF16>(runs) : prepare_dim<64, EPIKV_CACHE_E2M1>(runs);
+  if (dm.d == 128) return bf16 ? prepare_dim<128, EPIKV_CACHE_BF16>(runs) : prepare_dim<128, EPIKV_CACHE_E2M1>(runs);
+  return bf16 ? prepare_dim<256, EPIKV_CACHE_BF16>(runs) : prepare_dim<256, EPIKV_CACHE_E2M1>(runs);
 }
 
 size_t weights_part_floats() { return (size_t)2 * kAttnCtas * 256; }
