@@ -136,7 +136,7 @@ struct SegmentWalk {
 template <int D>
 struct alignas(16) ChunkShared {
   static constexpr int kStages = ChunkShape<D>::kStages;
-  uint64_t query, full[kStages], empty[kStages], scores[2], weights[2][2], sums, done, landed;
+  uint64_t query, full[kStages], empty[kStages], scores[2], weights[2][2], sums, done, landed, drained;
   uint32_t tmem;
   int gave_up;
   volatile int unclean[4];                  // 1 + the last segment with an infinite or NaN value in a slot that not all its rows see
@@ -772,6 +772,7 @@ __global__ void __launch_bounds__(chunk_threads(FMT), 1)
     mbar_init(&sh.sums, 1);
     mbar_init(&sh.done, 1);
     mbar_init(&sh.landed, 1);
+    mbar_init(&sh.drained, 1);
     sh.gave_up = 0;
     sh.split = {};
     for (int i = 0; i < 4; ++i) sh.unclean[i] = 0;
@@ -845,7 +846,9 @@ __global__ void __launch_bounds__(chunk_threads(FMT), 1)
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(other_regs(FMT)));
       if (warp == 8) {
         issue_products<D, FMT, kTiles>(smem_u32(smem), smem_u32(ring), sh, wait, walk, tmem);
+        if (elected()) products_done(&sh.drained);   // tensor memory is not freed under products, whatever waits gave up
         __syncwarp();
+        mbar_wait_bounded(&sh.drained, 0, kTensorWaitNs);
       } else if (warp > 8) {
         const Copier<D, FMT> copier{ring, sh, wait, dm, kv, maps, layer, st.err, tid - 288, lane, warp - 9};
         copier.run(walk);

@@ -342,19 +342,29 @@ struct CodeRows {
       }
     }
   }
+  // Lane by lane the four 16-byte parts of a piece are written in an order that gives eight neighbouring lanes eight places of
+  // a swizzled block's 128 bytes: part k becomes k ^ turn.
   __device__ __forceinline__ void store(uint32_t tile, int first, int rows, int tid) const {
     const int p = tid % kPer, r0 = first + tid / kPer;
+    static_assert(kPer != 4 || kStep % 2 == 0, "a thread's rows have one parity");
+    const int turn = kPer == 2 ? 0 : kPer == 4 ? (p >> 1) ^ ((r0 & 1) << 1) : p >> 1;
     uint32_t at[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) at[k] = tile + tile_at<D>(r0, p * 4 + k);
+    for (int k = 0; k < 4; ++k) at[k] = tile + tile_at<D>(r0, p * 4 + (k ^ turn));
 #pragma unroll
     for (int u = 0; u < R; ++u) {
       if (r0 + u * kStep >= rows) break;
-      uint4 v[4];
-      expand32(code[u], scale[u], v);
+      uint4 w = code[u], v[4];
+      uint32_t s = scale[u];
+      if (kPer != 2 && (turn & 1)) w = make_uint4(w.y, w.x, w.w, w.z);
+      if (kPer != 2 && (turn & 2)) {
+        w = make_uint4(w.z, w.w, w.x, w.y);
+        s = __byte_perm(s, 0, 0x3201);
+      }
+      expand32(w, s, v);
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        sts16(kStep % 8 == 0 ? at[k] + u * (kStep / 8) * (D * 16) : tile + tile_at<D>(r0 + u * kStep, p * 4 + k), v[k]);
+        sts16(kStep % 8 == 0 ? at[k] + u * (kStep / 8) * (D * 16) : tile + tile_at<D>(r0 + u * kStep, p * 4 + (k ^ turn)), v[k]);
     }
   }
 };

@@ -36,7 +36,12 @@ struct WeightShape {
   static constexpr int kKeys = kSlots * D * 2;         // bytes of a unit's keys
   static constexpr int kQuery = N * D * 2;             // of a step's rows
   static constexpr int kKeyStages = N == 16 ? (D == 64 ? 5 : D == 128 ? 3 : 2) : D == 64 ? 2 : 1;
-  static constexpr int kQueryStages = N == 16 ? kKeyStages : D == 256 ? 2 : 4;
+  static constexpr int kQueryStages = N == 16 ? (D == 256 ? 4 : kKeyStages) : D == 256 ? 2 : 4;
+  // A step's rows come by one of those warps, the steps in turn; else by all.  No more of them take turns than the ring has
+  // stages: a warp then knows, by its last step's wait for a stage, that all uses of the next step's stage are over but the
+  // last, and one bit tells that one's end.
+  static constexpr bool kTurns = N == 16;
+  static constexpr int kTurnWarps = kQueryWarps < kQueryStages ? kQueryWarps : kQueryStages;
   static constexpr int kRing = kKeyStages * kKeys + kQueryStages * kQuery;
   static constexpr int kMmaWarp = 4 * T, kQueryWarp = kMmaWarp + 1, kKeyWarp = kQueryWarp + kQueryWarps;
   static constexpr int kKeyWarps = kThreads / 32 - kKeyWarp;
@@ -54,7 +59,7 @@ template <int D, int N>
 struct alignas(16) WeightShared {
   using Shape = WeightShape<D, N>;
   uint64_t keys[Shape::kKeyStages], keys_left[Shape::kKeyStages], query[Shape::kQueryStages], query_left[Shape::kQueryStages];
-  uint64_t scores[2][2], taken[2][2];
+  uint64_t scores[2][2], taken[2][2], drained;
   uint32_t tmem;
   int gave_up;
   uint32_t there[Shape::kKeyStages][Shape::kSlots / 32];   // the slot is in the view
@@ -410,21 +415,21 @@ struct KeyCopier {
 };
 
 // ------------------------------------------------------------------ query rows
-// Each warp brings so many rows of each step.  bf16 rows are copied as they are, some steps in flight; those that become
-// halves are under way while the step before is stored.
+// bf16 rows are copied as they are, those that become halves are under way while the warp's step before is stored.  (A unit of
+// a decode step takes a warp 2,900 cycles from end to end, so several take turns; of 128 rows each takes a quarter.)
 template <int D, int FMT, int N>
 __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh, const TensorWaiter& wait, const AttnState& st,
                                              const AttnDims& dm, const WeightCall& call, const Rows& q, WeightWalk& walk,
                                              int warp, int lane) {
   using Shape = WeightShape<D, N>;
   constexpr bool kHalf = FMT != EPIKV_CACHE_BF16;
-  constexpr int R = N / Shape::kQueryWarps;                     // rows of the warp
+  constexpr int R = Shape::kTurns ? N : N / Shape::kQueryWarps;   // rows of the warp
   constexpr int kPer = D / 8, kRows = 32 / kPer;         // pieces of a row; rows at once
   constexpr int kLoads = (R + kRows - 1) / kRows;
   const int piece = lane % kPer, sub = lane / kPer;
   const WeightSegment& g = walk.now;
   // the lane's row of a step is head `head` of the unit's token `token`; both go on from step to step
-  const int rep = dm.rep, own = warp * R + lane, own_token = own / rep, own_head = own - own_token * rep;
+  const int rep = dm.rep, row0 = Shape::kTurns ? 0 : warp * R, own = row0 + lane, own_token = own / rep, own_head = own - own_token * rep;
   const int more_tokens = N / rep, more_heads = N - more_tokens * rep;
   int k = -1, token = 0, head = 0;
   struct Row {
@@ -474,7 +479,7 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh,
     }
     const int upto = min(g.unit * Shape::kSlots + Shape::kSlots, g.slots);
     const bool partly = __any_sync(0xffffffffu, lane < R && (r.lse == -INFINITY || r.seen < upto));
-    if (lane == 0) sh.partly[qs][warp] = partly;
+    if (lane == 0) sh.partly[qs][Shape::kTurns ? 0 : warp] = partly;
   };
   auto deliver = [&](int step) {
     fence_proxy_async_smem();
@@ -486,31 +491,42 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh,
     if (step >= Shape::kQueryStages) wait(&sh.query_left[qs], (uint32_t)(step / Shape::kQueryStages - 1) & 1);
     return smem_u32(ring + Shape::kKeyStages * Shape::kKeys + qs * Shape::kQuery);
   };
-  bool more = advance();
+  int step = -1;
+  auto go_on = [&] {   // to the warp's next step
+    do {
+      if (!advance()) return false;
+      ++step;
+    } while (Shape::kTurns && step % Shape::kTurnWarps != warp);
+    return true;
+  };
+  bool more = go_on();
   Row next = {};
   if (more) next = row_of();
-  int step = 0;
   if constexpr (!kHalf) {
-    constexpr int kLag = Shape::kQueryStages - 1 < 2 ? Shape::kQueryStages - 1 : 2;   // steps in flight behind the newest
-    for (; more; ++step) {
+    // Steps in flight behind the newest: none where warps take turns (the stage of a warp's next step may be that of one
+    // behind this one's).
+    constexpr int kLag = Shape::kTurns ? 0 : Shape::kQueryStages - 1 < 2 ? Shape::kQueryStages - 1 : 2;
+    int last = -1;
+    while (more) {
       const uint32_t dst = stage(step);
 #pragma unroll
       for (int l = 0; l < kLoads; ++l) {
         const int row = l * kRows + sub;
         const uint4* from = source(next, row);
-        if (row < R) copy_async16(dst + tile_at<D>(warp * R + row, piece), from, 16);
+        if (row < R) copy_async16(dst + tile_at<D>(row0 + row, piece), from, 16);
       }
       copy_commit();
       tell(next, step % Shape::kQueryStages, 1.f);
-      more = advance();
+      last = step;
+      more = go_on();
       if (more) next = row_of();
-      if (step >= kLag) {
+      if (last >= kLag) {
         copy_wait<kLag>();
-        deliver(step - kLag);
+        deliver(last - kLag);
       }
     }
     copy_wait<0>();
-    for (int k0 = max(0, step - kLag); k0 < step; ++k0) deliver(k0);
+    for (int k0 = max(0, last + 1 - kLag); k0 <= last; ++k0) deliver(k0);
   } else {
     constexpr int kBatch = kLoads < 8 ? kLoads : 8;   // loads in flight
     uint4 v[kBatch];
@@ -519,7 +535,7 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh,
       for (int l = 0; l < kBatch; ++l) v[l] = load_now(source(r, (l0 + l) * kRows + sub));
     };
     if (more) load(next, 0);
-    for (; more; ++step) {
+    while (more) {
       const Row now = next;
       const uint32_t dst = stage(step);
       float back = 1.f;
@@ -533,12 +549,12 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh,
           const float undo = halves_of<kPer>(x);   // of the row that the lane's piece is of
           const float mine = __shfl_sync(0xffffffffu, undo, lane % kRows * kPer);
           if (lane / kRows == l0 + l) back = mine;
-          if (row < R) sts16(dst + tile_at<D>(warp * R + row, piece), x);
+          if (row < R) sts16(dst + tile_at<D>(row0 + row, piece), x);
         }
       }
       tell(now, step % Shape::kQueryStages, back);
       deliver(step);
-      more = advance();
+      more = go_on();
       if (more) {
         next = row_of();
         load(next, 0);
@@ -619,7 +635,7 @@ __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaite
       const float4* factor = reinterpret_cast<const float4*>(sh.factor[qs]);
       bool partly = false;
 #pragma unroll
-      for (int w = 0; w < Shape::kQueryWarps; ++w) partly |= sh.partly[qs][w] != 0;
+      for (int w = 0; w < (Shape::kTurns ? 1 : Shape::kQueryWarps); ++w) partly |= sh.partly[qs][w] != 0;
       uint32_t x[N];   // all columns at once: their exponentials follow one another without a pause
       const uint32_t from = tmem + (2 * t + buf) * N;
       if constexpr (N == 16) {
@@ -686,7 +702,7 @@ __global__ void __launch_bounds__(WeightShape<D, N>::kThreads, 1)
   if (warp == Shape::kMmaWarp) tmem_alloc(&sh.tmem, Shape::kColumns);
   if (tid == 0) {
     for (int i = 0; i < Shape::kQueryStages; ++i) {
-      mbar_init(&sh.query[i], Shape::kQueryWarps);
+      mbar_init(&sh.query[i], Shape::kTurns ? 1 : Shape::kQueryWarps);
       mbar_init(&sh.query_left[i], 1 + Shape::kMmaWarp);
     }
     for (int i = 0; i < Shape::kKeyStages; ++i) {
@@ -697,6 +713,7 @@ __global__ void __launch_bounds__(WeightShape<D, N>::kThreads, 1)
       mbar_init(&sh.scores[i >> 1][i & 1], 1);
       mbar_init(&sh.taken[i >> 1][i & 1], 128);
     }
+    mbar_init(&sh.drained, 1);
     sh.gave_up = 0;
     fence_barrier_init();
   }
@@ -737,6 +754,9 @@ __global__ void __launch_bounds__(WeightShape<D, N>::kThreads, 1)
       if constexpr (N != 16) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kOtherRegs));
       if (warp == Shape::kMmaWarp) {
         issue_units<D, FMT, N>(smem_u32(ring), sh, wait, own, tmem);
+        if (elected()) products_done(&sh.drained);   // tensor memory is not freed under products, whatever waits gave up
+        __syncwarp();
+        mbar_wait_bounded(&sh.drained, 0, kTensorWaitNs);
       } else if (warp < Shape::kKeyWarp) {
         copy_queries<D, FMT, N>(ring, sh, wait, st, dm, call, q, walk, warp - Shape::kQueryWarp, lane);
       } else {

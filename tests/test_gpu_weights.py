@@ -80,6 +80,22 @@ def test_prompts(gpu_lib, bits, H, Hq, d):
 
 
 @pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("H,Hq,d,block", [(8, 32, 128, 16), (16, 32, 64, 0), (4, 8, 256, 32), (3, 24, 128, 7)])
+def test_decode_steps_of_long_caches(gpu_lib, bits, H, Hq, d, block):
+    """One token of sequences with so many slots that each SM takes dozens of runs of them: every ring goes round often."""
+    held = [5999 - 123 * b for b in range(24)]
+    c = R.Cache(seqs=24, T=6000, H=H, d=d, bits=bits, block=block, seed=d)
+    ctx = c.context(Hq, 1)
+    q = queries(24, Hq, d)
+    lse = lse64(c, q, [1] * 24, held)
+    w = fresh(c)
+    before = w.clone()
+    weigh(c, ctx, q, lse, [1] * 24, held, w)
+    check_weights(c, q, lse, [1] * 24, held, w, before)
+    assert E.epikv_attn_get_error(ctx) == OK
+
+
+@pytest.mark.parametrize("bits", [16, 4])
 def test_prefix_without_the_new_tokens(gpu_lib, bits):
     c = R.Cache(seqs=3, T=400, H=2, d=64, bits=bits, seed=2)
     ctx = c.context(6, 90)
