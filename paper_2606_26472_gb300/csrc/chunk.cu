@@ -420,8 +420,8 @@ struct Copier {
     deliver(i + 1);
   }
 
-  // 4-bit rows: a stage's codes are under way while the one before becomes halves, and the table's entries of the next tile
-  // before those.
+  // 4-bit rows: the next tile's codes are under way while this one's become halves, and the table's entries of the one behind
+  // it.
   __device__ __forceinline__ void q4_segment(const Segment& g, int i, int seg) const {
     constexpr int kStep = kCopyThreads / (D / 32), kRounds = (Shape::kSlots + kStep - 1) / kStep;
     static_assert(kCopyThreads >= Shape::kSlots, "a thread a slot");
@@ -438,20 +438,25 @@ struct Copier {
       if (tid < Shape::kSlots) sh.offset[j & 1][tid] = o;
       named_sync(1, kCopyThreads);
     };
+    auto load = [&](Codes& c, int w, int j) {
+      c.load(kv.base[w], sh.offset[j & 1], codes, scales, 0, Shape::kSlots, tid);
+    };
     Codes k, v;
     tell(g.t0, look(g.t0));
-    k.load(kv.base[0], sh.offset[g.t0 & 1], codes, scales, 0, Shape::kSlots, tid);
+    load(k, 0, g.t0);
+    load(v, 1, g.t0);
+    int64_t ahead = g.t0 + 1 < g.t1 ? look(g.t0 + 1) : -1;
     for (int j = g.t0; j < g.t1; ++j, i += 2) {
       const int s0 = j * Shape::kSlots;
-      v.load(kv.base[1], sh.offset[j & 1], codes, scales, 0, Shape::kSlots, tid);
-      const int64_t ahead = j + 1 < g.t1 ? look(j + 1) : -1;
+      const bool more = j + 1 < g.t1;
+      if (more) {
+        tell(j + 1, ahead);
+        ahead = j + 2 < g.t1 ? look(j + 2) : -1;
+      }
       left(i);
       k.store(stage(i), 0, Shape::kSlots, tid);
       deliver(i);
-      if (j + 1 < g.t1) {
-        tell(j + 1, ahead);
-        k.load(kv.base[0], sh.offset[(j + 1) & 1], codes, scales, 0, Shape::kSlots, tid);
-      }
+      if (more) load(k, 0, j + 1);
       left(i + 1);
       v.store(stage(i + 1), 0, Shape::kSlots, tid);
       if (s0 + Shape::kSlots > g.least) {
@@ -459,6 +464,7 @@ struct Copier {
         clean(i + 1, s0, g, seg);
       }
       deliver(i + 1);
+      if (more) load(v, 1, j + 1);
     }
     named_sync(1, kCopyThreads);   // the offsets are free for the next segment
   }
@@ -583,25 +589,39 @@ __device__ __forceinline__ void soften(ChunkShared<D>& sh, const TensorWaiter& w
     const uint32_t s = tmem + buf * 128;
     wait(&sh.scores[buf], kTiles == 1 ? (uint32_t)(a >> 1) & 1 : (uint32_t)a & 1);
     tensor_fence_after();
-    uint32_t x[N];
-#pragma unroll
-    for (int i = 0; i < N; i += 32) tmem_load32(s + i, x + i);
-    tmem_wait_load();
+    // With the registers for it a tile's scores are held; else they are read twice, 32 on their way beside those in use.
+    constexpr bool kHeld = kBf16;
+    constexpr int kParts = N / 32;
+    uint32_t x[kHeld ? kParts : 2][32];
     const int s0 = j * N;
-    if (__any_sync(0xffffffffu, seen < s0 + N)) {
+    const bool edge = __any_sync(0xffffffffu, seen < s0 + N);   // (warp-uniform)
+    auto load = [&](int i) { tmem_load32(s + 32 * i, x[kHeld ? i : i & 1]); };
+    auto part = [&](int i) -> uint32_t(&)[32] { return x[kHeld ? i : i & 1]; };
+    auto ready = [&](int i) {   // part i is there, the next one on its way; what the row does not see is minus infinity
+      tmem_wait_load();
+      if (!kHeld && i + 1 < kParts) load(i + 1);
+      if (edge) {
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (s0 + i >= seen) x[i] = 0xff800000u;
+        for (int u = 0; u < 32; ++u)
+          if (s0 + 32 * i + u >= seen) part(i)[u] = 0xff800000u;
+      }
+    };
+    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    if constexpr (kHeld) {
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) load(i);
+    } else {
+      load(0);
     }
-    float top[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top[i] = max3(__uint_as_float(x[i]), __uint_as_float(x[i + 4]), __uint_as_float(x[i + 8]));
+    for (int i = 0; i < kParts; ++i) {
+      ready(i);
 #pragma unroll
-    for (int i = 12; i + 7 < N; i += 8)
+      for (int u = 0; u < 32; u += 8)
 #pragma unroll
-      for (int u = 0; u < 4; ++u) top[u] = max3(top[u], __uint_as_float(x[i + u]), __uint_as_float(x[i + u + 4]));
-#pragma unroll
-    for (int u = 0; u < 4; ++u) top[u] = fmaxf(top[u], __uint_as_float(x[N - 4 + u]));
+        for (int w = 0; w < 4; ++w)
+          top[w] = max3(top[w], __uint_as_float(part(i)[u + w]), __uint_as_float(part(i)[u + w + 4]));
+    }
     const float high = fmaxf(max3(top[0], top[1], top[2]), top[3]) * c;
     const bool up = high > m + kSlack;
     if (__any_sync(0xffffffffu, up)) {
@@ -628,12 +648,15 @@ __device__ __forceinline__ void soften(ChunkShared<D>& sh, const TensorWaiter& w
     const float base = (m == -INFINITY ? 0.f : m) - (kBf16 ? 0.f : 7.f);
     const f32x2 cc = f2_pack(c, c), bb = f2_pack(-base, -base);
     f32x2 sum[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
+    if constexpr (!kHeld) load(0);
 #pragma unroll
     for (int i = 0; i < N; i += 32) {
       uint32_t y[16];
+      if constexpr (!kHeld) ready(i / 32);
+      const uint32_t(&x)[32] = part(i / 32);
 #pragma unroll
       for (int u = 0; u < 32; u += 2) {
-        const f32x2 z = f2_fma(f2_pack(__uint_as_float(x[i + u]), __uint_as_float(x[i + u + 1])), cc, bb);
+        const f32x2 z = f2_fma(f2_pack(__uint_as_float(x[u]), __uint_as_float(x[u + 1])), cc, bb);
         const float p = exp2_fast(f2_lo(z)), q = exp2_fast(f2_hi(z));
         sum[u >> 1 & 1] = f2_add(sum[u >> 1 & 1], f2_pack(p, q));
         y[u / 2] = kBf16 ? bf16_pair(p, q) : half_pair(p, q);

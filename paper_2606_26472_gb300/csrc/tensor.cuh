@@ -172,6 +172,11 @@ __device__ __forceinline__ float load_now(const float* p) {
   asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(v) : "l"(p));
   return v;
 }
+__device__ __forceinline__ uint32_t load_now(const uint16_t* p) {
+  uint16_t v;
+  asm volatile("ld.global.nc.u16 %0, [%1];" : "=h"(v) : "l"(p));
+  return v;
+}
 __device__ __forceinline__ uint4 load_now(const uint4* p) {
   uint4 v;
   asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
@@ -264,22 +269,31 @@ __device__ __forceinline__ void expand32(const uint4& codes, uint32_t scales, ui
   }
 }
 
-// Eight bf16 queries as halves.  The kPer lanes that hold a row scale it by a power of two to below 2^15: exact down to 2^-31
-// of the row's largest.  Returns what undoes the scaling.
-template <int kPer>
-__device__ __forceinline__ float halves_of(uint4& x) {
-  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-  uint32_t top = 0;   // largest magnitude, as bf16 bits: they are ordered like the values
+// Pieces of eight bf16 queries, M rows', as halves.  The kPer lanes that hold a row scale it by a power of two to below 2^15:
+// exact down to 2^-31 of the row's largest.  undo: what undoes the scaling.
+template <int kPer, int M>
+__device__ __forceinline__ void halves_of(uint4 (&x)[M], float (&undo)[M]) {
+  uint32_t top[M];   // largest magnitudes, as bf16 bits: they are ordered like the values
 #pragma unroll
-  for (int u = 0; u < 4; ++u) top = max(top, max(w[u] & 0x7fffu, w[u] >> 16 & 0x7fffu));
+  for (int i = 0; i < M; ++i) {
+    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+    top[i] = 0;
 #pragma unroll
-  for (int o = kPer / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-  // 2^e <= largest < 2^(e + 1); up to 2^100, so that neither factor leaves the normal numbers
-  const int up = min(14 - ((int)(top >> 7) - 127), 100);
-  const float mul = __uint_as_float((uint32_t)(up + 127) << 23);
-  x = make_uint4(half_pair(bf16_lo(x.x) * mul, bf16_hi(x.x) * mul), half_pair(bf16_lo(x.y) * mul, bf16_hi(x.y) * mul),
-                 half_pair(bf16_lo(x.z) * mul, bf16_hi(x.z) * mul), half_pair(bf16_lo(x.w) * mul, bf16_hi(x.w) * mul));
-  return __uint_as_float((uint32_t)(127 - up) << 23);
+    for (int u = 0; u < 4; ++u) top[i] = max(top[i], max(w[u] & 0x7fffu, w[u] >> 16 & 0x7fffu));
+  }
+#pragma unroll
+  for (int o = kPer / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < M; ++i) top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], o));
+#pragma unroll
+  for (int i = 0; i < M; ++i) {
+    // 2^e <= largest < 2^(e + 1); up to 2^100, so that neither factor leaves the normal numbers
+    const int up = min(14 - ((int)(top[i] >> 7) - 127), 100);
+    const float mul = __uint_as_float((uint32_t)(up + 127) << 23);
+    undo[i] = __uint_as_float((uint32_t)(127 - up) << 23);
+    x[i] = make_uint4(half_pair(bf16_lo(x[i].x) * mul, bf16_hi(x[i].x) * mul), half_pair(bf16_lo(x[i].y) * mul, bf16_hi(x[i].y) * mul),
+                      half_pair(bf16_lo(x[i].z) * mul, bf16_hi(x[i].z) * mul), half_pair(bf16_lo(x[i].w) * mul, bf16_hi(x[i].w) * mul));
+  }
 }
 
 // A warp's 32 rows of D bf16 queries into rows `row0` to row0 + 31 of a tile; src: each lane's row.  Lanes beside each other
@@ -289,7 +303,7 @@ template <int D, bool kHalf>
 __device__ __forceinline__ float store_queries(uint32_t tile, int row0, const void* src, int lane) {
   constexpr int kPer = D / 8;            // 16-byte pieces of a row: 8, 16 or 32
   constexpr int kRows = 32 / kPer;       // rows at once
-  constexpr int kAtOnce = 16;            // loads in flight
+  constexpr int kAtOnce = 32 / kRows < 16 ? 32 / kRows : 16;   // loads in flight
   const int piece = lane % kPer, sub = lane / kPer;
   const uint64_t mine = (uint64_t)src;
   float back = 1.f;
@@ -298,73 +312,66 @@ __device__ __forceinline__ float store_queries(uint32_t tile, int row0, const vo
     uint4 v[kAtOnce];
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i)
-      if (r0 + i < 32 / kRows)
-        v[i] = __ldg(reinterpret_cast<const uint4*>(__shfl_sync(0xffffffffu, mine, (r0 + i) * kRows + sub)) + piece);
+      v[i] = __ldg(reinterpret_cast<const uint4*>(__shfl_sync(0xffffffffu, mine, (r0 + i) * kRows + sub)) + piece);
+    float undo[kAtOnce];   // of the row that the lane's piece is of
+    if constexpr (kHalf) halves_of<kPer, kAtOnce>(v, undo);
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
-      if (r0 + i >= 32 / kRows) continue;
-      uint4 x = v[i];
       if constexpr (kHalf) {
-        const float undo = __shfl_sync(0xffffffffu, halves_of<kPer>(x), lane % kRows * kPer);   // to the lane that owns the row
-        if (lane / kRows == r0 + i) back = undo;
+        const float mine = __shfl_sync(0xffffffffu, undo[i], lane % kRows * kPer);   // to the lane that owns the row
+        if (lane / kRows == r0 + i) back = mine;
       }
-      sts16(tile + tile_at<D>(row0 + (r0 + i) * kRows + sub, piece), x);
+      sts16(tile + tile_at<D>(row0 + (r0 + i) * kRows + sub, piece), v[i]);
     }
   }
   return back;
 }
 
 // Pieces of 4-bit rows that each of kThreads threads turns into halves: 32 channels of every kStep-th row from row `first` on,
-// R rows at a time.
+// R rows at a time.  Eight neighbouring lanes have two pieces of four rows, whose parts fall on all eight places of a
+// swizzled block's 128 bytes.
 template <int D, int kThreads, int R>
 struct CodeRows {
   static constexpr int kPer = D / 32, kStep = kThreads / kPer;
-  static_assert(kThreads % kPer == 0, "a thread's pieces are of the same channels");
+  static_assert(kThreads % 32 == 0 && kPer <= 8, "a warp has whole rows");
   uint4 code[R];
   uint32_t scale[R];
+  uint32_t in;       // bit u: row u of the thread's is one
+  static __device__ __forceinline__ int piece_of(int tid) { return (tid >> 3) % (kPer / 2) * 2 + (tid & 1); }
+  static __device__ __forceinline__ int row_of(int tid) {
+    return tid / 32 * (32 / kPer) + (tid & 31) / (4 * kPer) * 4 + (tid >> 1 & 3);
+  }
   // `codes`, `scales`: the head's, in bytes of a row; offset: of the rows, elements (-1: zeros)
   __device__ __forceinline__ void load(const char* base, const int64_t* offset, int codes, int scales, int first, int rows,
                                        int tid) {
-    const int p = tid % kPer, r0 = first + tid / kPer;
+    const int p = piece_of(tid), r0 = first + row_of(tid);
     int64_t o[R];
 #pragma unroll
-    for (int u = 0; u < R; ++u) o[u] = r0 + u * kStep < rows ? offset[r0 + u * kStep] : -1;
+    for (int u = 0; u < R; ++u) o[u] = offset[min(r0 + u * kStep, rows - 1)];
     codes += p * 16;
     scales += p * 2;
+    in = 0;
 #pragma unroll
-    for (int u = 0; u < R; ++u) {
-      code[u] = make_uint4(0, 0, 0, 0);
-      scale[u] = 0;
-      if (o[u] >= 0) {
-        const char* row = base + o[u] * 2;
-        code[u] = __ldg(reinterpret_cast<const uint4*>(row + codes));
-        scale[u] = __ldg(reinterpret_cast<const uint16_t*>(row + scales));
-      }
+    for (int u = 0; u < R; ++u) {   // (a row that is not there: the first one's memory, times 0)
+      if (o[u] >= 0) in |= 1u << u;
+      const char* row = base + max(o[u], (int64_t)0) * 2;
+      code[u] = load_now(reinterpret_cast<const uint4*>(row + codes));
+      scale[u] = load_now(reinterpret_cast<const uint16_t*>(row + scales));
     }
   }
-  // Lane by lane the four 16-byte parts of a piece are written in an order that gives eight neighbouring lanes eight places of
-  // a swizzled block's 128 bytes: part k becomes k ^ turn.
   __device__ __forceinline__ void store(uint32_t tile, int first, int rows, int tid) const {
-    const int p = tid % kPer, r0 = first + tid / kPer;
-    static_assert(kPer != 4 || kStep % 2 == 0, "a thread's rows have one parity");
-    const int turn = kPer == 2 ? 0 : kPer == 4 ? (p >> 1) ^ ((r0 & 1) << 1) : p >> 1;
+    const int p = piece_of(tid), r0 = first + row_of(tid);
     uint32_t at[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) at[k] = tile + tile_at<D>(r0, p * 4 + (k ^ turn));
+    for (int k = 0; k < 4; ++k) at[k] = tile + tile_at<D>(r0, p * 4 + k);
 #pragma unroll
     for (int u = 0; u < R; ++u) {
       if (r0 + u * kStep >= rows) break;
-      uint4 w = code[u], v[4];
-      uint32_t s = scale[u];
-      if (kPer != 2 && (turn & 1)) w = make_uint4(w.y, w.x, w.w, w.z);
-      if (kPer != 2 && (turn & 2)) {
-        w = make_uint4(w.z, w.w, w.x, w.y);
-        s = __byte_perm(s, 0, 0x3201);
-      }
-      expand32(w, s, v);
+      uint4 v[4];
+      expand32(code[u], in >> u & 1 ? scale[u] : 0u, v);
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        sts16(kStep % 8 == 0 ? at[k] + u * (kStep / 8) * (D * 16) : tile + tile_at<D>(r0 + u * kStep, p * 4 + (k ^ turn)), v[k]);
+        sts16(kStep % 8 == 0 ? at[k] + u * (kStep / 8) * (D * 16) : tile + tile_at<D>(r0 + u * kStep, p * 4 + k), v[k]);
     }
   }
 };

@@ -49,6 +49,8 @@ struct WeightShape {
   static constexpr uint32_t kColumns = 2 * N * T < 32 ? 32 : 2 * N * T;   // two tiles of scores for each tile of slots
 };
 
+constexpr int kViews = 8;   // units that are on their way, at most: the ring of keys (up to 5) and two that are read
+
 // Where a CTA's share starts, and a walk along it.
 struct WeightStart {
   int b, unit, kh, step;
@@ -62,12 +64,13 @@ struct alignas(16) WeightShared {
   uint64_t scores[2][2], taken[2][2], drained;
   uint32_t tmem;
   int gave_up;
-  uint32_t there[Shape::kKeyStages][Shape::kSlots / 32];   // the slot is in the view
+  uint32_t there[kViews][Shape::kSlots / 32];              // the slot is in the view; units in turn
   alignas(16) float factor[Shape::kQueryStages][N];        // of a row's scores (4-bit rows; else the same for all)
   alignas(16) float lse2[Shape::kQueryStages][N];          // minus log2 of a row's sum
   alignas(16) int seen[Shape::kQueryStages][N];            // slots that the row sees
   int partly[Shape::kQueryStages][Shape::kQueryWarps];            // not every row sees all slots of the unit
   int64_t offset[2][Shape::kSlots];
+  uint32_t in_view[2][Shape::kSlots / 32];                 // beside the offsets: which of them are some
   WeightStart start;
 };
 
@@ -119,23 +122,43 @@ struct WeightWalk {
     all = weight_steps(plan, now.e.n, now.e.len, now.unit);
     places = all > 1 ? all : 1;
   }
-  // Moves `now` on to the next segment; false at the share's end.
+  __device__ __forceinline__ void to_next_unit() {
+    if (++now.kh < plan.heads) return;
+    now.kh = 0;
+    if (++now.unit == units) {
+      now.unit = 0;
+      do ++now.b;
+      while (pre[now.b + 1] == pre[now.b]);
+      now.e.tok0 = ba.cu_new[now.b];
+      now.e.n = ba.cu_new[now.b + 1] - now.e.tok0;
+      now.e.seq = ba.seq_ids[now.b];
+      now.e.len = ba.len[(int64_t)now.b * ba.len_stride];
+      entry();
+    }
+    unit();
+  }
+  // Where units have one step or none: on to the n-th of those with one that follow; false at the share's end.
+  __device__ __forceinline__ bool skip(int n) {
+    do {
+      if (x >= end) return false;
+      to_next_unit();
+      ++x;
+    } while (all == 0 || --n > 0);
+    now.step = 0;
+    now.steps = 1;
+    return true;
+  }
+  // Moves `now` on to the next segment; false at the share's end.  kOne: units have one step or none.
+  template <bool kOne>
   __device__ __forceinline__ bool next() {
     if (x >= end) return false;
-    // (a segment that does not end its unit is the share's last)
-    if (++now.kh == plan.heads) {
-      now.kh = 0;
-      if (++now.unit == units) {
-        now.unit = 0;
-        do ++now.b;
-        while (pre[now.b + 1] == pre[now.b]);
-        now.e.tok0 = ba.cu_new[now.b];
-        now.e.n = ba.cu_new[now.b + 1] - now.e.tok0;
-        now.e.seq = ba.seq_ids[now.b];
-        now.e.len = ba.len[(int64_t)now.b * ba.len_stride];
-        entry();
-      }
-      unit();
+    to_next_unit();   // (a segment that does not end its unit is the share's last)
+    if constexpr (kOne) {
+      ++x;
+      now.step = 0;
+      now.steps = all;
+      now.first = now.last = true;
+      return true;
     }
     const int take = (int)min((unsigned)(places - step), end - x);
     now.step = step;
@@ -149,13 +172,14 @@ struct WeightWalk {
   }
 };
 
-// kShared: the walk stands in shared memory, for a warp whose registers are full, and its first lane moves it on.
+// kShared: the walk stands in shared memory, for a warp whose registers are full (steps of 128 rows), and its first lane moves
+// it on.
 template <bool kShared>
 __device__ __forceinline__ bool move_on(WeightWalk& walk, int lane) {
-  if constexpr (!kShared) return walk.next();
+  if constexpr (!kShared) return walk.next<true>();
   __syncwarp();
   int more = 0;
-  if (lane == 0) more = walk.next();
+  if (lane == 0) more = walk.next<false>();
   return __shfl_sync(0xffffffffu, more, 0);
 }
 
@@ -257,7 +281,7 @@ struct KeyCopier {
     if (lane == 0) mbar_arrive_one(&sh.keys[i % Shape::kKeyStages]);
   }
   // Element offsets of a unit's slots (-1: none) and which of them are there, for all key threads.
-  __device__ __forceinline__ void offsets(int64_t* offset, const WeightSegment& g) const {
+  __device__ __forceinline__ void offsets(int64_t* offset, uint32_t* there, const WeightSegment& g) const {
     const int s0 = g.unit * Shape::kSlots;
     for (int r = tid; r < Shape::kSlots; r += kThreads) {
       int64_t o = -1;
@@ -266,24 +290,23 @@ struct KeyCopier {
         if (o < 0) set_error(err, EPIKV_DEV_SLOT);
       }
       offset[r] = o;
+      const uint32_t in = __ballot_sync(0xffffffffu, o >= 0);
+      if (lane == 0) there[r / 32] = in;
     }
     named_sync(1, kThreads);
   }
-  __device__ __forceinline__ void mark(int i, const int64_t* offset) const {   // (a warp's 32 slots a word)
-    for (int w = warp; w < Shape::kSlots / 32; w += Shape::kKeyWarps) {
-      const uint32_t in = offset ? __ballot_sync(0xffffffffu, offset[w * 32 + lane] >= 0) : 0xffffffffu;
-      if (lane == 0) sh.there[i % Shape::kKeyStages][w] = in;
-    }
+  __device__ __forceinline__ void mark(int i, const uint32_t* there) const {   // null: all of them
+    for (int w = tid; w < Shape::kSlots / 32; w += kThreads) sh.there[i % kViews][w] = there ? there[w] : 0xffffffffu;
   }
 
   __device__ __forceinline__ void run_bf16(WeightWalk walk) const {
     const bool flat = kv.layout == EPIKV_LAYOUT_CONTIGUOUS;
-    int i = 0, pending = 0, tables = 0, unit = -1, b = -1;
+    int i = 0, pending = 0, tables = 0, table = 0, unit = -1, b = -1;
     int64_t* offset = sh.offset[0];
     int y = 0, z = 0;
     bool whole = false, known = false;
     const WeightSegment& g = walk.now;
-    while (walk.next()) {
+    while (walk.next<N == 16>()) {
       if (g.steps == 0) continue;
       const int s0 = g.unit * Shape::kSlots;
       if (g.unit != unit || g.b != b) {   // the heads of the same slots follow one another
@@ -328,12 +351,13 @@ struct KeyCopier {
         continue;
       }
       if (!known) {   // the table before may still be read: two take turns, and all threads were here for the last one
-        offset = sh.offset[tables++ & 1];
-        offsets(offset, g);
+        table = tables++ & 1;
+        offset = sh.offset[table];
+        offsets(offset, sh.in_view[table], g);
         known = true;
       }
       left(i);
-      mark(i, offset);
+      mark(i, sh.in_view[table]);
       const uint32_t dst = stage(i);
       constexpr int kRound = 8;
       for (int x0 = tid; x0 < kPieces; x0 += kRound * kThreads) {
@@ -362,53 +386,54 @@ struct KeyCopier {
         mbar_wait_bounded(&sh.keys[k % Shape::kKeyStages], (uint32_t)(k / Shape::kKeyStages) & 1, kTensorWaitNs);
   }
 
-  // 4-bit rows: a unit's codes are under way while the one before becomes halves.
+  // 4-bit rows: the codes of the next two units are under way while one's become halves (one ahead, with what a unit takes
+  // in the ring, waited 1,000 cycles for them).
   __device__ __forceinline__ void run_q4(WeightWalk walk) const {
-    int i = 0, tables = 0, unit = -1, b = -1;
-    const int64_t* offset = sh.offset[0];
+    int tables = 0, table = 0, unit = -1, b = -1, found = 0;
     const WeightSegment& g = walk.now;
-    auto ahead = [&] {   // the next segment with rows, and its slots' offsets
-      while (walk.next()) {
+    auto ahead = [&] {   // the next segment with rows, its slots' offsets, and which of them are there
+      while (walk.next<N == 16>()) {
         if (g.steps == 0) continue;
         if (g.unit != unit || g.b != b) {
           unit = g.unit;
           b = g.b;
-          int64_t* o = sh.offset[tables++ & 1];
-          offsets(o, g);
-          offset = o;
+          table = tables++ & 1;
+          offsets(sh.offset[table], sh.in_view[table], g);
         }
+        mark(found++, sh.in_view[table]);
         return true;
       }
       return false;
     };
     using Codes = CodeRows<D, kThreads, kAtOnce>;
     auto load = [&](Codes& c, int first) {
-      c.load(kv.base[0], offset, g.kh * (D / 2), scale_offset(dm, g.kh), first, Shape::kSlots, tid);
+      c.load(kv.base[0], sh.offset[table], g.kh * (D / 2), scale_offset(dm, g.kh), first, Shape::kSlots, tid);
     };
-    bool more = ahead();
     if constexpr (kAhead) {
-      Codes now, next;
-      if (more) load(next, 0);
-      while (more) {
-        now = next;
-        left(i);
-        mark(i, offset);
-        more = ahead();
-        if (more) load(next, 0);
-        now.store(stage(i), 0, Shape::kSlots, tid);
-        deliver(i++);
+      Codes c[2];
+      bool more = true;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (more && (more = ahead())) load(c[u], 0);
+      for (int i = 0; i < found;) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          if (i >= found) break;
+          left(i);
+          c[u].store(stage(i), 0, Shape::kSlots, tid);
+          deliver(i++);
+          if (more && (more = ahead())) load(c[u], 0);
+        }
       }
     } else {
-      while (more) {
+      for (int i = 0; ahead(); ++i) {
         left(i);
-        mark(i, offset);
         for (int first = 0; first < Shape::kSlots; first += kAtOnce * kStep) {
           Codes c;
           load(c, first);
           c.store(stage(i), first, Shape::kSlots, tid);
         }
-        deliver(i++);
-        more = ahead();
+        deliver(i);
       }
     }
   }
@@ -493,11 +518,16 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh,
   };
   int step = -1;
   auto go_on = [&] {   // to the warp's next step
-    do {
-      if (!advance()) return false;
+    if constexpr (Shape::kTurns) {
+      const int by = step < 0 ? warp + 1 : Shape::kTurnWarps;
+      token = own_token;
+      head = own_head;
+      step += by;
+      return warp < Shape::kTurnWarps && walk.skip(by);
+    } else {
       ++step;
-    } while (Shape::kTurns && step % Shape::kTurnWarps != warp);
-    return true;
+      return advance();
+    }
   };
   bool more = go_on();
   Row next = {};
@@ -542,14 +572,14 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh,
 #pragma unroll
       for (int l0 = 0; l0 < kLoads; l0 += kBatch) {
         if (l0) load(now, l0);
+        float undo[kBatch];   // of the row that the lane's piece is of
+        halves_of<kPer, kBatch>(v, undo);
 #pragma unroll
         for (int l = 0; l < kBatch; ++l) {
           const int row = (l0 + l) * kRows + sub;
-          uint4 x = v[l];
-          const float undo = halves_of<kPer>(x);   // of the row that the lane's piece is of
-          const float mine = __shfl_sync(0xffffffffu, undo, lane % kRows * kPer);
+          const float mine = __shfl_sync(0xffffffffu, undo[l], lane % kRows * kPer);
           if (lane / kRows == l0 + l) back = mine;
-          if (row < R) sts16(dst + tile_at<D>(row0 + row, piece), x);
+          if (row < R) sts16(dst + tile_at<D>(row0 + row, piece), v[l]);
         }
       }
       tell(now, step % Shape::kQueryStages, back);
@@ -572,7 +602,7 @@ __device__ __forceinline__ void issue_units(uint32_t ring, WeightShared<D, N>& s
   const uint64_t k0 = rows_operand<D>(ring), q0 = rows_operand<D>(ring + Shape::kKeyStages * Shape::kKeys);
   const WeightSegment& g = walk.now;
   int step = 0;
-  for (int i = 0; walk.next();) {
+  for (int i = 0; walk.next<N == 16>();) {
     const int steps = __shfl_sync(0xffffffffu, g.steps, 0);
     if (steps == 0) continue;
     const int ks = i % Shape::kKeyStages;
@@ -673,7 +703,7 @@ __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaite
     }
     const f32x2 both = f2_add(f2_add(sum[0], sum[1]), f2_add(sum[2], sum[3]));
     float w = f2_lo(both) + f2_hi(both);
-    const bool there = sh.there[ks][own / 32] >> lane & 1;
+    const bool there = sh.there[i % kViews][own / 32] >> lane & 1;
     __syncwarp();
     if (lane == 0) mbar_arrive_one(&sh.keys_left[ks]);
     if (!there) w = 0.f;
