@@ -589,17 +589,17 @@ __device__ __forceinline__ void soften(ChunkShared<D>& sh, const TensorWaiter& w
     const uint32_t s = tmem + buf * 128;
     wait(&sh.scores[buf], kTiles == 1 ? (uint32_t)(a >> 1) & 1 : (uint32_t)a & 1);
     tensor_fence_after();
-    // With the registers for it a tile's scores are held; else they are read twice, 32 on their way beside those in use.
+    // bf16: a tile's scores are held, its columns one run of instructions.  Where warps beside these turn 4-bit rows into
+    // halves, that run and theirs do not fit the instruction cache together (8 x 256 tokens: 160 us, the cache behind it at
+    // 72 % of its rate): the scores are read twice there, in a loop over 32 columns.
     constexpr bool kHeld = kBf16;
     constexpr int kParts = N / 32;
-    uint32_t x[kHeld ? kParts : 2][32];
+    uint32_t x[kHeld ? kParts : 1][32];
     const int s0 = j * N;
     const bool edge = __any_sync(0xffffffffu, seen < s0 + N);   // (warp-uniform)
-    auto load = [&](int i) { tmem_load32(s + 32 * i, x[kHeld ? i : i & 1]); };
-    auto part = [&](int i) -> uint32_t(&)[32] { return x[kHeld ? i : i & 1]; };
-    auto ready = [&](int i) {   // part i is there, the next one on its way; what the row does not see is minus infinity
-      tmem_wait_load();
-      if (!kHeld && i + 1 < kParts) load(i + 1);
+    auto load = [&](int i) { tmem_load32(s + 32 * i, x[kHeld ? i : 0]); };
+    auto part = [&](int i) -> uint32_t(&)[32] { return x[kHeld ? i : 0]; };
+    auto mask = [&](int i) {   // what the row does not see is minus infinity
       if (edge) {
 #pragma unroll
         for (int u = 0; u < 32; ++u)
@@ -607,20 +607,27 @@ __device__ __forceinline__ void soften(ChunkShared<D>& sh, const TensorWaiter& w
       }
     };
     float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    if constexpr (kHeld) {
-#pragma unroll
-      for (int i = 0; i < kParts; ++i) load(i);
-    } else {
-      load(0);
-    }
-#pragma unroll
-    for (int i = 0; i < kParts; ++i) {
-      ready(i);
+    auto highest = [&](int i) {
+      mask(i);
 #pragma unroll
       for (int u = 0; u < 32; u += 8)
 #pragma unroll
         for (int w = 0; w < 4; ++w)
           top[w] = max3(top[w], __uint_as_float(part(i)[u + w]), __uint_as_float(part(i)[u + w + 4]));
+    };
+    if constexpr (kHeld) {
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) load(i);
+      tmem_wait_load();
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) highest(i);
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < kParts; ++i) {
+        load(i);
+        tmem_wait_load();
+        highest(i);
+      }
     }
     const float high = fmaxf(max3(top[0], top[1], top[2]), top[3]) * c;
     const bool up = high > m + kSlack;
@@ -648,12 +655,9 @@ __device__ __forceinline__ void soften(ChunkShared<D>& sh, const TensorWaiter& w
     const float base = (m == -INFINITY ? 0.f : m) - (kBf16 ? 0.f : 7.f);
     const f32x2 cc = f2_pack(c, c), bb = f2_pack(-base, -base);
     f32x2 sum[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
-    if constexpr (!kHeld) load(0);
-#pragma unroll
-    for (int i = 0; i < N; i += 32) {
+    auto soft = [&](int i) {
       uint32_t y[16];
-      if constexpr (!kHeld) ready(i / 32);
-      const uint32_t(&x)[32] = part(i / 32);
+      const uint32_t(&x)[32] = part(i);
 #pragma unroll
       for (int u = 0; u < 32; u += 2) {
         const f32x2 z = f2_fma(f2_pack(__uint_as_float(x[u]), __uint_as_float(x[u + 1])), cc, bb);
@@ -661,11 +665,23 @@ __device__ __forceinline__ void soften(ChunkShared<D>& sh, const TensorWaiter& w
         sum[u >> 1 & 1] = f2_add(sum[u >> 1 & 1], f2_pack(p, q));
         y[u / 2] = kBf16 ? bf16_pair(p, q) : half_pair(p, q);
       }
-      tmem_store16(s + i / 2, y);
-      if (i + 32 == N / 2 || i + 32 == N) {
+      tmem_store16(s + 16 * i, y);
+      if (i + 1 == kParts / 2 || i + 1 == kParts) {
         tmem_wait_store();
         tensor_fence_before();
-        mbar_arrive_one(&sh.weights[buf][i + 32 == N]);
+        mbar_arrive_one(&sh.weights[buf][i + 1 == kParts]);
+      }
+    };
+    if constexpr (kHeld) {
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) soft(i);
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < kParts; ++i) {
+        load(i);
+        tmem_wait_load();
+        mask(i);
+        soft(i);
       }
     }
     const f32x2 both = f2_add(sum[0], sum[1]);
