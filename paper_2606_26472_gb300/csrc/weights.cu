@@ -386,8 +386,7 @@ struct KeyCopier {
         mbar_wait_bounded(&sh.keys[k % Shape::kKeyStages], (uint32_t)(k / Shape::kKeyStages) & 1, kTensorWaitNs);
   }
 
-  // 4-bit rows: the codes of the next two units are under way while one's become halves (one ahead, with what a unit takes
-  // in the ring, waited 1,000 cycles for them).
+  // 4-bit rows: the next unit's codes are under way while one's become halves.
   __device__ __forceinline__ void run_q4(WeightWalk walk) const {
     int tables = 0, table = 0, unit = -1, b = -1, found = 0;
     const WeightSegment& g = walk.now;
@@ -410,20 +409,17 @@ struct KeyCopier {
       c.load(kv.base[0], sh.offset[table], g.kh * (D / 2), scale_offset(dm, g.kh), first, Shape::kSlots, tid);
     };
     if constexpr (kAhead) {
-      Codes c[2];
-      bool more = true;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-        if (more && (more = ahead())) load(c[u], 0);
-      for (int i = 0; i < found;) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          if (i >= found) break;
-          left(i);
-          c[u].store(stage(i), 0, Shape::kSlots, tid);
-          deliver(i++);
-          if (more && (more = ahead())) load(c[u], 0);
-        }
+      Codes now, next;
+      bool more = ahead();
+      if (more) load(next, 0);
+#pragma unroll 1
+      for (int i = 0; more; ++i) {
+        now = next;
+        more = ahead();
+        if (more) load(next, 0);
+        left(i);
+        now.store(stage(i), 0, Shape::kSlots, tid);
+        deliver(i);
       }
     } else {
       for (int i = 0; ahead(); ++i) {
