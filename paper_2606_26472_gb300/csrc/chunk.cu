@@ -47,10 +47,10 @@ struct Segment {
   int t0, t1;        // tiles of slots
   int least, most;   // slots that the item's first row sees, and its last
   bool first, last;  // the item starts, ends here
-  unsigned end;      // the line's tile behind the item
+  unsigned at, places;   // of the item in the line
 };
 
-// Where a CTA's share starts: entry, KV head, block, and the line's tile that the block starts at.
+// Where a CTA's share starts: entry, KV head, block, and the line's place that the block starts at.
 struct ShareStart {
   int b, kh, block;
   unsigned at;
@@ -61,7 +61,7 @@ struct ShareStart {
 // need stays out of their registers.  Segment i stands in now[i & 1] while the next one is looked at.
 struct WarpWalk {
   ShareStart here;
-  unsigned x;          // the share's next tile
+  unsigned x;          // the share's next place
   Segment now[2];
 };
 
@@ -76,7 +76,7 @@ __device__ __forceinline__ Entry entry_of(const Batch& ba, int b) {
 
 struct SegmentWalk {
   WarpWalk* w;
-  const unsigned* pre;   // [n_seq + 1] tiles before each entry
+  const unsigned* pre;   // [n_seq + 1] places before each entry
   const Batch& ba;
   const ChunkPlan& plan;
   unsigned end;          // of the share
@@ -92,7 +92,7 @@ struct SegmentWalk {
     ShareStart h = w->here;
     const Entry e = h.e;
     const unsigned x = w->x;
-    const unsigned tiles = (unsigned)block_tiles(plan, e.n, e.len, h.block), take = min(h.at + tiles, end) - x;
+    const unsigned places = (unsigned)block_places(plan, e.n, e.len, h.block), take = min(h.at + places, end) - x;
     s->e = e;
     s->b = h.b;
     s->kh = h.kh;
@@ -100,14 +100,15 @@ struct SegmentWalk {
     s->rows = min(e.n * plan.rep - s->row0, plan.rows);
     s->least = row_sees(plan, e.len, s->row0);
     s->most = block_sees(plan, e.n, e.len, h.block);
-    s->t0 = (int)(x - h.at);
-    s->t1 = min(s->t0 + (int)take, (s->most + plan.slots - 1) >> plan.slots_log);
+    s->t0 = tile_of_place((int)(x - h.at));
+    s->t1 = tile_of_place((int)(x - h.at + take));
     s->first = x == h.at;
-    s->last = x + take == h.at + tiles;
-    s->end = h.at + tiles;
+    s->last = x + take == h.at + places;
+    s->at = h.at;
+    s->places = places;
     w->x = x + take;
     if (s->last) {
-      h.at += tiles;
+      h.at += places;
       if (++h.block == chunk_blocks(plan, e.n)) {
         h.block = 0;
         if (++h.kh == plan.heads) {
@@ -142,11 +143,12 @@ struct alignas(16) ChunkShared {
   volatile int unclean[4];                  // 1 + the last segment with an infinite or NaN value in a slot that not all its rows see
   int64_t offset[2][ChunkShape<D>::kSlots]; // of a tile's slots, elements; -1: none
   ShareStart start;
+  unsigned from, to;                        // the CTA's share
   WarpWalk walk[16];
   ChunkSplit split;
 };
 
-// Tiles before each entry of the batch, by a warp; returns the items.  An entry that cannot be taken has none, nor has one
+// Places before each entry of the batch, by a warp; returns the items.  An entry that cannot be taken has none, nor has one
 // that takes the sum to kTooManyTiles and those behind it.
 __device__ __forceinline__ int64_t line_up(unsigned* pre, const Batch& ba, const AttnDims& dm, const ChunkPlan& plan,
                                            int32_t* err, int lane) {
@@ -161,14 +163,14 @@ __device__ __forceinline__ int64_t line_up(unsigned* pre, const Batch& ba, const
     const int blocks = taken ? chunk_blocks(plan, e.n) : 0;
     int64_t tiles = 0;
     if (__all_sync(0xffffffffu, blocks <= 8)) {
-      if (taken) tiles = head_tiles(plan, e.n, e.len);
+      if (taken) tiles = head_places(plan, e.n, e.len);
     } else {   // long entries one by one
       for (unsigned left = __ballot_sync(0xffffffffu, blocks > 0); left; left &= left - 1) {
         const int who = __ffs(left) - 1;
         const int en = __shfl_sync(0xffffffffu, e.n, who), len = __shfl_sync(0xffffffffu, e.len, who);
         const int eb = __shfl_sync(0xffffffffu, blocks, who);
         int64_t sum = 0;
-        for (int i = lane; i < eb; i += 32) sum += block_tiles(plan, en, len, i);
+        for (int i = lane; i < eb; i += 32) sum += block_places(plan, en, len, i);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         if (lane == who) tiles = sum;
@@ -204,8 +206,8 @@ __device__ __forceinline__ int64_t line_up(unsigned* pre, const Batch& ba, const
   return items;
 }
 
-// Where in the line tile x is, by a warp.
-__device__ __forceinline__ void find_tile(ShareStart* start, unsigned x, const unsigned* pre, const Batch& ba, const ChunkPlan& plan,
+// Where in the line place x is, by a warp; returns where a share that starts there does.
+__device__ __forceinline__ unsigned find_place(ShareStart* start, unsigned x, const unsigned* pre, const Batch& ba, const ChunkPlan& plan,
                                           int lane) {
   int lo = 0, hi = ba.n_seq - 1;   // the entry with pre[b] <= x < pre[b + 1]
   while (lo < hi) {
@@ -219,8 +221,9 @@ __device__ __forceinline__ void find_tile(ShareStart* start, unsigned x, const u
   unsigned at = pre[lo] + kh * of_head;
   const int blocks = chunk_blocks(plan, n);
   int block = 0;
+  unsigned places = 0;
   for (int b0 = 0; b0 < blocks; b0 += 32) {
-    const unsigned t = b0 + lane < blocks ? (unsigned)block_tiles(plan, n, len, b0 + lane) : 0u;
+    const unsigned t = b0 + lane < blocks ? (unsigned)block_places(plan, n, len, b0 + lane) : 0u;
     unsigned upto = t;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -232,11 +235,13 @@ __device__ __forceinline__ void find_tile(ShareStart* start, unsigned x, const u
       const int k = __ffs(behind) - 1;
       block = b0 + k;
       at += __shfl_sync(0xffffffffu, upto - t, k);
+      places = __shfl_sync(0xffffffffu, t, k);
       break;
     }
     at += __shfl_sync(0xffffffffu, upto, 31);
   }
   if (lane == 0) *start = {lo, (int)kh, block, at, e};
+  return moved_start(x, at, places);
 }
 
 // Element offset of each of the tile's slots, or -1.
@@ -825,8 +830,17 @@ __global__ void __launch_bounds__(chunk_threads(FMT), 1)
     if (lane == 0) items = n;
     __syncwarp();
     const unsigned total = pre[ba.n_seq];
-    const int ctas = chunk_ctas(total, n);
-    if ((int)blockIdx.x < ctas) find_tile(&sh.start, share_start(blockIdx.x, total, ctas), pre, ba, plan, lane);
+    const int ctas = chunk_ctas(total, n), cta = blockIdx.x;
+    if (cta < ctas) {
+      unsigned to = total;
+      if (cta + 1 < ctas) to = find_place(&sh.start, share_start(cta + 1, total, ctas), pre, ba, plan, lane);
+      unsigned from = find_place(&sh.start, share_start(cta, total, ctas), pre, ba, plan, lane);
+      if (from < to) from = find_place(&sh.start, from, pre, ba, plan, lane);   // (the item behind, or the same)
+      if (lane == 0) {
+        sh.from = from;
+        sh.to = to;
+      }
+    }
   }
   tensor_fence_before();
   __syncthreads();
@@ -836,8 +850,8 @@ __global__ void __launch_bounds__(chunk_threads(FMT), 1)
   const int cta = blockIdx.x, ctas = chunk_ctas(total, items);
   if (cta < ctas) {
     const TensorWaiter wait{&sh.gave_up, st.err};
-    const SegmentWalk walk{&sh.walk[warp], pre, ba, plan, share_start(cta + 1, total, ctas), lane};
-    walk.begin(sh.start, share_start(cta, total, ctas));
+    const SegmentWalk walk{&sh.walk[warp], pre, ba, plan, sh.to, lane};
+    walk.begin(sh.start, sh.from);
     if (warp < 4 * kTiles) {
       asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(owner_regs(FMT, kTiles)));
       const int t = warp >> 2;
@@ -879,7 +893,7 @@ __global__ void __launch_bounds__(chunk_threads(FMT), 1)
                                             : st.part + (int64_t)(2 * cta + (now.first ? 1 : 0)) * part_rows * (D + 2);
         put_rows<D, FMT>(st, dm, now, out, lse, kv, layer, part, part_rows, lanes + 256 + t * 128, tid, m, l, saw, unclean);
         if (tid == 0 && now.first && !now.last)
-          sh.split = {1, now.b, now.kh, now.row0, now.rows, share_of(now.end - 1, total, ctas) - cta + 1, {0, 0}};
+          sh.split = {1, now.b, now.kh, now.row0, now.rows, last_share(now.at, now.places, total, ctas) - cta + 1, {0, 0}};
       }
     } else {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(other_regs(FMT)));

@@ -3,7 +3,7 @@
 //
 // An item of the chunk's attention is (batch entry, KV head, block of query
 // rows).  Its slots are cut into tiles; all items' tiles stand in one line, which
-// the CTAs take in equal contiguous shares.  A share's piece of an item is a
+// the CTAs take in about equal contiguous shares.  A share's piece of an item is a
 // segment; an item of several segments is joined by a second kernel.
 #pragma once
 
@@ -30,38 +30,55 @@ EPIKV_PLAN int block_sees(const ChunkPlan& p, int n, int len, int block) {
   const int end = (block + 1) << p.rows_log, rows = n * p.rep;
   return row_sees(p, len, (end < rows ? end : rows) - 1);
 }
-// An item that sees nothing still has a place in the line: its rows' zeros are written.
-EPIKV_PLAN int block_tiles(const ChunkPlan& p, int n, int len, int block) {
-  const int t = (block_sees(p, n, len, block) + p.slots - 1) >> p.slots_log;
-  return t > 1 ? t : 1;
+// An item's places in the line: its tiles and kItemPlaces for its queries and results, which cost about as much as so many
+// tiles (4 to 8 us; counted by tiles alone, the shares of a prompt's first, short blocks took twice the others' time).  An
+// item that sees nothing has these all the same: its rows' zeros are written.
+constexpr int kItemPlaces = 4;
+EPIKV_PLAN int block_places(const ChunkPlan& p, int n, int len, int block) {
+  return ((block_sees(p, n, len, block) + p.slots - 1) >> p.slots_log) + kItemPlaces;
 }
-EPIKV_PLAN int64_t head_tiles(const ChunkPlan& p, int n, int len) {
+EPIKV_PLAN int64_t head_places(const ChunkPlan& p, int n, int len) {
   int64_t t = 0;
-  for (int i = 0; i < chunk_blocks(p, n); ++i) t += block_tiles(p, n, len, i);
+  for (int i = 0; i < chunk_blocks(p, n); ++i) t += block_places(p, n, len, i);
   return t;
 }
+// First tile behind so many of an item's places.
+EPIKV_PLAN int tile_of_place(int places) { return places > kItemPlaces ? places - kItemPlaces : 0; }
 
-// CTAs that share the line: one an item up to the GPU's, more where a share would be of over kLeastTiles tiles (a segment
-// costs its rows' queries and results, and a join, about as much as two to four tiles).
-constexpr int kLeastTiles = 4;
+// CTAs that share the line: one an item up to the GPU's, more where a share would be of over kLeastPlaces.
+constexpr int kLeastPlaces = 8;
 EPIKV_PLAN int chunk_ctas(unsigned total, int64_t items) {
-  int64_t n = ((int64_t)total + kLeastTiles - 1) / kLeastTiles;
+  int64_t n = ((int64_t)total + kLeastPlaces - 1) / kLeastPlaces;
   if (n < items) n = items;
   if (n > kAttnCtas) n = kAttnCtas;
   return n < (int64_t)total ? (int)n : (int)total;
 }
-// First tile of CTA c's share, floor(total * c / ctas) in 32 bits.
+// First place of CTA c's share, floor(total * c / ctas) in 32 bits.
 EPIKV_PLAN unsigned share_start(int c, unsigned total, int ctas) {
   const unsigned q = total / (unsigned)ctas, r = total % (unsigned)ctas;
   return q * c + r * c / (unsigned)ctas;
 }
-// The CTA whose share tile x is in.
+// The CTA whose share place x is in.
 EPIKV_PLAN int share_of(unsigned x, unsigned total, int ctas) {
   int c = (int)((float)x * (float)ctas / (float)total);   // near it; put right by the shares themselves
   if (c > ctas - 1) c = ctas - 1;
   while (share_start(c, total, ctas) > x) --c;
   while (share_start(c + 1, total, ctas) <= x) ++c;
   return c;
+}
+
+// A share that would start among the first or behind the last few tiles of an item starts with it or behind it: a segment of
+// so few tiles is not worth a part.
+constexpr int kFewTiles = 2;
+EPIKV_PLAN unsigned moved_start(unsigned x, unsigned at, unsigned places) {
+  if (x - at <= (unsigned)(kItemPlaces + kFewTiles)) return at;
+  return at + places - x <= (unsigned)kFewTiles ? at + places : x;
+}
+// The CTA that an item's last segment stands in.
+EPIKV_PLAN int last_share(unsigned at, unsigned places, unsigned total, int ctas) {
+  const int c = share_of(at + places - 1, total, ctas);
+  const unsigned x = share_start(c, total, ctas);
+  return x > at && moved_start(x, at, places) == at + places ? c - 1 : c;
 }
 
 // ---- what slots receive
