@@ -90,7 +90,10 @@ struct WeightPlan {
   int rows, rows_log;     // of a step
   int rep, causal, heads;
   int last;               // tokens that count, 0: all
+  int extra;              // places of a unit besides its steps: 0 or kUnitPlaces
 };
+// What a unit's keys and results cost, in steps of 128 rows (of 16 rows a unit has one step at most, and all cost the same).
+constexpr int kUnitPlaces = 4;
 
 EPIKV_PLAN int weight_slots(const WeightPlan& p, int n, int len) { return len + (p.causal ? n : 0); }
 EPIKV_PLAN int weight_units(const WeightPlan& p, int n, int len) {
@@ -108,9 +111,13 @@ EPIKV_PLAN int weight_steps(const WeightPlan& p, int n, int len, int unit) {
 }
 // ... which still has a place in the line: its zeros are stored.
 EPIKV_PLAN int weight_places(const WeightPlan& p, int n, int len, int unit) {
-  const int t = weight_steps(p, n, len, unit);
+  const int t = weight_steps(p, n, len, unit) + p.extra;
   return t > 1 ? t : 1;
 }
+// First step behind so many of a unit's places; where a share starts that would start at place x of the line, in a unit
+// whose places start at `at` (with the unit rather than before its first step).
+EPIKV_PLAN int step_of_place(const WeightPlan& p, int places) { return places > p.extra ? places - p.extra : 0; }
+EPIKV_PLAN unsigned moved_unit_start(const WeightPlan& p, unsigned x, unsigned at) { return x - at <= (unsigned)p.extra ? at : x; }
 // Units from an entry's start on that have as many places as its first.
 EPIKV_PLAN int weight_alike(const WeightPlan& p, int n, int len) {
   const int all = weight_units(p, n, len);

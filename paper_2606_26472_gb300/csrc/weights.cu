@@ -53,7 +53,7 @@ constexpr int kViews = 8;   // units that are on their way, at most: the ring of
 
 // Where a CTA's share starts, and a walk along it.
 struct WeightStart {
-  int b, unit, kh, step;
+  int b, unit, kh, place;   // places of the unit that are behind
   Entry e;
 };
 
@@ -71,7 +71,8 @@ struct alignas(16) WeightShared {
   int partly[Shape::kQueryStages][Shape::kQueryWarps];            // not every row sees all slots of the unit
   int64_t offset[2][Shape::kSlots];
   uint32_t in_view[2][Shape::kSlots / 32];                 // beside the offsets: which of them are some
-  WeightStart start;
+  WeightStart start[2];                                    // of the CTA's share, of the next one's
+  unsigned from[2];
 };
 
 struct WeightCall {
@@ -99,11 +100,11 @@ struct WeightWalk {
   const Batch& ba;
   const WeightPlan& plan;
   unsigned x, end;
-  int step, units, all, places;
+  int place, units, all, places;
   WeightSegment now;
   __device__ __forceinline__ WeightWalk(const unsigned* pre_, const Batch& ba_, const WeightPlan& plan_, const WeightStart& s,
                                         unsigned x_, unsigned end_)
-      : pre(pre_), ba(ba_), plan(plan_), x(x_), end(end_), step(s.step) {
+      : pre(pre_), ba(ba_), plan(plan_), x(x_), end(end_), place(s.place) {
     now = {};
     now.e = s.e;
     now.b = s.b;
@@ -120,7 +121,7 @@ struct WeightWalk {
   __device__ __forceinline__ void unit() {
     now.token = weight_token(plan, now.e.n, now.e.len, now.unit);
     all = weight_steps(plan, now.e.n, now.e.len, now.unit);
-    places = all > 1 ? all : 1;
+    places = max(all + plan.extra, 1);
   }
   __device__ __forceinline__ void to_next_unit() {
     if (++now.kh < plan.heads) return;
@@ -160,14 +161,14 @@ struct WeightWalk {
       now.first = now.last = true;
       return true;
     }
-    const int take = (int)min((unsigned)(places - step), end - x);
-    now.step = step;
-    now.steps = min(take, all - step);
-    now.first = step == 0;
-    now.last = step + take == places;
-    now.end = x + (places - step);
+    const int take = (int)min((unsigned)(places - place), end - x);
+    now.step = step_of_place(plan, place);
+    now.steps = min(step_of_place(plan, place + take), all) - now.step;
+    now.first = place == 0;
+    now.last = place + take == places;
+    now.end = x + (places - place);
     x += take;
-    step = 0;
+    place = 0;
     return true;
   }
 };
@@ -215,8 +216,8 @@ __device__ __forceinline__ void line_up_weights(unsigned* pre, const Batch& ba, 
   if (lane == 0) pre[0] = 0;
 }
 
-// Where in the line place x is, by one thread.
-__device__ __forceinline__ void find_place(WeightStart* s, unsigned x, const unsigned* pre, const Batch& ba,
+// Where in the line place x is, by one thread; returns where a share that starts there does.
+__device__ __forceinline__ unsigned find_place(WeightStart* s, unsigned x, const unsigned* pre, const Batch& ba,
                                            const WeightPlan& plan) {
   int lo = 0, hi = ba.n_seq - 1;   // the entry with pre[b] <= x < pre[b + 1]
   while (lo < hi) {
@@ -243,8 +244,10 @@ __device__ __forceinline__ void find_place(WeightStart* s, unsigned x, const uns
   s->b = lo;
   s->unit = unit;
   s->kh = (int)(at / places);
-  s->step = (int)(at % places);
+  const unsigned behind = at % places, from = moved_unit_start(plan, x, x - behind);
+  s->place = (int)(from - (x - behind));
   s->e = e;
+  return from;
 }
 
 // ------------------------------------------------------------------ keys
@@ -531,9 +534,18 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh,
   if constexpr (!kHalf) {
     // Steps in flight behind the newest: none where warps take turns (the stage of a warp's next step may be that of one
     // behind this one's).
-    constexpr int kLag = Shape::kTurns ? 0 : Shape::kQueryStages - 1 < 2 ? Shape::kQueryStages - 1 : 2;
-    int last = -1;
+    constexpr int kLag = Shape::kTurns ? 0 : 1;
+    int pending = 0, last = -1;
+    auto drain = [&] {
+      copy_wait<0>();
+      for (; pending > 0; --pending) deliver(last + 1 - pending);
+    };
     while (more) {
+      // before it waits for a stage the warp hands on what is on its way
+      if (step >= Shape::kQueryStages && pending &&
+          !__all_sync(0xffffffffu, mbar_try_wait(&sh.query_left[step % Shape::kQueryStages],
+                                                 (uint32_t)(step / Shape::kQueryStages - 1) & 1)))
+        drain();
       const uint32_t dst = stage(step);
 #pragma unroll
       for (int l = 0; l < kLoads; ++l) {
@@ -546,13 +558,13 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh,
       last = step;
       more = go_on();
       if (more) next = row_of();
-      if (last >= kLag) {
+      if (++pending > kLag) {
         copy_wait<kLag>();
-        deliver(last - kLag);
+        deliver(last + 1 - pending);
+        --pending;
       }
     }
-    copy_wait<0>();
-    for (int k0 = max(0, last + 1 - kLag); k0 <= last; ++k0) deliver(k0);
+    drain();
   } else {
     constexpr int kBatch = kLoads < 8 ? kLoads : 8;   // loads in flight
     uint4 v[kBatch];
@@ -751,10 +763,11 @@ __global__ void __launch_bounds__(WeightShape<D, N>::kThreads, 1)
     __syncwarp();
     const unsigned total = pre[ba.n_seq];
     const int ctas = (int)min(total, (unsigned)kAttnCtas);
-    if (lane == 0) {
-      *split = {};
-      if ((int)blockIdx.x < ctas) find_place(&sh.start, share_start(blockIdx.x, total, ctas), pre, ba, plan);
-    }
+    if (lane == 0) *split = {};
+    if (lane < 2 && (int)blockIdx.x < ctas)
+      sh.from[lane] = (int)blockIdx.x + lane < ctas
+                          ? find_place(&sh.start[lane], share_start(blockIdx.x + lane, total, ctas), pre, ba, plan)
+                          : total;
   }
   tensor_fence_before();
   __syncthreads();
@@ -764,7 +777,7 @@ __global__ void __launch_bounds__(WeightShape<D, N>::kThreads, 1)
   const int cta = blockIdx.x, ctas = (int)min(total, (unsigned)kAttnCtas);
   if (cta < ctas) {
     const TensorWaiter wait{&sh.gave_up, st.err};
-    const WeightWalk start(pre, ba, plan, sh.start, share_start(cta, total, ctas), share_start(cta + 1, total, ctas));
+    const WeightWalk start(pre, ba, plan, sh.start[0], sh.from[0], sh.from[1]);
     __shared__ alignas(16) char walks[N == 16 ? 1 : Shape::kKeyWarp][sizeof(WeightWalk)];
     WeightWalk own = start;
     WeightWalk* shared = reinterpret_cast<WeightWalk*>(walks[N == 16 ? 0 : min(warp, Shape::kKeyWarp - 1)]);
@@ -821,7 +834,7 @@ cudaError_t run_weights(const AttnState& st, const AttnDims& dm, const Batch& ba
                         const WeightCall& call, const Rows& q, const KvDev& kv, cudaStream_t stream) {
   using Shape = WeightShape<D, N>;
   static_assert(weights_smem<D, N>(kMaxSeqs) + sizeof(WeightShared<D, N>) <= 227 * 1024, "shared memory");
-  const WeightPlan plan = {Shape::kSlots, Shape::T == 1 ? 7 : 8, N, N == 16 ? 4 : 7, dm.rep, causal ? 1 : 0, dm.H, last};
+  const WeightPlan plan = {Shape::kSlots, Shape::T == 1 ? 7 : 8, N, N == 16 ? 4 : 7, dm.rep, causal ? 1 : 0, dm.H, last, N == 16 ? 0 : kUnitPlaces};
   const cudaError_t e = pdl_launch(weights_kernel<D, FMT, N>, dim3(kAttnCtas), Shape::kThreads, weights_smem<D, N>(ba.n_seq),
                                    stream, st, dm, plan, ba, call, q, kv, layer_maps(dm, call.layer, kv, 128));
   if (e != cudaSuccess || N == 16) return e;   // 16 rows are one step: no unit is split
