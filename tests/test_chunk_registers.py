@@ -111,25 +111,3 @@ for fmt in (E.EPIKV_CACHE_BF16, E.EPIKV_CACHE_E2M1):
 def test_refusals(runtime):  # noqa: F811
     """Registers that all of these calls would be refused by, had they come that far: EPIKV_ECUDA, not EPIKV_EINVAL."""
     assert run(runtime, _REFUSED, 120) == 2 * (["0"] * 4 + ["2"] * 12)
-
-
-_WEIGH = _HEAD + r"""
-def context(kinds):
-    cfg = E.make_config(max_seqs=3, max_cache_tokens=50, max_new_tokens=4, score_kinds=kinds)
-    return E.epikv_init(cfg, P, E.epikv_workspace_bytes(cfg), stream=0)
-ctx, other = context(E.EPIKV_SCORE_WEIGHT), context(63)
-before = count.value
-call = lib.epikv_weigh
-w = E.epikv_weights(P, 100, 50)
-nan, inf = float("nan"), float("inf")
-bad = [(other, 1, P, w, 2, 1.0), (None, 1, P, w, 2, 1.0), (ctx, -1, P, w, 2, 1.0), (ctx, 4, P, w, 2, 1.0), (ctx, 1, None, w, 2, 1.0),
-       (ctx, 1, P, None, 2, 1.0), (ctx, 1, P, E.epikv_weights(None, 100, 50), 2, 1.0), (ctx, 1, P, E.epikv_weights(P + 1, 100, 50), 2, 1.0),
-       (ctx, 1, P, E.epikv_weights(P, -100, 50), 2, 1.0), (ctx, 1, P, E.epikv_weights(P, 100, -50), 2, 1.0), (ctx, 1, P, w, 0, 1.0),
-       (ctx, 1, P, w, -1, 1.0), (ctx, 1, P, w, 1025, 1.0)] + [(ctx, 1, P, w, 2, d) for d in (-0.5, 1.5, nan, inf, -inf)]
-print(*[x for x in bad if call(*x, None) != E.EPIKV_EINVAL], count.value - before, call(ctx, 0, None, None, 0, 9.0, None),
-      count.value - before, call(ctx, 3, P, w, 2, 0.0, None), call(ctx, 1, P, w, 1, 1.0, None), count.value - before)
-"""
-
-
-def test_refusals_of_weigh(runtime):  # noqa: F811
-    assert run(runtime, _WEIGH, 168) == ["0", "0", "0", "0", "0", "2"]

@@ -397,3 +397,41 @@ def test_step_with_weights(gpu_lib):
     assert n == 64 and int(n_out) == 64
     np.testing.assert_array_equal(np.asarray(pos), kept)
     np.testing.assert_array_equal(np.asarray(got, np.float32), score[kept])
+
+
+def test_refusals_of_weigh(gpu_lib):
+    def context(kinds):
+        cfg = E.make_config(max_seqs=3, max_cache_tokens=50, max_new_tokens=4, score_kinds=kinds)
+        space = torch.empty(E.epikv_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+        return E.epikv_init(cfg, space, space.numel()), space
+    (ctx, _a), (other, _b) = context(E.EPIKV_SCORE_WEIGHT), context(63)
+    t = torch.zeros(3, 2, 50, device="cuda")
+    ids = torch.zeros(3, dtype=torch.int32, device="cuda")
+    w, p = E.weights_view(t), ids.data_ptr()
+    nan, inf = float("nan"), float("inf")
+    bad = [(other, 1, p, w, 2, 1.0), (None, 1, p, w, 2, 1.0), (ctx, -1, p, w, 2, 1.0), (ctx, 4, p, w, 2, 1.0), (ctx, 1, None, w, 2, 1.0),
+           (ctx, 1, p, None, 2, 1.0), (ctx, 1, p, E.epikv_weights(None, 100, 50), 2, 1.0),
+           (ctx, 1, p, E.epikv_weights(t.data_ptr() + 1, 100, 50), 2, 1.0), (ctx, 1, p, E.epikv_weights(t.data_ptr(), -100, 50), 2, 1.0),
+           (ctx, 1, p, E.epikv_weights(t.data_ptr(), 100, -50), 2, 1.0), (ctx, 1, p, w, 0, 1.0), (ctx, 1, p, w, -1, 1.0),
+           (ctx, 1, p, w, 1025, 1.0)] + [(ctx, 1, p, w, 2, d) for d in (-0.5, 1.5, nan, inf, -inf)]
+    for a in bad:
+        assert gpu_lib.epikv_weigh(*a, None) == E.EPIKV_EINVAL, a
+    assert gpu_lib.epikv_weigh(ctx, 0, None, None, 0, 9.0, None) == E.EPIKV_OK      # no sequences
+    assert gpu_lib.epikv_weigh(ctx, 1, p, w, 2, 0.0, None) == E.EPIKV_OK
+    assert E.epikv_get_error(ctx) == OK
+    for c in (ctx, other):
+        E.epikv_destroy(c)
+
+
+def test_weigh_of_sequences_that_are_none(gpu_lib):
+    """Reported, and the others' scores are as without them."""
+    cfg = E.make_config(max_seqs=2, max_cache_tokens=50, max_new_tokens=4, score_kinds=E.EPIKV_SCORE_WEIGHT)
+    space = torch.empty(E.epikv_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+    ctx = E.epikv_init(cfg, space, space.numel())
+    ids = torch.tensor([7, 1], dtype=torch.int32, device="cuda")
+    w = torch.rand(2, 1, 50, device="cuda")
+    E.epikv_score_update(ctx, 1, ids[1:].clone(), torch.tensor([0, 3], dtype=torch.int32, device="cuda"), 3, None, None)
+    E.epikv_weigh(ctx, 2, ids, E.weights_view(w))
+    assert E.epikv_get_error(ctx) == (E.EPIKV_EDEVICE, E.EPIKV_DEV_BATCH)
+    assert E.epikv_read_slots(ctx, 1, E.EPIKV_SCORE_WEIGHT, 50)[1] == w[1, 0, :3].tolist()
+    E.epikv_destroy(ctx)
