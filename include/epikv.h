@@ -504,12 +504,15 @@ epikv_status epikv_attention(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, 
 /* The same attention for many query rows: chunks of prompts, drafts, turns, of one token or more a sequence.
  * Arguments, order of the slots, what a row sees, empty rows and d_lse as in epikv_attention; nothing is split
  * between calls, so a prompt may be taken in by pieces.  It reads the cache once for 256 rows (tokens times
- * num_heads / num_kv_heads; 128 at head_dim 256) where epikv_attention does so for 8 to 32, and is the faster one
- * from about 16 new tokens a sequence on.
+ * num_heads / num_kv_heads; 128 at head_dim 256) where epikv_attention does so for 8 to 32.
  * A probability is held in 8 significant bits over a bf16 cache, in 11 (down to 2^-31 of about the row's largest)
- * over a 4-bit one; sums, maxima and d_lse in 32 bits.  In a channel where a slot that a row sees holds an infinity or a NaN the
- * row's output is infinite or NaN.  Slots that a row does not see do not reach it, whatever they hold; no memory
- * behind them is read. */
+ * over a 4-bit one; sums, maxima and d_lse in 32 bits.  In a channel where a slot that a row sees holds an infinity or
+ * a NaN the row's output is infinite or NaN.  Slots that a row does not see do not reach it, whatever they hold (memory
+ * of the view behind them may be read, up to the end of the block, or of the max_cache_tokens slots of a contiguous
+ * sequence; where stride_seq / stride_token is between 1 and max_cache_tokens - 1, only slots that are seen).
+ * Where an item of rows is cut between the SMs depends on the whole batch, and with it how a row's parts are rounded: the
+ * same batch gives the same bits, an entry of another batch may differ in its last ones.  The work is counted in 32 bits,
+ * in tiles of 128 slots (64 at head_dim 256) of an item; entries behind 2^31 - 1 are skipped (EPIKV_DEV_CAPACITY). */
 epikv_status epikv_attention_chunk(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* d_seq_ids,
                                    const int32_t* d_cu_new, int32_t max_new, const int32_t* d_len, int32_t len_stride,
                                    int32_t causal, const epikv_rows* q, const epikv_rows* out, float* d_lse,
@@ -525,7 +528,8 @@ typedef struct {
 
 /* What each slot of one layer's cache receives of the attention of the batch's queries: for KV head h,
  *   sum over the entry's new tokens and the query heads that read h of exp(scale q.k - lse)
- * over the queries that see the slot.  In 32 bits, in an order that depends on the sizes alone.
+ * over the queries that see the slot.  Sums in 32 bits, in the order of the queries, cut where the batch's sizes say:
+ * the same batch gives the same bits.
  *   d_seq_ids .. causal, q, kv   as in the attention call that gave d_lse
  *   last      only the last so many of each entry's new tokens count; 0: all of them
  *   d_lse     float [total_new][num_heads]: the attention's, or its joined parts'

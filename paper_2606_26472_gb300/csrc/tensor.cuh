@@ -153,6 +153,11 @@ __device__ __forceinline__ void named_sync(int id, int threads) {
   asm volatile("bar.sync %0, %1;" :: "r"(id), "r"(threads) : "memory");
 }
 
+__device__ __forceinline__ uint32_t lds2(uint32_t p) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(p) : "memory");
+  return v;
+}
 __device__ __forceinline__ uint4 lds16(uint32_t p) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(p) : "memory");
@@ -372,6 +377,59 @@ struct CodeRows {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         sts16(kStep % 8 == 0 ? at[k] + u * (kStep / 8) * (D * 16) : tile + tile_at<D>(r0 + u * kStep, p * 4 + k), v[k]);
+    }
+  }
+};
+
+// The same rows by way of a ring of raw codes in shared memory, kStages tiles of kRows rows: asynchronous copies keep more of
+// them under way than registers would hold.  A thread turns into halves what it has copied itself; the scales (the 16 bytes
+// that hold a row's) are copied by one lane of the row's.
+template <int D, int kThreads, int kRows, int kStages>
+struct CodeRing {
+  using Rows = CodeRows<D, kThreads, 1>;
+  static constexpr int kPer = Rows::kPer, kStep = Rows::kStep, kRounds = (kRows + kStep - 1) / kStep;
+  static_assert(kRows % (32 / kPer) == 0, "the last round's warps have whole rows");
+  static constexpr int kCodes = kRows * kPer * 16, kStage = kCodes + kRows * 16, kBytes = kStages * kStage;
+  uint32_t ring;
+  __device__ __forceinline__ uint32_t codes_at(int i, int u, int tid) const {
+    return ring + i % kStages * kStage + (u * kThreads + tid) * 16;
+  }
+  __device__ __forceinline__ uint32_t scales_at(int i, int u, int row) const {
+    return ring + i % kStages * kStage + kCodes + (u * kStep + row) * 16;
+  }
+  // Copies of tile i; codes, scales, offset as in CodeRows (rows that are not there become zeros).
+  __device__ __forceinline__ void issue(int i, const char* base, const int64_t* offset, int codes, int scales, int tid) const {
+    constexpr int kWarpRows = 32 / kPer;
+    const int own = Rows::row_of(tid), lane = tid & 31, scaled = tid / 32 * kWarpRows + lane;
+    codes += Rows::piece_of(tid) * 16;
+    scales &= ~15;
+#pragma unroll
+    for (int u = 0; u < kRounds; ++u) {
+      if (u * kStep + own < kRows) {
+        const int64_t o = offset[u * kStep + own];
+        copy_async16(codes_at(i, u, tid), base + (o < 0 ? 0 : o * 2 + codes), o < 0 ? 0 : 16);
+      }
+      if (lane < kWarpRows && u * kStep + scaled < kRows) {
+        const int64_t o = offset[u * kStep + scaled];
+        copy_async16(scales_at(i, u, scaled), base + (o < 0 ? 0 : o * 2 + scales), o < 0 ? 0 : 16);
+      }
+    }
+  }
+  // Tile i, which is there for the whole warp, as halves; scales: the head's first in the 16 bytes.
+  __device__ __forceinline__ void store(int i, uint32_t tile, int scales, int tid) const {
+    const int p = Rows::piece_of(tid), own = Rows::row_of(tid);
+    uint32_t at[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) at[k] = tile + tile_at<D>(own, p * 4 + k);
+    scales += p * 2;
+#pragma unroll
+    for (int u = 0; u < kRounds; ++u) {
+      if (u * kStep + own >= kRows) break;
+      uint4 v[4];
+      expand32(lds16(codes_at(i, u, tid)), lds2(scales_at(i, u, own) + scales), v);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        sts16(kStep % 8 == 0 ? at[k] + u * (kStep / 8) * (D * 16) : tile + tile_at<D>(own + u * kStep, p * 4 + k), v[k]);
     }
   }
 };

@@ -27,29 +27,34 @@ constexpr int kLaunchRegs = 128, kOwnerRegs = 168, kOtherRegs = 88;
 static_assert(kOwnerRegs + kOtherRegs <= 2 * kLaunchRegs, "the owners would wait for registers that nobody gives");
 
 // N query rows a step; T tiles of 128 slots a unit, each with four warps that own its slots.
-template <int D, int N>
+template <int D, int FMT, int N>
 struct WeightShape {
+  static constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
   static constexpr int T = D == 256 ? 1 : 2;
   static constexpr int kThreads = N == 16 ? 768 : 512;
   static constexpr int kQueryWarps = 4;
   static constexpr int kSlots = 128 * T;
   static constexpr int kKeys = kSlots * D * 2;         // bytes of a unit's keys
   static constexpr int kQuery = N * D * 2;             // of a step's rows
-  static constexpr int kKeyStages = N == 16 ? (D == 64 ? 5 : D == 128 ? 3 : 2) : D == 64 ? 2 : 1;
-  static constexpr int kQueryStages = N == 16 ? (D == 256 ? 4 : kKeyStages) : D == 256 ? 2 : 4;
+  static constexpr int kKeyStages = N != 16 ? (D == 64 ? 2 : 1) : kBf16 ? (D == 64 ? 5 : D == 128 ? 3 : 2) : D == 64 ? 4 : 2;
+  static constexpr int kQueryStages = N == 16 ? (D == 256 ? 4 : kBf16 ? kKeyStages : 3) : D == 256 ? 2 : 4;
   // A step's rows come by one of those warps, the steps in turn; else by all.  No more of them take turns than the ring has
   // stages: a warp then knows, by its last step's wait for a stage, that all uses of the next step's stage are over but the
   // last, and one bit tells that one's end.
   static constexpr bool kTurns = N == 16;
   static constexpr int kTurnWarps = kQueryWarps < kQueryStages ? kQueryWarps : kQueryStages;
-  static constexpr int kRing = kKeyStages * kKeys + kQueryStages * kQuery;
   static constexpr int kMmaWarp = 4 * T, kQueryWarp = kMmaWarp + 1, kKeyWarp = kQueryWarp + kQueryWarps;
   static constexpr int kKeyWarps = kThreads / 32 - kKeyWarp;
   static constexpr int kKeyThreads = kKeyWarps * 32;
+  // Units of 4-bit rows on their way.  (Beside steps of 128 rows there is no room.)
+  static constexpr int kCodeStages = kBf16 || N != 16 ? 0 : D == 64 ? 5 : D == 128 ? 3 : 2;
+  using Codes = CodeRing<D, kKeyThreads, kSlots, kCodeStages>;
+  static constexpr int kCodes = kKeyStages * kKeys + kQueryStages * kQuery, kRing = kCodes + Codes::kBytes;
   static constexpr uint32_t kColumns = 2 * N * T < 32 ? 32 : 2 * N * T;   // two tiles of scores for each tile of slots
 };
 
-constexpr int kViews = 8;   // units that are on their way, at most: the ring of keys (up to 5) and two that are read
+// Units on their way, at most: codes (up to 5), the ring of keys (up to 5), two that are read and two at the waits.
+constexpr int kViews = 16;
 
 // Where a CTA's share starts, and a walk along it.
 struct WeightStart {
@@ -57,9 +62,9 @@ struct WeightStart {
   Entry e;
 };
 
-template <int D, int N>
+template <int D, int FMT, int N>
 struct alignas(16) WeightShared {
-  using Shape = WeightShape<D, N>;
+  using Shape = WeightShape<D, FMT, N>;
   uint64_t keys[Shape::kKeyStages], keys_left[Shape::kKeyStages], query[Shape::kQueryStages], query_left[Shape::kQueryStages];
   uint64_t scores[2][2], taken[2][2], drained;
   uint32_t tmem;
@@ -253,19 +258,15 @@ __device__ __forceinline__ unsigned find_place(WeightStart* s, unsigned x, const
 // ------------------------------------------------------------------ keys
 template <int D, int FMT, int N>
 struct KeyCopier {
-  using Shape = WeightShape<D, N>;
+  using Shape = WeightShape<D, FMT, N>;
   static constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
   static constexpr int kThreads = Shape::kKeyThreads, kPer = kBf16 ? D / 8 : D / 32;   // 16-byte pieces of a head's row in the cache
   enum {
     kPieces = Shape::kSlots * kPer,
-    kStep = kThreads / (D / 32),              // 4-bit rows: rows at once, rounds of them
-    kRounds = (Shape::kSlots + kStep - 1) / kStep,
-    kAtOnce = kRounds < 6 ? kRounds : 6,
-    kAhead = kAtOnce == kRounds,              // a unit's codes are read while the last one's become halves
     kLag = Shape::kKeyStages - 1 < 3 ? Shape::kKeyStages - 1 : 3,   // units in flight behind the newest
   };
   char* ring;
-  WeightShared<D, N>& sh;
+  WeightShared<D, FMT, N>& sh;
   const TensorWaiter& wait;
   const AttnDims& dm;
   const KvDev& kv;
@@ -389,14 +390,14 @@ struct KeyCopier {
         mbar_wait_bounded(&sh.keys[k % Shape::kKeyStages], (uint32_t)(k / Shape::kKeyStages) & 1, kTensorWaitNs);
   }
 
-  // 4-bit rows: the next unit's codes are under way while one's become halves.
+  // 4-bit rows: the codes of the next units are under way while one's become halves.
   __device__ __forceinline__ void run_q4(WeightWalk walk) const {
-    int tables = 0, table = 0, unit = -1, b = -1, found = 0;
+    int tables = 0, unit = -1, b = -1, found = 0, table = 0;
     const WeightSegment& g = walk.now;
     auto ahead = [&] {   // the next segment with rows, its slots' offsets, and which of them are there
       while (walk.next<N == 16>()) {
         if (g.steps == 0) continue;
-        if (g.unit != unit || g.b != b) {
+        if (g.unit != unit || g.b != b) {   // the heads of the same slots follow one another
           unit = g.unit;
           b = g.b;
           table = tables++ & 1;
@@ -407,29 +408,37 @@ struct KeyCopier {
       }
       return false;
     };
-    using Codes = CodeRows<D, kThreads, kAtOnce>;
-    auto load = [&](Codes& c, int first) {
-      c.load(kv.base[0], sh.offset[table], g.kh * (D / 2), scale_offset(dm, g.kh), first, Shape::kSlots, tid);
-    };
-    if constexpr (kAhead) {
-      Codes now, next;
-      bool more = ahead();
-      if (more) load(next, 0);
+    if constexpr (Shape::kCodeStages > 0) {
+      constexpr int kStages = Shape::kCodeStages;
+      static_assert(kStages <= 8, "places");
+      const typename Shape::Codes raw{smem_u32(ring + Shape::kCodes)};
+      uint32_t places = 0;   // 4 bits for each unit on its way: where the head's scales stand in their 16 bytes
+      auto send = [&] {      // a group for each unit, empty behind the share's end
+        if (ahead()) {
+          const int scales = scale_offset(dm, g.kh), at = (found - 1) % 8 * 4;
+          raw.issue(found - 1, kv.base[0], sh.offset[table], g.kh * (D / 2), scales, tid);
+          places = (places & ~(15u << at)) | (scales & 15u) << at;
+        }
+        copy_commit();
+      };
 #pragma unroll 1
-      for (int i = 0; more; ++i) {
-        now = next;
-        more = ahead();
-        if (more) load(next, 0);
+      for (int k = 0; k < kStages; ++k) send();
+#pragma unroll 1
+      for (int i = 0; i < found; ++i) {
+        copy_wait<kStages - 1>();
+        __syncwarp();
         left(i);
-        now.store(stage(i), 0, Shape::kSlots, tid);
+        raw.store(i, stage(i), places >> i % 8 * 4 & 15, tid);
         deliver(i);
+        send();
       }
     } else {
+      constexpr int kStep = kThreads / (D / 32), kRounds = (Shape::kSlots + kStep - 1) / kStep, kAtOnce = kRounds < 6 ? kRounds : 6;
       for (int i = 0; ahead(); ++i) {
         left(i);
         for (int first = 0; first < Shape::kSlots; first += kAtOnce * kStep) {
-          Codes c;
-          load(c, first);
+          CodeRows<D, kThreads, kAtOnce> c;
+          c.load(kv.base[0], sh.offset[table], g.kh * (D / 2), scale_offset(dm, g.kh), first, Shape::kSlots, tid);
           c.store(stage(i), first, Shape::kSlots, tid);
         }
         deliver(i);
@@ -442,10 +451,10 @@ struct KeyCopier {
 // bf16 rows are copied as they are, those that become halves are under way while the warp's step before is stored.  (A unit of
 // a decode step takes a warp 2,900 cycles from end to end, so several take turns; of 128 rows each takes a quarter.)
 template <int D, int FMT, int N>
-__device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh, const TensorWaiter& wait, const AttnState& st,
+__device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, FMT, N>& sh, const TensorWaiter& wait, const AttnState& st,
                                              const AttnDims& dm, const WeightCall& call, const Rows& q, WeightWalk& walk,
                                              int warp, int lane) {
-  using Shape = WeightShape<D, N>;
+  using Shape = WeightShape<D, FMT, N>;
   constexpr bool kHalf = FMT != EPIKV_CACHE_BF16;
   constexpr int R = Shape::kTurns ? N : N / Shape::kQueryWarps;   // rows of the warp
   constexpr int kPer = D / 8, kRows = 32 / kPer;         // pieces of a row; rows at once
@@ -603,9 +612,9 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, N>& sh,
 
 // ------------------------------------------------------------------ products
 template <int D, int FMT, int N>
-__device__ __forceinline__ void issue_units(uint32_t ring, WeightShared<D, N>& sh, const TensorWaiter& wait, WeightWalk walk,
+__device__ __forceinline__ void issue_units(uint32_t ring, WeightShared<D, FMT, N>& sh, const TensorWaiter& wait, WeightWalk walk,
                                             uint32_t tmem) {
-  using Shape = WeightShape<D, N>;
+  using Shape = WeightShape<D, FMT, N>;
   constexpr uint32_t kScores = product_of(128, N, FMT == EPIKV_CACHE_BF16, false);
   const uint64_t k0 = rows_operand<D>(ring), q0 = rows_operand<D>(ring + Shape::kKeyStages * Shape::kKeys);
   const WeightSegment& g = walk.now;
@@ -643,10 +652,10 @@ __device__ __forceinline__ void issue_units(uint32_t ring, WeightShared<D, N>& s
 
 // ------------------------------------------------------------------ sums
 template <int D, int FMT, int N>
-__device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaiter& wait, const WeightCall& call, float* part0,
+__device__ __forceinline__ void add_up(WeightShared<D, FMT, N>& sh, const TensorWaiter& wait, const WeightCall& call, float* part0,
                                        float* part1, ChunkSplit* split, unsigned total, int ctas, WeightWalk& walk,
                                        uint32_t tmem, int t, int tid) {
-  using Shape = WeightShape<D, N>;
+  using Shape = WeightShape<D, FMT, N>;
   constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
   const WeightSegment& g = walk.now;
   int step = 0;
@@ -728,14 +737,14 @@ __device__ __forceinline__ void add_up(WeightShared<D, N>& sh, const TensorWaite
 }
 
 template <int D, int FMT, int N>
-__global__ void __launch_bounds__(WeightShape<D, N>::kThreads, 1)
+__global__ void __launch_bounds__(WeightShape<D, FMT, N>::kThreads, 1)
     weights_kernel(AttnState st, AttnDims dm, WeightPlan plan, Batch ba, WeightCall call, Rows q, KvDev kv,
                    const __grid_constant__ LayerMaps maps) {
-  using Shape = WeightShape<D, N>;
+  using Shape = WeightShape<D, FMT, N>;
   extern __shared__ char dynamic[];
   char* ring = dynamic + ((1024 - (smem_u32(dynamic) & 1023)) & 1023);
   unsigned* pre = reinterpret_cast<unsigned*>(ring + Shape::kRing);
-  __shared__ WeightShared<D, N> sh;
+  __shared__ WeightShared<D, FMT, N> sh;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (warp == Shape::kMmaWarp) tmem_alloc(&sh.tmem, Shape::kColumns);
   if (tid == 0) {
@@ -826,16 +835,16 @@ __global__ void __launch_bounds__(256) weights_join_kernel(AttnState st, Batch b
   *to = call.add ? *to + w : w;
 }
 
-template <int D, int N>
-constexpr int weights_smem(int n_seq) { return WeightShape<D, N>::kRing + 1024 + (n_seq + 1) * 4; }
+template <int D, int FMT, int N>
+constexpr int weights_smem(int n_seq) { return WeightShape<D, FMT, N>::kRing + 1024 + (n_seq + 1) * 4; }
 
 template <int D, int FMT, int N>
 cudaError_t run_weights(const AttnState& st, const AttnDims& dm, const Batch& ba, bool causal, int last,
                         const WeightCall& call, const Rows& q, const KvDev& kv, cudaStream_t stream) {
-  using Shape = WeightShape<D, N>;
-  static_assert(weights_smem<D, N>(kMaxSeqs) + sizeof(WeightShared<D, N>) <= 227 * 1024, "shared memory");
+  using Shape = WeightShape<D, FMT, N>;
+  static_assert(weights_smem<D, FMT, N>(kMaxSeqs) + sizeof(WeightShared<D, FMT, N>) <= 227 * 1024, "shared memory");
   const WeightPlan plan = {Shape::kSlots, Shape::T == 1 ? 7 : 8, N, N == 16 ? 4 : 7, dm.rep, causal ? 1 : 0, dm.H, last, N == 16 ? 0 : kUnitPlaces};
-  const cudaError_t e = pdl_launch(weights_kernel<D, FMT, N>, dim3(kAttnCtas), Shape::kThreads, weights_smem<D, N>(ba.n_seq),
+  const cudaError_t e = pdl_launch(weights_kernel<D, FMT, N>, dim3(kAttnCtas), Shape::kThreads, weights_smem<D, FMT, N>(ba.n_seq),
                                    stream, st, dm, plan, ba, call, q, kv, layer_maps(dm, call.layer, kv, 128));
   if (e != cudaSuccess || N == 16) return e;   // 16 rows are one step: no unit is split
   return pdl_launch(weights_join_kernel, dim3(kAttnCtas), Shape::kSlots, 0, stream, st, ba, call, (int)Shape::kSlots);
@@ -849,7 +858,7 @@ cudaError_t allow_weights(bool* runs) {
   if (e != cudaSuccess) return e;
   if (N != 16 && at.numRegs != kLaunchRegs) *runs = false;
   return cudaFuncSetAttribute(weights_kernel<D, FMT, N>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              weights_smem<D, N>(kMaxSeqs));
+                              weights_smem<D, FMT, N>(kMaxSeqs));
 }
 
 template <int D, int FMT>
