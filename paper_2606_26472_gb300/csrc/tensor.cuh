@@ -397,22 +397,36 @@ struct CodeRing {
   __device__ __forceinline__ uint32_t scales_at(int i, int u, int row) const {
     return ring + i % kStages * kStage + kCodes + (u * kStep + row) * 16;
   }
-  // Copies of tile i; codes, scales, offset as in CodeRows (rows that are not there become zeros).
-  __device__ __forceinline__ void issue(int i, const char* base, const int64_t* offset, int codes, int scales, int tid) const {
+  // Where the thread's pieces come from, of a head's that begin a row: the same for all heads of the same slots.
+  struct Sources {
+    const char *code[kRounds], *scale[kRounds];
+    uint32_t codes, scales;   // bit u: there is such a row, which is there
+  };
+  __device__ __forceinline__ void look(Sources* from, const char* base, const int64_t* offset, int tid) const {
     constexpr int kWarpRows = 32 / kPer;
     const int own = Rows::row_of(tid), lane = tid & 31, scaled = tid / 32 * kWarpRows + lane;
-    codes += Rows::piece_of(tid) * 16;
+    from->codes = from->scales = 0;
+#pragma unroll
+    for (int u = 0; u < kRounds; ++u) {
+      const int64_t o = u * kStep + own < kRows ? offset[u * kStep + own] : -1;
+      from->code[u] = base + (o < 0 ? 0 : o * 2 + Rows::piece_of(tid) * 16);
+      if (o >= 0) from->codes |= 1u << u;
+      const int64_t p = lane < kWarpRows && u * kStep + scaled < kRows ? offset[u * kStep + scaled] : -1;
+      from->scale[u] = base + (p < 0 ? 0 : p * 2);
+      if (p >= 0) from->scales |= 1u << u;
+    }
+  }
+  // Copies of tile i (rows that are not there become zeros); codes, scales: where the head's start in a row, bytes.
+  __device__ __forceinline__ void issue(int i, const Sources& from, int codes, int scales, int tid) const {
+    constexpr int kWarpRows = 32 / kPer;
+    const int own = Rows::row_of(tid), lane = tid & 31, scaled = tid / 32 * kWarpRows + lane;
     scales &= ~15;
 #pragma unroll
     for (int u = 0; u < kRounds; ++u) {
-      if (u * kStep + own < kRows) {
-        const int64_t o = offset[u * kStep + own];
-        copy_async16(codes_at(i, u, tid), base + (o < 0 ? 0 : o * 2 + codes), o < 0 ? 0 : 16);
-      }
-      if (lane < kWarpRows && u * kStep + scaled < kRows) {
-        const int64_t o = offset[u * kStep + scaled];
-        copy_async16(scales_at(i, u, scaled), base + (o < 0 ? 0 : o * 2 + scales), o < 0 ? 0 : 16);
-      }
+      const bool code = from.codes >> u & 1, scale = from.scales >> u & 1;
+      if (u * kStep + own < kRows) copy_async16(codes_at(i, u, tid), from.code[u] + (code ? codes : 0), code ? 16 : 0);
+      if (lane < kWarpRows && u * kStep + scaled < kRows)
+        copy_async16(scales_at(i, u, scaled), from.scale[u] + (scale ? scales : 0), scale ? 16 : 0);
     }
   }
   // Tile i, which is there for the whole warp, as halves; scales: the head's first in the 16 bytes.
@@ -422,7 +436,7 @@ struct CodeRing {
 #pragma unroll
     for (int k = 0; k < 4; ++k) at[k] = tile + tile_at<D>(own, p * 4 + k);
     scales += p * 2;
-#pragma unroll
+#pragma unroll 1   // (instructions are what these kernels are short of room for)
     for (int u = 0; u < kRounds; ++u) {
       if (u * kStep + own >= kRows) break;
       uint4 v[4];

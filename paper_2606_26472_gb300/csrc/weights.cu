@@ -73,7 +73,7 @@ struct alignas(16) WeightShared {
   alignas(16) float factor[Shape::kQueryStages][N];        // of a row's scores (4-bit rows; else the same for all)
   alignas(16) float lse2[Shape::kQueryStages][N];          // minus log2 of a row's sum
   alignas(16) int seen[Shape::kQueryStages][N];            // slots that the row sees
-  int partly[Shape::kQueryStages][Shape::kQueryWarps];            // not every row sees all slots of the unit
+  int partly[Shape::kQueryStages][Shape::kQueryWarps];     // steps of 128 rows: not every row sees all slots of the unit
   int64_t offset[2][Shape::kSlots];
   uint32_t in_view[2][Shape::kSlots / 32];                 // beside the offsets: which of them are some
   WeightStart start[2];                                    // of the CTA's share, of the next one's
@@ -394,10 +394,12 @@ struct KeyCopier {
   __device__ __forceinline__ void run_q4(WeightWalk walk) const {
     int tables = 0, unit = -1, b = -1, found = 0, table = 0;
     const WeightSegment& g = walk.now;
+    bool moved = false;  // to other slots
     auto ahead = [&] {   // the next segment with rows, its slots' offsets, and which of them are there
       while (walk.next<N == 16>()) {
         if (g.steps == 0) continue;
-        if (g.unit != unit || g.b != b) {   // the heads of the same slots follow one another
+        moved = g.unit != unit || g.b != b;   // the heads of the same slots follow one another
+        if (moved) {
           unit = g.unit;
           b = g.b;
           table = tables++ & 1;
@@ -412,11 +414,13 @@ struct KeyCopier {
       constexpr int kStages = Shape::kCodeStages;
       static_assert(kStages <= 8, "places");
       const typename Shape::Codes raw{smem_u32(ring + Shape::kCodes)};
+      typename Shape::Codes::Sources from;
       uint32_t places = 0;   // 4 bits for each unit on its way: where the head's scales stand in their 16 bytes
       auto send = [&] {      // a group for each unit, empty behind the share's end
         if (ahead()) {
           const int scales = scale_offset(dm, g.kh), at = (found - 1) % 8 * 4;
-          raw.issue(found - 1, kv.base[0], sh.offset[table], g.kh * (D / 2), scales, tid);
+          if (moved) raw.look(&from, kv.base[0], sh.offset[table], tid);
+          raw.issue(found - 1, from, g.kh * (D / 2), scales, tid);
           places = (places & ~(15u << at)) | (scales & 15u) << at;
         }
         copy_commit();
@@ -510,9 +514,11 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, FMT, N>
       if constexpr (kHalf) sh.factor[qs][own] = call.c * head_scale(st, dm, 0, call.layer, g.kh) * back;
       sh.seen[qs][own] = r.lse == -INFINITY ? 0 : r.seen;   // (the row saw nothing)
     }
-    const int upto = min(g.unit * Shape::kSlots + Shape::kSlots, g.slots);
-    const bool partly = __any_sync(0xffffffffu, lane < R && (r.lse == -INFINITY || r.seen < upto));
-    if (lane == 0) sh.partly[qs][Shape::kTurns ? 0 : warp] = partly;
+    if constexpr (N != 16) {
+      const int upto = min(g.unit * Shape::kSlots + Shape::kSlots, g.slots);
+      const bool partly = __any_sync(0xffffffffu, lane < R && (r.lse == -INFINITY || r.seen < upto));
+      if (lane == 0) sh.partly[qs][warp] = partly;
+    }
   };
   auto deliver = [&](int step) {
     fence_proxy_async_smem();
@@ -524,6 +530,8 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, FMT, N>
     if (step >= Shape::kQueryStages) wait(&sh.query_left[qs], (uint32_t)(step / Shape::kQueryStages - 1) & 1);
     return smem_u32(ring + Shape::kKeyStages * Shape::kKeys + qs * Shape::kQuery);
   };
+  // Of a step of 16 rows only those that are some: what stands in the others' columns is not looked at.
+  auto loads_of = [&] { return N == 16 ? (min(N, (g.e.n - g.token) * rep) + kRows - 1) / kRows : kLoads; };
   int step = -1;
   auto go_on = [&] {   // to the warp's next step
     if constexpr (Shape::kTurns) {
@@ -556,8 +564,10 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, FMT, N>
                                                  (uint32_t)(step / Shape::kQueryStages - 1) & 1)))
         drain();
       const uint32_t dst = stage(step);
+      const int loads = loads_of();
 #pragma unroll
       for (int l = 0; l < kLoads; ++l) {
+        if (l >= loads) break;
         const int row = l * kRows + sub;
         const uint4* from = source(next, row);
         if (row < R) copy_async16(dst + tile_at<D>(row0 + row, piece), from, 16);
@@ -575,7 +585,7 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, FMT, N>
     }
     drain();
   } else {
-    constexpr int kBatch = kLoads < 8 ? kLoads : 8;   // loads in flight
+    constexpr int kMost = N == 16 ? 4 : 8, kBatch = kLoads < kMost ? kLoads : kMost;   // loads in flight
     uint4 v[kBatch];
     auto load = [&](const Row& r, int l0) {
 #pragma unroll
@@ -584,10 +594,11 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, FMT, N>
     if (more) load(next, 0);
     while (more) {
       const Row now = next;
+      const int loads = loads_of();
       const uint32_t dst = stage(step);
       float back = 1.f;
-#pragma unroll
-      for (int l0 = 0; l0 < kLoads; l0 += kBatch) {
+#pragma unroll 1
+      for (int l0 = 0; l0 < loads; l0 += kBatch) {
         if (l0) load(now, l0);
         float undo[kBatch];   // of the row that the lane's piece is of
         halves_of<kPer, kBatch>(v, undo);
@@ -670,7 +681,7 @@ __device__ __forceinline__ void add_up(WeightShared<D, FMT, N>& sh, const Tensor
       if (mine && !call.add) *to = 0.f;
       continue;
     }
-    const int ks = i % Shape::kKeyStages;
+    const int ks = i % Shape::kKeyStages, rows = (g.e.n - g.token) * walk.plan.rep;   // (16 rows are one step)
     f32x2 sum[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) sum[j] = f2_pack(0.f, 0.f);
@@ -681,8 +692,10 @@ __device__ __forceinline__ void add_up(WeightShared<D, FMT, N>& sh, const Tensor
       const float4* lse2 = reinterpret_cast<const float4*>(sh.lse2[qs]);
       const float4* factor = reinterpret_cast<const float4*>(sh.factor[qs]);
       bool partly = false;
+      if constexpr (N != 16) {
 #pragma unroll
-      for (int w = 0; w < (Shape::kTurns ? 1 : Shape::kQueryWarps); ++w) partly |= sh.partly[qs][w] != 0;
+        for (int w = 0; w < Shape::kQueryWarps; ++w) partly |= sh.partly[qs][w] != 0;
+      }
       uint32_t x[N];   // all columns at once: their exponentials follow one another without a pause
       const uint32_t from = tmem + (2 * t + buf) * N;
       if constexpr (N == 16) {
@@ -697,6 +710,7 @@ __device__ __forceinline__ void add_up(WeightShared<D, FMT, N>& sh, const Tensor
       auto columns = [&](auto masked) {
 #pragma unroll
         for (int j = 0; j < N; j += 4) {
+          if (N == 16 && j >= rows) break;
           const float4 l = lse2[j / 4];
           const float4 f = kBf16 ? make_float4(call.c, call.c, call.c, call.c) : factor[j / 4];
           const f32x2 a = f2_fma(f2_pack(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), f2_pack(f.x, f.y), f2_pack(l.x, l.y));
@@ -713,7 +727,7 @@ __device__ __forceinline__ void add_up(WeightShared<D, FMT, N>& sh, const Tensor
           sum[(j / 2 & 2) + 1] = f2_add(sum[(j / 2 & 2) + 1], f2_pack(p[2], p[3]));
         }
       };
-      if (partly) columns(std::true_type{});
+      if (N == 16 || partly) columns(std::true_type{});
       else columns(std::false_type{});
       __syncwarp();
       if (lane == 0) mbar_arrive_one(&sh.query_left[qs]);
