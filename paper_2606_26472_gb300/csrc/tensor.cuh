@@ -436,7 +436,7 @@ struct CodeRing {
 #pragma unroll
     for (int k = 0; k < 4; ++k) at[k] = tile + tile_at<D>(own, p * 4 + k);
     scales += p * 2;
-#pragma unroll 1   // (instructions are what these kernels are short of room for)
+#pragma unroll
     for (int u = 0; u < kRounds; ++u) {
       if (u * kStep + own >= kRows) break;
       uint4 v[4];

@@ -12,6 +12,7 @@
 // chunk: exponentials and products).  One CTA an SM takes an equal share of all
 // units' steps (chunk_plan.h); the few units that two shares meet in are joined
 // by a second kernel, part by part.
+#include <algorithm>
 #include <new>
 
 #include "chunk_plan.h"
@@ -935,8 +936,8 @@ cudaError_t launch_attention_weights(const AttnState& st, const AttnDims& dm, in
 
 cudaError_t launch_weigh(const DevState& st, const Dims& dm, int n_seq, const int32_t* seq_ids, const float* w,
                          int64_t stride_seq, int64_t stride_head, int heads, float decay, cudaStream_t stream) {
-  const int blocks = (dm.T + 255) / 256;
-  return pdl_launch(weigh_kernel, dim3(blocks < 64 ? blocks : 64, n_seq), 256, 0, stream, st, dm, seq_ids, w, stride_seq,
+  const int blocks = (dm.T + 255) / 256, most = kAttnCtas * 8 / n_seq;   // 8 fit an SM
+  return pdl_launch(weigh_kernel, dim3(std::max(1, std::min(blocks, most)), n_seq), 256, 0, stream, st, dm, seq_ids, w, stride_seq,
                     stride_head, heads, decay);
 }
 
