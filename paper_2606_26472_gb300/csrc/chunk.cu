@@ -623,14 +623,14 @@ __device__ __forceinline__ void soften(ChunkShared<D>& sh, const TensorWaiter& w
     if constexpr (kHeld) {
 #pragma unroll
       for (int i = 0; i < kParts; ++i) load(i);
-      tmem_wait_load();
+      tmem_wait_load<32 * kParts>(x[0]);
 #pragma unroll
       for (int i = 0; i < kParts; ++i) highest(i);
     } else {
 #pragma unroll 1
       for (int i = 0; i < kParts; ++i) {
         load(i);
-        tmem_wait_load();
+        tmem_wait_load<32>(x[0]);
         highest(i);
       }
     }
@@ -649,7 +649,7 @@ __device__ __forceinline__ void soften(ChunkShared<D>& sh, const TensorWaiter& w
         for (int i = 0; i < D; i += 16) {
           uint32_t y[16];
           tmem_load16(o + i, y);
-          tmem_wait_load();
+          tmem_wait_load<16>(y);
 #pragma unroll
           for (int u = 0; u < 16; ++u) y[u] = __float_as_uint(__uint_as_float(y[u]) * mul);
           tmem_store16(o + i, y);
@@ -684,7 +684,7 @@ __device__ __forceinline__ void soften(ChunkShared<D>& sh, const TensorWaiter& w
 #pragma unroll 1
       for (int i = 0; i < kParts; ++i) {
         load(i);
-        tmem_wait_load();
+        tmem_wait_load<32>(x[0]);
         mask(i);
         soft(i);
       }
@@ -736,7 +736,7 @@ __device__ __forceinline__ void put_rows(const AttnState& st, const AttnDims& dm
     uint32_t y[32];
     if (g.t0 < g.t1) {
       tmem_load32(o + i, y);
-      tmem_wait_load();
+      tmem_wait_load<32>(y);
     }
 #pragma unroll
     for (int u = 0; u < 32; ++u) y[u] = none ? 0u : __float_as_uint(__uint_as_float(y[u]) * mul);

@@ -705,7 +705,7 @@ __device__ __forceinline__ void add_up(WeightShared<D, FMT, N>& sh, const Tensor
 #pragma unroll
         for (int j = 0; j < N; j += 32) tmem_load32(from + j, x + j);
       }
-      tmem_wait_load();
+      tmem_wait_load<N>(x);
       tensor_fence_before();
       mbar_arrive_one(&sh.taken[t][buf]);
       auto columns = [&](auto masked) {
