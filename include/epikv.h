@@ -503,7 +503,7 @@ epikv_status epikv_attention(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, 
 
 /* The same attention for many query rows: chunks of prompts, drafts, turns, of one token or more a sequence.
  * Arguments, order of the slots, what a row sees, empty rows and d_lse as in epikv_attention; nothing is split
- * between calls, so a prompt may be taken in by pieces.  It reads the cache once for 256 rows (tokens times
+ * between calls, so a prompt may be taken in by pieces.  out may not overlap q.  It reads the cache once for 256 rows (tokens times
  * num_heads / num_kv_heads; 128 at head_dim 256) where epikv_attention does so for 8 to 32.
  * A probability is held in 8 significant bits over a bf16 cache, in 11 (down to 2^-31 of about the row's largest)
  * over a 4-bit one; sums, maxima and d_lse in 32 bits.  In a channel where a slot that a row sees holds an infinity or

@@ -214,6 +214,12 @@ __device__ __forceinline__ uint32_t half_pair_times(uint32_t a, uint32_t b, bool
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 
+__device__ __forceinline__ uint32_t bf16_pair_times(uint32_t a, uint32_t b, bool high) {
+  const __nv_bfloat162 s = *reinterpret_cast<const __nv_bfloat162*>(&b);
+  const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), high ? __high2bfloat162(s) : __low2bfloat162(s));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -267,16 +273,27 @@ inline LayerMaps layer_maps(const AttnDims& dm, int layer, const KvDev& kv, int 
 
 // ------------------------------------------------------------ rows of a tile
 // 32 channels of a 4-bit row (16 bytes of codes, two scales) as 64 bytes of halves, exact: 2 + 4 significant bits between
-// 2^-10 and 2688.
+// 2^-10 and 2688.  kWide: as bf16, exact too.  A code's half, moved by the three bits that bf16 has fewer of, is the bf16 of
+// 2^-112 times the value; the scale makes good for it.
+template <bool kWide>
 __device__ __forceinline__ void expand32(const uint4& codes, uint32_t scales, uint4 (&out)[4]) {
-  const uint32_t s = e4m3x2_to_half2((uint16_t)scales);
+  uint32_t s = e4m3x2_to_half2((uint16_t)scales);
+  if constexpr (kWide) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&s));
+    const float up = __uint_as_float(0x77800000u);   // 2^112
+    s = bf16_pair(f.x * up, f.y * up);
+  }
   const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     uint32_t h[4];
     e2m1x8_to_half2(w[i], h);
-    out[i] = make_uint4(half_pair_times(h[0], s, i >= 2), half_pair_times(h[1], s, i >= 2),
-                        half_pair_times(h[2], s, i >= 2), half_pair_times(h[3], s, i >= 2));
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if constexpr (kWide) h[u] = bf16_pair_times((h[u] >> 3 & 0x0fff0fffu) | (h[u] & 0x80008000u), s, i >= 2);
+      else h[u] = half_pair_times(h[u], s, i >= 2);
+    }
+    out[i] = make_uint4(h[0], h[1], h[2], h[3]);
   }
 }
 
@@ -338,10 +355,10 @@ __device__ __forceinline__ float store_queries(uint32_t tile, int row0, const vo
   return back;
 }
 
-// Pieces of 4-bit rows that each of kThreads threads turns into halves: 32 channels of every kStep-th row from row `first` on,
+// Pieces of 4-bit rows that each of kThreads threads turns into halves (kWide: bf16): 32 channels of every kStep-th row from row `first` on,
 // R rows at a time.  Eight neighbouring lanes have two pieces of four rows, whose parts fall on all eight places of a
 // swizzled block's 128 bytes.
-template <int D, int kThreads, int R>
+template <int D, int kThreads, int R, bool kWide = false>
 struct CodeRows {
   static constexpr int kPer = D / 32, kStep = kThreads / kPer;
   static_assert(kThreads % 32 == 0 && kPer <= 8, "a warp has whole rows");
@@ -379,7 +396,7 @@ struct CodeRows {
     for (int u = 0; u < R; ++u) {
       if (r0 + u * kStep >= rows) break;
       uint4 v[4];
-      expand32(code[u], in >> u & 1 ? scale[u] : 0u, v);
+      expand32<kWide>(code[u], in >> u & 1 ? scale[u] : 0u, v);
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         sts16(kStep % 8 == 0 ? at[k] + u * (kStep / 8) * (D * 16) : tile + tile_at<D>(r0 + u * kStep, p * 4 + k), v[k]);
@@ -446,7 +463,7 @@ struct CodeRing {
     for (int u = 0; u < kRounds; ++u) {
       if (u * kStep + own >= kRows) break;
       uint4 v[4];
-      expand32(lds16(codes_at(i, u, tid)), lds2(scales_at(i, u, own) + scales), v);
+      expand32<false>(lds16(codes_at(i, u, tid)), lds2(scales_at(i, u, own) + scales), v);
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         sts16(kStep % 8 == 0 ? at[k] + u * (kStep / 8) * (D * 16) : tile + tile_at<D>(own + u * kStep, p * 4 + k), v[k]);

@@ -38,6 +38,9 @@ static_assert(kOwnerRegs + kOtherRegs <= 2 * kLaunchRegs, "the owners would wait
 template <int D, int FMT, int N>
 struct WeightShape {
   static constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
+  // What 4-bit keys become: halves beside steps of 16 rows, which become halves too (that many are soon done); bf16, which takes
+  // two instructions more a pair, where each step's 128 rows would have to (a prompt of 4,096: 89 us, 208 by halves).
+  static constexpr bool kHalf = !kBf16 && N == 16;
   static constexpr int T = D == 256 ? 1 : 2;
   static constexpr int kThreads = N == 16 ? 768 : 512;
   static constexpr int kQueryWarps = 4;
@@ -78,7 +81,7 @@ struct alignas(16) WeightShared {
   uint32_t tmem;
   int gave_up;
   uint32_t there[kViews][Shape::kSlots / 32];              // the slot is in the view; units in turn
-  alignas(16) float factor[Shape::kQueryStages][N];        // of a row's scores (4-bit rows; else the same for all)
+  alignas(16) float factor[Shape::kQueryStages][N];        // of a row's scores (halves; else the same for all)
   alignas(16) float lse2[Shape::kQueryStages][N];          // minus log2 of a row's sum
   alignas(16) int seen[Shape::kQueryStages][N];            // slots that the row sees
   int partly[Shape::kQueryStages][Shape::kQueryWarps];     // steps of 128 rows: not every row sees all slots of the unit
@@ -449,7 +452,7 @@ struct KeyCopier {
       for (int i = 0; ahead(); ++i) {
         left(i);
         for (int first = 0; first < Shape::kSlots; first += kAtOnce * kStep) {
-          CodeRows<D, kThreads, kAtOnce> c;
+          CodeRows<D, kThreads, kAtOnce, true> c;
           c.load(kv.base[0], sh.offset[table], g.kh * (D / 2), scale_offset(dm, g.kh), first, Shape::kSlots, tid);
           c.store(stage(i), first, Shape::kSlots, tid);
         }
@@ -467,7 +470,7 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, FMT, N>
                                              const AttnDims& dm, const WeightCall& call, const Rows& q, WeightWalk& walk,
                                              int warp, int lane) {
   using Shape = WeightShape<D, FMT, N>;
-  constexpr bool kHalf = FMT != EPIKV_CACHE_BF16;
+  constexpr bool kHalf = Shape::kHalf;
   constexpr int R = Shape::kTurns ? N : N / Shape::kQueryWarps;   // rows of the warp
   constexpr int kPer = D / 8, kRows = 32 / kPer;         // pieces of a row; rows at once
   constexpr int kLoads = (R + kRows - 1) / kRows;
@@ -634,7 +637,7 @@ template <int D, int FMT, int N>
 __device__ __forceinline__ void issue_units(uint32_t ring, WeightShared<D, FMT, N>& sh, const TensorWaiter& wait, WeightWalk walk,
                                             uint32_t tmem) {
   using Shape = WeightShape<D, FMT, N>;
-  constexpr uint32_t kScores = product_of(128, N, FMT == EPIKV_CACHE_BF16, false);
+  constexpr uint32_t kScores = product_of(128, N, !Shape::kHalf, false);
   const uint64_t k0 = rows_operand<D>(ring), q0 = rows_operand<D>(ring + Shape::kKeyStages * Shape::kKeys);
   const WeightSegment& g = walk.now;
   int step = 0;
@@ -671,11 +674,11 @@ __device__ __forceinline__ void issue_units(uint32_t ring, WeightShared<D, FMT, 
 
 // ------------------------------------------------------------------ sums
 template <int D, int FMT, int N>
-__device__ __forceinline__ void add_up(WeightShared<D, FMT, N>& sh, const TensorWaiter& wait, const WeightCall& call, float* part0,
+__device__ __forceinline__ void add_up(WeightShared<D, FMT, N>& sh, const TensorWaiter& wait, const AttnState& st,
+                                       const AttnDims& dm, const WeightCall& call, float* part0,
                                        float* part1, ChunkSplit* split, unsigned total, int ctas, WeightWalk& walk,
                                        uint32_t tmem, int t, int tid) {
   using Shape = WeightShape<D, FMT, N>;
-  constexpr bool kBf16 = FMT == EPIKV_CACHE_BF16;
   const WeightSegment& g = walk.now;
   int step = 0;
   const int lane = tid & 31, own = t * 128 + tid;
@@ -690,6 +693,7 @@ __device__ __forceinline__ void add_up(WeightShared<D, FMT, N>& sh, const Tensor
       continue;
     }
     const int ks = i % Shape::kKeyStages, rows = (g.e.n - g.token) * walk.plan.rep;   // (16 rows are one step)
+    const float c = FMT == EPIKV_CACHE_BF16 ? call.c : call.c * head_scale(st, dm, 0, call.layer, g.kh);
     f32x2 sum[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) sum[j] = f2_pack(0.f, 0.f);
@@ -720,7 +724,7 @@ __device__ __forceinline__ void add_up(WeightShared<D, FMT, N>& sh, const Tensor
         for (int j = 0; j < N; j += 4) {
           if (N == 16 && j >= rows) break;
           const float4 l = lse2[j / 4];
-          const float4 f = kBf16 ? make_float4(call.c, call.c, call.c, call.c) : factor[j / 4];
+          const float4 f = Shape::kHalf ? factor[j / 4] : make_float4(c, c, c, c);
           const f32x2 a = f2_fma(f2_pack(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), f2_pack(f.x, f.y), f2_pack(l.x, l.y));
           const f32x2 b = f2_fma(f2_pack(__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])), f2_pack(f.z, f.w), f2_pack(l.z, l.w));
           float p[4] = {exp2_fast(f2_lo(a)), exp2_fast(f2_hi(a)), exp2_fast(f2_lo(b)), exp2_fast(f2_hi(b))};
@@ -818,7 +822,7 @@ __global__ void __launch_bounds__(WeightShape<D, FMT, N>::kThreads, 1)
     if (warp < Shape::kMmaWarp) {
       if constexpr (N != 16) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kOwnerRegs));
       float* part = st.part + (int64_t)cta * 2 * Shape::kSlots;
-      add_up<D, FMT, N>(sh, wait, call, part, part + Shape::kSlots, split, total, ctas, walk,
+      add_up<D, FMT, N>(sh, wait, st, dm, call, part, part + Shape::kSlots, split, total, ctas, walk,
                         tmem + ((uint32_t)(warp & 3) << 21), warp >> 2, tid & 127);
     } else {
       if constexpr (N != 16) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kOtherRegs));
