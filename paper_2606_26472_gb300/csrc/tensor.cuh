@@ -340,7 +340,7 @@ __device__ __forceinline__ float store_queries(uint32_t tile, int row0, const vo
     uint4 v[kAtOnce];
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i)
-      v[i] = __ldg(reinterpret_cast<const uint4*>(__shfl_sync(0xffffffffu, mine, (r0 + i) * kRows + sub)) + piece);
+      v[i] = load_now(reinterpret_cast<const uint4*>(__shfl_sync(0xffffffffu, mine, (r0 + i) * kRows + sub)) + piece);
     float undo[kAtOnce];   // of the row that the lane's piece is of
     if constexpr (kHalf) halves_of<kPer, kAtOnce>(v, undo);
 #pragma unroll
