@@ -36,11 +36,11 @@ constexpr float kSlack = 8.f;           // a maximum is moved when a score passe
 // registers: launched with the same number each, the owners of rows take more from the others.
 constexpr int chunk_threads(int fmt) { return fmt == EPIKV_CACHE_BF16 ? 384 : 512; }
 constexpr int launch_regs(int fmt) { return 65536 / chunk_threads(fmt) & ~7; }
-constexpr int other_regs(int fmt) { return fmt == EPIKV_CACHE_BF16 ? 104 : 88; }
-constexpr int owner_regs(int fmt, int tiles) { return tiles == 1 ? 232 : fmt == EPIKV_CACHE_BF16 ? 200 : 168; }
+constexpr int kOtherRegs = 88;
+constexpr int owner_regs(int fmt, int tiles) { return tiles == 1 ? 232 : fmt == EPIKV_CACHE_BF16 ? 208 : 168; }
 constexpr bool enough_regs(int fmt, int tiles) {
   const int groups = chunk_threads(fmt) / 128;
-  return tiles * owner_regs(fmt, tiles) + (groups - tiles) * other_regs(fmt) <= groups * launch_regs(fmt);
+  return tiles * owner_regs(fmt, tiles) + (groups - tiles) * kOtherRegs <= groups * launch_regs(fmt);
 }
 static_assert(enough_regs(EPIKV_CACHE_BF16, 1) && enough_regs(EPIKV_CACHE_BF16, 2) && enough_regs(EPIKV_CACHE_E2M1, 1) &&
               enough_regs(EPIKV_CACHE_E2M1, 2), "the owners would wait for registers that nobody gives");
@@ -910,7 +910,7 @@ __global__ void __launch_bounds__(chunk_threads(FMT), 1)
           sh.split = {1, now.b, now.kh, now.row0, now.rows, last_share(now.at, now.places, total, ctas) - cta + 1, {0, 0}};
       }
     } else {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(other_regs(FMT)));
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kOtherRegs));
       if (warp == 8) {
         issue_products<D, FMT, kTiles>(smem_u32(smem), smem_u32(ring), sh, wait, walk, tmem);
         if (elected()) products_done(&sh.drained);   // tensor memory is not freed under products, whatever waits gave up

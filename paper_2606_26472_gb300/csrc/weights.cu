@@ -31,7 +31,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 // Steps of 128 rows: the 8 warps that own slots hold 128 scores each, and take registers from the 8 others.
-constexpr int kLaunchRegs = 128, kOwnerRegs = 168, kOtherRegs = 88;
+constexpr int kLaunchRegs = 128, kOwnerRegs = 184, kOtherRegs = 72;
 static_assert(kOwnerRegs + kOtherRegs <= 2 * kLaunchRegs, "the owners would wait for registers that nobody gives");
 
 // N query rows a step; T tiles of 128 slots a unit, each with four warps that own its slots.
