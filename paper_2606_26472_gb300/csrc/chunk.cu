@@ -160,11 +160,12 @@ struct alignas(16) ChunkShared {
   unsigned from, to;                        // the CTA's share
   WarpWalk walk[16];
   ChunkSplit split;
+  Entry entries[32];                        // the batch's first
 };
 
 // Places before each entry of the batch, by a warp; returns the items.  An entry that cannot be taken has none, nor has one
 // that takes the sum to kTooManyTiles and those behind it.
-__device__ __forceinline__ int64_t line_up(unsigned* pre, const Batch& ba, const AttnDims& dm, const ChunkPlan& plan,
+__device__ __forceinline__ int64_t line_up(unsigned* pre, Entry* entries, const Batch& ba, const AttnDims& dm, const ChunkPlan& plan,
                                            int32_t* err, int lane) {
   unsigned before = 0;
   int64_t items = 0;
@@ -174,6 +175,7 @@ __device__ __forceinline__ int64_t line_up(unsigned* pre, const Batch& ba, const
     unsigned n = 0;
     int64_t it = 0;
     const bool taken = b < ba.n_seq && batch_entry(ba, dm, b, plan.causal, err, &e);
+    if (b0 == 0 && taken) entries[lane] = e;
     const int blocks = taken ? chunk_blocks(plan, e.n) : 0;
     int64_t tiles = 0;
     if (__all_sync(0xffffffffu, blocks <= 8)) {
@@ -221,15 +223,15 @@ __device__ __forceinline__ int64_t line_up(unsigned* pre, const Batch& ba, const
 }
 
 // Where in the line place x is, by a warp; returns where a share that starts there does.
-__device__ __forceinline__ unsigned find_place(ShareStart* start, unsigned x, const unsigned* pre, const Batch& ba, const ChunkPlan& plan,
-                                          int lane) {
+__device__ __forceinline__ unsigned find_place(ShareStart* start, unsigned x, const unsigned* pre, const Entry* entries,
+                                               const Batch& ba, const ChunkPlan& plan, int lane) {
   int lo = 0, hi = ba.n_seq - 1;   // the entry with pre[b] <= x < pre[b + 1]
   while (lo < hi) {
     const int mid = (lo + hi) / 2;
     if (x < pre[mid + 1]) hi = mid;
     else lo = mid + 1;
   }
-  const Entry e = entry_of(ba, lo);
+  const Entry e = lo < 32 ? entries[lo] : entry_of(ba, lo);
   const int n = e.n, len = e.len;
   const unsigned of_head = (pre[lo + 1] - pre[lo]) / (unsigned)plan.heads, kh = (x - pre[lo]) / of_head;
   unsigned at = pre[lo] + kh * of_head;
@@ -840,16 +842,16 @@ __global__ void __launch_bounds__(chunk_threads(FMT), 1)
   pdl_trigger();
   __shared__ int64_t items;
   if (warp == 0) {
-    const int64_t n = line_up(pre, ba, dm, plan, st.err, lane);
+    const int64_t n = line_up(pre, sh.entries, ba, dm, plan, st.err, lane);
     if (lane == 0) items = n;
     __syncwarp();
     const unsigned total = pre[ba.n_seq];
     const int ctas = chunk_ctas(total, n), cta = blockIdx.x;
     if (cta < ctas) {
       unsigned to = total;
-      if (cta + 1 < ctas) to = find_place(&sh.start, share_start(cta + 1, total, ctas), pre, ba, plan, lane);
-      unsigned from = find_place(&sh.start, share_start(cta, total, ctas), pre, ba, plan, lane);
-      if (from < to) from = find_place(&sh.start, from, pre, ba, plan, lane);   // (the item behind, or the same)
+      if (cta + 1 < ctas) to = find_place(&sh.start, share_start(cta + 1, total, ctas), pre, sh.entries, ba, plan, lane);
+      unsigned from = find_place(&sh.start, share_start(cta, total, ctas), pre, sh.entries, ba, plan, lane);
+      if (from < to) from = find_place(&sh.start, from, pre, sh.entries, ba, plan, lane);   // (the item behind, or the same)
       if (lane == 0) {
         sh.from = from;
         sh.to = to;

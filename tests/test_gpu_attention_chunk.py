@@ -229,6 +229,21 @@ def test_repeated_calls_agree(gpu_lib, bits):
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
+@pytest.mark.parametrize("bits", [16, 4])
+def test_many_sequences(gpu_lib, bits):
+    """More of them than a warp has lanes, most with little or nothing to do."""
+    S = 200
+    c = R.Cache(seqs=S, T=330, H=2, d=64, bits=bits, seed=19)
+    ctx = c.context(6, 90)
+    new = [(0, 1, 3, 90, 0, 7, 2)[b % 7] for b in range(S)]
+    held = [(b * 37) % 240 if b % 5 else 0 for b in range(S)]
+    seqs = [(b * 73 + 11) % S for b in range(S)]
+    q = queries(sum(new), 6, 64)
+    o, l = attend(c, ctx, q, new, held, seqs=seqs)
+    check_attention(c, q, o, l, new, held, seqs=seqs)
+    assert E.epikv_attn_get_error(ctx) == OK
+
+
 def test_offsets_past_32_bits(gpu_lib):
     """A contiguous cache of more than 2^32 bytes, its last sequence's slots far behind that."""
     S, T, H, d = 5, 262144, 8, 128

@@ -226,6 +226,73 @@ def test_reported_and_skipped(gpu_lib):
     assert torch.equal(w[0][:, keep], good[0][:, keep])
 
 
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("new,H,Hq,d", [(1, 2, 8, 64), (1, 3, 12, 128), (4, 2, 8, 256), (40, 2, 8, 128), (40, 1, 4, 64)])
+def test_blocks_that_are_none(gpu_lib, bits, new, H, Hq, d):
+    """Slots of blocks that the pool does not have receive nothing, all others what they did."""
+    c = R.Cache(seqs=2, T=1600, H=H, d=d, bits=bits, seed=16)
+    ctx = c.context(Hq, 40)
+    held = [1500, 1201]
+    q = queries(2 * new, Hq, d)
+    lse = lse64(c, q, [new, new], held)
+    good, w = fresh(c), fresh(c)
+    weigh(c, ctx, q, lse, [new, new], held, good)
+    table = c.c.block_table.clone()
+    gone = torch.zeros(2, 1600 + 16, dtype=torch.bool, device="cuda")
+    for s, blocks in ((0, (0, 16, 31, 40)), (1, (7, 60, 75))):
+        for b, bad in zip(blocks, (c.c.num_blocks, -1, 1 << 30, -(1 << 31))):
+            table[s, b] = bad
+            gone[s, 16 * b:16 * b + 16] = True
+    seq_ids, cu, ln = R.batch([new, new], held)
+    E.epikv_attention_weights(ctx, 0, 2, seq_ids, cu, new, ln, E.rows(q), lse, E.weights_view(w), c.c.view(table))
+    assert E.epikv_attn_get_error(ctx) == (E.EPIKV_EDEVICE, E.EPIKV_DEV_SLOT)
+    for s in range(2):
+        top = held[s] + new
+        here = gone[s, :top]
+        assert not w[s, :, :top][:, here].any()
+        assert torch.equal(w[s, :, :top][:, ~here], good[s, :, :top][:, ~here])
+        assert bool((w[s, :, top:] == -7.5).all())
+
+
+def test_two_contexts_at_once(gpu_lib):
+    """Calls of two contexts on two streams, a captured one and an eager one: the bits of each alone."""
+    calls = []
+    for bits, new, seed in ((16, [1, 1, 1], 17), (4, [60, 3, 1], 18)):
+        c = R.Cache(seqs=3, T=2600, H=4, d=128, bits=bits, seed=seed)
+        ctx = c.context(16, 60)
+        held = [2500, 17, 1300]
+        q = queries(sum(new), 16, 128, seed)
+        o, lse, w = torch.empty_like(q), torch.empty(sum(new), 16, device="cuda"), fresh(c)
+        seq_ids, cu, ln = R.batch(new, held)
+        s = torch.cuda.Stream()
+
+        def call(c=c, ctx=ctx, q=q, o=o, lse=lse, w=w, seq_ids=seq_ids, cu=cu, ln=ln, s=s, most=max(new)):
+            E.epikv_attention_chunk(ctx, 0, 3, seq_ids, cu, most, ln, E.rows(q), E.rows(o), c.c.view(), lse=lse, stream=s)
+            E.epikv_attention_weights(ctx, 0, 3, seq_ids, cu, most, ln, E.rows(q), lse, E.weights_view(w), c.c.view(), stream=s)
+        torch.cuda.synchronize()
+        call()
+        torch.cuda.synchronize()
+        calls.append((call, s, (o, lse, w), [x.clone() for x in (o, lse, w)], ctx))
+    (eager, _, _, _, _), (other, s, _, _, _) = calls
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        other()
+    for _, _, got, _, _ in calls:
+        for x in got:
+            x.zero_()
+    calls[0][2][2].fill_(-7.5), calls[1][2][2].fill_(-7.5)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        eager()
+        with torch.cuda.stream(s):
+            g.replay()
+    torch.cuda.synchronize()
+    for _, _, got, want, ctx in calls:
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+        assert E.epikv_attn_get_error(ctx) == OK
+
+
 # ------------------------------------------------------------------ eviction by the weights
 def plain_kept(score, K, prefill, cap=128):
     n = len(score)
