@@ -5,13 +5,13 @@
 // The products run on tcgen05 with the slots as the instruction's 128 rows and
 // the query rows as its columns, so that a thread owns a slot and adds up its
 // columns: no exchange between threads, and each slot's sum is formed in the
-// order of the rows.  A unit is a run of slots of one entry and KV head: its
-// keys stay in shared memory while tiles of query rows (steps) pass by.  Two
-// forms: units of 128 slots and 16 rows a step, where a call has no more (a
-// decode step: reading the keys bounds it), and of 256 slots and 128 rows (a
-// chunk: exponentials and products).  One CTA an SM takes an equal share of all
-// units' steps (chunk_plan.h); the few units that two shares meet in are joined
-// by a second kernel, part by part.
+// order of the rows.  A unit is a run of 256 slots (128 at 256 channels) of one
+// entry and KV head: its keys stay in shared memory while tiles of query rows
+// (steps) pass by.  Two forms: steps of 16 rows where a call has no more (a
+// decode step: reading the keys bounds it), and of 128 (a chunk: exponentials
+// and products).  One CTA an SM takes an equal share of all units' steps
+// (chunk_plan.h); the few units that two shares meet in are joined by a second
+// kernel, part by part.
 //
 // 32 query and 8 KV heads of 128: a decode step of 64 bf16 caches of 2,048 to
 // 8,192 slots 112 us (6.1 TB/s, 90 % of the measured rate); of 32 4-bit caches of
