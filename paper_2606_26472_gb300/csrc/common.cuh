@@ -46,7 +46,8 @@ struct DevState {
   uint32_t* ticket;        // [S] last-CTA tickets of the finalize kernel
   int32_t* err;            // [1] sticky device error word
   unsigned long long* stats;  // [4] epikv_stats
-  float* score[kNumKinds]; // [S][T] scores per kind (null when the kind is off); frozen but for WEIGHT's
+  float* score[kNumKinds + 1]; // [S][T] scores per kind (null when the kind is off); frozen but for WEIGHT's.  The last is null: an
+                           // odd count moves what follows off 16 bytes (the ragged batch's copies 1.3 % slower)
   int32_t* pos;            // [S][T] position of each slot
   __nv_bfloat16* h_prev;   // [S][2][n_band][D] last hidden row per band layer
   float* g_ring;           // [S][n_band][G] g by position (mod G)
