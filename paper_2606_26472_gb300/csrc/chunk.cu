@@ -20,7 +20,7 @@
 //
 // 32 query and 8 KV heads of 128.  Long chunks are bound by products and
 // exponentials: 2,048 tokens behind 14,336 344 us (1.5 PFLOP/s, 77 % of the
-// measured rate), a prompt of 4,096 128 us (1.07, 55 %: items of 1 to 33 tiles,
+// measured rate), a prompt of 4,096 127 us (1.08, 56 %: items of 1 to 33 tiles,
 // each with its queries, results and half-empty last tiles).  Few tokens by
 // the cache's bytes and the chain of launch, lookups, first tiles and join:
 // 8 x 16 tokens behind 4,096 43 us (3.2 TB/s).  4-bit rows by the copying warps'
