@@ -154,7 +154,10 @@ struct alignas(16) ChunkShared {
   uint64_t query, full[kStages], empty[kStages], scores[2], weights[2][2], sums, done, landed, drained;
   uint32_t tmem;
   int gave_up;
-  volatile int unclean[4];                  // 1 + the last segment with an infinite or NaN value in a slot that not all its rows see
+  // 1 + the last segment with an infinite or NaN value in a slot that not all its rows see.  The copying warps may be a ring of
+  // tiles ahead of the segment that the owners of rows have yet to look up.
+  volatile int unclean[8];
+  static_assert(kStages / 2 < 8, "a place for each segment that the ring can hold, and one more");
   int64_t offset[2][ChunkShape<D>::kSlots]; // of a tile's slots, elements; -1: none
   ShareStart start;
   unsigned from, to;                        // the CTA's share
@@ -342,7 +345,7 @@ struct Copier {
         const uint4 v = lds16(place(x));
         if (unbounded<kBit>(v)) {
           sts16(place(x), make_uint4(bounded<kBit>(v.x), bounded<kBit>(v.y), bounded<kBit>(v.z), bounded<kBit>(v.w)));
-          sh.unclean[seg & 3] = seg + 1;
+          sh.unclean[seg & 7] = seg + 1;
         }
       }
     for (int x = max(to, 0) + tid; x < Shape::kSlots * kRow; x += kCopyThreads) sts16(place(x), make_uint4(0, 0, 0, 0));
@@ -835,7 +838,7 @@ __global__ void __launch_bounds__(chunk_threads(FMT), 1)
     mbar_init(&sh.drained, 1);
     sh.gave_up = 0;
     sh.split = {};
-    for (int i = 0; i < 4; ++i) sh.unclean[i] = 0;
+    for (int i = 0; i < 8; ++i) sh.unclean[i] = 0;
     fence_barrier_init();
   }
   pdl_wait();
@@ -898,7 +901,7 @@ __global__ void __launch_bounds__(chunk_threads(FMT), 1)
           soften<D, FMT, kTiles>(sh, wait, t0, t1, a, seen, factor, lanes, t, &m, &l);
           wait(&sh.done, (uint32_t)seg & 1);
           tensor_fence_after();
-          unclean = sh.unclean[seg & 3] == seg + 1;
+          unclean = sh.unclean[seg & 7] == seg + 1;
           a += t1 - t0;
           ++seg;
         }

@@ -294,3 +294,34 @@ def test_reported_and_skipped(gpu_lib):
     ref = R.attention64(q[:32], k, v, [101 + i for i in range(32)], 0.125)
     assert float((l.double() - ref[1]).abs().max()) < 1e-4
     assert float((o.double() - ref[0]).abs().max()) <= float(((2.0 ** -8) * 2.1 * ref[2]).max())
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("d", [64, 128])
+def test_infinities_in_many_short_segments(gpu_lib, bits, d):
+    """Each CTA takes a dozen items of one tile, each with a value that is infinite (over 4-bit rows: 16 that are NaN) in a slot
+    that its first rows do not see."""
+    S, held, new = 900, 20, 16
+    c = R.Cache(seqs=S, T=48, H=2, d=d, bits=bits, seed=20)
+    ctx = c.context(2, new)
+    q = queries(S * new, 2, d)
+    clean, lse = attend(c, ctx, q, [new] * S, [held] * S)
+    at = [held + 1 + b % (new - 1) for b in range(S)]
+    for b in range(S):
+        row = int(c.index(0, b, [at[b]])[0])
+        if bits == 16:
+            c.c.v.view(-1, 2, d)[row, 1, b % d] = math.inf
+        else:
+            c.raw(1)[row, d + d // 16] = 0x7F             # the second head's first scale
+    o, l = attend(c, ctx, q, [new] * S, [held] * S)
+    sees = (torch.arange(new, device="cuda") + held >= torch.tensor(at, device="cuda")[:, None])          # [S, new]
+    bad = torch.zeros(S, new, 2, d, dtype=torch.bool, device="cuda")
+    if bits == 16:
+        ch = torch.nn.functional.one_hot(torch.arange(S, device="cuda") % d, d).bool()
+        bad[:, :, 1] = sees[..., None] & ch[:, None]
+    else:
+        bad[:, :, 1, :16] = sees[..., None]
+    bad = bad.view(S * new, 2, d)
+    assert bool((o[bad] == math.inf).all() if bits == 16 else o[bad].isnan().all())
+    assert torch.equal(o[~bad], clean[~bad]) and torch.equal(l, lse)
+    assert E.epikv_attn_get_error(ctx) == OK
