@@ -379,6 +379,8 @@ struct Copier {
       }
       if (bar == full) continue;
       wait(bar, (uint32_t)(*turns)++ & 1);
+      // One bit tells the phase, and the first warp arms the next one: not before all are behind this one's wait.
+      named_sync(1, kCopyThreads);
       clean(i, s0, g, seg);
       deliver(i);
     }

@@ -64,3 +64,68 @@ def test_as_many_places_as_tiles_would_not_do():
     with pytest.raises(AssertionError):
         for seed in range(200):
             flags(4, 4, 60, np.random.default_rng(seed), 0.95)
+
+
+def body(head):
+    """The text of the member function whose declaration starts so."""
+    start = TEXT.index("{", TEXT.index(head))
+    depth = 0
+    for i in range(start, len(TEXT)):
+        depth += (TEXT[i] == "{") - (TEXT[i] == "}")
+        if depth == 0:
+            return TEXT[start:i + 1]
+
+
+def landings(ring, warps, tiles, together, rng):
+    """Tensor copies of values that are to be looked through: the first copying warp arms one barrier for each, all wait on it by
+    one bit of its phases, look through what came and hand it on.  The ring has room once all have handed on the tile that stood
+    there.  together: the warps meet behind the wait."""
+    armed = landed = 0
+    at = [0] * warps                  # tiles that a warp has handed on
+    passed = [0] * warps              # waits that a warp is behind
+    phase = lambda w, n: landed % 2 != n % 2          # the wait for phase n ends while another parity is current  # noqa: E731
+    while min(at) < tiles:
+        moves = []
+        for w in range(warps):
+            n = at[w]
+            if n >= tiles:
+                continue
+            if w == 0 and armed == n and min(at) > n - ring:
+                moves.append(("arm", w))
+            if passed[w] == n and (w or armed > n) and min(at) > n - ring and phase(w, n):
+                assert landed > n, "read before it is there"
+                moves.append(("pass", w))
+            if passed[w] > n and (not together or min(passed) > n):
+                moves.append(("hand on", w))
+        if landed < armed:
+            moves.append(("land", 0))
+        assert moves, "everybody waits"
+        move, w = moves[rng.integers(len(moves))]
+        if move == "arm":
+            armed += 1
+        elif move == "land":
+            landed += 1
+        elif move == "pass":
+            passed[w] += 1
+        else:
+            at[w] += 1
+
+
+def warps_meet():
+    """Whether all copying warps meet between the wait for a tile's values and the looking through."""
+    text = body("void tensor_tile(")
+    wait = text.index("wait(bar,")
+    return "named_sync(1, kCopyThreads)" in text[wait:text.index("clean(", wait)]
+
+
+@pytest.mark.parametrize("which", [0, 1])
+def test_no_copying_warp_is_left_a_phase_behind(which):
+    rng = np.random.default_rng(which)
+    for _ in range(200):
+        landings(ring_tiles()[which], 3, 30, warps_meet(), rng)
+
+
+def test_one_bit_would_not_do_without_meeting():
+    with pytest.raises(AssertionError):
+        for seed in range(200):
+            landings(4, 3, 30, False, np.random.default_rng(seed))

@@ -325,3 +325,26 @@ def test_infinities_in_many_short_segments(gpu_lib, bits, d):
     assert bool((o[bad] == math.inf).all() if bits == 16 else o[bad].isnan().all())
     assert torch.equal(o[~bad], clean[~bad]) and torch.equal(l, lse)
     assert E.epikv_attn_get_error(ctx) == OK
+
+
+@pytest.mark.parametrize("H,Hq,d", [(2, 2, 64), (1, 1, 128), (2, 4, 64), (1, 2, 256)])
+def test_infinities_in_every_tile_that_not_all_rows_see(gpu_lib, H, Hq, d):
+    """Items whose rows end in three tiles in a row: the copying warps look through each, and find some in one warp's rows."""
+    S, held, new = 120, 100, 300
+    c = R.Cache(seqs=S, T=400, H=H, d=d, seed=21)
+    ctx = c.context(Hq, new)
+    q = queries(S * new, Hq, d)
+    clean, lse = attend(c, ctx, q, [new] * S, [held] * S)
+    at = torch.arange(S, device="cuda") % 7 + held + torch.tensor([[20], [140], [290]], device="cuda")      # [3, S]
+    pool, bad = c.c.v.view(-1, H, d), torch.zeros(S, new, Hq, d, dtype=torch.bool, device="cuda")
+    for i in range(3):
+        for b in range(S):
+            pool[int(c.index(0, b, [int(at[i, b])])[0]), H - 1, (5 * b + i) % d] = -math.inf
+        sees = torch.arange(new, device="cuda") + held >= at[i][:, None]
+        ch = torch.nn.functional.one_hot((5 * torch.arange(S, device="cuda") + i) % d, d).bool()
+        bad[:, :, Hq - Hq // H:] |= (sees[..., None] & ch[:, None])[:, :, None]
+    o, l = attend(c, ctx, q, [new] * S, [held] * S)
+    assert E.epikv_attn_get_error(ctx) == OK
+    bad = bad.view(S * new, Hq, d)
+    # (beside the infinity a row may also have probabilities of exactly 0 in slots that all rows of an item see: NaN there)
+    assert bool((~o[bad].isfinite()).all()) and torch.equal(o[~bad], clean[~bad]) and torch.equal(l, lse)
