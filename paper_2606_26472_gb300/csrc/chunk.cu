@@ -388,6 +388,7 @@ struct Copier {
 
   __device__ __forceinline__ void bf16_segment(const Segment& g, int i, int seg, int* turns) const {
     const bool flat = kv.layout == EPIKV_LAYOUT_CONTIGUOUS;
+    int tables = 0;
     for (int j = g.t0; j < g.t1; ++j, i += 2) {
       const int s0 = j * Shape::kSlots;
       bool whole = maps.slots && min(s0 + Shape::kSlots, g.most) <= maps.end;
@@ -405,15 +406,16 @@ struct Copier {
         whole = __all_sync(0xffffffffu, there);   // else by lanes, which report it
         if (whole) tensor_tile(i, j, y, z, g, seg, turns);
       }
-      if (!whole) lane_tile(i, j, g, seg);
+      if (!whole) lane_tile(i, j, g, seg, &tables);
     }
     named_sync(1, kCopyThreads);   // the offsets are free for the next segment
   }
 
   // By lanes: the values' copies are under way while the keys' are waited for.
-  __device__ __forceinline__ void lane_tile(int i, int j, const Segment& g, int seg) const {
+  __device__ __forceinline__ void lane_tile(int i, int j, const Segment& g, int seg, int* tables) const {
     const int s0 = j * Shape::kSlots;
-    int64_t* offset = sh.offset[j & 1];   // all threads were here for the tile before, so this one's is free
+    // two take turns among the tiles that come here: all threads met at the last such tile, behind reading the one before it
+    int64_t* offset = sh.offset[(*tables)++ & 1];
     tile_offsets(offset, Shape::kSlots, s0, g.most, kv, layer, g.e.seq, dm.T, err, tid, kCopyThreads);
     named_sync(1, kCopyThreads);
 #pragma unroll 1

@@ -129,3 +129,38 @@ def test_one_bit_would_not_do_without_meeting():
     with pytest.raises(AssertionError):
         for seed in range(200):
             landings(4, 3, 30, False, np.random.default_rng(seed))
+
+
+def offsets(by_lanes, by_tile, warps, rng):
+    """Tiles that are copied by lanes (else by tensor copies, at which these warps need not meet): each warp writes its part of the
+    tile's table of offsets, all meet, each reads all of it.  by_tile: a tile's table goes by its number, else by how many were
+    copied by lanes before it."""
+    tables = [[None] * warps, [None] * warps]
+    mine = [j for j, lanes in enumerate(by_lanes) if lanes]
+    of = lambda i: tables[(mine[i] if by_tile else i) & 1]    # noqa: E731
+    wrote, read = [0] * warps, [0] * warps
+    while min(read) < len(mine):
+        w = int(rng.integers(warps))
+        if read[w] == len(mine):
+            continue
+        if wrote[w] == read[w]:
+            of(wrote[w])[w] = mine[wrote[w]]
+            wrote[w] += 1
+        elif min(wrote) > read[w]:
+            assert all(x == mine[read[w]] for x in of(read[w])), "another tile's offsets"
+            read[w] += 1
+
+
+def test_offsets_outlive_their_reading():
+    text = body("void lane_tile(")
+    by_tile = "sh.offset[j & 1]" in text
+    assert by_tile or "sh.offset[(*tables)++ & 1]" in text
+    rng = np.random.default_rng(0)
+    for _ in range(300):
+        offsets(rng.random(12) < rng.random(), by_tile, 3, rng)
+
+
+def test_tables_by_the_tile_would_not_do():
+    with pytest.raises(AssertionError):
+        for seed in range(200):
+            offsets([True, False, True], True, 3, np.random.default_rng(seed))

@@ -348,3 +348,34 @@ def test_infinities_in_every_tile_that_not_all_rows_see(gpu_lib, H, Hq, d):
     bad = bad.view(S * new, Hq, d)
     # (beside the infinity a row may also have probabilities of exactly 0 in slots that all rows of an item see: NaN there)
     assert bool((~o[bad].isfinite()).all()) and torch.equal(o[~bad], clean[~bad]) and torch.equal(l, lse)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("new,H,Hq,d", [(1, 2, 8, 64), (90, 2, 2, 128), (40, 1, 8, 256), (200, 3, 3, 64)])
+def test_blocks_that_are_none(gpu_lib, bits, new, H, Hq, d):
+    """Slots of blocks that the pool does not have are rows of zeros, all others what they are: tiles with such blocks between
+    tiles without, in several sequences."""
+    S, T, held = 12, 1700, 1400
+    c = R.Cache(seqs=S, T=T, H=H, d=d, bits=bits, seed=22)
+    ctx = c.context(Hq, new)
+    q = queries(S * new, Hq, d)
+    table = c.c.block_table.clone()
+    gone = torch.zeros(S, T + 16, dtype=torch.bool, device="cuda")
+    for s in range(S):
+        for i, t in enumerate(range(s % 3, 12, 2)):          # every second tile of 128 slots
+            b = 8 * t + (3 * i + s) % 8
+            if 16 * b < held:
+                table[s, b] = (c.c.num_blocks, -1, 1 << 30, -(1 << 31))[i % 4]
+                gone[s, 16 * b:16 * b + 16] = True
+    seq_ids, cu, ln = R.batch([new] * S, [held] * S)
+    o, l = torch.empty_like(q), torch.empty(S * new, Hq, device="cuda")
+    E.epikv_attention_chunk(ctx, 0, S, seq_ids, cu, new, ln, E.rows(q), E.rows(o), c.c.view(table), lse=l)
+    assert E.epikv_attn_get_error(ctx) == (E.EPIKV_EDEVICE, E.EPIKV_DEV_SLOT)
+    whole = c.read
+
+    def with_zeros(w, layer, s, top):
+        x = whole(w, layer, s, top).clone()
+        x[gone[s, :top]] = 0
+        return x
+    c.read = with_zeros
+    check_attention(c, q, o, l, [new] * S, [held] * S)
