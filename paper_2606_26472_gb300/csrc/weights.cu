@@ -197,6 +197,7 @@ __device__ __forceinline__ bool move_on(WeightWalk& walk, int lane) {
   __syncwarp();
   int more = 0;
   if (lane == 0) more = walk.next<false>();
+  __syncwarp();   // (a shuffle does not order what the others read of the walk)
   return __shfl_sync(0xffffffffu, more, 0);
 }
 

@@ -10,6 +10,7 @@ import pytest
 from .plans import CSRC
 
 TEXT = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "chunk.cu")).read())
+WEIGHTS = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "weights.cu")).read())
 
 
 def number(pattern):
@@ -66,14 +67,14 @@ def test_as_many_places_as_tiles_would_not_do():
             flags(4, 4, 60, np.random.default_rng(seed), 0.95)
 
 
-def body(head):
-    """The text of the member function whose declaration starts so."""
-    start = TEXT.index("{", TEXT.index(head))
+def body(head, text=TEXT):
+    """The text of the function whose declaration starts so."""
+    start = text.index("{", text.index(head))
     depth = 0
-    for i in range(start, len(TEXT)):
-        depth += (TEXT[i] == "{") - (TEXT[i] == "}")
+    for i in range(start, len(text)):
+        depth += (text[i] == "{") - (text[i] == "}")
         if depth == 0:
-            return TEXT[start:i + 1]
+            return text[start:i + 1]
 
 
 def landings(ring, warps, tiles, together, rng):
@@ -164,3 +165,10 @@ def test_tables_by_the_tile_would_not_do():
     with pytest.raises(AssertionError):
         for seed in range(200):
             offsets([True, False, True], True, 3, np.random.default_rng(seed))
+
+
+@pytest.mark.parametrize("file,head,step", [("chunk", "bool next(", "step("), ("weights", "bool move_on(", "next<false>()")])
+def test_a_walk_in_shared_memory_is_read_behind_a_warp_barrier(file, head, step):
+    """One lane moves the walk on and the others read it: a shuffle alone does not order memory."""
+    inside = body(head, {"chunk": TEXT, "weights": WEIGHTS}[file])
+    assert "__syncwarp()" in inside[:inside.index(step)] and "__syncwarp()" in inside[inside.index(step):]
