@@ -765,8 +765,8 @@ __device__ __forceinline__ void add_up(WeightShared<D, FMT, N>& sh, const Tensor
 
 template <int D, int FMT, int N>
 __global__ void __launch_bounds__(WeightShape<D, FMT, N>::kThreads, 1)
-    weights_kernel(AttnState st, AttnDims dm, WeightPlan plan, Batch ba, WeightCall call, Rows q, KvDev kv,
-                   const __grid_constant__ LayerMaps maps) {
+    weights_kernel(AttnState st, AttnDims dm, const __grid_constant__ WeightPlan plan, const __grid_constant__ Batch ba,
+                   WeightCall call, Rows q, KvDev kv, const __grid_constant__ LayerMaps maps) {
   using Shape = WeightShape<D, FMT, N>;
   extern __shared__ char dynamic[];
   char* ring = dynamic + ((1024 - (smem_u32(dynamic) & 1023)) & 1023);

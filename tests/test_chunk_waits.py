@@ -172,3 +172,14 @@ def test_a_walk_in_shared_memory_is_read_behind_a_warp_barrier(file, head, step)
     """One lane moves the walk on and the others read it: a shuffle alone does not order memory."""
     inside = body(head, {"chunk": TEXT, "weights": WEIGHTS}[file])
     assert "__syncwarp()" in inside[:inside.index(step)] and "__syncwarp()" in inside[inside.index(step):]
+
+
+def test_what_a_walk_in_shared_memory_refers_to_is_every_threads():
+    """One lane's addresses of the batch and the plan serve the whole warp, so neither may be a thread's own copy."""
+    walk = body("struct WeightWalk", WEIGHTS)
+    kept = set(re.findall(r"const (\w+)& \w+;", walk))
+    assert kept == {"Batch", "WeightPlan"}
+    kernel = WEIGHTS[WEIGHTS.index("weights_kernel(AttnState"):]
+    parameters = kernel[:kernel.index("{")]
+    for kind in kept:
+        assert re.search(rf"const __grid_constant__ {kind} \w+", parameters), kind
