@@ -548,7 +548,8 @@ epikv_status epikv_attention_weights(epikv_attn_ctx* ctx, int32_t layer, int32_t
  *   score = decay * score + sum over h = 0 .. n_heads-1 of w(seq, h, slot)
  * (32 bits, each product and sum rounded, heads first, in order).  decay is in 0 .. 1; 1 accumulates for good.
  * Belongs between epikv_score_update, which registers the step's tokens, and epikv_select; the scores move with their
- * tokens from then on, and epikv_read_slots returns them. */
+ * tokens from then on, and epikv_read_slots returns them.  An entry whose eviction is selected but not yet compacted is
+ * reported (EPIKV_DEV_KEPT) and keeps its scores: they stand by its new slots already. */
 epikv_status epikv_weigh(epikv_ctx* ctx, int32_t n_seq, const int32_t* d_seq_ids, const epikv_weights* w, int32_t n_heads,
                          float decay, cudaStream_t stream);
 

@@ -906,6 +906,10 @@ __global__ void __launch_bounds__(256) weigh_kernel(DevState st, Dims dm, const 
     return;
   }
   const int n = st.n_cache[seq];
+  if (st.first_changed[seq] < n) {   // selected, not compacted: the scores stand by other slots than the weights
+    if (threadIdx.x == 0) set_error(st.err, EPIKV_DEV_KEPT);
+    return;
+  }
   float* score = st.score[kind_index(EPIKV_SCORE_WEIGHT)] + (size_t)seq * dm.T;
   for (int s = blockIdx.x * blockDim.x + threadIdx.x; s < n; s += gridDim.x * blockDim.x) {
     const float* p = w + seq * stride_seq + s;

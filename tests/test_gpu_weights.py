@@ -502,3 +502,26 @@ def test_weigh_of_sequences_that_are_none(gpu_lib):
     assert E.epikv_get_error(ctx) == (E.EPIKV_EDEVICE, E.EPIKV_DEV_BATCH)
     assert E.epikv_read_slots(ctx, 1, E.EPIKV_SCORE_WEIGHT, 50)[1] == w[1, 0, :3].tolist()
     E.epikv_destroy(ctx)
+
+
+def test_weigh_between_selection_and_compaction(gpu_lib):
+    """The slots are others already: reported, the scores stay, and a sequence that was not cut takes its weights."""
+    lp = Loop(E.EPIKV_SCORE_WEIGHT)
+    lp.update([0, 1, 2], [150, 40, 300])
+    lp.weigh([0, 1, 2], 1.0)
+    seq_ids = R.batch([0] * 3, [0] * 3)[0]
+    kept = torch.full((3, lp.T), -1, dtype=torch.int32, device="cuda")
+    E.epikv_select(lp.ctx, 3, seq_ids, torch.full((3,), 100, dtype=torch.int32, device="cuda"), None, kept, lp.T, None)
+    for s in (0, 2):
+        got = plain_kept(lp.score[s], 100, lp.prefill[s])
+        lp.score[s], lp.pos[s] = lp.score[s][got], lp.pos[s][got]
+    lp.check()
+    before = [x.copy() for x in lp.score]
+    lp.weigh([0, 1, 2], 0.5)
+    lp.score[0], lp.score[2] = before[0], before[2]
+    assert E.epikv_get_error(lp.ctx) == (E.EPIKV_EDEVICE, E.EPIKV_DEV_KEPT)
+    lp.check()
+    E.epikv_compact(lp.ctx, 3, seq_ids, kept, lp.T, lp.cache.view())
+    lp.weigh([0, 1, 2], 0.5)
+    lp.check()
+    assert E.epikv_get_error(lp.ctx) == OK
