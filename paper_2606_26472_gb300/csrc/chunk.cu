@@ -892,6 +892,7 @@ __global__ void __launch_bounds__(chunk_threads(FMT), 1)
                                       : (int64_t)(g.e.tok0 + g.row0 / dm.rep) * q.st + (g.kh * dm.rep + g.row0 % dm.rep) * q.sh) * 2;
         factor = c * store_queries<D, !kBf16>(smem_u32(smem + t * Shape::kQuery), tid & 96, src, lane);
         if constexpr (!kBf16) factor *= head_scale(st, dm, 0, layer, g.kh);
+        factor = score_factor(factor);
         fence_proxy_async_smem();
         mbar_arrive_one(&sh.query);
       };

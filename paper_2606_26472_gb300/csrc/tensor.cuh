@@ -297,8 +297,15 @@ __device__ __forceinline__ void expand32(const uint4& codes, uint32_t scales, ui
   }
 }
 
+// What turns a score as it is summed into log2 units, kept a normal number: 0 x -inf (a slot that a row does not see) and
+// inf x 0 are NaN.
+__host__ __device__ __forceinline__ float score_factor(float f) {
+  return f < 0x1p-126f ? 0x1p-126f : f > 0x1.fffffep127f ? 0x1.fffffep127f : f;
+}
+
 // Pieces of eight bf16 queries, M rows', as halves.  The kPer lanes that hold a row scale it by a power of two to below 2^15:
-// exact down to 2^-31 of the row's largest.  undo: what undoes the scaling.
+// bf16's 8 bits then stand whole in channels down to 2^-31 of the row's largest (of rows below 2^-112, which get 2^126, down to
+// 2^-17 or more).  undo: what undoes the scaling.
 template <int kPer, int M>
 __device__ __forceinline__ void halves_of(uint4 (&x)[M], float (&undo)[M]) {
   uint32_t top[M];   // largest magnitudes, as bf16 bits: they are ordered like the values
@@ -315,10 +322,10 @@ __device__ __forceinline__ void halves_of(uint4 (&x)[M], float (&undo)[M]) {
     for (int i = 0; i < M; ++i) top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], o));
 #pragma unroll
   for (int i = 0; i < M; ++i) {
-    // 2^e <= largest < 2^(e + 1); up to 2^100, so that neither factor leaves the normal numbers
-    const int up = min(14 - ((int)(top[i] >> 7) - 127), 100);
-    const float mul = __uint_as_float((uint32_t)(up + 127) << 23);
-    undo[i] = __uint_as_float((uint32_t)(127 - up) << 23);
+    // 2^(141 - ex) of the biased exponent ex and its inverse, both normal numbers (ex = 255: the finite ones' largest)
+    const int ex = min(max((int)(top[i] >> 7), 15), 254);
+    const float mul = __uint_as_float((uint32_t)(268 - ex) << 23);
+    undo[i] = __uint_as_float((uint32_t)(ex - 14) << 23);
     x[i] = make_uint4(half_pair(bf16_lo(x[i].x) * mul, bf16_hi(x[i].x) * mul), half_pair(bf16_lo(x[i].y) * mul, bf16_hi(x[i].y) * mul),
                       half_pair(bf16_lo(x[i].z) * mul, bf16_hi(x[i].z) * mul), half_pair(bf16_lo(x[i].w) * mul, bf16_hi(x[i].w) * mul));
   }

@@ -523,7 +523,7 @@ __device__ __forceinline__ void copy_queries(char* ring, WeightShared<D, FMT, N>
   auto tell = [&](const Row& r, int qs, float back) {   // what is needed beside the rows
     if (lane < R) {
       sh.lse2[qs][own] = -r.lse * kLog2e;
-      if constexpr (kHalf) sh.factor[qs][own] = call.c * head_scale(st, dm, 0, call.layer, g.kh) * back;
+      if constexpr (kHalf) sh.factor[qs][own] = score_factor(call.c * back * head_scale(st, dm, 0, call.layer, g.kh));
       sh.seen[qs][own] = r.lse == -INFINITY ? 0 : r.seen;   // (the row saw nothing)
     }
     if constexpr (N != 16) {
@@ -694,7 +694,7 @@ __device__ __forceinline__ void add_up(WeightShared<D, FMT, N>& sh, const Tensor
       continue;
     }
     const int ks = i % Shape::kKeyStages, rows = (g.e.n - g.token) * walk.plan.rep;   // (16 rows are one step)
-    const float c = FMT == EPIKV_CACHE_BF16 ? call.c : call.c * head_scale(st, dm, 0, call.layer, g.kh);
+    const float c = score_factor(FMT == EPIKV_CACHE_BF16 ? call.c : call.c * head_scale(st, dm, 0, call.layer, g.kh));
     f32x2 sum[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) sum[j] = f2_pack(0.f, 0.f);

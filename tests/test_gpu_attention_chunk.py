@@ -379,3 +379,20 @@ def test_blocks_that_are_none(gpu_lib, bits, new, H, Hq, d):
         return x
     c.read = with_zeros
     check_attention(c, q, o, l, [new] * S, [held] * S)
+
+
+@pytest.mark.parametrize("d", [64, 256])
+@pytest.mark.parametrize("bits,scale,keys", [(4, 0.0, 2.0 ** -60), (4, 1e-30, 1.0), (4, 0.0, 2.0 ** -100), (16, 3e38, 1.0), (4, 3e38, 1.0),
+                                             (16, 1e-45, 1.0)])
+def test_factors_that_leave_the_normal_numbers(gpu_lib, bits, scale, keys, d):
+    """Query rows of zeros (a padded batch's) and of tiny numbers beside small or large scales: a score of 0 stays one, and what a
+    row does not see stays unseen."""
+    ks = None if bits == 16 else torch.tensor([[[keys, 1.0]], [[1.0, 0.5]]], device="cuda")
+    c = R.Cache(seqs=1, T=300, H=2, d=d, bits=bits, kv_scale=ks, seed=23)
+    ctx = c.context(4, 60, softmax_scale=scale)
+    q = queries(60, 4, d)
+    q[1::2] = (q[1::2].float() * 2.0 ** -120).to(torch.bfloat16)
+    q[::4 if scale < 1 else 1] = 0
+    o, l = attend(c, ctx, q, [60], [200])
+    check_attention(c, q, o, l, [60], [200], scale=scale or None)
+    assert bool(o.isfinite().all())

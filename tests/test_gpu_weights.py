@@ -525,3 +525,21 @@ def test_weigh_between_selection_and_compaction(gpu_lib):
     lp.weigh([0, 1, 2], 0.5)
     lp.check()
     assert E.epikv_get_error(lp.ctx) == OK
+
+
+@pytest.mark.parametrize("new", [2, 60])
+@pytest.mark.parametrize("bits,scale,keys", [(4, 0.0, 2.0 ** -60), (4, 0.0, 2.0 ** -100), (16, 3e38, 1.0), (4, 3e38, 1.0)])
+def test_factors_that_leave_the_normal_numbers(gpu_lib, bits, scale, keys, new):
+    """Query rows of zeros and of tiny numbers beside small or large scales."""
+    ks = None if bits == 16 else torch.tensor([[[keys, 1.0]], [[1.0, 0.5]]], device="cuda")
+    c = R.Cache(seqs=1, T=300, H=2, d=64, bits=bits, kv_scale=ks, seed=23)
+    ctx = c.context(4, 60, softmax_scale=scale)
+    q = queries(new, 4, 64)
+    q[1::2] = (q[1::2].float() * 2.0 ** -120).to(torch.bfloat16)
+    q[::4 if scale < 1 else 1] = 0
+    lse = lse64(c, q, [new], [200], scale=scale or None)
+    w = fresh(c)
+    before = w.clone()
+    weigh(c, ctx, q, lse, [new], [200], w)
+    check_weights(c, q, lse, [new], [200], w, before, scale=scale or None)
+    assert bool(w[:, :, :200 + new].isfinite().all())
