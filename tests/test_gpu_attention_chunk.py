@@ -396,3 +396,49 @@ def test_factors_that_leave_the_normal_numbers(gpu_lib, bits, scale, keys, d):
     o, l = attend(c, ctx, q, [60], [200])
     check_attention(c, q, o, l, [60], [200], scale=scale or None)
     assert bool(o.isfinite().all())
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_a_long_prompt(gpu_lib, bits):
+    """70,001 tokens at once, some of its rows against 64 bits."""
+    n, d = 70001, 64
+    c = R.Cache(seqs=1, T=n, H=1, d=d, bits=bits, seed=26)
+    ctx = c.context(1, n)
+    q = queries(n, 1, d)
+    o, l = attend(c, ctx, q, [n], [0])
+    k, v = c.read(0, 0, 0, n), c.read(1, 0, 0, n)
+    for i in (0, 1, 127, 128, 129, 255, 256, 4096, 33333, 65535, 65536, n - 130, n - 1):
+        ref, lse, big, qk = R.attention64(q[i:i + 1], k[:i + 1], v[:i + 1], [i + 1], d ** -0.5)
+        ds = d * 2.0 ** -24 * qk + 1e-6
+        p = (2.0 ** -8 if bits == 16 else 2.0 ** -11) + 2.0 ** -21 + i * 2.0 ** -24
+        tiny = 0.0 if bits == 16 else (i + 1) * 2.0 ** -32 * float(v[:i + 1].abs().max())
+        assert bool(((o[i].double() - ref[0]).abs() <= 2.0 ** -8 * ref[0].abs() + (p + 2 * ds[0, :, None]) * big[0] + tiny).all()), i
+        assert bool(((l[i].double() - lse[0]).abs() <= ds[0] + 2.0 ** -22 * (1 + lse[0].abs()) + (i + 1) * 2.0 ** -24).all()), i
+    assert E.epikv_attn_get_error(ctx) == OK
+
+
+def test_rows_behind_the_last_sequence(gpu_lib):
+    """A batch padded with entries of no tokens and rows behind them: those stay as they were."""
+    c = R.Cache(seqs=4, T=200, H=2, d=128, seed=27)
+    ctx = c.context(8, 40)
+    q = queries(64, 8, 128)
+    o, l = torch.full_like(q, 3.0), torch.full((64, 8), 3.0, device="cuda")
+    seq_ids, cu, ln = R.batch([40, 0, 7, 0], [30, 100, 0, 0])
+    E.epikv_attention_chunk(ctx, 0, 4, seq_ids, cu, 40, ln, E.rows(q), E.rows(o), c.c.view(), lse=l)
+    check_attention(c, q[:47], o[:47], l[:47], [40, 0, 7, 0], [30, 100, 0, 0])
+    assert bool((o[47:] == 3.0).all()) and bool((l[47:] == 3.0).all())
+    again = torch.full_like(q, 3.0)                      # without the log-sums
+    E.epikv_attention_chunk(ctx, 0, 4, seq_ids, cu, 40, ln, E.rows(q), E.rows(again), c.c.view())
+    assert torch.equal(again, o)
+    assert E.epikv_attn_get_error(ctx) == OK
+
+
+@pytest.mark.parametrize("H,Hq", [(1, 1024), (2, 600)])
+def test_many_query_heads(gpu_lib, H, Hq):
+    """More query heads of a KV head than an item has rows."""
+    c = R.Cache(seqs=2, T=300, H=H, d=64, seed=28)
+    ctx = c.context(Hq, 5)
+    q = queries(7, Hq, 64)
+    o, l = attend(c, ctx, q, [5, 2], [250, 3])
+    check_attention(c, q, o, l, [5, 2], [250, 3])
+    assert E.epikv_attn_get_error(ctx) == OK

@@ -9,7 +9,8 @@ from paper_2606_26472_gb300 import epikv as E
 from paper_2606_26472_gb300.cache import KVCache
 
 from . import cache_ops as R
-from .chunk_ops import attend, check_weights, lse64, queries, weigh
+from .chunk_ops import attend, check_attention, check_weights, lse64, queries, weigh
+from .harness import oracle_kept
 
 pytestmark = pytest.mark.gpu
 
@@ -543,3 +544,61 @@ def test_factors_that_leave_the_normal_numbers(gpu_lib, bits, scale, keys, new):
     weigh(c, ctx, q, lse, [new], [200], w)
     check_weights(c, q, lse, [new], [200], w, before, scale=scale or None)
     assert bool(w[:, :, :200 + new].isfinite().all())
+
+
+@pytest.mark.parametrize("kinds", [E.EPIKV_SCORE_WEIGHT, E.EPIKV_SCORE_WEIGHT | E.EPIKV_SCORE_BANDZ | E.EPIKV_SCORE_HSVAR])
+@pytest.mark.parametrize("T,C", [(700, 8), (700, 65536), (30000, 16)])
+def test_chunks_of_positions_by_weight(gpu_lib, kinds, T, C):
+    """Chunk-level selection ranks by the weights' column, whichever columns stand before it."""
+    cfg = E.make_config(max_seqs=2, max_cache_tokens=T, max_new_tokens=T, hidden=64, n_band_a=1, n_band_b=1, score_kinds=kinds,
+                        select_chunk=C)
+    ws = torch.empty(E.epikv_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+    ctx = E.epikv_init(cfg, ws, ws.numel())
+    for s in range(2):
+        E.epikv_seq_reset(ctx, s, 5 * s, E.EPIKV_SCORE_WEIGHT)
+    g = torch.Generator(device="cuda").manual_seed(24)
+    new = [T, T - 33]
+    hidden = [torch.randn(sum(new), 64, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    seq_ids, cu, _ = R.batch(new, [0, 0])
+    E.epikv_score_update(ctx, 2, seq_ids, cu, T, E.hidden_view(hidden, 64), None)
+    w = torch.rand(2, 1, T, generator=g, device="cuda").pow(8)
+    w[0, 0, 55] = float("nan")
+    E.epikv_weigh(ctx, 2, seq_ids, E.weights_view(w))
+    before = [E.epikv_read_slots(ctx, s, E.EPIKV_SCORE_WEIGHT, T) for s in range(2)]
+    budgets = [T // 2, T // 5]
+    kept = torch.full((2, T), -1, dtype=torch.int32, device="cuda")
+    n_kept = torch.zeros(2, dtype=torch.int32, device="cuda")
+    E.epikv_select(ctx, 2, seq_ids, torch.tensor(budgets, dtype=torch.int32, device="cuda"), None, kept, T, n_kept)
+    for s in range(2):
+        pos, score, n = before[s]
+        assert n == new[s]
+        np.testing.assert_array_equal(np.asarray(score, np.float32), w[s, 0, :n].cpu().numpy())
+        want = oracle_kept(np.asarray(score), np.asarray(pos), budgets[s], 5 * s, 128, C)
+        assert kept[s, :int(n_kept[s])].tolist() == list(want)
+        after = E.epikv_read_slots(ctx, s, E.EPIKV_SCORE_WEIGHT, T)
+        np.testing.assert_array_equal(np.asarray(after[1], np.float32), w[s, 0].cpu().numpy()[want])
+    assert E.epikv_get_error(ctx) == OK
+
+
+def test_more_work_than_is_counted(gpu_lib):
+    """The entry that takes the sum to the limit and those behind it are reported and store nothing; those before it are done."""
+    T, most = 1 << 24, 1 << 20
+    c = R.Cache(seqs=3, T=64, H=1, d=64, seed=25)
+    cfg = E.make_attn_config(max_seqs=3, max_cache_tokens=T, max_new_tokens=most, num_layers=1, num_heads=64, num_kv_heads=1,
+                             head_dim=64)
+    ws = torch.empty(E.epikv_attn_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+    ctx = E.epikv_attn_init(cfg, ws, ws.numel())
+    new, held = [3, most, 2], [50, T - most, 40]
+    q = queries(3, 64, 64)
+    seq_ids, cu, ln = R.batch(new, held)
+    lse = lse64(c, q, [3], [50])
+    w = torch.full((3, 1, 64), -7.5, device="cuda")
+    before = w.clone()
+    E.epikv_attention_weights(ctx, 0, 3, seq_ids, cu, most, ln, E.rows(q), lse, E.epikv_weights(w.data_ptr(), T, T), c.c.view())
+    assert E.epikv_attn_get_error(ctx) == (E.EPIKV_EDEVICE, E.EPIKV_DEV_CAPACITY)
+    check_weights(c, q, lse, [3], [50], w, before)
+    o, l = torch.full_like(q, float("nan")), torch.full((3, 64), float("nan"), device="cuda")
+    E.epikv_attention_chunk(ctx, 0, 3, seq_ids, cu, most, ln, E.rows(q), E.rows(o), c.c.view(), lse=l)
+    assert E.epikv_attn_get_error(ctx) == (E.EPIKV_EDEVICE, E.EPIKV_DEV_CAPACITY)
+    check_attention(c, q, o, l, [3], [50])
+    assert bool(o[3:].isnan().all()) and bool(l[3:].isnan().all())
