@@ -433,7 +433,8 @@ typedef struct epikv_attn_ctx epikv_attn_ctx;
 epikv_status epikv_cache_row(int32_t num_kv_heads, int32_t head_dim, int32_t cache_format, int32_t* heads,
                              int32_t* dim);
 
-/* Bytes of device workspace for cfg (0 if cfg is invalid). */
+/* Bytes of device workspace for cfg (0 if cfg is invalid): room for the partial results of rows that are split between SMs.  32
+ * query and 8 KV heads of 128: 10 MB for one new token a sequence, 20 for 8, 40 from 64 on (epikv_attention_chunk's). */
 size_t epikv_attn_workspace_bytes(const epikv_attn_config* cfg);
 
 /* Create a context over a caller-allocated workspace (256-byte aligned). */
@@ -504,15 +505,20 @@ epikv_status epikv_attention(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, 
 /* The same attention for many query rows: chunks of prompts, drafts, turns, of one token or more a sequence.
  * Arguments, order of the slots, what a row sees, empty rows and d_lse as in epikv_attention; nothing is split
  * between calls, so a prompt may be taken in by pieces.  out may not overlap q.  It reads the cache once for 256 rows (tokens times
- * num_heads / num_kv_heads; 128 at head_dim 256) where epikv_attention does so for 8 to 32.
- * A probability is held in 8 significant bits over a bf16 cache, in 11 (down to 2^-31 of about the row's largest)
- * over a 4-bit one; sums, maxima and d_lse in 32 bits.  In a channel where a slot that a row sees holds an infinity or
- * a NaN the row's output is infinite or NaN.  Slots that a row does not see do not reach it, whatever they hold (memory
+ * num_heads / num_kv_heads; 128 at head_dim 256) where epikv_attention does so for 8 to 32.  It is the faster one from 16 to 64
+ * such rows of an entry on; a single token of many sequences is slower here (64 sequences over a bf16 cache 156 us and 132, over
+ * a 4-bit one 213 and 61).
+ * A probability is held in 8 significant bits over a bf16 cache, where epikv_attention holds 16: the outputs' error against
+ * 64 bits is 0.0023 of their size, there 0.0017, which their own rounding gives.  Over a 4-bit cache it is held as in
+ * epikv_attention: in 11 bits down to 2^-21 of about the row's largest and to within 2^-32 of it below.  Sums, maxima and d_lse
+ * are held in 32 bits.  In a channel where a slot that a row sees holds an infinity or a NaN the row's output is infinite or NaN
+ * (in epikv_attention it is the infinity).  Slots that a row does not see do not reach it, whatever they hold (memory
  * of the view behind them may be read, up to the end of the block, or of the max_cache_tokens slots of a contiguous
  * sequence; where stride_seq / stride_token is between 1 and max_cache_tokens - 1, only slots that are seen).
  * Where an item of rows is cut between the SMs depends on the whole batch, and with it how a row's parts are rounded: the
  * same batch gives the same bits, an entry of another batch may differ in its last ones.  The work is counted in 32 bits,
- * in tiles of 128 slots (64 at head_dim 256) of an item; entries behind 2^31 - 1 are skipped (EPIKV_DEV_CAPACITY). */
+ * in tiles of 128 slots (64 at head_dim 256) of an item and four more for each item; the entry that takes the sum to 2^31 - 1
+ * and those behind it are skipped (EPIKV_DEV_CAPACITY). */
 epikv_status epikv_attention_chunk(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* d_seq_ids,
                                    const int32_t* d_cu_new, int32_t max_new, const int32_t* d_len, int32_t len_stride,
                                    int32_t causal, const epikv_rows* q, const epikv_rows* out, float* d_lse,
@@ -528,8 +534,9 @@ typedef struct {
 
 /* What each slot of one layer's cache receives of the attention of the batch's queries: for KV head h,
  *   sum over the entry's new tokens and the query heads that read h of exp(scale q.k - lse)
- * over the queries that see the slot.  Sums in 32 bits, in the order of the queries, cut where the batch's sizes say:
- * the same batch gives the same bits.
+ * over the queries that see the slot.  Sums in 32 bits and in an order that the batch's sizes give: eight partial sums, each of
+ * every eighth row (a token's query heads, then the next token's), added up where the batch's work is cut.  The same batch
+ * gives the same bits.
  *   d_seq_ids .. causal, q, kv   as in the attention call that gave d_lse
  *   last      only the last so many of each entry's new tokens count; 0: all of them
  *   d_lse     float [total_new][num_heads]: the attention's, or its joined parts'
@@ -537,7 +544,9 @@ typedef struct {
  *   w         written for the entries' sequences and all KV heads, slots 0 .. d_len + n - 1 (causal = 0: 0 ..
  *             d_len - 1), nothing else.  An entry without new tokens stores zeros
  * A query whose lse is minus infinity saw nothing and gives nothing; a NaN in what a slot receives is NaN there.
- * A slot outside the view receives nothing (EPIKV_DEV_SLOT). */
+ * A slot outside the view receives nothing (EPIKV_DEV_SLOT).  The work is counted as in epikv_attention_chunk: for each KV head
+ * and 256 slots (128 at head_dim 256) the steps of 128 rows that see some of them and four more, or one where no entry has more
+ * than 16 rows that count. */
 epikv_status epikv_attention_weights(epikv_attn_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* d_seq_ids,
                                      const int32_t* d_cu_new, int32_t max_new, const int32_t* d_len, int32_t len_stride,
                                      int32_t causal, int32_t last, const epikv_rows* q, const float* d_lse, int32_t add,

@@ -4,19 +4,19 @@
 //
 // The products run on tcgen05 with the slots as the instruction's 128 rows and
 // the query rows as its columns, so that a thread owns a slot and adds up its
-// columns: no exchange between threads, and each slot's sum is formed in the
-// order of the rows.  A unit is a run of 256 slots (128 at 256 channels) of one
-// entry and KV head: its keys stay in shared memory while tiles of query rows
-// (steps) pass by.  Two forms: steps of 16 rows where a call has no more (a
-// decode step: reading the keys bounds it), and of 128 (a chunk: exponentials
-// and products).  One CTA an SM takes an equal share of all units' steps
-// (chunk_plan.h); the few units that two shares meet in are joined by a second
-// kernel, part by part.
+// columns: no exchange between threads, and each slot's sum is formed in a fixed
+// order (eight partial sums, each of every eighth column).  A unit is a run of
+// 256 slots (128 at 256 channels) of one entry and KV head: its keys stay in
+// shared memory while tiles of query rows (steps) pass by.  Two forms: steps of
+// 16 rows where a call has no more (a decode step: reading the keys bounds it),
+// and of 128 (a chunk: exponentials and products).  One CTA an SM takes an equal
+// share of all units' steps (chunk_plan.h); the few units that two shares meet in
+// are joined by a second kernel, part by part.
 //
 // 32 query and 8 KV heads of 128: a decode step of 64 bf16 caches of 2,048 to
 // 8,192 slots 112 us (6.1 TB/s, 90 % of the measured rate); of 32 4-bit caches of
 // 8,192 72 us (2.2 TB/s; 6,000 warp instructions a unit at 2.3 a cycle, two
-// thirds of them the expansion to halves); a prompt of 4,096 79 us (57 steps an
+// thirds of them the expansion to halves); a prompt of 4,096 81 us (57 steps an
 // SM of 2,200 cycles, of which products and exponentials take 1,030 each: the two
 // warps of a scheduler that own slots load, raise and add up at the same time).
 #include <algorithm>
