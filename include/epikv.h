@@ -357,7 +357,7 @@ epikv_status epikv_lagkv_score_noalloc(const epikv_kv_view* kv, int32_t seq, int
  *          epikv_cache_row's size.
  * Strides of a view count 2-byte units for both, so a 4-bit cache is described
  * by the same epikv_kv_view, and epikv_select, epikv_compact and epikv_step
- * (with the band kinds, which do not read K and V) move its rows as they are:
+ * (with the band kinds or WEIGHT, which do not read K and V) move its rows as they are:
  * their context is configured with the num_kv_heads and head_dim that
  * epikv_cache_row returns. */
 enum { EPIKV_CACHE_BF16 = 0, EPIKV_CACHE_E2M1 = 1 };
