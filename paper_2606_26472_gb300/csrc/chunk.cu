@@ -18,13 +18,15 @@
 // 0.0023 of the output's size instead of 0.0017, which the output's own
 // rounding gives), halves beside 4-bit ones.
 //
-// 32 query and 8 KV heads of 128.  Long chunks are bound by products and
-// exponentials: 2,048 tokens behind 14,336 344 us (1.5 PFLOP/s, 77 % of the
-// measured rate), a prompt of 4,096 127 us (1.08, 56 %: items of 1 to 33 tiles,
-// each with its queries, results and half-empty last tiles).  Few tokens by
-// the cache's bytes and the chain of launch, lookups, first tiles and join:
-// 8 x 16 tokens behind 4,096 43 us (3.2 TB/s).  4-bit rows by the copying warps'
-// instructions: 8 x 256 behind 2,048 to 4,096 131 us, over bf16 111.
+// 32 query and 8 KV heads of 128.  Long chunks wait from warp to warp (the
+// tensor pipe is busy 67 % of the cycles, the exponential unit 34): 2,048 tokens
+// behind 14,336 369 us in a long run of them, 341 in a short one, at higher
+// clocks (1.4 and 1.5 PFLOP/s, 72 and 78 % of the measured rate), a prompt of
+// 4,096 128 us (1.08, 56 %: items of 1 to 32 tiles, each with its queries,
+// results and half-empty last tiles).  Few tokens are bound by the cache's bytes
+// and the chain of launch, lookups, first tiles and join: 8 x 16 tokens behind
+// 4,096 43 us (3.2 TB/s).  4-bit rows by the copying warps' instructions: 8 x 256
+// behind 2,048 to 4,096 133 us, over bf16 109.
 #include "chunk_plan.h"
 #include "tensor.cuh"
 

@@ -15,8 +15,9 @@
 //
 // 32 query and 8 KV heads of 128: a decode step of 64 bf16 caches of 2,048 to
 // 8,192 slots 112 us (6.1 TB/s, 90 % of the measured rate); of 32 4-bit caches of
-// 8,192 72 us (2.2 TB/s; 6,000 warp instructions a unit at 2.3 a cycle, two
-// thirds of them the expansion to halves); a prompt of 4,096 81 us (57 steps an
+// 8,192 72 us (2.2 TB/s; 6,000 warp instructions a unit at 2.3 a cycle, some
+// 1,700 of them the expansion to halves, the others walks, addresses and copies);
+// a prompt of 4,096 81 us (57 steps an
 // SM of 2,200 cycles, of which products and exponentials take 1,030 each: the two
 // warps of a scheduler that own slots load, raise and add up at the same time).
 #include <algorithm>
