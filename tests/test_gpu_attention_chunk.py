@@ -8,7 +8,7 @@ import torch
 from paper_2606_26472_gb300 import epikv as E
 
 from . import cache_ops as R
-from .chunk_ops import attend, check_attention, queries
+from .chunk_ops import attend, check_attention, check_weights, queries
 
 pytestmark = pytest.mark.gpu
 
@@ -441,4 +441,55 @@ def test_many_query_heads(gpu_lib, H, Hq):
     q = queries(7, Hq, 64)
     o, l = attend(c, ctx, q, [5, 2], [250, 3])
     check_attention(c, q, o, l, [5, 2], [250, 3])
+    assert E.epikv_attn_get_error(ctx) == OK
+
+
+@pytest.mark.parametrize("layout", ["layer tables", "contiguous", "contiguous, closer than long"])
+@pytest.mark.parametrize("H,Hq,d,new,held", [(2, 8, 64, [50, 1, 0], [200, 131, 77]), (1, 2, 128, [140, 3, 9], [0, 160, 255]),
+                                             (2, 2, 256, [1, 1, 1], [16, 299, 100])])
+def test_rows_within_wider_rows(gpu_lib, layout, H, Hq, d, new, held):
+    """K and V of a token side by side in one pool, by blocks of each layer's own table, or contiguous with a gap behind each
+    sequence or with its end within the next one: the chunk's attention, and the weights that its log-sums give."""
+    S, T, L, bs = 3, 304, 2, 16
+    g = torch.Generator(device="cuda").manual_seed(29)
+    row = 2 * H * d + 64                                       # and 64 values more
+    at = torch.empty(L, S, T, dtype=torch.long, device="cuda")  # of a slot's row
+    if layout == "layer tables":
+        mb = T // bs
+        table = torch.randperm(L * S * mb, generator=g, device="cuda").int().view(L, S, mb)
+        at[:] = (table.long()[..., None] * bs + torch.arange(bs, device="cuda")).view(L, S, T)
+        rows = L * S * mb * bs
+        kw = dict(layout=E.EPIKV_LAYOUT_PAGED, block_table=table, max_blocks_per_seq=mb, block_size=bs, num_blocks=L * S * mb,
+                  stride_layer=0, stride_block=bs * row, stride_table_layer=S * mb)
+    else:
+        apart = T + 5 if layout == "contiguous" else T - 4      # (no sequence here holds its last 4 slots)
+        at[:] = (torch.arange(L, device="cuda")[:, None, None] * (S * apart + 7) + torch.arange(S, device="cuda")[:, None] * apart
+                 + torch.arange(T, device="cuda"))
+        rows = int(at.max()) + 1
+        kw = dict(layout=E.EPIKV_LAYOUT_CONTIGUOUS, stride_layer=(S * apart + 7) * row, stride_seq=apart * row)
+    pool = torch.randn(rows, row, generator=g, device="cuda").to(torch.bfloat16)
+    kv = E.kv_view(pool, pool[:, H * d:], stride_token=row, **kw)
+    cfg = E.make_attn_config(max_seqs=S, max_cache_tokens=T, max_new_tokens=200, num_layers=L, num_heads=Hq, num_kv_heads=H,
+                             head_dim=d)
+    ws = torch.empty(E.epikv_attn_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+    ctx = E.epikv_attn_init(cfg, ws, ws.numel())
+
+    class Rows:
+        def __init__(self):
+            self.d, self.H, self.bits = d, H, 16
+
+        def read(self, w, layer, s, n):
+            return pool[at[layer, s, :n]][:, w * H * d:(w + 1) * H * d].view(n, H, d).double()
+    q = queries(sum(new), Hq, d)
+    seq_ids, cu, ln = R.batch(new, held)
+    for layer in range(L):
+        o, l = torch.empty_like(q), torch.empty(sum(new), Hq, device="cuda")
+        E.epikv_attention_chunk(ctx, layer, S, seq_ids, cu, 200, ln, E.rows(q), E.rows(o), kv, lse=l)
+        check_attention(Rows(), q, o, l, new, held, layer=layer, what=f"layer {layer}")
+        w = torch.full((S, H, T), -7.5, device="cuda")
+        before = w.clone()
+        E.epikv_attention_weights(ctx, layer, S, seq_ids, cu, 200, ln, E.rows(q), l, E.weights_view(w), kv)
+        check_weights(Rows(), q, l, new, held, w, before, layer=layer, what=f"layer {layer}")
+        E.epikv_attention_weights(ctx, layer, S, seq_ids, cu, 200, ln, E.rows(q), l, E.weights_view(w), kv, last=1)
+        check_weights(Rows(), q, l, new, held, w, w.clone(), layer=layer, last=1, what=f"layer {layer}, one token")
     assert E.epikv_attn_get_error(ctx) == OK
